@@ -232,7 +232,7 @@ def _loss_own(s):
         v.xent_fwd(s["h"], s["words"], s["loss_sum"], s["n_tok"], s["tok_loss"], s["argmax"])
         got["argmax"] = s["argmax"]
     if case["back"]:
-        (v.distill_bwd if soft else v.xent_bwd)(s["h"], s["words"], s["dh"], s["dW"], s["db"])
+        (v.distill_bwd if soft else v.xent_bwd)(s["dh"], s["dW"], s["db"])
         got.update(dh=s["dh"], dW=s["dW"], db=s["db"])
     return got
 
