@@ -1,4 +1,4 @@
-"""ctypes binding of include/attn_softmax.h: same names, argument marshalling only.
+"""ctypes binding of include/attn_softmax.h, lstm_stack.h and vocab_ops.h: same names, argument marshalling only.
 
 PyTorch is used for device memory and streams; every step of the path runs in
 the HIP library.  There is no fallback: if libattn_softmax.so is missing the
@@ -30,6 +30,9 @@ EXPORTS = ["attn_softmax_workspace_bytes", "attn_softmax_fwd", "attn_softmax_fwd
            "attn_softmax_adam_step", "attn_softmax_step_workspace_bytes", "attn_softmax_step_prepare",
            "attn_softmax_step_fwd", "lstm_stack_workspace_bytes", "lstm_stack_fwd", "lstm_stack_bwd"]
 
+VOCAB_EXPORTS = ["vocab_embed_workspace_bytes", "vocab_embed_fwd", "vocab_embed_bwd", "vocab_xent_workspace_bytes",
+                 "vocab_xent_fwd", "vocab_xent_bwd", "vocab_distill_fwd", "vocab_distill_bwd"]
+
 
 class AttnSoftmaxError(RuntimeError):
     def __init__(self, code: int, msg: str):
@@ -54,6 +57,20 @@ class LsShape(ctypes.Structure):
 class AsAdam(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_float), ("beta1", ctypes.c_float), ("beta2", ctypes.c_float),
                 ("eps", ctypes.c_float), ("step", ctypes.c_int32)]
+
+
+class VoEmbed(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int32), ("I", ctypes.c_int32), ("V", ctypes.c_int32), ("pad_id", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class VoShape(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int32), ("H", ctypes.c_int32), ("V", ctypes.c_int32), ("pad_id", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32), ("grad_scale", ctypes.c_float)]
+
+
+class VoTeacher(ctypes.Structure):
+    _fields_ = [("K", ctypes.c_int32), ("temperature", ctypes.c_float), ("scale", ctypes.c_float)]
 
 
 def library_path() -> str:
@@ -105,6 +122,23 @@ def load_library():
     lib.lstm_stack_fwd.argtypes = [ctypes.POINTER(LsShape)] + [vp] * 10 + [vp, sz, vp]
     lib.lstm_stack_bwd.restype = ctypes.c_int
     lib.lstm_stack_bwd.argtypes = [ctypes.POINTER(LsShape)] + [vp] * 7 + [vp, sz] + [vp] * 6 + [vp]
+    pe, ps, pt = ctypes.POINTER(VoEmbed), ctypes.POINTER(VoShape), ctypes.POINTER(VoTeacher)
+    lib.vocab_embed_workspace_bytes.restype = sz
+    lib.vocab_embed_workspace_bytes.argtypes = [pe]
+    lib.vocab_embed_fwd.restype = ctypes.c_int
+    lib.vocab_embed_fwd.argtypes = [pe] + [vp] * 4
+    lib.vocab_embed_bwd.restype = ctypes.c_int
+    lib.vocab_embed_bwd.argtypes = [pe] + [vp] * 3 + [ctypes.c_int, vp, sz, vp]
+    lib.vocab_xent_workspace_bytes.restype = sz
+    lib.vocab_xent_workspace_bytes.argtypes = [ps, pt]
+    lib.vocab_xent_fwd.restype = ctypes.c_int
+    lib.vocab_xent_fwd.argtypes = [ps] + [vp] * 9 + [sz, vp]
+    lib.vocab_xent_bwd.restype = ctypes.c_int
+    lib.vocab_xent_bwd.argtypes = [ps] + [vp] * 3 + [sz] + [vp] * 4
+    lib.vocab_distill_fwd.restype = ctypes.c_int
+    lib.vocab_distill_fwd.argtypes = [ps, pt] + [vp] * 12 + [sz, vp]
+    lib.vocab_distill_bwd.restype = ctypes.c_int
+    lib.vocab_distill_bwd.argtypes = [ps, pt] + [vp] * 3 + [sz] + [vp] * 4
     _lib = lib
     return lib
 
@@ -239,6 +273,70 @@ def lstm_stack_bwd(shape, x, lengths, W_ih, W_hh, dy, dhT, dcT, workspace, works
                                        *[a[0] if a else None for a in ins], _ptr(dy), _ptr(dhT), _ptr(dcT),
                                        _ptr(workspace), int(workspace_bytes), _ptr(dx),
                                        *[a[0] if a else None for a in outs], _ptr(dh0), _ptr(dc0), stream or None)
+    if check:
+        _check(rc)
+    return rc
+
+
+def _ref(struct):
+    return ctypes.byref(struct) if struct is not None else None
+
+
+def vocab_embed_workspace_bytes(shape: VoEmbed) -> int:
+    return int(load_library().vocab_embed_workspace_bytes(_ref(shape)))
+
+
+def vocab_embed_fwd(shape, table, ids, x, stream=0, check=True) -> int:
+    rc = load_library().vocab_embed_fwd(_ref(shape), _ptr(table), _ptr(ids), _ptr(x), stream or None)
+    if check:
+        _check(rc)
+    return rc
+
+
+def vocab_embed_bwd(shape, ids, dy, d_table, accumulate, workspace, workspace_bytes, stream=0, check=True) -> int:
+    rc = load_library().vocab_embed_bwd(_ref(shape), _ptr(ids), _ptr(dy), _ptr(d_table), int(accumulate),
+                                        _ptr(workspace), int(workspace_bytes), stream or None)
+    if check:
+        _check(rc)
+    return rc
+
+
+def vocab_xent_workspace_bytes(shape: VoShape, teacher=None) -> int:
+    return int(load_library().vocab_xent_workspace_bytes(_ref(shape), _ref(teacher)))
+
+
+def vocab_xent_fwd(shape, h, W, b, targets, loss_sum, n_tok, tok_loss, argmax, workspace, workspace_bytes, stream=0,
+                   check=True) -> int:
+    rc = load_library().vocab_xent_fwd(_ref(shape), _ptr(h), _ptr(W), _ptr(b), _ptr(targets), _ptr(loss_sum),
+                                       _ptr(n_tok), _ptr(tok_loss), _ptr(argmax), _ptr(workspace),
+                                       int(workspace_bytes), stream or None)
+    if check:
+        _check(rc)
+    return rc
+
+
+def vocab_xent_bwd(shape, W, b, workspace, workspace_bytes, dh, dW, db, stream=0, check=True) -> int:
+    rc = load_library().vocab_xent_bwd(_ref(shape), _ptr(W), _ptr(b), _ptr(workspace), int(workspace_bytes), _ptr(dh),
+                                       _ptr(dW), _ptr(db), stream or None)
+    if check:
+        _check(rc)
+    return rc
+
+
+def vocab_distill_fwd(shape, teacher, h, W, b, targets, teacher_ids, teacher_logits, loss_sum, n_tok, distill_sum,
+                      tok_loss, tok_distill, workspace, workspace_bytes, stream=0, check=True) -> int:
+    rc = load_library().vocab_distill_fwd(_ref(shape), _ref(teacher), _ptr(h), _ptr(W), _ptr(b), _ptr(targets),
+                                          _ptr(teacher_ids), _ptr(teacher_logits), _ptr(loss_sum), _ptr(n_tok),
+                                          _ptr(distill_sum), _ptr(tok_loss), _ptr(tok_distill), _ptr(workspace),
+                                          int(workspace_bytes), stream or None)
+    if check:
+        _check(rc)
+    return rc
+
+
+def vocab_distill_bwd(shape, teacher, W, b, workspace, workspace_bytes, dh, dW, db, stream=0, check=True) -> int:
+    rc = load_library().vocab_distill_bwd(_ref(shape), _ref(teacher), _ptr(W), _ptr(b), _ptr(workspace),
+                                          int(workspace_bytes), _ptr(dh), _ptr(dW), _ptr(db), stream or None)
     if check:
         _check(rc)
     return rc
@@ -412,3 +510,157 @@ class DeviceLstm:
 
     def sync(self):
         self.torch.cuda.synchronize(self.dev)
+
+
+def _as_dtype(t) -> int:
+    import torch
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise AttnSoftmaxError(3, f"storage type {t.dtype}")
+    return AS_BF16 if t.dtype == torch.bfloat16 else AS_F32
+
+
+def _grad_dtype(grad_dtype, dtype: int) -> int:
+    return dtype if grad_dtype is None else AS_BF16 if grad_dtype == "bf16" else AS_F32
+
+
+class _DeviceOp:
+    """Checks of the tensors that a call is given (shape, type, device, dense rows) and the stream it goes to: the
+    current one of the tensors' device, with that device current for the call."""
+
+    def _tensor(self, t, shape, dtype, name, optional=False):
+        if t is None:
+            if not optional:
+                raise AttnSoftmaxError(1, f"{name} is None")
+            return None
+        if tuple(t.shape) != tuple(shape):
+            raise AttnSoftmaxError(2, f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+        if t.dtype != dtype:
+            raise AttnSoftmaxError(3, f"{name} is {t.dtype}, expected {dtype}")
+        if t.device != self.dev:
+            raise AttnSoftmaxError(2, f"{name} is on {t.device}, expected {self.dev}")
+        if not t.is_contiguous():
+            raise AttnSoftmaxError(5, f"{name} is not dense row-major")
+        return t
+
+    def _stream(self) -> int:
+        return int(self.torch.cuda.current_stream(self.dev).cuda_stream)
+
+
+class DeviceEmbed(_DeviceOp):
+    """Embedding of up to N positions at a time in a table [V,I] (a device tensor, not copied): owns the workspace of the
+    backward pass and forwards to the C ABI.  grad_dtype: "f32" or "bf16", the type of dy and of the table's gradient."""
+
+    def __init__(self, table, N, pad_id=-1, scale=1.0, grad_dtype=None):
+        import torch
+        self.torch, self.table, self.dev = torch, table, table.device
+        dtype = _as_dtype(table)
+        V, I = table.shape
+        self._tensor(table, (V, I), table.dtype, "table")
+        self.shape = VoEmbed(N, I, V, pad_id, dtype, _grad_dtype(grad_dtype, dtype), float(scale))
+        self.gdt = torch.bfloat16 if self.shape.grad_dtype == AS_BF16 else torch.float32
+        self.ws_bytes = vocab_embed_workspace_bytes(self.shape)
+        if self.ws_bytes == 0:
+            raise AttnSoftmaxError(2, "invalid shape for the embedding")
+        self.workspace = None
+
+    def fwd(self, ids, x=None):
+        """x [N,I] = scale * table[ids]; ids [N] int32."""
+        torch, s = self.torch, self.shape
+        self._tensor(ids, (s.N,), torch.int32, "ids")
+        if x is None:
+            x = torch.empty(s.N, s.I, dtype=self.table.dtype, device=self.dev)
+        self._tensor(x, (s.N, s.I), self.table.dtype, "x")
+        with torch.cuda.device(self.dev):
+            vocab_embed_fwd(s, self.table, ids, x, self._stream())
+        return x
+
+    def bwd(self, ids, dy, d_table=None, accumulate=False):
+        """d_table [V,I] = (d_table +) scale * sums of the rows of dy [N,I] per word."""
+        torch, s = self.torch, self.shape
+        self._tensor(ids, (s.N,), torch.int32, "ids")
+        self._tensor(dy, (s.N, s.I), self.gdt, "dy")
+        if d_table is None:
+            if accumulate:
+                raise AttnSoftmaxError(1, "d_table is None")
+            d_table = torch.empty(s.V, s.I, dtype=self.gdt, device=self.dev)
+        self._tensor(d_table, (s.V, s.I), self.gdt, "d_table")
+        if self.workspace is None:
+            self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.dev)
+        with torch.cuda.device(self.dev):
+            vocab_embed_bwd(s, ids, dy, d_table, accumulate, self.workspace, self.ws_bytes, self._stream())
+        return d_table
+
+
+class DeviceVocabLoss(_DeviceOp):
+    """Cross-entropy (and, with K > 0, distillation from a teacher's top K logits) of N positions over a vocabulary with the
+    projection W [V,H] and bias b [V] or None (device tensors, not copied): owns the workspace, which carries what a
+    backward pass needs of the forward pass ahead of it, and forwards to the C ABI.  grad_dtype: "f32" or "bf16"."""
+
+    def __init__(self, W, b, N, pad_id=-1, grad_scale=1.0, grad_dtype=None, K=0, temperature=1.0, distill_scale=1.0):
+        import torch
+        self.torch, self.W, self.b, self.dev = torch, W, b, W.device
+        dtype = _as_dtype(W)
+        V, H = W.shape
+        self._tensor(W, (V, H), W.dtype, "W")
+        self._tensor(b, (V,), W.dtype, "b", optional=True)
+        self.shape = VoShape(N, H, V, pad_id, dtype, _grad_dtype(grad_dtype, dtype), float(grad_scale))
+        self.gdt = torch.bfloat16 if self.shape.grad_dtype == AS_BF16 else torch.float32
+        self.teacher = VoTeacher(K, float(temperature), float(distill_scale)) if K else None
+        self.ws_bytes = vocab_xent_workspace_bytes(self.shape, self.teacher)
+        if self.ws_bytes == 0:
+            raise AttnSoftmaxError(2, "invalid shape for the vocabulary loss")
+        self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.dev)
+        self.done = None
+
+    def _outputs(self, h, targets, loss_sum, n_tok, rows):
+        torch, s = self.torch, self.shape
+        self._tensor(h, (s.N, s.H), self.W.dtype, "h")
+        self._tensor(targets, (s.N,), torch.int32, "targets")
+        self._tensor(loss_sum, (1,), torch.float32, "loss_sum")
+        self._tensor(n_tok, (1,), torch.int32, "n_tok")
+        for name, t, dt in rows:
+            self._tensor(t, (s.N,), dt, name, optional=True)
+
+    def xent_fwd(self, h, targets, loss_sum, n_tok, tok_loss=None, argmax=None):
+        torch = self.torch
+        if self.teacher is not None:
+            raise AttnSoftmaxError(2, "this workspace is for distillation (K > 0): distill_fwd")
+        self._outputs(h, targets, loss_sum, n_tok, (("tok_loss", tok_loss, torch.float32), ("argmax", argmax, torch.int32)))
+        with torch.cuda.device(self.dev):
+            vocab_xent_fwd(self.shape, h, self.W, self.b, targets, loss_sum, n_tok, tok_loss, argmax, self.workspace,
+                           self.ws_bytes, self._stream())
+        self.done = "xent"
+
+    def distill_fwd(self, h, targets, teacher_ids, teacher_logits, loss_sum, n_tok, distill_sum, tok_loss=None,
+                    tok_distill=None):
+        torch, s = self.torch, self.shape
+        if self.teacher is None:
+            raise AttnSoftmaxError(1, "no teacher (K = 0): xent_fwd")
+        self._outputs(h, targets, loss_sum, n_tok, (("tok_loss", tok_loss, torch.float32),
+                                                    ("tok_distill", tok_distill, torch.float32)))
+        self._tensor(teacher_ids, (s.N, self.teacher.K), torch.int32, "teacher_ids")
+        self._tensor(teacher_logits, (s.N, self.teacher.K), torch.float32, "teacher_logits")
+        self._tensor(distill_sum, (1,), torch.float32, "distill_sum")
+        with torch.cuda.device(self.dev):
+            vocab_distill_fwd(s, self.teacher, h, self.W, self.b, targets, teacher_ids, teacher_logits, loss_sum,
+                              n_tok, distill_sum, tok_loss, tok_distill, self.workspace, self.ws_bytes, self._stream())
+        self.done = "distill"
+
+    def _gradients(self, done, dh, dW, db):
+        s = self.shape
+        if self.done != done:
+            raise AttnSoftmaxError(2, "a backward pass without the forward pass ahead of it")
+        self._tensor(dh, (s.N, s.H), self.gdt, "dh")
+        self._tensor(dW, (s.V, s.H), self.gdt, "dW")
+        self._tensor(db, (s.V,), self.gdt, "db", optional=True)
+
+    def xent_bwd(self, dh, dW, db=None):
+        self._gradients("xent", dh, dW, db)
+        with self.torch.cuda.device(self.dev):
+            vocab_xent_bwd(self.shape, self.W, self.b, self.workspace, self.ws_bytes, dh, dW, db, self._stream())
+
+    def distill_bwd(self, dh, dW, db=None):
+        self._gradients("distill", dh, dW, db)
+        with self.torch.cuda.device(self.dev):
+            vocab_distill_bwd(self.shape, self.teacher, self.W, self.b, self.workspace, self.ws_bytes, dh, dW, db,
+                              self._stream())

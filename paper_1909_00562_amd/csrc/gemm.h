@@ -72,9 +72,9 @@ struct GemmArgs {
   // Sizes known only on the device (a row count made by an earlier kernel of the same stream).  M and K[0]
   // stay the upper bounds every grid, plan and buffer is sized for; a kernel reads the count once and
   // uses min(count, bound) in their place: rows >= *M_dev of A are not read and of C not written, reduction
-  // indices >= *K_dev of segment 0 are not read (so neither operand has to be defined there).
+  // indices >= *K_dev of a segment are not read (so neither operand has to be defined there).
   const int32_t* M_dev = nullptr;   // batch == 1 only
-  const int32_t* K_dev = nullptr;   // single segment only
+  const int32_t* K_dev = nullptr;   // (bf16; fp32: single segment only)
   // With M_dev, the 256x256 persistent kernel and a product of few, long work items (fewer output tiles than a
   // few rounds of the grid): `splits` (>= 2) is then only the bound `partial` is sized for; the kernel picks the
   // split of the reduction from the row count it reads (pp_dyn_splits below), so that the shrunken work list

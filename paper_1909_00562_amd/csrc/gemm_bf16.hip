@@ -28,6 +28,7 @@
 #include "gemm.h"
 #include "gemm_dev.h"
 #include "lds_limit.h"
+#include "vocab.h"
 
 #include <type_traits>
 
@@ -540,7 +541,7 @@ __global__ __launch_bounds__(512) void gemm_bf16_pp_kernel(GemmDev p, int work_t
     }
     return it;
   };
-  const int nk_rest = (p.nseg - 1) * ((p.K + BK - 1) / BK);   // reduction tiles of all segments but the first
+  const int nk_rest = (p.nseg - 1) * (K0 > 0 ? (K0 + BK - 1) / BK : 1);   // reduction tiles of all segments but the first
 
   acc_t acc[TM][TN];
   auto zero_acc = [&]() {
@@ -583,7 +584,7 @@ __global__ __launch_bounds__(512) void gemm_bf16_pp_kernel(GemmDev p, int work_t
       if (++cseg < p.nseg) {
         cA = p.A[cseg] + (int64_t)lbatch * p.sA + offA;
         cB = p.B[cseg] + (int64_t)lbatch * p.sB + offB;
-        ck_left = p.K;
+        ck_left = K0;
       } else {
         lw += nbx;
         lvalid = lw < wend;
@@ -795,7 +796,7 @@ __global__ __launch_bounds__(512) void gemm_bf16_ring_kernel(
     }
     return it;
   };
-  const int nk_rest = (p.nseg - 1) * ((p.K + RK - 1) / RK);   // reduction tiles of all segments but the first
+  const int nk_rest = (p.nseg - 1) * (K0 > 0 ? (K0 + RK - 1) / RK : 1);   // reduction tiles of all segments but the first
 
   f32x16_t acc[TM][TN];
   auto zero_acc = [&]() {
@@ -838,7 +839,7 @@ __global__ __launch_bounds__(512) void gemm_bf16_ring_kernel(
       if (++cseg < p.nseg) {
         cA = p.A[cseg] + (int64_t)lbatch * p.sA + offA;
         cB = p.B[cseg] + (int64_t)lbatch * p.sB + offB;
-        ck_left = p.K;
+        ck_left = K0;
       } else {
         lw += nbx;
         lvalid = lw < wend;
@@ -1049,7 +1050,6 @@ static hipError_t gemm_describe(const GemmArgs& g, GemmTile tile, GemmDev& d) {
   d.splits = g.splits;
   d.partial = g.partial;
   if (g.M_dev && g.batch != 1) return hipErrorInvalidValue;
-  if (g.K_dev && g.K[1] != 0) return hipErrorInvalidValue;
   d.M_dev = g.M_dev;
   d.K_dev = g.K_dev;
   d.nz = g.batch * g.splits;
@@ -1079,6 +1079,16 @@ static hipError_t gemm_describe(const GemmArgs& g, GemmTile tile, GemmDev& d) {
   if (g.splits > 1 && !g.dyn_split && (int64_t)(d.kper / BK) * (g.splits - 1) >= ktiles)
     return hipErrorInvalidValue;   // an empty split
   return hipSuccess;
+}
+
+int vocab_tile_edge(GemmTile tile) { return tile == kTile64 ? 64 : 128; }
+GemmTile vocab_tile(int N, int V, int K) { return gemm_plan(N, V, K, 1, true, false).tile == kTile64 ? kTile64 : kTile128; }
+hipError_t launch_gemm_vocab(const GemmArgs& g, GemmTile tile, const VocabEpi& v, int terms, bool teacher, bool arg, hipStream_t st) {
+  if (!g.a_kc || !g.b_kc || g.splits != 1 || g.batch != 1 || g.K_dev || g.C || g.bias) return hipErrorInvalidValue;
+  GemmDev d;
+  const hipError_t e = gemm_describe(g, tile, d);
+  if (e != hipSuccess) return e;
+  return launch_gemm_bf16_vocab_tile(d, tile, v, terms, teacher, arg, st);
 }
 
 hipError_t launch_gemm_bf16_together(const GemmArgs* g, const GemmTile* tile, int n, const DbReduce* sums, hipStream_t st) {

@@ -38,7 +38,7 @@ struct GemmDev {
   int kper;    // reduction elements per split, multiple of 64
   int vec_ok;  // rows of C (and C_lo, C_dact, gate) allow 8/16-byte vector access
   const int32_t* M_dev;   // device-side row count (or null): min(*M_dev, M) rows are valid
-  const int32_t* K_dev;   // device-side reduction length of segment 0 (or null)
+  const int32_t* K_dev;   // device-side reduction length of each segment (or null)
   int nz;                 // batch * splits
   int dyn_split;          // splits is the bound of a split chosen in the kernel from the row count (pp kernel)
 };
@@ -120,6 +120,9 @@ struct TileForm {
 hipError_t launch_gemm_bf16_tiles_together(const GemmDev* d, const TileForm* f, int n, const DbReduce* sums, hipStream_t st);
 // whether that kernel's fragment reads run between its matrix instructions
 bool gemm_tile_laced(bool a_kc, int64_t blocks);
+// its products whose write-out is the vocabulary's (vocab.h)
+struct VocabEpi;
+hipError_t launch_gemm_bf16_vocab_tile(const GemmDev& d, GemmTile tile, const VocabEpi& e, int terms, bool teacher, bool arg, hipStream_t st);
 // the kernel for few rows: both operands reduction-contiguous, up to three segments of the same length, no split, no batch
 hipError_t launch_gemm_bf16_few(const GemmDev& d, bool out_bf16, hipStream_t st);
 

@@ -25,6 +25,7 @@
 #include "gemm.h"
 #include "gemm_dev.h"
 #include "lds_limit.h"
+#include "vocab_epi_dev.h"
 #include "wave_pipe.h"
 
 #include <type_traits>
@@ -215,8 +216,18 @@ template <int BM> __device__ __forceinline__ TileStat gs_stats(const float* row,
 
 // Block `id` of a launch's tiles of all batches and splits; dynamic LDS: NST * 2 * 32 TW * ROWB bytes.  (p by value: by reference the
 // instances take five registers more and 182 x 51130 x 128 18.7 us for 17.2.)
-template <int TW, bool AKC, bool BKC, int NST, bool LACED, TileExtra EXTRA>
-__device__ __forceinline__ void gemm_bf16_tile_block(GemmDev p, int out_bf16, int id) {
+// VOC: the vocabulary's own write-out in place of C's (VocabOut), with its arguments.
+struct NoVocabOut {
+  static constexpr bool kOn = false;
+  struct Args {};
+};
+template <bool TEACH, bool ARG, int TERMS> struct VocabOut {
+  static constexpr bool kOn = true, kTeach = TEACH, kArg = ARG;
+  static constexpr int kTerms = TERMS;
+  using Args = VocabEpi;
+};
+template <int TW, bool AKC, bool BKC, int NST, bool LACED, TileExtra EXTRA, typename VOC = NoVocabOut>
+__device__ __forceinline__ void gemm_bf16_tile_block(GemmDev p, int out_bf16, int id, typename VOC::Args voc = {}) {
   extern __shared__ __align__(1024) unsigned char smem[];
   constexpr int BM = 32 * TW, TILE = BM * ROWB, STAGE = 2 * TILE;   // square block tile; bytes of an operand tile, a stage
   constexpr int NL = TW, LD = BM + 4;                               // loads per wave, operand and tile; staging row (floats)
@@ -244,13 +255,13 @@ __device__ __forceinline__ void gemm_bf16_tile_block(GemmDev p, int out_bf16, in
   const int nseg = second ? 1 : p.nseg;
 
   // reduction tiles of this block: [t0, t1) of the sequence that runs through the segments one after the other
-  const int ks = (p.K + BK - 1) / BK;
-  int nk = (K0 + BK - 1) / BK + (nseg - 1) * ks, seg = 0, skip = 0;
+  const int ks = (K0 + BK - 1) / BK;
+  int nk = nseg * ks, seg = 0, skip = 0;
   if (p.splits > 1) {
     const int per = p.K_dev ? (nk + p.splits - 1) / p.splits : p.kper / BK;
     skip = split * per;
     nk = nk - skip < per ? nk - skip : per;
-    for (; seg < nseg - 1 && skip >= ks; ++seg) skip -= ks;   // (K0 = K where there are more segments than one)
+    for (; seg < nseg - 1 && skip >= ks; ++seg) skip -= ks;
   }
   typename std::conditional<AKC, DirectLoader<BM, 4>, StridedLoader<BM>>::type la;
   typename std::conditional<BKC, DirectLoader<BM, 4>, StridedLoader<BM>>::type lb;
@@ -266,7 +277,7 @@ __device__ __forceinline__ void gemm_bf16_tile_block(GemmDev p, int out_bf16, in
       if (++seg < nseg) {
         cA = p.A[seg] + (int64_t)batch * p.sA + offA;
         cB = p.B[seg] + (int64_t)batch * p.sB + offB;
-        k_left = p.K;
+        k_left = K0;
       } else {
         seg = nseg - 1;           // all loads below are out of range
       }
@@ -395,6 +406,43 @@ __device__ __forceinline__ void gemm_bf16_tile_block(GemmDev p, int out_bf16, in
   __syncthreads();
   float* stage = reinterpret_cast<float*>(smem);
   const int q = lane >> 4, c = lane & 15;
+  if constexpr (VOC::kOn) {
+    float vbias[TW];
+#pragma unroll
+    for (int j = 0; j < TW; ++j) {
+      const int col = n0 + wn + 16 * j + c;
+      vbias[j] = col < p.N ? vocab_bias(voc, col) : 0.f;
+    }
+    f32x4_t cs = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int half = 0; half < BM / 64; ++half) {   // 64 rows at a time
+      if (wm / 64 == half) {
+#pragma unroll
+        for (int i = 0; i < TW; ++i)
+#pragma unroll
+          for (int j = 0; j < TW; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) stage[(wm % 64 + 16 * i + 4 * q + r) * LD + wn + 16 * j + c] = acc[i][j][r] + vbias[j];
+      }
+      __syncthreads();
+      const int row0 = m0 + half * 64, left = Mv - row0 < 64 ? Mv - row0 : 64;
+      if constexpr (VOC::kTerms == 0) vocab_stats64<BM, VOC::kTeach, VOC::kArg>(voc, stage, LD, row0, left, n0, p.N - n0);
+      else vocab_grad64<BM, VOC::kTeach, VOC::kTerms>(voc, stage, LD, row0, left, n0, p.N - n0, cs);
+      __syncthreads();
+    }
+    if (VOC::kTerms > 0 && voc.col_sums) {         // of the tile's rows, in a fixed order
+      constexpr int VPR = BM / 4, RP = 256 / VPR;
+      *reinterpret_cast<f32x4_t*>(stage + (tid / VPR) * BM + (tid % VPR) * 4) = cs;
+      __syncthreads();
+      if (tid < BM && n0 + tid < p.N) {
+        float sum = stage[tid];
+#pragma unroll
+        for (int r = 1; r < RP; ++r) sum += stage[r * BM + tid];
+        voc.col_sums[(int64_t)(m0 / BM) * voc.ld_sums + n0 + tid] = sum;
+      }
+    }
+    return;
+  }
   constexpr int VPR = BM / 4;                 // groups of four columns per row
   const int col = n0 + (tid % VPR) * 4;
   const bool fuse = p.splits <= 1;
@@ -486,6 +534,33 @@ static hipError_t launch_tile_shape(const GemmDev& d, int out_bf16, hipStream_t 
   const dim3 grid((unsigned)blocks);
   hipLaunchKernelGGL(kfn, grid, dim3(256), smem, st, d, out_bf16);
   return hipGetLastError();
+}
+
+template <int TW, int NST, typename VOC>
+__global__ __launch_bounds__(256, 2) void gemm_bf16_vocab_kernel(GemmDev p, VocabEpi e) {
+  gemm_bf16_tile_block<TW, true, true, NST, true, kNoExtra, VOC>(p, 0, blockIdx.x, e);
+}
+template <int TW, int NST, typename VOC>
+static hipError_t launch_vocab_shape(const GemmDev& d, const VocabEpi& e, hipStream_t st) {
+  constexpr int BM = 32 * TW, smem = NST * 2 * BM * ROWB;
+  auto kfn = gemm_bf16_vocab_kernel<TW, NST, VOC>;
+  static LdsLimit limit;
+  const hipError_t rc = limit.raise(reinterpret_cast<const void*>(kfn), smem);
+  if (rc != hipSuccess) return rc;
+  const int64_t blocks = (int64_t)d.tiles_m * d.tiles_n;
+  if (blocks > (1 << 24)) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(kfn, dim3((unsigned)blocks), dim3(256), smem, st, d, e);
+  return hipGetLastError();
+}
+template <typename VOC> static hipError_t launch_vocab_tile(const GemmDev& d, GemmTile tile, const VocabEpi& e, hipStream_t st) {
+  if (tile == kTile64) return launch_vocab_shape<2, 4, VOC>(d, e, st);
+  return (int64_t)d.tiles_m * d.tiles_n <= 256 ? launch_vocab_shape<4, 4, VOC>(d, e, st) : launch_vocab_shape<4, 2, VOC>(d, e, st);
+}
+hipError_t launch_gemm_bf16_vocab_tile(const GemmDev& d, GemmTile tile, const VocabEpi& e, int terms, bool teacher, bool arg, hipStream_t st) {
+  if (terms == 1) return teacher ? launch_vocab_tile<VocabOut<true, false, 1>>(d, tile, e, st) : launch_vocab_tile<VocabOut<false, false, 1>>(d, tile, e, st);
+  if (terms == 3) return teacher ? launch_vocab_tile<VocabOut<true, false, 3>>(d, tile, e, st) : launch_vocab_tile<VocabOut<false, false, 3>>(d, tile, e, st);
+  if (teacher) return launch_vocab_tile<VocabOut<true, false, 0>>(d, tile, e, st);
+  return arg ? launch_vocab_tile<VocabOut<false, true, 0>>(d, tile, e, st) : launch_vocab_tile<VocabOut<false, false, 0>>(d, tile, e, st);
 }
 
 // Reads first and laced, us, 128 x 128 tiles (64 x 64 where it says so): up to 256 blocks 1024 x 1024 x 6400 TN 62.6 / 53.8, 2257 x

@@ -1,0 +1,119 @@
+// The operators over the vocabulary without logits: what their products' write-out needs, and the launchers of their kernels.
+//
+// Rows are the compacted rows of words (R of them, counted on the device), columns those of a piece of the vocabulary.
+// The products leave no logits: the forward one the softmax statistics of each row's part of a tile, the logit of the
+// row's word and those of its teacher entries; the backward one the derivative dl as one or three bf16 planes and its column sums.
+//
+// Teacher entries are kept in lists: rows in groups of 16, columns in strips of 64, the entries of a group ordered by strip, so
+// that a tile finds those of its rows and columns as one run per group.  An entry is (column << 4 | row of the group) and its
+// probability, that of all entries of the row with this id.
+#pragma once
+#include "gemm.h"
+
+namespace asx {
+
+constexpr int kVocabGroup = 16, kVocabStrip = 64;   // rows and columns of the lists of teacher entries
+constexpr int kTeacherMaxK = 256;
+
+struct VocabEpi {
+  int32_t v0;                 // first column of the product in the vocabulary
+  const int32_t* y;           // [R] word of each row
+  const void* bias;           // of the product's columns, or null
+  int32_t bias_f32;           // float or bf16
+  float inv_tau;
+  // statistics: [tile column][ldr] each
+  float2* stat;               // maximum, sum of exp relative to it
+  float* stat_tau;            // teacher: sum of exp((l - maximum) / tau)
+  int32_t* stat_idx;          // lowest column that attains the maximum (INT_MAX: none), or null
+  int64_t ldr;
+  float* at_word;             // [R]
+  // teacher entries
+  const int32_t* runs;        // [group][strips + 1]: a strip's first entry
+  const uint32_t* ent;
+  const float* ent_p;
+  float* ent_l;               // out (statistics): an entry's logit
+  int32_t strips;             // of the whole vocabulary
+  // gradient
+  const float* lse;           // [R]
+  const float* lse_tau;       // [R], +inf where a row has no entries
+  float g, c2;                // grad_scale; teacher's scale * tau
+  uint16_t* dl;               // planes of [R, ldd]
+  int64_t ldd, plane;
+  float* col_sums;            // [tile row][ld_sums], or null
+  int64_t ld_sums;
+};
+
+// Columns of the statistics' tiles, rows of the column sums' tiles
+int vocab_tile_edge(GemmTile tile);
+GemmTile vocab_tile(int N, int V, int K);
+
+// terms: planes of dl (1 or 3), or 0: statistics; arg: stat_idx is wanted.  g: A, B contiguous, M_dev, no split, no C.
+hipError_t launch_gemm_vocab(const GemmArgs& g, GemmTile tile, const VocabEpi& e, int terms, bool teacher, bool arg, hipStream_t st);
+
+// ---- rows of words -------------------------------------------------------------------
+struct VocabRows {
+  const void* h;              // [N, H]
+  bool f32;
+  const int32_t* targets;
+  int N, H, V, pad_id;
+  int32_t *row_pos, *rows, *y, *n_act;   // y[r]: word of row r
+  uint16_t* hc;               // terms of the rows of words, [plane][N, ldH]
+  int64_t ldH, plane;
+  float *tok_loss, *tok_distill;         // optional: 0 at padding
+  int32_t* argmax;            // optional: pad_id at padding
+  int32_t* ticket;            // cleared
+};
+hipError_t launch_vocab_rows(const VocabRows& p, hipStream_t st);
+// float [rows, H] -> three bf16 planes of [rows, ldH], zeros behind column H
+hipError_t launch_vocab_terms(const float* src, int rows, int H, uint16_t* dst, int64_t ldH, int64_t plane, hipStream_t st);
+
+// ---- teacher -------------------------------------------------------------------------
+struct VocabTeacher {
+  const int32_t* ids;         // [N, K]
+  const float* logits;
+  int N, K, V;
+  float inv_tau;
+  const int32_t *rows, *n_act;
+  int32_t* runs;
+  uint32_t* ent;              // [group][16 K]
+  float* ent_p;
+  int32_t* place;             // [R, K]: entry's index in ent, -1: none
+  float* p_log_p;             // [R]: sum of p log p; NaN-free; seen[r] says whether there are entries
+  int32_t* seen;
+  int32_t strips;
+};
+hipError_t launch_vocab_teacher(const VocabTeacher& p, hipStream_t st);
+
+// ---- joining the statistics ------------------------------------------------------------
+struct VocabFinish {
+  const float2* stat;
+  const float* stat_tau;      // teacher, or null
+  const int32_t* stat_idx;    // or null
+  int64_t ldr;
+  int parts;                  // tile columns of this piece
+  bool first, last;           // of the pieces
+  float4* run;                // [N] maximum, sum, sum at temperature, (bits) index so far: pieces in between
+  const float* at_word;
+  const int32_t *rows, *n_act;
+  int N;
+  float *lse, *lse_tau, *loss_ws, *distill_ws;
+  float *tok_loss, *tok_distill;
+  int32_t* argmax;
+  float *loss_sum, *distill_sum;
+  int32_t *n_tok, *ticket;
+  // teacher
+  int K;
+  float inv_tau, tau2;
+  const int32_t *place, *seen;
+  const float *ent_p, *ent_l, *p_log_p;
+};
+hipError_t launch_vocab_finish(const VocabFinish& p, hipStream_t st);
+
+// ---- gradients on their way out ----------------------------------------------------------
+// db[v] = sum over the tile rows of col_sums, in order
+hipError_t launch_vocab_col_sums(const float* col_sums, int64_t ld, int tile_rows, int edge, const int32_t* n_act, int V, void* db,
+                                 bool bf16, hipStream_t st);
+// dh[n] = src[row_pos[n]], zeros at padding
+hipError_t launch_vocab_scatter(const float* src, const int32_t* row_pos, int N, int H, int64_t ld, void* dh, bool bf16, hipStream_t st);
+
+}  // namespace asx

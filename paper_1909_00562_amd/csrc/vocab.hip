@@ -1,0 +1,485 @@
+// Softmax cross-entropy over a vocabulary and distillation without keeping the logits: argument checks, workspace and the
+// order of the kernels.
+//
+// Forward: the rows of words of h are gathered (a count that stays on the device), one product h W^T whose write-out leaves the
+// softmax statistics of each row's part of a tile instead of the logits, and a pass that joins them.
+// Backward, a piece of the vocabulary at a time: the product again, its write-out now dl = g (exp(l - lse) - onehot) [+ s tau
+// (q - p)] as bf16 and its column sums (db), then dW_piece = dl^T h and dh += dl W_piece while dl is still in the caches.
+// Four products of 2 R V H where three would do with the logits kept: what that buys is R V elements of memory.
+//
+// Float gradients: dl as the sum of three bf16 terms (24 bits of mantissa), each in a plane of its own, whose products with the
+// other operand are reduction segments of one launch.  fp32 storage: h and W as three terms too, the six products of terms whose
+// ranks add up to two at most; what is left out is 2^-24 of a product.  The planes of W are made a piece at a time.
+#include "../../include/vocab_ops.h"
+
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "common.h"
+#include "gemm.h"
+#include "status.h"
+#include "vocab.h"
+
+namespace asx {
+namespace {
+
+constexpr size_t kAlignV = 256;
+size_t upv(size_t x) { return (x + kAlignV - 1) / kAlignV * kAlignV; }
+int64_t round_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
+
+// What a piece of the vocabulary may take: dl of the backward pass, or the statistics or terms of W of the forward one.  It is
+// read back at once, so that most of it is found in the 256 MB memory-side cache.
+constexpr int64_t kPieceBytes = (int64_t)128 << 20;
+constexpr int64_t kPieceColumns = 256;   // pieces are multiples of it
+
+struct VocabLayout {
+  bool f32, g_bf16;
+  int h_terms, dl_terms;
+  int64_t ldH, fwd_cols, bwd_cols, ldd;
+  int strips, groups;
+  GemmTile t_fwd, t_bwd;
+  int e_fwd, e_bwd;                       // edges of their tiles
+  GemmPlan p_dw, p_dh;
+  bool dh_dyn;
+  // kept from the forward to the backward pass
+  size_t rows, row_pos, y, n_act, ticket, hc, lse, lse_tau, at_word, loss_ws, distill_ws, run;
+  size_t runs, ent, ent_p, ent_l, place, p_log_p, seen;
+  // one area for the pieces of either pass
+  size_t stat, stat_tau, stat_idx, w_fwd;
+  size_t dl, w_bwd, col_sums, dh_acc, partial;
+  size_t total;
+};
+
+bool types_ok(const vo_shape* s) {
+  return (s->dtype == AS_F32 && s->grad_dtype == AS_F32) ||
+         (s->dtype == AS_BF16 && (s->grad_dtype == AS_F32 || s->grad_dtype == AS_BF16));
+}
+bool shape_ok(const vo_shape* s) {
+  if (s->N < 1 || s->N > (1 << 24) || s->H < 1 || s->H > (1 << 16) || s->V < 1 || s->V > (1 << 26)) return false;
+  if ((int64_t)s->V * s->H >= (int64_t)1 << 40) return false;
+  return s->pad_id >= -1 && s->pad_id < s->V && std::isfinite(s->grad_scale);
+}
+bool teacher_ok(const vo_shape* s, const vo_teacher* t) {
+  return t->K >= 1 && t->K <= kTeacherMaxK && s->V <= (1 << 20) && round_up(s->N, kVocabGroup) * t->K < ((int64_t)1 << 31) && t->temperature > 0.f &&
+         std::isfinite(t->temperature) && std::isfinite(1.f / t->temperature) && std::isfinite(t->scale);
+}
+
+// pairs of terms (rank of A, rank of B), the smallest products first
+int term_pairs(int a_terms, int b_terms, int (&pairs)[kMaxSeg][2]) {
+  int n = 0;
+  for (int sum = 2; sum >= 0; --sum)
+    for (int a = 0; a <= sum; ++a)
+      if (a < a_terms && sum - a < b_terms) {
+        pairs[n][0] = a;
+        pairs[n++][1] = sum - a;
+      }
+  return n;
+}
+int pair_count(int a_terms, int b_terms) {
+  int pairs[kMaxSeg][2];
+  return term_pairs(a_terms, b_terms, pairs);
+}
+
+int64_t piece_columns(int64_t V, int64_t bytes_per_column) {
+  int64_t c = kPieceBytes / bytes_per_column / kPieceColumns * kPieceColumns;
+  if (c < kPieceColumns) c = kPieceColumns;
+  if (c > (1 << 20)) c = 1 << 20;
+  const int64_t pieces = (V + c - 1) / c;
+  return round_up((V + pieces - 1) / pieces, kPieceColumns);   // of the same size
+}
+
+VocabLayout vocab_layout(const vo_shape* s, const vo_teacher* t) {
+  VocabLayout L;
+  const int64_t N = s->N, H = s->H, V = s->V;
+  L.f32 = s->dtype == AS_F32;
+  L.g_bf16 = s->grad_dtype == AS_BF16;
+  L.h_terms = L.f32 ? 3 : 1;
+  L.dl_terms = L.g_bf16 ? 1 : 3;
+  L.ldH = round_up(H, 8);
+  L.strips = (int)((V + kVocabStrip - 1) / kVocabStrip);
+  L.groups = (int)((N + kVocabGroup - 1) / kVocabGroup);
+  const int64_t w_col = L.f32 ? L.ldH * 6 : 0;   // bytes of a column's terms of W
+  // forward
+  L.t_fwd = vocab_tile((int)N, (int)(V < (1 << 20) ? V : (1 << 20)), (int)L.ldH * pair_count(L.h_terms, L.h_terms));
+  L.e_fwd = vocab_tile_edge(L.t_fwd);
+  const int64_t stat_col = (N * 16 + L.e_fwd - 1) / L.e_fwd;
+  L.fwd_cols = piece_columns(V, stat_col > w_col ? stat_col : w_col);
+  // backward
+  const int64_t dl_col = N * 2 * L.dl_terms;
+  L.bwd_cols = piece_columns(V, dl_col > w_col ? dl_col : w_col);
+  L.ldd = round_up(L.bwd_cols < V ? L.bwd_cols : V, 8);
+  L.t_bwd = vocab_tile((int)N, (int)L.ldd, (int)L.ldH * pair_count(L.h_terms, L.h_terms));
+  L.e_bwd = vocab_tile_edge(L.t_bwd);
+  const int n_dw = pair_count(L.dl_terms, L.h_terms);
+  // (fp32 widths that are no whole vectors cannot be combined: no split of dW there)
+  L.p_dw = gemm_plan((int)L.ldd, (int)H, (int)(n_dw == 1 ? N : n_dw * round_up(N, 64)), 1, true, H % 8 == 0, n_dw > 1, true);
+  L.p_dh = gemm_plan((int)N, (int)L.ldH, (int)(n_dw == 1 ? L.ldd : n_dw * round_up(L.ldd, 64)), 1, true, true, n_dw > 1, true);
+  // one segment in 256 x 256 tiles: the split is chosen on the device, from the rows that there are
+  L.dh_dyn = false;
+  if (n_dw == 1 && L.p_dh.tile == kTile256) {
+    int64_t most = kPieceBytes / (N * L.ldH * 4);
+    if (most > 8) most = 8;
+    if (most >= 2) {
+      L.dh_dyn = true;
+      L.p_dh.splits = (int)most;
+    } else {
+      L.p_dh.splits = 1;
+    }
+  }
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t o = off;
+    off += upv(bytes);
+    return o;
+  };
+  L.rows = take(N * 4);
+  L.row_pos = take(N * 4);
+  L.y = take(N * 4);
+  L.n_act = take(16);
+  L.ticket = take(16);
+  L.hc = take((size_t)L.h_terms * N * L.ldH * 2);
+  L.lse = take(N * 4);
+  L.at_word = take(N * 4);
+  L.loss_ws = take(N * 4);
+  L.run = take(L.fwd_cols < V ? N * 16 : 0);
+  L.lse_tau = L.distill_ws = L.runs = L.ent = L.ent_p = L.ent_l = L.place = L.p_log_p = L.seen = 0;
+  if (t) {
+    const size_t entries = (size_t)L.groups * kVocabGroup * t->K;
+    L.lse_tau = take(N * 4);
+    L.distill_ws = take(N * 4);
+    L.runs = take((size_t)L.groups * (L.strips + 1) * 4);
+    L.ent = take(entries * 4);
+    L.ent_p = take(entries * 4);
+    L.ent_l = take(entries * 4);
+    L.place = take((size_t)N * t->K * 4);
+    L.p_log_p = take(N * 4);
+    L.seen = take(N * 4);
+  }
+  const size_t area = off;
+  const int64_t parts = (L.fwd_cols + L.e_fwd - 1) / L.e_fwd;
+  L.stat = take((size_t)parts * N * 8);
+  L.stat_tau = take(t ? (size_t)parts * N * 4 : 0);
+  L.stat_idx = take((size_t)parts * N * 4);
+  L.w_fwd = take((size_t)L.fwd_cols * w_col);
+  size_t end = off;
+  off = area;
+  L.dl = take((size_t)L.dl_terms * N * L.ldd * 2);
+  L.w_bwd = take((size_t)L.bwd_cols * w_col);
+  L.col_sums = take((size_t)((N + L.e_bwd - 1) / L.e_bwd) * L.ldd * 4);
+  L.dh_acc = take((size_t)N * L.ldH * 4);
+  const size_t pw = gemm_partial_bytes((int)L.ldd, (int)H, 1, L.p_dw.splits), ph = gemm_partial_bytes((int)N, (int)L.ldH, 1, L.p_dh.splits);
+  L.partial = take(pw > ph ? pw : ph);
+  L.total = off > end ? off : end;
+  return L;
+}
+
+// the last piece may have fewer reduction tiles than the others, and no split may be empty
+int whole_splits(int segments, int k, int splits) {
+  const int tiles = segments * ((k + 63) / 64);
+  if (splits > tiles) splits = tiles;
+  const int per = (tiles + splits - 1) / splits;
+  return (tiles + per - 1) / per;
+}
+
+bool al16v(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+as_status check_shape(const vo_shape* s, const vo_teacher* t, bool wants_teacher) {
+  if (!s) return set_error(AS_ERR_NULL, "shape is NULL");
+  if (wants_teacher && !t) return set_error(AS_ERR_NULL, "teacher is NULL");
+  if (!types_ok(s)) return set_error(AS_ERR_DTYPE, "vocabulary loss: dtype %d with grad_dtype %d", s->dtype, s->grad_dtype);
+  if (!shape_ok(s))
+    return set_error(AS_ERR_SHAPE, "bad shape N=%d H=%d V=%d pad_id=%d grad_scale=%g", s->N, s->H, s->V, s->pad_id, (double)s->grad_scale);
+  if (t && !teacher_ok(s, t))
+    return set_error(AS_ERR_SHAPE, "bad teacher K=%d temperature=%g scale=%g (V=%d)", t->K, (double)t->temperature, (double)t->scale, s->V);
+  if (s->dtype == AS_BF16 && s->H % 8 != 0) return set_error(AS_ERR_ALIGN, "AS_BF16 requires H %% 8 == 0 (H=%d)", s->H);
+  return AS_OK;
+}
+as_status check_workspace(const VocabLayout& L, const void* ws, size_t bytes) {
+  if (bytes < L.total) return set_error(AS_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", bytes, L.total);
+  if (!al16v(ws)) return set_error(AS_ERR_ALIGN, "workspace is not 16-byte aligned");
+  return AS_OK;
+}
+
+struct Ws {
+  unsigned char* base;
+  template <typename T> T* at(size_t off) const { return reinterpret_cast<T*>(base + off); }
+};
+
+// h W_piece^T for the columns [v0, v0 + cols), with the terms of W in `planes` where there are any
+GemmArgs logits_product(const vo_shape* s, const VocabLayout& L, const Ws& w, const void* W, const uint16_t* planes, int64_t plane,
+                        int64_t v0, int cols) {
+  GemmArgs g;
+  int pairs[kMaxSeg][2];
+  const int n = term_pairs(L.h_terms, L.h_terms, pairs);
+  const uint16_t* hc = w.at<uint16_t>(L.hc);
+  const int64_t h_plane = (int64_t)s->N * L.ldH;
+  for (int i = 0; i < n; ++i) {
+    const uint16_t* b = L.f32 ? planes + pairs[i][1] * plane : reinterpret_cast<const uint16_t*>(W) + v0 * s->H;
+    g.seg(hc + pairs[i][0] * h_plane, L.ldH, 0, b, L.ldH, 0, (int)L.ldH);
+  }
+  g.M = s->N;
+  g.N = cols;
+  g.ldc = round_up(cols, 8);
+  g.M_dev = w.at<int32_t>(L.n_act);
+  return g;
+}
+const void* bias_at(const vo_shape* s, const void* b, int64_t v0) {
+  if (!b) return nullptr;
+  return reinterpret_cast<const unsigned char*>(b) + v0 * (s->dtype == AS_F32 ? 4 : 2);
+}
+
+as_status hip_fail(hipError_t e, const char* what) { return set_error(AS_ERR_HIP, "%s: %s", what, hipGetErrorString(e)); }
+
+as_status forward(const vo_shape* s, const vo_teacher* t, const void* h, const void* W, const void* b, const int32_t* targets,
+                  const int32_t* teacher_ids, const float* teacher_logits, float* loss_sum, int32_t* n_tok, float* distill_sum,
+                  float* tok_loss, float* tok_distill, int32_t* argmax, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (!h || !W || !targets || !loss_sum || !n_tok || !workspace) return set_error(AS_ERR_NULL, "a required pointer is NULL");
+  if (t && (!teacher_ids || !teacher_logits || !distill_sum)) return set_error(AS_ERR_NULL, "a required pointer is NULL");
+  const VocabLayout L = vocab_layout(s, t);
+  const as_status rc = check_workspace(L, workspace, workspace_bytes);
+  if (rc != AS_OK) return rc;
+  for (const void* p : {h, W, b, (const void*)targets, (const void*)teacher_ids, (const void*)teacher_logits, (const void*)loss_sum,
+                        (const void*)n_tok, (const void*)distill_sum, (const void*)tok_loss, (const void*)tok_distill, (const void*)argmax})
+    if (!al16v(p)) return set_error(AS_ERR_ALIGN, "a pointer is not 16-byte aligned");
+  hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+  const Ws w{reinterpret_cast<unsigned char*>(workspace)};
+  const int N = s->N;
+  const int64_t h_plane = (int64_t)N * L.ldH;
+
+  VocabRows r{};
+  r.h = h;
+  r.f32 = L.f32;
+  r.targets = targets;
+  r.N = N;
+  r.H = s->H;
+  r.V = s->V;
+  r.pad_id = s->pad_id;
+  r.row_pos = w.at<int32_t>(L.row_pos);
+  r.rows = w.at<int32_t>(L.rows);
+  r.y = w.at<int32_t>(L.y);
+  r.n_act = w.at<int32_t>(L.n_act);
+  r.hc = w.at<uint16_t>(L.hc);
+  r.ldH = L.ldH;
+  r.plane = h_plane;
+  r.tok_loss = tok_loss;
+  r.tok_distill = tok_distill;
+  r.argmax = argmax;
+  r.ticket = w.at<int32_t>(L.ticket);
+  hipError_t e = launch_vocab_rows(r, st);
+  if (e != hipSuccess) return hip_fail(e, "rows of words");
+
+  const float inv_tau = t ? 1.f / t->temperature : 1.f;
+  if (t) {
+    VocabTeacher q{};
+    q.ids = teacher_ids;
+    q.logits = teacher_logits;
+    q.N = N;
+    q.K = t->K;
+    q.V = s->V;
+    q.inv_tau = inv_tau;
+    q.rows = r.rows;
+    q.n_act = r.n_act;
+    q.runs = w.at<int32_t>(L.runs);
+    q.ent = w.at<uint32_t>(L.ent);
+    q.ent_p = w.at<float>(L.ent_p);
+    q.place = w.at<int32_t>(L.place);
+    q.p_log_p = w.at<float>(L.p_log_p);
+    q.seen = w.at<int32_t>(L.seen);
+    q.strips = L.strips;
+    e = launch_vocab_teacher(q, st);
+    if (e != hipSuccess) return hip_fail(e, "teacher's lists");
+  }
+
+  VocabFinish f{};
+  f.stat = w.at<float2>(L.stat);
+  f.stat_tau = t ? w.at<float>(L.stat_tau) : nullptr;
+  f.stat_idx = argmax ? w.at<int32_t>(L.stat_idx) : nullptr;
+  f.ldr = N;
+  f.run = w.at<float4>(L.run);
+  f.at_word = w.at<float>(L.at_word);
+  f.rows = r.rows;
+  f.n_act = r.n_act;
+  f.N = N;
+  f.lse = w.at<float>(L.lse);
+  f.loss_ws = w.at<float>(L.loss_ws);
+  f.tok_loss = tok_loss;
+  f.tok_distill = tok_distill;
+  f.argmax = argmax;
+  f.loss_sum = loss_sum;
+  f.distill_sum = distill_sum;
+  f.n_tok = n_tok;
+  f.ticket = r.ticket;
+  f.inv_tau = inv_tau;
+  if (t) {
+    f.lse_tau = w.at<float>(L.lse_tau);
+    f.distill_ws = w.at<float>(L.distill_ws);
+    f.K = t->K;
+    f.tau2 = t->temperature * t->temperature;
+    f.place = w.at<int32_t>(L.place);
+    f.seen = w.at<int32_t>(L.seen);
+    f.ent_p = w.at<float>(L.ent_p);
+    f.ent_l = w.at<float>(L.ent_l);
+    f.p_log_p = w.at<float>(L.p_log_p);
+  }
+  for (int64_t v0 = 0; v0 < s->V; v0 += L.fwd_cols) {
+    const int cols = (int)(s->V - v0 < L.fwd_cols ? s->V - v0 : L.fwd_cols);
+    uint16_t* planes = w.at<uint16_t>(L.w_fwd);
+    const int64_t plane = L.fwd_cols * L.ldH;
+    if (L.f32) {
+      e = launch_vocab_terms(reinterpret_cast<const float*>(W) + v0 * s->H, cols, s->H, planes, L.ldH, plane, st);
+      if (e != hipSuccess) return hip_fail(e, "terms of W");
+    }
+    VocabEpi v{};
+    v.v0 = (int32_t)v0;
+    v.y = r.y;
+    v.bias = bias_at(s, b, v0);
+    v.bias_f32 = L.f32;
+    v.inv_tau = inv_tau;
+    v.stat = w.at<float2>(L.stat);
+    v.stat_tau = w.at<float>(L.stat_tau);
+    v.stat_idx = w.at<int32_t>(L.stat_idx);
+    v.ldr = N;
+    v.at_word = w.at<float>(L.at_word);
+    v.runs = w.at<int32_t>(L.runs);
+    v.ent = w.at<uint32_t>(L.ent);
+    v.ent_l = w.at<float>(L.ent_l);
+    v.strips = L.strips;
+    e = launch_gemm_vocab(logits_product(s, L, w, W, planes, plane, v0, cols), L.t_fwd, v, 0, t != nullptr, argmax != nullptr, st);
+    if (e != hipSuccess) return hip_fail(e, "statistics of the logits");
+    f.parts = (cols + L.e_fwd - 1) / L.e_fwd;
+    f.first = v0 == 0;
+    f.last = v0 + L.fwd_cols >= s->V;
+    e = launch_vocab_finish(f, st);
+    if (e != hipSuccess) return hip_fail(e, "losses");
+  }
+  return AS_OK;
+}
+
+as_status backward(const vo_shape* s, const vo_teacher* t, const void* W, const void* b, void* workspace, size_t workspace_bytes,
+                   void* dh, void* dW, void* db, void* hip_stream) {
+  if (!W || !workspace || !dh || !dW) return set_error(AS_ERR_NULL, "a required pointer is NULL");
+  const VocabLayout L = vocab_layout(s, t);
+  const as_status rc = check_workspace(L, workspace, workspace_bytes);
+  if (rc != AS_OK) return rc;
+  for (const void* p : {W, b, (const void*)dh, (const void*)dW, (const void*)db})
+    if (!al16v(p)) return set_error(AS_ERR_ALIGN, "a pointer is not 16-byte aligned");
+  hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+  const Ws w{reinterpret_cast<unsigned char*>(workspace)};
+  const int N = s->N, H = s->H;
+  const int32_t* n_act = w.at<int32_t>(L.n_act);
+  const int64_t h_plane = (int64_t)N * L.ldH, dl_plane = (int64_t)N * L.ldd, w_plane = L.bwd_cols * L.ldH;
+  uint16_t *dl = w.at<uint16_t>(L.dl), *planes = w.at<uint16_t>(L.w_bwd);
+  const size_t ge = L.g_bf16 ? 2 : 4;
+  int pairs[kMaxSeg][2];
+  const int n = term_pairs(L.dl_terms, L.h_terms, pairs);
+  hipError_t e;
+  for (int64_t v0 = 0; v0 < s->V; v0 += L.bwd_cols) {
+    const int cols = (int)(s->V - v0 < L.bwd_cols ? s->V - v0 : L.bwd_cols);
+    if (L.f32) {
+      e = launch_vocab_terms(reinterpret_cast<const float*>(W) + v0 * H, cols, H, planes, L.ldH, w_plane, st);
+      if (e != hipSuccess) return hip_fail(e, "terms of W");
+    }
+    VocabEpi v{};
+    v.v0 = (int32_t)v0;
+    v.y = w.at<int32_t>(L.y);
+    v.bias = bias_at(s, b, v0);
+    v.bias_f32 = L.f32;
+    v.inv_tau = t ? 1.f / t->temperature : 1.f;
+    v.runs = w.at<int32_t>(L.runs);
+    v.ent = w.at<uint32_t>(L.ent);
+    v.ent_p = w.at<float>(L.ent_p);
+    v.strips = L.strips;
+    v.lse = w.at<float>(L.lse);
+    v.lse_tau = w.at<float>(L.lse_tau);
+    v.g = s->grad_scale;
+    v.c2 = t ? t->scale * t->temperature : 0.f;
+    v.dl = dl;
+    v.ldd = L.ldd;
+    v.plane = dl_plane;
+    v.col_sums = db ? w.at<float>(L.col_sums) : nullptr;
+    v.ld_sums = L.ldd;
+    e = launch_gemm_vocab(logits_product(s, L, w, W, planes, w_plane, v0, cols), L.t_bwd, v, L.dl_terms, t != nullptr, false, st);
+    if (e != hipSuccess) return hip_fail(e, "derivative of the logits");
+    if (db) {
+      e = launch_vocab_col_sums(v.col_sums, L.ldd, (N + L.e_bwd - 1) / L.e_bwd, L.e_bwd, n_act, cols,
+                                reinterpret_cast<unsigned char*>(db) + v0 * ge, L.g_bf16, st);
+      if (e != hipSuccess) return hip_fail(e, "db");
+    }
+    GemmArgs gw;   // dW_piece = dl^T h
+    for (int i = 0; i < n; ++i)
+      gw.seg(dl + pairs[i][0] * dl_plane, L.ldd, 0, w.at<uint16_t>(L.hc) + pairs[i][1] * h_plane, L.ldH, 0, N);
+    gw.a_kc = gw.b_kc = false;
+    gw.M = cols;
+    gw.N = H;
+    gw.C = reinterpret_cast<unsigned char*>(dW) + (size_t)v0 * H * ge;
+    gw.ldc = H;
+    gw.c_bf16 = L.g_bf16;
+    gw.K_dev = n_act;
+    gw.splits = L.p_dw.splits;
+    gw.partial = w.at<float>(L.partial);
+    e = launch_gemm(gw, true, L.p_dw.tile, st);
+    if (e != hipSuccess) return hip_fail(e, "dW");
+    GemmArgs gh;   // dh += dl W_piece
+    for (int i = 0; i < n; ++i) {
+      const uint16_t* wb = L.f32 ? planes + pairs[i][1] * w_plane : reinterpret_cast<const uint16_t*>(W) + v0 * H;
+      gh.seg(dl + pairs[i][0] * dl_plane, L.ldd, 0, wb, L.ldH, 0, cols);
+    }
+    gh.b_kc = false;
+    gh.M = N;
+    gh.N = (int)L.ldH;
+    gh.C = w.at<float>(L.dh_acc);
+    gh.ldc = L.ldH;
+    gh.accumulate = v0 > 0;
+    gh.M_dev = n_act;
+    gh.splits = L.dh_dyn ? L.p_dh.splits : whole_splits(n, cols, L.p_dh.splits);
+    gh.dyn_split = L.dh_dyn;
+    gh.partial = w.at<float>(L.partial);
+    e = launch_gemm(gh, true, L.p_dh.tile, st);
+    if (e != hipSuccess) return hip_fail(e, "dh");
+  }
+  e = launch_vocab_scatter(w.at<float>(L.dh_acc), w.at<int32_t>(L.row_pos), N, H, L.ldH, dh, L.g_bf16, st);
+  if (e != hipSuccess) return hip_fail(e, "dh to its rows");
+  return AS_OK;
+}
+
+}  // namespace
+}  // namespace asx
+
+using namespace asx;
+
+extern "C" size_t vocab_xent_workspace_bytes(const vo_shape* shape, const vo_teacher* teacher) {
+  if (!shape || !types_ok(shape) || !shape_ok(shape) || (shape->dtype == AS_BF16 && shape->H % 8 != 0)) return 0;
+  if (teacher && !teacher_ok(shape, teacher)) return 0;
+  return vocab_layout(shape, teacher).total;
+}
+
+extern "C" as_status vocab_xent_fwd(const vo_shape* shape, const void* h, const void* W, const void* b, const int32_t* targets,
+                                    float* loss_sum, int32_t* n_tok, float* tok_loss, int32_t* argmax,
+                                    void* workspace, size_t workspace_bytes, void* hip_stream) {
+  const as_status rc = check_shape(shape, nullptr, false);
+  if (rc != AS_OK) return rc;
+  return forward(shape, nullptr, h, W, b, targets, nullptr, nullptr, loss_sum, n_tok, nullptr, tok_loss, nullptr, argmax, workspace,
+                 workspace_bytes, hip_stream);
+}
+extern "C" as_status vocab_xent_bwd(const vo_shape* shape, const void* W, const void* b, void* workspace, size_t workspace_bytes,
+                                    void* dh, void* dW, void* db, void* hip_stream) {
+  const as_status rc = check_shape(shape, nullptr, false);
+  if (rc != AS_OK) return rc;
+  return backward(shape, nullptr, W, b, workspace, workspace_bytes, dh, dW, db, hip_stream);
+}
+extern "C" as_status vocab_distill_fwd(const vo_shape* shape, const vo_teacher* teacher, const void* h, const void* W, const void* b,
+                                       const int32_t* targets, const int32_t* teacher_ids, const float* teacher_logits,
+                                       float* loss_sum, int32_t* n_tok, float* distill_sum, float* tok_loss, float* tok_distill,
+                                       void* workspace, size_t workspace_bytes, void* hip_stream) {
+  const as_status rc = check_shape(shape, teacher, true);
+  if (rc != AS_OK) return rc;
+  return forward(shape, teacher, h, W, b, targets, teacher_ids, teacher_logits, loss_sum, n_tok, distill_sum, tok_loss, tok_distill,
+                 nullptr, workspace, workspace_bytes, hip_stream);
+}
+extern "C" as_status vocab_distill_bwd(const vo_shape* shape, const vo_teacher* teacher, const void* W, const void* b,
+                                       void* workspace, size_t workspace_bytes, void* dh, void* dW, void* db, void* hip_stream) {
+  const as_status rc = check_shape(shape, teacher, true);
+  if (rc != AS_OK) return rc;
+  return backward(shape, teacher, W, b, workspace, workspace_bytes, dh, dW, db, hip_stream);
+}

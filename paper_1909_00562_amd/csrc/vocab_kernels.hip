@@ -1,0 +1,444 @@
+// Kernels around the products of the vocabulary operators: the rows of words, the teacher's lists, the join of the tiles'
+// statistics, and what takes gradients to where the caller wants them.
+#include <climits>
+
+#include "common.h"
+#include "lds_limit.h"
+#include "vocab.h"
+#include "vocab_epi_dev.h"
+
+namespace asx {
+namespace {
+
+__device__ __forceinline__ int row_count(const int32_t* n_act, int N) {
+  const int v = *n_act;
+  return v < 0 ? 0 : (v < N ? v : N);
+}
+
+// ---- rows of words --------------------------------------------------------------------
+// 16 positions per block.  A block counts the words ahead of its own by reading all targets there (64 KiB at 16384 positions,
+// from the L2): a list made ahead by one block would be a launch of its own that everything waits for.
+constexpr int kRowsBlock = 16;
+__device__ __forceinline__ bool is_word(int y, int V, int pad_id) { return y >= 0 && y < V && y != pad_id; }
+__global__ __launch_bounds__(256) void vocab_rows_kernel(VocabRows p) {
+  __shared__ int part[4], place[kRowsBlock];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n0 = blockIdx.x * kRowsBlock;
+  int before = 0;
+  for (int i = tid * 4; i < n0; i += 1024) {
+    const int4 y = *reinterpret_cast<const int4*>(p.targets + i);
+    before += is_word(y.x, p.V, p.pad_id) + is_word(y.y, p.V, p.pad_id) + is_word(y.z, p.V, p.pad_id) + is_word(y.w, p.V, p.pad_id);
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) before += __shfl_xor(before, o, 64);
+  if (lane == 0) part[wave] = before;
+  __syncthreads();
+  before = part[0] + part[1] + part[2] + part[3];
+  if (wave == 0) {
+    const int n = n0 + lane;
+    const bool in = lane < kRowsBlock && n < p.N;
+    const int y = in ? p.targets[n] : -1;
+    const bool word = in && is_word(y, p.V, p.pad_id);
+    const uint64_t m = __ballot(word);
+    const int r = before + __popcll(m & ((1ull << lane) - 1));
+    if (lane < kRowsBlock) place[lane] = word ? r : -1;
+    if (in) {
+      p.row_pos[n] = word ? r : -1;
+      if (word) {
+        p.rows[r] = n;
+        p.y[r] = y;
+      } else {
+        if (p.tok_loss) p.tok_loss[n] = 0.f;
+        if (p.tok_distill) p.tok_distill[n] = 0.f;
+        if (p.argmax) p.argmax[n] = p.pad_id;
+      }
+    }
+    if (lane == 0 && n0 + kRowsBlock >= p.N) *p.n_act = before + __popcll(m);
+    if (lane == 0 && blockIdx.x == 0) *p.ticket = 0;
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (int j = wave; j < kRowsBlock; j += 4) {
+    const int r = place[j];
+    if (r < 0) continue;
+    uint16_t* out = p.hc + (int64_t)r * p.ldH;
+    if (!p.f32) {   // H % 8 == 0
+      const uint16_t* src = reinterpret_cast<const uint16_t*>(p.h) + (int64_t)(n0 + j) * p.H;
+      for (int c = lane * 8; c < p.H; c += 512) *reinterpret_cast<uint4*>(out + c) = *reinterpret_cast<const uint4*>(src + c);
+    } else {
+      const float* src = reinterpret_cast<const float*>(p.h) + (int64_t)(n0 + j) * p.H;
+      for (int c = lane; c < p.ldH; c += 64) {
+        float x = c < p.H ? src[c] : 0.f;
+#pragma unroll
+        for (int t = 0; t < 3; ++t) out[t * p.plane + c] = (uint16_t)bf16_term(x);
+      }
+    }
+  }
+}
+
+// ---- fp32 operands as terms -------------------------------------------------------------
+// Four columns per thread; bound by memory (4 bytes in, 6 out).
+__global__ __launch_bounds__(256) void vocab_terms_kernel(const float* __restrict__ src, int rows, int H, uint16_t* __restrict__ dst,
+                                                          int64_t ldH, int64_t plane, int quads_log) {
+  const int64_t r = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> quads_log;
+  if (r >= rows) return;
+  const int lane = threadIdx.x & ((1 << quads_log) - 1);
+  const float* x0 = src + r * H;
+  for (int c = lane * 4; c < ldH; c += 4 << quads_log) {
+    float x[4];
+    if (H % 4 == 0 && c + 4 <= H) {
+      const f32x4_t v = *reinterpret_cast<const f32x4_t*>(x0 + c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = v[e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = c + e < H ? x0[c + e] : 0.f;
+    }
+#pragma unroll
+    for (int t = 0; t < 3; ++t) {
+      uint32_t b[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) b[e] = bf16_term(x[e]);
+      *reinterpret_cast<uint2*>(dst + t * plane + r * ldH + c) = make_uint2(b[0] | (b[1] << 16), b[2] | (b[3] << 16));
+    }
+  }
+}
+
+// ---- the teacher's lists ------------------------------------------------------------------
+// A block per group of 16 rows, a wave per row.  Softmax over the row's entries; entries with the same id become one with all
+// of their probability (the first of them); a counting sort of the group's entries by strip of 64 columns.  The order inside a
+// strip is not fixed and nothing depends on it: no two entries are of the same row and column, and place[] finds a row's entries.
+__global__ __launch_bounds__(1024) void vocab_teacher_kernel(VocabTeacher p) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  __shared__ int wsum[16];
+  const int R = row_count(p.n_act, p.N), g = blockIdx.x;
+  if (g * kVocabGroup >= R) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, K = p.K, r = g * kVocabGroup + wave;
+  int* ids = reinterpret_cast<int*>(smem) + wave * K;
+  float* prob = reinterpret_cast<float*>(smem) + 16 * K + wave * K;
+  int* hist = reinterpret_cast<int*>(smem) + 32 * K;
+  for (int i = tid; i < p.strips; i += 1024) hist[i] = 0;
+  constexpr int PER = kTeacherMaxK / 64;
+  int id[PER];
+  float P[PER];
+  bool first[PER];
+  const bool row = r < R;
+  const int64_t at = row ? (int64_t)p.rows[r] * K : 0;
+  float z[PER], top = -INFINITY;
+  bool any = false, in[PER];
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const int k = lane + 64 * j;
+    id[j] = row && k < K ? p.ids[at + k] : -1;
+    in[j] = id[j] >= 0 && id[j] < p.V;
+    z[j] = in[j] ? p.logits[at + k] : -INFINITY;
+    in[j] = in[j] && z[j] != -INFINITY;
+    if (!in[j]) id[j] = -1;
+    any = any || in[j];
+    top = in[j] ? fmaxf(top, z[j]) : top;
+  }
+  top = wave_max(top);
+  any = __ballot(any) != 0;
+  float sum = 0.f;
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    z[j] = (z[j] - top) * p.inv_tau;
+    P[j] = in[j] ? expf(z[j]) : 0.f;
+    sum += P[j];
+  }
+  sum = wave_sum(sum);
+  const float log_sum = logf(sum), inv = 1.f / sum;
+  float plp = 0.f;
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    P[j] = in[j] ? P[j] * inv : 0.f;
+    if (P[j] != 0.f) plp += P[j] * (z[j] - log_sum);   // (NaN stays)
+    if (lane + 64 * j < K) {
+      ids[lane + 64 * j] = id[j];
+      prob[lane + 64 * j] = P[j];
+    }
+  }
+  plp = wave_sum(plp);
+  if (row && lane == 0) {
+    p.p_log_p[r] = any ? plp : 0.f;
+    p.seen[r] = any ? 1 : 0;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    first[j] = in[j];
+    P[j] = 0.f;
+  }
+  for (int k = 0; k < K; ++k) {
+    const int o = ids[k];
+    const float q = prob[k];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      if (!in[j] || o != id[j]) continue;
+      P[j] += q;
+      first[j] = first[j] && k >= lane + 64 * j;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < PER; ++j)
+    if (first[j]) atomicAdd(hist + id[j] / kVocabStrip, 1);
+  __syncthreads();
+  // exclusive prefix of the strips' counts
+  const int per = (p.strips + 1023) / 1024, beg = tid * per;
+  int mine = 0;
+  for (int i = beg; i < beg + per && i < p.strips; ++i) mine += hist[i];
+  int pre = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int t = __shfl_up(pre, o, 64);
+    if (lane >= o) pre += t;
+  }
+  if (lane == 63) wsum[wave] = pre;
+  __syncthreads();
+  int base = g * kVocabGroup * K, total = 0;
+  for (int w = 0; w < 16; ++w) {
+    if (w < wave) base += wsum[w];
+    total += wsum[w];
+  }
+  int32_t* runs = p.runs + (int64_t)g * (p.strips + 1);
+  int here = base + pre - mine;
+  for (int i = beg; i < beg + per && i < p.strips; ++i) {
+    const int c = hist[i];
+    runs[i] = here;
+    hist[i] = here;
+    here += c;
+  }
+  if (tid == 0) runs[p.strips] = g * kVocabGroup * K + total;
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const int k = lane + 64 * j;
+    int to = -1;
+    if (first[j]) {
+      to = atomicAdd(hist + id[j] / kVocabStrip, 1);
+      p.ent[to] = (uint32_t)id[j] << 4 | (uint32_t)wave;
+      p.ent_p[to] = P[j];
+    }
+    if (row && k < K) p.place[(int64_t)r * K + k] = to;
+  }
+}
+
+// ---- joining the statistics ------------------------------------------------------------------
+struct Stat {
+  float m, s, t;
+  int idx;
+};
+__device__ __forceinline__ Stat join(const Stat& a, const Stat& b, float inv_tau) {
+  constexpr float L2E = 1.4426950408889634f;
+  Stat r;
+  r.m = fmaxf(a.m, b.m);
+  const float da = a.m == r.m ? 0.f : (a.m - r.m) * L2E, db = b.m == r.m ? 0.f : (b.m - r.m) * L2E;
+  r.s = a.s * __builtin_amdgcn_exp2f(da) + b.s * __builtin_amdgcn_exp2f(db);
+  r.t = a.t * __builtin_amdgcn_exp2f(da * inv_tau) + b.t * __builtin_amdgcn_exp2f(db * inv_tau);
+  r.idx = a.m > b.m ? a.idx : (b.m > a.m ? b.idx : (a.idx < b.idx ? a.idx : b.idx));
+  return r;
+}
+
+// RPB rows per block, 1024 / RPB threads per row that take every (1024 / RPB)-th tile; losses of the rows, and by the block that is
+// through last their sums in double, in a fixed order.
+template <int RPB>
+__global__ __launch_bounds__(1024) void vocab_finish_kernel(VocabFinish p) {
+  constexpr int PH = 1024 / RPB;
+  __shared__ Stat part[1024];
+  __shared__ float sh_lse[RPB], sh_tau[RPB];
+  __shared__ double sd[2][16];
+  __shared__ int last_block;
+  const int R = row_count(p.n_act, p.N), tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int row0 = blockIdx.x * RPB, r = row0 + tid % RPB, phase = tid / RPB;
+  if (row0 < R) {
+    Stat st{-INFINITY, 0.f, 0.f, INT_MAX};
+    if (r < R) {
+#pragma unroll 4
+      for (int i = phase; i < p.parts; i += PH) {
+        const int64_t at = (int64_t)i * p.ldr + r;
+        const float2 ms = p.stat[at];
+        st = join(st, Stat{ms.x, ms.y, p.stat_tau ? p.stat_tau[at] : 0.f, p.stat_idx ? p.stat_idx[at] : INT_MAX}, p.inv_tau);
+      }
+    }
+    part[tid] = st;
+    __syncthreads();
+#pragma unroll 1
+    for (int o = PH / 2; o > 0; o >>= 1) {
+      if (phase < o) part[tid] = join(part[tid], part[tid + o * RPB], p.inv_tau);
+      __syncthreads();
+    }
+    if (phase == 0 && r < R) {
+      st = part[tid];
+      if (!p.first) {
+        const float4 q = p.run[r];
+        st = join(Stat{q.x, q.y, q.z, __builtin_bit_cast(int, q.w)}, st, p.inv_tau);
+      }
+      if (!p.last) {
+        p.run[r] = make_float4(st.m, st.s, st.t, __builtin_bit_cast(float, st.idx));
+      } else {
+        const float lse = st.m + logf(st.s), loss = lse - p.at_word[r];
+        const int n = p.rows[r];
+        p.lse[r] = lse;
+        __hip_atomic_store(p.loss_ws + r, loss, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (p.tok_loss) p.tok_loss[n] = loss;
+        if (p.argmax) p.argmax[n] = st.idx == INT_MAX ? 0 : st.idx;
+        if (p.stat_tau) {
+          const float lt = p.seen[r] ? st.m * p.inv_tau + logf(st.t) : INFINITY;
+          p.lse_tau[r] = lt;
+          sh_tau[tid] = lt;
+        }
+      }
+    }
+    if (p.last && p.stat_tau) {   // a wave per row
+      __syncthreads();
+#pragma unroll 1
+      for (int j = wave; j < RPB && row0 + j < R; j += 16) {
+        const int row = row0 + j;
+        float pl = 0.f;
+        for (int k = lane; k < p.K; k += 64) {
+          const int at = p.place[(int64_t)row * p.K + k];
+          if (at < 0) continue;
+          const float q = p.ent_p[at];
+          if (q != 0.f) pl += q * (p.ent_l[at] * p.inv_tau - sh_tau[j]);
+        }
+        pl = wave_sum(pl);
+        if (lane == 0) {
+          const float d = p.seen[row] ? p.tau2 * (p.p_log_p[row] - pl) : 0.f;
+          __hip_atomic_store(p.distill_ws + row, d, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          if (p.tok_distill) p.tok_distill[p.rows[row]] = d;
+        }
+      }
+    }
+  }
+  if (!p.last) return;
+  if (gridDim.x > 1) {
+    __builtin_amdgcn_s_waitcnt(0);   // the wave's losses are where every XCD sees them (stored past the caches)
+    __syncthreads();
+    if (tid == 0) last_block = __hip_atomic_fetch_add(p.ticket, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
+    __syncthreads();
+    if (!last_block) return;
+  } else {
+    __syncthreads();
+  }
+  double a = 0.0, b = 0.0;
+  for (int i = tid; i < R; i += 1024) {
+    a += (double)__hip_atomic_load(p.loss_ws + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (p.stat_tau) b += (double)__hip_atomic_load(p.distill_ws + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    a += __shfl_xor(a, o, 64);
+    b += __shfl_xor(b, o, 64);
+  }
+  if (lane == 0) {
+    sd[0][wave] = a;
+    sd[1][wave] = b;
+  }
+  __syncthreads();
+  if (tid == 0) {
+    a = b = 0.0;
+    for (int w = 0; w < 16; ++w) {
+      a += sd[0][w];
+      b += sd[1][w];
+    }
+    *p.loss_sum = (float)a;
+    *p.n_tok = R;
+    if (p.stat_tau) *p.distill_sum = (float)b;
+  }
+}
+
+// ---- gradients on their way out ------------------------------------------------------------------
+// 64 columns x 16 phases, the phases added in order
+template <typename TE>
+__global__ __launch_bounds__(1024) void vocab_col_sums_kernel(const float* __restrict__ part, int64_t ld, int tile_rows, int edge,
+                                                              const int32_t* __restrict__ n_act, int V, TE* __restrict__ db) {
+  __shared__ float red[16][64];
+  const int c = threadIdx.x & 63, phase = threadIdx.x >> 6, v = blockIdx.x * 64 + c;
+  const int used = (row_count(n_act, INT_MAX) + edge - 1) / edge, rows = used < tile_rows ? used : tile_rows;
+  float s = 0.f;
+  if (v < V)
+#pragma unroll 4
+    for (int r = phase; r < rows; r += 16) s += part[(int64_t)r * ld + v];
+  red[phase][c] = s;
+  __syncthreads();
+  if (phase != 0 || v >= V) return;
+#pragma unroll
+  for (int q = 1; q < 16; ++q) s += red[q][c];
+  st_elem<TE>(db, v, s);
+}
+
+template <typename TE, int VEC>
+__global__ __launch_bounds__(256) void vocab_scatter_kernel(const float* __restrict__ src, const int32_t* __restrict__ row_pos, int N,
+                                                            int H, int64_t ld, TE* __restrict__ dh, int tpr_log) {
+  const int64_t n = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> tpr_log;
+  if (n >= N) return;
+  const int lane = threadIdx.x & ((1 << tpr_log) - 1), r = row_pos[n];
+  const float* from = src + (int64_t)(r < 0 ? 0 : r) * ld;
+  TE* out = dh + n * H;
+  for (int c = lane * VEC; c < H; c += VEC << tpr_log) {
+    if constexpr (VEC == 1) {
+      st_elem<TE>(out, c, r < 0 ? 0.f : from[c]);
+    } else {
+      f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+      if (r >= 0) v = *reinterpret_cast<const f32x4_t*>(from + c);
+      if constexpr (sizeof(TE) == 2) *reinterpret_cast<uint2*>(out + c) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+      else *reinterpret_cast<f32x4_t*>(out + c) = v;
+    }
+  }
+}
+
+int threads_log(int64_t vecs) {
+  int b = 0;
+  while (b < 8 && ((int64_t)1 << b) < vecs) ++b;
+  return b;
+}
+
+}  // namespace
+
+hipError_t launch_vocab_rows(const VocabRows& p, hipStream_t st) {
+  hipLaunchKernelGGL(vocab_rows_kernel, dim3((p.N + kRowsBlock - 1) / kRowsBlock), dim3(256), 0, st, p);
+  return hipGetLastError();
+}
+
+hipError_t launch_vocab_terms(const float* src, int rows, int H, uint16_t* dst, int64_t ldH, int64_t plane, hipStream_t st) {
+  const int log = threads_log(ldH / 4);
+  const int64_t blocks = (((int64_t)rows << log) + 255) / 256;
+  hipLaunchKernelGGL(vocab_terms_kernel, dim3((unsigned)blocks), dim3(256), 0, st, src, rows, H, dst, ldH, plane, log);
+  return hipGetLastError();
+}
+
+hipError_t launch_vocab_teacher(const VocabTeacher& p, hipStream_t st) {
+  const int smem = (32 * p.K + p.strips) * 4;
+  static LdsLimit limit;
+  const hipError_t e = limit.raise(reinterpret_cast<const void*>(vocab_teacher_kernel), 128 * 1024);
+  if (e != hipSuccess) return e;
+  if (smem > 128 * 1024) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(vocab_teacher_kernel, dim3((p.N + kVocabGroup - 1) / kVocabGroup), dim3(1024), smem, st, p);
+  return hipGetLastError();
+}
+
+hipError_t launch_vocab_finish(const VocabFinish& p, hipStream_t st) {
+  // Few rows: more threads per row, since a row's tiles are read one after the other.
+  if (p.N <= 1024) hipLaunchKernelGGL(vocab_finish_kernel<16>, dim3((p.N + 15) / 16), dim3(1024), 0, st, p);
+  else hipLaunchKernelGGL(vocab_finish_kernel<64>, dim3((p.N + 63) / 64), dim3(1024), 0, st, p);
+  return hipGetLastError();
+}
+
+hipError_t launch_vocab_col_sums(const float* col_sums, int64_t ld, int tile_rows, int edge, const int32_t* n_act, int V, void* db,
+                                 bool bf16, hipStream_t st) {
+  const dim3 grid((V + 63) / 64);
+  if (bf16) hipLaunchKernelGGL(vocab_col_sums_kernel<uint16_t>, grid, dim3(1024), 0, st, col_sums, ld, tile_rows, edge, n_act, V, reinterpret_cast<uint16_t*>(db));
+  else hipLaunchKernelGGL(vocab_col_sums_kernel<float>, grid, dim3(1024), 0, st, col_sums, ld, tile_rows, edge, n_act, V, reinterpret_cast<float*>(db));
+  return hipGetLastError();
+}
+
+hipError_t launch_vocab_scatter(const float* src, const int32_t* row_pos, int N, int H, int64_t ld, void* dh, bool bf16, hipStream_t st) {
+  const bool vec = H % 4 == 0;   // (bf16 rows: H % 8 == 0)
+  const int log = threads_log(vec ? H / 4 : H);
+  const dim3 grid((unsigned)((((int64_t)N << log) + 255) / 256));
+  if (bf16) hipLaunchKernelGGL((vocab_scatter_kernel<uint16_t, 4>), grid, dim3(256), 0, st, src, row_pos, N, H, ld, reinterpret_cast<uint16_t*>(dh), log);
+  else if (vec) hipLaunchKernelGGL((vocab_scatter_kernel<float, 4>), grid, dim3(256), 0, st, src, row_pos, N, H, ld, reinterpret_cast<float*>(dh), log);
+  else hipLaunchKernelGGL((vocab_scatter_kernel<float, 1>), grid, dim3(256), 0, st, src, row_pos, N, H, ld, reinterpret_cast<float*>(dh), log);
+  return hipGetLastError();
+}
+
+}  // namespace asx

@@ -1,0 +1,541 @@
+"""The operators over the vocabulary (include/vocab_ops.h) on the GPU against their float64 oracle.
+
+Tolerances are elementwise bounds from the arithmetic, computed with each case: u = 2^-24 is half a step of fp32, a sum of n
+fp32 products is off by at most 2 (n + 8) u times the sum of their magnitudes (twice, for the matrix instructions' own
+order and rounding), a rounding to bf16 by 2^-8 of the value; exp(x) with an argument off by d is off by the factor e^d."""
+import numpy as np
+import pytest
+
+from oracle import vocab_ops_oracle as oracle
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+import paper_1909_00562_amd as lib  # noqa: E402
+from paper_1909_00562_amd import binding as bd  # noqa: E402
+
+U = 2.0 ** -24
+BF = 2.0 ** -8
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+GUARD = 64     # elements behind an output that must stay as they are
+
+
+def _round(a, dtype):
+    """Values representable in the storage type, as float64."""
+    t = torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).to(TYPES[dtype])
+    return t, t.double().numpy()
+
+
+def _guarded(shape, dtype):
+    n = int(np.prod(shape))
+    base = torch.full((n + GUARD,), 7.0, device="cuda", dtype=dtype)
+    return base, base[:n].view(*shape)
+
+
+def _untouched(*bases):
+    for b in bases:
+        assert (b[-GUARD:].float() == 7.0).all()
+
+
+def _near(name, x, o, bound):
+    x = x.double().cpu().numpy() if isinstance(x, torch.Tensor) else np.asarray(x, dtype=np.float64)
+    assert x.shape == o.shape, name
+    assert np.isfinite(x).all(), f"{name}: not finite"
+    over = np.abs(x - o) - (bound + 1e-36)
+    assert (over <= 0).all(), f"{name}: off by {np.abs(x - o).flat[over.argmax()]:.3g}, bound {np.broadcast_to(bound, o.shape).flat[over.argmax()]:.3g}"
+
+
+# ---- embedding -----------------------------------------------------------------------------------------------------------
+
+
+def _embed_case(N, I, V, dtype, grad, pad, seed, ids=None):
+    r = np.random.default_rng(seed)
+    table, table64 = _round(r.uniform(-1, 1, (V, I)), dtype)
+    dy, dy64 = _round(r.normal(size=(N, I)), grad)
+    if ids is None:
+        ids = np.minimum(np.exp(r.uniform(size=N) * np.log(V + 1)).astype(np.int64), V) - 1     # Zipf-like
+        hit = r.uniform(size=N) < pad
+        ids[hit] = r.choice([0, -1, V, -2 ** 31, 2 ** 31 - 1], size=int(hit.sum()))
+    word = oracle.is_word(ids, V, 0)
+    dy[~torch.from_numpy(word)] = float("nan")
+    return table, table64, dy, np.where(word[:, None], dy64, 0.0), torch.from_numpy(ids.astype(np.int32)).cuda(), ids
+
+
+@pytest.mark.parametrize("N, I, V, dtype, grad, pad", [
+    (1, 8, 5, "bf16", "f32", 0.0), (1, 1, 1, "f32", "f32", 0.0), (3, 7, 2, "f32", "f32", 0.3), (16, 512, 3000, "bf16", "f32", 0.0),
+    (63, 64, 700, "bf16", "bf16", 0.3), (1237, 1000, 2003, "bf16", "bf16", 0.25), (1000, 111, 999, "f32", "f32", 0.4),
+    (8192, 72, 513, "bf16", "f32", 0.2), (8193, 72, 512, "bf16", "f32", 0.2), (8193, 20, 511, "f32", "f32", 0.9),
+    (20000, 40, 300000, "bf16", "bf16", 0.1), (40000, 1032, 65, "f32", "f32", 0.0), (70001, 24, 128000, "bf16", "f32", 0.5),
+    (9000, 5, 1 << 19, "f32", "f32", 0.1), (300, 4200, 40, "f32", "f32", 0.1)])
+def test_embedding(N, I, V, dtype, grad, pad):
+    table, t64, dy, dy64, ids, ids_np = _embed_case(N, I, V, dtype, grad, pad, seed=N + I)
+    scale = float(np.float32(1.7))
+    e = lib.DeviceEmbed(table.cuda(), N, pad_id=0, scale=scale, grad_dtype=grad)
+    xb, x = _guarded((N, I), TYPES[dtype])
+    e.fwd(ids, x)
+    o = oracle.embed_fwd(t64, ids_np, scale, 0)
+    _near("x", x, o, np.abs(o) * (2 * U + (BF if dtype == "bf16" else 0)))
+    db, d = _guarded((V, I), TYPES[grad])
+    dyc = dy.cuda()
+    e.bwd(ids, dyc, d)
+    od, mag = oracle.embed_bwd(ids_np, dy64, scale, V, 0), oracle.embed_bwd(ids_np, np.abs(dy64), scale, V, 0)
+    count = np.bincount(ids_np[oracle.is_word(ids_np, V, 0)], minlength=V)[:, None]
+    bound = mag * (count + 4) * U + (np.abs(od) + mag * (count + 4) * U) * (BF if grad == "bf16" else 0)
+    _near("d_table", d, od, bound)
+    d2 = torch.empty_like(d)
+    e.bwd(ids, dyc, d2)
+    assert torch.equal(d, d2)
+    # onto what is there: rows of other words keep their bits
+    old = torch.randn(V, I, device="cuda").to(TYPES[grad])
+    d3 = old.clone()
+    e.bwd(ids, dyc, d3, accumulate=True)
+    o3 = od + old.double().cpu().numpy()
+    grow = bound + (np.abs(old.double().cpu().numpy()) + np.abs(od)) * 2 * U + np.abs(o3) * (BF if grad == "bf16" else 0)
+    _near("accumulated", d3, o3, grow)
+    none = torch.from_numpy(count[:, 0] == 0).cuda()
+    assert torch.equal(d3[none], old[none])
+    _untouched(xb, db)
+
+
+@pytest.mark.parametrize("N, word", [(1, -1), (50, -1), (50, 3), (16, 3), (17, 3), (16384, 3), (16385, 3), (100000, 3), (100000, -1)])
+def test_embedding_of_one_word_or_none(N, word):
+    ids_np = np.full(N, word)
+    table, t64, dy, dy64, ids, _ = _embed_case(N, 64, 9, "bf16", "f32", 0.0, seed=1, ids=ids_np)
+    e = lib.DeviceEmbed(table.cuda(), N, scale=1.0, grad_dtype="f32")
+    d = e.bwd(ids, dy.cuda())
+    od = oracle.embed_bwd(ids_np, dy64, 1.0, 9, -1)
+    mag = np.abs(dy64).sum(axis=0)
+    _near("d_table", d, od, np.broadcast_to(mag * (N + 4) * U, od.shape))
+    assert not d[torch.arange(9, device="cuda") != word].any()
+    x = e.fwd(ids)
+    if word < 0:
+        assert not x.any()
+
+
+def test_embedding_wants_dense_tensors_of_its_types():
+    e = lib.DeviceEmbed(torch.zeros(10, 16, device="cuda"), 4)
+    ids = torch.zeros(4, dtype=torch.int32, device="cuda")
+    with pytest.raises(lib.AttnSoftmaxError, match="AS_ERR_DTYPE"):
+        e.fwd(ids.long())
+    with pytest.raises(lib.AttnSoftmaxError, match="AS_ERR_SHAPE"):
+        e.fwd(ids[:3])
+    with pytest.raises(lib.AttnSoftmaxError, match="AS_ERR_ALIGN"):
+        e.bwd(ids, torch.zeros(16, 4, device="cuda").t())
+    with pytest.raises(lib.AttnSoftmaxError, match="AS_ERR_SHAPE"):
+        e.fwd(ids.cpu())
+    with pytest.raises(lib.AttnSoftmaxError, match="AS_ERR_ALIGN"):
+        lib.DeviceEmbed(torch.zeros(16, 10, device="cuda").t(), 4)
+    with pytest.raises(lib.AttnSoftmaxError, match="AS_ERR_NULL"):
+        e.bwd(ids, torch.zeros(4, 16, device="cuda"), None, accumulate=True)
+
+
+# ---- losses --------------------------------------------------------------------------------------------------------------
+
+
+class Case:
+    def __init__(self, N, H, V, dtype, grad, K=0, tau=1.0, pad=0.25, bias=True, seed=0, g=0.7, s=0.4, spread=1.0, targets=None):
+        r = np.random.default_rng(seed)
+        self.N, self.H, self.V, self.dtype, self.grad, self.K, self.tau, self.g, self.s = N, H, V, dtype, grad, K, tau, g, s
+        self.g, self.s, self.tau = (float(np.float32(v)) for v in (g, s, tau))
+        self.h, self.h64 = _round(np.tanh(r.normal(size=(N, H))), dtype)
+        self.W, self.W64 = _round(r.uniform(-1, 1, (V, H)) * spread * 3 / np.sqrt(H), dtype)
+        self.b, self.b64 = _round(r.uniform(-1, 1, V), dtype) if bias else (None, None)
+        y = r.integers(min(1, V - 1), V, size=N)
+        hit = r.uniform(size=N) < pad
+        y[hit] = r.choice([0, -1, V, 2 ** 31 - 1], size=int(hit.sum()))
+        self.pad_id = 0 if V > 1 else -1
+        self.y = y if targets is None else targets
+        self.word = oracle.is_word(self.y, V, self.pad_id)
+        self.h[~torch.from_numpy(self.word)] = float("nan")
+        self.h64[~self.word] = 0.0
+        self.teacher = None
+        if K:
+            ids = r.integers(0, V, size=(N, K))
+            if K > 2:
+                ids[::3, 1] = ids[::3, 0]                        # the same word twice
+            z = r.normal(size=(N, K)) * 2
+            some = r.integers(0, K + 1, size=N)
+            gone = (np.arange(K)[None] >= some[:, None]) & (r.uniform(size=(N, 1)) < 0.5)
+            ids[gone] = r.choice([-1, V, -2 ** 31], size=int(gone.sum()))
+            z = z.astype(np.float32)
+            zz = z.copy()
+            zz[gone] = np.nan
+            if K > 1:
+                zz[1::4, 0] = -np.inf                             # an entry without weight
+                z[1::4, 0] = -np.inf
+            self.ids, self.z = ids, zz
+            self.teacher = (ids, z.astype(np.float64), self.tau, self.s)
+
+    def device(self):
+        c = lambda t: None if t is None else t.cuda()  # noqa: E731
+        extra = dict(K=self.K, temperature=self.tau, distill_scale=self.s) if self.K else {}
+        v = lib.DeviceVocabLoss(c(self.W), c(self.b), self.N, pad_id=self.pad_id, grad_scale=self.g, grad_dtype=self.grad, **extra)
+        v.workspace.fill_(0xff)                                   # nothing in it has to be anything (all NaN)
+        self.h_d, self.y_d = self.h.cuda(), torch.from_numpy(self.y.astype(np.int32)).cuda()
+        if self.K:
+            self.ids_d, self.z_d = torch.from_numpy(self.ids.astype(np.int32)).cuda(), torch.from_numpy(self.z).cuda()
+        gt, f32 = TYPES[self.grad], torch.float32
+        self.bases, self.out = {}, {}
+        for name, shape, t in (("loss_sum", (1,), f32), ("n_tok", (1,), torch.int32), ("tok_loss", (self.N,), f32),
+                               ("argmax", (self.N,), torch.int32), ("distill_sum", (1,), f32), ("tok_distill", (self.N,), f32),
+                               ("dh", (self.N, self.H), gt), ("dW", (self.V, self.H), gt), ("db", (self.V,), gt)):
+            self.bases[name], self.out[name] = _guarded(shape, t)
+        return v
+
+    def fwd(self, v, argmax=True):
+        o = self.out
+        if self.K:
+            v.distill_fwd(self.h_d, self.y_d, self.ids_d, self.z_d, o["loss_sum"], o["n_tok"], o["distill_sum"], o["tok_loss"], o["tok_distill"])
+        else:
+            v.xent_fwd(self.h_d, self.y_d, o["loss_sum"], o["n_tok"], o["tok_loss"], o["argmax"] if argmax else None)
+
+    def bwd(self, v):
+        (v.distill_bwd if self.K else v.xent_bwd)(self.out["dh"], self.out["dW"], self.out["db"])
+
+    def check(self, back=True, argmax=True):
+        o = oracle.loss(self.h64, self.W64, self.b64, self.y, self.pad_id, self.g, self.teacher)
+        H, V, w = self.H, self.V, self.word[:, None]
+        ah, aW = np.abs(self.h64), np.abs(self.W64)
+        ab = 0.0 if self.b64 is None else np.abs(np.where(np.isfinite(self.b64), self.b64, 0.0))
+        El = np.where(w, 2 * (6 * H + 8) * U * (ah @ aW.T + ab), 0.0)          # (fp32 storage: six products of terms)
+        with np.errstate(invalid="ignore"):
+            top = o["l"].max(axis=1, keepdims=True)
+            lse = top + np.log(np.exp(o["l"] - top).sum(axis=1, keepdims=True))
+            top_t = top / self.tau
+            lse_t = top_t + np.log(np.exp(o["l"] / self.tau - top_t).sum(axis=1, keepdims=True))
+        worst = El.max(axis=1, keepdims=True)
+        far = np.where(np.isfinite(o["l"]), np.abs(o["l"] - lse), 0.0)
+        sums = (V / 32 + 80) * U
+        E_lse = worst + 8 * U * (np.abs(top) + np.abs(lse) + 1) + sums
+        E_tok = (worst + E_lse + 4 * U * (np.abs(lse) + np.abs(top) + far.max(axis=1, keepdims=True)))[:, 0] * self.word
+        _near("tok_loss", self.out["tok_loss"], o["tok_loss"], E_tok)
+        _near("loss_sum", self.out["loss_sum"], np.array([o["loss_sum"]]), E_tok.sum() + 4 * U * abs(o["loss_sum"]))
+        assert int(self.out["n_tok"]) == o["n_tok"]
+        if argmax and not self.K:
+            got = self.out["argmax"].cpu().numpy()
+            assert (got[~self.word] == self.pad_id).all()
+            at = np.nonzero(self.word)[0]
+            assert (got[at] >= 0).all() and (got[at] < V).all()
+            # the logits that the kernel compares are off by at most El: no other one may be larger by more than both errors
+            assert (o["l"][at, got[at]] + 2 * worst[at, 0] >= o["l"][at].max(axis=1)).all()
+        E_dl = self.g * np.exp(o["l"] - lse) * np.expm1(2 * El + 2 * E_lse + 16 * U * (1 + far))
+        if self.K:
+            z = np.where((self.ids >= 0) & (self.ids < V) & np.isfinite(self.teacher[1]), self.teacher[1], 0.0)
+            span = (np.abs(z).max(axis=1, keepdims=True) * 2 + 20) / self.tau
+            E_p = 16 * U * (1 + span) + 2 * self.K * U                                # relative, of a probability
+            far_t = np.abs(np.where(np.isfinite(o["l"]), o["l"] / self.tau, 0.0) - lse_t)
+            E_lt = E_lse / self.tau + 16 * U * (np.abs(top_t) + np.abs(lse_t) + 1) + sums
+            E_d = self.tau ** 2 * ((E_p + 2 * self.K * U) * (span + far_t.max(axis=1, keepdims=True) + 10) + worst / self.tau + E_lt)[:, 0] * self.word
+            _near("tok_distill", self.out["tok_distill"], o["tok_distill"], E_d)
+            _near("distill_sum", self.out["distill_sum"], np.array([o["distill_sum"]]), E_d.sum() + 4 * U * abs(o["distill_sum"]))
+            E_dl = E_dl + self.s * self.tau * (np.exp(o["l"] / self.tau - lse_t) * np.expm1(2 * El / self.tau + 2 * E_lt + 16 * U * (1 + far_t)))
+            p = np.zeros_like(E_dl)
+            for n in range(self.N):
+                there = [k for k in range(self.K) if 0 <= self.ids[n, k] < V and self.teacher[1][n, k] != -np.inf]
+                for k in there:                                                        # (at most 1 each)
+                    p[n, self.ids[n, k]] += 1.0 / len(there) if len(there) == 1 else 1.0
+            E_dl = E_dl + self.s * self.tau * np.minimum(p, 1.0) * (E_p + 2 * U)
+        E_dl = np.where(w, E_dl + 4 * U * (np.abs(o["dl"]) + self.g + self.s * self.tau) * (E_dl > 0) + 0.0, 0.0)
+        if back:
+            E_dl = np.nan_to_num(E_dl)
+            rough = BF if self.grad == "bf16" else 2.0 ** -22
+            adl, R = np.abs(o["dl"]) + E_dl, self.N
+            for name, err, mag, n in (("dW", E_dl.T @ ah, adl.T @ ah, R), ("dh", E_dl @ aW, adl @ aW, V), ("db", E_dl.sum(axis=0), adl.sum(axis=0), R)):
+                _near(name, self.out[name], o[name], err + mag * (rough + 2 * (6 * n + 8) * U) + (np.abs(o[name]) + err) * (BF if self.grad == "bf16" else U))
+        _untouched(*(b for k, b in self.bases.items()))
+
+
+XENT = [(1, 8, 1, "bf16", "f32"), (1, 1, 2, "f32", "f32"), (1, 64, 1000, "bf16", "bf16"), (2, 5, 3, "f32", "f32"), (16, 512, 2000, "bf16", "f32"),
+        (17, 72, 515, "bf16", "bf16"), (33, 111, 777, "f32", "f32"), (64, 64, 64, "bf16", "bf16"), (65, 136, 4001, "bf16", "f32"),
+        (130, 64, 129, "f32", "f32"), (200, 264, 1003, "bf16", "bf16"), (300, 8, 9000, "bf16", "f32"), (511, 200, 2050, "bf16", "bf16"),
+        (700, 40, 257, "f32", "f32"), (1300, 96, 700, "bf16", "bf16"), (257, 1000, 300, "bf16", "f32")]
+
+
+@pytest.mark.parametrize("N, H, V, dtype, grad", XENT)
+def test_cross_entropy(N, H, V, dtype, grad):
+    c = Case(N, H, V, dtype, grad, seed=N)
+    v = c.device()
+    c.fwd(v)
+    c.bwd(v)
+    c.check()
+    first = {k: t.clone() for k, t in c.out.items() if k in ("dh", "dW", "db")}
+    c.bwd(v)                                                      # a second backward call of one forward call
+    assert all(torch.equal(first[k], c.out[k]) for k in first)
+    c.fwd(v, argmax=False)
+    c.check(back=False, argmax=False)
+
+
+@pytest.mark.parametrize("N, H, V, dtype, grad, K, tau", [
+    (1, 8, 1, "bf16", "f32", 1, 1.0), (3, 16, 40, "f32", "f32", 5, 2.0), (16, 64, 1000, "bf16", "bf16", 8, 2.0), (17, 72, 515, "bf16", "f32", 20, 4.0),
+    (40, 33, 100, "f32", "f32", 256, 0.7), (66, 136, 4001, "bf16", "bf16", 64, 1.0), (130, 64, 70, "bf16", "f32", 100, 3.0),
+    (300, 264, 1003, "bf16", "bf16", 33, 2.0), (700, 40, 257, "f32", "f32", 7, 1.0)])
+def test_distillation(N, H, V, dtype, grad, K, tau):
+    c = Case(N, H, V, dtype, grad, K=K, tau=tau, seed=N + K)
+    v = c.device()
+    c.fwd(v)
+    c.bwd(v)
+    c.check()
+    first = {k: t.clone() for k, t in c.out.items() if k not in ("argmax",)}
+    c.fwd(v)
+    c.bwd(v)
+    assert all(torch.equal(first[k], c.out[k]) for k in first)
+
+
+@pytest.mark.parametrize("K", [0, 6])
+def test_nothing_but_padding(K):
+    c = Case(70, 64, 300, "bf16", "f32", K=K, targets=np.full(70, -1))
+    v = c.device()
+    c.fwd(v)
+    c.bwd(v)
+    assert int(c.out["n_tok"]) == 0
+    for k in ("loss_sum", "tok_loss", "dh", "dW", "db") + (("distill_sum", "tok_distill") if K else ()):
+        assert not c.out[k].any(), k
+
+
+@pytest.mark.parametrize("N", [40, 300])
+def test_pure_distillation_and_extreme_teachers(N):
+    c = Case(N, 64, 500, "bf16", "f32", K=4, tau=2.0, g=0.0, s=1.0, pad=0.1, seed=2)
+    low = np.finfo(np.float32).min
+    for n, z in ((0, [low] * 4), (1, [-np.inf] * 4), (2, [low, low, 3.0, 3.0]), (3, [80.0, -80.0, 0.0, 1.0])):
+        c.ids[n] = [1, 2, 3, 4]
+        c.z[n] = z
+        c.y[n] = 5
+    ok = (c.ids >= 0) & (c.ids < 500)
+    c = _again(c, np.where(ok, c.z, 0.0))
+    v = c.device()
+    c.fwd(v)
+    c.bwd(v)
+    got = c.out["tok_distill"].cpu().numpy()
+    o = oracle.loss(c.h64, c.W64, c.b64, c.y, 0, 0.0, c.teacher)
+    assert got[1] == 0 and o["tok_distill"][1] == 0
+    assert np.isfinite(got).all()
+    # a probability off by 2^-16 at most (logits of 80 over tau); log q is off by less
+    assert np.abs(got - o["tok_distill"]).max() <= 4 * (2.0 ** -16 * 60 + 1e-4)
+    for k in ("dh", "dW", "db"):
+        x, want = c.out[k].double().cpu().numpy(), o[k]
+        assert np.isfinite(x).all() and np.linalg.norm(x - want) <= 2.0 ** -14 * np.linalg.norm(want)
+
+
+def _again(c, z):
+    c.word = oracle.is_word(c.y, c.V, c.pad_id)
+    c.h[~torch.from_numpy(c.word)] = float("nan")
+    h = c.h.double().numpy()
+    c.h[torch.from_numpy(c.word)] = torch.nan_to_num(c.h[torch.from_numpy(c.word)], nan=0.25)
+    h = c.h.double().numpy()
+    c.h64 = np.where(c.word[:, None], h, 0.0)
+    c.teacher = (c.ids, z.astype(np.float64), c.tau, c.s)
+    return c
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_words_that_the_bias_forbids(dtype):
+    c = Case(90, 64, 400, dtype, "f32", seed=5)
+    c.b[torch.arange(0, 400, 3)] = float("-inf")
+    c.b[64:320] = float("-inf")                                   # whole tiles
+    c.b[1] = 0.0
+    c.b64 = c.b.double().numpy()
+    c.y = np.where(c.word, 1, c.y)
+    v = c.device()
+    c.fwd(v)
+    c.bwd(v)
+    c.check()
+    assert not c.out["dW"][64:320].any() and not c.out["db"][64:320].any()
+    got = c.out["argmax"].cpu().numpy()
+    assert np.isfinite(c.b64[got[c.word]]).all()
+
+
+@pytest.mark.parametrize("N", [5, 200])
+def test_the_lowest_of_equal_words_wins(N):
+    c = Case(N, 64, 1000, "bf16", "f32", pad=0.0, seed=8)
+    c.W[500:] = c.W[:500]
+    c.b[500:] = c.b[:500]
+    c.W64, c.b64 = c.W.double().numpy(), c.b.double().numpy()
+    v = c.device()
+    c.fwd(v)
+    assert (c.out["argmax"] < 500).all()
+    c.check(back=False)
+
+
+def test_no_bias():
+    c = Case(150, 72, 515, "bf16", "f32", bias=False, seed=9)
+    v = c.device()
+    c.fwd(v)
+    c.out["db"].zero_()
+    v.xent_bwd(c.out["dh"], c.out["dW"], None)
+    o = oracle.loss(c.h64, c.W64, None, c.y, 0, c.g)
+    assert not c.out["db"].any()
+    for k in ("dh", "dW"):                                        # as with a bias of zeros, bit by bit
+        first = c.out[k].clone()
+        z = Case(150, 72, 515, "bf16", "f32", bias=False, seed=9)
+        z.b, z.b64 = torch.zeros(515, dtype=torch.bfloat16), np.zeros(515)
+        w = z.device()
+        z.fwd(w)
+        z.bwd(w)
+        z.check()
+        assert torch.equal(first, z.out[k])
+    assert abs(float(c.out["loss_sum"]) - o["loss_sum"]) < 1e-3 * o["loss_sum"]
+
+
+# V past a piece: fp32 (terms of W, both passes) and bf16 (dl; 2^20 columns at most)
+@pytest.mark.parametrize("N, H, V, dtype, grad, K", [(5, 512, 50001, "f32", "f32", 0), (70, 512, 90001, "f32", "f32", 9), (60, 8, 380003, "bf16", "f32", 0),
+                                                     (200, 8, 400001, "bf16", "bf16", 5)])
+def test_several_pieces(N, H, V, dtype, grad, K):
+    c = Case(N, H, V, dtype, grad, K=K, tau=2.0, seed=N)
+    v = c.device()
+    c.fwd(v)
+    c.bwd(v)
+    c.check()
+
+
+def _in_64_bits(c, h, y):
+    """dh, dW, db, losses by torch in float64 on the GPU, 1000 rows at a time."""
+    W, b = c.W.cuda().double(), c.b.cuda().double()
+    word = torch.from_numpy(c.word).cuda()
+    rows = torch.nonzero(word)[:, 0]
+    tok = torch.zeros(c.N, device="cuda", dtype=torch.float64)
+    dh, dW, db = torch.zeros(c.N, c.H, device="cuda", dtype=torch.float64), torch.zeros_like(W), torch.zeros_like(b)
+    for at in rows.split(1000):
+        x = h[at].double()
+        l = x @ W.t() + b
+        lse = torch.logsumexp(l, 1, keepdim=True)
+        t = y[at].long()[:, None]
+        tok[at] = (lse - l.gather(1, t))[:, 0]
+        dl = torch.exp(l - lse)
+        dl.scatter_add_(1, t, torch.full_like(lse, -1.0))
+        dl *= c.g
+        dh[at] = dl @ W
+        dW += dl.t() @ x
+        db += dl.sum(0)
+    return dict(tok_loss=tok, dh=dh, dW=dW, db=db)
+
+
+@pytest.mark.parametrize("N, H, V, dtype, grad", [(9000, 64, 130003, "bf16", "bf16"), (5000, 256, 33000, "bf16", "f32"), (3000, 136, 20001, "f32", "f32")])
+def test_large(N, H, V, dtype, grad):
+    c = Case(N, H, V, dtype, grad, seed=1, g=1.0)
+    v = c.device()
+    c.fwd(v)
+    c.bwd(v)
+    o = _in_64_bits(c, c.h_d, c.y_d)
+    # norms: fp32 sums of up to 10^5 terms of either sign, 2^-24 sqrt(10^5); bf16 adds the roundings of dl and of the result
+    for k in ("tok_loss", "dh", "dW", "db"):
+        off = float((c.out[k].double() - o[k]).norm() / o[k].norm())
+        assert off < (2 * BF if grad == "bf16" and k != "tok_loss" else 320 * U), (k, off)
+    _untouched(*c.bases.values())
+
+
+# ---- streams, graphs, used together ---------------------------------------------------------------------------------------
+
+
+def test_another_stream_and_two_at_once():
+    a, b = Case(200, 264, 1003, "bf16", "f32", seed=1), Case(150, 72, 2003, "bf16", "bf16", K=9, tau=2.0, seed=2)
+    va, vb = a.device(), b.device()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        with torch.cuda.stream(s1):
+            a.fwd(va)
+        with torch.cuda.stream(s2):
+            b.fwd(vb)
+        with torch.cuda.stream(s1):
+            a.bwd(va)
+        with torch.cuda.stream(s2):
+            b.bwd(vb)
+    torch.cuda.synchronize()
+    a.check()
+    b.check()
+
+
+@pytest.mark.parametrize("N, K", [(12, 0), (200, 0), (200, 9)])
+def test_captured_and_replayed(N, K):
+    c = Case(N, 264, 1003, "bf16", "f32", K=K, tau=2.0, seed=3)
+    v = c.device()
+    table = torch.randn(1003, 264, device="cuda").bfloat16()
+    e = lib.DeviceEmbed(table, N, pad_id=0, scale=2.0, grad_dtype="f32")
+    dt = torch.empty(1003, 264, device="cuda")
+
+    def step():
+        c.fwd(v)
+        c.bwd(v)
+        e.bwd(c.y_d, c.out["dh"], dt)
+
+    step()
+    torch.cuda.synchronize()
+    names = [k for k in c.out if k in ("loss_sum", "n_tok", "tok_loss", "dh", "dW", "db") or (K and "distill" in k)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for k in range(4):                                            # new words before each replay
+        y = np.roll(c.y, k + 1)
+        c.h_d.copy_(torch.nan_to_num(c.h_d, nan=0.5))
+        c.y_d.copy_(torch.from_numpy(y.astype(np.int32)))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = {n: c.out[n].clone() for n in names} | {"dt": dt.clone()}
+        (torch.randn(500, 500, device="cuda") @ torch.randn(500, 500, device="cuda")).sum()
+        torch.cuda.synchronize()
+        step()
+        torch.cuda.synchronize()
+        for n in names:
+            assert torch.equal(got[n], c.out[n]), (k, n)
+        assert torch.equal(got["dt"], dt)
+
+
+def test_a_backward_pass_wants_its_forward_pass():
+    c = Case(8, 64, 100, "bf16", "f32")
+    v = c.device()
+    with pytest.raises(lib.AttnSoftmaxError):
+        c.bwd(v)
+    with pytest.raises(lib.AttnSoftmaxError):
+        v.distill_fwd(c.h_d, c.y_d, None, None, c.out["loss_sum"], c.out["n_tok"], c.out["distill_sum"])
+
+
+@pytest.mark.parametrize("dtype, tied", [("f32", True), ("bf16", True), ("bf16", False)])
+def test_a_language_model_of_them(dtype, tied):
+    """ids -> embedding -> stacked LSTM -> cross-entropy, and all the way back, against the oracles chained in float64."""
+    from oracle import lstm_stack_oracle as lo
+    T, B, H, V, L, pad = 5, 6, 40, 130, 2, 0
+    r = np.random.default_rng(11)
+    I = H
+    table, t64 = _round(r.uniform(-0.5, 0.5, (V, I)), dtype)
+    W, W64 = (table, t64) if tied else _round(r.uniform(-0.5, 0.5, (V, H)), dtype)
+    b, b64 = _round(r.uniform(-0.5, 0.5, V), dtype)
+    lengths = np.array([5, 3, 0, 1, 4, 5])
+    ids, y = r.integers(1, V, size=(T, B)), r.integers(1, V, size=(T, B))
+    past = np.arange(T)[:, None] >= lengths[None]
+    ids[past], y[past] = pad, pad
+    Wi = [_round(r.uniform(-0.2, 0.2, (4 * H, I if l == 0 else H)), dtype)[1] for l in range(L)]
+    Wh = [_round(r.uniform(-0.2, 0.2, (4 * H, H)), dtype)[1] for _ in range(L)]
+    bl = [_round(r.uniform(-0.2, 0.2, 4 * H), dtype)[1] for _ in range(L)]
+    scale = float(np.float32(np.sqrt(I)))
+    # the library
+    td = table.cuda()
+    e = lib.DeviceEmbed(td, T * B, pad_id=pad, scale=scale, grad_dtype="f32")
+    ids_d, y_d = (torch.from_numpy(a.reshape(-1).astype(np.int32)).cuda() for a in (ids, y))
+    lstm = lib.DeviceLstm(np.zeros((T, B, I)), lengths, Wi, Wh, bl, dtype=dtype)
+    e.fwd(ids_d, lstm.x.view(T * B, I))
+    lstm.fwd()
+    v = lib.DeviceVocabLoss(td if tied else W.cuda(), b.cuda(), T * B, pad_id=pad, grad_scale=0.25, grad_dtype="f32")
+    f32 = dict(device="cuda", dtype=torch.float32)
+    loss_sum, n_tok = torch.empty(1, **f32), torch.empty(1, device="cuda", dtype=torch.int32)
+    v.xent_fwd(lstm.y.view(T * B, H), y_d, loss_sum, n_tok)
+    dh, dW, db = torch.empty(T, B, H, **f32), torch.empty(V, H, **f32), torch.empty(V, **f32)
+    v.xent_bwd(dh.view(T * B, H), dW, db)
+    lstm.bwd(dh)
+    d_table = dW if tied else torch.empty(V, I, **f32)
+    e.bwd(ids_d, lstm.dx.view(T * B, I), d_table, accumulate=tied)
+    torch.cuda.synchronize()
+    # the oracles
+    x = oracle.embed_fwd(t64, ids.reshape(-1), scale, pad).reshape(T, B, I)
+    if dtype == "bf16":
+        x = _round(x, "bf16")[1]
+    saved = lo.forward(x, lengths, Wi, Wh, bl)
+    o = oracle.loss(np.asarray(saved["y"]).reshape(T * B, H), W64, b64, y.reshape(-1), pad, 0.25)
+    back = lo.backward(saved, o["dh"].reshape(T, B, H))
+    od = oracle.embed_bwd(ids.reshape(-1), back["dx"].reshape(T * B, I), scale, V, pad, old=o["dW"] if tied else None)
+    # the LSTM's own tolerances: 1e-4 in fp32, 2e-2 in bf16 (its states are rounded to bf16), by norm
+    tol = 1e-4 if dtype == "f32" else 2e-2
+    for name, got, want in (("dW" if not tied else "dW + d_table", d_table if tied else dW, od if tied else o["dW"]), ("db", db, o["db"]),
+                            ("d_table", d_table, od)):
+        got = got.double().cpu().numpy()
+        assert np.linalg.norm(got - want) <= tol * np.linalg.norm(want), name
+    assert abs(float(loss_sum) - o["loss_sum"]) <= tol * o["loss_sum"] and int(n_tok) == o["n_tok"]
