@@ -2,11 +2,11 @@
 //
 // Forward: a row copy with a multiplication; bound by memory.
 // Backward: d_table[v] = scale * sum of dy[n] over the positions n of word v.  Words are Zipf-like: one word has a tenth of all
-// positions, most have none.  The positions are sorted by word (stable radix sort, so each word's rows are added in increasing
+// positions, most have none.  The positions are sorted by word (a stable sort, so each word's rows are added in increasing
 // n, whatever the launch looks like: no float atomics), the sorted list is cut into pieces of the same length, and a group of
 // threads adds up the rows of its piece, whatever words they are of.  Words that lie inside a piece are written at once; parts
 // of words that reach over a piece's edge go to the workspace, and a second pass adds those up.  Rows of words that no position has
-// are zeroed by further blocks of the same launch, by a bitmap that the sort leaves: d_table is written once.
+// are zeroed by further blocks of the same launch, which look them up in the sorted list: d_table is written once.
 #include "../../include/vocab_ops.h"
 
 #include <hip/hip_runtime.h>
@@ -84,16 +84,89 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(const TE* __restrict__ t
 }
 
 // ---- the sort ----------------------------------------------------------------------
-// Stable radix sort of (word, position) by digits of up to 9 bits.  A wave owns a contiguous run of the keys and walks it 64 at a
-// time: lanes with the same digit find each other by ballots, their rank is the number of lower such lanes, the wave's
-// running count of the digit is in its own row of LDS.  Digits' places: all counts of lower digits, then those of earlier
-// waves (and blocks).
-constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kDigitBits = 9;
-constexpr int kSortOne = 8192;   // keys that one block sorts in LDS
+// Up to kRankMost positions: every position's place is the number of positions that sort ahead of it, counted by brute force over
+// the whole chip: N^2 comparisons of two instructions, 3 us of arithmetic at 6400 and 14 at 16384, and one launch.  (One block that
+// sorts 6400 in its LDS took 34 us.)  A block places 32 positions: a thread compares every 32nd vector of four keys with four of them.
+constexpr int kRankMost = 16384, kRankBlock = 32;
+struct SortDev {
+  const int32_t* ids;
+  int N, V, pad_id;
+  uint32_t *key, *pos;   // the sorted words and positions
+};
+__global__ __launch_bounds__(256) void embed_rank_kernel(SortDev p) {
+  extern __shared__ __align__(16) uint32_t keys[];   // of all positions, to a multiple of 32
+  const int N = p.N, N32 = (N + 31) & ~31, tid = threadIdx.x, n0 = blockIdx.x * kRankBlock;
+  for (int i0 = tid * 4; i0 < N32; i0 += 4096) {   // four vectors of ids together
+    int4 id[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = i0 + u * 1024;
+      if (i + 3 < N) {
+        id[u] = *reinterpret_cast<const int4*>(p.ids + i);
+      } else {
+        id[u].x = i < N ? p.ids[i] : -1;
+        id[u].y = i + 1 < N ? p.ids[i + 1] : -1;
+        id[u].z = i + 2 < N ? p.ids[i + 2] : -1;
+        id[u].w = -1;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = i0 + u * 1024;
+      if (i >= N32) continue;
+      auto key = [&](int w) { return w >= 0 && w < p.V && w != p.pad_id ? (uint32_t)w : (uint32_t)p.V; };
+      *reinterpret_cast<uint4*>(keys + i) = make_uint4(key(id[u].x), key(id[u].y), key(id[u].z), key(id[u].w));
+    }
+  }
+  __syncthreads();
+  const int part = tid & 31, first = n0 + (tid >> 5) * 4;   // this thread's four positions
+  uint32_t mine[4], at_most[4], rank[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    mine[k] = keys[first + k];
+    rank[k] = 0;
+  }
+  auto count = [&](uint4 q) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) rank[k] += (q.x < at_most[k]) + (q.y < at_most[k]) + (q.z < at_most[k]) + (q.w < at_most[k]);
+  };
+  // positions ahead of the block's: equal words sort ahead too
+#pragma unroll
+  for (int k = 0; k < 4; ++k) at_most[k] = mine[k] + 1;
+#pragma unroll 2
+  for (int i = part * 4; i < n0; i += 128) count(*reinterpret_cast<const uint4*>(keys + i));
+#pragma unroll
+  for (int k = 0; k < 4; ++k) at_most[k] = mine[k];
+#pragma unroll 2
+  for (int i = n0 + kRankBlock + part * 4; i < N32; i += 128) count(*reinterpret_cast<const uint4*>(keys + i));
+  {   // the block's own
+    const uint32_t q = keys[n0 + part];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) rank[k] += q < mine[k] + (n0 + part < first + k ? 1u : 0u);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) rank[k] += __shfl_xor(rank[k], o, 64);
+  if (part == 0)
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (first + k < N) {   // (what fills the last block up sorts behind everything)
+        p.key[rank[k]] = mine[k];
+        p.pos[rank[k]] = first + k;
+      }
+}
 
-__device__ __forceinline__ uint64_t same_digit(uint32_t d, int bits, uint64_t in) {
+// More positions: stable radix sort of (word, position) by digits of up to 9 bits.  A wave owns a contiguous run of the keys and
+// walks it 64 at a time: lanes with the same digit find each other by ballots, their rank is the number of lower such lanes, the
+// wave's running count of the digit is in its own row of LDS.  Digits' places: all counts of lower digits, then those of earlier
+// blocks and waves.
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kDigitBits = 9, kBins = 1 << kDigitBits;
+
+__device__ __forceinline__ uint64_t same_digit(uint32_t d, uint64_t in) {
   uint64_t m = in;
-  for (int b = 0; b < bits; ++b) {
+#pragma unroll
+  for (int b = 0; b < kDigitBits; ++b) {
     const uint64_t set = __ballot((d >> b) & 1u);
     m &= (d >> b) & 1u ? set : ~set;
   }
@@ -102,36 +175,6 @@ __device__ __forceinline__ uint64_t same_digit(uint32_t d, int bits, uint64_t in
 __device__ __forceinline__ void lds_in_order() {   // this wave's LDS accesses before it are done before those behind it
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
-}
-// count[wave][digit] of the keys [beg, end) of this wave
-template <typename Key>
-__device__ __forceinline__ void count_digits(Key key, int beg, int end, int shift, int bits, uint32_t* row) {
-  const int lane = threadIdx.x & 63;
-  for (int d = lane; d < 1 << bits; d += 64) row[d] = 0;
-  lds_in_order();
-  for (int i0 = beg; i0 < end; i0 += 64) {
-    const bool in = i0 + lane < end;
-    const uint32_t d = in ? (key(i0 + lane) >> shift) & ((1u << bits) - 1) : 0;
-    const uint64_t m = same_digit(d, bits, __ballot(in));
-    if (in && (m & ((1ull << lane) - 1)) == 0) row[d] += __popcll(m);
-    lds_in_order();
-  }
-}
-// put(place, i) for the keys [beg, end); row: the places of the wave's first key of each digit
-template <typename Key, typename Put>
-__device__ __forceinline__ void place_digits(Key key, Put put, int beg, int end, int shift, int bits, uint32_t* row) {
-  const int lane = threadIdx.x & 63;
-  for (int i0 = beg; i0 < end; i0 += 64) {
-    const bool in = i0 + lane < end;
-    const uint32_t k = in ? key(i0 + lane) : 0, d = (k >> shift) & ((1u << bits) - 1);
-    const uint64_t m = same_digit(d, bits, __ballot(in));
-    const int rank = __popcll(m & ((1ull << lane) - 1));
-    const uint32_t at = row[d] + rank;
-    lds_in_order();
-    if (in) put(at, i0 + lane, k);
-    if (in && rank == 0) row[d] += __popcll(m);
-    lds_in_order();
-  }
 }
 // exclusive prefix of one value per thread over the block; *total: the sum
 __device__ __forceinline__ uint32_t block_prefix(uint32_t v, uint32_t* waves, uint32_t* total) {
@@ -145,178 +188,198 @@ __device__ __forceinline__ uint32_t block_prefix(uint32_t v, uint32_t* waves, ui
   if (lane == 63) waves[wave] = s;
   __syncthreads();
   uint32_t base = 0, sum = 0;
+#pragma unroll
   for (int w = 0; w < kSortWaves; ++w) {
-    if (w < wave) base += waves[w];
-    sum += waves[w];
+    const uint32_t x = waves[w];
+    if (w < wave) base += x;
+    sum += x;
   }
   __syncthreads();
   *total = sum;
   return base + s - v;
 }
-// counts [wave][digit] of one block -> places, digit-major; base: where digit d of this block begins (or null: from 0 on)
-__device__ __forceinline__ void digit_places(uint32_t* count, int bits, const uint32_t* base, int64_t base_step, uint32_t* waves) {
-  const int bins = 1 << bits;
-  uint32_t carry = 0;
-  for (int d0 = 0; d0 < bins; d0 += kSortThreads) {
-    const int d = d0 + threadIdx.x;
-    uint32_t sum = 0, total;
-    if (d < bins)
-      for (int w = 0; w < kSortWaves; ++w) sum += count[w * bins + d];
-    uint32_t at = carry + block_prefix(sum, waves, &total);
-    carry += total;
-    if (d < bins) {
-      if (base) at = base[d * base_step];
-      for (int w = 0; w < kSortWaves; ++w) {
-        const uint32_t c = count[w * bins + d];
-        count[w * bins + d] = at;
-        at += c;
-      }
-    }
-  }
-  __syncthreads();
-}
 
-struct SortDev {
-  const int32_t* ids;
-  int N, V, pad_id;
-  int passes, bits;         // digits and their bits
-  uint32_t *key, *pos;      // the sorted words and positions
-  uint32_t* bitmap;         // a bit per word: some position has it
-  int bitmap_words;
-};
-
-// N <= kSortOne: one block, keys and positions in LDS
-__global__ __launch_bounds__(kSortThreads) void sort_one_kernel(SortDev p) {
-  extern __shared__ __align__(16) unsigned char smem[];
-  const int N = p.N, bins = 1 << p.bits, tid = threadIdx.x, wave = tid >> 6;
-  const int N64 = (N + 63) & ~63;
-  uint32_t* k0 = reinterpret_cast<uint32_t*>(smem);
-  uint32_t* k1 = k0 + N64;
-  uint32_t* count = k1 + N64;
-  uint32_t* waves = count + kSortWaves * bins;
-  uint16_t* p0 = reinterpret_cast<uint16_t*>(waves + kSortWaves);
-  uint16_t* p1 = p0 + N64;
-  for (int i = tid; i < p.bitmap_words; i += kSortThreads) p.bitmap[i] = 0;
-  for (int i = tid; i < N; i += kSortThreads) {
-    k0[i] = word_key(p.ids, i, p.V, p.pad_id);
-    p0[i] = (uint16_t)i;
-  }
-  __threadfence();   // the bitmap's zeros, ahead of the bits below
-  __syncthreads();
-  const int per = ((N + kSortWaves - 1) / kSortWaves + 63) & ~63;
-  const int beg = wave * per < N ? wave * per : N, end = beg + per < N ? beg + per : N;
-  for (int d = 0; d < p.passes; ++d) {
-    count_digits([&](int i) { return k0[i]; }, beg, end, d * p.bits, p.bits, count + wave * bins);
-    __syncthreads();
-    digit_places(count, p.bits, nullptr, 0, waves);
-    place_digits([&](int i) { return k0[i]; },
-                 [&](uint32_t at, int i, uint32_t k) {
-                   k1[at] = k;
-                   p1[at] = p0[i];
-                 },
-                 beg, end, d * p.bits, p.bits, count + wave * bins);
-    __syncthreads();
-    uint32_t* tk = k0; k0 = k1; k1 = tk;
-    uint16_t* tp = p0; p0 = p1; p1 = tp;
-  }
-  for (int i = tid; i < N; i += kSortThreads) {
-    const uint32_t k = k0[i];
-    p.key[i] = k;
-    p.pos[i] = p0[i];
-    if (k < (uint32_t)p.V && (i == 0 || k0[i - 1] != k)) atomicOr(p.bitmap + (k >> 5), 1u << (k & 31));
-  }
-}
-
-// More keys: per digit a count, the places of all digits of all blocks, and the move.  A block's waves own runs of `per` keys.
 struct SortPass {
   const uint32_t *key_in, *pos_in;   // null: the first pass, from the ids
   uint32_t *key_out, *pos_out;
   uint32_t* places;                  // [digit][block]
-  int blocks, per, shift;
+  int blocks, per, shift;            // per: keys of a wave, a multiple of 64
 };
 __device__ __forceinline__ uint32_t pass_key(const SortDev& p, const SortPass& s, int i) {
   return s.key_in ? s.key_in[i] : word_key(p.ids, i, p.V, p.pad_id);
 }
+// f(key, position or index, whether it is one) for the wave's keys, 64 at a time, four loads ahead
+template <typename F>
+__device__ __forceinline__ void wave_keys(const SortDev& p, const SortPass& s, int beg, int end, F f) {
+  const int lane = threadIdx.x & 63;
+  for (int i0 = beg; i0 < end; i0 += 256) {
+    uint32_t k[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = i0 + 64 * u + lane;
+      k[u] = i < end ? pass_key(p, s, i) : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (i0 + 64 * u < end) f(k[u], i0 + 64 * u + lane, i0 + 64 * u + lane < end);
+  }
+}
+// the wave's counts of its digits
+__device__ __forceinline__ void count_digits(const SortDev& p, const SortPass& s, int beg, int end, uint32_t* row) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 0; d < kBins; d += 64) row[d + lane] = 0;
+  lds_in_order();
+  wave_keys(p, s, beg, end, [&](uint32_t key, int, bool in) {
+    const uint32_t d = (key >> s.shift) & (kBins - 1);
+    const uint64_t m = same_digit(d, __ballot(in));
+    if (in && (m & ((1ull << lane) - 1)) == 0) row[d] += __popcll(m);
+    lds_in_order();
+  });
+}
+__device__ __forceinline__ void wave_range(const SortDev& p, const SortPass& s, int& beg, int& end) {
+  const int64_t b0 = ((int64_t)blockIdx.x * kSortWaves + (threadIdx.x >> 6)) * s.per;
+  beg = b0 < p.N ? (int)b0 : p.N;
+  end = b0 + s.per < p.N ? (int)(b0 + s.per) : p.N;
+}
 __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortDev p, SortPass s) {
-  __shared__ uint32_t count[kSortWaves << kDigitBits];
-  const int bins = 1 << p.bits, wave = threadIdx.x >> 6;
-  const int64_t b0 = ((int64_t)blockIdx.x * kSortWaves + wave) * s.per;
-  const int beg = b0 < p.N ? (int)b0 : p.N, end = b0 + s.per < p.N ? (int)(b0 + s.per) : p.N;
-  count_digits([&](int i) { return pass_key(p, s, i); }, beg, end, s.shift, p.bits, count + wave * bins);
+  __shared__ uint32_t count[kSortWaves * kBins];
+  int beg, end;
+  wave_range(p, s, beg, end);
+  count_digits(p, s, beg, end, count + (threadIdx.x >> 6) * kBins);
   __syncthreads();
-  for (int d = threadIdx.x; d < bins; d += kSortThreads) {
+  for (int d = threadIdx.x; d < kBins; d += kSortThreads) {
     uint32_t sum = 0;
-    for (int w = 0; w < kSortWaves; ++w) sum += count[w * bins + d];
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) sum += count[w * kBins + d];
     s.places[(int64_t)d * s.blocks + blockIdx.x] = sum;
   }
 }
-__global__ __launch_bounds__(kSortThreads) void sort_places_kernel(SortDev p, SortPass s) {
+__global__ __launch_bounds__(kSortThreads) void sort_places_kernel(SortPass s) {
   __shared__ uint32_t waves[kSortWaves];
-  if (!s.key_in)
-    for (int i = threadIdx.x; i < p.bitmap_words; i += kSortThreads) p.bitmap[i] = 0;
-  const int total = s.blocks << p.bits;   // <= 2^18
-  const int per = (total + kSortThreads - 1) / kSortThreads, beg = threadIdx.x * per;
-  uint32_t sum = 0, all;
-  for (int i = beg; i < beg + per && i < total; ++i) sum += s.places[i];
-  uint32_t at = block_prefix(sum, waves, &all);
-  for (int i = beg; i < beg + per && i < total; ++i) {
-    const uint32_t c = s.places[i];
-    s.places[i] = at;
-    at += c;
+  const int total = s.blocks * kBins;   // a multiple of 4, 2^18 at most
+  uint32_t carry = 0;
+  for (int i0 = 0; i0 < total; i0 += kSortThreads * 16) {   // sixteen per thread
+    uint4 v[4];
+    uint32_t sum = 0, all;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = i0 + threadIdx.x * 16 + u * 4;
+      v[u] = i < total ? *reinterpret_cast<const uint4*>(s.places + i) : make_uint4(0, 0, 0, 0);
+      sum += v[u].x + v[u].y + v[u].z + v[u].w;
+    }
+    uint32_t at = carry + block_prefix(sum, waves, &all);
+    carry += all;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = i0 + threadIdx.x * 16 + u * 4;
+      uint4 o;
+      o.x = at;
+      o.y = o.x + v[u].x;
+      o.z = o.y + v[u].y;
+      o.w = o.z + v[u].z;
+      at = o.w + v[u].w;
+      if (i < total) *reinterpret_cast<uint4*>(s.places + i) = o;
+    }
   }
 }
 __global__ __launch_bounds__(kSortThreads) void sort_move_kernel(SortDev p, SortPass s) {
-  __shared__ uint32_t count[kSortWaves << kDigitBits];
-  __shared__ uint32_t waves[kSortWaves];
-  const int bins = 1 << p.bits, wave = threadIdx.x >> 6;
-  const int64_t b0 = ((int64_t)blockIdx.x * kSortWaves + wave) * s.per;
-  const int beg = b0 < p.N ? (int)b0 : p.N, end = b0 + s.per < p.N ? (int)(b0 + s.per) : p.N;
-  auto key = [&](int i) { return pass_key(p, s, i); };
-  count_digits(key, beg, end, s.shift, p.bits, count + wave * bins);
+  __shared__ uint32_t count[kSortWaves * kBins];
+  const int lane = threadIdx.x & 63;
+  uint32_t* row = count + (threadIdx.x >> 6) * kBins;
+  int beg, end;
+  wave_range(p, s, beg, end);
+  count_digits(p, s, beg, end, row);
   __syncthreads();
-  digit_places(count, p.bits, s.places + blockIdx.x, s.blocks, waves);
-  place_digits(key,
-               [&](uint32_t at, int i, uint32_t k) {
-                 s.key_out[at] = k;
-                 s.pos_out[at] = s.key_in ? s.pos_in[i] : (uint32_t)i;
-                 if (!s.key_in && k < (uint32_t)p.V) {
-                   const uint32_t bit = 1u << (k & 31);
-                   if (!(__hip_atomic_load(p.bitmap + (k >> 5), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) & bit)) atomicOr(p.bitmap + (k >> 5), bit);
-                 }
-               },
-               beg, end, s.shift, p.bits, count + wave * bins);
+  for (int d = threadIdx.x; d < kBins; d += kSortThreads) {   // counts -> the waves' first places
+    uint32_t at = s.places[(int64_t)d * s.blocks + blockIdx.x];
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+      const uint32_t c = count[w * kBins + d];
+      count[w * kBins + d] = at;
+      at += c;
+    }
+  }
+  __syncthreads();
+  wave_keys(p, s, beg, end, [&](uint32_t key, int i, bool in) {
+    const uint32_t d = (key >> s.shift) & (kBins - 1);
+    const uint64_t m = same_digit(d, __ballot(in));
+    const int rank = __popcll(m & ((1ull << lane) - 1));
+    const uint32_t at = row[d] + rank;
+    lds_in_order();
+    if (in) {
+      s.key_out[at] = key;
+      s.pos_out[at] = s.key_in ? s.pos_in[i] : (uint32_t)i;
+      if (rank == 0) row[d] += __popcll(m);
+    }
+    lds_in_order();
+  });
 }
 
 // ---- the sums ----------------------------------------------------------------------
 struct SumsDev {
-  const uint32_t *key, *pos, *bitmap;
+  const uint32_t *key, *pos;
   const void* dy;
   void* d_table;
   float* edge;       // [piece][2][I]: the part of the word a piece begins within; of the word it ends within
   int N, I, V;
   float scale;
   int accumulate;
-  int piece_blocks, pieces;
-  int zero_rows;     // rows a zeroing block looks at
+  int zero_blocks, pieces;
 };
+constexpr int kZeroRows = 64;   // rows that a zeroing block looks at
 
-// 2^tpp_log threads per piece of L sorted positions (fewer than L rows in flight per thread: RU)
+// first sorted place whose word is >= v, by a wave: 64 probes at a time
+__device__ __forceinline__ int lower_bound_wave(const uint32_t* key, int N, uint32_t v) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, hi = N;
+  while (lo < hi) {
+    const int step = (hi - lo + 63) / 64, at = lo + lane * step;
+    const int below = __popcll(__ballot(at < hi && key[at < hi ? at : lo] < v));
+    if (below == 0) return lo;
+    const int next = lo + below * step;
+    lo += (below - 1) * step + 1;
+    hi = next < hi ? next : hi;
+  }
+  return lo;
+}
+
+// 2^tpp_log threads per piece of L sorted positions, RU rows of it in flight
 template <typename TE, int VEC, int L>
 __global__ __launch_bounds__(256) void embed_sums_kernel(SumsDev p, int tpp_log) {
-  constexpr int RU = L < 16 ? L : 16;
+  constexpr int RU = 16;
   const int I = p.I, lane = threadIdx.x & ((1 << tpp_log) - 1), step = VEC << tpp_log;
   TE* table = reinterpret_cast<TE*>(p.d_table);
-  if ((int)blockIdx.x >= p.piece_blocks) {   // rows of words that no position has
-    const int v0 = ((int)blockIdx.x - p.piece_blocks) * p.zero_rows, rows_at_once = 256 >> tpp_log;
-    const int v1 = v0 + p.zero_rows < p.V ? v0 + p.zero_rows : p.V;
+  if ((int)blockIdx.x < p.zero_blocks) {   // rows of words that no position has
+    __shared__ uint8_t has[kZeroRows];
+    __shared__ int range[2];
+    const int v0 = (int)blockIdx.x * kZeroRows, v1 = v0 + kZeroRows < p.V ? v0 + kZeroRows : p.V, wave = threadIdx.x >> 6;
+    if (wave < 2) {
+      const int at = lower_bound_wave(p.key, p.N, (uint32_t)(wave == 0 ? v0 : v1));
+      if ((threadIdx.x & 63) == 0) range[wave] = at;
+    }
+    __syncthreads();
+    if (threadIdx.x < kZeroRows) {
+      const uint32_t v = v0 + threadIdx.x;
+      int lo = range[0], hi = range[1];
+      const int end = hi;
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (p.key[mid] < v) lo = mid + 1;
+        else hi = mid;
+      }
+      has[threadIdx.x] = lo < end && p.key[lo] == v;
+    }
+    __syncthreads();
+    const int rows_at_once = 256 >> tpp_log;
     const float zero[VEC] = {};
     for (int v = v0 + (threadIdx.x >> tpp_log); v < v1; v += rows_at_once) {
-      if ((p.bitmap[v >> 5] >> (v & 31)) & 1u) continue;
+      if (has[v - v0]) continue;
       for (int c = lane * VEC; c < I; c += step) st_vec<TE, VEC>(table + (int64_t)v * I + c, zero);
     }
     return;
   }
-  const int piece = (int)(((int64_t)blockIdx.x * 256 + threadIdx.x) >> tpp_log);
+  const int piece = (int)(((int64_t)((int)blockIdx.x - p.zero_blocks) * 256 + threadIdx.x) >> tpp_log);
   if (piece >= p.pieces) return;
   const int i0 = piece * L, i1 = i0 + L < p.N ? i0 + L : p.N;
   const uint32_t first = p.key[i0];
@@ -383,11 +446,11 @@ __global__ __launch_bounds__(256) void embed_sums_kernel(SumsDev p, int tpp_log)
 }
 
 // Words that reach over a piece's edge: the block of the piece such a word begins in adds the parts of the pieces behind it up,
-// 64 threads' columns x 16 phases, the phases in order.
+// 64 threads' columns x 4 phases of every fourth piece, eight of them in flight, the phases in order.
 template <typename TE, int VEC, int L>
-__global__ __launch_bounds__(1024) void embed_edges_kernel(SumsDev p) {
-  constexpr int CV = VEC == 1 ? 1 : 4;
-  __shared__ float red[16][64 * CV];
+__global__ __launch_bounds__(256) void embed_edges_kernel(SumsDev p) {
+  constexpr int CV = VEC == 1 ? 1 : 4, PH = 4, U = 8;
+  __shared__ float red[PH][64 * CV];
   const int piece = blockIdx.x, last = piece * L + L - 1;
   if (last + 1 >= p.N) return;
   const uint32_t word = p.key[last];
@@ -398,21 +461,34 @@ __global__ __launch_bounds__(1024) void embed_edges_kernel(SumsDev p) {
 #pragma unroll
   for (int e = 0; e < CV; ++e) acc[e] = 0.f;
   if (c < I) {
-    auto add = [&](int piece_, int which) {
-      const float* q = p.edge + ((int64_t)piece_ * 2 + which) * I + c;
+    const float* edge = p.edge + c;
+    if (phase == 0) {
 #pragma unroll
-      for (int e = 0; e < CV; ++e) acc[e] += q[e];
-    };
-    if (phase == 0) add(piece, 1);
+      for (int e = 0; e < CV; ++e) acc[e] = edge[((int64_t)piece * 2 + 1) * I + e];
+    }
 #pragma unroll 1
-    for (int q = piece + 1 + phase; q < p.pieces && p.key[q * L] == word; q += 16) add(q, 0);
+    for (int q0 = piece + 1 + phase; q0 < p.pieces; q0 += PH * U) {
+      bool in[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) in[u] = q0 + PH * u < p.pieces && p.key[(q0 + PH * u) * L] == word;
+      if (!in[0]) break;
+      float x[U][CV];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < CV; ++e) x[u][e] = in[u] ? edge[(int64_t)(q0 + PH * u) * 2 * I + e] : 0.f;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < CV; ++e) acc[e] += x[u][e];
+    }
   }
 #pragma unroll
   for (int e = 0; e < CV; ++e) red[phase][col * CV + e] = acc[e];
   __syncthreads();
   if (phase != 0 || c >= I) return;
-#pragma unroll 1
-  for (int q = 1; q < 16; ++q)
+#pragma unroll
+  for (int q = 1; q < PH; ++q)
 #pragma unroll
     for (int e = 0; e < CV; ++e) acc[e] += red[q][col * CV + e];
   TE* out = reinterpret_cast<TE*>(p.d_table) + (int64_t)word * I + c;
@@ -434,9 +510,9 @@ int log2_up(int64_t x) {
 }
 
 struct EmbedLayout {
-  int L, pieces, passes, bits, blocks, per, bitmap_words;
-  bool one;
-  size_t key, pos, key2, pos2, places, bitmap, edge, total;
+  int L, pieces, passes, blocks, per;
+  bool rank;
+  size_t key, pos, key2, pos2, places, edge, total;
 };
 
 bool embed_ok(const vo_embed* s) {
@@ -452,17 +528,14 @@ bool embed_types(const vo_embed* s) {
 EmbedLayout embed_layout(const vo_embed* s) {
   EmbedLayout L;
   const int N = s->N;
-  L.one = N <= kSortOne;
-  const int key_bits = log2_up((int64_t)s->V + 1);   // words and the key of padding
-  L.passes = (key_bits + kDigitBits - 1) / kDigitBits;
-  L.bits = (key_bits + L.passes - 1) / L.passes;
+  L.rank = N <= kRankMost;
+  L.passes = (log2_up((int64_t)s->V + 1) + kDigitBits - 1) / kDigitBits;   // words and the key of padding
   L.blocks = (N + 4095) / 4096;
   if (L.blocks > 512) L.blocks = 512;
   L.per = ((N + L.blocks - 1) / L.blocks + kSortWaves - 1) / kSortWaves;
   L.per = (L.per + 63) & ~63;
   L.L = N <= 16384 ? 16 : 32;
   L.pieces = (N + L.L - 1) / L.L;
-  L.bitmap_words = (s->V + 31) / 32;
   size_t off = 0;
   auto take = [&](size_t bytes) {
     const size_t o = off;
@@ -471,12 +544,11 @@ EmbedLayout embed_layout(const vo_embed* s) {
   };
   L.key = take((size_t)N * 4);
   L.pos = take((size_t)N * 4);
-  L.bitmap = take((size_t)L.bitmap_words * 4);
   L.key2 = L.pos2 = L.places = 0;
-  if (!L.one) {
+  if (!L.rank) {
     L.key2 = take((size_t)N * 4);
     L.pos2 = take((size_t)N * 4);
-    L.places = take(((size_t)L.blocks << L.bits) * 4);
+    L.places = take((size_t)L.blocks * kBins * 4);
   }
   L.edge = take((size_t)L.pieces * 2 * s->I * 4);
   L.total = off;
@@ -510,19 +582,14 @@ hipError_t launch_sort(const vo_embed* s, const EmbedLayout& L, const int32_t* i
   p.N = s->N;
   p.V = s->V;
   p.pad_id = s->pad_id;
-  p.passes = L.passes;
-  p.bits = L.bits;
   p.key = u32(L.key);
   p.pos = u32(L.pos);
-  p.bitmap = u32(L.bitmap);
-  p.bitmap_words = L.bitmap_words;
-  if (L.one) {
-    const size_t n64 = ((size_t)s->N + 63) & ~(size_t)63;
-    const int smem = (int)(n64 * 12 + ((size_t)kSortWaves << L.bits) * 4 + kSortWaves * 4);
+  if (L.rank) {
     static LdsLimit limit;
-    const hipError_t e = limit.raise(reinterpret_cast<const void*>(sort_one_kernel), 160 * 1024);
+    const hipError_t e = limit.raise(reinterpret_cast<const void*>(embed_rank_kernel), kRankMost * 4);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(sort_one_kernel, dim3(1), dim3(kSortThreads), smem, st, p);
+    const int blocks = (s->N + kRankBlock - 1) / kRankBlock;
+    hipLaunchKernelGGL(embed_rank_kernel, dim3(blocks), dim3(256), (size_t)blocks * kRankBlock * 4, st, p);
     return hipGetLastError();
   }
   // the last pass writes key / pos
@@ -539,9 +606,9 @@ hipError_t launch_sort(const vo_embed* s, const EmbedLayout& L, const int32_t* i
   for (int d = 0; d < L.passes; ++d) {
     q.key_out = ka;
     q.pos_out = pa;
-    q.shift = d * L.bits;
+    q.shift = d * kDigitBits;
     hipLaunchKernelGGL(sort_count_kernel, dim3(L.blocks), dim3(kSortThreads), 0, st, p, q);
-    hipLaunchKernelGGL(sort_places_kernel, dim3(1), dim3(kSortThreads), 0, st, p, q);
+    hipLaunchKernelGGL(sort_places_kernel, dim3(1), dim3(kSortThreads), 0, st, q);
     hipLaunchKernelGGL(sort_move_kernel, dim3(L.blocks), dim3(kSortThreads), 0, st, p, q);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -556,16 +623,13 @@ hipError_t launch_sort(const vo_embed* s, const EmbedLayout& L, const int32_t* i
 template <typename TE, int VEC, int PL>
 hipError_t launch_sums(SumsDev p, hipStream_t st) {
   const int tpp = row_threads_log((p.I + VEC - 1) / VEC), per_block = 256 >> tpp;
-  p.piece_blocks = (p.pieces + per_block - 1) / per_block;
-  // (at most 2^16 rows of 2^16 columns per block and 2^20 blocks: 2^28 rows need 256 rows each at least)
-  p.zero_rows = 16 * per_block;
-  while ((p.V + p.zero_rows - 1) / p.zero_rows > 1 << 20) p.zero_rows *= 2;
-  const int zero_blocks = p.accumulate ? 0 : (p.V + p.zero_rows - 1) / p.zero_rows;
-  hipLaunchKernelGGL((embed_sums_kernel<TE, VEC, PL>), dim3(p.piece_blocks + zero_blocks), dim3(256), 0, st, p, tpp);
+  p.zero_blocks = p.accumulate ? 0 : (p.V + kZeroRows - 1) / kZeroRows;
+  const int piece_blocks = (p.pieces + per_block - 1) / per_block;
+  hipLaunchKernelGGL((embed_sums_kernel<TE, VEC, PL>), dim3(p.zero_blocks + piece_blocks), dim3(256), 0, st, p, tpp);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.pieces < 2) return e;
   constexpr int CV = VEC == 1 ? 1 : 4;
-  hipLaunchKernelGGL((embed_edges_kernel<TE, VEC, PL>), dim3(p.pieces, (p.I + 64 * CV - 1) / (64 * CV)), dim3(1024), 0, st, p);
+  hipLaunchKernelGGL((embed_edges_kernel<TE, VEC, PL>), dim3(p.pieces, (p.I + 64 * CV - 1) / (64 * CV)), dim3(256), 0, st, p);
   return hipGetLastError();
 }
 template <typename TE, int VEC> hipError_t launch_sums_any(const SumsDev& p, int L, hipStream_t st) {
@@ -622,7 +686,6 @@ extern "C" as_status vocab_embed_bwd(const vo_embed* shape, const int32_t* ids, 
   SumsDev p{};
   p.key = reinterpret_cast<const uint32_t*>(ws + L.key);
   p.pos = reinterpret_cast<const uint32_t*>(ws + L.pos);
-  p.bitmap = reinterpret_cast<const uint32_t*>(ws + L.bitmap);
   p.dy = dy;
   p.d_table = d_table;
   p.edge = reinterpret_cast<float*>(ws + L.edge);

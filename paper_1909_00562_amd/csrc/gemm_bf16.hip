@@ -28,7 +28,7 @@
 #include "gemm.h"
 #include "gemm_dev.h"
 #include "lds_limit.h"
-#include "vocab.h"
+#include "vocab_wave_dev.h"
 
 #include <type_traits>
 
@@ -485,8 +485,8 @@ constexpr int PP_SMEM = PP_EPI_OFF + 8 * 4096;
 // the smaller tile moves fewer accumulator bytes per flop); in the kernel it gains 4 % with both operands
 // reduction-contiguous and loses 2 % when one operand needs the transposing reads, so the launcher picks it for the
 // former only.
-template <bool AKC, bool BKC, bool OUT_BF16, bool VEC, bool DROP, bool MI16>
-__global__ __launch_bounds__(512) void gemm_bf16_pp_kernel(GemmDev p, int work_total) {
+template <bool AKC, bool BKC, bool OUT_BF16, bool VEC, bool DROP, bool MI16, typename VOC = NoVocabOut>
+__global__ __launch_bounds__(512) void gemm_bf16_pp_kernel(GemmDev p, int work_total, typename VOC::Args voc) {
   constexpr int BM = 256, BN = 256, WGN = 4;
   constexpr int WM = 128, WN = 64;
   constexpr int TM = MI16 ? 8 : 4, TN = MI16 ? 4 : 2;   // MFMA tiles per wave tile
@@ -680,8 +680,17 @@ __global__ __launch_bounds__(512) void gemm_bf16_pp_kernel(GemmDev p, int work_t
       }
     }
     // item done: write it out while the next item's first tile is already in flight
-    gemm_epilogue<TM, TN, OUT_BF16, VEC, DROP, 16, 64, MI16>(p, Mv, acc, smem + PP_EPI_OFF + wave * 4096, lane,
-                                                       it.m0 + wm * WM, it.n0 + wn * WN, it.batch, it.z);
+    if constexpr (VOC::kOn) {
+      static_assert(MI16, "the accumulators' layout");
+      float* region = reinterpret_cast<float*>(smem + PP_EPI_OFF + wave * 4096);
+      auto stage = [&](int i) { stage_round<true, 4, 16, 64>(region, acc, i, lane); };
+      const int row0 = it.m0 + wm * WM, col0 = it.n0 + wn * WN;
+      if constexpr (VOC::kTerms == 0) vocab_wave_stats<VOC::kTeach>(voc, acc, region, stage, lane, row0, Mv - row0, col0, p.N);
+      else vocab_wave_grad<VOC::kTeach, VOC::kTerms>(voc, acc, region, stage, lane, row0, Mv - row0, col0, p.N);
+    } else {
+      gemm_epilogue<TM, TN, OUT_BF16, VEC, DROP, 16, 64, MI16>(p, Mv, acc, smem + PP_EPI_OFF + wave * 4096, lane,
+                                                         it.m0 + wm * WM, it.n0 + wn * WN, it.batch, it.z);
+    }
     zero_acc();
   }
 }
@@ -923,6 +932,12 @@ __global__ __launch_bounds__(512) void gemm_bf16_ring_kernel(
       }
     }
     // item done: write it out while the next item's first sub-tiles are already in flight
+    if (p.alpha != 1.f) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] *= p.alpha;
+    }
     void* C_apart = nullptr;
     if constexpr (APART) C_apart = apart.C[it.batch];
     gemm_epilogue<TM, TN, OUT_BF16, VEC, DROP, 16, 64, false, APART>(p, Mv, acc, smem + RING_EPI_OFF + wave * 4096, lane,
@@ -966,7 +981,16 @@ static hipError_t launch_pp(const GemmDev& d, int batch, hipStream_t st) {
   // persistent: one block per CU (a multiple of the 8 XCDs), each walking its share of the work items
   const int work_total = d.tiles_m * d.tiles_n * batch * d.splits;
   const int blocks = pp_grid_blocks(work_total);
-  hipLaunchKernelGGL(kfn, dim3(blocks), dim3(512), smem, st, d, work_total);
+  hipLaunchKernelGGL(kfn, dim3(blocks), dim3(512), smem, st, d, work_total, NoVocabOut::Args{});
+  return hipGetLastError();
+}
+template <typename VOC> static hipError_t launch_pp_vocab(const GemmDev& d, const VocabEpi& e, hipStream_t st) {
+  auto kfn = gemm_bf16_pp_kernel<true, true, true, true, false, true, VOC>;
+  static LdsLimit limit;
+  const hipError_t rc = limit.raise(reinterpret_cast<const void*>(kfn), PP_SMEM);
+  if (rc != hipSuccess) return rc;
+  const int work_total = d.tiles_m * d.tiles_n;
+  hipLaunchKernelGGL(kfn, dim3(pp_grid_blocks(work_total)), dim3(512), PP_SMEM, st, d, work_total, e);
   return hipGetLastError();
 }
 
@@ -1017,6 +1041,8 @@ static hipError_t gemm_describe(const GemmArgs& g, GemmTile tile, GemmDev& d) {
   d.K = g.K[0];
   d.nseg = g.nseg;
   d.past_caches = g.past_caches;
+  if (g.alpha != 1.f && tile != kTile64 && tile != kTile128 && (!big_tile || g.a_kc || g.b_kc)) return hipErrorInvalidValue;
+  d.alpha = g.alpha;
   d.M = g.M;
   d.N = g.N;
   d.C = g.C;
@@ -1081,14 +1107,16 @@ static hipError_t gemm_describe(const GemmArgs& g, GemmTile tile, GemmDev& d) {
   return hipSuccess;
 }
 
-int vocab_tile_edge(GemmTile tile) { return tile == kTile64 ? 64 : 128; }
-GemmTile vocab_tile(int N, int V, int K) { return gemm_plan(N, V, K, 1, true, false).tile == kTile64 ? kTile64 : kTile128; }
 hipError_t launch_gemm_vocab(const GemmArgs& g, GemmTile tile, const VocabEpi& v, int terms, bool teacher, bool arg, hipStream_t st) {
   if (!g.a_kc || !g.b_kc || g.splits != 1 || g.batch != 1 || g.K_dev || g.C || g.bias) return hipErrorInvalidValue;
   GemmDev d;
   const hipError_t e = gemm_describe(g, tile, d);
   if (e != hipSuccess) return e;
-  return launch_gemm_bf16_vocab_tile(d, tile, v, terms, teacher, arg, st);
+  if (tile != kTile256) return launch_gemm_bf16_vocab_tile(d, tile, v, terms, teacher, arg, st);
+  if (arg) return hipErrorInvalidValue;
+  if (terms == 1) return teacher ? launch_pp_vocab<VocabOut<true, false, 1>>(d, v, st) : launch_pp_vocab<VocabOut<false, false, 1>>(d, v, st);
+  if (terms == 3) return teacher ? launch_pp_vocab<VocabOut<true, false, 3>>(d, v, st) : launch_pp_vocab<VocabOut<false, false, 3>>(d, v, st);
+  return teacher ? launch_pp_vocab<VocabOut<true, false, 0>>(d, v, st) : launch_pp_vocab<VocabOut<false, false, 0>>(d, v, st);
 }
 
 hipError_t launch_gemm_bf16_together(const GemmArgs* g, const GemmTile* tile, int n, const DbReduce* sums, hipStream_t st) {

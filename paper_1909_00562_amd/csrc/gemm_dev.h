@@ -16,6 +16,7 @@ struct GemmDev {
   int M, N;
   int n_out;   // columns the vector write-out covers: N, or N rounded up to 4 where C's rows have padding
   int past_caches;
+  float alpha;
   void* C;
   uint16_t* C_lo;
   float* C_dact;

@@ -172,7 +172,7 @@ static hipError_t launch_f32_oriented(GemmDevF& d, int batch, bool avec, bool bv
 
 // checks of a product and its description for the kernels; avec, bvec: 16-byte loads of the operand
 static hipError_t f32_describe(const GemmArgs& g, GemmDevF& d, bool& avec, bool& bvec) {
-  if (g.M < 1 || g.N < 1 || g.batch < 1 || g.splits < 1 || g.c_bf16 || g.nseg < 1 || g.K[g.nseg - 1] < 1) return hipErrorInvalidValue;
+  if (g.alpha != 1.f || g.M < 1 || g.N < 1 || g.batch < 1 || g.splits < 1 || g.c_bf16 || g.nseg < 1 || g.K[g.nseg - 1] < 1) return hipErrorInvalidValue;
   if (g.splits > 1 && (g.K[1] != 0 || g.partial == nullptr)) return hipErrorInvalidValue;
   if (g.splits > 1 && (g.C_dact || g.drop_thr)) return hipErrorInvalidValue;
   if (g.drop_thr && g.batch != 1) return hipErrorInvalidValue;

@@ -216,16 +216,7 @@ template <int BM> __device__ __forceinline__ TileStat gs_stats(const float* row,
 
 // Block `id` of a launch's tiles of all batches and splits; dynamic LDS: NST * 2 * 32 TW * ROWB bytes.  (p by value: by reference the
 // instances take five registers more and 182 x 51130 x 128 18.7 us for 17.2.)
-// VOC: the vocabulary's own write-out in place of C's (VocabOut), with its arguments.
-struct NoVocabOut {
-  static constexpr bool kOn = false;
-  struct Args {};
-};
-template <bool TEACH, bool ARG, int TERMS> struct VocabOut {
-  static constexpr bool kOn = true, kTeach = TEACH, kArg = ARG;
-  static constexpr int kTerms = TERMS;
-  using Args = VocabEpi;
-};
+// VOC: the vocabulary's own write-out in place of C's (VocabOut).
 template <int TW, bool AKC, bool BKC, int NST, bool LACED, TileExtra EXTRA, typename VOC = NoVocabOut>
 __device__ __forceinline__ void gemm_bf16_tile_block(GemmDev p, int out_bf16, int id, typename VOC::Args voc = {}) {
   extern __shared__ __align__(1024) unsigned char smem[];
@@ -305,6 +296,8 @@ __device__ __forceinline__ void gemm_bf16_tile_block(GemmDev p, int out_bf16, in
     for (int j = 0; j < TW; ++j)
 #pragma unroll
       for (int r = 0; r < 4; ++r) acc[i][j][r] = 0.f;
+  VocabRow vrow = {};   // what the vocabulary's write-out needs to know of a row, a thread per row: on its way during the reduction
+  if constexpr (VOC::kOn) vrow = vocab_row<VOC::kTeach, (VOC::kTerms > 0)>(voc, m0 + tid, tid < BM && m0 + tid < Mv);
 
   // Two sets of fragments, one per half (32 reduction elements) of a tile.  LACED: the reads of a half run between the matrix
   // instructions of the half before it; else all reads of a tile come first and the other blocks of the compute unit run
@@ -413,6 +406,9 @@ __device__ __forceinline__ void gemm_bf16_tile_block(GemmDev p, int out_bf16, in
       const int col = n0 + wn + 16 * j + c;
       vbias[j] = col < p.N ? vocab_bias(voc, col) : 0.f;
     }
+    VocabRow* rows = reinterpret_cast<VocabRow*>(stage + 64 * LD);
+    static_assert(NST * STAGE >= 64 * LD * 4 + BM * (int)sizeof(VocabRow), "staging of the rows");
+    if (tid < BM) rows[tid] = vrow;
     f32x4_t cs = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
     for (int half = 0; half < BM / 64; ++half) {   // 64 rows at a time
@@ -426,8 +422,8 @@ __device__ __forceinline__ void gemm_bf16_tile_block(GemmDev p, int out_bf16, in
       }
       __syncthreads();
       const int row0 = m0 + half * 64, left = Mv - row0 < 64 ? Mv - row0 : 64;
-      if constexpr (VOC::kTerms == 0) vocab_stats64<BM, VOC::kTeach, VOC::kArg>(voc, stage, LD, row0, left, n0, p.N - n0);
-      else vocab_grad64<BM, VOC::kTeach, VOC::kTerms>(voc, stage, LD, row0, left, n0, p.N - n0, cs);
+      if constexpr (VOC::kTerms == 0) vocab_stats64<BM, VOC::kTeach, VOC::kArg>(voc, stage, LD, rows + half * 64, row0, left, n0, p.N - n0);
+      else vocab_grad64<BM, VOC::kTeach, VOC::kTerms>(voc, stage, LD, rows + half * 64, row0, left, n0, p.N - n0, cs);
       __syncthreads();
     }
     if (VOC::kTerms > 0 && voc.col_sums) {         // of the tile's rows, in a fixed order
@@ -442,6 +438,12 @@ __device__ __forceinline__ void gemm_bf16_tile_block(GemmDev p, int out_bf16, in
       }
     }
     return;
+  }
+  if (p.alpha != 1.f) {
+#pragma unroll
+    for (int i = 0; i < TW; ++i)
+#pragma unroll
+      for (int j = 0; j < TW; ++j) acc[i][j] *= p.alpha;
   }
   constexpr int VPR = BM / 4;                 // groups of four columns per row
   const int col = n0 + (tid % VPR) * 4;

@@ -36,18 +36,20 @@ struct VocabEpi {
   // gradient
   const float* lse;           // [R]
   const float* lse_tau;       // [R], +inf where a row has no entries
-  float g, c2;                // grad_scale; teacher's scale * tau
+  float a1, a2;               // dl / alpha = a1 (q - onehot) + a2 (q at temperature - p); without a teacher a1 is 1
   uint16_t* dl;               // planes of [R, ldd]
   int64_t ldd, plane;
   float* col_sums;            // [tile row][ld_sums], or null
   int64_t ld_sums;
 };
 
-// Columns of the statistics' tiles, rows of the column sums' tiles
-int vocab_tile_edge(GemmTile tile);
-GemmTile vocab_tile(int N, int V, int K);
+// Columns of a part of a row's statistics, rows of a part of the column sums
+inline int vocab_stat_cols(GemmTile t) { return t == kTile128 ? 128 : 64; }    // 256: a wave's 64 columns
+inline int vocab_sum_rows(GemmTile t) { return t == kTile64 ? 64 : 128; }      // 256: a wave's 128 rows
+constexpr int kVocabRowPad = 256;   // y, lse, lse_tau are read in whole tiles: their allocations are multiples of this
 
-// terms: planes of dl (1 or 3), or 0: statistics; arg: stat_idx is wanted.  g: A, B contiguous, M_dev, no split, no C.
+// terms: planes of dl (1 or 3), or 0: statistics; arg: stat_idx is wanted (64 x 64 and 128 x 128).  g: A, B contiguous, M_dev, no
+// split, no C.
 hipError_t launch_gemm_vocab(const GemmArgs& g, GemmTile tile, const VocabEpi& e, int terms, bool teacher, bool arg, hipStream_t st);
 
 // ---- rows of words -------------------------------------------------------------------
@@ -110,10 +112,18 @@ struct VocabFinish {
 hipError_t launch_vocab_finish(const VocabFinish& p, hipStream_t st);
 
 // ---- gradients on their way out ----------------------------------------------------------
-// db[v] = sum over the tile rows of col_sums, in order
-hipError_t launch_vocab_col_sums(const float* col_sums, int64_t ld, int tile_rows, int edge, const int32_t* n_act, int V, void* db,
-                                 bool bf16, hipStream_t st);
-// dh[n] = src[row_pos[n]], zeros at padding
-hipError_t launch_vocab_scatter(const float* src, const int32_t* row_pos, int N, int H, int64_t ld, void* dh, bool bf16, hipStream_t st);
+// dh[n] = alpha src[row_pos[n]], zeros at padding; db[v] = alpha sums[v] (db: optional)
+struct VocabOutGrads {
+  const float* src;
+  const int32_t* row_pos;
+  int N, H;
+  int64_t ld;
+  void* dh;
+  const float* sums;
+  int V;
+  void* db;
+  float alpha;
+};
+hipError_t launch_vocab_out_grads(const VocabOutGrads& p, bool bf16, hipStream_t st);
 
 }  // namespace asx

@@ -9,7 +9,8 @@
 //
 // Float gradients: dl as the sum of three bf16 terms (24 bits of mantissa), each in a plane of its own, whose products with the
 // other operand are reduction segments of one launch.  fp32 storage: h and W as three terms too, the six products of terms whose
-// ranks add up to two at most; what is left out is 2^-24 of a product.  The planes of W are made a piece at a time.
+// ranks add up to two at most; what is left out is 2^-24 of a product.  The planes of W are made once, or a
+// piece at a time where all of them would take more than a piece may.
 #include "../../include/vocab_ops.h"
 
 #include <hip/hip_runtime.h>
@@ -18,6 +19,7 @@
 
 #include "common.h"
 #include "gemm.h"
+#include "kernels.h"
 #include "status.h"
 #include "vocab.h"
 
@@ -28,9 +30,11 @@ constexpr size_t kAlignV = 256;
 size_t upv(size_t x) { return (x + kAlignV - 1) / kAlignV * kAlignV; }
 int64_t round_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 
-// What a piece of the vocabulary may take: dl of the backward pass, or the statistics or terms of W of the forward one.  It is
-// read back at once, so that most of it is found in the 256 MB memory-side cache.
-constexpr int64_t kPieceBytes = (int64_t)128 << 20;
+// What a piece of the vocabulary may take: dl of the backward pass, or the statistics or terms of W of the forward one.  Larger
+// pieces fill the rounds of the compute units better, and the sums of dh are read and written once per piece: 64 / 128 / 256 / 512 MiB,
+// forward and backward, 6400 x 1024 x 32000 bf16 - / 1355 / 1190 / 1139 us, 16384 x 2048 x 128000 - / 22.7 / 22.3 / 21.8 ms, 2257 x 1000
+// x 32003 float gradients 1113 / 1088 / 1072 / 1161 us.
+constexpr int64_t kPieceBytes = (int64_t)256 << 20;
 constexpr int64_t kPieceColumns = 256;   // pieces are multiples of it
 
 struct VocabLayout {
@@ -39,15 +43,15 @@ struct VocabLayout {
   int64_t ldH, fwd_cols, bwd_cols, ldd;
   int strips, groups;
   GemmTile t_fwd, t_bwd;
-  int e_fwd, e_bwd;                       // edges of their tiles
   GemmPlan p_dw, p_dh;
-  bool dh_dyn;
+  bool dh_dyn = false;
   // kept from the forward to the backward pass
   size_t rows, row_pos, y, n_act, ticket, hc, lse, lse_tau, at_word, loss_ws, distill_ws, run;
   size_t runs, ent, ent_p, ent_l, place, p_log_p, seen;
   // one area for the pieces of either pass
   size_t stat, stat_tau, stat_idx, w_fwd;
-  size_t dl, w_bwd, col_sums, dh_acc, partial;
+  bool w_kept;                            // terms of all of W, made once for both passes
+  size_t dl, w_bwd, col_sums, db_acc, dh_acc, partial_dw, partial_dh;
   size_t total;
 };
 
@@ -81,12 +85,29 @@ int pair_count(int a_terms, int b_terms) {
   return term_pairs(a_terms, b_terms, pairs);
 }
 
+// no split may be empty (the last piece has fewer reduction tiles than the others)
+int whole_splits(int tiles, int splits) {
+  if (splits > tiles) splits = tiles;
+  const int per = (tiles + splits - 1) / splits;
+  return (tiles + per - 1) / per;
+}
+
 int64_t piece_columns(int64_t V, int64_t bytes_per_column) {
   int64_t c = kPieceBytes / bytes_per_column / kPieceColumns * kPieceColumns;
   if (c < kPieceColumns) c = kPieceColumns;
   if (c > (1 << 20)) c = 1 << 20;
   const int64_t pieces = (V + c - 1) / c;
   return round_up((V + pieces - 1) / pieces, kPieceColumns);   // of the same size
+}
+
+// tiles of the product that makes the logits
+GemmTile logits_tile(int64_t N, int64_t cols, int64_t ldH, int terms) {
+  const GemmTile t = gemm_plan((int)N, (int)cols, (int)ldH * pair_count(terms, terms), 1, true, false).tile;
+  // The 256 x 256 kernel's write-out runs with its matrix pipe idle, which the 128 x 128 one's second block on a compute unit hides:
+  // two rounds of tiles and more are the larger kernel's.  us, forward and backward, 128 / 256: 480 words x 512 x 16000 fp32 288
+  // / 396, 622 x 512 x 32003 forward 60.6 / 78.8; 1580 x 1000 x 32003 1080 / 1037, 4480 x 1024 x 32000 1264 / 1216.
+  if (t == kTile64) return t;
+  return ((N + 255) / 256) * ((cols + 255) / 256) >= 512 ? kTile256 : kTile128;
 }
 
 VocabLayout vocab_layout(const vo_shape* s, const vo_teacher* t) {
@@ -101,31 +122,43 @@ VocabLayout vocab_layout(const vo_shape* s, const vo_teacher* t) {
   L.groups = (int)((N + kVocabGroup - 1) / kVocabGroup);
   const int64_t w_col = L.f32 ? L.ldH * 6 : 0;   // bytes of a column's terms of W
   // forward
-  L.t_fwd = vocab_tile((int)N, (int)(V < (1 << 20) ? V : (1 << 20)), (int)L.ldH * pair_count(L.h_terms, L.h_terms));
-  L.e_fwd = vocab_tile_edge(L.t_fwd);
-  const int64_t stat_col = (N * 16 + L.e_fwd - 1) / L.e_fwd;
+  L.t_fwd = logits_tile(N, V, L.ldH, L.h_terms);
+  const int64_t stat_col = (N * 16 + 63) / 64;
   L.fwd_cols = piece_columns(V, stat_col > w_col ? stat_col : w_col);
   // backward
   const int64_t dl_col = N * 2 * L.dl_terms;
   L.bwd_cols = piece_columns(V, dl_col > w_col ? dl_col : w_col);
   L.ldd = round_up(L.bwd_cols < V ? L.bwd_cols : V, 8);
-  L.t_bwd = vocab_tile((int)N, (int)L.ldd, (int)L.ldH * pair_count(L.h_terms, L.h_terms));
-  L.e_bwd = vocab_tile_edge(L.t_bwd);
+  L.t_bwd = logits_tile(N, L.ldd, L.ldH, L.h_terms);
+  // The two products of a piece in one launch of 128 x 128 tiles, the blocks of dh first, whose reductions are the longer ones: as
+  // launches of their own, each is some part of a round of the compute units too long.  dh is split where one of its blocks
+  // would otherwise take longer than all blocks' share of a compute unit's two places.
   const int n_dw = pair_count(L.dl_terms, L.h_terms);
-  // (fp32 widths that are no whole vectors cannot be combined: no split of dW there)
-  L.p_dw = gemm_plan((int)L.ldd, (int)H, (int)(n_dw == 1 ? N : n_dw * round_up(N, 64)), 1, true, H % 8 == 0, n_dw > 1, true);
-  L.p_dh = gemm_plan((int)N, (int)L.ldH, (int)(n_dw == 1 ? L.ldd : n_dw * round_up(L.ldd, 64)), 1, true, true, n_dw > 1, true);
-  // one segment in 256 x 256 tiles: the split is chosen on the device, from the rows that there are
-  L.dh_dyn = false;
-  if (n_dw == 1 && L.p_dh.tile == kTile256) {
-    int64_t most = kPieceBytes / (N * L.ldH * 4);
-    if (most > 8) most = 8;
-    if (most >= 2) {
+  const int64_t k_dw = n_dw * ((N + 63) / 64), k_dh = n_dw * ((L.ldd + 63) / 64);
+  if (N > 256) {
+    const int64_t b_dw = ((L.ldd + 127) / 128) * ((H + 127) / 128), b_dh = ((N + 127) / 128) * ((L.ldH + 127) / 128);
+    int64_t share = (b_dw * k_dw + b_dh * k_dh + 511) / 512;
+    if (share < 8) share = 8;
+    int64_t splits = (k_dh + share - 1) / share;
+    if (splits > 32) splits = 32;
+    L.p_dw = {kTile128, 1};
+    L.p_dh = {kTile128, whole_splits((int)k_dh, (int)splits)};
+    // One term and whole rounds of 256 x 256 tiles of dW: those kernels, one behind the other, dh with a split that the device
+    // chooses from the rows that there are.  6400 x 1024 x 16128 (252 tiles) 1222 / 1190 us for the whole call, 16384 x 2048 x 8192
+    // (256) 23.1 / 22.3 ms; half a round, 6400 x 1024 x 8192, 1355 / 1486.
+    const int64_t tiles = ((L.ldd + 255) / 256) * ((H + 255) / 256), rounds = (tiles + 255) / 256;
+    const int64_t most = kPieceBytes / (N * L.ldH * 4);
+    if (n_dw == 1 && N >= 2048 && tiles * 8 >= rounds * 256 * 7 && most >= 2) {
+      L.p_dw = {kTile256, 1};
+      L.p_dh = {kTile256, most < 4 ? (int)most : 4};
       L.dh_dyn = true;
-      L.p_dh.splits = (int)most;
-    } else {
-      L.p_dh.splits = 1;
     }
+  } else {
+    // (fp32 widths that are no whole vectors cannot be combined: no split of dW there)
+    L.p_dw = gemm_plan((int)L.ldd, (int)H, (int)k_dw * 64, 1, true, H % 8 == 0, n_dw > 1, true);
+    L.p_dh = gemm_plan((int)N, (int)L.ldH, (int)k_dh * 64, 1, true, true, n_dw > 1, true);
+    if (L.p_dw.tile == kTile256) L.p_dw = {kTile128, 1};
+    if (L.p_dh.tile == kTile256) L.p_dh = {kTile128, 1};
   }
   size_t off = 0;
   auto take = [&](size_t bytes) {
@@ -133,20 +166,21 @@ VocabLayout vocab_layout(const vo_shape* s, const vo_teacher* t) {
     off += upv(bytes);
     return o;
   };
+  const int64_t Np = round_up(N, kVocabRowPad);
   L.rows = take(N * 4);
   L.row_pos = take(N * 4);
-  L.y = take(N * 4);
+  L.y = take(Np * 4);
   L.n_act = take(16);
   L.ticket = take(16);
   L.hc = take((size_t)L.h_terms * N * L.ldH * 2);
-  L.lse = take(N * 4);
+  L.lse = take(Np * 4);
   L.at_word = take(N * 4);
   L.loss_ws = take(N * 4);
   L.run = take(L.fwd_cols < V ? N * 16 : 0);
   L.lse_tau = L.distill_ws = L.runs = L.ent = L.ent_p = L.ent_l = L.place = L.p_log_p = L.seen = 0;
   if (t) {
     const size_t entries = (size_t)L.groups * kVocabGroup * t->K;
-    L.lse_tau = take(N * 4);
+    L.lse_tau = take(Np * 4);
     L.distill_ws = take(N * 4);
     L.runs = take((size_t)L.groups * (L.strips + 1) * 4);
     L.ent = take(entries * 4);
@@ -156,30 +190,25 @@ VocabLayout vocab_layout(const vo_shape* s, const vo_teacher* t) {
     L.p_log_p = take(N * 4);
     L.seen = take(N * 4);
   }
+  L.w_kept = L.f32 && V * w_col <= kPieceBytes;
+  L.w_fwd = L.w_bwd = take(L.w_kept ? (size_t)V * w_col : 0);
   const size_t area = off;
-  const int64_t parts = (L.fwd_cols + L.e_fwd - 1) / L.e_fwd;
+  const int64_t parts = L.fwd_cols / 64;
   L.stat = take((size_t)parts * N * 8);
   L.stat_tau = take(t ? (size_t)parts * N * 4 : 0);
   L.stat_idx = take((size_t)parts * N * 4);
-  L.w_fwd = take((size_t)L.fwd_cols * w_col);
+  if (!L.w_kept) L.w_fwd = take((size_t)L.fwd_cols * w_col);
   size_t end = off;
   off = area;
   L.dl = take((size_t)L.dl_terms * N * L.ldd * 2);
-  L.w_bwd = take((size_t)L.bwd_cols * w_col);
-  L.col_sums = take((size_t)((N + L.e_bwd - 1) / L.e_bwd) * L.ldd * 4);
+  if (!L.w_kept) L.w_bwd = take((size_t)L.bwd_cols * w_col);
+  L.col_sums = take((size_t)((N + 63) / 64) * L.ldd * 4);
+  L.db_acc = take((size_t)V * 4);
   L.dh_acc = take((size_t)N * L.ldH * 4);
-  const size_t pw = gemm_partial_bytes((int)L.ldd, (int)H, 1, L.p_dw.splits), ph = gemm_partial_bytes((int)N, (int)L.ldH, 1, L.p_dh.splits);
-  L.partial = take(pw > ph ? pw : ph);
+  L.partial_dw = take(gemm_partial_bytes((int)L.ldd, (int)H, 1, L.p_dw.splits));
+  L.partial_dh = take(gemm_partial_bytes((int)N, (int)L.ldH, 1, L.p_dh.splits));
   L.total = off > end ? off : end;
   return L;
-}
-
-// the last piece may have fewer reduction tiles than the others, and no split may be empty
-int whole_splits(int segments, int k, int splits) {
-  const int tiles = segments * ((k + 63) / 64);
-  if (splits > tiles) splits = tiles;
-  const int per = (tiles + splits - 1) / splits;
-  return (tiles + per - 1) / per;
 }
 
 bool al16v(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -324,9 +353,12 @@ as_status forward(const vo_shape* s, const vo_teacher* t, const void* h, const v
   }
   for (int64_t v0 = 0; v0 < s->V; v0 += L.fwd_cols) {
     const int cols = (int)(s->V - v0 < L.fwd_cols ? s->V - v0 : L.fwd_cols);
-    uint16_t* planes = w.at<uint16_t>(L.w_fwd);
-    const int64_t plane = L.fwd_cols * L.ldH;
-    if (L.f32) {
+    uint16_t* planes = w.at<uint16_t>(L.w_fwd) + (L.w_kept ? v0 * L.ldH : 0);
+    const int64_t plane = (L.w_kept ? s->V : L.fwd_cols) * L.ldH;
+    if (L.f32 && L.w_kept && v0 == 0) {
+      e = launch_vocab_terms(reinterpret_cast<const float*>(W), s->V, s->H, planes, L.ldH, plane, st);
+      if (e != hipSuccess) return hip_fail(e, "terms of W");
+    } else if (L.f32 && !L.w_kept) {
       e = launch_vocab_terms(reinterpret_cast<const float*>(W) + v0 * s->H, cols, s->H, planes, L.ldH, plane, st);
       if (e != hipSuccess) return hip_fail(e, "terms of W");
     }
@@ -345,9 +377,10 @@ as_status forward(const vo_shape* s, const vo_teacher* t, const void* h, const v
     v.ent = w.at<uint32_t>(L.ent);
     v.ent_l = w.at<float>(L.ent_l);
     v.strips = L.strips;
-    e = launch_gemm_vocab(logits_product(s, L, w, W, planes, plane, v0, cols), L.t_fwd, v, 0, t != nullptr, argmax != nullptr, st);
+    const GemmTile tile = argmax && L.t_fwd == kTile256 ? kTile128 : L.t_fwd;
+    e = launch_gemm_vocab(logits_product(s, L, w, W, planes, plane, v0, cols), tile, v, 0, t != nullptr, argmax != nullptr, st);
     if (e != hipSuccess) return hip_fail(e, "statistics of the logits");
-    f.parts = (cols + L.e_fwd - 1) / L.e_fwd;
+    f.parts = (cols + vocab_stat_cols(tile) - 1) / vocab_stat_cols(tile);
     f.first = v0 == 0;
     f.last = v0 + L.fwd_cols >= s->V;
     e = launch_vocab_finish(f, st);
@@ -368,15 +401,22 @@ as_status backward(const vo_shape* s, const vo_teacher* t, const void* W, const 
   const Ws w{reinterpret_cast<unsigned char*>(workspace)};
   const int N = s->N, H = s->H;
   const int32_t* n_act = w.at<int32_t>(L.n_act);
-  const int64_t h_plane = (int64_t)N * L.ldH, dl_plane = (int64_t)N * L.ldd, w_plane = L.bwd_cols * L.ldH;
-  uint16_t *dl = w.at<uint16_t>(L.dl), *planes = w.at<uint16_t>(L.w_bwd);
+  const int64_t h_plane = (int64_t)N * L.ldH, dl_plane = (int64_t)N * L.ldd;
+  const int64_t w_plane = (L.w_kept ? s->V : L.bwd_cols) * L.ldH;
+  uint16_t* dl = w.at<uint16_t>(L.dl);
   const size_t ge = L.g_bf16 ? 2 : 4;
   int pairs[kMaxSeg][2];
   const int n = term_pairs(L.dl_terms, L.h_terms, pairs);
+  // dl is kept relative to the larger of its two factors: with 1 / n_tok in it, the rounding of -1 / n_tok to bf16 would be that of
+  // all targets at once (2^-9 of dh; 12288 words 0.26 % off for 0.18)
+  const float c2 = t ? t->scale * t->temperature : 0.f;
+  float alpha = std::fabs(s->grad_scale) >= std::fabs(c2) ? s->grad_scale : c2;
+  if (alpha == 0.f) alpha = 1.f;
   hipError_t e;
   for (int64_t v0 = 0; v0 < s->V; v0 += L.bwd_cols) {
     const int cols = (int)(s->V - v0 < L.bwd_cols ? s->V - v0 : L.bwd_cols);
-    if (L.f32) {
+    uint16_t* planes = w.at<uint16_t>(L.w_bwd) + (L.w_kept ? v0 * L.ldH : 0);
+    if (L.f32 && !L.w_kept) {
       e = launch_vocab_terms(reinterpret_cast<const float*>(W) + v0 * H, cols, H, planes, L.ldH, w_plane, st);
       if (e != hipSuccess) return hip_fail(e, "terms of W");
     }
@@ -392,54 +432,64 @@ as_status backward(const vo_shape* s, const vo_teacher* t, const void* W, const 
     v.strips = L.strips;
     v.lse = w.at<float>(L.lse);
     v.lse_tau = w.at<float>(L.lse_tau);
-    v.g = s->grad_scale;
-    v.c2 = t ? t->scale * t->temperature : 0.f;
+    v.a1 = s->grad_scale / alpha;
+    v.a2 = c2 / alpha;
     v.dl = dl;
     v.ldd = L.ldd;
     v.plane = dl_plane;
     v.col_sums = db ? w.at<float>(L.col_sums) : nullptr;
-    v.ld_sums = L.ldd;
+    v.ld_sums = cols;
     e = launch_gemm_vocab(logits_product(s, L, w, W, planes, w_plane, v0, cols), L.t_bwd, v, L.dl_terms, t != nullptr, false, st);
     if (e != hipSuccess) return hip_fail(e, "derivative of the logits");
-    if (db) {
-      e = launch_vocab_col_sums(v.col_sums, L.ldd, (N + L.e_bwd - 1) / L.e_bwd, L.e_bwd, n_act, cols,
-                                reinterpret_cast<unsigned char*>(db) + v0 * ge, L.g_bf16, st);
-      if (e != hipSuccess) return hip_fail(e, "db");
-    }
-    GemmArgs gw;   // dW_piece = dl^T h
-    for (int i = 0; i < n; ++i)
-      gw.seg(dl + pairs[i][0] * dl_plane, L.ldd, 0, w.at<uint16_t>(L.hc) + pairs[i][1] * h_plane, L.ldH, 0, N);
-    gw.a_kc = gw.b_kc = false;
-    gw.M = cols;
-    gw.N = H;
-    gw.C = reinterpret_cast<unsigned char*>(dW) + (size_t)v0 * H * ge;
-    gw.ldc = H;
-    gw.c_bf16 = L.g_bf16;
-    gw.K_dev = n_act;
-    gw.splits = L.p_dw.splits;
-    gw.partial = w.at<float>(L.partial);
-    e = launch_gemm(gw, true, L.p_dw.tile, st);
-    if (e != hipSuccess) return hip_fail(e, "dW");
-    GemmArgs gh;   // dh += dl W_piece
+    GemmArgs g[2];   // dW_piece = dl^T h, dh += dl W_piece
     for (int i = 0; i < n; ++i) {
+      const uint16_t* a = dl + pairs[i][0] * dl_plane;
       const uint16_t* wb = L.f32 ? planes + pairs[i][1] * w_plane : reinterpret_cast<const uint16_t*>(W) + v0 * H;
-      gh.seg(dl + pairs[i][0] * dl_plane, L.ldd, 0, wb, L.ldH, 0, cols);
+      g[0].seg(a, L.ldd, 0, w.at<uint16_t>(L.hc) + pairs[i][1] * h_plane, L.ldH, 0, N);
+      g[1].seg(a, L.ldd, 0, wb, L.ldH, 0, cols);
     }
-    gh.b_kc = false;
-    gh.M = N;
-    gh.N = (int)L.ldH;
-    gh.C = w.at<float>(L.dh_acc);
-    gh.ldc = L.ldH;
-    gh.accumulate = v0 > 0;
-    gh.M_dev = n_act;
-    gh.splits = L.dh_dyn ? L.p_dh.splits : whole_splits(n, cols, L.p_dh.splits);
-    gh.dyn_split = L.dh_dyn;
-    gh.partial = w.at<float>(L.partial);
-    e = launch_gemm(gh, true, L.p_dh.tile, st);
-    if (e != hipSuccess) return hip_fail(e, "dh");
+    g[0].a_kc = g[0].b_kc = g[1].b_kc = false;
+    g[0].M = cols;
+    g[0].N = H;
+    g[0].C = reinterpret_cast<unsigned char*>(dW) + (size_t)v0 * H * ge;
+    g[0].ldc = H;
+    g[0].c_bf16 = L.g_bf16;
+    g[0].K_dev = n_act;
+    g[0].alpha = alpha;
+    g[0].splits = L.p_dw.splits;
+    g[0].partial = w.at<float>(L.partial_dw);
+    g[1].M = N;
+    g[1].N = (int)L.ldH;
+    g[1].C = w.at<float>(L.dh_acc);
+    g[1].ldc = L.ldH;
+    g[1].accumulate = v0 > 0;
+    g[1].M_dev = n_act;
+    g[1].splits = L.dh_dyn ? L.p_dh.splits : whole_splits(n * ((cols + 63) / 64), L.p_dh.splits);
+    g[1].dyn_split = L.dh_dyn;
+    g[1].partial = w.at<float>(L.partial_dh);
+    const GemmTile tiles[2] = {L.p_dw.tile, L.p_dh.tile};
+    const int sum_rows = vocab_sum_rows(L.t_bwd);
+    const DbReduce sums = {v.col_sums, (N + sum_rows - 1) / sum_rows, cols, w.at<float>(L.db_acc) + v0, n_act, sum_rows};
+    e = launch_gemm_joint(g, tiles, 2, true, st, db ? &sums : nullptr);
+    if (e == hipErrorNotSupported) {
+      e = db ? launch_db_reduce(sums, st) : hipSuccess;
+      for (int i = 0; i < 2 && e == hipSuccess; ++i) e = launch_gemm(g[i], true, tiles[i], st);
+    }
+    if (e != hipSuccess) return hip_fail(e, "dW and dh");
   }
-  e = launch_vocab_scatter(w.at<float>(L.dh_acc), w.at<int32_t>(L.row_pos), N, H, L.ldH, dh, L.g_bf16, st);
-  if (e != hipSuccess) return hip_fail(e, "dh to its rows");
+  VocabOutGrads o{};
+  o.src = w.at<float>(L.dh_acc);
+  o.row_pos = w.at<int32_t>(L.row_pos);
+  o.N = N;
+  o.H = H;
+  o.ld = L.ldH;
+  o.dh = dh;
+  o.sums = w.at<float>(L.db_acc);
+  o.V = s->V;
+  o.db = db;
+  o.alpha = alpha;
+  e = launch_vocab_out_grads(o, L.g_bf16, st);
+  if (e != hipSuccess) return hip_fail(e, "dh and db");
   return AS_OK;
 }
 

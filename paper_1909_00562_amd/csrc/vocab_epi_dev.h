@@ -5,6 +5,17 @@
 
 namespace asx {
 
+// What sets an instance of a product kernel apart: C's write-out, or the vocabulary's, and its arguments.
+struct NoVocabOut {
+  static constexpr bool kOn = false;
+  struct Args {};
+};
+template <bool TEACH, bool ARG, int TERMS> struct VocabOut {
+  static constexpr bool kOn = true, kTeach = TEACH, kArg = ARG;
+  static constexpr int kTerms = TERMS;
+  using Args = VocabEpi;
+};
+
 __device__ __forceinline__ float vocab_bias(const VocabEpi& e, int col) {
   if (!e.bias) return 0.f;
   return e.bias_f32 ? reinterpret_cast<const float*>(e.bias)[col] : bf16_bits_to_f32(reinterpret_cast<const uint16_t*>(e.bias)[col]);
@@ -30,44 +41,70 @@ __device__ __forceinline__ uint32_t bf16_term(float& x) {
   return b >> 16;
 }
 
+struct VocabRow {
+  int y;            // its word
+  float c, ct;      // gradient: lse, and at temperature
+};
+template <bool TEACH, bool GRAD> __device__ __forceinline__ VocabRow vocab_row(const VocabEpi& e, int row, bool in) {
+  VocabRow r = {-1, 0.f, 0.f};
+  if (in) {
+    r.y = e.y[row];
+    if constexpr (GRAD) r.c = e.lse[row];
+    if constexpr (GRAD && TEACH) r.ct = e.lse_tau[row];
+  }
+  return r;
+}
+
 // Statistics of the 64 staged rows, four lanes per row (every fourth vector of four columns each); row0: the first row,
 // left: rows inside, ncols: columns inside.
 template <int BM, bool TEACH, bool ARG>
-__device__ __forceinline__ void vocab_stats64(const VocabEpi& e, const float* stage, int LD, int row0, int left, int n0, int ncols) {
+__device__ __forceinline__ void vocab_stats64(const VocabEpi& e, const float* stage, int LD, const VocabRow* rows, int row0, int left,
+                                              int n0, int ncols) {
   constexpr int NV = BM / 16, XOR1 = 0xB1, XOR2 = 0x4E;
+  constexpr float L2E = 1.4426950408889634f;
   const int tid = threadIdx.x, r = tid >> 2, part = tid & 3;
   const float* row = stage + r * LD;
   f32x4_t x[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) x[i] = *reinterpret_cast<const f32x4_t*>(row + (part + 4 * i) * 4);
+  if (ncols < BM) {   // the vocabulary's last tile
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        if ((part + 4 * i) * 4 + c >= ncols) x[i][c] = -INFINITY;
+  }
   float m = -INFINITY;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    x[i] = *reinterpret_cast<const f32x4_t*>(row + (part + 4 * i) * 4);
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-      if ((part + 4 * i) * 4 + c >= ncols) x[i][c] = -INFINITY;
     m = fmaxf(fmaxf(m, x[i][0]), x[i][1]);
     m = fmaxf(fmaxf(m, x[i][2]), x[i][3]);
   }
   m = fmaxf(m, dpp_f<XOR1>(m));
   m = fmaxf(m, dpp_f<XOR2>(m));
-  const float mb = m > -INFINITY ? m : 0.f;
-  float s0 = 0.f, s1 = 0.f, t0 = 0.f;
+  // (the rounding of m log2 e is common to the row's part: |m| 2^-24 on its share of the log-sum-exp)
+  const float mb = m > -INFINITY ? -m * L2E : 0.f, scale_t = L2E * e.inv_tau, mbt = m > -INFINITY ? -m * scale_t : 0.f;
+  float s0 = 0.f, s1 = 0.f, t0 = 0.f, t1 = 0.f;
   int idx = 0x7fffffff;
 #pragma unroll
   for (int i = NV - 1; i >= 0; --i)
 #pragma unroll
     for (int c = 3; c >= 0; --c) {
-      const float d = (x[i][c] - mb) * 1.4426950408889634f;
-      const float p = __builtin_amdgcn_exp2f(d);
+      const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i][c], L2E, mb));
       if (c & 1) s1 += p;
       else s0 += p;
-      if constexpr (TEACH) t0 += __builtin_amdgcn_exp2f(d * e.inv_tau);
+      if constexpr (TEACH) {
+        const float q = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i][c], scale_t, mbt));
+        if (c & 1) t1 += q;
+        else t0 += q;
+      }
       if constexpr (ARG) idx = x[i][c] == m ? (part + 4 * i) * 4 + c : idx;
     }
   float s = s0 + s1;
   s += dpp_f<XOR1>(s);
   s += dpp_f<XOR2>(s);
   if constexpr (TEACH) {
+    t0 += t1;
     t0 += dpp_f<XOR1>(t0);
     t0 += dpp_f<XOR2>(t0);
   }
@@ -82,7 +119,7 @@ __device__ __forceinline__ void vocab_stats64(const VocabEpi& e, const float* st
     e.stat[at] = make_float2(m, s);
     if constexpr (TEACH) e.stat_tau[at] = t0;
     if constexpr (ARG) e.stat_idx[at] = idx < ncols && m > -INFINITY ? e.v0 + n0 + idx : 0x7fffffff;
-    const int c = e.y[row0 + r] - e.v0 - n0;
+    const int c = rows[r].y - e.v0 - n0;
     if (c >= 0 && c < BM && c < ncols) e.at_word[row0 + r] = row[c];
   }
   if constexpr (TEACH) {   // a wave per group of 16 rows
@@ -98,21 +135,39 @@ __device__ __forceinline__ void vocab_stats64(const VocabEpi& e, const float* st
   }
 }
 
-// dl of the 64 staged rows; cs: the thread's column sums.  256 threads, BM / 4 per row.
+// dl / alpha of the 64 staged rows; cs: the thread's column sums.  256 threads, BM / 4 per row.
+// One term (bf16): one fused multiply-add and one v_exp_f32 per probability, |l| 2^-23 off, 2^-8 is rounded away.  Three: vocab_exp.
 template <int BM, bool TEACH, int TERMS>
-__device__ __forceinline__ void vocab_grad64(const VocabEpi& e, float* stage, int LD, int row0, int left, int n0, int ncols, f32x4_t& cs) {
-  constexpr int VPR = BM / 4, RP = 256 / VPR;
+__device__ __forceinline__ void vocab_grad64(const VocabEpi& e, float* stage, int LD, const VocabRow* rows, int row0, int left, int n0,
+                                             int ncols, f32x4_t& cs) {
+  constexpr int VPR = BM / 4, RP = 256 / VPR, NR = 64 / RP;
+  constexpr float L2E = 1.4426950408889634f;
   const int tid = threadIdx.x, cv = (tid % VPR) * 4, col = n0 + cv;
+  const float scale_t = L2E * e.inv_tau;
   auto dl4 = [&](int r) {
-    f32x4_t v = *reinterpret_cast<const f32x4_t*>(stage + r * LD + cv);
-    const float lse = e.lse[row0 + r], lt = TEACH ? e.lse_tau[row0 + r] : 0.f;
-    const int at = e.y[row0 + r] - e.v0 - col;
+    const f32x4_t l = *reinterpret_cast<const f32x4_t*>(stage + r * LD + cv);
+    const VocabRow q = rows[r];
+    f32x4_t v;
+    const float c1 = -q.c * L2E, ct = -q.ct * L2E;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-      const float l = v[c];
-      float d = e.g * ((TERMS == 1 ? __expf(l - lse) : vocab_exp(l - lse)) - (c == at ? 1.f : 0.f));
-      if constexpr (TEACH) d += e.c2 * (TERMS == 1 ? __expf(l * e.inv_tau - lt) : vocab_exp(l * e.inv_tau - lt));
-      v[c] = cv + c < ncols ? d : 0.f;
+      const float lc = l[c];
+      float d = TERMS == 1 ? __builtin_amdgcn_exp2f(__builtin_fmaf(lc, L2E, c1)) : vocab_exp(lc - q.c);
+      if constexpr (TEACH) {
+        const float dt = TERMS == 1 ? __builtin_amdgcn_exp2f(__builtin_fmaf(lc, scale_t, ct)) : vocab_exp(lc * e.inv_tau - q.ct);
+        d = e.a1 * d + e.a2 * dt;
+      }
+      v[c] = d;
+    }
+    const int at = q.y - e.v0 - col;
+    if ((uint32_t)at < 4u) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        if (c == at) v[c] = TEACH ? v[c] - e.a1 : v[c] - 1.f;
+    }
+    if (ncols < BM) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c) v[c] = cv + c < ncols ? v[c] : 0.f;
     }
     return v;
   };
@@ -120,34 +175,29 @@ __device__ __forceinline__ void vocab_grad64(const VocabEpi& e, float* stage, in
     cs += v;
     if (col >= e.ldd) return;
     uint16_t* out = e.dl + (int64_t)(row0 + r) * e.ldd + col;
+    if constexpr (TERMS == 1) {
+      *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+    } else {
+      float x[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
-    for (int t = 0; t < TERMS; ++t) {
-      uint2 q;
-      if constexpr (TERMS == 1) {
-        q = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
-      } else {
-        float x[4] = {v[0], v[1], v[2], v[3]};
+      for (int t = 0; t < TERMS; ++t) {
         uint32_t b[4];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          b[c] = bf16_term(x[c]);
-          v[c] = x[c];
-        }
-        q = make_uint2(b[0] | (b[1] << 16), b[2] | (b[3] << 16));
+        for (int c = 0; c < 4; ++c) b[c] = bf16_term(x[c]);
+        *reinterpret_cast<uint2*>(out + t * e.plane) = make_uint2(b[0] | (b[1] << 16), b[2] | (b[3] << 16));
       }
-      *reinterpret_cast<uint2*>(out + t * e.plane) = q;
     }
   };
   if constexpr (!TEACH) {
 #pragma unroll
-    for (int u = 0; u < 64 / RP; ++u) {
+    for (int u = 0; u < NR; ++u) {
       const int r = u * RP + tid / VPR;
       if (r < left) put(r, dl4(r));
     }
   } else {
     // the dense part back into the staged rows, the entries' probabilities off it (each place comes once), then out
 #pragma unroll
-    for (int u = 0; u < 64 / RP; ++u) {
+    for (int u = 0; u < NR; ++u) {
       const int r = u * RP + tid / VPR;
       if (r < left) *reinterpret_cast<f32x4_t*>(stage + r * LD + cv) = dl4(r);
     }
@@ -158,12 +208,12 @@ __device__ __forceinline__ void vocab_grad64(const VocabEpi& e, float* stage, in
       const int s0i = (e.v0 + n0) / kVocabStrip, s1i = s0i + BM / kVocabStrip < e.strips ? s0i + BM / kVocabStrip : e.strips;
       for (int i = runs[s0i] + (tid & 63); i < runs[s1i]; i += 64) {
         const uint32_t k = e.ent[i];
-        stage[(w * kVocabGroup + (k & 15)) * LD + (int)(k >> 4) - e.v0 - n0] -= e.c2 * e.ent_p[i];
+        stage[(w * kVocabGroup + (k & 15)) * LD + (int)(k >> 4) - e.v0 - n0] -= e.a2 * e.ent_p[i];
       }
     }
     __syncthreads();
 #pragma unroll
-    for (int u = 0; u < 64 / RP; ++u) {
+    for (int u = 0; u < NR; ++u) {
       const int r = u * RP + tid / VPR;
       if (r < left) put(r, *reinterpret_cast<const f32x4_t*>(stage + r * LD + cv));
     }

@@ -24,9 +24,16 @@ __global__ __launch_bounds__(256) void vocab_rows_kernel(VocabRows p) {
   __shared__ int part[4], place[kRowsBlock];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n0 = blockIdx.x * kRowsBlock;
   int before = 0;
-  for (int i = tid * 4; i < n0; i += 1024) {
-    const int4 y = *reinterpret_cast<const int4*>(p.targets + i);
-    before += is_word(y.x, p.V, p.pad_id) + is_word(y.y, p.V, p.pad_id) + is_word(y.z, p.V, p.pad_id) + is_word(y.w, p.V, p.pad_id);
+  for (int i0 = 0; i0 < n0; i0 += 8192) {   // eight loads together
+    int4 y[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int i = i0 + u * 1024 + tid * 4;
+      y[u] = i < n0 ? *reinterpret_cast<const int4*>(p.targets + i) : make_int4(-1, -1, -1, -1);
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      before += is_word(y[u].x, p.V, p.pad_id) + is_word(y[u].y, p.V, p.pad_id) + is_word(y[u].z, p.V, p.pad_id) + is_word(y[u].w, p.V, p.pad_id);
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) before += __shfl_xor(before, o, 64);
@@ -56,20 +63,50 @@ __global__ __launch_bounds__(256) void vocab_rows_kernel(VocabRows p) {
     if (lane == 0 && blockIdx.x == 0) *p.ticket = 0;
   }
   __syncthreads();
-#pragma unroll 1
-  for (int j = wave; j < kRowsBlock; j += 4) {
-    const int r = place[j];
-    if (r < 0) continue;
-    uint16_t* out = p.hc + (int64_t)r * p.ldH;
-    if (!p.f32) {   // H % 8 == 0
-      const uint16_t* src = reinterpret_cast<const uint16_t*>(p.h) + (int64_t)(n0 + j) * p.H;
-      for (int c = lane * 8; c < p.H; c += 512) *reinterpret_cast<uint4*>(out + c) = *reinterpret_cast<const uint4*>(src + c);
-    } else {
-      const float* src = reinterpret_cast<const float*>(p.h) + (int64_t)(n0 + j) * p.H;
-      for (int c = lane; c < p.ldH; c += 64) {
-        float x = c < p.H ? src[c] : 0.f;
+  // the rows themselves, a wave each, its four rows' loads together
+  if (!p.f32) {   // H % 8 == 0
+    for (int c = lane * 8; c < p.H; c += 512) {
+      uint4 x[kRowsBlock / 4];
 #pragma unroll
-        for (int t = 0; t < 3; ++t) out[t * p.plane + c] = (uint16_t)bf16_term(x);
+      for (int k = 0; k < kRowsBlock / 4; ++k) {
+        const int j = wave + 4 * k;
+        x[k] = place[j] < 0 ? make_uint4(0, 0, 0, 0) : *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(p.h) + (int64_t)(n0 + j) * p.H + c);
+      }
+#pragma unroll
+      for (int k = 0; k < kRowsBlock / 4; ++k) {
+        const int r = place[wave + 4 * k];
+        if (r >= 0) *reinterpret_cast<uint4*>(p.hc + (int64_t)r * p.ldH + c) = x[k];
+      }
+    }
+  } else {
+    const bool vec = p.H % 4 == 0;
+    for (int c = lane * 4; c < p.ldH; c += 256) {
+      float x[kRowsBlock / 4][4];
+#pragma unroll
+      for (int k = 0; k < kRowsBlock / 4; ++k) {
+        const int j = wave + 4 * k;
+        const float* src = reinterpret_cast<const float*>(p.h) + (int64_t)(n0 + j) * p.H + c;
+        const bool in = place[j] >= 0;
+        if (vec && c < p.H) {
+          const f32x4_t v = in ? *reinterpret_cast<const f32x4_t*>(src) : f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[k][e] = v[e];
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[k][e] = in && c + e < p.H ? src[e] : 0.f;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < kRowsBlock / 4; ++k) {
+        const int r = place[wave + 4 * k];
+        if (r < 0) continue;
+#pragma unroll
+        for (int t = 0; t < 3; ++t) {
+          uint32_t b[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) b[e] = bf16_term(x[k][e]);
+          *reinterpret_cast<uint2*>(p.hc + t * p.plane + (int64_t)r * p.ldH + c) = make_uint2(b[0] | (b[1] << 16), b[2] | (b[3] << 16));
+        }
       }
     }
   }
@@ -168,14 +205,16 @@ __global__ __launch_bounds__(1024) void vocab_teacher_kernel(VocabTeacher p) {
     first[j] = in[j];
     P[j] = 0.f;
   }
+#pragma unroll 4
   for (int k = 0; k < K; ++k) {
     const int o = ids[k];
     const float q = prob[k];
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
-      if (!in[j] || o != id[j]) continue;
-      P[j] += q;
-      first[j] = first[j] && k >= lane + 64 * j;
+      if (64 * j >= K) continue;
+      const bool same = in[j] && o == id[j];
+      P[j] += same ? q : 0.f;
+      first[j] = first[j] && !(same && k < lane + 64 * j);
     }
   }
 #pragma unroll
@@ -238,13 +277,14 @@ __device__ __forceinline__ Stat join(const Stat& a, const Stat& b, float inv_tau
   return r;
 }
 
-// RPB rows per block, 1024 / RPB threads per row that take every (1024 / RPB)-th tile; losses of the rows, and by the block that is
-// through last their sums in double, in a fixed order.
-template <int RPB>
+// RPB rows per block, 1024 / RPB threads per row that take every (1024 / RPB)-th part, eight at a time: their loads together, one
+// maximum, and sums against it; losses of the rows, and by the block that is through last their sums in double, in a fixed order.
+template <int RPB, bool TEACH, bool ARG>
 __global__ __launch_bounds__(1024) void vocab_finish_kernel(VocabFinish p) {
-  constexpr int PH = 1024 / RPB;
+  constexpr int PH = 1024 / RPB, U = 8;
+  constexpr float L2E = 1.4426950408889634f;
   __shared__ Stat part[1024];
-  __shared__ float sh_lse[RPB], sh_tau[RPB];
+  __shared__ float sh_tau[RPB];
   __shared__ double sd[2][16];
   __shared__ int last_block;
   const int R = row_count(p.n_act, p.N), tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -252,11 +292,33 @@ __global__ __launch_bounds__(1024) void vocab_finish_kernel(VocabFinish p) {
   if (row0 < R) {
     Stat st{-INFINITY, 0.f, 0.f, INT_MAX};
     if (r < R) {
-#pragma unroll 4
-      for (int i = phase; i < p.parts; i += PH) {
-        const int64_t at = (int64_t)i * p.ldr + r;
-        const float2 ms = p.stat[at];
-        st = join(st, Stat{ms.x, ms.y, p.stat_tau ? p.stat_tau[at] : 0.f, p.stat_idx ? p.stat_idx[at] : INT_MAX}, p.inv_tau);
+      for (int i0 = phase; i0 < p.parts; i0 += U * PH) {
+        float2 ms[U];
+        float t[U];
+        int idx[U];
+        Stat g{-INFINITY, 0.f, 0.f, INT_MAX};
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int i = i0 + u * PH;
+          const int64_t at = (int64_t)(i < p.parts ? i : i0) * p.ldr + r;
+          ms[u] = p.stat[at];
+          t[u] = TEACH ? p.stat_tau[at] : 0.f;
+          idx[u] = ARG ? p.stat_idx[at] : INT_MAX;
+          if (i >= p.parts) {
+            ms[u] = make_float2(-INFINITY, 0.f);
+            t[u] = 0.f;
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) g.m = fmaxf(g.m, ms[u].x);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const float d = ms[u].x == g.m ? 0.f : (ms[u].x - g.m) * L2E;
+          g.s += ms[u].y * __builtin_amdgcn_exp2f(d);
+          if constexpr (TEACH) g.t += t[u] * __builtin_amdgcn_exp2f(d * p.inv_tau);
+          if constexpr (ARG) g.idx = ms[u].x == g.m && idx[u] < g.idx ? idx[u] : g.idx;
+        }
+        st = join(st, g, p.inv_tau);
       }
     }
     part[tid] = st;
@@ -281,14 +343,14 @@ __global__ __launch_bounds__(1024) void vocab_finish_kernel(VocabFinish p) {
         __hip_atomic_store(p.loss_ws + r, loss, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         if (p.tok_loss) p.tok_loss[n] = loss;
         if (p.argmax) p.argmax[n] = st.idx == INT_MAX ? 0 : st.idx;
-        if (p.stat_tau) {
+        if constexpr (TEACH) {
           const float lt = p.seen[r] ? st.m * p.inv_tau + logf(st.t) : INFINITY;
           p.lse_tau[r] = lt;
           sh_tau[tid] = lt;
         }
       }
     }
-    if (p.last && p.stat_tau) {   // a wave per row
+    if (TEACH && p.last) {   // a wave per row
       __syncthreads();
 #pragma unroll 1
       for (int j = wave; j < RPB && row0 + j < R; j += 16) {
@@ -322,7 +384,7 @@ __global__ __launch_bounds__(1024) void vocab_finish_kernel(VocabFinish p) {
   double a = 0.0, b = 0.0;
   for (int i = tid; i < R; i += 1024) {
     a += (double)__hip_atomic_load(p.loss_ws + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (p.stat_tau) b += (double)__hip_atomic_load(p.distill_ws + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if constexpr (TEACH) b += (double)__hip_atomic_load(p.distill_ws + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
@@ -342,44 +404,30 @@ __global__ __launch_bounds__(1024) void vocab_finish_kernel(VocabFinish p) {
     }
     *p.loss_sum = (float)a;
     *p.n_tok = R;
-    if (p.stat_tau) *p.distill_sum = (float)b;
+    if constexpr (TEACH) *p.distill_sum = (float)b;
   }
 }
 
 // ---- gradients on their way out ------------------------------------------------------------------
-// 64 columns x 16 phases, the phases added in order
-template <typename TE>
-__global__ __launch_bounds__(1024) void vocab_col_sums_kernel(const float* __restrict__ part, int64_t ld, int tile_rows, int edge,
-                                                              const int32_t* __restrict__ n_act, int V, TE* __restrict__ db) {
-  __shared__ float red[16][64];
-  const int c = threadIdx.x & 63, phase = threadIdx.x >> 6, v = blockIdx.x * 64 + c;
-  const int used = (row_count(n_act, INT_MAX) + edge - 1) / edge, rows = used < tile_rows ? used : tile_rows;
-  float s = 0.f;
-  if (v < V)
-#pragma unroll 4
-    for (int r = phase; r < rows; r += 16) s += part[(int64_t)r * ld + v];
-  red[phase][c] = s;
-  __syncthreads();
-  if (phase != 0 || v >= V) return;
-#pragma unroll
-  for (int q = 1; q < 16; ++q) s += red[q][c];
-  st_elem<TE>(db, v, s);
-}
-
+// 2^tpr_log threads per row of dh; further blocks for db, 256 words each
 template <typename TE, int VEC>
-__global__ __launch_bounds__(256) void vocab_scatter_kernel(const float* __restrict__ src, const int32_t* __restrict__ row_pos, int N,
-                                                            int H, int64_t ld, TE* __restrict__ dh, int tpr_log) {
+__global__ __launch_bounds__(256) void vocab_out_grads_kernel(VocabOutGrads p, int tpr_log, int row_blocks) {
+  if ((int)blockIdx.x >= row_blocks) {
+    const int v = ((int)blockIdx.x - row_blocks) * 256 + threadIdx.x;
+    if (v < p.V) st_elem<TE>(reinterpret_cast<TE*>(p.db), v, p.alpha * p.sums[v]);
+    return;
+  }
   const int64_t n = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> tpr_log;
-  if (n >= N) return;
-  const int lane = threadIdx.x & ((1 << tpr_log) - 1), r = row_pos[n];
-  const float* from = src + (int64_t)(r < 0 ? 0 : r) * ld;
-  TE* out = dh + n * H;
+  if (n >= p.N) return;
+  const int lane = threadIdx.x & ((1 << tpr_log) - 1), r = p.row_pos[n], H = p.H;
+  const float* from = p.src + (int64_t)(r < 0 ? 0 : r) * p.ld;
+  TE* out = reinterpret_cast<TE*>(p.dh) + n * H;
   for (int c = lane * VEC; c < H; c += VEC << tpr_log) {
     if constexpr (VEC == 1) {
-      st_elem<TE>(out, c, r < 0 ? 0.f : from[c]);
+      st_elem<TE>(out, c, r < 0 ? 0.f : p.alpha * from[c]);
     } else {
       f32x4_t v = {0.f, 0.f, 0.f, 0.f};
-      if (r >= 0) v = *reinterpret_cast<const f32x4_t*>(from + c);
+      if (r >= 0) v = *reinterpret_cast<const f32x4_t*>(from + c) * p.alpha;
       if constexpr (sizeof(TE) == 2) *reinterpret_cast<uint2*>(out + c) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
       else *reinterpret_cast<f32x4_t*>(out + c) = v;
     }
@@ -417,27 +465,30 @@ hipError_t launch_vocab_teacher(const VocabTeacher& p, hipStream_t st) {
 }
 
 hipError_t launch_vocab_finish(const VocabFinish& p, hipStream_t st) {
-  // Few rows: more threads per row, since a row's tiles are read one after the other.
-  if (p.N <= 1024) hipLaunchKernelGGL(vocab_finish_kernel<16>, dim3((p.N + 15) / 16), dim3(1024), 0, st, p);
-  else hipLaunchKernelGGL(vocab_finish_kernel<64>, dim3((p.N + 63) / 64), dim3(1024), 0, st, p);
+  // Few rows: more threads per row, since a row's parts are read one after the other.
+#define ASX_FINISH(RPB, TEACH, ARG) \
+  hipLaunchKernelGGL((vocab_finish_kernel<RPB, TEACH, ARG>), dim3((p.N + RPB - 1) / RPB), dim3(1024), 0, st, p)
+  if (p.stat_tau) {
+    if (p.N <= 8192) ASX_FINISH(16, true, false);
+    else ASX_FINISH(64, true, false);
+  } else if (p.stat_idx) {
+    if (p.N <= 8192) ASX_FINISH(16, false, true);
+    else ASX_FINISH(64, false, true);
+  } else {
+    if (p.N <= 8192) ASX_FINISH(16, false, false);
+    else ASX_FINISH(64, false, false);
+  }
+#undef ASX_FINISH
   return hipGetLastError();
 }
 
-hipError_t launch_vocab_col_sums(const float* col_sums, int64_t ld, int tile_rows, int edge, const int32_t* n_act, int V, void* db,
-                                 bool bf16, hipStream_t st) {
-  const dim3 grid((V + 63) / 64);
-  if (bf16) hipLaunchKernelGGL(vocab_col_sums_kernel<uint16_t>, grid, dim3(1024), 0, st, col_sums, ld, tile_rows, edge, n_act, V, reinterpret_cast<uint16_t*>(db));
-  else hipLaunchKernelGGL(vocab_col_sums_kernel<float>, grid, dim3(1024), 0, st, col_sums, ld, tile_rows, edge, n_act, V, reinterpret_cast<float*>(db));
-  return hipGetLastError();
-}
-
-hipError_t launch_vocab_scatter(const float* src, const int32_t* row_pos, int N, int H, int64_t ld, void* dh, bool bf16, hipStream_t st) {
-  const bool vec = H % 4 == 0;   // (bf16 rows: H % 8 == 0)
-  const int log = threads_log(vec ? H / 4 : H);
-  const dim3 grid((unsigned)((((int64_t)N << log) + 255) / 256));
-  if (bf16) hipLaunchKernelGGL((vocab_scatter_kernel<uint16_t, 4>), grid, dim3(256), 0, st, src, row_pos, N, H, ld, reinterpret_cast<uint16_t*>(dh), log);
-  else if (vec) hipLaunchKernelGGL((vocab_scatter_kernel<float, 4>), grid, dim3(256), 0, st, src, row_pos, N, H, ld, reinterpret_cast<float*>(dh), log);
-  else hipLaunchKernelGGL((vocab_scatter_kernel<float, 1>), grid, dim3(256), 0, st, src, row_pos, N, H, ld, reinterpret_cast<float*>(dh), log);
+hipError_t launch_vocab_out_grads(const VocabOutGrads& p, bool bf16, hipStream_t st) {
+  const bool vec = p.H % 4 == 0;   // (bf16 rows: H % 8 == 0)
+  const int log = threads_log(vec ? p.H / 4 : p.H);
+  const int row_blocks = (int)((((int64_t)p.N << log) + 255) / 256), blocks = row_blocks + (p.db ? (p.V + 255) / 256 : 0);
+  if (bf16) hipLaunchKernelGGL((vocab_out_grads_kernel<uint16_t, 4>), dim3(blocks), dim3(256), 0, st, p, log, row_blocks);
+  else if (vec) hipLaunchKernelGGL((vocab_out_grads_kernel<float, 4>), dim3(blocks), dim3(256), 0, st, p, log, row_blocks);
+  else hipLaunchKernelGGL((vocab_out_grads_kernel<float, 1>), dim3(blocks), dim3(256), 0, st, p, log, row_blocks);
   return hipGetLastError();
 }
 

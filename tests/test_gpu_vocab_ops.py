@@ -392,8 +392,8 @@ def _in_64_bits(c, h, y):
     W, b = c.W.cuda().double(), c.b.cuda().double()
     word = torch.from_numpy(c.word).cuda()
     rows = torch.nonzero(word)[:, 0]
-    tok = torch.zeros(c.N, device="cuda", dtype=torch.float64)
-    dh, dW, db = torch.zeros(c.N, c.H, device="cuda", dtype=torch.float64), torch.zeros_like(W), torch.zeros_like(b)
+    zeros = lambda *n: torch.zeros(*n, device="cuda", dtype=torch.float64)  # noqa: E731
+    tok, tok_d, dh, dW, db = zeros(c.N), zeros(c.N), zeros(c.N, c.H), torch.zeros_like(W), torch.zeros_like(b)
     for at in rows.split(1000):
         x = h[at].double()
         l = x @ W.t() + b
@@ -403,23 +403,37 @@ def _in_64_bits(c, h, y):
         dl = torch.exp(l - lse)
         dl.scatter_add_(1, t, torch.full_like(lse, -1.0))
         dl *= c.g
+        if c.K:
+            ids = c.ids_d[at].long()
+            inside = (ids >= 0) & (ids < c.V)
+            z = torch.where(inside, c.z_d[at].double() / c.tau, -np.inf)
+            seen = (z > -np.inf).any(1, keepdim=True)
+            log_p = torch.log_softmax(torch.where(seen, z, 0.0), 1)
+            p = torch.where(seen, log_p.exp(), 0.0)
+            log_q = torch.log_softmax(l / c.tau, 1)
+            k = torch.where(inside, ids, 0)
+            tok_d[at] = c.tau ** 2 * torch.where(p > 0, p * (log_p - log_q.gather(1, k)), 0.0).sum(1)
+            dl += torch.where(seen, c.s * c.tau, 0.0) * log_q.exp()
+            dl.scatter_add_(1, k, -c.s * c.tau * p)
         dh[at] = dl @ W
         dW += dl.t() @ x
         db += dl.sum(0)
-    return dict(tok_loss=tok, dh=dh, dW=dW, db=db)
+    return dict(tok_loss=tok, tok_distill=tok_d, dh=dh, dW=dW, db=db)
 
 
-@pytest.mark.parametrize("N, H, V, dtype, grad", [(9000, 64, 130003, "bf16", "bf16"), (5000, 256, 33000, "bf16", "f32"), (3000, 136, 20001, "f32", "f32")])
-def test_large(N, H, V, dtype, grad):
-    c = Case(N, H, V, dtype, grad, seed=1, g=1.0)
+@pytest.mark.parametrize("N, H, V, dtype, grad, K", [
+    (9000, 64, 130003, "bf16", "bf16", 0), (5000, 256, 33000, "bf16", "f32", 0), (3000, 136, 20001, "f32", "f32", 0),
+    (4001, 264, 20003, "bf16", "bf16", 40), (2500, 136, 33001, "bf16", "f32", 7), (1100, 72, 30011, "f32", "f32", 100)])
+def test_large(N, H, V, dtype, grad, K):
+    c = Case(N, H, V, dtype, grad, K=K, tau=2.0, seed=1, g=1.0)
     v = c.device()
-    c.fwd(v)
+    c.fwd(v, argmax=False)
     c.bwd(v)
     o = _in_64_bits(c, c.h_d, c.y_d)
     # norms: fp32 sums of up to 10^5 terms of either sign, 2^-24 sqrt(10^5); bf16 adds the roundings of dl and of the result
-    for k in ("tok_loss", "dh", "dW", "db"):
+    for k in ("tok_loss", "dh", "dW", "db") + (("tok_distill",) if K else ()):
         off = float((c.out[k].double() - o[k]).norm() / o[k].norm())
-        assert off < (2 * BF if grad == "bf16" and k != "tok_loss" else 320 * U), (k, off)
+        assert off < (2 * BF if grad == "bf16" and k in ("dh", "dW", "db") else 320 * U), (k, off)
     _untouched(*c.bases.values())
 
 
