@@ -6,7 +6,7 @@
 // n, whatever the launch looks like: no float atomics), the sorted list is cut into pieces of the same length, and a group of
 // threads adds up the rows of its piece, whatever words they are of.  Words that lie inside a piece are written at once; parts
 // of words that reach over a piece's edge go to the workspace, and a second pass adds those up.  Rows of words that no position has
-// are zeroed by further blocks of the same launch, which look them up in the sorted list: d_table is written once.
+// are zeroed by further blocks of the sort's launch, or of the sums' where the radix sort takes several: d_table is written once.
 #include "../../include/vocab_ops.h"
 
 #include <hip/hip_runtime.h>
@@ -86,40 +86,72 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(const TE* __restrict__ t
 // ---- the sort ----------------------------------------------------------------------
 // Up to kRankMost positions: every position's place is the number of positions that sort ahead of it, counted by brute force over
 // the whole chip: N^2 comparisons of two instructions, 3 us of arithmetic at 6400 and 14 at 16384, and one launch.  (One block that
-// sorts 6400 in its LDS took 34 us.)  A block places 32 positions: a thread compares every 32nd vector of four keys with four of them.
-constexpr int kRankMost = 16384, kRankBlock = 32;
+// sorts 6400 in its LDS took 34 us.)  A wave places four positions, a lane compares every 64th vector of four keys with them.
+constexpr int kRankMost = 16384, kRankBlock = 16;
 struct SortDev {
   const int32_t* ids;
   int N, V, pad_id;
   uint32_t *key, *pos;   // the sorted words and positions
 };
-__global__ __launch_bounds__(256) void embed_rank_kernel(SortDev p) {
-  extern __shared__ __align__(16) uint32_t keys[];   // of all positions, to a multiple of 32
-  const int N = p.N, N32 = (N + 31) & ~31, tid = threadIdx.x, n0 = blockIdx.x * kRankBlock;
-  for (int i0 = tid * 4; i0 < N32; i0 += 4096) {   // four vectors of ids together
-    int4 id[4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int i = i0 + u * 1024;
-      if (i + 3 < N) {
-        id[u] = *reinterpret_cast<const int4*>(p.ids + i);
-      } else {
-        id[u].x = i < N ? p.ids[i] : -1;
-        id[u].y = i + 1 < N ? p.ids[i + 1] : -1;
-        id[u].z = i + 2 < N ? p.ids[i + 2] : -1;
-        id[u].w = -1;
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int i = i0 + u * 1024;
-      if (i >= N32) continue;
-      auto key = [&](int w) { return w >= 0 && w < p.V && w != p.pad_id ? (uint32_t)w : (uint32_t)p.V; };
-      *reinterpret_cast<uint4*>(keys + i) = make_uint4(key(id[u].x), key(id[u].y), key(id[u].z), key(id[u].w));
-    }
+// Rows of words that no position has: a block per kZeroRows of them.
+struct ZeroDev {
+  void* d_table;
+  int I, blocks;
+};
+constexpr int kZeroRows = 64;
+template <typename TE, int VEC>
+__device__ __forceinline__ void zero_rows(TE* table, const uint8_t* has, int v0, int v1, int I, int tpp_log) {
+  const int lane = threadIdx.x & ((1 << tpp_log) - 1), step = VEC << tpp_log;
+  const float zero[VEC] = {};
+  for (int v = v0 + (threadIdx.x >> tpp_log); v < v1; v += 256 >> tpp_log) {
+    if (has[v - v0]) continue;
+    for (int c = lane * VEC; c < I; c += step) st_vec<TE, VEC>(table + (int64_t)v * I + c, zero);
   }
+}
+template <typename TE, int VEC> __global__ __launch_bounds__(256) void embed_rank_kernel(SortDev p, ZeroDev z, int tpp_log) {
+  extern __shared__ __align__(16) uint32_t keys[];   // of all positions, to a multiple of 16
+  const int N = p.N, N16 = (N + 15) & ~15, tid = threadIdx.x;
+  auto key = [&](int w) { return w >= 0 && w < p.V && w != p.pad_id ? (uint32_t)w : (uint32_t)p.V; };
+  auto all_ids = [&](auto use) {   // four vectors of ids together
+    for (int i0 = tid * 4; i0 < N16; i0 += 4096) {
+      int4 id[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int i = i0 + u * 1024;
+        if (i + 3 < N) {
+          id[u] = *reinterpret_cast<const int4*>(p.ids + i);
+        } else {
+          id[u].x = i < N ? p.ids[i] : -1;
+          id[u].y = i + 1 < N ? p.ids[i + 1] : -1;
+          id[u].z = i + 2 < N ? p.ids[i + 2] : -1;
+          id[u].w = -1;
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (i0 + u * 1024 < N16) use(i0 + u * 1024, make_uint4(key(id[u].x), key(id[u].y), key(id[u].z), key(id[u].w)));
+    }
+  };
+  const int rank_blocks = (N + kRankBlock - 1) / kRankBlock;
+  if ((int)blockIdx.x >= rank_blocks) {   // they need no order: which of their rows occur, from the ids themselves
+    uint8_t* has = reinterpret_cast<uint8_t*>(keys);
+    const uint32_t v0 = ((int)blockIdx.x - rank_blocks) * kZeroRows;
+    if (tid < kZeroRows) has[tid] = 0;
+    __syncthreads();
+    all_ids([&](int, uint4 k) {
+      if (k.x - v0 < (uint32_t)kZeroRows) has[k.x - v0] = 1;
+      if (k.y - v0 < (uint32_t)kZeroRows) has[k.y - v0] = 1;
+      if (k.z - v0 < (uint32_t)kZeroRows) has[k.z - v0] = 1;
+      if (k.w - v0 < (uint32_t)kZeroRows) has[k.w - v0] = 1;
+    });
+    __syncthreads();
+    const int end = (int)v0 + kZeroRows < p.V ? (int)v0 + kZeroRows : p.V;
+    zero_rows<TE, VEC>(reinterpret_cast<TE*>(z.d_table), has, (int)v0, end, z.I, tpp_log);
+    return;
+  }
+  all_ids([&](int i, uint4 k) { *reinterpret_cast<uint4*>(keys + i) = k; });
   __syncthreads();
-  const int part = tid & 31, first = n0 + (tid >> 5) * 4;   // this thread's four positions
+  const int lane = tid & 63, n0 = blockIdx.x * kRankBlock, first = n0 + (tid >> 6) * 4;   // this wave's four positions
   uint32_t mine[4], at_most[4], rank[4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
@@ -133,22 +165,22 @@ __global__ __launch_bounds__(256) void embed_rank_kernel(SortDev p) {
   // positions ahead of the block's: equal words sort ahead too
 #pragma unroll
   for (int k = 0; k < 4; ++k) at_most[k] = mine[k] + 1;
-#pragma unroll 2
-  for (int i = part * 4; i < n0; i += 128) count(*reinterpret_cast<const uint4*>(keys + i));
+#pragma unroll 4
+  for (int i = lane * 4; i < n0; i += 256) count(*reinterpret_cast<const uint4*>(keys + i));
 #pragma unroll
   for (int k = 0; k < 4; ++k) at_most[k] = mine[k];
-#pragma unroll 2
-  for (int i = n0 + kRankBlock + part * 4; i < N32; i += 128) count(*reinterpret_cast<const uint4*>(keys + i));
-  {   // the block's own
-    const uint32_t q = keys[n0 + part];
+#pragma unroll 4
+  for (int i = n0 + kRankBlock + lane * 4; i < N16; i += 256) count(*reinterpret_cast<const uint4*>(keys + i));
+  if (lane < kRankBlock) {   // the block's own
+    const uint32_t q = keys[n0 + lane];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) rank[k] += q < mine[k] + (n0 + part < first + k ? 1u : 0u);
+    for (int k = 0; k < 4; ++k) rank[k] += q < mine[k] + (n0 + lane < first + k ? 1u : 0u);
   }
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1)
+  for (int o = 32; o > 0; o >>= 1)
 #pragma unroll
     for (int k = 0; k < 4; ++k) rank[k] += __shfl_xor(rank[k], o, 64);
-  if (part == 0)
+  if (lane == 0)
 #pragma unroll
     for (int k = 0; k < 4; ++k)
       if (first + k < N) {   // (what fills the last block up sorts behind everything)
@@ -325,10 +357,8 @@ struct SumsDev {
   int N, I, V;
   float scale;
   int accumulate;
-  int zero_blocks, pieces;
+  int zero_blocks, pieces;   // zero_blocks: behind the radix sort alone
 };
-constexpr int kZeroRows = 64;   // rows that a zeroing block looks at
-
 // first sorted place whose word is >= v, by a wave: 64 probes at a time
 __device__ __forceinline__ int lower_bound_wave(const uint32_t* key, int N, uint32_t v) {
   const int lane = threadIdx.x & 63;
@@ -344,10 +374,11 @@ __device__ __forceinline__ int lower_bound_wave(const uint32_t* key, int N, uint
   return lo;
 }
 
-// 2^tpp_log threads per piece of L sorted positions, RU rows of it in flight
-template <typename TE, int VEC, int L>
+// 2^tpp_log (16 at least) threads per piece of L sorted positions, RU rows of it in flight: all of a short piece, whose launch is a
+// few latencies long; four where the blocks of a compute unit have enough on its way together (131072 x 1024, 16 / 4: 276 / 247 us).
+template <typename TE, int VEC, int L, int RU>
 __global__ __launch_bounds__(256) void embed_sums_kernel(SumsDev p, int tpp_log) {
-  constexpr int RU = 16;
+  __shared__ uint32_t list[2][16 * L + 1];   // the block's part of the sorted list: words, with the one ahead, and positions
   const int I = p.I, lane = threadIdx.x & ((1 << tpp_log) - 1), step = VEC << tpp_log;
   TE* table = reinterpret_cast<TE*>(p.d_table);
   if ((int)blockIdx.x < p.zero_blocks) {   // rows of words that no position has
@@ -371,21 +402,26 @@ __global__ __launch_bounds__(256) void embed_sums_kernel(SumsDev p, int tpp_log)
       has[threadIdx.x] = lo < end && p.key[lo] == v;
     }
     __syncthreads();
-    const int rows_at_once = 256 >> tpp_log;
-    const float zero[VEC] = {};
-    for (int v = v0 + (threadIdx.x >> tpp_log); v < v1; v += rows_at_once) {
-      if (has[v - v0]) continue;
-      for (int c = lane * VEC; c < I; c += step) st_vec<TE, VEC>(table + (int64_t)v * I + c, zero);
-    }
+    zero_rows<TE, VEC>(table, has, v0, v1, I, tpp_log);
     return;
   }
-  const int piece = (int)(((int64_t)((int)blockIdx.x - p.zero_blocks) * 256 + threadIdx.x) >> tpp_log);
+  const int per_block = 256 >> tpp_log, piece0 = ((int)blockIdx.x - p.zero_blocks) * per_block, piece = piece0 + ((int)threadIdx.x >> tpp_log);
+  for (int i = threadIdx.x; i < per_block * L; i += 256) {
+    const int at = piece0 * L + i;
+    list[0][i + 1] = at < p.N ? p.key[at] : (uint32_t)p.V;
+    list[1][i] = at < p.N ? p.pos[at] : 0;
+  }
+  if (threadIdx.x == 0) {
+    list[0][0] = piece0 > 0 ? p.key[piece0 * L - 1] : (uint32_t)p.V;
+    list[1][per_block * L] = (piece0 + per_block) * L < p.N ? p.key[(piece0 + per_block) * L] : (uint32_t)p.V;   // the word behind
+  }
+  __syncthreads();
   if (piece >= p.pieces) return;
-  const int i0 = piece * L, i1 = i0 + L < p.N ? i0 + L : p.N;
-  const uint32_t first = p.key[i0];
+  const uint32_t *key = list[0] + 1 + (piece - piece0) * L, *pos = list[1] + (piece - piece0) * L;
+  const uint32_t first = key[0];
   if (first >= (uint32_t)p.V) return;   // padding from here on
-  const bool begins = i0 == 0 || p.key[i0 - 1] != first;
-  const uint32_t after = i1 < p.N ? p.key[i1] : (uint32_t)p.V;
+  const bool begins = key[-1] != first;
+  const uint32_t after = piece - piece0 + 1 < per_block ? key[L] : list[1][per_block * L];
   const TE* dy = reinterpret_cast<const TE*>(p.dy);
   for (int c = lane * VEC; c < I; c += step) {
     float acc[VEC];
@@ -414,15 +450,13 @@ __global__ __launch_bounds__(256) void embed_sums_kernel(SumsDev p, int tpp_log)
     };
 #pragma unroll 1
     for (int u0 = 0; u0 < L; u0 += RU) {
-      if (i0 + u0 >= i1) break;
       float x[RU][VEC];
       uint32_t k[RU];
 #pragma unroll
       for (int u = 0; u < RU; ++u) {
-        const int i = i0 + u0 + u;
-        k[u] = i < i1 ? p.key[i] : (uint32_t)p.V;
+        k[u] = key[u0 + u];
         if (k[u] < (uint32_t)p.V) {
-          ld_vec<TE, VEC>(dy + (int64_t)p.pos[i] * I + c, x[u]);
+          ld_vec<TE, VEC>(dy + (int64_t)pos[u0 + u] * I + c, x[u]);
         } else {
 #pragma unroll
           for (int e = 0; e < VEC; ++e) x[u][e] = 0.f;
@@ -534,7 +568,7 @@ EmbedLayout embed_layout(const vo_embed* s) {
   if (L.blocks > 512) L.blocks = 512;
   L.per = ((N + L.blocks - 1) / L.blocks + kSortWaves - 1) / kSortWaves;
   L.per = (L.per + 63) & ~63;
-  L.L = N <= 16384 ? 16 : 32;
+  L.L = L.rank ? 16 : 64;
   L.pieces = (N + L.L - 1) / L.L;
   size_t off = 0;
   auto take = [&](size_t bytes) {
@@ -575,23 +609,8 @@ int row_threads_log(int vecs) {
   return b;
 }
 
-hipError_t launch_sort(const vo_embed* s, const EmbedLayout& L, const int32_t* ids, unsigned char* ws, hipStream_t st) {
+hipError_t launch_sort(const SortDev& p, const EmbedLayout& L, unsigned char* ws, hipStream_t st) {
   auto u32 = [&](size_t at) { return reinterpret_cast<uint32_t*>(ws + at); };
-  SortDev p;
-  p.ids = ids;
-  p.N = s->N;
-  p.V = s->V;
-  p.pad_id = s->pad_id;
-  p.key = u32(L.key);
-  p.pos = u32(L.pos);
-  if (L.rank) {
-    static LdsLimit limit;
-    const hipError_t e = limit.raise(reinterpret_cast<const void*>(embed_rank_kernel), kRankMost * 4);
-    if (e != hipSuccess) return e;
-    const int blocks = (s->N + kRankBlock - 1) / kRankBlock;
-    hipLaunchKernelGGL(embed_rank_kernel, dim3(blocks), dim3(256), (size_t)blocks * kRankBlock * 4, st, p);
-    return hipGetLastError();
-  }
   // the last pass writes key / pos
   uint32_t *ka = u32(L.key), *pa = u32(L.pos), *kb = u32(L.key2), *pb = u32(L.pos2);
   if (L.passes % 2 == 0) {
@@ -620,20 +639,35 @@ hipError_t launch_sort(const vo_embed* s, const EmbedLayout& L, const int32_t* i
   return hipSuccess;
 }
 
-template <typename TE, int VEC, int PL>
-hipError_t launch_sums(SumsDev p, hipStream_t st) {
-  const int tpp = row_threads_log((p.I + VEC - 1) / VEC), per_block = 256 >> tpp;
-  p.zero_blocks = p.accumulate ? 0 : (p.V + kZeroRows - 1) / kZeroRows;
-  const int piece_blocks = (p.pieces + per_block - 1) / per_block;
-  hipLaunchKernelGGL((embed_sums_kernel<TE, VEC, PL>), dim3(p.zero_blocks + piece_blocks), dim3(256), 0, st, p, tpp);
+template <typename TE, int VEC, int PL, int RU>
+hipError_t launch_sums(const SumsDev& p, int tpp, hipStream_t st) {
+  if (tpp < 4) tpp = 4;
+  const int per_block = 256 >> tpp, piece_blocks = (p.pieces + per_block - 1) / per_block;
+  hipLaunchKernelGGL((embed_sums_kernel<TE, VEC, PL, RU>), dim3(p.zero_blocks + piece_blocks), dim3(256), 0, st, p, tpp);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.pieces < 2) return e;
   constexpr int CV = VEC == 1 ? 1 : 4;
   hipLaunchKernelGGL((embed_edges_kernel<TE, VEC, PL>), dim3(p.pieces, (p.I + 64 * CV - 1) / (64 * CV)), dim3(256), 0, st, p);
   return hipGetLastError();
 }
-template <typename TE, int VEC> hipError_t launch_sums_any(const SumsDev& p, int L, hipStream_t st) {
-  return L == 16 ? launch_sums<TE, VEC, 16>(p, st) : launch_sums<TE, VEC, 32>(p, st);
+template <typename TE, int VEC>
+hipError_t launch_embed_bwd(const SortDev& q, SumsDev p, const EmbedLayout& L, unsigned char* ws, hipStream_t st) {
+  const int tpp = row_threads_log((p.I + VEC - 1) / VEC), zero_blocks = p.accumulate ? 0 : (p.V + kZeroRows - 1) / kZeroRows;
+  if (!L.rank) {
+    const hipError_t e = launch_sort(q, L, ws, st);
+    p.zero_blocks = zero_blocks;
+    return e == hipSuccess ? launch_sums<TE, VEC, 64, 4>(p, tpp, st) : e;
+  }
+  auto kfn = embed_rank_kernel<TE, VEC>;
+  static LdsLimit limit;
+  hipError_t e = limit.raise(reinterpret_cast<const void*>(kfn), kRankMost * 4);
+  if (e != hipSuccess) return e;
+  const int blocks = (q.N + kRankBlock - 1) / kRankBlock;
+  const size_t smem = (size_t)(blocks * kRankBlock < kZeroRows ? kZeroRows : blocks * kRankBlock) * 4;
+  hipLaunchKernelGGL(kfn, dim3(blocks + zero_blocks), dim3(256), smem, st, q, ZeroDev{p.d_table, p.I, zero_blocks}, tpp);
+  e = hipGetLastError();
+  p.zero_blocks = 0;
+  return e == hipSuccess ? launch_sums<TE, VEC, 16, 16>(p, tpp, st) : e;
 }
 
 }  // namespace
@@ -681,11 +715,16 @@ extern "C" as_status vocab_embed_bwd(const vo_embed* shape, const int32_t* ids, 
     return set_error(AS_ERR_ALIGN, "vocab_embed_bwd: a pointer is not 16-byte aligned");
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   unsigned char* ws = reinterpret_cast<unsigned char*>(workspace);
-  hipError_t e = launch_sort(shape, L, ids, ws, st);
-  if (e != hipSuccess) return hip_status(e, "vocab_embed_bwd, sort");
+  SortDev q;
+  q.ids = ids;
+  q.N = shape->N;
+  q.V = shape->V;
+  q.pad_id = shape->pad_id;
+  q.key = reinterpret_cast<uint32_t*>(ws + L.key);
+  q.pos = reinterpret_cast<uint32_t*>(ws + L.pos);
   SumsDev p{};
-  p.key = reinterpret_cast<const uint32_t*>(ws + L.key);
-  p.pos = reinterpret_cast<const uint32_t*>(ws + L.pos);
+  p.key = q.key;
+  p.pos = q.pos;
   p.dy = dy;
   p.d_table = d_table;
   p.edge = reinterpret_cast<float*>(ws + L.edge);
@@ -695,8 +734,9 @@ extern "C" as_status vocab_embed_bwd(const vo_embed* shape, const int32_t* ids, 
   p.scale = shape->scale;
   p.accumulate = accumulate;
   p.pieces = L.pieces;
-  if (shape->grad_dtype == AS_BF16) e = launch_sums_any<uint16_t, 8>(p, L.L, st);
-  else if (shape->I % 4 == 0) e = launch_sums_any<float, 4>(p, L.L, st);
-  else e = launch_sums_any<float, 1>(p, L.L, st);
+  hipError_t e;
+  if (shape->grad_dtype == AS_BF16) e = launch_embed_bwd<uint16_t, 8>(q, p, L, ws, st);
+  else if (shape->I % 4 == 0) e = launch_embed_bwd<float, 4>(q, p, L, ws, st);
+  else e = launch_embed_bwd<float, 1>(q, p, L, ws, st);
   return hip_status(e, "vocab_embed_bwd");
 }

@@ -685,7 +685,7 @@ __global__ __launch_bounds__(512) void gemm_bf16_pp_kernel(GemmDev p, int work_t
       float* region = reinterpret_cast<float*>(smem + PP_EPI_OFF + wave * 4096);
       auto stage = [&](int i) { stage_round<true, 4, 16, 64>(region, acc, i, lane); };
       const int row0 = it.m0 + wm * WM, col0 = it.n0 + wn * WN;
-      if constexpr (VOC::kTerms == 0) vocab_wave_stats<VOC::kTeach>(voc, acc, region, stage, lane, row0, Mv - row0, col0, p.N);
+      if constexpr (VOC::kTerms == 0) vocab_wave_stats<VOC::kTeach, VOC::kArg>(voc, acc, region, stage, lane, row0, Mv - row0, col0, p.N);
       else vocab_wave_grad<VOC::kTeach, VOC::kTerms>(voc, acc, region, stage, lane, row0, Mv - row0, col0, p.N);
     } else {
       gemm_epilogue<TM, TN, OUT_BF16, VEC, DROP, 16, 64, MI16>(p, Mv, acc, smem + PP_EPI_OFF + wave * 4096, lane,
@@ -1113,10 +1113,10 @@ hipError_t launch_gemm_vocab(const GemmArgs& g, GemmTile tile, const VocabEpi& v
   const hipError_t e = gemm_describe(g, tile, d);
   if (e != hipSuccess) return e;
   if (tile != kTile256) return launch_gemm_bf16_vocab_tile(d, tile, v, terms, teacher, arg, st);
-  if (arg) return hipErrorInvalidValue;
   if (terms == 1) return teacher ? launch_pp_vocab<VocabOut<true, false, 1>>(d, v, st) : launch_pp_vocab<VocabOut<false, false, 1>>(d, v, st);
   if (terms == 3) return teacher ? launch_pp_vocab<VocabOut<true, false, 3>>(d, v, st) : launch_pp_vocab<VocabOut<false, false, 3>>(d, v, st);
-  return teacher ? launch_pp_vocab<VocabOut<true, false, 0>>(d, v, st) : launch_pp_vocab<VocabOut<false, false, 0>>(d, v, st);
+  if (teacher) return launch_pp_vocab<VocabOut<true, false, 0>>(d, v, st);
+  return arg ? launch_pp_vocab<VocabOut<false, true, 0>>(d, v, st) : launch_pp_vocab<VocabOut<false, false, 0>>(d, v, st);
 }
 
 hipError_t launch_gemm_bf16_together(const GemmArgs* g, const GemmTile* tile, int n, const DbReduce* sums, hipStream_t st) {

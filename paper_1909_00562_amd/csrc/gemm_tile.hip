@@ -25,7 +25,7 @@
 #include "gemm.h"
 #include "gemm_dev.h"
 #include "lds_limit.h"
-#include "vocab_epi_dev.h"
+#include "vocab_wave_dev.h"
 #include "wave_pipe.h"
 
 #include <type_traits>
@@ -297,7 +297,7 @@ __device__ __forceinline__ void gemm_bf16_tile_block(GemmDev p, int out_bf16, in
 #pragma unroll
       for (int r = 0; r < 4; ++r) acc[i][j][r] = 0.f;
   VocabRow vrow = {};   // what the vocabulary's write-out needs to know of a row, a thread per row: on its way during the reduction
-  if constexpr (VOC::kOn) vrow = vocab_row<VOC::kTeach, (VOC::kTerms > 0)>(voc, m0 + tid, tid < BM && m0 + tid < Mv);
+  if constexpr (VOC::kOn && TW == 2) vrow = vocab_row<VOC::kTeach, (VOC::kTerms > 0)>(voc, m0 + tid, tid < BM && m0 + tid < Mv);
 
   // Two sets of fragments, one per half (32 reduction elements) of a tile.  LACED: the reads of a half run between the matrix
   // instructions of the half before it; else all reads of a tile come first and the other blocks of the compute unit run
@@ -399,7 +399,20 @@ __device__ __forceinline__ void gemm_bf16_tile_block(GemmDev p, int out_bf16, in
   __syncthreads();
   float* stage = reinterpret_cast<float*>(smem);
   const int q = lane >> 4, c = lane & 15;
-  if constexpr (VOC::kOn) {
+  if constexpr (VOC::kOn && TW == 4) {   // each wave by itself, through a slice of its own
+    float* region = stage + wave * 1024;
+    auto part = [&](int i) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) region[(4 * q + r) * 64 + (((j ^ q) & 3) << 4) + c] = acc[i][j][r];
+    };
+    const int row0 = m0 + wm, col0 = n0 + wn;
+    if constexpr (VOC::kTerms == 0) vocab_wave_stats<VOC::kTeach, VOC::kArg>(voc, acc, region, part, lane, row0, Mv - row0, col0, p.N);
+    else vocab_wave_grad<VOC::kTeach, VOC::kTerms>(voc, acc, region, part, lane, row0, Mv - row0, col0, p.N);
+    return;
+  }
+  if constexpr (VOC::kOn && TW == 2) {
     float vbias[TW];
 #pragma unroll
     for (int j = 0; j < TW; ++j) {
@@ -410,24 +423,18 @@ __device__ __forceinline__ void gemm_bf16_tile_block(GemmDev p, int out_bf16, in
     static_assert(NST * STAGE >= 64 * LD * 4 + BM * (int)sizeof(VocabRow), "staging of the rows");
     if (tid < BM) rows[tid] = vrow;
     f32x4_t cs = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 1
-    for (int half = 0; half < BM / 64; ++half) {   // 64 rows at a time
-      if (wm / 64 == half) {
 #pragma unroll
-        for (int i = 0; i < TW; ++i)
+    for (int i = 0; i < TW; ++i)
 #pragma unroll
-          for (int j = 0; j < TW; ++j)
+      for (int j = 0; j < TW; ++j)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) stage[(wm % 64 + 16 * i + 4 * q + r) * LD + wn + 16 * j + c] = acc[i][j][r] + vbias[j];
-      }
-      __syncthreads();
-      const int row0 = m0 + half * 64, left = Mv - row0 < 64 ? Mv - row0 : 64;
-      if constexpr (VOC::kTerms == 0) vocab_stats64<BM, VOC::kTeach, VOC::kArg>(voc, stage, LD, rows + half * 64, row0, left, n0, p.N - n0);
-      else vocab_grad64<BM, VOC::kTeach, VOC::kTerms>(voc, stage, LD, rows + half * 64, row0, left, n0, p.N - n0, cs);
-      __syncthreads();
-    }
+        for (int r = 0; r < 4; ++r) stage[(wm + 16 * i + 4 * q + r) * LD + wn + 16 * j + c] = acc[i][j][r] + vbias[j];
+    __syncthreads();
+    if constexpr (VOC::kTerms == 0) vocab_stats64<VOC::kTeach, VOC::kArg>(voc, stage, LD, rows, m0, Mv - m0, n0, p.N - n0);
+    else vocab_grad64<VOC::kTeach, VOC::kTerms>(voc, stage, LD, rows, m0, Mv - m0, n0, p.N - n0, cs);
     if (VOC::kTerms > 0 && voc.col_sums) {         // of the tile's rows, in a fixed order
       constexpr int VPR = BM / 4, RP = 256 / VPR;
+      __syncthreads();
       *reinterpret_cast<f32x4_t*>(stage + (tid / VPR) * BM + (tid % VPR) * 4) = cs;
       __syncthreads();
       if (tid < BM && n0 + tid < p.N) {

@@ -21,7 +21,7 @@ struct VocabEpi {
   const void* bias;           // of the product's columns, or null
   int32_t bias_f32;           // float or bf16
   float inv_tau;
-  // statistics: [tile column][ldr] each
+  // statistics: [64 columns][ldr] each
   float2* stat;               // maximum, sum of exp relative to it
   float* stat_tau;            // teacher: sum of exp((l - maximum) / tau)
   int32_t* stat_idx;          // lowest column that attains the maximum (INT_MAX: none), or null
@@ -43,13 +43,11 @@ struct VocabEpi {
   int64_t ld_sums;
 };
 
-// Columns of a part of a row's statistics, rows of a part of the column sums
-inline int vocab_stat_cols(GemmTile t) { return t == kTile128 ? 128 : 64; }    // 256: a wave's 64 columns
-inline int vocab_sum_rows(GemmTile t) { return t == kTile64 ? 64 : 128; }      // 256: a wave's 128 rows
+constexpr int kVocabStatCols = 64;                                             // columns of a part of a row's statistics
+inline int vocab_sum_rows(GemmTile t) { return t == kTile256 ? 128 : 64; }     // rows of a part of the column sums
 constexpr int kVocabRowPad = 256;   // y, lse, lse_tau are read in whole tiles: their allocations are multiples of this
 
-// terms: planes of dl (1 or 3), or 0: statistics; arg: stat_idx is wanted (64 x 64 and 128 x 128).  g: A, B contiguous, M_dev, no
-// split, no C.
+// terms: planes of dl (1 or 3), or 0: statistics; arg: stat_idx is wanted.  g: A, B contiguous, M_dev, no split, no C.
 hipError_t launch_gemm_vocab(const GemmArgs& g, GemmTile tile, const VocabEpi& e, int terms, bool teacher, bool arg, hipStream_t st);
 
 // ---- rows of words -------------------------------------------------------------------
@@ -112,14 +110,17 @@ struct VocabFinish {
 hipError_t launch_vocab_finish(const VocabFinish& p, hipStream_t st);
 
 // ---- gradients on their way out ----------------------------------------------------------
-// dh[n] = alpha src[row_pos[n]], zeros at padding; db[v] = alpha sums[v] (db: optional)
+// dh[n] = alpha src[row_pos[n]], zeros at padding; db[v] = alpha times the column sums' parts, in order (db: optional)
 struct VocabOutGrads {
   const float* src;
   const int32_t* row_pos;
   int N, H;
   int64_t ld;
   void* dh;
-  const float* sums;
+  const float* sums;          // [parts of sum_rows rows of words][ld_sums]
+  int64_t ld_sums;
+  int sum_rows;
+  const int32_t* n_act;
   int V;
   void* db;
   float alpha;

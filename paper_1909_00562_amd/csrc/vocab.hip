@@ -51,7 +51,8 @@ struct VocabLayout {
   // one area for the pieces of either pass
   size_t stat, stat_tau, stat_idx, w_fwd;
   bool w_kept;                            // terms of all of W, made once for both passes
-  size_t dl, w_bwd, col_sums, db_acc, dh_acc, partial_dw, partial_dh;
+  size_t dl, w_bwd, col_sums, dh_acc, partial_dw, partial_dh;
+  int64_t ld_sums;
   size_t total;
 };
 
@@ -132,14 +133,14 @@ VocabLayout vocab_layout(const vo_shape* s, const vo_teacher* t) {
   L.t_bwd = logits_tile(N, L.ldd, L.ldH, L.h_terms);
   // The two products of a piece in one launch of 128 x 128 tiles, the blocks of dh first, whose reductions are the longer ones: as
   // launches of their own, each is some part of a round of the compute units too long.  dh is split where one of its blocks
-  // would otherwise take longer than all blocks' share of a compute unit's two places.
+  // would otherwise take longer than half of all blocks' share of a compute unit's two places.
   const int n_dw = pair_count(L.dl_terms, L.h_terms);
   const int64_t k_dw = n_dw * ((N + 63) / 64), k_dh = n_dw * ((L.ldd + 63) / 64);
   if (N > 256) {
     const int64_t b_dw = ((L.ldd + 127) / 128) * ((H + 127) / 128), b_dh = ((N + 127) / 128) * ((L.ldH + 127) / 128);
     int64_t share = (b_dw * k_dw + b_dh * k_dh + 511) / 512;
     if (share < 8) share = 8;
-    int64_t splits = (k_dh + share - 1) / share;
+    int64_t splits = (2 * k_dh + share - 1) / share;
     if (splits > 32) splits = 32;
     L.p_dw = {kTile128, 1};
     L.p_dh = {kTile128, whole_splits((int)k_dh, (int)splits)};
@@ -193,7 +194,7 @@ VocabLayout vocab_layout(const vo_shape* s, const vo_teacher* t) {
   L.w_kept = L.f32 && V * w_col <= kPieceBytes;
   L.w_fwd = L.w_bwd = take(L.w_kept ? (size_t)V * w_col : 0);
   const size_t area = off;
-  const int64_t parts = L.fwd_cols / 64;
+  const int64_t parts = L.fwd_cols / kVocabStatCols;
   L.stat = take((size_t)parts * N * 8);
   L.stat_tau = take(t ? (size_t)parts * N * 4 : 0);
   L.stat_idx = take((size_t)parts * N * 4);
@@ -202,8 +203,8 @@ VocabLayout vocab_layout(const vo_shape* s, const vo_teacher* t) {
   off = area;
   L.dl = take((size_t)L.dl_terms * N * L.ldd * 2);
   if (!L.w_kept) L.w_bwd = take((size_t)L.bwd_cols * w_col);
-  L.col_sums = take((size_t)((N + 63) / 64) * L.ldd * 4);
-  L.db_acc = take((size_t)V * 4);
+  L.ld_sums = round_up(V, 4);
+  L.col_sums = take((size_t)((N + vocab_sum_rows(L.t_bwd) - 1) / vocab_sum_rows(L.t_bwd)) * L.ld_sums * 4);
   L.dh_acc = take((size_t)N * L.ldH * 4);
   L.partial_dw = take(gemm_partial_bytes((int)L.ldd, (int)H, 1, L.p_dw.splits));
   L.partial_dh = take(gemm_partial_bytes((int)N, (int)L.ldH, 1, L.p_dh.splits));
@@ -377,10 +378,9 @@ as_status forward(const vo_shape* s, const vo_teacher* t, const void* h, const v
     v.ent = w.at<uint32_t>(L.ent);
     v.ent_l = w.at<float>(L.ent_l);
     v.strips = L.strips;
-    const GemmTile tile = argmax && L.t_fwd == kTile256 ? kTile128 : L.t_fwd;
-    e = launch_gemm_vocab(logits_product(s, L, w, W, planes, plane, v0, cols), tile, v, 0, t != nullptr, argmax != nullptr, st);
+    e = launch_gemm_vocab(logits_product(s, L, w, W, planes, plane, v0, cols), L.t_fwd, v, 0, t != nullptr, argmax != nullptr, st);
     if (e != hipSuccess) return hip_fail(e, "statistics of the logits");
-    f.parts = (cols + vocab_stat_cols(tile) - 1) / vocab_stat_cols(tile);
+    f.parts = (cols + kVocabStatCols - 1) / kVocabStatCols;
     f.first = v0 == 0;
     f.last = v0 + L.fwd_cols >= s->V;
     e = launch_vocab_finish(f, st);
@@ -437,8 +437,8 @@ as_status backward(const vo_shape* s, const vo_teacher* t, const void* W, const 
     v.dl = dl;
     v.ldd = L.ldd;
     v.plane = dl_plane;
-    v.col_sums = db ? w.at<float>(L.col_sums) : nullptr;
-    v.ld_sums = cols;
+    v.col_sums = db ? w.at<float>(L.col_sums) + v0 : nullptr;
+    v.ld_sums = L.ld_sums;
     e = launch_gemm_vocab(logits_product(s, L, w, W, planes, w_plane, v0, cols), L.t_bwd, v, L.dl_terms, t != nullptr, false, st);
     if (e != hipSuccess) return hip_fail(e, "derivative of the logits");
     GemmArgs g[2];   // dW_piece = dl^T h, dh += dl W_piece
@@ -468,13 +468,11 @@ as_status backward(const vo_shape* s, const vo_teacher* t, const void* W, const 
     g[1].dyn_split = L.dh_dyn;
     g[1].partial = w.at<float>(L.partial_dh);
     const GemmTile tiles[2] = {L.p_dw.tile, L.p_dh.tile};
-    const int sum_rows = vocab_sum_rows(L.t_bwd);
-    const DbReduce sums = {v.col_sums, (N + sum_rows - 1) / sum_rows, cols, w.at<float>(L.db_acc) + v0, n_act, sum_rows};
-    e = launch_gemm_joint(g, tiles, 2, true, st, db ? &sums : nullptr);
-    if (e == hipErrorNotSupported) {
-      e = db ? launch_db_reduce(sums, st) : hipSuccess;
-      for (int i = 0; i < 2 && e == hipSuccess; ++i) e = launch_gemm(g[i], true, tiles[i], st);
-    }
+    const DbReduce no_sums = {nullptr, 0, 0, nullptr, nullptr, 1};   // (db is added up with the last pass)
+    e = launch_gemm_joint(g, tiles, 2, true, st, &no_sums);
+    if (e == hipErrorNotSupported) e = hipSuccess;
+    else if (e == hipSuccess) continue;
+    for (int i = 0; i < 2 && e == hipSuccess; ++i) e = launch_gemm(g[i], true, tiles[i], st);
     if (e != hipSuccess) return hip_fail(e, "dW and dh");
   }
   VocabOutGrads o{};
@@ -484,7 +482,10 @@ as_status backward(const vo_shape* s, const vo_teacher* t, const void* W, const 
   o.H = H;
   o.ld = L.ldH;
   o.dh = dh;
-  o.sums = w.at<float>(L.db_acc);
+  o.sums = w.at<float>(L.col_sums);
+  o.ld_sums = L.ld_sums;
+  o.sum_rows = vocab_sum_rows(L.t_bwd);
+  o.n_act = n_act;
   o.V = s->V;
   o.db = db;
   o.alpha = alpha;

@@ -1,4 +1,5 @@
-// Write-out of the vocabulary products in the 64 x 64 and 128 x 128 kernel: 64 rows of the tile at a time in LDS (with the bias).
+// Write-out of the vocabulary products: what all kernels share, and that of the 64 x 64 kernel, from the tile in LDS (with the
+// bias); that of the larger tiles is in vocab_wave_dev.h.
 #pragma once
 #include "common.h"
 #include "vocab.h"
@@ -20,14 +21,22 @@ __device__ __forceinline__ float vocab_bias(const VocabEpi& e, int col) {
   if (!e.bias) return 0.f;
   return e.bias_f32 ? reinterpret_cast<const float*>(e.bias)[col] : bf16_bits_to_f32(reinterpret_cast<const uint16_t*>(e.bias)[col]);
 }
-// exp(x) with the product by log2 e compensated: its rounding alone is |x| 2^-24, a row's probabilities reach down to e^-30
-__device__ __forceinline__ float vocab_exp(float x) {
-  constexpr float L2E = 1.4426950408889634f, L2E_LO = 1.9259629911266175e-8f;
-  const float t = x * L2E;
-  const float lo = __builtin_fmaf(x, L2E, -t) + x * L2E_LO;
-  const float r = __builtin_amdgcn_exp2f(t);
-  return t > -126.f ? __builtin_fmaf(r, lo * 0.6931471805599453f, r) : r;   // (x = -inf: lo is NaN)
-}
+// exp(l scale - lse) = k exp2(fma(l, scale log2 e, c)): one fused multiply-add and one v_exp_f32 per element.  k makes up for the
+// rounding of c, which is the same for a whole row (|lse| 2^-24 of all of its probabilities); three bf16 terms of dl keep it, one
+// would round it away.
+template <bool EXACT> struct RowExp {
+  float c, k;
+  __device__ __forceinline__ explicit RowExp(float lse) {
+    constexpr float L2E = 1.4426950408889634f, L2E_LO = 1.9259629911266175e-8f, LN2 = 0.6931471805599453f;
+    c = -lse * L2E;
+    k = 1.f;
+    if constexpr (EXACT) {
+      const float lo = __builtin_fmaf(-lse, L2E, -c) - lse * L2E_LO;
+      k = c > -INFINITY ? __builtin_fmaf(lo, LN2, 1.f) : 1.f;   // (no entries: lse is +inf)
+    }
+  }
+  __device__ __forceinline__ float operator()(float l, float scale_l2e) const { return __builtin_amdgcn_exp2f(__builtin_fmaf(l, scale_l2e, c)); }
+};
 
 template <int CTRL> __device__ __forceinline__ float dpp_f(float v) {
   return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, false));
@@ -57,10 +66,10 @@ template <bool TEACH, bool GRAD> __device__ __forceinline__ VocabRow vocab_row(c
 
 // Statistics of the 64 staged rows, four lanes per row (every fourth vector of four columns each); row0: the first row,
 // left: rows inside, ncols: columns inside.
-template <int BM, bool TEACH, bool ARG>
+template <bool TEACH, bool ARG>
 __device__ __forceinline__ void vocab_stats64(const VocabEpi& e, const float* stage, int LD, const VocabRow* rows, int row0, int left,
                                               int n0, int ncols) {
-  constexpr int NV = BM / 16, XOR1 = 0xB1, XOR2 = 0x4E;
+  constexpr int BM = 64, NV = BM / 16, XOR1 = 0xB1, XOR2 = 0x4E;
   constexpr float L2E = 1.4426950408889634f;
   const int tid = threadIdx.x, r = tid >> 2, part = tid & 3;
   const float* row = stage + r * LD;
@@ -136,11 +145,10 @@ __device__ __forceinline__ void vocab_stats64(const VocabEpi& e, const float* st
 }
 
 // dl / alpha of the 64 staged rows; cs: the thread's column sums.  256 threads, BM / 4 per row.
-// One term (bf16): one fused multiply-add and one v_exp_f32 per probability, |l| 2^-23 off, 2^-8 is rounded away.  Three: vocab_exp.
-template <int BM, bool TEACH, int TERMS>
+template <bool TEACH, int TERMS>
 __device__ __forceinline__ void vocab_grad64(const VocabEpi& e, float* stage, int LD, const VocabRow* rows, int row0, int left, int n0,
                                              int ncols, f32x4_t& cs) {
-  constexpr int VPR = BM / 4, RP = 256 / VPR, NR = 64 / RP;
+  constexpr int BM = 64, VPR = BM / 4, RP = 256 / VPR, NR = 64 / RP;
   constexpr float L2E = 1.4426950408889634f;
   const int tid = threadIdx.x, cv = (tid % VPR) * 4, col = n0 + cv;
   const float scale_t = L2E * e.inv_tau;
@@ -148,16 +156,13 @@ __device__ __forceinline__ void vocab_grad64(const VocabEpi& e, float* stage, in
     const f32x4_t l = *reinterpret_cast<const f32x4_t*>(stage + r * LD + cv);
     const VocabRow q = rows[r];
     f32x4_t v;
-    const float c1 = -q.c * L2E, ct = -q.ct * L2E;
+    const RowExp<TERMS == 3> e1(q.c), et(q.ct);
+    const float a1 = e.a1 * e1.k, a2 = e.a2 * et.k;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-      const float lc = l[c];
-      float d = TERMS == 1 ? __builtin_amdgcn_exp2f(__builtin_fmaf(lc, L2E, c1)) : vocab_exp(lc - q.c);
-      if constexpr (TEACH) {
-        const float dt = TERMS == 1 ? __builtin_amdgcn_exp2f(__builtin_fmaf(lc, scale_t, ct)) : vocab_exp(lc * e.inv_tau - q.ct);
-        d = e.a1 * d + e.a2 * dt;
-      }
-      v[c] = d;
+      const float p = e1(l[c], L2E);
+      if constexpr (TEACH) v[c] = a1 * p + a2 * et(l[c], scale_t);
+      else v[c] = TERMS == 3 ? e1.k * p : p;
     }
     const int at = q.y - e.v0 - col;
     if ((uint32_t)at < 4u) {

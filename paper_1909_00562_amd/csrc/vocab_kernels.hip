@@ -149,10 +149,10 @@ __global__ __launch_bounds__(1024) void vocab_teacher_kernel(VocabTeacher p) {
   __shared__ int wsum[16];
   const int R = row_count(p.n_act, p.N), g = blockIdx.x;
   if (g * kVocabGroup >= R) return;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, K = p.K, r = g * kVocabGroup + wave;
-  int* ids = reinterpret_cast<int*>(smem) + wave * K;
-  float* prob = reinterpret_cast<float*>(smem) + 16 * K + wave * K;
-  int* hist = reinterpret_cast<int*>(smem) + 32 * K;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, K = p.K, K4 = (K + 3) & ~3, r = g * kVocabGroup + wave;
+  int* ids = reinterpret_cast<int*>(smem) + wave * K4;
+  float* prob = reinterpret_cast<float*>(smem) + 16 * K4 + wave * K4;
+  int* hist = reinterpret_cast<int*>(smem) + 32 * K4;
   for (int i = tid; i < p.strips; i += 1024) hist[i] = 0;
   constexpr int PER = kTeacherMaxK / 64;
   int id[PER];
@@ -166,9 +166,8 @@ __global__ __launch_bounds__(1024) void vocab_teacher_kernel(VocabTeacher p) {
   for (int j = 0; j < PER; ++j) {
     const int k = lane + 64 * j;
     id[j] = row && k < K ? p.ids[at + k] : -1;
-    in[j] = id[j] >= 0 && id[j] < p.V;
-    z[j] = in[j] ? p.logits[at + k] : -INFINITY;
-    in[j] = in[j] && z[j] != -INFINITY;
+    z[j] = row && k < K ? p.logits[at + k] : -INFINITY;   // (not used where the id is none)
+    in[j] = id[j] >= 0 && id[j] < p.V && z[j] != -INFINITY;
     if (!in[j]) id[j] = -1;
     any = any || in[j];
     top = in[j] ? fmaxf(top, z[j]) : top;
@@ -189,7 +188,7 @@ __global__ __launch_bounds__(1024) void vocab_teacher_kernel(VocabTeacher p) {
   for (int j = 0; j < PER; ++j) {
     P[j] = in[j] ? P[j] * inv : 0.f;
     if (P[j] != 0.f) plp += P[j] * (z[j] - log_sum);   // (NaN stays)
-    if (lane + 64 * j < K) {
+    if (lane + 64 * j < K4) {
       ids[lane + 64 * j] = id[j];
       prob[lane + 64 * j] = P[j];
     }
@@ -205,16 +204,20 @@ __global__ __launch_bounds__(1024) void vocab_teacher_kernel(VocabTeacher p) {
     first[j] = in[j];
     P[j] = 0.f;
   }
-#pragma unroll 4
-  for (int k = 0; k < K; ++k) {
-    const int o = ids[k];
-    const float q = prob[k];
+  for (int k0 = 0; k0 < K4; k0 += 4) {
+    const int4 o4 = *reinterpret_cast<const int4*>(ids + k0);
+    const float4 q4 = *reinterpret_cast<const float4*>(prob + k0);
+    const int o[4] = {o4.x, o4.y, o4.z, o4.w};
+    const float q[4] = {q4.x, q4.y, q4.z, q4.w};
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
       if (64 * j >= K) continue;
-      const bool same = in[j] && o == id[j];
-      P[j] += same ? q : 0.f;
-      first[j] = first[j] && !(same && k < lane + 64 * j);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const bool same = in[j] && o[u] == id[j];
+        P[j] += same ? q[u] : 0.f;
+        first[j] = first[j] && !(same && k0 + u < lane + 64 * j);
+      }
     }
   }
 #pragma unroll
@@ -290,6 +293,25 @@ __global__ __launch_bounds__(1024) void vocab_finish_kernel(VocabFinish p) {
   const int R = row_count(p.n_act, p.N), tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int row0 = blockIdx.x * RPB, r = row0 + tid % RPB, phase = tid / RPB;
   if (row0 < R) {
+    // A wave per row of the teacher's entries: their probabilities' sum and that of p l / tau, ahead of what log q needs besides
+    constexpr int RW = RPB / 16;
+    float pl[RW] = {}, ps[RW] = {};
+    if (TEACH && p.last) {
+#pragma unroll
+      for (int j = 0; j < RW; ++j) {
+        const int row = row0 + wave + 16 * j;
+        if (row >= R) continue;
+        for (int k = lane; k < p.K; k += 64) {
+          const int at = p.place[(int64_t)row * p.K + k];
+          if (at < 0) continue;
+          const float q = p.ent_p[at];
+          if (q != 0.f) {
+            pl[j] += q * (p.ent_l[at] * p.inv_tau);
+            ps[j] += q;
+          }
+        }
+      }
+    }
     Stat st{-INFINITY, 0.f, 0.f, INT_MAX};
     if (r < R) {
       for (int i0 = phase; i0 < p.parts; i0 += U * PH) {
@@ -350,32 +372,29 @@ __global__ __launch_bounds__(1024) void vocab_finish_kernel(VocabFinish p) {
         }
       }
     }
-    if (TEACH && p.last) {   // a wave per row
+    if (TEACH && p.last) {
+#pragma unroll
+      for (int j = 0; j < RW; ++j) {
+        pl[j] = wave_sum(pl[j]);
+        ps[j] = wave_sum(ps[j]);
+      }
       __syncthreads();
-#pragma unroll 1
-      for (int j = wave; j < RPB && row0 + j < R; j += 16) {
-        const int row = row0 + j;
-        float pl = 0.f;
-        for (int k = lane; k < p.K; k += 64) {
-          const int at = p.place[(int64_t)row * p.K + k];
-          if (at < 0) continue;
-          const float q = p.ent_p[at];
-          if (q != 0.f) pl += q * (p.ent_l[at] * p.inv_tau - sh_tau[j]);
-        }
-        pl = wave_sum(pl);
-        if (lane == 0) {
-          const float d = p.seen[row] ? p.tau2 * (p.p_log_p[row] - pl) : 0.f;
-          __hip_atomic_store(p.distill_ws + row, d, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-          if (p.tok_distill) p.tok_distill[p.rows[row]] = d;
-        }
+#pragma unroll
+      for (int j = 0; j < RW; ++j) {
+        const int row = row0 + wave + 16 * j;
+        if (row >= R || lane != 0) continue;
+        const float lt = sh_tau[wave + 16 * j], d = lt < INFINITY ? p.tau2 * (p.p_log_p[row] - (pl[j] - ps[j] * lt)) : 0.f;
+        __hip_atomic_store(p.distill_ws + row, d, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (p.tok_distill) p.tok_distill[p.rows[row]] = d;
       }
     }
   }
-  if (!p.last) return;
-  if (gridDim.x > 1) {
+  const int blocks = R > 0 ? (R + RPB - 1) / RPB : 1;   // with rows; the others are done
+  if (!p.last || (int)blockIdx.x >= blocks) return;
+  if (blocks > 1) {
     __builtin_amdgcn_s_waitcnt(0);   // the wave's losses are where every XCD sees them (stored past the caches)
     __syncthreads();
-    if (tid == 0) last_block = __hip_atomic_fetch_add(p.ticket, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
+    if (tid == 0) last_block = __hip_atomic_fetch_add(p.ticket, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == blocks - 1;
     __syncthreads();
     if (!last_block) return;
   } else {
@@ -409,12 +428,22 @@ __global__ __launch_bounds__(1024) void vocab_finish_kernel(VocabFinish p) {
 }
 
 // ---- gradients on their way out ------------------------------------------------------------------
-// 2^tpr_log threads per row of dh; further blocks for db, 256 words each
+// 2^tpr_log threads per row of dh; further blocks for db: 64 words each, four phases of every fourth part of the rows, eight loads
+// together, the phases in order
 template <typename TE, int VEC>
 __global__ __launch_bounds__(256) void vocab_out_grads_kernel(VocabOutGrads p, int tpr_log, int row_blocks) {
   if ((int)blockIdx.x >= row_blocks) {
-    const int v = ((int)blockIdx.x - row_blocks) * 256 + threadIdx.x;
-    if (v < p.V) st_elem<TE>(reinterpret_cast<TE*>(p.db), v, p.alpha * p.sums[v]);
+    __shared__ float red[4][64];
+    const int c = threadIdx.x & 63, phase = threadIdx.x >> 6, v = ((int)blockIdx.x - row_blocks) * 64 + c;
+    const int parts = (row_count(p.n_act, p.N) + p.sum_rows - 1) / p.sum_rows;
+    float s = 0.f;
+    if (v < p.V) {
+#pragma unroll 8
+      for (int i = phase; i < parts; i += 4) s += p.sums[(int64_t)i * p.ld_sums + v];
+    }
+    red[phase][c] = s;
+    __syncthreads();
+    if (phase == 0 && v < p.V) st_elem<TE>(reinterpret_cast<TE*>(p.db), v, p.alpha * (((red[0][c] + red[1][c]) + red[2][c]) + red[3][c]));
     return;
   }
   const int64_t n = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> tpr_log;
@@ -455,7 +484,7 @@ hipError_t launch_vocab_terms(const float* src, int rows, int H, uint16_t* dst, 
 }
 
 hipError_t launch_vocab_teacher(const VocabTeacher& p, hipStream_t st) {
-  const int smem = (32 * p.K + p.strips) * 4;
+  const int smem = (32 * ((p.K + 3) / 4 * 4) + p.strips) * 4;
   static LdsLimit limit;
   const hipError_t e = limit.raise(reinterpret_cast<const void*>(vocab_teacher_kernel), 128 * 1024);
   if (e != hipSuccess) return e;
@@ -468,16 +497,15 @@ hipError_t launch_vocab_finish(const VocabFinish& p, hipStream_t st) {
   // Few rows: more threads per row, since a row's parts are read one after the other.
 #define ASX_FINISH(RPB, TEACH, ARG) \
   hipLaunchKernelGGL((vocab_finish_kernel<RPB, TEACH, ARG>), dim3((p.N + RPB - 1) / RPB), dim3(1024), 0, st, p)
-  if (p.stat_tau) {
-    if (p.N <= 8192) ASX_FINISH(16, true, false);
-    else ASX_FINISH(64, true, false);
-  } else if (p.stat_idx) {
-    if (p.N <= 8192) ASX_FINISH(16, false, true);
-    else ASX_FINISH(64, false, true);
-  } else {
-    if (p.N <= 8192) ASX_FINISH(16, false, false);
-    else ASX_FINISH(64, false, false);
-  }
+#define ASX_FINISH_OF(TEACH, ARG)               \
+  do {                                          \
+    if (p.N <= 1024) ASX_FINISH(16, TEACH, ARG); \
+    else ASX_FINISH(32, TEACH, ARG);            \
+  } while (0)
+  if (p.stat_tau) ASX_FINISH_OF(true, false);
+  else if (p.stat_idx) ASX_FINISH_OF(false, true);
+  else ASX_FINISH_OF(false, false);
+#undef ASX_FINISH_OF
 #undef ASX_FINISH
   return hipGetLastError();
 }
@@ -485,7 +513,7 @@ hipError_t launch_vocab_finish(const VocabFinish& p, hipStream_t st) {
 hipError_t launch_vocab_out_grads(const VocabOutGrads& p, bool bf16, hipStream_t st) {
   const bool vec = p.H % 4 == 0;   // (bf16 rows: H % 8 == 0)
   const int log = threads_log(vec ? p.H / 4 : p.H);
-  const int row_blocks = (int)((((int64_t)p.N << log) + 255) / 256), blocks = row_blocks + (p.db ? (p.V + 255) / 256 : 0);
+  const int row_blocks = (int)((((int64_t)p.N << log) + 255) / 256), blocks = row_blocks + (p.db ? (p.V + 63) / 64 : 0);
   if (bf16) hipLaunchKernelGGL((vocab_out_grads_kernel<uint16_t, 4>), dim3(blocks), dim3(256), 0, st, p, log, row_blocks);
   else if (vec) hipLaunchKernelGGL((vocab_out_grads_kernel<float, 4>), dim3(blocks), dim3(256), 0, st, p, log, row_blocks);
   else hipLaunchKernelGGL((vocab_out_grads_kernel<float, 1>), dim3(blocks), dim3(256), 0, st, p, log, row_blocks);
