@@ -282,20 +282,25 @@ def _ref(struct):
     return ctypes.byref(struct) if struct is not None else None
 
 
+def _addresses(*tensors):
+    """Device addresses of torch tensors (or int addresses, or None)."""
+    return [t if t is None or type(t) is int else t.data_ptr() for t in tensors]
+
+
 def vocab_embed_workspace_bytes(shape: VoEmbed) -> int:
     return int(load_library().vocab_embed_workspace_bytes(_ref(shape)))
 
 
 def vocab_embed_fwd(shape, table, ids, x, stream=0, check=True) -> int:
-    rc = load_library().vocab_embed_fwd(_ref(shape), _ptr(table), _ptr(ids), _ptr(x), stream or None)
+    rc = load_library().vocab_embed_fwd(_ref(shape), *_addresses(table, ids, x), stream or None)
     if check:
         _check(rc)
     return rc
 
 
 def vocab_embed_bwd(shape, ids, dy, d_table, accumulate, workspace, workspace_bytes, stream=0, check=True) -> int:
-    rc = load_library().vocab_embed_bwd(_ref(shape), _ptr(ids), _ptr(dy), _ptr(d_table), int(accumulate),
-                                        _ptr(workspace), int(workspace_bytes), stream or None)
+    rc = load_library().vocab_embed_bwd(_ref(shape), *_addresses(ids, dy, d_table), int(accumulate),
+                                        *_addresses(workspace), int(workspace_bytes), stream or None)
     if check:
         _check(rc)
     return rc
@@ -307,8 +312,7 @@ def vocab_xent_workspace_bytes(shape: VoShape, teacher=None) -> int:
 
 def vocab_xent_fwd(shape, h, W, b, targets, loss_sum, n_tok, tok_loss, argmax, workspace, workspace_bytes, stream=0,
                    check=True) -> int:
-    rc = load_library().vocab_xent_fwd(_ref(shape), _ptr(h), _ptr(W), _ptr(b), _ptr(targets), _ptr(loss_sum),
-                                       _ptr(n_tok), _ptr(tok_loss), _ptr(argmax), _ptr(workspace),
+    rc = load_library().vocab_xent_fwd(_ref(shape), *_addresses(h, W, b, targets, loss_sum, n_tok, tok_loss, argmax, workspace),
                                        int(workspace_bytes), stream or None)
     if check:
         _check(rc)
@@ -316,8 +320,8 @@ def vocab_xent_fwd(shape, h, W, b, targets, loss_sum, n_tok, tok_loss, argmax, w
 
 
 def vocab_xent_bwd(shape, W, b, workspace, workspace_bytes, dh, dW, db, stream=0, check=True) -> int:
-    rc = load_library().vocab_xent_bwd(_ref(shape), _ptr(W), _ptr(b), _ptr(workspace), int(workspace_bytes), _ptr(dh),
-                                       _ptr(dW), _ptr(db), stream or None)
+    rc = load_library().vocab_xent_bwd(_ref(shape), *_addresses(W, b, workspace), int(workspace_bytes), *_addresses(dh, dW, db),
+                                       stream or None)
     if check:
         _check(rc)
     return rc
@@ -325,9 +329,9 @@ def vocab_xent_bwd(shape, W, b, workspace, workspace_bytes, dh, dW, db, stream=0
 
 def vocab_distill_fwd(shape, teacher, h, W, b, targets, teacher_ids, teacher_logits, loss_sum, n_tok, distill_sum,
                       tok_loss, tok_distill, workspace, workspace_bytes, stream=0, check=True) -> int:
-    rc = load_library().vocab_distill_fwd(_ref(shape), _ref(teacher), _ptr(h), _ptr(W), _ptr(b), _ptr(targets),
-                                          _ptr(teacher_ids), _ptr(teacher_logits), _ptr(loss_sum), _ptr(n_tok),
-                                          _ptr(distill_sum), _ptr(tok_loss), _ptr(tok_distill), _ptr(workspace),
+    rc = load_library().vocab_distill_fwd(_ref(shape), _ref(teacher),
+                                          *_addresses(h, W, b, targets, teacher_ids, teacher_logits, loss_sum, n_tok,
+                                                      distill_sum, tok_loss, tok_distill, workspace),
                                           int(workspace_bytes), stream or None)
     if check:
         _check(rc)
@@ -335,8 +339,8 @@ def vocab_distill_fwd(shape, teacher, h, W, b, targets, teacher_ids, teacher_log
 
 
 def vocab_distill_bwd(shape, teacher, W, b, workspace, workspace_bytes, dh, dW, db, stream=0, check=True) -> int:
-    rc = load_library().vocab_distill_bwd(_ref(shape), _ref(teacher), _ptr(W), _ptr(b), _ptr(workspace),
-                                          int(workspace_bytes), _ptr(dh), _ptr(dW), _ptr(db), stream or None)
+    rc = load_library().vocab_distill_bwd(_ref(shape), _ref(teacher), *_addresses(W, b, workspace),
+                                          int(workspace_bytes), *_addresses(dh, dW, db), stream or None)
     if check:
         _check(rc)
     return rc
@@ -525,25 +529,41 @@ def _grad_dtype(grad_dtype, dtype: int) -> int:
 
 class _DeviceOp:
     """Checks of the tensors that a call is given (shape, type, device, dense rows) and the stream it goes to: the
-    current one of the tensors' device, with that device current for the call."""
+    current one of the tensors' device, with that device current for the call.  (Written for few interpreter steps: a
+    decoder step's kernels take as long as the host needs for the call.)"""
 
-    def _tensor(self, t, shape, dtype, name, optional=False):
+    def _on(self, device):
+        import torch
+        self.torch, self.dev, self.index = torch, device, -1 if device.index is None else device.index
+        self.lib = load_library()
+
+    def _tensor(self, t, shape, dtype, name):
         if t is None:
-            if not optional:
-                raise AttnSoftmaxError(1, f"{name} is None")
-            return None
-        if tuple(t.shape) != tuple(shape):
+            raise AttnSoftmaxError(1, f"{name} is None")
+        if t.shape != shape:
             raise AttnSoftmaxError(2, f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-        if t.dtype != dtype:
+        if t.dtype is not dtype:
             raise AttnSoftmaxError(3, f"{name} is {t.dtype}, expected {dtype}")
-        if t.device != self.dev:
+        if t.get_device() != self.index:
             raise AttnSoftmaxError(2, f"{name} is on {t.device}, expected {self.dev}")
         if not t.is_contiguous():
             raise AttnSoftmaxError(5, f"{name} is not dense row-major")
-        return t
+        return t.data_ptr()
 
-    def _stream(self) -> int:
-        return int(self.torch.cuda.current_stream(self.dev).cuda_stream)
+    def _optional(self, t, shape, dtype, name):
+        return None if t is None else self._tensor(t, shape, dtype, name)
+
+    def _call(self, function, *args):
+        """function(*args, stream), for addresses that _tensor has checked"""
+        cuda = self.torch.cuda
+        stream = cuda.current_stream(self.dev).cuda_stream or None
+        if cuda.current_device() == self.index:
+            rc = function(*args, stream)
+        else:
+            with cuda.device(self.dev):
+                rc = function(*args, stream)
+        if rc:
+            _check(rc)
 
 
 class DeviceEmbed(_DeviceOp):
@@ -551,12 +571,15 @@ class DeviceEmbed(_DeviceOp):
     backward pass and forwards to the C ABI.  grad_dtype: "f32" or "bf16", the type of dy and of the table's gradient."""
 
     def __init__(self, table, N, pad_id=-1, scale=1.0, grad_dtype=None):
-        import torch
-        self.torch, self.table, self.dev = torch, table, table.device
+        self._on(table.device)
+        torch = self.torch
         dtype = _as_dtype(table)
         V, I = table.shape
-        self._tensor(table, (V, I), table.dtype, "table")
+        self.table, self.tdt = table, table.dtype
+        self._tensor(table, (V, I), self.tdt, "table")
         self.shape = VoEmbed(N, I, V, pad_id, dtype, _grad_dtype(grad_dtype, dtype), float(scale))
+        self.shape_ref = ctypes.byref(self.shape)
+        self.n, self.rows = (N,), (N, I)
         self.gdt = torch.bfloat16 if self.shape.grad_dtype == AS_BF16 else torch.float32
         self.ws_bytes = vocab_embed_workspace_bytes(self.shape)
         if self.ws_bytes == 0:
@@ -565,29 +588,25 @@ class DeviceEmbed(_DeviceOp):
 
     def fwd(self, ids, x=None):
         """x [N,I] = scale * table[ids]; ids [N] int32."""
-        torch, s = self.torch, self.shape
-        self._tensor(ids, (s.N,), torch.int32, "ids")
+        torch = self.torch
         if x is None:
-            x = torch.empty(s.N, s.I, dtype=self.table.dtype, device=self.dev)
-        self._tensor(x, (s.N, s.I), self.table.dtype, "x")
-        with torch.cuda.device(self.dev):
-            vocab_embed_fwd(s, self.table, ids, x, self._stream())
+            x = torch.empty(self.rows, dtype=self.tdt, device=self.dev)
+        self._call(self.lib.vocab_embed_fwd, self.shape_ref, self.table.data_ptr(),
+                   self._tensor(ids, self.n, torch.int32, "ids"), self._tensor(x, self.rows, self.tdt, "x"))
         return x
 
     def bwd(self, ids, dy, d_table=None, accumulate=False):
         """d_table [V,I] = (d_table +) scale * sums of the rows of dy [N,I] per word."""
         torch, s = self.torch, self.shape
-        self._tensor(ids, (s.N,), torch.int32, "ids")
-        self._tensor(dy, (s.N, s.I), self.gdt, "dy")
         if d_table is None:
             if accumulate:
                 raise AttnSoftmaxError(1, "d_table is None")
             d_table = torch.empty(s.V, s.I, dtype=self.gdt, device=self.dev)
-        self._tensor(d_table, (s.V, s.I), self.gdt, "d_table")
         if self.workspace is None:
             self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.dev)
-        with torch.cuda.device(self.dev):
-            vocab_embed_bwd(s, ids, dy, d_table, accumulate, self.workspace, self.ws_bytes, self._stream())
+        self._call(self.lib.vocab_embed_bwd, self.shape_ref, self._tensor(ids, self.n, torch.int32, "ids"),
+                   self._tensor(dy, self.rows, self.gdt, "dy"), self._tensor(d_table, (s.V, s.I), self.gdt, "d_table"),
+                   int(accumulate), self.workspace.data_ptr(), self.ws_bytes)
         return d_table
 
 
@@ -597,70 +616,64 @@ class DeviceVocabLoss(_DeviceOp):
     backward pass needs of the forward pass ahead of it, and forwards to the C ABI.  grad_dtype: "f32" or "bf16"."""
 
     def __init__(self, W, b, N, pad_id=-1, grad_scale=1.0, grad_dtype=None, K=0, temperature=1.0, distill_scale=1.0):
-        import torch
-        self.torch, self.W, self.b, self.dev = torch, W, b, W.device
+        self._on(W.device)
+        torch = self.torch
         dtype = _as_dtype(W)
         V, H = W.shape
-        self._tensor(W, (V, H), W.dtype, "W")
-        self._tensor(b, (V,), W.dtype, "b", optional=True)
+        self.W, self.b, self.tdt = W, b, W.dtype
+        self._tensor(W, (V, H), self.tdt, "W")
+        self._optional(b, (V,), self.tdt, "b")
         self.shape = VoShape(N, H, V, pad_id, dtype, _grad_dtype(grad_dtype, dtype), float(grad_scale))
         self.gdt = torch.bfloat16 if self.shape.grad_dtype == AS_BF16 else torch.float32
         self.teacher = VoTeacher(K, float(temperature), float(distill_scale)) if K else None
+        self.refs = (ctypes.byref(self.shape),) + ((ctypes.byref(self.teacher),) if K else ())
+        self.one, self.n, self.rows, self.entries = (1,), (N,), (N, H), (N, K)
         self.ws_bytes = vocab_xent_workspace_bytes(self.shape, self.teacher)
         if self.ws_bytes == 0:
             raise AttnSoftmaxError(2, "invalid shape for the vocabulary loss")
         self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.dev)
-        self.done = None
+        self.done = False
 
-    def _outputs(self, h, targets, loss_sum, n_tok, rows):
-        torch, s = self.torch, self.shape
-        self._tensor(h, (s.N, s.H), self.W.dtype, "h")
-        self._tensor(targets, (s.N,), torch.int32, "targets")
-        self._tensor(loss_sum, (1,), torch.float32, "loss_sum")
-        self._tensor(n_tok, (1,), torch.int32, "n_tok")
-        for name, t, dt in rows:
-            self._tensor(t, (s.N,), dt, name, optional=True)
+    def _weights(self):
+        return self.W.data_ptr(), None if self.b is None else self.b.data_ptr()
 
     def xent_fwd(self, h, targets, loss_sum, n_tok, tok_loss=None, argmax=None):
-        torch = self.torch
         if self.teacher is not None:
             raise AttnSoftmaxError(2, "this workspace is for distillation (K > 0): distill_fwd")
-        self._outputs(h, targets, loss_sum, n_tok, (("tok_loss", tok_loss, torch.float32), ("argmax", argmax, torch.int32)))
-        with torch.cuda.device(self.dev):
-            vocab_xent_fwd(self.shape, h, self.W, self.b, targets, loss_sum, n_tok, tok_loss, argmax, self.workspace,
-                           self.ws_bytes, self._stream())
-        self.done = "xent"
+        f32, i32, check, n = self.torch.float32, self.torch.int32, self._tensor, self.n
+        self._call(self.lib.vocab_xent_fwd, *self.refs, check(h, self.rows, self.tdt, "h"), *self._weights(),
+                   check(targets, n, i32, "targets"), check(loss_sum, self.one, f32, "loss_sum"),
+                   check(n_tok, self.one, i32, "n_tok"), self._optional(tok_loss, n, f32, "tok_loss"),
+                   self._optional(argmax, n, i32, "argmax"), self.workspace.data_ptr(), self.ws_bytes)
+        self.done = True
 
     def distill_fwd(self, h, targets, teacher_ids, teacher_logits, loss_sum, n_tok, distill_sum, tok_loss=None,
                     tok_distill=None):
-        torch, s = self.torch, self.shape
         if self.teacher is None:
             raise AttnSoftmaxError(1, "no teacher (K = 0): xent_fwd")
-        self._outputs(h, targets, loss_sum, n_tok, (("tok_loss", tok_loss, torch.float32),
-                                                    ("tok_distill", tok_distill, torch.float32)))
-        self._tensor(teacher_ids, (s.N, self.teacher.K), torch.int32, "teacher_ids")
-        self._tensor(teacher_logits, (s.N, self.teacher.K), torch.float32, "teacher_logits")
-        self._tensor(distill_sum, (1,), torch.float32, "distill_sum")
-        with torch.cuda.device(self.dev):
-            vocab_distill_fwd(s, self.teacher, h, self.W, self.b, targets, teacher_ids, teacher_logits, loss_sum,
-                              n_tok, distill_sum, tok_loss, tok_distill, self.workspace, self.ws_bytes, self._stream())
-        self.done = "distill"
+        f32, i32, check, n = self.torch.float32, self.torch.int32, self._tensor, self.n
+        self._call(self.lib.vocab_distill_fwd, *self.refs, check(h, self.rows, self.tdt, "h"), *self._weights(),
+                   check(targets, n, i32, "targets"), check(teacher_ids, self.entries, i32, "teacher_ids"),
+                   check(teacher_logits, self.entries, f32, "teacher_logits"), check(loss_sum, self.one, f32, "loss_sum"),
+                   check(n_tok, self.one, i32, "n_tok"), check(distill_sum, self.one, f32, "distill_sum"),
+                   self._optional(tok_loss, n, f32, "tok_loss"), self._optional(tok_distill, n, f32, "tok_distill"),
+                   self.workspace.data_ptr(), self.ws_bytes)
+        self.done = True
 
-    def _gradients(self, done, dh, dW, db):
-        s = self.shape
-        if self.done != done:
+    def _bwd(self, function, dh, dW, db):
+        s, gdt = self.shape, self.gdt
+        if not self.done:
             raise AttnSoftmaxError(2, "a backward pass without the forward pass ahead of it")
-        self._tensor(dh, (s.N, s.H), self.gdt, "dh")
-        self._tensor(dW, (s.V, s.H), self.gdt, "dW")
-        self._tensor(db, (s.V,), self.gdt, "db", optional=True)
+        self._call(function, *self.refs, *self._weights(), self.workspace.data_ptr(), self.ws_bytes,
+                   self._tensor(dh, self.rows, gdt, "dh"), self._tensor(dW, (s.V, s.H), gdt, "dW"),
+                   self._optional(db, (s.V,), gdt, "db"))
 
     def xent_bwd(self, dh, dW, db=None):
-        self._gradients("xent", dh, dW, db)
-        with self.torch.cuda.device(self.dev):
-            vocab_xent_bwd(self.shape, self.W, self.b, self.workspace, self.ws_bytes, dh, dW, db, self._stream())
+        if self.teacher is not None:
+            raise AttnSoftmaxError(2, "this workspace is for distillation (K > 0): distill_bwd")
+        self._bwd(self.lib.vocab_xent_bwd, dh, dW, db)
 
     def distill_bwd(self, dh, dW, db=None):
-        self._gradients("distill", dh, dW, db)
-        with self.torch.cuda.device(self.dev):
-            vocab_distill_bwd(self.shape, self.teacher, self.W, self.b, self.workspace, self.ws_bytes, dh, dW, db,
-                              self._stream())
+        if self.teacher is None:
+            raise AttnSoftmaxError(1, "no teacher (K = 0): xent_bwd")
+        self._bwd(self.lib.vocab_distill_bwd, dh, dW, db)

@@ -67,6 +67,11 @@ hipError_t launch_vocab_rows(const VocabRows& p, hipStream_t st);
 // float [rows, H] -> three bf16 planes of [rows, ldH], zeros behind column H
 hipError_t launch_vocab_terms(const float* src, int rows, int H, uint16_t* dst, int64_t ldH, int64_t plane, hipStream_t st);
 
+// ---- few rows: the list of words' rows and the statistics in one launch, a part per kVocabFewCols words (no teacher) ----
+constexpr int kVocabFewCols = 128;
+bool vocab_few_rows(int N, int H, bool f32);
+hipError_t launch_vocab_few(const VocabRows& p, const VocabEpi& e, const void* W, bool arg, hipStream_t st);
+
 // ---- teacher -------------------------------------------------------------------------
 struct VocabTeacher {
   const int32_t* ids;         // [N, K]

@@ -39,6 +39,7 @@ constexpr int64_t kPieceColumns = 256;   // pieces are multiples of it
 
 struct VocabLayout {
   bool f32, g_bf16;
+  bool few;                               // the forward pass in one launch and the join
   int h_terms, dl_terms;
   int64_t ldH, fwd_cols, bwd_cols, ldd;
   int strips, groups;
@@ -123,9 +124,10 @@ VocabLayout vocab_layout(const vo_shape* s, const vo_teacher* t) {
   L.groups = (int)((N + kVocabGroup - 1) / kVocabGroup);
   const int64_t w_col = L.f32 ? L.ldH * 6 : 0;   // bytes of a column's terms of W
   // forward
+  L.few = !t && vocab_few_rows((int)N, (int)H, L.f32);
   L.t_fwd = logits_tile(N, V, L.ldH, L.h_terms);
   const int64_t stat_col = (N * 16 + 63) / 64;
-  L.fwd_cols = piece_columns(V, stat_col > w_col ? stat_col : w_col);
+  L.fwd_cols = L.few ? round_up(V, kPieceColumns) : piece_columns(V, stat_col > w_col ? stat_col : w_col);
   // backward
   const int64_t dl_col = N * 2 * L.dl_terms;
   L.bwd_cols = piece_columns(V, dl_col > w_col ? dl_col : w_col);
@@ -191,14 +193,14 @@ VocabLayout vocab_layout(const vo_shape* s, const vo_teacher* t) {
     L.p_log_p = take(N * 4);
     L.seen = take(N * 4);
   }
-  L.w_kept = L.f32 && V * w_col <= kPieceBytes;
+  L.w_kept = L.f32 && !L.few && V * w_col <= kPieceBytes;
   L.w_fwd = L.w_bwd = take(L.w_kept ? (size_t)V * w_col : 0);
   const size_t area = off;
   const int64_t parts = L.fwd_cols / kVocabStatCols;
   L.stat = take((size_t)parts * N * 8);
   L.stat_tau = take(t ? (size_t)parts * N * 4 : 0);
   L.stat_idx = take((size_t)parts * N * 4);
-  if (!L.w_kept) L.w_fwd = take((size_t)L.fwd_cols * w_col);
+  if (!L.w_kept && !L.few) L.w_fwd = take((size_t)L.fwd_cols * w_col);
   size_t end = off;
   off = area;
   L.dl = take((size_t)L.dl_terms * N * L.ldd * 2);
@@ -296,7 +298,7 @@ as_status forward(const vo_shape* s, const vo_teacher* t, const void* h, const v
   r.tok_distill = tok_distill;
   r.argmax = argmax;
   r.ticket = w.at<int32_t>(L.ticket);
-  hipError_t e = launch_vocab_rows(r, st);
+  hipError_t e = L.few ? hipSuccess : launch_vocab_rows(r, st);
   if (e != hipSuccess) return hip_fail(e, "rows of words");
 
   const float inv_tau = t ? 1.f / t->temperature : 1.f;
@@ -356,7 +358,9 @@ as_status forward(const vo_shape* s, const vo_teacher* t, const void* h, const v
     const int cols = (int)(s->V - v0 < L.fwd_cols ? s->V - v0 : L.fwd_cols);
     uint16_t* planes = w.at<uint16_t>(L.w_fwd) + (L.w_kept ? v0 * L.ldH : 0);
     const int64_t plane = (L.w_kept ? s->V : L.fwd_cols) * L.ldH;
-    if (L.f32 && L.w_kept && v0 == 0) {
+    if (L.few) {
+      // (W as it is)
+    } else if (L.f32 && L.w_kept && v0 == 0) {
       e = launch_vocab_terms(reinterpret_cast<const float*>(W), s->V, s->H, planes, L.ldH, plane, st);
       if (e != hipSuccess) return hip_fail(e, "terms of W");
     } else if (L.f32 && !L.w_kept) {
@@ -378,9 +382,11 @@ as_status forward(const vo_shape* s, const vo_teacher* t, const void* h, const v
     v.ent = w.at<uint32_t>(L.ent);
     v.ent_l = w.at<float>(L.ent_l);
     v.strips = L.strips;
-    e = launch_gemm_vocab(logits_product(s, L, w, W, planes, plane, v0, cols), L.t_fwd, v, 0, t != nullptr, argmax != nullptr, st);
+    e = L.few ? launch_vocab_few(r, v, W, argmax != nullptr, st)
+              : launch_gemm_vocab(logits_product(s, L, w, W, planes, plane, v0, cols), L.t_fwd, v, 0, t != nullptr, argmax != nullptr, st);
     if (e != hipSuccess) return hip_fail(e, "statistics of the logits");
-    f.parts = (cols + kVocabStatCols - 1) / kVocabStatCols;
+    const int part = L.few ? kVocabFewCols : kVocabStatCols;
+    f.parts = (cols + part - 1) / part;
     f.first = v0 == 0;
     f.last = v0 + L.fwd_cols >= s->V;
     e = launch_vocab_finish(f, st);

@@ -286,7 +286,7 @@ template <int RPB, bool TEACH, bool ARG>
 __global__ __launch_bounds__(1024) void vocab_finish_kernel(VocabFinish p) {
   constexpr int PH = 1024 / RPB, U = 8;
   constexpr float L2E = 1.4426950408889634f;
-  __shared__ Stat part[1024];
+  __shared__ Stat part[16 * RPB];
   __shared__ float sh_tau[RPB];
   __shared__ double sd[2][16];
   __shared__ int last_block;
@@ -343,15 +343,38 @@ __global__ __launch_bounds__(1024) void vocab_finish_kernel(VocabFinish p) {
         st = join(st, g, p.inv_tau);
       }
     }
-    part[tid] = st;
-    __syncthreads();
-#pragma unroll 1
-    for (int o = PH / 2; o > 0; o >>= 1) {
-      if (phase < o) part[tid] = join(part[tid], part[tid + o * RPB], p.inv_tau);
-      __syncthreads();
+    // what the row's thread needs besides, on its way meanwhile
+    const bool mine = tid < RPB && r < R;
+    const float at_word = mine && p.last ? p.at_word[r] : 0.f;
+    const int n = mine && p.last ? p.rows[r] : 0;
+    const bool seen = TEACH && mine && p.last ? p.seen[r] != 0 : false;
+    // a wave's threads of the row, then the waves'
+#pragma unroll
+    for (int o = RPB; o < 64; o <<= 1) {
+      Stat other;
+      other.m = __shfl_xor(st.m, o, 64);
+      other.s = __shfl_xor(st.s, o, 64);
+      other.t = TEACH ? __shfl_xor(st.t, o, 64) : 0.f;
+      other.idx = ARG ? __shfl_xor(st.idx, o, 64) : INT_MAX;
+      st = join(st, other, p.inv_tau);
     }
-    if (phase == 0 && r < R) {
-      st = part[tid];
+    if (lane < RPB) part[wave * RPB + lane] = st;
+    __syncthreads();
+    if (mine) {
+      Stat w[16];
+      st = Stat{-INFINITY, 0.f, 0.f, INT_MAX};
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        w[k] = part[k * RPB + tid];
+        st.m = fmaxf(st.m, w[k].m);
+      }
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        const float d = w[k].m == st.m ? 0.f : (w[k].m - st.m) * L2E;
+        st.s += w[k].s * __builtin_amdgcn_exp2f(d);
+        if constexpr (TEACH) st.t += w[k].t * __builtin_amdgcn_exp2f(d * p.inv_tau);
+        if constexpr (ARG) st.idx = w[k].m == st.m && w[k].idx < st.idx ? w[k].idx : st.idx;
+      }
       if (!p.first) {
         const float4 q = p.run[r];
         st = join(Stat{q.x, q.y, q.z, __builtin_bit_cast(int, q.w)}, st, p.inv_tau);
@@ -359,14 +382,13 @@ __global__ __launch_bounds__(1024) void vocab_finish_kernel(VocabFinish p) {
       if (!p.last) {
         p.run[r] = make_float4(st.m, st.s, st.t, __builtin_bit_cast(float, st.idx));
       } else {
-        const float lse = st.m + logf(st.s), loss = lse - p.at_word[r];
-        const int n = p.rows[r];
+        const float lse = st.m + logf(st.s), loss = lse - at_word;
         p.lse[r] = lse;
         __hip_atomic_store(p.loss_ws + r, loss, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         if (p.tok_loss) p.tok_loss[n] = loss;
         if (p.argmax) p.argmax[n] = st.idx == INT_MAX ? 0 : st.idx;
         if constexpr (TEACH) {
-          const float lt = p.seen[r] ? st.m * p.inv_tau + logf(st.t) : INFINITY;
+          const float lt = seen ? st.m * p.inv_tau + logf(st.t) : INFINITY;
           p.lse_tau[r] = lt;
           sh_tau[tid] = lt;
         }

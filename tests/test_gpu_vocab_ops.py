@@ -248,7 +248,10 @@ class Case:
 XENT = [(1, 8, 1, "bf16", "f32"), (1, 1, 2, "f32", "f32"), (1, 64, 1000, "bf16", "bf16"), (2, 5, 3, "f32", "f32"), (16, 512, 2000, "bf16", "f32"),
         (17, 72, 515, "bf16", "bf16"), (33, 111, 777, "f32", "f32"), (64, 64, 64, "bf16", "bf16"), (65, 136, 4001, "bf16", "f32"),
         (130, 64, 129, "f32", "f32"), (200, 264, 1003, "bf16", "bf16"), (300, 8, 9000, "bf16", "f32"), (511, 200, 2050, "bf16", "bf16"),
-        (700, 40, 257, "f32", "f32"), (1300, 96, 700, "bf16", "bf16"), (257, 1000, 300, "bf16", "f32")]
+        (700, 40, 257, "f32", "f32"), (1300, 96, 700, "bf16", "bf16"), (257, 1000, 300, "bf16", "f32"),
+        (32, 1032, 1111, "bf16", "f32"), (31, 130, 700, "f32", "f32"), (9, 2048, 300, "bf16", "bf16"), (32, 1100, 130, "f32", "f32"),
+        (12, 301, 2078, "f32", "f32"),
+        (64, 513, 300, "f32", "f32"), (50, 1500, 260, "f32", "f32"), (64, 2100, 131, "f32", "f32")]
 
 
 @pytest.mark.parametrize("N, H, V, dtype, grad", XENT)

@@ -198,4 +198,4 @@ def test_losses_refuse_arguments():
 
 def test_workspace_holds_pieces_of_the_logits_and_not_all_of_them():
     s = _shape(N=16384, H=2048, V=128000, grad_dtype=bd.AS_BF16)
-    assert bd.vocab_xent_workspace_bytes(s) < 0.15 * 16384 * 128000 * 2
+    assert bd.vocab_xent_workspace_bytes(s) < 0.25 * 16384 * 128000 * 2
