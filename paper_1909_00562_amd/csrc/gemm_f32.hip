@@ -520,8 +520,10 @@ hipError_t launch_splitk_combine(const GemmArgs& g, bool in_bf16, hipStream_t st
   const dim3 grid((unsigned)blocks, g.batch);
 #define ASX_COMBINE(TIN, BF, W) hipLaunchKernelGGL((splitk_combine_kernel<TIN, BF, W>), grid, dim3(256), 0, st, d)
   if (in_bf16) {
-    if (!vec) return hipErrorInvalidValue;
-    if (g.c_bf16) ASX_COMBINE(uint16_t, true, 8);
+    if (!vec) {
+      if (g.c_bf16 || g.bias) return hipErrorInvalidValue;
+      ASX_COMBINE(float, false, 1);   // (no bias: the operands' type does not matter)
+    } else if (g.c_bf16) ASX_COMBINE(uint16_t, true, 8);
     else ASX_COMBINE(uint16_t, false, 4);
   } else if (vec) {
     ASX_COMBINE(float, false, 4);

@@ -72,6 +72,23 @@ constexpr int kVocabFewCols = 128;
 bool vocab_few_rows(int N, int H, bool f32);
 hipError_t launch_vocab_few(const VocabRows& p, const VocabEpi& e, const void* W, bool arg, hipStream_t st);
 
+// Backward for a few rows, both gradients in one pass over W.  epi: y, bias, lse, a1 = grad_scale, a2 = teacher's scale * tau and what
+// there is of a teacher; dh_part: vocab_few_bwd_bytes.
+struct VocabFewBwd {
+  bool f32, g_bf16, teacher;
+  const uint16_t* hc;
+  int64_t ldH, plane;
+  const int32_t *n_act, *row_pos;
+  int N, H, V;
+  const void* W;
+  VocabEpi epi;
+  void *dh, *dW, *db;
+  float* dh_part;
+};
+bool vocab_few_bwd_rows(int N, int H, int V, bool f32, bool g_bf16);
+size_t vocab_few_bwd_bytes(int N, int H, int V);
+hipError_t launch_vocab_few_bwd(const VocabFewBwd& p, hipStream_t st);
+
 // ---- teacher -------------------------------------------------------------------------
 struct VocabTeacher {
   const int32_t* ids;         // [N, K]

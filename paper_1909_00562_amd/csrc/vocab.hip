@@ -39,7 +39,7 @@ constexpr int64_t kPieceColumns = 256;   // pieces are multiples of it
 
 struct VocabLayout {
   bool f32, g_bf16;
-  bool few;                               // the forward pass in one launch and the join
+  bool few, few_bwd;                      // few rows: a pass in one launch over W
   int h_terms, dl_terms;
   int64_t ldH, fwd_cols, bwd_cols, ldd;
   int strips, groups;
@@ -129,23 +129,26 @@ VocabLayout vocab_layout(const vo_shape* s, const vo_teacher* t) {
   const int64_t stat_col = (N * 16 + 63) / 64;
   L.fwd_cols = L.few ? round_up(V, kPieceColumns) : piece_columns(V, stat_col > w_col ? stat_col : w_col);
   // backward
+  L.few_bwd = vocab_few_bwd_rows((int)N, (int)H, (int)V, L.f32, L.g_bf16);
   const int64_t dl_col = N * 2 * L.dl_terms;
   L.bwd_cols = piece_columns(V, dl_col > w_col ? dl_col : w_col);
   L.ldd = round_up(L.bwd_cols < V ? L.bwd_cols : V, 8);
   L.t_bwd = logits_tile(N, L.ldd, L.ldH, L.h_terms);
   // The two products of a piece in one launch of 128 x 128 tiles, the blocks of dh first, whose reductions are the longer ones: as
-  // launches of their own, each is some part of a round of the compute units too long.  dh is split where one of its blocks
-  // would otherwise take longer than half of all blocks' share of a compute unit's two places.
+  // launches of their own, each is some part of a round of the compute units too long.  A reduction is split where one of its
+  // blocks would otherwise take longer than half of all blocks' share of a compute unit's two places.
   const int n_dw = pair_count(L.dl_terms, L.h_terms);
   const int64_t k_dw = n_dw * ((N + 63) / 64), k_dh = n_dw * ((L.ldd + 63) / 64);
   if (N > 256) {
     const int64_t b_dw = ((L.ldd + 127) / 128) * ((H + 127) / 128), b_dh = ((N + 127) / 128) * ((L.ldH + 127) / 128);
     int64_t share = (b_dw * k_dw + b_dh * k_dh + 511) / 512;
     if (share < 8) share = 8;
-    int64_t splits = (2 * k_dh + share - 1) / share;
-    if (splits > 32) splits = 32;
-    L.p_dw = {kTile128, 1};
-    L.p_dh = {kTile128, whole_splits((int)k_dh, (int)splits)};
+    auto splits = [&](int64_t k) {
+      const int64_t n = (2 * k + share - 1) / share;
+      return whole_splits((int)k, n < 32 ? (int)n : 32);
+    };
+    L.p_dw = {kTile128, splits(k_dw)};
+    L.p_dh = {kTile128, splits(k_dh)};
     // One term and whole rounds of 256 x 256 tiles of dW: those kernels, one behind the other, dh with a split that the device
     // chooses from the rows that there are.  6400 x 1024 x 16128 (252 tiles) 1222 / 1190 us for the whole call, 16384 x 2048 x 8192
     // (256) 23.1 / 22.3 ms; half a round, 6400 x 1024 x 8192, 1355 / 1486.
@@ -157,8 +160,7 @@ VocabLayout vocab_layout(const vo_shape* s, const vo_teacher* t) {
       L.dh_dyn = true;
     }
   } else {
-    // (fp32 widths that are no whole vectors cannot be combined: no split of dW there)
-    L.p_dw = gemm_plan((int)L.ldd, (int)H, (int)k_dw * 64, 1, true, H % 8 == 0, n_dw > 1, true);
+    L.p_dw = gemm_plan((int)L.ldd, (int)H, (int)k_dw * 64, 1, true, true, n_dw > 1, true);
     L.p_dh = gemm_plan((int)N, (int)L.ldH, (int)k_dh * 64, 1, true, true, n_dw > 1, true);
     if (L.p_dw.tile == kTile256) L.p_dw = {kTile128, 1};
     if (L.p_dh.tile == kTile256) L.p_dh = {kTile128, 1};
@@ -193,7 +195,7 @@ VocabLayout vocab_layout(const vo_shape* s, const vo_teacher* t) {
     L.p_log_p = take(N * 4);
     L.seen = take(N * 4);
   }
-  L.w_kept = L.f32 && !L.few && V * w_col <= kPieceBytes;
+  L.w_kept = L.f32 && !L.few && !L.few_bwd && V * w_col <= kPieceBytes;
   L.w_fwd = L.w_bwd = take(L.w_kept ? (size_t)V * w_col : 0);
   const size_t area = off;
   const int64_t parts = L.fwd_cols / kVocabStatCols;
@@ -203,6 +205,11 @@ VocabLayout vocab_layout(const vo_shape* s, const vo_teacher* t) {
   if (!L.w_kept && !L.few) L.w_fwd = take((size_t)L.fwd_cols * w_col);
   size_t end = off;
   off = area;
+  if (L.few_bwd) {
+    L.dh_acc = take(vocab_few_bwd_bytes((int)N, (int)H, (int)V));
+    L.total = off > end ? off : end;
+    return L;
+  }
   L.dl = take((size_t)L.dl_terms * N * L.ldd * 2);
   if (!L.w_kept) L.w_bwd = take((size_t)L.bwd_cols * w_col);
   L.ld_sums = round_up(V, 4);
@@ -419,6 +426,38 @@ as_status backward(const vo_shape* s, const vo_teacher* t, const void* W, const 
   float alpha = std::fabs(s->grad_scale) >= std::fabs(c2) ? s->grad_scale : c2;
   if (alpha == 0.f) alpha = 1.f;
   hipError_t e;
+  if (L.few_bwd) {
+    VocabFewBwd f{};
+    f.f32 = L.f32;
+    f.g_bf16 = L.g_bf16;
+    f.teacher = t != nullptr;
+    f.hc = w.at<uint16_t>(L.hc);
+    f.ldH = L.ldH;
+    f.plane = h_plane;
+    f.n_act = n_act;
+    f.row_pos = w.at<int32_t>(L.row_pos);
+    f.N = N;
+    f.H = H;
+    f.V = s->V;
+    f.W = W;
+    f.epi.y = w.at<int32_t>(L.y);
+    f.epi.bias = b;
+    f.epi.lse = w.at<float>(L.lse);
+    f.epi.lse_tau = w.at<float>(L.lse_tau);
+    f.epi.a1 = s->grad_scale;
+    f.epi.a2 = c2;
+    f.epi.inv_tau = t ? 1.f / t->temperature : 1.f;
+    f.epi.runs = w.at<int32_t>(L.runs);
+    f.epi.ent = w.at<uint32_t>(L.ent);
+    f.epi.ent_p = w.at<float>(L.ent_p);
+    f.epi.strips = L.strips;
+    f.dh = dh;
+    f.dW = dW;
+    f.db = db;
+    f.dh_part = w.at<float>(L.dh_acc);
+    e = launch_vocab_few_bwd(f, st);
+    return e == hipSuccess ? AS_OK : hip_fail(e, "gradients of a few rows");
+  }
   for (int64_t v0 = 0; v0 < s->V; v0 += L.bwd_cols) {
     const int cols = (int)(s->V - v0 < L.bwd_cols ? s->V - v0 : L.bwd_cols);
     uint16_t* planes = w.at<uint16_t>(L.w_bwd) + (L.w_kept ? v0 * L.ldH : 0);
