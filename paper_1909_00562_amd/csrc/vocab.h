@@ -62,7 +62,9 @@ struct VocabRows {
   float *tok_loss, *tok_distill;         // optional: 0 at padding
   int32_t* argmax;            // optional: pad_id at padding
   int32_t* ticket;            // cleared
+  int32_t* chunk_words;       // words of every kRowsChunk positions, or null: not more than kRowsDirect of them
 };
+constexpr int kRowsChunk = 8192, kRowsDirect = 32768;
 hipError_t launch_vocab_rows(const VocabRows& p, hipStream_t st);
 // float [rows, H] -> three bf16 planes of [rows, ldH], zeros behind column H
 hipError_t launch_vocab_terms(const float* src, int rows, int H, uint16_t* dst, int64_t ldH, int64_t plane, hipStream_t st);

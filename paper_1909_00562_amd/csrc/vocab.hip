@@ -47,7 +47,7 @@ struct VocabLayout {
   GemmPlan p_dw, p_dh;
   bool dh_dyn = false;
   // kept from the forward to the backward pass
-  size_t rows, row_pos, y, n_act, ticket, hc, lse, lse_tau, at_word, loss_ws, distill_ws, run;
+  size_t rows, row_pos, chunk_words, y, n_act, ticket, hc, lse, lse_tau, at_word, loss_ws, distill_ws, run;
   size_t runs, ent, ent_p, ent_l, place, p_log_p, seen;
   // one area for the pieces of either pass
   size_t stat, stat_tau, stat_idx, w_fwd;
@@ -174,6 +174,7 @@ VocabLayout vocab_layout(const vo_shape* s, const vo_teacher* t) {
   const int64_t Np = round_up(N, kVocabRowPad);
   L.rows = take(N * 4);
   L.row_pos = take(N * 4);
+  L.chunk_words = take(N > kRowsDirect ? (N + kRowsChunk - 1) / kRowsChunk * 4 : 0);
   L.y = take(Np * 4);
   L.n_act = take(16);
   L.ticket = take(16);
@@ -305,6 +306,7 @@ as_status forward(const vo_shape* s, const vo_teacher* t, const void* h, const v
   r.tok_distill = tok_distill;
   r.argmax = argmax;
   r.ticket = w.at<int32_t>(L.ticket);
+  r.chunk_words = N > kRowsDirect ? w.at<int32_t>(L.chunk_words) : nullptr;
   hipError_t e = L.few ? hipSuccess : launch_vocab_rows(r, st);
   if (e != hipSuccess) return hip_fail(e, "rows of words");
 

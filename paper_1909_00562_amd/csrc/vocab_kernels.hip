@@ -17,29 +17,59 @@ __device__ __forceinline__ int row_count(const int32_t* n_act, int N) {
 
 // ---- rows of words --------------------------------------------------------------------
 // 16 positions per block.  A block counts the words ahead of its own by reading all targets there (64 KiB at 16384 positions,
-// from the L2): a list made ahead by one block would be a launch of its own that everything waits for.
+// from the L2): a list made ahead by one block would be a launch of its own that everything waits for.  Behind kRowsDirect positions,
+// where that reading would grow with their square, a launch counts the words of every kRowsChunk ahead (us, direct / counted: 65536
+// positions 33.7 / 21.8, 131072 101 / 34.5; a launch is 5).
 constexpr int kRowsBlock = 16;
 __device__ __forceinline__ bool is_word(int y, int V, int pad_id) { return y >= 0 && y < V && y != pad_id; }
-__global__ __launch_bounds__(256) void vocab_rows_kernel(VocabRows p) {
-  __shared__ int part[4], place[kRowsBlock];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n0 = blockIdx.x * kRowsBlock;
-  int before = 0;
-  for (int i0 = 0; i0 < n0; i0 += 8192) {   // eight loads together
+// words among positions [beg, end), beg % 4 == 0; the sum over the block's 256 threads
+__device__ __forceinline__ int count_words(const VocabRows& p, int beg, int end, int* part) {
+  const int tid = threadIdx.x;
+  int n = 0;
+  for (int i0 = beg; i0 < end; i0 += 8192) {   // eight loads together
     int4 y[8];
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
       const int i = i0 + u * 1024 + tid * 4;
-      y[u] = i < n0 ? *reinterpret_cast<const int4*>(p.targets + i) : make_int4(-1, -1, -1, -1);
+      y[u] = make_int4(-1, -1, -1, -1);
+      if (i + 4 <= end) {
+        y[u] = *reinterpret_cast<const int4*>(p.targets + i);
+      } else if (i < end) {
+        y[u].x = p.targets[i];
+        if (i + 1 < end) y[u].y = p.targets[i + 1];
+        if (i + 2 < end) y[u].z = p.targets[i + 2];
+      }
     }
 #pragma unroll
     for (int u = 0; u < 8; ++u)
-      before += is_word(y[u].x, p.V, p.pad_id) + is_word(y[u].y, p.V, p.pad_id) + is_word(y[u].z, p.V, p.pad_id) + is_word(y[u].w, p.V, p.pad_id);
+      n += is_word(y[u].x, p.V, p.pad_id) + is_word(y[u].y, p.V, p.pad_id) + is_word(y[u].z, p.V, p.pad_id) + is_word(y[u].w, p.V, p.pad_id);
   }
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) before += __shfl_xor(before, o, 64);
-  if (lane == 0) part[wave] = before;
+  for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
+  if ((tid & 63) == 0) part[tid >> 6] = n;
   __syncthreads();
-  before = part[0] + part[1] + part[2] + part[3];
+  return part[0] + part[1] + part[2] + part[3];
+}
+__global__ __launch_bounds__(256) void vocab_count_kernel(VocabRows p) {
+  __shared__ int part[4];
+  const int64_t beg = (int64_t)blockIdx.x * kRowsChunk;
+  const int n = count_words(p, (int)beg, beg + kRowsChunk < p.N ? (int)(beg + kRowsChunk) : p.N, part);
+  if (threadIdx.x == 0) p.chunk_words[blockIdx.x] = n;
+}
+__global__ __launch_bounds__(256) void vocab_rows_kernel(VocabRows p) {
+  __shared__ int part[4], chunk_part[4], place[kRowsBlock];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n0 = blockIdx.x * kRowsBlock;
+  const int chunks = p.chunk_words ? n0 / kRowsChunk : 0;
+  int ahead = 0;   // in whole chunks
+  if (chunks > 0) {
+    for (int i = tid; i < chunks; i += 256) ahead += p.chunk_words[i];
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) ahead += __shfl_xor(ahead, o, 64);
+    if (lane == 0) chunk_part[wave] = ahead;
+    __syncthreads();
+    ahead = chunk_part[0] + chunk_part[1] + chunk_part[2] + chunk_part[3];
+  }
+  const int before = ahead + count_words(p, chunks * kRowsChunk, n0, part);
   if (wave == 0) {
     const int n = n0 + lane;
     const bool in = lane < kRowsBlock && n < p.N;
@@ -423,9 +453,21 @@ __global__ __launch_bounds__(1024) void vocab_finish_kernel(VocabFinish p) {
     __syncthreads();
   }
   double a = 0.0, b = 0.0;
-  for (int i = tid; i < R; i += 1024) {
-    a += (double)__hip_atomic_load(p.loss_ws + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if constexpr (TEACH) b += (double)__hip_atomic_load(p.distill_ws + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  for (int i0 = tid; i0 < R; i0 += 8192) {   // eight loads together
+    float x[8], y[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int i = i0 + u * 1024 < R ? i0 + u * 1024 : i0;
+      x[u] = __hip_atomic_load(p.loss_ws + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      y[u] = TEACH ? __hip_atomic_load(p.distill_ws + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      if (i0 + u * 1024 < R) {
+        a += (double)x[u];
+        b += (double)y[u];
+      }
+    }
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
@@ -494,6 +536,11 @@ int threads_log(int64_t vecs) {
 }  // namespace
 
 hipError_t launch_vocab_rows(const VocabRows& p, hipStream_t st) {
+  if (p.chunk_words) {
+    hipLaunchKernelGGL(vocab_count_kernel, dim3((p.N + kRowsChunk - 1) / kRowsChunk), dim3(256), 0, st, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
   hipLaunchKernelGGL(vocab_rows_kernel, dim3((p.N + kRowsBlock - 1) / kRowsBlock), dim3(256), 0, st, p);
   return hipGetLastError();
 }

@@ -97,6 +97,30 @@ def test_embedding(N, I, V, dtype, grad, pad):
     _untouched(xb, db)
 
 
+# Rows past the caches, offsets past 32 bits (elements, and bytes): against float64 on the GPU.  A sum of n products is off by n 2^-24 of
+# its terms' magnitudes, a bf16 result by 2^-8 of itself.
+@pytest.mark.parametrize("N, I, V, dtype, grad", [(66000, 1020, 900, "f32", "f32"), (20000, 424, 300000, "bf16", "bf16"), (1100000, 2048, 5000, "bf16", "bf16")])
+def test_embedding_of_large_tensors(N, I, V, dtype, grad):
+    gen = torch.Generator(device="cuda").manual_seed(N)
+    t = TYPES[dtype]
+    table = torch.empty(V, I, device="cuda", dtype=t).uniform_(-1, 1, generator=gen)
+    ids = torch.randint(-V // 4, V, (N,), device="cuda", dtype=torch.int32, generator=gen)
+    dy = torch.empty(N, I, device="cuda", dtype=TYPES[grad]).normal_(generator=gen)
+    e = lib.DeviceEmbed(table, N, pad_id=0, scale=2.0, grad_dtype=grad)
+    x, d = e.fwd(ids), e.bwd(ids, dy)
+    od, mag = (torch.zeros(V, I, device="cuda", dtype=torch.float64) for _ in range(2))
+    word = ids > 0
+    for at in torch.arange(N, device="cuda").split(50000):
+        w = word[at][:, None]
+        assert torch.equal(x[at], torch.where(w, table[ids[at].clamp(min=0).long()] * 2, 0))       # (twice a value is exact)
+        k, y = ids[at].clamp(min=0).long(), torch.where(w, dy[at], 0).double() * 2
+        od.index_add_(0, k, y)
+        mag.index_add_(0, k, y.abs())
+    count = torch.bincount(ids[word].long(), minlength=V)[:, None]
+    bound = mag * (count + 4) * U + (od.abs() + mag * (count + 4) * U) * (BF if grad == "bf16" else 0)
+    assert ((d.double() - od).abs() <= bound).all()
+
+
 @pytest.mark.parametrize("N, word", [(1, -1), (50, -1), (50, 3), (16, 3), (17, 3), (16384, 3), (16385, 3), (100000, 3), (100000, -1)])
 def test_embedding_of_one_word_or_none(N, word):
     ids_np = np.full(N, word)
@@ -438,6 +462,51 @@ def test_large(N, H, V, dtype, grad, K):
         off = float((c.out[k].double() - o[k]).norm() / o[k].norm())
         assert off < (2 * BF if grad == "bf16" and k in ("dh", "dW", "db") else 320 * U), (k, off)
     _untouched(*c.bases.values())
+
+
+# past the positions whose words are counted directly
+@pytest.mark.parametrize("N, H, V, dtype, grad, K", [(32768, 8, 21, "bf16", "bf16", 0), (32769, 8, 21, "bf16", "f32", 0), (49154, 5, 40, "f32", "f32", 3)])
+def test_many_positions(N, H, V, dtype, grad, K):
+    c = Case(N, H, V, dtype, grad, K=K, tau=2.0, seed=N)
+    v = c.device()
+    c.fwd(v)
+    c.bwd(v)
+    c.check()
+
+
+def test_rows_past_32_bits():
+    N, H, V, bf = 1100000, 2048, 260, torch.bfloat16
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    W = torch.empty(V, H, device="cuda", dtype=bf).uniform_(-0.06, 0.06, generator=gen)
+    b = torch.empty(V, device="cuda", dtype=bf).uniform_(-1, 1, generator=gen)
+    h = torch.empty(N, H, device="cuda", dtype=bf).uniform_(-1, 1, generator=gen)
+    y = torch.randint(-20, V, (N,), device="cuda", dtype=torch.int32, generator=gen)
+    v = lib.DeviceVocabLoss(W, b, N, pad_id=0, grad_scale=1.0, grad_dtype="bf16")
+    loss, n_tok, tok = torch.empty(1, device="cuda"), torch.empty(1, device="cuda", dtype=torch.int32), torch.empty(N, device="cuda")
+    v.xent_fwd(h, y, loss, n_tok, tok)
+    dh, dW, db = torch.empty_like(h), torch.empty_like(W), torch.empty_like(b)
+    v.xent_bwd(dh, dW, db)
+    assert int(n_tok) == int((y > 0).sum())
+    W64, zero = W.double(), lambda *n: torch.zeros(*n, device="cuda", dtype=torch.float64)  # noqa: E731
+    o_dW, o_db, loss64, off = zero(V, H), zero(V), zero(1), {"tok": zero(2), "dh": zero(2)}
+    for at in torch.arange(N, device="cuda").split(20000):
+        x, t, word = h[at].double(), y[at].clamp(min=0).long()[:, None], (y[at] > 0)[:, None]
+        l = x @ W64.t() + b.double()
+        lse = torch.logsumexp(l, 1, keepdim=True)
+        want = torch.where(word, lse - l.gather(1, t), 0.0)[:, 0]
+        dl = torch.where(word, torch.exp(l - lse).scatter_add_(1, t, torch.full_like(lse, -1.0)), 0.0)
+        o_dW += dl.t() @ x
+        o_db += dl.sum(0)
+        loss64 += want.sum()
+        for k, got, o in (("tok", tok[at], want), ("dh", dh[at], dl @ W64)):
+            off[k] += torch.stack([(got.double() - o).square().sum(), o.square().sum()])
+            assert not got[~word[:, 0]].any()
+    # norms, as in the large cases above
+    assert float((off["tok"][0] / off["tok"][1]).sqrt()) < 320 * U
+    assert float((off["dh"][0] / off["dh"][1]).sqrt()) < 2 * BF
+    for k, got, o in (("dW", dW, o_dW), ("db", db, o_db)):
+        assert float((got.double() - o).norm() / o.norm()) < 2 * BF, k
+    assert abs(float(loss) - float(loss64)) < 1e-5 * float(loss64)
 
 
 # ---- streams, graphs, used together ---------------------------------------------------------------------------------------
