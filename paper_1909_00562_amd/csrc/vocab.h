@@ -69,10 +69,11 @@ hipError_t launch_vocab_rows(const VocabRows& p, hipStream_t st);
 // float [rows, H] -> three bf16 planes of [rows, ldH], zeros behind column H
 hipError_t launch_vocab_terms(const float* src, int rows, int H, uint16_t* dst, int64_t ldH, int64_t plane, hipStream_t st);
 
-// ---- few rows: the list of words' rows and the statistics in one launch, a part per kVocabFewCols words (no teacher) ----
+// ---- few rows: the list of words' rows and the statistics in one launch, a part per kVocabFewCols words; with a teacher, whose lists want
+// the rows of words first, the statistics ----
 constexpr int kVocabFewCols = 128;
-bool vocab_few_rows(int N, int H, bool f32);
-hipError_t launch_vocab_few(const VocabRows& p, const VocabEpi& e, const void* W, bool arg, hipStream_t st);
+bool vocab_few_rows(int N, int H, bool f32, bool teacher);
+hipError_t launch_vocab_few(const VocabRows& p, const VocabEpi& e, const void* W, bool arg, bool teacher, hipStream_t st);
 
 // Backward for a few rows, both gradients in one pass over W.  epi: y, bias, lse, a1 = grad_scale, a2 = teacher's scale * tau and what
 // there is of a teacher; dh_part: vocab_few_bwd_bytes.

@@ -124,7 +124,7 @@ VocabLayout vocab_layout(const vo_shape* s, const vo_teacher* t) {
   L.groups = (int)((N + kVocabGroup - 1) / kVocabGroup);
   const int64_t w_col = L.f32 ? L.ldH * 6 : 0;   // bytes of a column's terms of W
   // forward
-  L.few = !t && vocab_few_rows((int)N, (int)H, L.f32);
+  L.few = vocab_few_rows((int)N, (int)H, L.f32, t != nullptr);
   L.t_fwd = logits_tile(N, V, L.ldH, L.h_terms);
   const int64_t stat_col = (N * 16 + 63) / 64;
   L.fwd_cols = L.few ? round_up(V, kPieceColumns) : piece_columns(V, stat_col > w_col ? stat_col : w_col);
@@ -307,7 +307,7 @@ as_status forward(const vo_shape* s, const vo_teacher* t, const void* h, const v
   r.argmax = argmax;
   r.ticket = w.at<int32_t>(L.ticket);
   r.chunk_words = N > kRowsDirect ? w.at<int32_t>(L.chunk_words) : nullptr;
-  hipError_t e = L.few ? hipSuccess : launch_vocab_rows(r, st);
+  hipError_t e = L.few && !t ? hipSuccess : launch_vocab_rows(r, st);
   if (e != hipSuccess) return hip_fail(e, "rows of words");
 
   const float inv_tau = t ? 1.f / t->temperature : 1.f;
@@ -391,7 +391,7 @@ as_status forward(const vo_shape* s, const vo_teacher* t, const void* h, const v
     v.ent = w.at<uint32_t>(L.ent);
     v.ent_l = w.at<float>(L.ent_l);
     v.strips = L.strips;
-    e = L.few ? launch_vocab_few(r, v, W, argmax != nullptr, st)
+    e = L.few ? launch_vocab_few(r, v, W, argmax != nullptr, t != nullptr, st)
               : launch_gemm_vocab(logits_product(s, L, w, W, planes, plane, v0, cols), L.t_fwd, v, 0, t != nullptr, argmax != nullptr, st);
     if (e != hipSuccess) return hip_fail(e, "statistics of the logits");
     const int part = L.few ? kVocabFewCols : kVocabStatCols;

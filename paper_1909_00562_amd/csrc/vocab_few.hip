@@ -18,34 +18,42 @@ namespace asx {
 namespace {
 
 typedef uint32_t fu32x4_t __attribute__((ext_vector_type(4)));
-constexpr int kFewThreads = 512, kFewWords = kVocabFewCols;
+constexpr int kFewThreads = 512, kFewWords = kVocabFewCols, kFewMost = 128;   // kFewMost: positions
 
 // 16 bytes of a row of W, KS reduction elements per step of 64 lanes
 template <typename TE> struct FewType;
 template <> struct FewType<uint16_t> { static constexpr int kVec = 8, kStep = 32; };
 template <> struct FewType<float> { static constexpr int kVec = 4, kStep = 16; };
 
-template <typename TE, bool ALIGNED> __device__ __forceinline__ fu32x4_t few_load(const TE* row, int k, int H) {
-  constexpr int VEC = FewType<TE>::kVec;
+// A vector as it lies in memory, from inside the row, and what makes elements k .. of it, with zeros behind the row: apart, because what is
+// done to a load's result where it is asked for waits for it there.
+template <typename TE, bool ALIGNED> __device__ __forceinline__ fu32x4_t few_ask(const TE* row, int k, int H) {
   if constexpr (ALIGNED) {   // H % VEC == 0
-    fu32x4_t q = *reinterpret_cast<const fu32x4_t*>(row + (k < H ? k : 0));
-#pragma unroll
-    for (int e = 0; e < 4; ++e) q[e] = k < H ? q[e] : 0u;
-    return q;
-  } else {   // H >= 4, rows start on 4 bytes; the last vector of a row from its end, moved into place
+    return *reinterpret_cast<const fu32x4_t*>(row + (k < H ? k : 0));
+  } else {   // H >= 4, rows start on 4 bytes; the last vector of a row from its end
     static_assert(sizeof(TE) == 4, "bf16 rows are whole vectors");
     typedef fu32x4_t __attribute__((aligned(4))) u32x4_on4_t;
-    const int at = k + 4 <= H ? k : H - 4, by = k < H ? k - at : 0;
-    const fu32x4_t x = *reinterpret_cast<const u32x4_on4_t*>(row + at);
-    fu32x4_t q;
+    return *reinterpret_cast<const u32x4_on4_t*>(row + (k + 4 <= H ? k : H - 4));
+  }
+}
+template <typename TE, bool ALIGNED> __device__ __forceinline__ fu32x4_t few_fit(const fu32x4_t& x, int k, int H) {
+  fu32x4_t q;
+  if constexpr (ALIGNED) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) q[e] = k < H ? x[e] : 0u;
+  } else {
+    const int by = k < H && k + 4 > H ? k + 4 - H : 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const uint32_t x1 = e + 1 < 4 ? x[e + 1 < 4 ? e + 1 : 3] : 0u, x2 = e + 2 < 4 ? x[e + 2 < 4 ? e + 2 : 3] : 0u, x3 = e == 0 ? x[3] : 0u;
       const uint32_t moved = by == 0 ? x[e] : by == 1 ? x1 : by == 2 ? x2 : x3;
       q[e] = k < H ? moved : 0u;
     }
-    return q;
   }
+  return q;
+}
+template <typename TE, bool ALIGNED> __device__ __forceinline__ fu32x4_t few_load(const TE* row, int k, int H) {
+  return few_fit<TE, ALIGNED>(few_ask<TE, ALIGNED>(row, k, H), k, H);
 }
 template <typename TE> __device__ __forceinline__ f32x4_t few_mul(const fu32x4_t& a, const fu32x4_t& b, f32x4_t acc) {
   if constexpr (sizeof(TE) == 2) {
@@ -66,55 +74,69 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// Words' rows 16 NJ blockIdx.y on; dynamic LDS: 16 NJ rows of ldk elements of TE
-template <typename TE, bool ALIGNED, int NJ, bool ARG>
-__global__ __launch_bounds__(kFewThreads) void vocab_few_kernel(VocabRows p, VocabEpi e, const TE* __restrict__ W, int ldk) {
+// Words' rows 16 NJ y on (row_blocks of them); dynamic LDS: 16 NJ rows of ldk elements of TE, with a teacher 16 NJ rows of kDlLd floats at least.
+// The row blocks of the same words follow each other on one XCD: the second one finds W in its L2.
+// With a teacher the list and its rows are there already.
+constexpr int kDlLd = 132;   // floats of a row in LDS of what there is per word: 128 words
+template <typename TE, bool ALIGNED, int NJ, bool ARG, bool TEACH>
+__global__ __launch_bounds__(kFewThreads) void vocab_few_kernel(VocabRows p, VocabEpi e, const TE* __restrict__ W, int ldk, int row_blocks) {
   constexpr int VEC = FewType<TE>::kVec, STEP = FewType<TE>::kStep, U = 8, ROWS = 16 * NJ;
   extern __shared__ __align__(16) unsigned char smem[];
-  __shared__ int from[64], word[64], count;
-  __shared__ float sm[8][ROWS], ss[8][ROWS];
+  __shared__ int from[kFewMost], word[kFewMost], count;
+  __shared__ float sm[8][ROWS], ss[8][ROWS], st[8][TEACH ? ROWS : 1];
   __shared__ int si[8][ROWS];
   TE* hs = reinterpret_cast<TE*>(smem);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane >> 4, c = lane & 15;
   const int H = p.H, nk = (H + STEP - 1) / STEP;
-  const int v0 = blockIdx.x * kFewWords + wave * 16;
+  const int words = (p.V + kFewWords - 1) / kFewWords, slot = blockIdx.x >> 3;
+  const int xb = row_blocks == 1 ? (int)blockIdx.x : slot / row_blocks * 8 + (blockIdx.x & 7), yb = row_blocks == 1 ? 0 : slot % row_blocks;
+  if (xb >= words) return;
+  const int v0 = xb * kFewWords + wave * 16;
   const TE* row = W + (int64_t)(v0 + c < p.V ? v0 + c : p.V - 1) * H;   // words outside repeat the last one
   fu32x4_t wa[U], wb[U];
   auto load = [&](fu32x4_t (&w)[U], int s0) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) w[u] = few_load<TE, ALIGNED>(row, (s0 + u) * STEP + q * VEC, H);
+    for (int u = 0; u < U; ++u) w[u] = few_ask<TE, ALIGNED>(row, (s0 + u) * STEP + q * VEC, H);
   };
-  const int y_lane = lane < p.N ? p.targets[lane] : -1;
+  int y_lane[kFewMost / 64];
+#pragma unroll
+  for (int k = 0; k < kFewMost / 64; ++k) y_lane[k] = lane + 64 * k < p.N ? p.targets[lane + 64 * k] : -1;
   load(wa, 0);
   load(wb, U);
-  if (wave == 0) {   // the words among the positions (at most 64), in order
-    const bool in = lane < p.N;
-    const int y = y_lane;
-    const bool is = in && y >= 0 && y < p.V && y != p.pad_id;
-    const uint64_t m = __ballot(is);
-    const int r = __popcll(m & ((1ull << lane) - 1));
-    if (is) {
-      from[r] = lane;
-      word[r] = y;
-    }
-    if (lane == 0) count = __popcll(m);
-    if (blockIdx.x == 0 && blockIdx.y == 0) {
-      if (in) p.row_pos[lane] = is ? r : -1;
+  if (wave == 0) {   // the words among the positions, in order
+    int before = 0;
+#pragma unroll
+    for (int k = 0; k < kFewMost / 64; ++k) {
+      const int n = lane + 64 * k, y = y_lane[k];
+      const bool in = n < p.N, is = in && y >= 0 && y < p.V && y != p.pad_id;
+      const uint64_t m = __ballot(is);
+      const int r = before + __popcll(m & ((1ull << lane) - 1));
+      before += __popcll(m);
       if (is) {
-        p.rows[r] = lane;
-        p.y[r] = y;
-      } else if (in) {
-        if (p.tok_loss) p.tok_loss[lane] = 0.f;
-        if (p.argmax) p.argmax[lane] = p.pad_id;
+        from[r] = n;
+        word[r] = y;
       }
-      if (lane == 0) {
-        *p.n_act = __popcll(m);
+      if (!TEACH && xb == 0 && yb == 0) {
+        if (in) p.row_pos[n] = is ? r : -1;
+        if (is) {
+          p.rows[r] = n;
+          p.y[r] = y;
+        } else if (in) {
+          if (p.tok_loss) p.tok_loss[n] = 0.f;
+          if (p.argmax) p.argmax[n] = p.pad_id;
+        }
+      }
+    }
+    if (lane == 0) {
+      count = before;
+      if (!TEACH && xb == 0 && yb == 0) {
+        *p.n_act = before;
         *p.ticket = 0;
       }
     }
   }
   lds_barrier();
-  const int r0 = blockIdx.y * ROWS, R = count - r0 < ROWS ? count - r0 : ROWS;   // this block's rows
+  const int r0 = yb * ROWS, R = count - r0 < ROWS ? count - r0 : ROWS;   // this block's rows
   if (R <= 0) return;
   for (int i = tid; i < ROWS * (ldk / VEC); i += kFewThreads) {
     const int r = i / (ldk / VEC), k = (i - r * (ldk / VEC)) * VEC;
@@ -123,7 +145,7 @@ __global__ __launch_bounds__(kFewThreads) void vocab_few_kernel(VocabRows p, Voc
     *reinterpret_cast<fu32x4_t*>(hs + r * ldk + k) = x;
   }
   lds_barrier();
-  for (int r = blockIdx.x; r < R; r += gridDim.x) {   // the rows of words for a backward pass, a block each
+  for (int r = TEACH ? R : xb; r < R; r += words) {   // the rows of words for a backward pass, a block each
     for (int k = tid; k < p.ldH; k += kFewThreads) {
       uint16_t* out = p.hc + (int64_t)(r0 + r) * p.ldH + k;
       if constexpr (sizeof(TE) == 2) {
@@ -138,10 +160,12 @@ __global__ __launch_bounds__(kFewThreads) void vocab_few_kernel(VocabRows p, Voc
   f32x4_t acc[NJ];
 #pragma unroll
   for (int j = 0; j < NJ; ++j) acc[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  auto mul = [&](fu32x4_t (&w)[U], int s0) {   // (steps past the end: w is zero, and LDS is read at its last step)
+  auto mul = [&](fu32x4_t (&w)[U], int s0) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int s = s0 + u < nk ? s0 + u : nk - 1;
+      const int s = s0 + u;
+      if (s >= nk) continue;
+      if ((s + 1) * STEP > H) w[u] = few_fit<TE, ALIGNED>(w[u], s * STEP + q * VEC, H);
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
         acc[j] = few_mul<TE>(w[u], *reinterpret_cast<const fu32x4_t*>(hs + (16 * j + c) * ldk + s * STEP + q * VEC), acc[j]);
@@ -152,12 +176,11 @@ __global__ __launch_bounds__(kFewThreads) void vocab_few_kernel(VocabRows p, Voc
     if (s0 + 2 * U < nk) load(wa, s0 + 2 * U);
     mul(wb, s0 + U);
     if (s0 + 3 * U < nk) load(wb, s0 + 3 * U);
-    else if (s0 + 2 * U < nk) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) wb[u] = fu32x4_t{0u, 0u, 0u, 0u};
-    }
   }
   constexpr float L2E = 1.4426950408889634f;
+  const float scale_t = L2E * e.inv_tau;
+  float* stage = reinterpret_cast<float*>(smem);
+  if constexpr (TEACH) __syncthreads();   // hs has been read
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {   // lane: words v0 + 4 q .. + 3 of position 16 j + c
     float x[4], m = -INFINITY;
@@ -169,18 +192,24 @@ __global__ __launch_bounds__(kFewThreads) void vocab_few_kernel(VocabRows p, Voc
       if (r == y) e.at_word[r0 + n] = x[r];
       m = fmaxf(m, x[r]);
     }
+    if constexpr (TEACH) *reinterpret_cast<f32x4_t*>(stage + n * kDlLd + wave * 16 + 4 * q) = f32x4_t{x[0], x[1], x[2], x[3]};
     m = fmaxf(m, __shfl_xor(m, 16, 64));
     m = fmaxf(m, __shfl_xor(m, 32, 64));
     const float mb = m > -INFINITY ? m : 0.f;
-    float s = 0.f;
+    float s = 0.f, t = 0.f;
     int idx = INT_MAX;
 #pragma unroll
     for (int r = 3; r >= 0; --r) {
       s += __builtin_amdgcn_exp2f((x[r] - mb) * L2E);
+      if constexpr (TEACH) t += __builtin_amdgcn_exp2f((x[r] - mb) * scale_t);
       if constexpr (ARG) idx = x[r] == m ? v0 + 4 * q + r : idx;
     }
     s += __shfl_xor(s, 16, 64);
     s += __shfl_xor(s, 32, 64);
+    if constexpr (TEACH) {
+      t += __shfl_xor(t, 16, 64);
+      t += __shfl_xor(t, 32, 64);
+    }
     if constexpr (ARG) {
       int o = __shfl_xor(idx, 16, 64);
       idx = o < idx ? o : idx;
@@ -190,24 +219,40 @@ __global__ __launch_bounds__(kFewThreads) void vocab_few_kernel(VocabRows p, Voc
     if (q == 0) {
       sm[wave][n] = m;
       ss[wave][n] = s;
+      if constexpr (TEACH) st[wave][n] = t;
       if constexpr (ARG) si[wave][n] = m > -INFINITY ? idx : INT_MAX;
     }
   }
   __syncthreads();
+  if constexpr (TEACH) {   // logits of the entries: strips of 64 words, a wave per strip and group of rows
+    for (int i = wave; i < 2 * NJ; i += 8) {
+      const int g = r0 / kVocabGroup + (i >> 1), strip = xb * (kFewWords / kVocabStrip) + (i & 1);
+      if (16 * (i >> 1) >= R || strip >= e.strips) continue;
+      const int32_t* runs = e.runs + (int64_t)g * (e.strips + 1) + strip;
+      const int end = runs[1];
+      for (int k = runs[0] + lane; k < end; k += 64) {
+        const uint32_t w = e.ent[k];
+        e.ent_l[k] = stage[(16 * (i >> 1) + (int)(w & 15)) * kDlLd + (int)(w >> 4) - xb * kFewWords];
+      }
+    }
+  }
   if (tid >= R) return;
   float m = sm[0][tid];
 #pragma unroll
   for (int w = 1; w < 8; ++w) m = fmaxf(m, sm[w][tid]);
   const float mb = m > -INFINITY ? m : 0.f;
-  float s = 0.f;
+  float s = 0.f, t = 0.f;
   int idx = INT_MAX;
 #pragma unroll
   for (int w = 0; w < 8; ++w) {
-    s += ss[w][tid] * __builtin_amdgcn_exp2f((sm[w][tid] - mb) * L2E);
+    const float d = sm[w][tid] - mb;
+    s += ss[w][tid] * __builtin_amdgcn_exp2f(d * L2E);
+    if constexpr (TEACH) t += st[w][tid] * __builtin_amdgcn_exp2f(d * scale_t);
     if constexpr (ARG) idx = sm[w][tid] == m && si[w][tid] < idx ? si[w][tid] : idx;
   }
-  const int64_t at = (int64_t)blockIdx.x * e.ldr + r0 + tid;
+  const int64_t at = (int64_t)xb * e.ldr + r0 + tid;
   e.stat[at] = make_float2(m, s);
+  if constexpr (TEACH) e.stat_tau[at] = t;
   if constexpr (ARG) e.stat_idx[at] = idx;
 }
 
@@ -216,15 +261,17 @@ int few_ldk(int H, bool f32) {   // whole steps, and 16 bytes that put 16 rows a
   const int step = f32 ? 16 : 32;
   return (H + step - 1) / step * step + (f32 ? 4 : 8);
 }
-template <typename TE, bool ALIGNED, int NJ, bool ARG>
+template <typename TE, bool ALIGNED, int NJ, bool ARG, bool TEACH>
 hipError_t launch_few(const VocabRows& p, const VocabEpi& e, const void* W, hipStream_t st) {
-  auto kfn = vocab_few_kernel<TE, ALIGNED, NJ, ARG>;
+  auto kfn = vocab_few_kernel<TE, ALIGNED, NJ, ARG, TEACH>;
   static LdsLimit limit;
   const hipError_t rc = limit.raise(reinterpret_cast<const void*>(kfn), kFewLds);
   if (rc != hipSuccess) return rc;
-  const int ldk = few_ldk(p.H, sizeof(TE) == 4);
-  hipLaunchKernelGGL(kfn, dim3((p.V + kFewWords - 1) / kFewWords, (p.N + 16 * NJ - 1) / (16 * NJ)), dim3(kFewThreads), (size_t)16 * NJ * ldk * sizeof(TE), st, p, e,
-                     reinterpret_cast<const TE*>(W), ldk);
+  const int ldk = few_ldk(p.H, sizeof(TE) == 4), words = (p.V + kFewWords - 1) / kFewWords, row_blocks = (p.N + 16 * NJ - 1) / (16 * NJ);
+  size_t smem = (size_t)16 * NJ * ldk * sizeof(TE);
+  if (TEACH && smem < (size_t)16 * NJ * kDlLd * 4) smem = (size_t)16 * NJ * kDlLd * 4;
+  const int blocks = row_blocks == 1 ? words : (words + 7) / 8 * 8 * row_blocks;
+  hipLaunchKernelGGL(kfn, dim3(blocks), dim3(kFewThreads), smem, st, p, e, reinterpret_cast<const TE*>(W), ldk, row_blocks);
   return hipGetLastError();
 }
 // tiles of 16 rows per block: all of them, or as many as fit
@@ -234,12 +281,18 @@ int few_tiles(int N, int H, bool f32) {
     if (nj * tile <= most) return nj;
   return 0;
 }
+template <typename TE, bool ALIGNED, int NJ>
+hipError_t launch_few_rows(const VocabRows& p, const VocabEpi& e, const void* W, bool arg, bool teacher, hipStream_t st) {
+  if constexpr (sizeof(TE) == 4)
+    if (teacher) return launch_few<TE, ALIGNED, NJ, false, true>(p, e, W, st);
+  return arg ? launch_few<TE, ALIGNED, NJ, true, false>(p, e, W, st) : launch_few<TE, ALIGNED, NJ, false, false>(p, e, W, st);
+}
 template <typename TE, bool ALIGNED>
-hipError_t launch_few_of(const VocabRows& p, const VocabEpi& e, const void* W, bool arg, hipStream_t st) {
+hipError_t launch_few_of(const VocabRows& p, const VocabEpi& e, const void* W, bool arg, bool teacher, hipStream_t st) {
   const int nj = few_tiles(p.N, p.H, sizeof(TE) == 4);
-  if (nj == 1) return arg ? launch_few<TE, ALIGNED, 1, true>(p, e, W, st) : launch_few<TE, ALIGNED, 1, false>(p, e, W, st);
-  if (nj == 2) return arg ? launch_few<TE, ALIGNED, 2, true>(p, e, W, st) : launch_few<TE, ALIGNED, 2, false>(p, e, W, st);
-  if constexpr (sizeof(TE) == 4) return arg ? launch_few<TE, ALIGNED, 4, true>(p, e, W, st) : launch_few<TE, ALIGNED, 4, false>(p, e, W, st);
+  if (nj == 1) return launch_few_rows<TE, ALIGNED, 1>(p, e, W, arg, teacher, st);
+  if (nj == 2) return launch_few_rows<TE, ALIGNED, 2>(p, e, W, arg, teacher, st);
+  if constexpr (sizeof(TE) == 4) return launch_few_rows<TE, ALIGNED, 4>(p, e, W, arg, teacher, st);
   return hipErrorInvalidValue;
 }
 
@@ -266,17 +319,22 @@ struct FewBwd {
   void *dW, *db;
   float* dh_part;        // [block][16 NJ][ldH]
 };
-constexpr int kDlLd = 132;   // floats of a row of dl in LDS: 128 words
 
-template <typename TE, bool ALIGNED> __device__ __forceinline__ void few_load4(const TE* row, int k, int H, float (&x)[4]) {
-  if constexpr (sizeof(TE) == 2) {   // H % 8 == 0
-    const uint2 q = *reinterpret_cast<const uint2*>(row + (k < H ? k : 0));
-    x[0] = k < H ? lo_bf16(q.x) : 0.f;
-    x[1] = k < H ? hi_bf16(q.x) : 0.f;
-    x[2] = k < H ? lo_bf16(q.y) : 0.f;
-    x[3] = k < H ? hi_bf16(q.y) : 0.f;
+// Four columns of a row, as they lie and as floats (columns behind H are not used: of any value, but not out of the row)
+template <typename TE> struct Four { using type = fu32x4_t; };
+template <> struct Four<uint16_t> { using type = uint2; };
+template <typename TE, bool ALIGNED> __device__ __forceinline__ typename Four<TE>::type few_ask4(const TE* row, int k, int H) {
+  if constexpr (sizeof(TE) == 2) return *reinterpret_cast<const uint2*>(row + (k < H ? k : 0));   // H % 8 == 0
+  else return few_ask<float, ALIGNED>(row, k, H);
+}
+template <typename TE, bool ALIGNED> __device__ __forceinline__ void few_get4(const typename Four<TE>::type& q0, int k, int H, float (&x)[4]) {
+  if constexpr (sizeof(TE) == 2) {
+    x[0] = lo_bf16(q0.x);
+    x[1] = hi_bf16(q0.x);
+    x[2] = lo_bf16(q0.y);
+    x[3] = hi_bf16(q0.y);
   } else {
-    const fu32x4_t q = few_load<float, ALIGNED>(row, k, H);
+    const fu32x4_t q = ALIGNED ? q0 : few_fit<float, ALIGNED>(q0, k, H);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const uint32_t w = q[e];
@@ -303,7 +361,7 @@ __global__ __launch_bounds__(kFewThreads) void vocab_few_bwd_kernel(FewBwd p) {
   const TE* row = W;
   auto load = [&](fu32x4_t (&w)[U], int s0) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) w[u] = few_load<TE, ALIGNED>(row, (s0 + u) * STEP + q * VEC, H);
+    for (int u = 0; u < U; ++u) w[u] = few_ask<TE, ALIGNED>(row, (s0 + u) * STEP + q * VEC, H);
   };
   auto first_loads = [&](int g) {
     const int v = g * 16 + c;
@@ -350,6 +408,7 @@ __global__ __launch_bounds__(kFewThreads) void vocab_few_bwd_kernel(FewBwd p) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           if (s0 + u >= nk) continue;
+          if ((s0 + u + 1) * STEP > H) w[u] = few_fit<TE, ALIGNED>(w[u], (s0 + u) * STEP + q * VEC, H);
 #pragma unroll
           for (int j = 0; j < NJ; ++j) {
             const float* h = hs + (16 * j + c) * ldk + (s0 + u) * STEP + q * VEC;
@@ -466,28 +525,31 @@ __global__ __launch_bounds__(kFewThreads) void vocab_few_bwd_kernel(FewBwd p) {
     lds_barrier();
     // 3. this wave's columns: 64 G from 64 G wave on, column 4 i + e of a group being row i of tile e
     constexpr int AHEAD = G * NJ <= 2 ? 2 : 1;   // words' values asked for while the ones ahead are multiplied, where registers allow
-    float w[AHEAD][G][4][4];
-    auto ask = [&](int i, float (&x)[G][4][4]) {
+    typename Four<TE>::type w[AHEAD][G][4];
+    auto ask = [&](int i, typename Four<TE>::type (&x)[G][4]) {
 #pragma unroll
       for (int g = 0; g < G; ++g)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int v = (base + i) * 16 + 4 * q + r;
-          few_load4<TE, ALIGNED>(W + (int64_t)(v < p.V ? v : p.V - 1) * H, (wave * G + g) * 64 + 4 * c, H, x[g][r]);   // (dl of words outside is 0)
+          x[g][r] = few_ask4<TE, ALIGNED>(W + (int64_t)(v < p.V ? v : p.V - 1) * H, (wave * G + g) * 64 + 4 * c, H);
         }
     };
-    auto times = [&](int i, const float (&x)[G][4][4]) {
+    auto times = [&](int i, const typename Four<TE>::type (&x)[G][4]) {
       f32x4_t dl[NJ];
 #pragma unroll
       for (int j = 0; j < NJ; ++j) dl[j] = *reinterpret_cast<const f32x4_t*>(dlt + (16 * j + c) * kDlLd + 16 * i + 4 * q);
 #pragma unroll
       for (int r = 0; r < 4; ++r)
 #pragma unroll
-        for (int g = 0; g < G; ++g)
+        for (int g = 0; g < G; ++g) {
+          float f[4];
+          few_get4<TE, ALIGNED>(x[g][r], (wave * G + g) * 64 + 4 * c, H, f);
 #pragma unroll
           for (int e = 0; e < 4; ++e)
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) dh[j][g][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[g][r][e], dl[j][r], dh[j][g][e], 0, 0, 0);
+            for (int j = 0; j < NJ; ++j) dh[j][g][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(f[e], dl[j][r], dh[j][g][e], 0, 0, 0);
+        }
     };
     if (wave * G * 64 < H) {
       const int n = g1 - base < 8 ? g1 - base : 8;
@@ -571,12 +633,15 @@ template <typename TE, bool ALIGNED, typename TG, int NJ, int G, bool TEACH> hip
 template <typename TE, bool ALIGNED, typename TG, bool TEACH> hipError_t launch_few_bwd_of(const FewBwd& p, hipStream_t st) {
   const int nj = (p.N + 15) / 16, g = few_bwd_groups(p.H);
   if (nj == 1 && g == 1) return launch_few_bwd<TE, ALIGNED, TG, 1, 1, TEACH>(p, st);
-  if constexpr (sizeof(TE) == 4) {
+  if constexpr (sizeof(TG) == 4) {
     if (nj == 1 && g == 2) return launch_few_bwd<TE, ALIGNED, TG, 1, 2, TEACH>(p, st);
-    if (nj == 1 && g == 4) return launch_few_bwd<TE, ALIGNED, TG, 1, 4, TEACH>(p, st);
     if (nj == 2 && g == 1) return launch_few_bwd<TE, ALIGNED, TG, 2, 1, TEACH>(p, st);
+  }
+  if constexpr (sizeof(TE) == 4) {
+    if (nj == 1 && g == 4) return launch_few_bwd<TE, ALIGNED, TG, 1, 4, TEACH>(p, st);
     if (nj == 2 && g == 2) return launch_few_bwd<TE, ALIGNED, TG, 2, 2, TEACH>(p, st);
-    if (nj <= 4 && g == 1) return launch_few_bwd<TE, ALIGNED, TG, 4, 1, TEACH>(p, st);
+    if (nj == 3 && g == 1) return launch_few_bwd<TE, ALIGNED, TG, 3, 1, TEACH>(p, st);
+    if (nj == 4 && g == 1) return launch_few_bwd<TE, ALIGNED, TG, 4, 1, TEACH>(p, st);
   }
   return hipErrorInvalidValue;
 }
@@ -588,28 +653,29 @@ template <typename TE, bool ALIGNED, typename TG> hipError_t launch_few_bwd_any(
 
 // us, forward, this / the tile kernels behind the list of rows: bf16 1 x 512 x 32000 16.4 / 18.6 (15 of them the host's), 16 x 2048 x 64000
 // 63.2 / 68.1, 32 x 512 x 32000 19.1 / 20.0, past the line 33 - / 20.5; fp32, whose tiles want W as bf16 terms first, 1 x 1024 x 32000
-// 39.4 / 127, 16 x 1024 41.7 / 136, 32 x 512 29.3 / 72.4.
-bool vocab_few_rows(int N, int H, bool f32) {
-  return f32 ? N <= 64 && H >= 4 && few_tiles(N, H, true) > 0 : N <= 32 && 16 * few_tiles(N, H, false) >= N;
+// 39.4 / 127, 32 x 512 29.3 / 72.4, 128 x 256 39.8 / 46.9, 128 x 1024 136 / 150, 128 x 2048 321 / 397; with a teacher 8 x 1024 56.1 / 139, 128 x
+// 1024 160 / 162, 40 x 256 x 4000 38.5 / 35.5.
+bool vocab_few_rows(int N, int H, bool f32, bool teacher) {
+  return f32 ? N <= kFewMost && H >= 4 && few_tiles(N, H, true) > 0 : !teacher && N <= 32 && 16 * few_tiles(N, H, false) >= N;
 }
-hipError_t launch_vocab_few(const VocabRows& p, const VocabEpi& e, const void* W, bool arg, hipStream_t st) {
-  if (!vocab_few_rows(p.N, p.H, p.f32)) return hipErrorInvalidValue;
-  if (!p.f32) return launch_few_of<uint16_t, true>(p, e, W, arg, st);
-  return p.H % 4 == 0 ? launch_few_of<float, true>(p, e, W, arg, st) : launch_few_of<float, false>(p, e, W, arg, st);
+hipError_t launch_vocab_few(const VocabRows& p, const VocabEpi& e, const void* W, bool arg, bool teacher, hipStream_t st) {
+  if (!vocab_few_rows(p.N, p.H, p.f32, teacher)) return hipErrorInvalidValue;
+  if (!p.f32) return launch_few_of<uint16_t, true>(p, e, W, arg, teacher, st);
+  return p.H % 4 == 0 ? launch_few_of<float, true>(p, e, W, arg, teacher, st) : launch_few_of<float, false>(p, e, W, arg, teacher, st);
 }
 
-
-// us, forward and backward, this / the tile kernels: fp32, whose tiles want W as bf16 terms, 1 x 512 x 32000 70 / 134, 16 x 1024 x 32000 148 /
-// 256, 32 x 184 x 112000 137 / 228, 32 x 1024 x 4000 104 / 93; bf16, 16 x 512 x 32000 51.6 / 52.6 (float gradients 54.7 / 65.5), 1 x 184 x
-// 112000 80.6 / 73.5 (89.4 / 97.7), and past the line 16 x 1024 x 32000 94.9 / 82.1 (108 / 108), 32 x 512 x 32000 69.6 / 55.5 (69.8 / 69.7).
+// us, forward and backward, this / the tile kernels: fp32, whose tiles want W as bf16 terms, 1 x 512 x 32000 69 / 135, 16 x 1024 x 32000 143 /
+// 256, 32 x 1024 x 4000 93.4 / 90.8, 48 x 512 x 32000 116 / 159, 64 x 184 x 112000 184 / 281, 64 x 256 x 4000 56.8 / 56.2; bf16, 16 x 512 x 32000 49.4
+// / 53.0, 16 x 184 x 112000 67.6 / 75.2, with float gradients 53.6 / 66.0, 16 x 1024 x 32000 95.4 / 107, 32 x 512 x 32000 65.5 / 70.4, 16 x 1024 x 4000
+// 50.4 / 45.3, and past the line, bf16 gradients, 16 x 1024 x 32000 94.9 / 82.1, 32 x 512 x 32000 69.6 / 55.5.
 bool vocab_few_bwd_rows(int N, int H, int V, bool f32, bool g_bf16) {
-  const int nj = (N + 15) / 16, g = few_bwd_groups(H), tiles = nj == 3 ? 4 : nj;
-  if (!f32) return N <= 16 && H <= 512 && !(g_bf16 && V > 65536);
-  return N <= 64 && H >= 4 && H <= 2048 && tiles * g <= 4 && few_bwd_lds(tiles, H) <= 156 * 1024;
+  const int nj = (N + 15) / 16, g = few_bwd_groups(H);
+  if (!f32) return nj * g <= (g_bf16 ? 1 : 2) && H <= 1024;
+  return N <= 64 && H >= 4 && H <= 2048 && nj * g <= 4 && few_bwd_lds(nj, H) <= 156 * 1024;
 }
 size_t vocab_few_bwd_bytes(int N, int H, int V) {
   const int nj = (N + 15) / 16;
-  return (size_t)few_bwd_blocks(V) * 16 * (nj == 3 ? 4 : nj) * ((H + 7) / 8 * 8) * 4;
+  return (size_t)few_bwd_blocks(V) * 16 * nj * ((H + 7) / 8 * 8) * 4;
 }
 hipError_t launch_vocab_few_bwd(const VocabFewBwd& q, hipStream_t st) {
   if (!vocab_few_bwd_rows(q.N, q.H, q.V, q.f32, q.g_bf16)) return hipErrorInvalidValue;
@@ -642,7 +708,7 @@ hipError_t launch_vocab_few_bwd(const VocabFewBwd& q, hipStream_t st) {
   else if (q.H % 4 == 0) e = launch_few_bwd_any<float, true, float>(p, q.teacher, st);
   else e = launch_few_bwd_any<float, false, float>(p, q.teacher, st);
   if (e != hipSuccess) return e;
-  const int nj = (q.N + 15) / 16, rows = 16 * (nj == 3 ? 4 : nj);
+  const int rows = (q.N + 15) / 16 * 16;
   const dim3 grid((unsigned)((q.ldH + 63) / 64), q.N);
   if (q.g_bf16)
     hipLaunchKernelGGL(vocab_few_dh_kernel<uint16_t>, grid, dim3(256), 0, st, q.dh_part, few_bwd_blocks(q.V), rows, q.ldH, q.row_pos, q.H, reinterpret_cast<uint16_t*>(q.dh));
