@@ -7,7 +7,7 @@
 // (q - p)] as bf16 and its column sums (db), then dW_piece = dl^T h and dh += dl W_piece while dl is still in the caches.
 // Four products of 2 R V H where three would do with the logits kept: what that buys is R V elements of memory.
 //
-// Float gradients: dl as the sum of three bf16 terms (24 bits of mantissa), each in a plane of its own, whose products with the
+// Float gradients, and bf16 ones of few rows: dl as the sum of three bf16 terms (24 bits of mantissa), each in a plane of its own, whose products with the
 // other operand are reduction segments of one launch.  fp32 storage: h and W as three terms too, the six products of terms whose
 // ranks add up to two at most; what is left out is 2^-24 of a product.  The planes of W are made once, or a
 // piece at a time where all of them would take more than a piece may.
@@ -118,7 +118,9 @@ VocabLayout vocab_layout(const vo_shape* s, const vo_teacher* t) {
   L.f32 = s->dtype == AS_F32;
   L.g_bf16 = s->grad_dtype == AS_BF16;
   L.h_terms = L.f32 ? 3 : 1;
-  L.dl_terms = L.g_bf16 ? 1 : 3;
+  // bf16 gradients: one rounding of dl, which sums over many rows average out; those of a few rows do not (2 rows at H = 1288: dW off by
+  // 0.19 % where the rounding on its way out makes 0.11), and up to 16 the kernel that keeps dl in fp32 costs next to nothing.
+  L.dl_terms = L.g_bf16 && N > 16 ? 1 : 3;
   L.ldH = round_up(H, 8);
   L.strips = (int)((V + kVocabStrip - 1) / kVocabStrip);
   L.groups = (int)((N + kVocabGroup - 1) / kVocabGroup);
@@ -267,6 +269,30 @@ GemmArgs logits_product(const vo_shape* s, const VocabLayout& L, const Ws& w, co
 const void* bias_at(const vo_shape* s, const void* b, int64_t v0) {
   if (!b) return nullptr;
   return reinterpret_cast<const unsigned char*>(b) + v0 * (s->dtype == AS_F32 ? 4 : 2);
+}
+
+// dl is kept relative to alpha, a factor of g and s tau.  What all targets have about in common is -g / alpha, and what all
+// of a teacher's entries with the same probability have is -s tau / alpha: the rounding of either to bf16 would be that of them all
+// at once, and no sum averages it out.  (With 1 / n_tok in dl, 2^-9 of dh: 12288 words 0.26 % off for 0.18; 18 rows at temperature 3.4,
+// alpha = s tau, 0.28 % for 0.16.)  So g / alpha is one of the 128 bf16 values of [1, 2), that for which s tau / alpha is the nearest to one.
+struct DlUnit {
+  float alpha, a1, a2;   // dl / alpha = a1 (..) + a2 (..)
+};
+DlUnit dl_unit(float g, float c2) {
+  if (g == 0.f) return c2 == 0.f ? DlUnit{0.f, 1.f, 0.f} : DlUnit{c2, 0.f, 1.f};
+  const float ratio = c2 / g, size = std::fabs(ratio);
+  if (!(size > 0x1p-60f && size < 0x1p60f)) return size < 1.f ? DlUnit{g, 1.f, ratio} : DlUnit{c2, g / c2, 1.f};
+  float best = 1.f, off = 1.f;
+  for (int m = 128; m < 256 && off > 0.f; ++m) {
+    const float x = (float)m / 128.f, a2 = std::fabs(ratio * x);
+    int e;
+    const float f = std::frexp(a2, &e) * 256.f, d = std::fabs(f - std::nearbyint(f)) / f;   // 8 bits of mantissa
+    if (d < off) {
+      off = d;
+      best = x;
+    }
+  }
+  return {g / best, best, ratio * best};
 }
 
 as_status hip_fail(hipError_t e, const char* what) { return set_error(AS_ERR_HIP, "%s: %s", what, hipGetErrorString(e)); }
@@ -422,11 +448,9 @@ as_status backward(const vo_shape* s, const vo_teacher* t, const void* W, const 
   const size_t ge = L.g_bf16 ? 2 : 4;
   int pairs[kMaxSeg][2];
   const int n = term_pairs(L.dl_terms, L.h_terms, pairs);
-  // dl is kept relative to the larger of its two factors: with 1 / n_tok in it, the rounding of -1 / n_tok to bf16 would be that of
-  // all targets at once (2^-9 of dh; 12288 words 0.26 % off for 0.18)
   const float c2 = t ? t->scale * t->temperature : 0.f;
-  float alpha = std::fabs(s->grad_scale) >= std::fabs(c2) ? s->grad_scale : c2;
-  if (alpha == 0.f) alpha = 1.f;
+  const DlUnit unit = dl_unit(s->grad_scale, c2);
+  const float alpha = unit.alpha;
   hipError_t e;
   if (L.few_bwd) {
     VocabFewBwd f{};
@@ -479,8 +503,8 @@ as_status backward(const vo_shape* s, const vo_teacher* t, const void* W, const 
     v.strips = L.strips;
     v.lse = w.at<float>(L.lse);
     v.lse_tau = w.at<float>(L.lse_tau);
-    v.a1 = s->grad_scale / alpha;
-    v.a2 = c2 / alpha;
+    v.a1 = unit.a1;
+    v.a2 = unit.a2;
     v.dl = dl;
     v.ldd = L.ldd;
     v.plane = dl_plane;

@@ -633,12 +633,12 @@ template <typename TE, bool ALIGNED, typename TG, int NJ, int G, bool TEACH> hip
 template <typename TE, bool ALIGNED, typename TG, bool TEACH> hipError_t launch_few_bwd_of(const FewBwd& p, hipStream_t st) {
   const int nj = (p.N + 15) / 16, g = few_bwd_groups(p.H);
   if (nj == 1 && g == 1) return launch_few_bwd<TE, ALIGNED, TG, 1, 1, TEACH>(p, st);
+  if (nj == 1 && g == 2) return launch_few_bwd<TE, ALIGNED, TG, 1, 2, TEACH>(p, st);
   if constexpr (sizeof(TG) == 4) {
-    if (nj == 1 && g == 2) return launch_few_bwd<TE, ALIGNED, TG, 1, 2, TEACH>(p, st);
     if (nj == 2 && g == 1) return launch_few_bwd<TE, ALIGNED, TG, 2, 1, TEACH>(p, st);
   }
+  if (nj == 1 && g == 4) return launch_few_bwd<TE, ALIGNED, TG, 1, 4, TEACH>(p, st);
   if constexpr (sizeof(TE) == 4) {
-    if (nj == 1 && g == 4) return launch_few_bwd<TE, ALIGNED, TG, 1, 4, TEACH>(p, st);
     if (nj == 2 && g == 2) return launch_few_bwd<TE, ALIGNED, TG, 2, 2, TEACH>(p, st);
     if (nj == 3 && g == 1) return launch_few_bwd<TE, ALIGNED, TG, 3, 1, TEACH>(p, st);
     if (nj == 4 && g == 1) return launch_few_bwd<TE, ALIGNED, TG, 4, 1, TEACH>(p, st);
@@ -666,12 +666,13 @@ hipError_t launch_vocab_few(const VocabRows& p, const VocabEpi& e, const void* W
 
 // us, forward and backward, this / the tile kernels: fp32, whose tiles want W as bf16 terms, 1 x 512 x 32000 69 / 135, 16 x 1024 x 32000 143 /
 // 256, 32 x 1024 x 4000 93.4 / 90.8, 48 x 512 x 32000 116 / 159, 64 x 184 x 112000 184 / 281, 64 x 256 x 4000 56.8 / 56.2; bf16, 16 x 512 x 32000 49.4
-// / 53.0, 16 x 184 x 112000 67.6 / 75.2, with float gradients 53.6 / 66.0, 16 x 1024 x 32000 95.4 / 107, 32 x 512 x 32000 65.5 / 70.4, 16 x 1024 x 4000
-// 50.4 / 45.3, and past the line, bf16 gradients, 16 x 1024 x 32000 94.9 / 82.1, 32 x 512 x 32000 69.6 / 55.5.
+// / 53.0, 16 x 184 x 112000 67.6 / 75.2, 16 x 1024 x 32000 82.4 / 82.7 (tiles that round dl once; 102 that do not), 16 x 2048 x 64000 273 / 258,
+// with float gradients 53.6 / 66.0, 74.9 / 100, 98.4 / 107, 328 / 384, 32 x 512 x 32000 65.5 / 70.4, 16 x 1024 x 4000 50.2 / 45.3; past the line, bf16
+// gradients, 32 x 512 x 32000 69.6 / 55.5.
 bool vocab_few_bwd_rows(int N, int H, int V, bool f32, bool g_bf16) {
   const int nj = (N + 15) / 16, g = few_bwd_groups(H);
-  if (!f32) return nj * g <= (g_bf16 ? 1 : 2) && H <= 1024;
-  return N <= 64 && H >= 4 && H <= 2048 && nj * g <= 4 && few_bwd_lds(nj, H) <= 156 * 1024;
+  if (H < 4 || H > 2048 || nj * g > 4 || few_bwd_lds(nj, H) > 156 * 1024) return false;
+  return f32 || nj == 1 || (nj * g == 2 && !g_bf16);
 }
 size_t vocab_few_bwd_bytes(int N, int H, int V) {
   const int nj = (N + 15) / 16;

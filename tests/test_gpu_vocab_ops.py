@@ -277,7 +277,8 @@ XENT = [(1, 8, 1, "bf16", "f32"), (1, 1, 2, "f32", "f32"), (1, 64, 1000, "bf16",
         (12, 301, 2078, "f32", "f32"),
         (64, 513, 300, "f32", "f32"), (50, 1500, 260, "f32", "f32"), (64, 2100, 131, "f32", "f32"),
         (128, 300, 1270, "f32", "f32"), (97, 1201, 140, "f32", "f32"), (66, 3, 50, "f32", "f32"),
-        (32, 504, 700, "bf16", "f32"), (11, 1024, 310, "bf16", "f32"), (48, 500, 900, "f32", "f32")]
+        (32, 504, 700, "bf16", "f32"), (11, 1024, 310, "bf16", "f32"), (48, 500, 900, "f32", "f32"),
+        (16, 2040, 270, "bf16", "bf16"), (5, 1504, 300, "bf16", "f32"), (13, 1000, 310, "bf16", "bf16"), (16, 2056, 140, "bf16", "bf16")]
 
 
 @pytest.mark.parametrize("N, H, V, dtype, grad", XENT)
@@ -355,6 +356,30 @@ def _again(c, z):
     c.h64 = np.where(c.word[:, None], h, 0.0)
     c.teacher = (c.ids, z.astype(np.float64), c.tau, c.s)
     return c
+
+
+@pytest.mark.parametrize("N, H, V, dtype, grad", [(3, 64, 500, "bf16", "f32"), (200, 72, 515, "bf16", "bf16"), (40, 30, 90, "f32", "f32"), (2100, 256, 33000, "bf16", "bf16")])
+def test_a_gradient_of_scale_zero(N, H, V, dtype, grad):
+    c = Case(N, H, V, dtype, grad, g=0.0, seed=4)
+    v = c.device()
+    c.fwd(v)
+    c.bwd(v)
+    for k in ("dh", "dW", "db"):
+        assert not c.out[k].any(), k
+
+
+# The factor that all targets have in common may not be rounded for all of them at once: the part of dh along its exact value is off by
+# less than 2^-10 (probabilities of about 2^-12 that 1 - q rounds away, and independent roundings of 2^-9.3 of 700 entries at least,
+# 2^-14), where g / (s tau) lies half way between two bf16 values (2^-8 of it, and of half of dh).
+@pytest.mark.parametrize("g, s, tau, K", [(1.00390625, 1.0, 2.0, 8), (2.0, 1.00390625, 1.0, 8), (1.0, 0.5, 1.0, 1), (0.7, 0.31, 1.3, 1)])
+def test_factors_are_not_rounded_for_all_rows(g, s, tau, K):
+    c = Case(700, 136, 4001, "bf16", "bf16", K=K, tau=tau, g=g, s=s, pad=0.0, spread=0.1, seed=6)
+    v = c.device()
+    c.fwd(v)
+    c.bwd(v)
+    o = oracle.loss(c.h64, c.W64, c.b64, c.y, c.pad_id, c.g, c.teacher)["dh"]
+    x = c.out["dh"].double().cpu().numpy()
+    assert abs((x * o).sum() / (o * o).sum() - 1) < 2.0 ** -10
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
