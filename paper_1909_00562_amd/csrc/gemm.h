@@ -62,7 +62,7 @@ struct GemmArgs {
   bool pad_out = false;         // columns N .. ldc - 1 of C's rows are padding: they may be written (with anything finite)
   int act_tanh = 0;
   int accumulate = 0;
-  float alpha = 1.f;            // factor of the sums, ahead of the epilogue and of a split's partial sums (not by the two-stage 256x256 kernel)
+  float alpha = 1.f;            // factor of the sums, ahead of the epilogue and of a split's partial sums (B strided; not by the two-stage 256x256 kernel, nor with dropout)
   bool past_caches = false;     // a float result past the caches (64x64 and 128x128 kernels of strided operands, no split)
   uint32_t drop_thr = 0;        // 0 = no dropout
   float drop_scale = 1.f;       // 1 / (1 - p)

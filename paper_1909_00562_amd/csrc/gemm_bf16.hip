@@ -932,11 +932,13 @@ __global__ __launch_bounds__(512) void gemm_bf16_ring_kernel(
       }
     }
     // item done: write it out while the next item's first sub-tiles are already in flight
-    if (p.alpha != 1.f) {
+    if constexpr (!DROP) {
+      if (p.drop_scale != 1.f) {
 #pragma unroll
-      for (int i = 0; i < TM; ++i)
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] *= p.alpha;
+          for (int j = 0; j < TN; ++j) acc[i][j] *= p.drop_scale;
+      }
     }
     void* C_apart = nullptr;
     if constexpr (APART) C_apart = apart.C[it.batch];
@@ -1041,8 +1043,7 @@ static hipError_t gemm_describe(const GemmArgs& g, GemmTile tile, GemmDev& d) {
   d.K = g.K[0];
   d.nseg = g.nseg;
   d.past_caches = g.past_caches;
-  if (g.alpha != 1.f && tile != kTile64 && tile != kTile128 && (!big_tile || g.a_kc || g.b_kc)) return hipErrorInvalidValue;
-  d.alpha = g.alpha;
+  if (g.alpha != 1.f && (g.drop_thr || g.past_caches || g.C_second || g.b_kc || (tile != kTile64 && tile != kTile128 && (!big_tile || g.a_kc)))) return hipErrorInvalidValue;
   d.M = g.M;
   d.N = g.N;
   d.C = g.C;
@@ -1070,7 +1071,7 @@ static hipError_t gemm_describe(const GemmArgs& g, GemmTile tile, GemmDev& d) {
   d.ldg = g.ldg;
   d.act_tanh = g.act_tanh;
   d.drop_thr = g.splits > 1 ? 0u : g.drop_thr;   // with split-K the combine step applies the epilogue
-  d.drop_scale = g.drop_scale;
+  d.drop_scale = g.drop_thr ? g.drop_scale : g.alpha;
   d.drop_seed = g.drop_seed;
   d.accumulate = g.accumulate;
   d.splits = g.splits;

@@ -16,7 +16,6 @@ struct GemmDev {
   int M, N;
   int n_out;   // columns the vector write-out covers: N, or N rounded up to 4 where C's rows have padding
   int past_caches;
-  float alpha;
   void* C;
   uint16_t* C_lo;
   float* C_dact;
@@ -30,7 +29,7 @@ struct GemmDev {
   int64_t ldg;
   int act_tanh, accumulate;
   uint32_t drop_thr;
-  float drop_scale;
+  float drop_scale;   // where nothing is dropped: GemmArgs::alpha
   uint64_t drop_seed;
   int splits;
   float* partial;

@@ -446,11 +446,13 @@ __device__ __forceinline__ void gemm_bf16_tile_block(GemmDev p, int out_bf16, in
     }
     return;
   }
-  if (p.alpha != 1.f) {
+  if constexpr (!BKC && EXTRA == kNoExtra) {   // (the products with a factor of their own)
+    if (!p.drop_thr && p.drop_scale != 1.f) {
 #pragma unroll
-    for (int i = 0; i < TW; ++i)
+      for (int i = 0; i < TW; ++i)
 #pragma unroll
-      for (int j = 0; j < TW; ++j) acc[i][j] *= p.alpha;
+        for (int j = 0; j < TW; ++j) acc[i][j] *= p.drop_scale;
+    }
   }
   constexpr int VPR = BM / 4;                 // groups of four columns per row
   const int col = n0 + (tid % VPR) * 4;
