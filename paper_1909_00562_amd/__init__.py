@@ -1,7 +1,8 @@
 """MI355X-native attention-softmax forward/backward (section 3.2 of the hybrid
-data-model parallel Seq2Seq RNN MT paper), and the stacked-LSTM part that feeds
-it, and the operators over the vocabulary at both ends, as a C-ABI HIP library plus this thin ctypes binding.  Importing the package does not load the library; the first
-call does, and fails loudly if it has not been built."""
+data-model parallel Seq2Seq RNN MT paper), the stacked-LSTM part that feeds it,
+and the operators over the vocabulary at the two ends of a model over words, as a
+C-ABI HIP library plus this thin ctypes binding.  Importing the package does not
+load the library; the first call does, and fails loudly if it has not been built."""
 from .binding import (  # noqa: F401
     AS_BF16, AS_F32, STAGE_NAMES, AsAdam, AsShape, AttnSoftmaxError, DeviceBatch, DeviceEmbed, DeviceLstm,
     DeviceVocabLoss, LsShape, VoEmbed, VoShape, VoTeacher, vocab_distill_bwd, vocab_distill_fwd, vocab_embed_bwd,

@@ -592,7 +592,7 @@ template <typename TG>
 __global__ __launch_bounds__(256) void vocab_few_dh_kernel(const float* __restrict__ part, int parts, int rows, int64_t ldH,
                                                            const int32_t* __restrict__ row_pos, int H, TG* __restrict__ dh) {
   __shared__ f32x4_t red[16][16];
-  const int n = blockIdx.y, r = row_pos[n], t = threadIdx.x & 15, phase = threadIdx.x >> 4, col = blockIdx.x * 64 + 4 * t;
+  const int n = blockIdx.y, at = row_pos[n], r = at < rows ? at : -1, t = threadIdx.x & 15, phase = threadIdx.x >> 4, col = blockIdx.x * 64 + 4 * t;
   f32x4_t s = {0.f, 0.f, 0.f, 0.f};
   if (r >= 0 && col < (int)ldH) {
     const float* from = part + (int64_t)r * ldH + col;

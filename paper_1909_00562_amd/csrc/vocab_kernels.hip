@@ -512,7 +512,7 @@ __global__ __launch_bounds__(256) void vocab_out_grads_kernel(VocabOutGrads p, i
   }
   const int64_t n = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> tpr_log;
   if (n >= p.N) return;
-  const int lane = threadIdx.x & ((1 << tpr_log) - 1), r = p.row_pos[n], H = p.H;
+  const int lane = threadIdx.x & ((1 << tpr_log) - 1), at = p.row_pos[n], r = at < p.N ? at : -1, H = p.H;
   const float* from = p.src + (int64_t)(r < 0 ? 0 : r) * p.ld;
   TE* out = reinterpret_cast<TE*>(p.dh) + n * H;
   for (int c = lane * VEC; c < H; c += VEC << tpr_log) {

@@ -312,6 +312,28 @@ def test_distillation(N, H, V, dtype, grad, K, tau):
     assert all(torch.equal(first[k], c.out[k]) for k in first)
 
 
+@pytest.mark.parametrize("N, H, V, dtype, grad, K", [(2100, 256, 33000, "bf16", "bf16", 0), (5, 64, 300, "f32", "f32", 0), (1, 64, 300, "bf16", "bf16", 4), (700, 72, 515, "bf16", "f32", 3)])
+def test_nothing_but_padding_in_larger_and_smaller_calls(N, H, V, dtype, grad, K):
+    c = Case(N, H, V, dtype, grad, K=K, targets=np.full(N, V))
+    v = c.device()
+    c.fwd(v)
+    c.bwd(v)
+    assert int(c.out["n_tok"]) == 0
+    for k in ("loss_sum", "tok_loss", "dh", "dW", "db") + (("distill_sum", "tok_distill") if K else ()):
+        assert not c.out[k].any(), k
+
+
+@pytest.mark.parametrize("N, H, V, dtype, grad, K", [(2500, 256, 33000, "bf16", "bf16", 0), (2100, 64, 700, "bf16", "bf16", 5), (900, 72, 515, "bf16", "f32", 0), (300, 40, 257, "f32", "f32", 7)])
+def test_a_few_words_among_many_positions(N, H, V, dtype, grad, K):
+    y = np.full(N, -1)
+    y[[0, N // 2, N - 1]] = [1, V - 1, V // 3]
+    c = Case(N, H, V, dtype, grad, K=K, tau=2.0, targets=y, seed=N)
+    v = c.device()
+    c.fwd(v)
+    c.bwd(v)
+    c.check()
+
+
 @pytest.mark.parametrize("K", [0, 6])
 def test_nothing_but_padding(K):
     c = Case(70, 64, 300, "bf16", "f32", K=K, targets=np.full(70, -1))
