@@ -68,7 +68,8 @@ bool shape_ok(const vo_shape* s) {
 }
 bool teacher_ok(const vo_shape* s, const vo_teacher* t) {
   return t->K >= 1 && t->K <= kTeacherMaxK && s->V <= (1 << 20) && round_up(s->N, kVocabGroup) * t->K < ((int64_t)1 << 31) && t->temperature > 0.f &&
-         std::isfinite(t->temperature) && std::isfinite(1.f / t->temperature) && std::isfinite(t->scale);
+         std::isfinite(t->temperature * t->temperature) && std::isfinite(1.f / t->temperature) && std::isfinite(t->scale) &&
+         std::isfinite(t->scale * t->temperature);
 }
 
 // pairs of terms (rank of A, rank of B), the smallest products first
@@ -271,22 +272,26 @@ const void* bias_at(const vo_shape* s, const void* b, int64_t v0) {
   return reinterpret_cast<const unsigned char*>(b) + v0 * (s->dtype == AS_F32 ? 4 : 2);
 }
 
-// dl is kept relative to alpha, a factor of g and s tau.  What all targets have about in common is -g / alpha, and what all
-// of a teacher's entries with the same probability have is -s tau / alpha: the rounding of either to bf16 would be that of them all
-// at once, and no sum averages it out.  (With 1 / n_tok in dl, 2^-9 of dh: 12288 words 0.26 % off for 0.18; 18 rows at temperature 3.4,
-// alpha = s tau, 0.28 % for 0.16.)  So g / alpha is one of the 128 bf16 values of [1, 2), that for which s tau / alpha is the nearest to one.
+// dl is kept relative to alpha, a factor of g and s tau.  What all targets have about in common is g (1 / V - 1) + s tau / V over alpha (of a
+// model that knows nothing; one that does tells its rows apart), and what all entries of teachers with one entry each have is s tau
+// (1 / V - 1) + g / V: the rounding of either to bf16 would be that of them all at once, and no sum averages it out.  (With 1 / n_tok in
+// dl, 2^-9 of dh: 12288 words 0.26 % off for 0.18; 18 rows at temperature 3.4, alpha = s tau, 0.28 % for 0.16.)  So the first is one of
+// the 128 bf16 values of [1, 2), that for which the second is the nearest to one.
 struct DlUnit {
   float alpha, a1, a2;   // dl / alpha = a1 (..) + a2 (..)
 };
-DlUnit dl_unit(float g, float c2) {
+DlUnit dl_unit(float g, float c2, int V) {
   if (g == 0.f) return c2 == 0.f ? DlUnit{0.f, 1.f, 0.f} : DlUnit{c2, 0.f, 1.f};
   const float ratio = c2 / g, size = std::fabs(ratio);
   if (!(size > 0x1p-60f && size < 0x1p60f)) return size < 1.f ? DlUnit{g, 1.f, ratio} : DlUnit{c2, g / c2, 1.f};
-  float best = 1.f, off = 1.f;
+  const float q = 1.f / (float)V;
+  float common = 1.f - q - ratio * q, entry = ratio * (1.f - q) - q;   // times a1
+  if (!(std::fabs(common) > 0x1p-8f)) common = 1.f;
+  float best = 1.f / common, off = 1.f;
   for (int m = 128; m < 256 && off > 0.f; ++m) {
-    const float x = (float)m / 128.f, a2 = std::fabs(ratio * x);
+    const float x = (float)m / 128.f / common;
     int e;
-    const float f = std::frexp(a2, &e) * 256.f, d = std::fabs(f - std::nearbyint(f)) / f;   // 8 bits of mantissa
+    const float f = std::frexp(std::fabs(entry * x), &e) * 256.f, d = std::fabs(f - std::nearbyint(f)) / (f + 1e-30f);   // 8 bits of mantissa
     if (d < off) {
       off = d;
       best = x;
@@ -449,7 +454,7 @@ as_status backward(const vo_shape* s, const vo_teacher* t, const void* W, const 
   int pairs[kMaxSeg][2];
   const int n = term_pairs(L.dl_terms, L.h_terms, pairs);
   const float c2 = t ? t->scale * t->temperature : 0.f;
-  const DlUnit unit = dl_unit(s->grad_scale, c2);
+  const DlUnit unit = dl_unit(s->grad_scale, c2, s->V);
   const float alpha = unit.alpha;
   hipError_t e;
   if (L.few_bwd) {

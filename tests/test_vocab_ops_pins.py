@@ -160,6 +160,14 @@ def test_losses_refuse_teachers(teacher):
     assert bd.vocab_xent_workspace_bytes(_shape(V=(1 << 20) + 1), bd.VoTeacher(4, 1.0, 1.0)) == 0
 
 
+@pytest.mark.parametrize("teacher", [(4, 1e20, 1.0), (4, 1e10, 1e30)])                # tau^2, s tau
+def test_losses_refuse_teachers_whose_factors_overflow(teacher):
+    s, t = _shape(), bd.VoTeacher(*teacher)
+    assert bd.vocab_xent_workspace_bytes(s, t) == 0
+    assert bd.vocab_distill_fwd(s, t, *A[:12], 1 << 50, check=False) == SHAPE
+    assert bd.vocab_distill_bwd(s, t, A[0], A[1], A[2], 1 << 50, A[3], A[4], A[5], check=False) == SHAPE
+
+
 def test_losses_refuse_arguments():
     s, t = _shape(), bd.VoTeacher(4, 2.0, 1.0)
     n, nt = bd.vocab_xent_workspace_bytes(s), bd.vocab_xent_workspace_bytes(s, t)
