@@ -524,6 +524,8 @@ def _as_dtype(t) -> int:
 
 
 def _grad_dtype(grad_dtype, dtype: int) -> int:
+    if grad_dtype not in (None, "f32", "bf16"):
+        raise AttnSoftmaxError(3, f"gradient type {grad_dtype!r}")
     return dtype if grad_dtype is None else AS_BF16 if grad_dtype == "bf16" else AS_F32
 
 
@@ -534,7 +536,9 @@ class _DeviceOp:
 
     def _on(self, device):
         import torch
-        self.torch, self.dev, self.index = torch, device, -1 if device.index is None else device.index
+        if device.type != "cuda":
+            raise AttnSoftmaxError(2, f"tensors are on {device}, expected a GPU")
+        self.torch, self.dev, self.index = torch, device, device.index
         self.lib = load_library()
 
     def _tensor(self, t, shape, dtype, name):

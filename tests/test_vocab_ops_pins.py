@@ -207,3 +207,14 @@ def test_losses_refuse_arguments():
 def test_workspace_holds_pieces_of_the_logits_and_not_all_of_them():
     s = _shape(N=16384, H=2048, V=128000, grad_dtype=bd.AS_BF16)
     assert bd.vocab_xent_workspace_bytes(s) < 0.25 * 16384 * 128000 * 2
+
+
+def test_handles_refuse_tensors_of_the_host_and_types_they_do_not_know():
+    torch = pytest.importorskip("torch")
+    W = torch.zeros(10, 8)
+    with pytest.raises(lib.AttnSoftmaxError, match="AS_ERR_SHAPE"):
+        lib.DeviceEmbed(W, 4)
+    with pytest.raises(lib.AttnSoftmaxError, match="AS_ERR_SHAPE"):
+        lib.DeviceVocabLoss(W, None, 4)
+    with pytest.raises(lib.AttnSoftmaxError, match="AS_ERR_DTYPE"):
+        bd._grad_dtype("fp32", bd.AS_F32)
