@@ -616,6 +616,45 @@ def test_captured_and_replayed(N, K):
         assert torch.equal(got["dt"], dt)
 
 
+# the kernels for few rows, with and without a teacher, and for many positions (words counted ahead, the radix sort)
+@pytest.mark.parametrize("N, H, V, dtype, grad, K", [(40, 60, 700, "f32", "f32", 9), (5, 263, 1003, "f32", "f32", 0), (14, 1000, 500, "bf16", "bf16", 4),
+                                                     (33000, 16, 50, "bf16", "bf16", 0)])
+def test_captured_beside_eager_calls_of_another_handle(N, H, V, dtype, grad, K):
+    c, other = Case(N, H, V, dtype, grad, K=K, tau=2.0, seed=3), Case(N, H, V, dtype, grad, K=K, tau=2.0, seed=5)
+    v, w = c.device(), other.device()
+    e = lib.DeviceEmbed(torch.zeros(V, H, device="cuda", dtype=TYPES[dtype]), N, pad_id=0, scale=2.0, grad_dtype=grad)
+    dt = torch.empty(V, H, device="cuda", dtype=TYPES[grad])
+
+    def step():
+        c.fwd(v)
+        c.bwd(v)
+        e.bwd(c.y_d, c.out["dh"], dt)
+
+    step()
+    torch.cuda.synchronize()
+    names = [k for k in c.out if k in ("loss_sum", "n_tok", "tok_loss", "dh", "dW", "db") or (K and "distill" in k)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    side = torch.cuda.Stream()
+    for k in range(3):
+        c.h_d.copy_(torch.nan_to_num(c.h_d, nan=0.5))
+        c.y_d.copy_(torch.from_numpy(np.roll(c.y, k + 1).astype(np.int32)))
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):                             # meanwhile, from another handle
+            other.fwd(w)
+            other.bwd(w)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = {n: c.out[n].clone() for n in names} | {"dt": dt.clone()}
+        other.check()
+        step()
+        torch.cuda.synchronize()
+        for n in names:
+            assert torch.equal(got[n], c.out[n]), (k, n)
+        assert torch.equal(got["dt"], dt)
+
+
 def test_a_backward_pass_wants_its_forward_pass():
     c = Case(8, 64, 100, "bf16", "f32")
     v = c.device()
