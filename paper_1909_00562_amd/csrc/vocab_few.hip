@@ -74,12 +74,13 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// Words' rows 16 NJ y on (row_blocks of them); dynamic LDS: 16 NJ rows of ldk elements of TE, with a teacher 16 NJ rows of kDlLd floats at least.
+// Words' rows 16 NJ y on (row_blocks of them), kc columns of them in LDS at a time: all, or kFewSteps steps, which is a pass over W less than
+// fewer rows with all of theirs.  Dynamic LDS: 16 NJ rows of ldk elements of TE, with a teacher 16 NJ rows of kDlLd floats at least.
 // The row blocks of the same words follow each other on one XCD: the second one finds W in its L2.
 // With a teacher the list and its rows are there already.
 constexpr int kDlLd = 132;   // floats of a row in LDS of what there is per word: 128 words
 template <typename TE, bool ALIGNED, int NJ, bool ARG, bool TEACH>
-__global__ __launch_bounds__(kFewThreads) void vocab_few_kernel(VocabRows p, VocabEpi e, const TE* __restrict__ W, int ldk, int row_blocks) {
+__global__ __launch_bounds__(kFewThreads) void vocab_few_kernel(VocabRows p, VocabEpi e, const TE* __restrict__ W, int ldk, int kc, int row_blocks) {
   constexpr int VEC = FewType<TE>::kVec, STEP = FewType<TE>::kStep, U = 8, ROWS = 16 * NJ;
   extern __shared__ __align__(16) unsigned char smem[];
   __shared__ int from[kFewMost], word[kFewMost], count;
@@ -138,28 +139,34 @@ __global__ __launch_bounds__(kFewThreads) void vocab_few_kernel(VocabRows p, Voc
   lds_barrier();
   const int r0 = yb * ROWS, R = count - r0 < ROWS ? count - r0 : ROWS;   // this block's rows
   if (R <= 0) return;
-  for (int i = tid; i < ROWS * (ldk / VEC); i += kFewThreads) {
-    const int r = i / (ldk / VEC), k = (i - r * (ldk / VEC)) * VEC;
-    fu32x4_t x = {0u, 0u, 0u, 0u};
-    if (r < R && k < H) x = few_load<TE, ALIGNED>(reinterpret_cast<const TE*>(p.h) + (int64_t)from[r0 + r] * H, k, H);
-    *reinterpret_cast<fu32x4_t*>(hs + r * ldk + k) = x;
-  }
-  lds_barrier();
-  for (int r = TEACH ? R : xb; r < R; r += words) {   // the rows of words for a backward pass, a block each
-    for (int k = tid; k < p.ldH; k += kFewThreads) {
-      uint16_t* out = p.hc + (int64_t)(r0 + r) * p.ldH + k;
-      if constexpr (sizeof(TE) == 2) {
-        *out = hs[r * ldk + k];
-      } else {
-        float x = hs[r * ldk + k];   // (ldk covers ldH)
+  auto columns = [&](int k0) {   // of the rows to LDS, and as the backward pass wants them, a block each
+    const int vecs = kc / VEC;
+    for (int i = tid; i < ROWS * vecs; i += kFewThreads) {
+      const int r = i / vecs, k = (i - r * vecs) * VEC;
+      fu32x4_t x = {0u, 0u, 0u, 0u};
+      if (r < R && k0 + k < H) x = few_load<TE, ALIGNED>(reinterpret_cast<const TE*>(p.h) + (int64_t)from[r0 + r] * H, k0 + k, H);
+      *reinterpret_cast<fu32x4_t*>(hs + r * ldk + k) = x;
+    }
+    lds_barrier();
+    const int end = k0 + kc < p.ldH ? kc : (int)p.ldH - k0;
+    for (int r = TEACH ? R : xb; r < R; r += words) {
+      for (int k = tid; k < end; k += kFewThreads) {
+        uint16_t* out = p.hc + (int64_t)(r0 + r) * p.ldH + k0 + k;
+        if constexpr (sizeof(TE) == 2) {
+          *out = hs[r * ldk + k];
+        } else {
+          float x = hs[r * ldk + k];
 #pragma unroll
-        for (int t = 0; t < 3; ++t) out[t * p.plane] = (uint16_t)bf16_term(x);
+          for (int t = 0; t < 3; ++t) out[t * p.plane] = (uint16_t)bf16_term(x);
+        }
       }
     }
-  }
+  };
+  columns(0);
   f32x4_t acc[NJ];
 #pragma unroll
   for (int j = 0; j < NJ; ++j) acc[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  int first = 0;   // step that LDS begins with
   auto mul = [&](fu32x4_t (&w)[U], int s0) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -168,10 +175,15 @@ __global__ __launch_bounds__(kFewThreads) void vocab_few_kernel(VocabRows p, Voc
       if ((s + 1) * STEP > H) w[u] = few_fit<TE, ALIGNED>(w[u], s * STEP + q * VEC, H);
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
-        acc[j] = few_mul<TE>(w[u], *reinterpret_cast<const fu32x4_t*>(hs + (16 * j + c) * ldk + s * STEP + q * VEC), acc[j]);
+        acc[j] = few_mul<TE>(w[u], *reinterpret_cast<const fu32x4_t*>(hs + (16 * j + c) * ldk + (s - first) * STEP + q * VEC), acc[j]);
     }
   };
   for (int s0 = 0; s0 < nk; s0 += 2 * U) {
+    if ((s0 - first) * STEP == kc) {
+      lds_barrier();   // all waves are through with these columns
+      first = s0;
+      columns(s0 * STEP);
+    }
     mul(wa, s0);
     if (s0 + 2 * U < nk) load(wa, s0 + 2 * U);
     mul(wb, s0 + U);
@@ -257,9 +269,12 @@ __global__ __launch_bounds__(kFewThreads) void vocab_few_kernel(VocabRows p, Voc
 }
 
 constexpr size_t kFewLds = 144 * 1024, kFewLdsBf16 = 80 * 1024;
-int few_ldk(int H, bool f32) {   // whole steps, and 16 bytes that put 16 rows at one k into different banks
-  const int step = f32 ? 16 : 32;
-  return (H + step - 1) / step * step + (f32 ? 4 : 8);
+constexpr int kFewSteps = 32;   // a multiple of the loop's 16
+// columns of nj tiles of rows in LDS at a time: whole steps; a row of it has 16 bytes more, which put 16 rows at one k into different banks
+int few_columns(int nj, int H, bool f32) {
+  const int step = f32 ? 16 : 32, all = (H + step - 1) / step * step;
+  const size_t e = f32 ? 4 : 2;
+  return (size_t)16 * nj * (all * e + 16) <= (f32 ? kFewLds : kFewLdsBf16) ? all : kFewSteps * step;
 }
 template <typename TE, bool ALIGNED, int NJ, bool ARG, bool TEACH>
 hipError_t launch_few(const VocabRows& p, const VocabEpi& e, const void* W, hipStream_t st) {
@@ -267,19 +282,12 @@ hipError_t launch_few(const VocabRows& p, const VocabEpi& e, const void* W, hipS
   static LdsLimit limit;
   const hipError_t rc = limit.raise(reinterpret_cast<const void*>(kfn), kFewLds);
   if (rc != hipSuccess) return rc;
-  const int ldk = few_ldk(p.H, sizeof(TE) == 4), words = (p.V + kFewWords - 1) / kFewWords, row_blocks = (p.N + 16 * NJ - 1) / (16 * NJ);
+  const int kc = few_columns(NJ, p.H, sizeof(TE) == 4), ldk = kc + FewType<TE>::kVec, words = (p.V + kFewWords - 1) / kFewWords, row_blocks = (p.N + 16 * NJ - 1) / (16 * NJ);
   size_t smem = (size_t)16 * NJ * ldk * sizeof(TE);
   if (TEACH && smem < (size_t)16 * NJ * kDlLd * 4) smem = (size_t)16 * NJ * kDlLd * 4;
   const int blocks = row_blocks == 1 ? words : (words + 7) / 8 * 8 * row_blocks;
-  hipLaunchKernelGGL(kfn, dim3(blocks), dim3(kFewThreads), smem, st, p, e, reinterpret_cast<const TE*>(W), ldk, row_blocks);
+  hipLaunchKernelGGL(kfn, dim3(blocks), dim3(kFewThreads), smem, st, p, e, reinterpret_cast<const TE*>(W), ldk, kc, row_blocks);
   return hipGetLastError();
-}
-// tiles of 16 rows per block: all of them, or as many as fit
-int few_tiles(int N, int H, bool f32) {
-  const size_t tile = (size_t)16 * few_ldk(H, f32) * (f32 ? 4 : 2), most = f32 ? kFewLds : kFewLdsBf16;
-  for (int nj = N <= 16 ? 1 : N <= 32 ? 2 : 4; nj > 0; nj >>= 1)
-    if (nj * tile <= most) return nj;
-  return 0;
 }
 template <typename TE, bool ALIGNED, int NJ>
 hipError_t launch_few_rows(const VocabRows& p, const VocabEpi& e, const void* W, bool arg, bool teacher, hipStream_t st) {
@@ -289,10 +297,11 @@ hipError_t launch_few_rows(const VocabRows& p, const VocabEpi& e, const void* W,
 }
 template <typename TE, bool ALIGNED>
 hipError_t launch_few_of(const VocabRows& p, const VocabEpi& e, const void* W, bool arg, bool teacher, hipStream_t st) {
-  const int nj = few_tiles(p.N, p.H, sizeof(TE) == 4);
+  const int tiles = (p.N + 15) / 16, blocks = (tiles + 3) / 4, nj = (tiles + blocks - 1) / blocks;   // up to four tiles of 16 rows per block, as many in each
   if (nj == 1) return launch_few_rows<TE, ALIGNED, 1>(p, e, W, arg, teacher, st);
   if (nj == 2) return launch_few_rows<TE, ALIGNED, 2>(p, e, W, arg, teacher, st);
-  if constexpr (sizeof(TE) == 4) return launch_few_rows<TE, ALIGNED, 4>(p, e, W, arg, teacher, st);
+  if constexpr (sizeof(TE) == 4)
+    return nj == 3 ? launch_few_rows<TE, ALIGNED, 3>(p, e, W, arg, teacher, st) : launch_few_rows<TE, ALIGNED, 4>(p, e, W, arg, teacher, st);
   return hipErrorInvalidValue;
 }
 
@@ -652,11 +661,11 @@ template <typename TE, bool ALIGNED, typename TG> hipError_t launch_few_bwd_any(
 }  // namespace
 
 // us, forward, this / the tile kernels behind the list of rows: bf16 1 x 512 x 32000 16.4 / 18.6 (15 of them the host's), 16 x 2048 x 64000
-// 63.2 / 68.1, 32 x 512 x 32000 19.1 / 20.0, past the line 33 - / 20.5; fp32, whose tiles want W as bf16 terms first, 1 x 1024 x 32000
-// 39.4 / 127, 32 x 512 29.3 / 72.4, 128 x 256 39.8 / 46.9, 128 x 1024 136 / 150, 128 x 2048 321 / 397; with a teacher 8 x 1024 56.1 / 139, 128 x
-// 1024 160 / 162, 40 x 256 x 4000 38.5 / 35.5.
+// 63.0 / 68.1, 32 x 512 x 32000 19.1 / 20.0, 32 x 2048 x 64000 65.7 / 69.5, past the line 33 - / 20.5; fp32, whose tiles want W as bf16 terms
+// first, 1 x 1024 x 32000 39.4 / 127, 32 x 512 29.3 / 72.4, 16 x 4096 123 / 587, 128 x 256 38.8 / 46.9, 128 x 1024 120 / 150, 128 x 2048 220 / 397;
+// with a teacher 8 x 1024 56.1 / 139, 128 x 1024 142 / 162, 40 x 256 x 4000 35.7 / 35.5.
 bool vocab_few_rows(int N, int H, bool f32, bool teacher) {
-  return f32 ? N <= kFewMost && H >= 4 && few_tiles(N, H, true) > 0 : !teacher && N <= 32 && 16 * few_tiles(N, H, false) >= N;
+  return f32 ? N <= kFewMost && H >= 4 : !teacher && N <= 32;
 }
 hipError_t launch_vocab_few(const VocabRows& p, const VocabEpi& e, const void* W, bool arg, bool teacher, hipStream_t st) {
   if (!vocab_few_rows(p.N, p.H, p.f32, teacher)) return hipErrorInvalidValue;

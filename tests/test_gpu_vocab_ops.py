@@ -278,7 +278,8 @@ XENT = [(1, 8, 1, "bf16", "f32"), (1, 1, 2, "f32", "f32"), (1, 64, 1000, "bf16",
         (64, 513, 300, "f32", "f32"), (50, 1500, 260, "f32", "f32"), (64, 2100, 131, "f32", "f32"),
         (128, 300, 1270, "f32", "f32"), (97, 1201, 140, "f32", "f32"), (66, 3, 50, "f32", "f32"),
         (32, 504, 700, "bf16", "f32"), (11, 1024, 310, "bf16", "f32"), (48, 500, 900, "f32", "f32"),
-        (16, 2040, 270, "bf16", "bf16"), (5, 1504, 300, "bf16", "f32"), (13, 1000, 310, "bf16", "bf16"), (16, 2056, 140, "bf16", "bf16")]
+        (16, 2040, 270, "bf16", "bf16"), (5, 1504, 300, "bf16", "f32"), (13, 1000, 310, "bf16", "bf16"), (16, 2056, 140, "bf16", "bf16"),
+        (90, 700, 600, "f32", "f32"), (40, 1029, 300, "f32", "f32"), (2, 3001, 200, "f32", "f32"), (31, 2600, 300, "bf16", "f32"), (128, 513, 130, "f32", "f32")]
 
 
 @pytest.mark.parametrize("N, H, V, dtype, grad", XENT)
@@ -299,7 +300,7 @@ def test_cross_entropy(N, H, V, dtype, grad):
     (1, 8, 1, "bf16", "f32", 1, 1.0), (3, 16, 40, "f32", "f32", 5, 2.0), (16, 64, 1000, "bf16", "bf16", 8, 2.0), (17, 72, 515, "bf16", "f32", 20, 4.0),
     (40, 33, 100, "f32", "f32", 256, 0.7), (66, 136, 4001, "bf16", "bf16", 64, 1.0), (130, 64, 70, "bf16", "f32", 100, 3.0),
     (300, 264, 1003, "bf16", "bf16", 33, 2.0), (700, 40, 257, "f32", "f32", 7, 1.0),
-    (20, 600, 300, "f32", "f32", 5, 1.0), (90, 61, 1330, "f32", "f32", 30, 2.0), (128, 1202, 150, "f32", "f32", 60, 1.5), (1, 7, 2200, "f32", "f32", 200, 1.0)])
+    (20, 600, 300, "f32", "f32", 5, 1.0), (90, 61, 1330, "f32", "f32", 30, 2.0), (128, 1202, 150, "f32", "f32", 60, 1.5), (1, 7, 2200, "f32", "f32", 200, 1.0), (75, 1100, 210, "f32", "f32", 9, 2.0)])
 def test_distillation(N, H, V, dtype, grad, K, tau):
     c = Case(N, H, V, dtype, grad, K=K, tau=tau, seed=N + K)
     v = c.device()
