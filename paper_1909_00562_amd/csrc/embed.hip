@@ -23,36 +23,45 @@ namespace {
 
 typedef uint32_t eu32x4_t __attribute__((ext_vector_type(4)));
 
-// Elements a thread moves at a time (16 bytes, or one where rows do not start on 16 bytes), as floats.
+// Elements a thread moves at a time (16 bytes), as floats.  VEC < 0: rows that do not start on 16 bytes, `left` elements to their end.
+// (One element at a time there and vectors, us: 66000 x 1021, 900 words, forward and backward 241 / 177, 131072 x 1023, 128000 words 663 / 472.)
 // PAST: past the caches, where a call moves more than they hold (past_caches).
-template <typename TE, int VEC, bool PAST = false> __device__ __forceinline__ void ld_vec(const TE* p, float (&f)[VEC]) {
-  if constexpr (VEC == 1) {
-    f[0] = ld_elem<TE>(p, 0);
-  } else {
-    const eu32x4_t* from = reinterpret_cast<const eu32x4_t*>(p);
-    const eu32x4_t q = PAST ? __builtin_nontemporal_load(from) : *from;
+template <int VEC> constexpr int kWidth = VEC < 0 ? -VEC : VEC;
+typedef eu32x4_t __attribute__((aligned(4))) eu32x4_on4_t;
+template <typename TE, int VEC, bool PAST = false> __device__ __forceinline__ void ld_vec(const TE* p, float (&f)[kWidth<VEC>], int left) {
+  if (VEC < 0 && left < kWidth<VEC>) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (sizeof(TE) == 2) {
-        f[2 * i] = lo_bf16(q[i]);
-        f[2 * i + 1] = hi_bf16(q[i]);
-      } else {
-        const uint32_t w = q[i];   // (a bit cast of the vector's element itself reads element 0)
-        f[i] = __builtin_bit_cast(float, w);
-      }
+    for (int i = 0; i < kWidth<VEC>; ++i) f[i] = i < left ? ld_elem<TE>(p, i) : 0.f;
+    return;
+  }
+  using Q = typename std::conditional<(VEC < 0), eu32x4_on4_t, eu32x4_t>::type;
+  const Q* from = reinterpret_cast<const Q*>(p);
+  const eu32x4_t q = PAST ? __builtin_nontemporal_load(from) : *from;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(TE) == 2) {
+      f[2 * i] = lo_bf16(q[i]);
+      f[2 * i + 1] = hi_bf16(q[i]);
+    } else {
+      const uint32_t w = q[i];   // (a bit cast of the vector's element itself reads element 0)
+      f[i] = __builtin_bit_cast(float, w);
     }
   }
 }
-template <typename TE, int VEC, bool PAST = false> __device__ __forceinline__ void st_vec(TE* p, const float (&f)[VEC]) {
-  if constexpr (VEC == 1) {
-    st_elem<TE>(p, 0, f[0]);
-  } else {
-    eu32x4_t q;
+template <typename TE, int VEC, bool PAST = false> __device__ __forceinline__ void st_vec(TE* p, const float (&f)[kWidth<VEC>], int left) {
+  constexpr int W = kWidth<VEC>;
+  if (VEC < 0 && left < W) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) q[i] = sizeof(TE) == 2 ? pack_bf16(f[VEC / 4 * i], f[VEC / 4 * i + VEC / 4 - 1]) : __builtin_bit_cast(uint32_t, f[i]);
-    if constexpr (PAST) __builtin_nontemporal_store(q, reinterpret_cast<eu32x4_t*>(p));
-    else *reinterpret_cast<eu32x4_t*>(p) = q;
+    for (int i = 0; i < W; ++i)
+      if (i < left) st_elem<TE>(p, i, f[i]);
+    return;
   }
+  eu32x4_t q;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) q[i] = sizeof(TE) == 2 ? pack_bf16(f[W / 4 * i], f[W / 4 * i + W / 4 - 1]) : __builtin_bit_cast(uint32_t, f[i]);
+  using Q = typename std::conditional<(VEC < 0), eu32x4_on4_t, eu32x4_t>::type;
+  if constexpr (PAST) __builtin_nontemporal_store(q, reinterpret_cast<Q*>(p));
+  else *reinterpret_cast<Q*>(p) = q;
 }
 
 // the word of position n, V at padding (sorts behind all words)
@@ -68,21 +77,21 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(const TE* __restrict__ t
                                                         int I, int V, int pad_id, float scale, TE* __restrict__ x, int tpr_log) {
   const int64_t n = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> tpr_log;
   if (n >= N) return;
-  const int lane = threadIdx.x & ((1 << tpr_log) - 1), step = VEC << tpr_log;
+  const int lane = threadIdx.x & ((1 << tpr_log) - 1), step = kWidth<VEC> << tpr_log;
   const uint32_t w = word_key(ids, (int)n, V, pad_id);
   TE* out = x + n * I;
   const TE* row = table + (int64_t)(w < (uint32_t)V ? w : 0) * I;
-  for (int c = lane * VEC; c < I; c += step) {
-    float f[VEC];
+  for (int c = lane * kWidth<VEC>; c < I; c += step) {
+    float f[kWidth<VEC>];
     if (w < (uint32_t)V) {
-      ld_vec<TE, VEC>(row + c, f);
+      ld_vec<TE, VEC>(row + c, f, I - c);
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) f[i] *= scale;
+      for (int i = 0; i < kWidth<VEC>; ++i) f[i] *= scale;
     } else {
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) f[i] = 0.f;
+      for (int i = 0; i < kWidth<VEC>; ++i) f[i] = 0.f;
     }
-    st_vec<TE, VEC, PAST>(out + c, f);
+    st_vec<TE, VEC, PAST>(out + c, f, I - c);
   }
 }
 
@@ -102,16 +111,37 @@ struct ZeroDev {
   int I, blocks;
 };
 constexpr int kZeroRows = 64;
-template <typename TE, int VEC, bool PAST = false>
+// v0: a multiple of kZeroRows, so that these rows together start on 16 bytes whatever I is.
+template <typename TE, int VEC, bool PAST>
 __device__ __forceinline__ void zero_rows(TE* table, const uint8_t* has, int v0, int v1, int I, int tpp_log) {
-  const int lane = threadIdx.x & ((1 << tpp_log) - 1), step = VEC << tpp_log;
-  const float zero[VEC] = {};
-  for (int v = v0 + (threadIdx.x >> tpp_log); v < v1; v += 256 >> tpp_log) {
-    if (has[v - v0]) continue;
-    for (int c = lane * VEC; c < I; c += step) st_vec<TE, VEC, PAST>(table + (int64_t)v * I + c, zero);
+  constexpr int W = kWidth<VEC>;
+  const float zero[W] = {};
+  if constexpr (VEC < 0) {   // vectors across the rows' ends where both rows are absent (inside each row: 120000 x 1001 152 us for 121)
+    const uint32_t end = (uint32_t)(v1 - v0) * (uint32_t)I, width = I;
+    TE* out = table + (int64_t)v0 * I;
+    for (uint32_t g = threadIdx.x * W; g < end; g += 256 * W) {
+      const uint32_t r = g / width;
+      const bool inside = g + W <= (r + 1) * width, two = width >= W && g + W <= end;
+      if (inside || two) {
+        if (!has[r] && (inside || !has[r + 1])) {
+          st_vec<TE, W, PAST>(out + g, zero, W);
+          continue;
+        }
+        if (inside) continue;
+      }
+#pragma unroll
+      for (int e = 0; e < W; ++e)
+        if (g + e < end && !has[(g + e) / width]) st_elem<TE>(out, g + e, 0.f);
+    }
+  } else {
+    const int lane = threadIdx.x & ((1 << tpp_log) - 1), step = W << tpp_log;
+    for (int v = v0 + (threadIdx.x >> tpp_log); v < v1; v += 256 >> tpp_log) {
+      if (has[v - v0]) continue;
+      for (int c = lane * W; c < I; c += step) st_vec<TE, VEC, PAST>(table + (int64_t)v * I + c, zero, I - c);
+    }
   }
 }
-template <typename TE, int VEC> __global__ __launch_bounds__(256) void embed_rank_kernel(SortDev p, ZeroDev z, int tpp_log) {
+template <typename TE, int VEC, bool PAST> __global__ __launch_bounds__(256) void embed_rank_kernel(SortDev p, ZeroDev z, int tpp_log) {
   extern __shared__ __align__(16) uint32_t keys[];   // of all positions, to a multiple of 16
   const int N = p.N, N16 = (N + 15) & ~15, tid = threadIdx.x;
   auto key = [&](int w) { return w >= 0 && w < p.V && w != p.pad_id ? (uint32_t)w : (uint32_t)p.V; };
@@ -149,7 +179,7 @@ template <typename TE, int VEC> __global__ __launch_bounds__(256) void embed_ran
     });
     __syncthreads();
     const int end = (int)v0 + kZeroRows < p.V ? (int)v0 + kZeroRows : p.V;
-    zero_rows<TE, VEC>(reinterpret_cast<TE*>(z.d_table), has, (int)v0, end, z.I, tpp_log);
+    zero_rows<TE, VEC, PAST>(reinterpret_cast<TE*>(z.d_table), has, (int)v0, end, z.I, tpp_log);
     return;
   }
   all_ids([&](int i, uint4 k) { *reinterpret_cast<uint4*>(keys + i) = k; });
@@ -382,7 +412,7 @@ __device__ __forceinline__ int lower_bound_wave(const uint32_t* key, int N, uint
 template <typename TE, int VEC, int L, int RU, bool PAST>
 __global__ __launch_bounds__(256) void embed_sums_kernel(SumsDev p, int tpp_log) {
   __shared__ uint32_t list[2][16 * L + 1];   // the block's part of the sorted list: words, with the one ahead, and positions
-  const int I = p.I, lane = threadIdx.x & ((1 << tpp_log) - 1), step = VEC << tpp_log;
+  const int I = p.I, lane = threadIdx.x & ((1 << tpp_log) - 1), step = kWidth<VEC> << tpp_log;
   TE* table = reinterpret_cast<TE*>(p.d_table);
   if ((int)blockIdx.x < p.zero_blocks) {   // rows of words that no position has
     __shared__ uint8_t has[kZeroRows];
@@ -426,43 +456,44 @@ __global__ __launch_bounds__(256) void embed_sums_kernel(SumsDev p, int tpp_log)
   const bool begins = key[-1] != first;
   const uint32_t after = piece - piece0 + 1 < per_block ? key[L] : list[1][per_block * L];
   const TE* dy = reinterpret_cast<const TE*>(p.dy);
-  for (int c = lane * VEC; c < I; c += step) {
-    float acc[VEC];
+  for (int c = lane * kWidth<VEC>; c < I; c += step) {
+    float acc[kWidth<VEC>];
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
+    for (int e = 0; e < kWidth<VEC>; ++e) acc[e] = 0.f;
     uint32_t cur = first;
     bool whole = begins;   // the run that is being added up began in this piece
     auto flush = [&](bool ends) {
       if (whole && ends) {
-        float f[VEC];
+        float f[kWidth<VEC>];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) f[e] = acc[e] * p.scale;
+        for (int e = 0; e < kWidth<VEC>; ++e) f[e] = acc[e] * p.scale;
         TE* out = table + (int64_t)cur * I + c;
         if (p.accumulate) {
-          float old[VEC];
-          ld_vec<TE, VEC>(out, old);
+          float old[kWidth<VEC>];
+          ld_vec<TE, VEC>(out, old, I - c);
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) f[e] += old[e];
+          for (int e = 0; e < kWidth<VEC>; ++e) f[e] += old[e];
         }
-        st_vec<TE, VEC, PAST>(out, f);
+        st_vec<TE, VEC, PAST>(out, f, I - c);
       } else {
         float* out = p.edge + ((int64_t)piece * 2 + (whole ? 1 : 0)) * I + c;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) out[e] = acc[e];
+        for (int e = 0; e < kWidth<VEC>; ++e)
+          if (VEC > 0 || c + e < I) out[e] = acc[e];
       }
     };
 #pragma unroll 1
     for (int u0 = 0; u0 < L; u0 += RU) {
-      float x[RU][VEC];
+      float x[RU][kWidth<VEC>];
       uint32_t k[RU];
 #pragma unroll
       for (int u = 0; u < RU; ++u) {
         k[u] = key[u0 + u];
         if (k[u] < (uint32_t)p.V) {
-          ld_vec<TE, VEC, PAST>(dy + (int64_t)pos[u0 + u] * I + c, x[u]);
+          ld_vec<TE, VEC, PAST>(dy + (int64_t)pos[u0 + u] * I + c, x[u], I - c);
         } else {
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) x[u][e] = 0.f;
+          for (int e = 0; e < kWidth<VEC>; ++e) x[u][e] = 0.f;
         }
       }
 #pragma unroll
@@ -472,10 +503,10 @@ __global__ __launch_bounds__(256) void embed_sums_kernel(SumsDev p, int tpp_log)
           whole = true;
           cur = k[u];
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
+          for (int e = 0; e < kWidth<VEC>; ++e) acc[e] = 0.f;
         }
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) acc[e] += x[u][e];
+        for (int e = 0; e < kWidth<VEC>; ++e) acc[e] += x[u][e];
       }
     }
     if (cur < (uint32_t)p.V) flush(after != cur);
@@ -486,7 +517,7 @@ __global__ __launch_bounds__(256) void embed_sums_kernel(SumsDev p, int tpp_log)
 // 64 threads' columns x 4 phases of every fourth piece, eight of them in flight, the phases in order.
 template <typename TE, int VEC, int L>
 __global__ __launch_bounds__(256) void embed_edges_kernel(SumsDev p) {
-  constexpr int CV = VEC == 1 ? 1 : 4, PH = 4, U = 8;
+  constexpr int CV = 4, PH = 4, U = 8;
   __shared__ float red[PH][64 * CV];
   const int piece = blockIdx.x, last = piece * L + L - 1;
   if (last + 1 >= p.N) return;
@@ -501,7 +532,7 @@ __global__ __launch_bounds__(256) void embed_edges_kernel(SumsDev p) {
     const float* edge = p.edge + c;
     if (phase == 0) {
 #pragma unroll
-      for (int e = 0; e < CV; ++e) acc[e] = edge[((int64_t)piece * 2 + 1) * I + e];
+      for (int e = 0; e < CV; ++e) acc[e] = VEC > 0 || c + e < I ? edge[((int64_t)piece * 2 + 1) * I + e] : 0.f;
     }
 #pragma unroll 1
     for (int q0 = piece + 1 + phase; q0 < p.pieces; q0 += PH * U) {
@@ -513,7 +544,7 @@ __global__ __launch_bounds__(256) void embed_edges_kernel(SumsDev p) {
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int e = 0; e < CV; ++e) x[u][e] = in[u] ? edge[(int64_t)(q0 + PH * u) * 2 * I + e] : 0.f;
+        for (int e = 0; e < CV; ++e) x[u][e] = in[u] && (VEC > 0 || c + e < I) ? edge[(int64_t)(q0 + PH * u) * 2 * I + e] : 0.f;
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -531,6 +562,7 @@ __global__ __launch_bounds__(256) void embed_edges_kernel(SumsDev p) {
   TE* out = reinterpret_cast<TE*>(p.d_table) + (int64_t)word * I + c;
 #pragma unroll
   for (int e = 0; e < CV; ++e) {
+    if (VEC < 0 && c + e >= I) continue;
     acc[e] *= p.scale;
     if (p.accumulate) acc[e] += ld_elem<TE>(out, e);
     st_elem<TE>(out, e, acc[e]);
@@ -545,6 +577,10 @@ int log2_up(int64_t x) {
   while (((int64_t)1 << b) < x) ++b;
   return b;
 }
+
+// Up to here pieces of 16 positions, whose launch is over in fewer latencies; behind it of 64, which are fewer edges.  us, 16 / 64: 22548 x 141 65
+// / 82, 20566 x 264 bf16 64 / 79, 40000 x 512 126 / 113, 60713 x 92 84 / 75, 84157 x 648 bf16 210 / 147.
+constexpr int kShortMost = 32768;
 
 struct EmbedLayout {
   int L, pieces, passes, blocks, per;
@@ -571,7 +607,7 @@ EmbedLayout embed_layout(const vo_embed* s) {
   if (L.blocks > 512) L.blocks = 512;
   L.per = ((N + L.blocks - 1) / L.blocks + kSortWaves - 1) / kSortWaves;
   L.per = (L.per + 63) & ~63;
-  L.L = L.rank ? 16 : 64;
+  L.L = N <= kShortMost ? 16 : 64;
   L.pieces = (N + L.L - 1) / L.L;
   size_t off = 0;
   auto take = [&](size_t bytes) {
@@ -654,29 +690,35 @@ hipError_t launch_sums(const SumsDev& p, int tpp, hipStream_t st) {
   hipLaunchKernelGGL((embed_sums_kernel<TE, VEC, PL, RU, PAST>), dim3(p.zero_blocks + piece_blocks), dim3(256), 0, st, p, tpp);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.pieces < 2) return e;
-  constexpr int CV = VEC == 1 ? 1 : 4;
+  constexpr int CV = 4;   // columns of a thread there
   hipLaunchKernelGGL((embed_edges_kernel<TE, VEC, PL>), dim3(p.pieces, (p.I + 64 * CV - 1) / (64 * CV)), dim3(256), 0, st, p);
   return hipGetLastError();
 }
-template <typename TE, int VEC>
+template <typename TE, int VEC, bool PAST>
 hipError_t launch_embed_bwd(const SortDev& q, SumsDev p, const EmbedLayout& L, unsigned char* ws, hipStream_t st) {
-  const int tpp = row_threads_log((p.I + VEC - 1) / VEC), zero_blocks = p.accumulate ? 0 : (p.V + kZeroRows - 1) / kZeroRows;
+  const int tpp = row_threads_log((p.I + kWidth<VEC> - 1) / kWidth<VEC>), zero_blocks = p.accumulate ? 0 : (p.V + kZeroRows - 1) / kZeroRows;
+  hipError_t e;
   if (!L.rank) {
-    const hipError_t e = launch_sort(q, L, ws, st);
+    e = launch_sort(q, L, ws, st);
     p.zero_blocks = zero_blocks;
+  } else {
+    auto kfn = embed_rank_kernel<TE, VEC, PAST>;
+    static LdsLimit limit;
+    e = limit.raise(reinterpret_cast<const void*>(kfn), kRankMost * 4);
     if (e != hipSuccess) return e;
-    return past_caches(q.N, p.I, sizeof(TE), p.accumulate ? 0 : p.V) ? launch_sums<TE, VEC, 64, 4, true>(p, tpp, st) : launch_sums<TE, VEC, 64, 4, false>(p, tpp, st);
+    const int blocks = (q.N + kRankBlock - 1) / kRankBlock;
+    const size_t smem = (size_t)(blocks * kRankBlock < kZeroRows ? kZeroRows : blocks * kRankBlock) * 4;
+    hipLaunchKernelGGL(kfn, dim3(blocks + zero_blocks), dim3(256), smem, st, q, ZeroDev{p.d_table, p.I, zero_blocks}, tpp);
+    e = hipGetLastError();
+    p.zero_blocks = 0;
   }
-  auto kfn = embed_rank_kernel<TE, VEC>;
-  static LdsLimit limit;
-  hipError_t e = limit.raise(reinterpret_cast<const void*>(kfn), kRankMost * 4);
   if (e != hipSuccess) return e;
-  const int blocks = (q.N + kRankBlock - 1) / kRankBlock;
-  const size_t smem = (size_t)(blocks * kRankBlock < kZeroRows ? kZeroRows : blocks * kRankBlock) * 4;
-  hipLaunchKernelGGL(kfn, dim3(blocks + zero_blocks), dim3(256), smem, st, q, ZeroDev{p.d_table, p.I, zero_blocks}, tpp);
-  e = hipGetLastError();
-  p.zero_blocks = 0;
-  return e == hipSuccess ? launch_sums<TE, VEC, 16, 16, false>(p, tpp, st) : e;
+  return L.L == 16 ? launch_sums<TE, VEC, 16, 16, PAST>(p, tpp, st) : launch_sums<TE, VEC, 64, 4, PAST>(p, tpp, st);
+}
+template <typename TE, int VEC>
+hipError_t launch_embed_bwd_any(const SortDev& q, const SumsDev& p, const EmbedLayout& L, unsigned char* ws, hipStream_t st) {
+  return past_caches(q.N, p.I, sizeof(TE), p.accumulate ? 0 : p.V) ? launch_embed_bwd<TE, VEC, true>(q, p, L, ws, st)
+                                                                 : launch_embed_bwd<TE, VEC, false>(q, p, L, ws, st);
 }
 
 }  // namespace
@@ -699,7 +741,7 @@ extern "C" as_status vocab_embed_fwd(const vo_embed* shape, const void* table, c
   auto run = [&](auto* t, auto vec) {
     using TE = typename std::remove_pointer<decltype(t)>::type;
     constexpr int VEC = decltype(vec)::value;
-    const int tpr = row_threads_log((I + VEC - 1) / VEC);
+    const int tpr = row_threads_log((I + kWidth<VEC> - 1) / kWidth<VEC>);
     const int64_t blocks = (((int64_t)N << tpr) + 255) / 256;
     auto kfn = past_caches(N, I, sizeof(TE), 0) ? embed_fwd_kernel<TE, VEC, true> : embed_fwd_kernel<TE, VEC, false>;
     hipLaunchKernelGGL(kfn, dim3((unsigned)blocks), dim3(256), 0, st, reinterpret_cast<const TE*>(table), ids, N, I, V,
@@ -709,7 +751,7 @@ extern "C" as_status vocab_embed_fwd(const vo_embed* shape, const void* table, c
   hipError_t e;
   if (shape->dtype == AS_BF16) e = run((uint16_t*)nullptr, std::integral_constant<int, 8>{});
   else if (I % 4 == 0) e = run((float*)nullptr, std::integral_constant<int, 4>{});
-  else e = run((float*)nullptr, std::integral_constant<int, 1>{});
+  else e = run((float*)nullptr, std::integral_constant<int, -4>{});
   return hip_status(e, "vocab_embed_fwd");
 }
 
@@ -745,8 +787,8 @@ extern "C" as_status vocab_embed_bwd(const vo_embed* shape, const int32_t* ids, 
   p.accumulate = accumulate;
   p.pieces = L.pieces;
   hipError_t e;
-  if (shape->grad_dtype == AS_BF16) e = launch_embed_bwd<uint16_t, 8>(q, p, L, ws, st);
-  else if (shape->I % 4 == 0) e = launch_embed_bwd<float, 4>(q, p, L, ws, st);
-  else e = launch_embed_bwd<float, 1>(q, p, L, ws, st);
+  if (shape->grad_dtype == AS_BF16) e = launch_embed_bwd_any<uint16_t, 8>(q, p, L, ws, st);
+  else if (shape->I % 4 == 0) e = launch_embed_bwd_any<float, 4>(q, p, L, ws, st);
+  else e = launch_embed_bwd_any<float, -4>(q, p, L, ws, st);
   return hip_status(e, "vocab_embed_bwd");
 }

@@ -66,7 +66,9 @@ def _embed_case(N, I, V, dtype, grad, pad, seed, ids=None):
     (63, 64, 700, "bf16", "bf16", 0.3), (1237, 1000, 2003, "bf16", "bf16", 0.25), (1000, 111, 999, "f32", "f32", 0.4),
     (8192, 72, 513, "bf16", "f32", 0.2), (8193, 72, 512, "bf16", "f32", 0.2), (8193, 20, 511, "f32", "f32", 0.9),
     (20000, 40, 300000, "bf16", "bf16", 0.1), (40000, 1032, 65, "f32", "f32", 0.0), (70001, 24, 128000, "bf16", "f32", 0.5),
-    (9000, 5, 1 << 19, "f32", "f32", 0.1), (300, 4200, 40, "f32", "f32", 0.1)])
+    (9000, 5, 1 << 19, "f32", "f32", 0.1), (300, 4200, 40, "f32", "f32", 0.1),
+    (50, 3, 200, "f32", "f32", 0.1), (20, 2, 130, "f32", "f32", 0.0), (17000, 1, 3000, "f32", "f32", 0.1), (100, 1023, 333, "f32", "f32", 0.2),
+    (20000, 6, 1000, "f32", "f32", 0.2), (33000, 141, 700, "f32", "f32", 0.2)])
 def test_embedding(N, I, V, dtype, grad, pad):
     table, t64, dy, dy64, ids, ids_np = _embed_case(N, I, V, dtype, grad, pad, seed=N + I)
     scale = float(np.float32(1.7))
@@ -99,7 +101,7 @@ def test_embedding(N, I, V, dtype, grad, pad):
 
 # Rows past the caches, offsets past 32 bits (elements, and bytes): against float64 on the GPU.  A sum of n products is off by n 2^-24 of
 # its terms' magnitudes, a bf16 result by 2^-8 of itself.
-@pytest.mark.parametrize("N, I, V, dtype, grad", [(66000, 1020, 900, "f32", "f32"), (20000, 424, 300000, "bf16", "bf16"), (1100000, 2048, 5000, "bf16", "bf16")])
+@pytest.mark.parametrize("N, I, V, dtype, grad", [(66000, 1020, 900, "f32", "f32"), (66000, 1021, 900, "f32", "f32"), (2000, 1001, 70000, "f32", "f32"), (20000, 424, 300000, "bf16", "bf16"), (1100000, 2048, 5000, "bf16", "bf16")])
 def test_embedding_of_large_tensors(N, I, V, dtype, grad):
     gen = torch.Generator(device="cuda").manual_seed(N)
     t = TYPES[dtype]
