@@ -23,7 +23,7 @@
  * fp32 and rounded once on the way out.  Losses are float whatever the types.
  *   AS_F32 / AS_F32    fp32 products: operands as the sum of three bf16 terms, six products on the bf16 matrix cores
  *   AS_BF16 / AS_F32   the derivative of the logits as the sum of three bf16 terms, h and W as they are: fp32 products
- *   AS_BF16 / AS_BF16  the derivative of the logits rounded once to bf16 (up to 16 positions: not rounded)
+ *   AS_BF16 / AS_BF16  the derivative of the logits as the sum of two bf16 terms (2^-17 of it; up to 16 positions and H <= 2048: fp32)
  *
  * Padding: a position whose id (target) equals pad_id or lies outside [0,V) is padding (pad_id = -1: only the latter).  Its row of
  * table, dy, h and of the teacher is not read (it may hold anything, NaN too), its output row is 0, and it contributes

@@ -1114,7 +1114,7 @@ hipError_t launch_gemm_vocab(const GemmArgs& g, GemmTile tile, const VocabEpi& v
   const hipError_t e = gemm_describe(g, tile, d);
   if (e != hipSuccess) return e;
   if (tile != kTile256) return launch_gemm_bf16_vocab_tile(d, tile, v, terms, teacher, arg, st);
-  if (terms == 1) return teacher ? launch_pp_vocab<VocabOut<true, false, 1>>(d, v, st) : launch_pp_vocab<VocabOut<false, false, 1>>(d, v, st);
+  if (terms == 2) return teacher ? launch_pp_vocab<VocabOut<true, false, 2>>(d, v, st) : launch_pp_vocab<VocabOut<false, false, 2>>(d, v, st);
   if (terms == 3) return teacher ? launch_pp_vocab<VocabOut<true, false, 3>>(d, v, st) : launch_pp_vocab<VocabOut<false, false, 3>>(d, v, st);
   if (teacher) return launch_pp_vocab<VocabOut<true, false, 0>>(d, v, st);
   return arg ? launch_pp_vocab<VocabOut<false, true, 0>>(d, v, st) : launch_pp_vocab<VocabOut<false, false, 0>>(d, v, st);

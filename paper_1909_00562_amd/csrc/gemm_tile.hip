@@ -568,7 +568,7 @@ template <typename VOC> static hipError_t launch_vocab_tile(const GemmDev& d, Ge
   return (int64_t)d.tiles_m * d.tiles_n <= 256 ? launch_vocab_shape<4, 4, VOC>(d, e, st) : launch_vocab_shape<4, 2, VOC>(d, e, st);
 }
 hipError_t launch_gemm_bf16_vocab_tile(const GemmDev& d, GemmTile tile, const VocabEpi& e, int terms, bool teacher, bool arg, hipStream_t st) {
-  if (terms == 1) return teacher ? launch_vocab_tile<VocabOut<true, false, 1>>(d, tile, e, st) : launch_vocab_tile<VocabOut<false, false, 1>>(d, tile, e, st);
+  if (terms == 2) return teacher ? launch_vocab_tile<VocabOut<true, false, 2>>(d, tile, e, st) : launch_vocab_tile<VocabOut<false, false, 2>>(d, tile, e, st);
   if (terms == 3) return teacher ? launch_vocab_tile<VocabOut<true, false, 3>>(d, tile, e, st) : launch_vocab_tile<VocabOut<false, false, 3>>(d, tile, e, st);
   if (teacher) return launch_vocab_tile<VocabOut<true, false, 0>>(d, tile, e, st);
   return arg ? launch_vocab_tile<VocabOut<false, true, 0>>(d, tile, e, st) : launch_vocab_tile<VocabOut<false, false, 0>>(d, tile, e, st);

@@ -2,7 +2,7 @@
 //
 // Rows are the compacted rows of words (R of them, counted on the device), columns those of a piece of the vocabulary.
 // The products leave no logits: the forward one the softmax statistics of each row's part of a tile, the logit of the
-// row's word and those of its teacher entries; the backward one the derivative dl as one or three bf16 planes and its column sums.
+// row's word and those of its teacher entries; the backward one the derivative dl as two or three bf16 planes and its column sums.
 //
 // Teacher entries are kept in lists: rows in groups of 16, columns in strips of 64, the entries of a group ordered by strip, so
 // that a tile finds those of its rows and columns as one run per group.  An entry is (column << 4 | row of the group) and its
@@ -47,7 +47,7 @@ constexpr int kVocabStatCols = 64;                                             /
 inline int vocab_sum_rows(GemmTile t) { return t == kTile256 ? 128 : 64; }     // rows of a part of the column sums
 constexpr int kVocabRowPad = 256;   // y, lse, lse_tau are read in whole tiles: their allocations are multiples of this
 
-// terms: planes of dl (1 or 3), or 0: statistics; arg: stat_idx is wanted.  g: A, B contiguous, M_dev, no split, no C.
+// terms: planes of dl (2 or 3), or 0: statistics; arg: stat_idx is wanted.  g: A, B contiguous, M_dev, no split, no C.
 hipError_t launch_gemm_vocab(const GemmArgs& g, GemmTile tile, const VocabEpi& e, int terms, bool teacher, bool arg, hipStream_t st);
 
 // ---- rows of words -------------------------------------------------------------------

@@ -4,13 +4,16 @@
 // Forward: the rows of words of h are gathered (a count that stays on the device), one product h W^T whose write-out leaves the
 // softmax statistics of each row's part of a tile instead of the logits, and a pass that joins them.
 // Backward, a piece of the vocabulary at a time: the product again, its write-out now dl = g (exp(l - lse) - onehot) [+ s tau
-// (q - p)] as bf16 and its column sums (db), then dW_piece = dl^T h and dh += dl W_piece while dl is still in the caches.
+// (q - p)] and its column sums (db), then dW_piece = dl^T h and dh += dl W_piece while dl is still in the caches.
 // Four products of 2 R V H where three would do with the logits kept: what that buys is R V elements of memory.
 //
-// Float gradients, and bf16 ones of few rows: dl as the sum of three bf16 terms (24 bits of mantissa), each in a plane of its own, whose products with the
-// other operand are reduction segments of one launch.  fp32 storage: h and W as three terms too, the six products of terms whose
-// ranks add up to two at most; what is left out is 2^-24 of a product.  The planes of W are made once, or a
-// piece at a time where all of them would take more than a piece may.
+// dl is the sum of bf16 terms, each in a plane of its own, whose products with the other operand are reduction segments of one launch:
+// three for float gradients (24 bits of mantissa), two for bf16 ones (2^-17).  One alone would be a rounding by up to 2^-8 that does not
+// average out where sums cancel: sum_v dl_nv is 0, so what all rows of W have in common cancels in dh, and what the positions ask of a
+// word's row cancels in dW as training goes on.  (A softmax over 4000 words x 256 fitted to 2000 positions for 20 steps: dW 0.51 % off where
+// the rounding of the result makes 0.17, dh 0.31; for 60 steps 4.3 %; with two terms 0.17 throughout.)
+// fp32 storage: h and W as three terms too, the six products of terms whose ranks add up to two at most; what is left out is 2^-24 of a
+// product.  The planes of W are made once, or a piece at a time where all of them would take more than a piece may.
 #include "../../include/vocab_ops.h"
 
 #include <hip/hip_runtime.h>
@@ -31,9 +34,9 @@ size_t upv(size_t x) { return (x + kAlignV - 1) / kAlignV * kAlignV; }
 int64_t round_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 
 // What a piece of the vocabulary may take: dl of the backward pass, or the statistics or terms of W of the forward one.  Larger
-// pieces fill the rounds of the compute units better, and the sums of dh are read and written once per piece: 64 / 128 / 256 / 512 MiB,
-// forward and backward, 6400 x 1024 x 32000 bf16 - / 1355 / 1190 / 1139 us, 16384 x 2048 x 128000 - / 22.7 / 22.3 / 21.8 ms, 2257 x 1000
-// x 32003 float gradients 1113 / 1088 / 1072 / 1161 us.
+// pieces fill the rounds of the compute units better, and the sums of dh are read and written once per piece; past the 256 MB of the
+// memory-side cache dW and dh read dl from memory: 64 / 128 / 256 / 512 MiB, forward and backward, 2257 x 1000 x 32003 float gradients 1113 /
+// 1088 / 1072 / 1161 us; bf16 gradients, 256 / 512, 2257 x 1000 x 32003 759 / 905, 5000 x 2048 x 60000 5.50 / 5.73 ms.
 constexpr int64_t kPieceBytes = (int64_t)256 << 20;
 constexpr int64_t kPieceColumns = 256;   // pieces are multiples of it
 
@@ -45,7 +48,7 @@ struct VocabLayout {
   int strips, groups;
   GemmTile t_fwd, t_bwd;
   GemmPlan p_dw, p_dh;
-  bool dh_dyn = false;
+  bool apart = false;                     // dW, and dh a term at a time, in launches of their own
   // kept from the forward to the backward pass
   size_t rows, row_pos, chunk_words, y, n_act, ticket, hc, lse, lse_tau, at_word, loss_ws, distill_ws, run;
   size_t runs, ent, ent_p, ent_l, place, p_log_p, seen;
@@ -119,9 +122,7 @@ VocabLayout vocab_layout(const vo_shape* s, const vo_teacher* t) {
   L.f32 = s->dtype == AS_F32;
   L.g_bf16 = s->grad_dtype == AS_BF16;
   L.h_terms = L.f32 ? 3 : 1;
-  // bf16 gradients: one rounding of dl, which sums over many rows average out; those of a few rows do not (2 rows at H = 1288: dW off by
-  // 0.19 % where the rounding on its way out makes 0.11), and up to 16 the kernel that keeps dl in fp32 costs next to nothing.
-  L.dl_terms = L.g_bf16 && N > 16 ? 1 : 3;
+  L.dl_terms = L.g_bf16 ? 2 : 3;
   L.ldH = round_up(H, 8);
   L.strips = (int)((V + kVocabStrip - 1) / kVocabStrip);
   L.groups = (int)((N + kVocabGroup - 1) / kVocabGroup);
@@ -135,6 +136,20 @@ VocabLayout vocab_layout(const vo_shape* s, const vo_teacher* t) {
   L.few_bwd = vocab_few_bwd_rows((int)N, (int)H, (int)V, L.f32, L.g_bf16);
   const int64_t dl_col = N * 2 * L.dl_terms;
   L.bwd_cols = piece_columns(V, dl_col > w_col ? dl_col : w_col);
+  // bf16 gradients of many rows, pieces of twice the columns that are whole rounds of 256 x 256 tiles of dW: those kernels, one behind the
+  // other, dh a term at a time with a split that the device chooses from the rows that there are.  us, the whole call, joint launch of
+  // 128 x 128 tiles / this: 4096 x 1024 x 32000 1667 / 1533, 5120 2246 / 1995, 6400 with 30 % padding 2103 / 1846, 8192 x 1024 x 16000 with
+  // 30 % 1187 / 1218, 16384 x 2048 x 128000 with 25 % 36070 / 34820; below the line 2257 x 1000 x 32003 with 30 % 759 / 950.
+  if (L.dl_terms == 2 && N >= 4096) {
+    const int64_t cols = piece_columns(V, N * 2), ldd = round_up(cols < V ? cols : V, 8), most = kPieceBytes / (N * L.ldH * 4);
+    const int64_t tiles = ((ldd + 255) / 256) * ((H + 255) / 256), rounds = (tiles + 255) / 256;
+    if (tiles * 8 >= rounds * 256 * 7 && most >= 2) {
+      L.apart = true;
+      L.bwd_cols = cols;
+      L.p_dw = {kTile256, 1};
+      L.p_dh = {kTile256, most < 4 ? (int)most : 4};
+    }
+  }
   L.ldd = round_up(L.bwd_cols < V ? L.bwd_cols : V, 8);
   L.t_bwd = logits_tile(N, L.ldd, L.ldH, L.h_terms);
   // The two products of a piece in one launch of 128 x 128 tiles, the blocks of dh first, whose reductions are the longer ones: as
@@ -142,7 +157,7 @@ VocabLayout vocab_layout(const vo_shape* s, const vo_teacher* t) {
   // blocks would otherwise take longer than half of all blocks' share of a compute unit's two places.
   const int n_dw = pair_count(L.dl_terms, L.h_terms);
   const int64_t k_dw = n_dw * ((N + 63) / 64), k_dh = n_dw * ((L.ldd + 63) / 64);
-  if (N > 256) {
+  if (!L.apart && N > 256) {
     const int64_t b_dw = ((L.ldd + 127) / 128) * ((H + 127) / 128), b_dh = ((N + 127) / 128) * ((L.ldH + 127) / 128);
     int64_t share = (b_dw * k_dw + b_dh * k_dh + 511) / 512;
     if (share < 8) share = 8;
@@ -152,19 +167,9 @@ VocabLayout vocab_layout(const vo_shape* s, const vo_teacher* t) {
     };
     L.p_dw = {kTile128, splits(k_dw)};
     L.p_dh = {kTile128, splits(k_dh)};
-    // One term and whole rounds of 256 x 256 tiles of dW: those kernels, one behind the other, dh with a split that the device
-    // chooses from the rows that there are.  6400 x 1024 x 16128 (252 tiles) 1222 / 1190 us for the whole call, 16384 x 2048 x 8192
-    // (256) 23.1 / 22.3 ms; half a round, 6400 x 1024 x 8192, 1355 / 1486.
-    const int64_t tiles = ((L.ldd + 255) / 256) * ((H + 255) / 256), rounds = (tiles + 255) / 256;
-    const int64_t most = kPieceBytes / (N * L.ldH * 4);
-    if (n_dw == 1 && N >= 2048 && tiles * 8 >= rounds * 256 * 7 && most >= 2) {
-      L.p_dw = {kTile256, 1};
-      L.p_dh = {kTile256, most < 4 ? (int)most : 4};
-      L.dh_dyn = true;
-    }
-  } else {
-    L.p_dw = gemm_plan((int)L.ldd, (int)H, (int)k_dw * 64, 1, true, true, n_dw > 1, true);
-    L.p_dh = gemm_plan((int)N, (int)L.ldH, (int)k_dh * 64, 1, true, true, n_dw > 1, true);
+  } else if (!L.apart) {
+    L.p_dw = gemm_plan((int)L.ldd, (int)H, (int)k_dw * 64, 1, true, true, true, true);
+    L.p_dh = gemm_plan((int)N, (int)L.ldH, (int)k_dh * 64, 1, true, true, true, true);
     if (L.p_dw.tile == kTile256) L.p_dw = {kTile128, 1};
     if (L.p_dh.tile == kTile256) L.p_dh = {kTile128, 1};
   }
@@ -272,32 +277,13 @@ const void* bias_at(const vo_shape* s, const void* b, int64_t v0) {
   return reinterpret_cast<const unsigned char*>(b) + v0 * (s->dtype == AS_F32 ? 4 : 2);
 }
 
-// dl is kept relative to alpha, a factor of g and s tau.  What all targets have about in common is g (1 / V - 1) + s tau / V over alpha (of a
-// model that knows nothing; one that does tells its rows apart), and what all entries of teachers with one entry each have is s tau
-// (1 / V - 1) + g / V: the rounding of either to bf16 would be that of them all at once, and no sum averages it out.  (With 1 / n_tok in
-// dl, 2^-9 of dh: 12288 words 0.26 % off for 0.18; 18 rows at temperature 3.4, alpha = s tau, 0.28 % for 0.16.)  So the first is one of
-// the 128 bf16 values of [1, 2), that for which the second is the nearest to one.
+// dl is kept relative to alpha, the larger of its factors g and s tau: its terms stay in bf16's range whatever these are.
 struct DlUnit {
   float alpha, a1, a2;   // dl / alpha = a1 (..) + a2 (..)
 };
-DlUnit dl_unit(float g, float c2, int V) {
-  if (g == 0.f) return c2 == 0.f ? DlUnit{0.f, 1.f, 0.f} : DlUnit{c2, 0.f, 1.f};
-  const float ratio = c2 / g, size = std::fabs(ratio);
-  if (!(size > 0x1p-60f && size < 0x1p60f)) return size < 1.f ? DlUnit{g, 1.f, ratio} : DlUnit{c2, g / c2, 1.f};
-  const float q = 1.f / (float)V;
-  float common = 1.f - q - ratio * q, entry = ratio * (1.f - q) - q;   // times a1
-  if (!(std::fabs(common) > 0x1p-8f)) common = 1.f;
-  float best = 1.f / common, off = 1.f;
-  for (int m = 128; m < 256 && off > 0.f; ++m) {
-    const float x = (float)m / 128.f / common;
-    int e;
-    const float f = std::frexp(std::fabs(entry * x), &e) * 256.f, d = std::fabs(f - std::nearbyint(f)) / (f + 1e-30f);   // 8 bits of mantissa
-    if (d < off) {
-      off = d;
-      best = x;
-    }
-  }
-  return {g / best, best, ratio * best};
+DlUnit dl_unit(float g, float c2) {
+  if (std::fabs(g) >= std::fabs(c2)) return {g, 1.f, g == 0.f ? 0.f : c2 / g};
+  return {c2, g / c2, 1.f};
 }
 
 as_status hip_fail(hipError_t e, const char* what) { return set_error(AS_ERR_HIP, "%s: %s", what, hipGetErrorString(e)); }
@@ -454,7 +440,7 @@ as_status backward(const vo_shape* s, const vo_teacher* t, const void* W, const 
   int pairs[kMaxSeg][2];
   const int n = term_pairs(L.dl_terms, L.h_terms, pairs);
   const float c2 = t ? t->scale * t->temperature : 0.f;
-  const DlUnit unit = dl_unit(s->grad_scale, c2, s->V);
+  const DlUnit unit = dl_unit(s->grad_scale, c2);
   const float alpha = unit.alpha;
   hipError_t e;
   if (L.few_bwd) {
@@ -540,9 +526,23 @@ as_status backward(const vo_shape* s, const vo_teacher* t, const void* W, const 
     g[1].ldc = L.ldH;
     g[1].accumulate = v0 > 0;
     g[1].M_dev = n_act;
-    g[1].splits = L.dh_dyn ? L.p_dh.splits : whole_splits(n * ((cols + 63) / 64), L.p_dh.splits);
-    g[1].dyn_split = L.dh_dyn;
+    g[1].splits = whole_splits(n * ((cols + 63) / 64), L.p_dh.splits);
     g[1].partial = w.at<float>(L.partial_dh);
+    if (L.apart) {
+      e = launch_gemm(g[0], true, L.p_dw.tile, st);
+      for (int i = 0; i < n && e == hipSuccess; ++i) {
+        GemmArgs one = g[1];
+        one.A[0] = g[1].A[i];   // (h and W have one term, so every segment's B is the same)
+        one.K[1] = 0;
+        one.nseg = 1;
+        one.accumulate = v0 > 0 || i > 0;
+        one.splits = L.p_dh.splits;
+        one.dyn_split = true;
+        e = launch_gemm(one, true, L.p_dh.tile, st);
+      }
+      if (e != hipSuccess) return hip_fail(e, "dW and dh");
+      continue;
+    }
     const GemmTile tiles[2] = {L.p_dw.tile, L.p_dh.tile};
     const DbReduce no_sums = {nullptr, 0, 0, nullptr, nullptr, 1};   // (db is added up with the last pass)
     e = launch_gemm_joint(g, tiles, 2, true, st, &no_sums);

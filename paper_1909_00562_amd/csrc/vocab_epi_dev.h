@@ -22,18 +22,14 @@ __device__ __forceinline__ float vocab_bias(const VocabEpi& e, int col) {
   return e.bias_f32 ? reinterpret_cast<const float*>(e.bias)[col] : bf16_bits_to_f32(reinterpret_cast<const uint16_t*>(e.bias)[col]);
 }
 // exp(l scale - lse) = k exp2(fma(l, scale log2 e, c)): one fused multiply-add and one v_exp_f32 per element.  k makes up for the
-// rounding of c, which is the same for a whole row (|lse| 2^-24 of all of its probabilities); three bf16 terms of dl keep it, one
-// would round it away.
-template <bool EXACT> struct RowExp {
+// rounding of c, which is the same for a whole row (|lse| 2^-24 of all of its probabilities, and of 1 - p where a word is nearly certain).
+struct RowExp {
   float c, k;
   __device__ __forceinline__ explicit RowExp(float lse) {
     constexpr float L2E = 1.4426950408889634f, L2E_LO = 1.9259629911266175e-8f, LN2 = 0.6931471805599453f;
     c = -lse * L2E;
-    k = 1.f;
-    if constexpr (EXACT) {
-      const float lo = __builtin_fmaf(-lse, L2E, -c) - lse * L2E_LO;
-      k = c > -INFINITY ? __builtin_fmaf(lo, LN2, 1.f) : 1.f;   // (no entries: lse is +inf)
-    }
+    const float lo = __builtin_fmaf(-lse, L2E, -c) - lse * L2E_LO;
+    k = c > -INFINITY ? __builtin_fmaf(lo, LN2, 1.f) : 1.f;   // (no entries: lse is +inf)
   }
   __device__ __forceinline__ float operator()(float l, float scale_l2e) const { return __builtin_amdgcn_exp2f(__builtin_fmaf(l, scale_l2e, c)); }
 };
@@ -48,6 +44,25 @@ __device__ __forceinline__ uint32_t bf16_term(float& x) {
   const uint32_t b = __builtin_bit_cast(uint32_t, x) & 0xffff0000u;
   x -= __builtin_bit_cast(float, b);
   return b >> 16;
+}
+
+// Four elements of dl as terms, a plane each.  Three are truncated and hold all 24 bits; two are rounded to nearest and off by 2^-17.
+template <int TERMS> __device__ __forceinline__ void put_terms(uint16_t* out, int64_t plane, const f32x4_t& v) {
+  if constexpr (TERMS == 2) {
+    const uint2 hi = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+    *reinterpret_cast<uint2*>(out) = hi;
+    *reinterpret_cast<uint2*>(out + plane) =
+        make_uint2(pack_bf16(v[0] - lo_bf16(hi.x), v[1] - hi_bf16(hi.x)), pack_bf16(v[2] - lo_bf16(hi.y), v[3] - hi_bf16(hi.y)));
+  } else {
+    float x[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+    for (int t = 0; t < TERMS; ++t) {
+      uint32_t b[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) b[c] = bf16_term(x[c]);
+      *reinterpret_cast<uint2*>(out + t * plane) = make_uint2(b[0] | (b[1] << 16), b[2] | (b[3] << 16));
+    }
+  }
 }
 
 struct VocabRow {
@@ -156,13 +171,13 @@ __device__ __forceinline__ void vocab_grad64(const VocabEpi& e, float* stage, in
     const f32x4_t l = *reinterpret_cast<const f32x4_t*>(stage + r * LD + cv);
     const VocabRow q = rows[r];
     f32x4_t v;
-    const RowExp<TERMS == 3> e1(q.c), et(q.ct);
+    const RowExp e1(q.c), et(q.ct);
     const float a1 = e.a1 * e1.k, a2 = e.a2 * et.k;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       const float p = e1(l[c], L2E);
       if constexpr (TEACH) v[c] = a1 * p + a2 * et(l[c], scale_t);
-      else v[c] = TERMS == 3 ? e1.k * p : p;
+      else v[c] = e1.k * p;
     }
     const int at = q.y - e.v0 - col;
     if ((uint32_t)at < 4u) {
@@ -179,19 +194,7 @@ __device__ __forceinline__ void vocab_grad64(const VocabEpi& e, float* stage, in
   auto put = [&](int r, f32x4_t v) {
     cs += v;
     if (col >= e.ldd) return;
-    uint16_t* out = e.dl + (int64_t)(row0 + r) * e.ldd + col;
-    if constexpr (TERMS == 1) {
-      *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
-    } else {
-      float x[4] = {v[0], v[1], v[2], v[3]};
-#pragma unroll
-      for (int t = 0; t < TERMS; ++t) {
-        uint32_t b[4];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) b[c] = bf16_term(x[c]);
-        *reinterpret_cast<uint2*>(out + t * e.plane) = make_uint2(b[0] | (b[1] << 16), b[2] | (b[3] << 16));
-      }
-    }
+    put_terms<TERMS>(e.dl + (int64_t)(row0 + r) * e.ldd + col, e.plane, v);
   };
   if constexpr (!TEACH) {
 #pragma unroll

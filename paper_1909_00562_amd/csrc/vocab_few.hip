@@ -449,10 +449,10 @@ __global__ __launch_bounds__(kFewThreads) void vocab_few_bwd_kernel(FewBwd p) {
         for (int r = 0; r < 4; ++r) {
           const int n = 16 * j + 4 * q + r;
           const float l = acc[j][r] + b;
-          const RowExp<true> e1(s_lse[n]);
+          const RowExp e1(s_lse[n]);
           float d = p.a1 * (e1.k * e1(l, L2E) - (s_y[n] == v ? 1.f : 0.f));
           if constexpr (TEACH) {
-            const RowExp<true> et(s_lt[n]);
+            const RowExp et(s_lt[n]);
             d += p.a2 * (et.k * et(l, L2E * p.inv_tau));
           }
           acc[j][r] = in && n < R ? d : 0.f;
@@ -674,10 +674,10 @@ hipError_t launch_vocab_few(const VocabRows& p, const VocabEpi& e, const void* W
 }
 
 // us, forward and backward, this / the tile kernels: fp32, whose tiles want W as bf16 terms, 1 x 512 x 32000 69 / 135, 16 x 1024 x 32000 143 /
-// 256, 32 x 1024 x 4000 93.4 / 90.8, 48 x 512 x 32000 116 / 159, 64 x 184 x 112000 184 / 281, 64 x 256 x 4000 56.8 / 56.2; bf16, 16 x 512 x 32000 49.4
-// / 53.0, 16 x 184 x 112000 67.6 / 75.2, 16 x 1024 x 32000 82.4 / 82.7 (tiles that round dl once; 102 that do not), 16 x 2048 x 64000 273 / 258,
-// with float gradients 53.6 / 66.0, 74.9 / 100, 98.4 / 107, 328 / 384, 32 x 512 x 32000 65.5 / 70.4, 16 x 1024 x 4000 50.2 / 45.3; past the line, bf16
-// gradients, 32 x 512 x 32000 69.6 / 55.5.
+// 256, 32 x 1024 x 4000 93.4 / 90.8, 48 x 512 x 32000 116 / 159, 64 x 184 x 112000 184 / 281, 64 x 256 x 4000 56.8 / 56.2; bf16, 16 x 512 x 32000 49.1
+// / 57.7, 16 x 184 x 112000 68.5 / 83.1, 16 x 1024 x 32000 82.4 / 91.3, 16 x 2048 x 64000 273 / 298, 16 x 1024 x 4000 50.3 / 42.0, with float
+// gradients 53.2 / 66.1, 75.3 / 101, 97.3 / 109, 327 / 386, 50.1 / 43.9, 32 x 512 x 32000 64.9 / 69.9; past the line, bf16 gradients, 32 x 512 x
+// 32000 69.6 / 61.1.
 bool vocab_few_bwd_rows(int N, int H, int V, bool f32, bool g_bf16) {
   const int nj = (N + 15) / 16, g = few_bwd_groups(H);
   if (H < 4 || H > 2048 || nj * g > 4 || few_bwd_lds(nj, H) > 156 * 1024) return false;

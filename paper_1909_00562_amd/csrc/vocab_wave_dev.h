@@ -182,13 +182,13 @@ __device__ __forceinline__ void vocab_wave_grad(const VocabEpi& e, f32x4_t (&acc
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int at = (r == 0 ? y.x : r == 1 ? y.y : r == 2 ? y.z : y.w) - e.v0 - col0 - c;
-      const RowExp<TERMS == 3> e1(lse[r]), et(lt[r]);
+      const RowExp e1(lse[r]), et(lt[r]);
       const float a1 = e.a1 * e1.k, a2 = e.a2 * et.k;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const float l = acc[i][j][r] + bias[j], p = e1(l, L2E);
         if constexpr (TEACH) acc[i][j][r] = a1 * p + a2 * et(l, scale_t);
-        else acc[i][j][r] = TERMS == 3 ? e1.k * p : p;
+        else acc[i][j][r] = e1.k * p;
       }
       if ((at & ~48) == 0) {
 #pragma unroll
@@ -219,21 +219,7 @@ __device__ __forceinline__ void vocab_wave_grad(const VocabEpi& e, f32x4_t (&acc
       const int row = 16 * i + it * 4 + q;
       const f32x4_t v = v4[it];
       cs += v;
-      if (row < rows_left && col0 + vcol < e.ldd) {
-        uint16_t* out = e.dl + (int64_t)(row0 + row) * e.ldd + col0 + vcol;
-        if constexpr (TERMS == 1) {
-          *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
-        } else {
-          float x[4] = {v[0], v[1], v[2], v[3]};
-#pragma unroll
-          for (int t = 0; t < TERMS; ++t) {
-            uint32_t b[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) b[k] = bf16_term(x[k]);
-            *reinterpret_cast<uint2*>(out + t * e.plane) = make_uint2(b[0] | (b[1] << 16), b[2] | (b[3] << 16));
-          }
-        }
-      }
+      if (row < rows_left && col0 + vcol < e.ldd) put_terms<TERMS>(e.dl + (int64_t)(row0 + row) * e.ldd + col0 + vcol, e.plane, v);
     }
     __builtin_amdgcn_s_waitcnt(kWaitLgkm);   // the slice has been read
   }

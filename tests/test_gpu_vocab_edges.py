@@ -1,0 +1,40 @@
+"""The operators over the vocabulary (include/vocab_ops.h) where their errors would hide: sums that cancel, and further edges of
+their range.  Against the float64 oracle, or torch in float64 for larger calls."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from oracle import vocab_ops_oracle as oracle  # noqa: E402
+from test_gpu_vocab_ops import BF, Case, _round  # noqa: E402
+
+
+def _with(c, h, W, b):
+    """The case with other states, weights and bias."""
+    (c.h, c.h64), (c.W, c.W64), (c.b, c.b64) = (_round(x, c.dtype) for x in (h, W, b))
+    c.h[~torch.from_numpy(c.word)] = float("nan")
+    c.h64[~c.word] = 0.0
+    return c
+
+
+# A model that has learnt how often words come: W and h are mostly what their rows have in common, which cancels in dh (rows of dl sum to 0)
+# and in dW (the words' probabilities are their shares of the targets).  Bound by the norm: the rounding of the result, 2^-8 of it at most, and dl
+# within 2^-17 of itself, together with fp32 sums 2^-16 of the sum of magnitudes.  dl rounded once to bf16 is 1.5 to 2.1 times the bound off in dh.
+@pytest.mark.parametrize("N, H, V, K", [(5, 64, 40, 0), (40, 64, 50, 0), (300, 72, 515, 0), (700, 136, 1003, 0), (700, 136, 1003, 9), (2100, 64, 16500, 0)])
+def test_bf16_gradients_where_the_sums_cancel(N, H, V, K):
+    r = np.random.default_rng(N)
+    y = np.clip(np.exp(r.uniform(size=N) * np.log(V)).astype(np.int64), 1, V - 1)
+    c = Case(N, H, V, "bf16", "bf16", K=K, tau=2.0, targets=y, seed=N)
+    mostly_common = lambda n, s: s * (6 * r.uniform(-1, 1, (1, H)) + r.uniform(-1, 1, (n, H)))  # noqa: E731
+    often = np.bincount(y, minlength=V) + 0.02
+    _with(c, mostly_common(N, 0.12), mostly_common(V, 0.05), np.log(often / often.max()))
+    v = c.device()
+    c.fwd(v)
+    c.bwd(v)
+    o = oracle.loss(c.h64, c.W64, c.b64, c.y, c.pad_id, c.g, c.teacher)
+    dl = np.abs(o["dl"])
+    for k, mag in (("dh", dl @ np.abs(c.W64)), ("dW", dl.T @ np.abs(c.h64)), ("db", dl.sum(axis=0))):
+        off = np.linalg.norm(c.out[k].double().cpu().numpy() - o[k])
+        bound = BF * np.linalg.norm(o[k]) + 2.0 ** -16 * np.linalg.norm(mag)
+        assert off <= bound, (k, off / bound)
