@@ -48,7 +48,7 @@ struct VocabLayout {
   int strips, groups;
   GemmTile t_fwd, t_bwd;
   GemmPlan p_dw, p_dh;
-  bool apart = false;                     // dW, and dh a term at a time, in launches of their own
+  bool apart = false;                     // dW and dh in launches of their own
   // kept from the forward to the backward pass
   size_t rows, row_pos, chunk_words, y, n_act, ticket, hc, lse, lse_tau, at_word, loss_ws, distill_ws, run;
   size_t runs, ent, ent_p, ent_l, place, p_log_p, seen;
@@ -137,17 +137,20 @@ VocabLayout vocab_layout(const vo_shape* s, const vo_teacher* t) {
   const int64_t dl_col = N * 2 * L.dl_terms;
   L.bwd_cols = piece_columns(V, dl_col > w_col ? dl_col : w_col);
   // bf16 gradients of many rows, pieces of twice the columns that are whole rounds of 256 x 256 tiles of dW: those kernels, one behind the
-  // other, dh a term at a time with a split that the device chooses from the rows that there are.  us, the whole call, joint launch of
+  // other; a split of dh's, a term at a time, is chosen by the device from the rows that there are.  us, the whole call, joint launch of
   // 128 x 128 tiles / this: 4096 x 1024 x 32000 1667 / 1533, 5120 2246 / 1995, 6400 with 30 % padding 2103 / 1846, 8192 x 1024 x 16000 with
-  // 30 % 1187 / 1218, 16384 x 2048 x 128000 with 25 % 36070 / 34820; below the line 2257 x 1000 x 32003 with 30 % 759 / 950.
+  // 30 % 1187 / 1218, 16384 x 2048 x 128000 with 25 % 36070 / 34080; below the line 2257 x 1000 x 32003 with 30 % 759 / 950.
   if (L.dl_terms == 2 && N >= 4096) {
     const int64_t cols = piece_columns(V, N * 2), ldd = round_up(cols < V ? cols : V, 8), most = kPieceBytes / (N * L.ldH * 4);
     const int64_t tiles = ((ldd + 255) / 256) * ((H + 255) / 256), rounds = (tiles + 255) / 256;
-    if (tiles * 8 >= rounds * 256 * 7 && most >= 2) {
+    // two rounds of dh's tiles and more: not split, both terms in one launch (split / not, 16384 x 2048 x 128000 with 25 % padding 35010 / 34080
+    // us, 16384 x 2048 x 32000 11500 / 10840)
+    const bool split = ((N + 255) / 256) * ((L.ldH + 255) / 256) < 512;
+    if (tiles * 8 >= rounds * 256 * 7 && (!split || most >= 2)) {
       L.apart = true;
       L.bwd_cols = cols;
       L.p_dw = {kTile256, 1};
-      L.p_dh = {kTile256, most < 4 ? (int)most : 4};
+      L.p_dh = {kTile256, !split ? 1 : most < 4 ? (int)most : 4};
     }
   }
   L.ldd = round_up(L.bwd_cols < V ? L.bwd_cols : V, 8);
@@ -530,7 +533,8 @@ as_status backward(const vo_shape* s, const vo_teacher* t, const void* W, const 
     g[1].partial = w.at<float>(L.partial_dh);
     if (L.apart) {
       e = launch_gemm(g[0], true, L.p_dw.tile, st);
-      for (int i = 0; i < n && e == hipSuccess; ++i) {
+      if (L.p_dh.splits == 1 && e == hipSuccess) e = launch_gemm(g[1], true, L.p_dh.tile, st);
+      for (int i = 0; i < n && L.p_dh.splits > 1 && e == hipSuccess; ++i) {
         GemmArgs one = g[1];
         one.A[0] = g[1].A[i];   // (h and W have one term, so every segment's B is the same)
         one.K[1] = 0;

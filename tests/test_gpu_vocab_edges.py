@@ -7,7 +7,7 @@ torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
 from oracle import vocab_ops_oracle as oracle  # noqa: E402
-from test_gpu_vocab_ops import BF, Case, _round  # noqa: E402
+from test_gpu_vocab_ops import BF, Case, _in_64_bits, _round  # noqa: E402
 
 
 def _with(c, h, W, b):
@@ -38,3 +38,22 @@ def test_bf16_gradients_where_the_sums_cancel(N, H, V, K):
         off = np.linalg.norm(c.out[k].double().cpu().numpy() - o[k])
         bound = BF * np.linalg.norm(o[k]) + 2.0 ** -16 * np.linalg.norm(mag)
         assert off <= bound, (k, off / bound)
+
+
+# dW and dh in launches of their own (from 4096 positions on), dh split and, behind two rounds of its tiles, not; pieces of the vocabulary.  By the
+# norm: the result's rounding, 2^-8 at most, and dl's two terms, 2^-17 of magnitudes that are less than 32 times the result.
+@pytest.mark.parametrize("N, H, V, K", [(4100, 1000, 16003, 0), (4100, 1000, 48001, 6), (16384, 2048, 16001, 0)])
+def test_bf16_gradients_of_many_positions(N, H, V, K):
+    c = Case(N, H, V, "bf16", "bf16", K=K, tau=2.0, seed=N, g=1.0)
+    v = c.device()
+    c.fwd(v)
+    c.bwd(v)
+    o = _in_64_bits(c, c.h_d, c.y_d)
+    first = {}
+    for k in ("dh", "dW", "db"):
+        off = float((c.out[k].double() - o[k]).norm() / o[k].norm())
+        assert off < 17 / 16 * BF, (k, off)
+        assert not c.out["dh"][~torch.from_numpy(c.word).cuda()].any()
+        first[k] = c.out[k].clone()
+    c.bwd(v)
+    assert all(torch.equal(first[k], c.out[k]) for k in first)
