@@ -143,7 +143,7 @@ __device__ __forceinline__ void vocab_wave_grad(const VocabEpi& e, f32x4_t (&acc
   constexpr float L2E = 1.4426950408889634f;
   const int c = lane & 15, q = lane >> 4, strip = (e.v0 + col0) / kVocabStrip;
   const int vcol = c * 4;
-  if (col0 >= ncols) return;
+  if (rows_left <= 0 || col0 >= ncols) return;   // (the teacher's runs end with the last group of rows)
   const float scale_t = L2E * e.inv_tau;
   float bias[4];
 #pragma unroll
@@ -229,7 +229,7 @@ __device__ __forceinline__ void vocab_wave_grad(const VocabEpi& e, f32x4_t (&acc
       cs[k] += __shfl_xor(cs[k], 16, 64);
       cs[k] += __shfl_xor(cs[k], 32, 64);
     }
-    if (q == 0 && rows_left > 0) {
+    if (q == 0) {
       float* out = e.col_sums + (int64_t)(row0 / (16 * TM)) * e.ld_sums + col0 + vcol;
 #pragma unroll
       for (int k = 0; k < 4; ++k)

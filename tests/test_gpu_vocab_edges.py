@@ -57,3 +57,13 @@ def test_bf16_gradients_of_many_positions(N, H, V, K):
         first[k] = c.out[k].clone()
     c.bwd(v)
     assert all(torch.equal(first[k], c.out[k]) for k in first)
+
+
+# Waves of 128 x 128 and 256 x 256 tiles whose rows all lie behind the last word's: they have no entries of the teacher to read.
+@pytest.mark.parametrize("N, H, V, dtype, grad", [(140, 64, 20003, "bf16", "f32"), (300, 64, 65600, "bf16", "bf16"), (385, 40, 33000, "bf16", "f32"), (300, 40, 2001, "f32", "f32")])
+def test_tiles_with_waves_behind_the_last_row(N, H, V, dtype, grad):
+    c = Case(N, H, V, dtype, grad, K=6, tau=2.0, pad=0.0, seed=N)
+    v = c.device()
+    c.fwd(v)
+    c.bwd(v)
+    c.check()
