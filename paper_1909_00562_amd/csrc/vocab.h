@@ -103,7 +103,7 @@ struct VocabTeacher {
   uint32_t* ent;              // [group][16 K]
   float* ent_p;
   int32_t* place;             // [R, K]: entry's index in ent, -1: none
-  float* p_log_p;             // [R]: sum of p log p; NaN-free; seen[r] says whether there are entries
+  float* p_log_p;             // [R]: sum of p log p, 0 without entries; seen[r] says whether there are any
   int32_t* seen;
   int32_t strips;
 };

@@ -326,11 +326,13 @@ __global__ __launch_bounds__(1024) void vocab_finish_kernel(VocabFinish p) {
     // A wave per row of the teacher's entries: their probabilities' sum and that of p l / tau, ahead of what log q needs besides
     constexpr int RW = RPB / 16;
     float pl[RW] = {}, ps[RW] = {};
+    bool has[RW] = {};   // an entry
     if (TEACH && p.last) {
 #pragma unroll
       for (int j = 0; j < RW; ++j) {
         const int row = row0 + wave + 16 * j;
         if (row >= R) continue;
+        has[j] = p.seen[row] != 0;
         for (int k = lane; k < p.K; k += 64) {
           const int at = p.place[(int64_t)row * p.K + k];
           if (at < 0) continue;
@@ -435,7 +437,7 @@ __global__ __launch_bounds__(1024) void vocab_finish_kernel(VocabFinish p) {
       for (int j = 0; j < RW; ++j) {
         const int row = row0 + wave + 16 * j;
         if (row >= R || lane != 0) continue;
-        const float lt = sh_tau[wave + 16 * j], d = lt < INFINITY ? p.tau2 * (p.p_log_p[row] - (pl[j] - ps[j] * lt)) : 0.f;
+        const float lt = sh_tau[wave + 16 * j], d = has[j] ? p.tau2 * (p.p_log_p[row] - (pl[j] - ps[j] * lt)) : 0.f;   // (NaN stays)
         __hip_atomic_store(p.distill_ws + row, d, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         if (p.tok_distill) p.tok_distill[p.rows[row]] = d;
       }

@@ -67,3 +67,36 @@ def test_tiles_with_waves_behind_the_last_row(N, H, V, dtype, grad):
     c.fwd(v)
     c.bwd(v)
     c.check()
+
+
+# A row of a word whose states hold a NaN or an infinity: its losses and the sums say so, whatever the kernels, and so do the gradients that it is
+# part of; other rows keep their bits.
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("N, H, V, dtype, grad, K", [
+    (20, 40, 300, "f32", "f32", 5), (20, 40, 300, "f32", "f32", 0), (14, 64, 300, "bf16", "bf16", 5), (40, 64, 500, "bf16", "bf16", 5), (200, 33, 300, "f32", "f32", 4),
+    (700, 72, 4001, "bf16", "f32", 5), (700, 72, 4001, "bf16", "bf16", 0), (2100, 64, 16500, "bf16", "bf16", 5), (2100, 40, 16500, "f32", "f32", 3)])
+def test_a_row_that_is_not_finite(N, H, V, dtype, grad, K, value):
+    c = Case(N, H, V, dtype, grad, K=K, tau=2.0, pad=0.2, seed=N)
+    at = int(np.nonzero(c.word)[0][N // 3])
+    if K:
+        c.ids[at], c.z[at] = np.arange(K), 0.5                        # it has entries
+    names = ("tok_loss", "loss_sum", "dh", "dW", "db") + (("tok_distill", "distill_sum") if K else ("argmax",))
+    v = c.device()
+    got = []
+    for x in (None, value):
+        if x is not None:
+            c.h_d[at, H // 2] = x
+        c.fwd(v)
+        c.bwd(v)
+        got.append({k: c.out[k].clone() for k in names})
+    clean, dirty = got
+    for k in names:
+        if k in ("loss_sum", "distill_sum", "dW", "db"):
+            assert dirty[k].isnan().all(), k
+            continue
+        others = torch.arange(N, device="cuda") != at
+        assert torch.equal(clean[k][others], dirty[k][others]), k
+        if k == "argmax":
+            assert 0 <= int(dirty[k][at]) < V
+        else:
+            assert dirty[k][at].isnan().all() and clean[k].isfinite().all(), k
