@@ -16,6 +16,7 @@
 
 #include "common.h"
 #include "lds_limit.h"
+#include "row_threads.h"
 #include "status.h"
 
 namespace asx {
@@ -646,13 +647,6 @@ as_status hip_status(hipError_t e, const char* what) {
 // result next finds it there (6400 x 512 30.3 and 33.0, 1237 x 1000 29.6 and 37.7).
 bool past_caches(int64_t rows, int64_t I, int64_t e, int64_t others) { return (rows + others) * I * e > (int64_t)256 << 20; }
 
-// threads for a row of `vecs` vectors, at most a block's
-int row_threads_log(int vecs) {
-  int b = 0;
-  while (b < 8 && (1 << b) < vecs) ++b;
-  return b;
-}
-
 hipError_t launch_sort(const SortDev& p, const EmbedLayout& L, unsigned char* ws, hipStream_t st) {
   auto u32 = [&](size_t at) { return reinterpret_cast<uint32_t*>(ws + at); };
   // the last pass writes key / pos
@@ -696,7 +690,7 @@ hipError_t launch_sums(const SumsDev& p, int tpp, hipStream_t st) {
 }
 template <typename TE, int VEC, bool PAST>
 hipError_t launch_embed_bwd(const SortDev& q, SumsDev p, const EmbedLayout& L, unsigned char* ws, hipStream_t st) {
-  const int tpp = row_threads_log((p.I + kWidth<VEC> - 1) / kWidth<VEC>), zero_blocks = p.accumulate ? 0 : (p.V + kZeroRows - 1) / kZeroRows;
+  const int tpp = row_threads_log(p.pieces, (p.I + kWidth<VEC> - 1) / kWidth<VEC>), zero_blocks = p.accumulate ? 0 : (p.V + kZeroRows - 1) / kZeroRows;
   hipError_t e;
   if (!L.rank) {
     e = launch_sort(q, L, ws, st);
@@ -741,7 +735,7 @@ extern "C" as_status vocab_embed_fwd(const vo_embed* shape, const void* table, c
   auto run = [&](auto* t, auto vec) {
     using TE = typename std::remove_pointer<decltype(t)>::type;
     constexpr int VEC = decltype(vec)::value;
-    const int tpr = row_threads_log((I + kWidth<VEC> - 1) / kWidth<VEC>);
+    const int tpr = row_threads_log(N, (I + kWidth<VEC> - 1) / kWidth<VEC>);
     const int64_t blocks = (((int64_t)N << tpr) + 255) / 256;
     auto kfn = past_caches(N, I, sizeof(TE), 0) ? embed_fwd_kernel<TE, VEC, true> : embed_fwd_kernel<TE, VEC, false>;
     hipLaunchKernelGGL(kfn, dim3((unsigned)blocks), dim3(256), 0, st, reinterpret_cast<const TE*>(table), ids, N, I, V,

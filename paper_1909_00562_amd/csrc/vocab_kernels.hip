@@ -4,6 +4,7 @@
 
 #include "common.h"
 #include "lds_limit.h"
+#include "row_threads.h"
 #include "vocab.h"
 #include "vocab_epi_dev.h"
 
@@ -529,12 +530,6 @@ __global__ __launch_bounds__(256) void vocab_out_grads_kernel(VocabOutGrads p, i
   }
 }
 
-int threads_log(int64_t vecs) {
-  int b = 0;
-  while (b < 8 && ((int64_t)1 << b) < vecs) ++b;
-  return b;
-}
-
 }  // namespace
 
 hipError_t launch_vocab_rows(const VocabRows& p, hipStream_t st) {
@@ -548,7 +543,7 @@ hipError_t launch_vocab_rows(const VocabRows& p, hipStream_t st) {
 }
 
 hipError_t launch_vocab_terms(const float* src, int rows, int H, uint16_t* dst, int64_t ldH, int64_t plane, hipStream_t st) {
-  const int log = threads_log(ldH / 4);
+  const int log = row_threads_log(rows, ldH / 4);
   const int64_t blocks = (((int64_t)rows << log) + 255) / 256;
   hipLaunchKernelGGL(vocab_terms_kernel, dim3((unsigned)blocks), dim3(256), 0, st, src, rows, H, dst, ldH, plane, log);
   return hipGetLastError();
@@ -583,7 +578,7 @@ hipError_t launch_vocab_finish(const VocabFinish& p, hipStream_t st) {
 
 hipError_t launch_vocab_out_grads(const VocabOutGrads& p, bool bf16, hipStream_t st) {
   const bool vec = p.H % 4 == 0;   // (bf16 rows: H % 8 == 0)
-  const int log = threads_log(vec ? p.H / 4 : p.H);
+  const int log = row_threads_log(p.N, vec ? p.H / 4 : p.H);
   const int row_blocks = (int)((((int64_t)p.N << log) + 255) / 256), blocks = row_blocks + (p.db ? (p.V + 63) / 64 : 0);
   if (bf16) hipLaunchKernelGGL((vocab_out_grads_kernel<uint16_t, 4>), dim3(blocks), dim3(256), 0, st, p, log, row_blocks);
   else if (vec) hipLaunchKernelGGL((vocab_out_grads_kernel<float, 4>), dim3(blocks), dim3(256), 0, st, p, log, row_blocks);

@@ -6,6 +6,7 @@ import pytest
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
+import paper_1909_00562_amd as lib  # noqa: E402
 from oracle import vocab_ops_oracle as oracle  # noqa: E402
 from test_gpu_vocab_ops import BF, Case, _in_64_bits, _round  # noqa: E402
 
@@ -100,3 +101,56 @@ def test_a_row_that_is_not_finite(N, H, V, dtype, grad, K, value):
             assert 0 <= int(dirty[k][at]) < V
         else:
             assert dirty[k][at].isnan().all() and clean[k].isfinite().all(), k
+
+
+# The most positions that there may be, with rows of more vectors than half a block has threads.
+def _room(gib):
+    torch.cuda.empty_cache()
+    free = torch.cuda.mem_get_info()[0]
+    if free < gib << 30:
+        pytest.skip(f"{free >> 30} GiB free")
+
+
+def test_embedding_of_the_most_positions():
+    _room(48)
+    N, I, V = 1 << 24, 516, 1000
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    table = torch.empty(V, I, device="cuda").uniform_(-1, 1, generator=gen)
+    ids = torch.randint(-V // 4, V, (N,), device="cuda", dtype=torch.int32, generator=gen)
+    x = lib.DeviceEmbed(table, N, pad_id=0, scale=2.0).fwd(ids)
+    for at in torch.arange(N, device="cuda").split(1 << 21):
+        want = torch.where((ids[at] > 0)[:, None], table[ids[at].clamp(min=0).long()] * 2, 0)       # (twice a value is exact)
+        assert torch.equal(x[at], want)
+
+
+def test_cross_entropy_of_the_most_positions():
+    _room(130)
+    N, H, V, bf = 1 << 24, 520, 8, torch.bfloat16
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    W = torch.empty(V, H, device="cuda", dtype=bf).uniform_(-0.06, 0.06, generator=gen)
+    h = torch.empty(N, H, device="cuda", dtype=bf).uniform_(-1, 1, generator=gen)
+    y = torch.randint(-2, V, (N,), device="cuda", dtype=torch.int32, generator=gen)
+    v = lib.DeviceVocabLoss(W, None, N, pad_id=0, grad_scale=1.0)
+    loss, n_tok = torch.empty(1, device="cuda"), torch.empty(1, device="cuda", dtype=torch.int32)
+    v.xent_fwd(h, y, loss, n_tok)
+    dh, dW, db = torch.full_like(h, 7.0), torch.empty_like(W), torch.empty(V, device="cuda", dtype=bf)
+    v.xent_bwd(dh, dW, db)
+    assert int(n_tok) == int((y > 0).sum())
+    zero = lambda *n: torch.zeros(*n, device="cuda", dtype=torch.float64)  # noqa: E731
+    W64, o_dW, o_db, loss64, off = W.double(), zero(V, H), zero(V), zero(1), zero(2)
+    for at in torch.arange(N, device="cuda").split(1 << 20):
+        x, t, word = h[at].double(), y[at].clamp(min=0).long()[:, None], (y[at] > 0)[:, None]
+        l = x @ W64.t()
+        lse = torch.logsumexp(l, 1, keepdim=True)
+        dl = torch.where(word, torch.exp(l - lse).scatter_add_(1, t, torch.full_like(lse, -1.0)), 0.0)
+        loss64 += torch.where(word, lse - l.gather(1, t), 0.0).sum()
+        o_dW += dl.t() @ x
+        o_db += dl.sum(0)
+        o = dl @ W64
+        off += torch.stack([(dh[at].double() - o).square().sum(), o.square().sum()])
+        assert not dh[at][~word[:, 0]].any()
+    # norms: the results' rounding, and fp32 sums of 2^24 terms in a few hundred parts, 2^-24 sqrt(2^24) of their magnitudes at most
+    assert float((off[0] / off[1]).sqrt()) < 2 * BF
+    for k, got, o in (("dW", dW, o_dW), ("db", db, o_db)):
+        assert float((got.double() - o).norm() / o.norm()) < 2 * BF, k
+    assert abs(float(loss) - float(loss64)) < 1e-5 * float(loss64)

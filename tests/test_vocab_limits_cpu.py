@@ -1,0 +1,40 @@
+"""Host arithmetic of the operators over the vocabulary at the edges of their documented range, without a GPU."""
+import os
+import shutil
+import subprocess
+
+import pytest
+
+from paper_1909_00562_amd import binding as bd
+
+CSRC = os.path.join(os.path.dirname(bd.library_path()), "csrc")
+
+ROW_THREADS_MAIN = """
+#include "row_threads.h"
+int main() {
+  auto expect = [](bool ok) { if (!ok) __builtin_trap(); };
+  for (int64_t rows = 1; rows <= 1 << 24; rows = rows < 1000 ? rows + 1 : rows * 2 - 7)
+    for (int64_t vecs = 1; vecs <= 1 << 16; vecs = vecs * 3 / 2 + 1) {
+      const int b = asx::row_threads_log(rows, vecs);
+      expect(b >= 0 && b <= 8 && (b == 0 || (1 << (b - 1)) < vecs));                   // no more than its vectors
+      expect((((rows << b) + 255) / 256) * 256 <= (int64_t)1 << 31);
+      if (rows <= 1 << 23) expect(b == 8 || (1 << b) >= vecs);                         // and no fewer
+    }
+  const int64_t most = 1 << 24;
+  expect(asx::row_threads_log(most, 1 << 14) == 7 && asx::row_threads_log(most, 130) == 7 && asx::row_threads_log(most, 128) == 7);
+  expect(asx::row_threads_log(most, 5) == 3 && asx::row_threads_log(1 << 23, 130) == 8);
+}
+"""
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="no host compiler")
+def test_threads_of_the_most_rows_fit_a_launch(tmp_path):
+    """2^24 rows of 256 threads are 2^32, one more than a launch takes along a dimension."""
+    (tmp_path / "main.cpp").write_text(ROW_THREADS_MAIN)
+    exe = tmp_path / "main"
+    subprocess.run(["g++", "-std=c++17", f"-I{CSRC}", str(tmp_path / "main.cpp"), "-o", str(exe)], check=True)
+    subprocess.run([str(exe)], check=True)
+    # and the launchers that walk rows go by it
+    for name, calls in (("embed.hip", 2), ("vocab_kernels.hip", 2)):
+        text = open(os.path.join(CSRC, name)).read()
+        assert text.count("row_threads_log(") == calls and "threads_log(" not in text.replace("row_threads_log(", ""), name
