@@ -92,6 +92,9 @@ struct GemmArgs {
   // contiguous, bf16 C, bias alone): row_stats[row * tile columns + tile column]
   struct TileStat* row_stats = nullptr;
 };
+// The one factor in a product kernel's arguments: dropout's where the kernel itself drops elements, else alpha.  With a split the
+// combine drops elements, with a drop_scale of its own, so the partial sums are not scaled.
+inline float gemm_kernel_scale(const GemmArgs& g) { return g.drop_thr && g.splits <= 1 ? g.drop_scale : g.alpha; }
 // maximum, sum of exp relative to it, lowest column that attains it (INT_MAX: none, all values are -inf or NaN)
 struct alignas(16) TileStat {
   float m, s;

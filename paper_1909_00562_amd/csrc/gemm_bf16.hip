@@ -1071,7 +1071,7 @@ static hipError_t gemm_describe(const GemmArgs& g, GemmTile tile, GemmDev& d) {
   d.ldg = g.ldg;
   d.act_tanh = g.act_tanh;
   d.drop_thr = g.splits > 1 ? 0u : g.drop_thr;   // with split-K the combine step applies the epilogue
-  d.drop_scale = g.drop_thr ? g.drop_scale : g.alpha;
+  d.drop_scale = gemm_kernel_scale(g);
   d.drop_seed = g.drop_seed;
   d.accumulate = g.accumulate;
   d.splits = g.splits;

@@ -29,7 +29,7 @@ struct GemmDev {
   int64_t ldg;
   int act_tanh, accumulate;
   uint32_t drop_thr;
-  float drop_scale;   // where nothing is dropped: GemmArgs::alpha
+  float drop_scale;   // gemm_kernel_scale
   uint64_t drop_seed;
   int splits;
   float* partial;

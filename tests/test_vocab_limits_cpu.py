@@ -38,3 +38,43 @@ def test_threads_of_the_most_rows_fit_a_launch(tmp_path):
     for name, calls in (("embed.hip", 2), ("vocab_kernels.hip", 2)):
         text = open(os.path.join(CSRC, name)).read()
         assert text.count("row_threads_log(") == calls and "threads_log(" not in text.replace("row_threads_log(", ""), name
+
+
+HIP_STUB = """
+#pragma once
+#include <stddef.h>
+#define __host__
+#define __device__
+enum hipError_t { hipSuccess = 0 };
+typedef void* hipStream_t;
+"""
+SCALE_MAIN = """
+#include "gemm.h"
+int main() {
+  auto expect = [](bool ok) { if (!ok) __builtin_trap(); };
+  asx::GemmArgs g;
+  expect(asx::gemm_kernel_scale(g) == 1.f);
+  g.alpha = 0.25f;
+  expect(asx::gemm_kernel_scale(g) == 0.25f);
+  g.splits = 4;
+  expect(asx::gemm_kernel_scale(g) == 0.25f);
+  g.alpha = 1.f;                                  // dropout, in the kernel or by a split's combine
+  g.drop_thr = 1u << 30;
+  g.drop_scale = 4.f / 3.f;
+  expect(asx::gemm_kernel_scale(g) == 1.f);
+  g.splits = 1;
+  expect(asx::gemm_kernel_scale(g) == 4.f / 3.f);
+}
+"""
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="no host compiler")
+def test_dropout_of_a_split_product_scales_once(tmp_path):
+    """The partial sums of a split keep their size where the combine drops and scales elements."""
+    (tmp_path / "hip").mkdir()
+    (tmp_path / "hip" / "hip_runtime.h").write_text(HIP_STUB)
+    (tmp_path / "main.cpp").write_text(SCALE_MAIN)
+    exe = tmp_path / "main"
+    subprocess.run(["g++", "-std=c++17", f"-I{tmp_path}", f"-I{CSRC}", str(tmp_path / "main.cpp"), "-o", str(exe)], check=True)
+    subprocess.run([str(exe)], check=True)
+    assert "d.drop_scale = gemm_kernel_scale(g);" in open(os.path.join(CSRC, "gemm_bf16.hip")).read()
