@@ -540,6 +540,12 @@ class _DeviceOp:
             raise AttnSoftmaxError(2, f"tensors are on {device}, expected a GPU")
         self.torch, self.dev, self.index = torch, device, device.index
         self.lib = load_library()
+        self.workspace = None
+
+    def _own_workspace(self):
+        torch = self.torch
+        self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.dev)
+        self.home = torch.cuda.current_stream(self.dev).cuda_stream
 
     def _tensor(self, t, shape, dtype, name):
         if t is None:
@@ -558,9 +564,13 @@ class _DeviceOp:
         return None if t is None else self._tensor(t, shape, dtype, name)
 
     def _call(self, function, *args):
-        """function(*args, stream), for addresses that _tensor has checked"""
+        """function(*args, stream), for addresses that _tensor has checked.  The workspace is the handle's own, so the allocator is
+        told here of a stream other than the one it was allocated on: a handle may be dropped while calls are on their way."""
         cuda = self.torch.cuda
-        stream = cuda.current_stream(self.dev).cuda_stream or None
+        current = cuda.current_stream(self.dev)
+        stream = current.cuda_stream or None
+        if self.workspace is not None and current.cuda_stream != self.home:
+            self.workspace.record_stream(current)
         if cuda.current_device() == self.index:
             rc = function(*args, stream)
         else:
@@ -588,7 +598,6 @@ class DeviceEmbed(_DeviceOp):
         self.ws_bytes = vocab_embed_workspace_bytes(self.shape)
         if self.ws_bytes == 0:
             raise AttnSoftmaxError(2, "invalid shape for the embedding")
-        self.workspace = None
 
     def fwd(self, ids, x=None):
         """x [N,I] = scale * table[ids]; ids [N] int32."""
@@ -607,7 +616,7 @@ class DeviceEmbed(_DeviceOp):
                 raise AttnSoftmaxError(1, "d_table is None")
             d_table = torch.empty(s.V, s.I, dtype=self.gdt, device=self.dev)
         if self.workspace is None:
-            self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.dev)
+            self._own_workspace()
         self._call(self.lib.vocab_embed_bwd, self.shape_ref, self._tensor(ids, self.n, torch.int32, "ids"),
                    self._tensor(dy, self.rows, self.gdt, "dy"), self._tensor(d_table, (s.V, s.I), self.gdt, "d_table"),
                    int(accumulate), self.workspace.data_ptr(), self.ws_bytes)
@@ -635,7 +644,7 @@ class DeviceVocabLoss(_DeviceOp):
         self.ws_bytes = vocab_xent_workspace_bytes(self.shape, self.teacher)
         if self.ws_bytes == 0:
             raise AttnSoftmaxError(2, "invalid shape for the vocabulary loss")
-        self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.dev)
+        self._own_workspace()
         self.done = False
 
     def _weights(self):

@@ -22,7 +22,7 @@ def _with(c, h, W, b):
 # A model that has learnt how often words come: W and h are mostly what their rows have in common, which cancels in dh (rows of dl sum to 0)
 # and in dW (the words' probabilities are their shares of the targets).  Bound by the norm: the rounding of the result, 2^-8 of it at most, and dl
 # within 2^-17 of itself, together with fp32 sums 2^-16 of the sum of magnitudes.  dl rounded once to bf16 is 1.5 to 2.1 times the bound off in dh.
-@pytest.mark.parametrize("N, H, V, K", [(5, 64, 40, 0), (40, 64, 50, 0), (300, 72, 515, 0), (700, 136, 1003, 0), (700, 136, 1003, 9), (2100, 64, 16500, 0)])
+@pytest.mark.parametrize("N, H, V, K", [(5, 64, 40, 0), (16, 2056, 60, 0), (12, 64, 200, 5), (40, 64, 50, 0), (300, 72, 515, 0), (700, 136, 1003, 0), (700, 136, 1003, 9), (2100, 64, 16500, 0)])
 def test_bf16_gradients_where_the_sums_cancel(N, H, V, K):
     r = np.random.default_rng(N)
     y = np.clip(np.exp(r.uniform(size=N) * np.log(V)).astype(np.int64), 1, V - 1)
@@ -154,3 +154,26 @@ def test_cross_entropy_of_the_most_positions():
     for k, got, o in (("dW", dW, o_dW), ("db", db, o_db)):
         assert float((got.double() - o).norm() / o.norm()) < 2 * BF, k
     assert abs(float(loss) - float(loss64)) < 1e-5 * float(loss64)
+
+
+def test_a_handle_dropped_while_another_stream_works_on_it():
+    """Its workspace is not given to others before that stream is through."""
+    c = Case(40, 64, 500, "bf16", "f32", seed=7)
+    a = torch.randn(8192, 8192, device="cuda")
+    side = torch.cuda.Stream()
+    v, e = c.device(), lib.DeviceEmbed(torch.zeros(500, 64, device="cuda"), 40)
+    d = e.bwd(c.y_d, torch.zeros(40, 64, device="cuda"))             # (allocates its workspace here)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(20):
+            a @ a
+        c.fwd(v)
+        c.bwd(v)
+        e.bwd(c.y_d, c.out["dh"], d)
+    busy = {(w.data_ptr(), w.numel()) for w in (v.workspace, e.workspace)}
+    del v, e
+    others = [torch.empty(n, dtype=torch.uint8, device="cuda") for _, n in busy for _ in range(4)]
+    assert not side.query(), "the stream was through too early to tell"
+    assert not {t.data_ptr() for t in others} & {p for p, _ in busy}
+    torch.cuda.synchronize()
+    c.check()
