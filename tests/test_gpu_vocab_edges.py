@@ -1,5 +1,8 @@
 """The operators over the vocabulary (include/vocab_ops.h) where their errors would hide: sums that cancel, and further edges of
 their range.  Against the float64 oracle, or torch in float64 for larger calls."""
+import os
+import re
+
 import numpy as np
 import pytest
 
@@ -8,7 +11,8 @@ pytestmark = pytest.mark.gpu
 
 import paper_1909_00562_amd as lib  # noqa: E402
 from oracle import vocab_ops_oracle as oracle  # noqa: E402
-from test_gpu_vocab_ops import BF, Case, _in_64_bits, _round  # noqa: E402
+from paper_1909_00562_amd import binding as bd  # noqa: E402
+from test_gpu_vocab_ops import BF, U, Case, _in_64_bits, _round, _untouched  # noqa: E402
 
 
 def _with(c, h, W, b):
@@ -177,3 +181,70 @@ def test_a_handle_dropped_while_another_stream_works_on_it():
     assert not {t.data_ptr() for t in others} & {p for p, _ in busy}
     torch.cuda.synchronize()
     c.check()
+
+
+# ---- pieces of the vocabulary ----------------------------------------------------------------------------------------------
+# What a piece may take is a constant of vocab.hip: the cases below stay several pieces when it changes, or say so.
+def _piece_bytes():
+    text = open(os.path.join(os.path.dirname(bd.library_path()), "csrc", "vocab.hip")).read()
+    n, shift = re.search(r"constexpr int64_t kPieceBytes = \(int64_t\)(\d+) << (\d+);", text).groups()
+    return int(n) << int(shift)
+
+
+def _at_most_in_a_piece(N, H, dtype, grad):
+    """Columns of a piece (forward, backward): statistics or terms of W, dl or terms of W; 2^20 at most."""
+    terms = (H + 7) // 8 * 8 * 6 if dtype == "f32" else 0
+    dl = N * 2 * (1 if grad == "bf16" else 3)                          # (bf16 gradients of many positions: so much per term)
+    return tuple(min(1 << 20, _piece_bytes() // max(x, terms)) for x in (N * 16 // 64, dl))
+
+
+@pytest.mark.parametrize("N, H, V, dtype, grad, K, pieces", [
+    (140, 512, 180001, "f32", "f32", 0, (3, 3)), (140, 512, 180001, "f32", "f32", 7, (3, 3)),            # terms of W, both passes
+    (9000, 64, 130003, "bf16", "f32", 0, (2, 2)), (9000, 64, 260003, "bf16", "bf16", 4, (3, 3)),           # statistics and dl
+    (40, 8, (1 << 20) + 5, "bf16", "f32", 0, (2, 2)), (140, 8, (2 << 20) + 300, "f32", "f32", 0, (3, 3))])
+def test_pieces_of_the_vocabulary(N, H, V, dtype, grad, K, pieces):
+    assert all(V > (p - 1) * most for p, most in zip(pieces, _at_most_in_a_piece(N, H, dtype, grad)))
+    c = Case(N, H, V, dtype, grad, K=K, tau=2.0, seed=3, g=1.0, spread=2.0)
+    v = c.device()
+    c.fwd(v)
+    c.bwd(v)
+    o = _in_64_bits(c, c.h_d, c.y_d)
+    # norms: fp32 sums of up to 10^6 terms of either sign, 2^-24 sqrt(10^6); bf16 gradients: their rounding
+    for k in ("tok_loss", "dh", "dW", "db") + (("tok_distill",) if K else ()):
+        off = float((c.out[k].double() - o[k]).norm() / o[k].norm())
+        assert off < (17 / 16 * BF if grad == "bf16" and k in ("dh", "dW", "db") else 1000 * U), (k, off)
+        if k in ("dW", "db"):                                          # each piece by itself: none is lost among the others
+            for at in torch.arange(V, device="cuda").split(1 << 16):
+                part = o[k][at].norm()
+                assert float((c.out[k][at].double() - o[k][at]).norm() / part) < (17 / 16 * BF if grad == "bf16" else 2000 * U), (k, int(at[0]))
+    for k in ("loss_sum", "distill_sum")[:2 if K else 1]:
+        want = float(o["tok_loss" if k == "loss_sum" else "tok_distill"].sum())
+        assert abs(float(c.out[k]) - want) < 1e-5 * abs(want)
+    if not K:
+        word = torch.from_numpy(c.word).cuda()
+        W, b, got = c.W.cuda().double(), c.b.cuda().double(), c.out["argmax"].long()
+        assert (got[~word] == c.pad_id).all()
+        reach = set()
+        for at in torch.nonzero(word)[:, 0].split(500):
+            l = c.h_d[at].double() @ W.t() + b
+            # (logits off by 2^-24 (6 H + 8) times their terms' magnitudes, twice)
+            El = 2 * (6 * H + 8) * U * (c.h_d[at].double().abs() @ W.abs().t() + b.abs()).max(1).values
+            assert (l.gather(1, got[at][:, None])[:, 0] + 2 * El >= l.max(1).values).all()
+            reach |= set((got[at] * pieces[0] // V).tolist())
+        assert len(reach) == pieces[0]                                 # maxima lie in every piece
+    _untouched(*c.bases.values())
+
+
+# Equal words next to each other, in one strip of 64 columns and in tiles far apart, in the 64 x 64, 128 x 128 and 256 x 256 kernels and those for few rows
+@pytest.mark.parametrize("N, H, V, dtype", [(20, 40, 1000, "f32"), (30, 64, 1000, "bf16"), (40, 64, 400, "bf16"), (700, 72, 8004, "bf16"), (300, 40, 6000, "f32"),
+                                            (2100, 64, 33000, "bf16"), (2100, 40, 33000, "f32")])
+def test_the_lowest_of_equal_words_wins_in_all_kernels(N, H, V, dtype):
+    c = Case(N, H, V, dtype, "f32", pad=0.1, seed=N)
+    same = (np.arange(V) % (V // 2)) // 2 * 2                           # words v, v + 1 and both V / 2 further on, v even
+    c.W, c.b = c.W[same], c.b[same]
+    c.W64, c.b64 = c.W.double().numpy(), c.b.double().numpy()
+    v = c.device()
+    c.fwd(v)
+    got = c.out["argmax"][torch.from_numpy(c.word).cuda()]
+    assert (got < V // 2).all() and (got % 2 == 0).all()
+    c.check(back=False)
