@@ -75,7 +75,7 @@ typedef struct {
 /* A teacher's top logits.  Entries whose id lies outside [0,V) or whose logit is -inf are absent; an id may come twice. */
 typedef struct {
   int32_t K;          /* entries per position, 1 .. 256; V <= 2^20 then */
-  float temperature;  /* tau > 0; tau^2, 1 / tau and s tau are finite */
+  float temperature;  /* tau >= 2^-10 (fp32 logits over less have no digits left); tau^2 and s tau are finite */
   float scale;        /* s */
 } vo_teacher;
 

@@ -69,9 +69,11 @@ bool shape_ok(const vo_shape* s) {
   if ((int64_t)s->V * s->H >= (int64_t)1 << 40) return false;
   return s->pad_id >= -1 && s->pad_id < s->V && std::isfinite(s->grad_scale);
 }
+// Temperatures from 2^-10 on: a log-sum-exp of l / tau in fp32 is off by |l| / tau 2^-24, and far below that limit by so much that the
+// probabilities made from it would overflow (l = 30 at tau = 1e-9: e^1800).
 bool teacher_ok(const vo_shape* s, const vo_teacher* t) {
-  return t->K >= 1 && t->K <= kTeacherMaxK && s->V <= (1 << 20) && round_up(s->N, kVocabGroup) * t->K < ((int64_t)1 << 31) && t->temperature > 0.f &&
-         std::isfinite(t->temperature * t->temperature) && std::isfinite(1.f / t->temperature) && std::isfinite(t->scale) &&
+  return t->K >= 1 && t->K <= kTeacherMaxK && s->V <= (1 << 20) && round_up(s->N, kVocabGroup) * t->K < ((int64_t)1 << 31) &&
+         t->temperature >= 0x1p-10f && std::isfinite(t->temperature * t->temperature) && std::isfinite(t->scale) &&
          std::isfinite(t->scale * t->temperature);
 }
 

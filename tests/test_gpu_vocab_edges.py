@@ -248,3 +248,14 @@ def test_the_lowest_of_equal_words_wins_in_all_kernels(N, H, V, dtype):
     got = c.out["argmax"][torch.from_numpy(c.word).cuda()]
     assert (got < V // 2).all() and (got % 2 == 0).all()
     c.check(back=False)
+
+
+# The lowest temperature: probabilities of nearly 0 and 1
+@pytest.mark.parametrize("N, H, V, dtype, grad", [(20, 40, 300, "f32", "f32"), (40, 64, 500, "bf16", "f32"), (700, 72, 4001, "bf16", "bf16")])
+def test_the_lowest_temperature(N, H, V, dtype, grad):
+    c = Case(N, H, V, dtype, grad, K=6, tau=2.0 ** -10, seed=N)
+    v = c.device()
+    c.fwd(v)
+    c.bwd(v)
+    c.check()
+    assert all(c.out[k].isfinite().all() for k in ("tok_distill", "dh", "dW", "db"))

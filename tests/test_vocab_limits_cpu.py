@@ -78,3 +78,15 @@ def test_dropout_of_a_split_product_scales_once(tmp_path):
     subprocess.run(["g++", "-std=c++17", f"-I{tmp_path}", f"-I{CSRC}", str(tmp_path / "main.cpp"), "-o", str(exe)], check=True)
     subprocess.run([str(exe)], check=True)
     assert "d.drop_scale = gemm_kernel_scale(g);" in open(os.path.join(CSRC, "gemm_bf16.hip")).read()
+
+
+A = [0x10000 * (i + 1) for i in range(16)]     # addresses that are never read: the checks come first
+
+
+@pytest.mark.parametrize("tau, taken", [(2.0 ** -10, True), (2.0 ** -10 * (1 - 2.0 ** -24), False), (1e-9, False), (1e-30, False), (-1.0, False)])
+def test_temperatures_below_which_probabilities_overflow(tau, taken):
+    s, t = bd.VoShape(5, 16, 100, 0, bd.AS_BF16, bd.AS_F32, 1.0), bd.VoTeacher(4, tau, 1.0)
+    assert (bd.vocab_xent_workspace_bytes(s, t) > 0) == taken
+    code = 4 if taken else 2                   # (a workspace of no bytes, or the teacher)
+    assert bd.vocab_distill_fwd(s, t, *A[:12], 0, check=False) == code
+    assert bd.vocab_distill_bwd(s, t, A[0], A[1], A[2], 0, A[3], A[4], A[5], check=False) == code
