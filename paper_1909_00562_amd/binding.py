@@ -581,8 +581,8 @@ class _DeviceOp:
 
 
 class DeviceEmbed(_DeviceOp):
-    """Embedding of up to N positions at a time in a table [V,I] (a device tensor, not copied): owns the workspace of the
-    backward pass and forwards to the C ABI.  grad_dtype: "f32" or "bf16", the type of dy and of the table's gradient."""
+    """Embedding of N positions at a time (shorter batches: ids of -1 behind them, or a handle of their own length) in a table
+    [V,I] (a device tensor, not copied): owns the workspace of the backward pass and forwards to the C ABI.  grad_dtype: "f32" or "bf16", the type of dy and of the table's gradient."""
 
     def __init__(self, table, N, pad_id=-1, scale=1.0, grad_dtype=None):
         self._on(table.device)
