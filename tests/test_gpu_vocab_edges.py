@@ -259,3 +259,25 @@ def test_the_lowest_temperature(N, H, V, dtype, grad):
     c.bwd(v)
     c.check()
     assert all(c.out[k].isfinite().all() for k in ("tok_distill", "dh", "dW", "db"))
+
+
+# dW and dh in launches of their own, with three words and with none among the positions
+@pytest.mark.parametrize("N, H, V, K", [(5000, 1000, 16003, 0), (5000, 1000, 16003, 5), (16384, 2048, 8003, 0)])
+def test_a_few_words_or_none_among_many_positions(N, H, V, K):
+    y = np.full(N, -1)
+    y[[0, N // 2, N - 1]] = [1, V - 1, V // 3]
+    c = Case(N, H, V, "bf16", "bf16", K=K, tau=2.0, targets=y, seed=N)
+    v = c.device()
+    c.fwd(v)
+    c.bwd(v)
+    o = _in_64_bits(c, c.h_d, c.y_d)
+    for k in ("dh", "dW", "db"):
+        assert float((c.out[k].double() - o[k]).norm() / o[k].norm()) < 17 / 16 * BF, k
+    assert int(c.out["n_tok"]) == 3 and not c.out["dh"][1:N // 2].any()
+    c.y_d.fill_(V)
+    c.fwd(v)
+    c.bwd(v)
+    assert int(c.out["n_tok"]) == 0
+    for k in ("loss_sum", "tok_loss", "dh", "dW", "db") + (("distill_sum", "tok_distill") if K else ()):
+        assert not c.out[k].any(), k
+    _untouched(*c.bases.values())
