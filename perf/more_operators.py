@@ -1,0 +1,381 @@
+"""The operators of serving word by word as cases that can be timed and compared: a paged cache of keys and values, the attention
+that reads it, and the check of drafted words.
+
+  cache   new tokens' keys and values into the pages of their sequences (as they are, or in 8 bits with a scale for each token
+          and head), and places of the cache read back as dense rows
+  attn    attention of each sequence's newest T tokens over its cached ones; heads of queries share heads of the cache
+  verify  words that a small model drafted, accepted or not against the large model's probabilities, and the word that follows them
+
+`own` chooses between the plain form in elementary torch operations and the calls into `paper_1909_00562_amd`.
+
+Keys, values and queries are N(0,1), queries somewhat wider, so that the attention is neither flat nor a choice of one token; what
+lies behind a sequence's end in its last page is NaN, which no output may show.
+"""
+import math
+
+import torch
+
+own = False
+
+DEV = "cuda"
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "int8": torch.int8, "e4m3": torch.float8_e4m3fn}
+SIZE = {"f32": 4, "bf16": 2, "int8": 1, "e4m3": 1}
+LARGEST = {"int8": 127.0, "e4m3": 448.0}
+LEAST_SCALE = 2.0 ** -120
+
+
+def listed():
+    return [
+        # the tokens of one step of a few sentences, into an int8 cache
+        dict(name="cache_step", op="cache", B=32, T=1, L=700, even=False, kv=8, D=64, page=16, dtype="bf16", cache="int8", pad=0.0, back=0),
+        # a packed batch of prompts of uneven length with padding, sizes that fit nothing; earlier places are read back beside the new ones
+        dict(name="cache_ragged", op="cache", B=13, T=190, L=1237, even=False, kv=3, D=80, page=48, dtype="f32", cache="e4m3", pad=0.2, back=5000),
+        # sequences that leave the card: what they hold is read out of a cache in the storage type, while all others take a step
+        dict(name="cache_move", op="cache", B=64, T=1, L=2048, even=True, kv=8, D=128, page=64, dtype="bf16", cache="bf16", pad=0.0, back=30000),
+        # prompts of a large batch at once
+        dict(name="cache_prompt", op="cache", B=16, T=4096, L=0, even=True, kv=8, D=128, page=64, dtype="bf16", cache="int8", pad=0.0, back=0),
+        # interactive decoding of one sentence
+        dict(name="attn_one", op="attn", B=1, T=1, L=700, even=True, q=8, kv=8, D=64, page=16, window=0, dtype="bf16", cache="bf16"),
+        # fp32 throughout: validation of a small model
+        dict(name="attn_f32", op="attn", B=16, T=1, L=1999, even=False, q=16, kv=16, D=64, page=16, window=0, dtype="f32", cache="f32"),
+        # drafted tokens of a few sequences seen at once, a window, many queries to a head, e4m3
+        dict(name="attn_draft", op="attn", B=24, T=5, L=5000, even=False, q=16, kv=2, D=96, page=32, window=1000, dtype="bf16", cache="e4m3"),
+        # two very long documents in int8
+        dict(name="attn_long", op="attn", B=2, T=1, L=131071, even=True, q=32, kv=8, D=128, page=128, window=0, dtype="bf16", cache="int8"),
+        # a full server: sequences of every length up to 8192
+        dict(name="attn_batch", op="attn", B=64, T=1, L=8192, even=False, q=32, kv=8, D=128, page=64, window=0, dtype="bf16", cache="bf16"),
+        # one sentence, four drafted words
+        dict(name="verify_one", op="verify", B=1, T=4, V=32000, ld=32000, dtype="bf16", tau=1.0, short=0.0),
+        # drafts of uneven length, fp32 logits in padded rows
+        dict(name="verify_ragged", op="verify", B=37, T=5, V=32003, ld=32008, dtype="f32", tau=0.7, short=0.4),
+        # a full server with a large vocabulary
+        dict(name="verify_large", op="verify", B=128, T=4, V=128000, ld=128000, dtype="bf16", tau=1.0, short=0.0),
+    ]
+
+
+def _log(rng, lo, hi):
+    """A whole number of lo..hi, even over the logarithm."""
+    return min(hi, max(lo, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def draw(rng):
+    op = rng.choice(["cache", "attn", "attn", "verify"])
+    dtype = rng.choice(["bf16", "bf16", "f32"])
+    if op == "verify":
+        V, T = _log(rng, 1000, 128000), _log(rng, 1, 8)
+        most = 73000000 if dtype == "f32" else 147000000
+        B = _log(rng, 1, max(1, min(256, most // (V * (2 * T + 1)))))
+        return dict(op=op, B=B, T=T, V=V, ld=(V + 7) // 8 * 8, dtype=dtype, tau=rng.choice([1.0, rng.uniform(0.3, 1.5)]),
+                    short=rng.choice([0.0, rng.uniform(0.1, 0.9)]))
+    cache = rng.choice([dtype, "int8", "e4m3"])
+    D, kv = 16 * _log(rng, 2, 16), _log(rng, 1, 16)
+    c = dict(op=op, kv=kv, D=D, page=rng.choice([16, 32, 48, 64, 128]), dtype=dtype, cache=cache, even=rng.random() < 0.3)
+    if op == "cache":
+        most = 30000000 // (D * kv)
+        B = _log(rng, 1, 64)
+        T = rng.choice([1, _log(rng, 1, max(1, most // B))])
+        return dict(c, B=B, T=T, L=_log(rng, 1, 4096), pad=rng.choice([0.0, rng.uniform(0.05, 0.5)]), back=rng.choice([0, _log(rng, 1, max(1, most // 2))]))
+    most = 260000000 // (D * kv)
+    B = _log(rng, 1, max(1, min(256, most // 64)))
+    return dict(c, B=B, T=rng.choice([1, 1, _log(rng, 2, 8)]), L=_log(rng, 1, max(1, min(131072, most // B))), q=kv * rng.choice([1, 2, 3, 4, 8]),
+                window=rng.choice([0, 0, _log(rng, 1, 4096)]))
+
+
+def _lengths(n, top, even):
+    """n lengths up to `top`: all the same, or spread evenly from 1 on."""
+    return [top] * n if even else [1 + (top - 1) * i // max(1, n - 1) for i in range(n)]
+
+
+def _codes(x, cache):
+    """(codes, scales) of rows of floats in 8 bits: scale = max |x| / the type's largest value, code = x * (1 / scale) rounded to even."""
+    scale = (x.abs().amax(dim=-1) / LARGEST[cache]).clamp(min=LEAST_SCALE)
+    x = x * (1.0 / scale)[..., None]
+    return (x.round().to(torch.int8) if cache == "int8" else x.to(torch.float8_e4m3fn)), scale
+
+
+def _cache(s, case, totals, gen):
+    """A pool of pages in another order than the sequences', their table, and random contents."""
+    page, kv, D, t = case["page"], case["kv"], case["D"], TYPES[case["cache"]]
+    counts = [(n + page - 1) // page for n in totals]
+    P, most = sum(counts) + 3, max(1, max(counts))
+    order = torch.randperm(P, device=DEV, generator=gen).to(torch.int32)
+    table = torch.full((len(totals), most), -1, device=DEV, dtype=torch.int32)
+    live = torch.zeros(P, page, device=DEV, dtype=torch.bool)
+    at = 0
+    for b, n in enumerate(counts):
+        table[b, :n] = order[at:at + n]
+        if n:
+            live[order[at:at + n].long()] = True
+            live[order[at + n - 1].long(), totals[b] - (n - 1) * page:] = False
+        at += n
+    s["table"] = table
+    for name in ("k", "v"):
+        x = torch.randn(P, kv, page, D, device=DEV, generator=gen)
+        if case["cache"] in LARGEST:
+            codes, scale = _codes(x, case["cache"])
+            s[name + "_pages"], s[name + "_scales"] = codes, torch.where(live[:, None, :], scale, math.nan)
+        else:
+            s[name + "_pages"], s[name + "_scales"] = x.masked_fill_(~live[:, None, :, None], math.nan).to(t), None
+        del x
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(seed)
+    B, T, t = case["B"], case["T"], TYPES[case["dtype"]]
+    s = dict(case=case)
+    mixed = torch.randperm(B, generator=torch.Generator().manual_seed(seed)).tolist()
+    if case["op"] == "verify":
+        V, ld = case["V"], case["ld"]
+        # logits of a large vocabulary: few likely words, a long tail; the small model is off from the large one
+        base = torch.randn(B, T + 1, ld, device=DEV, generator=gen) * 2.5
+        s["target"] = base.to(t)[:, :, :V]
+        s["draft"] = (base[:, :T] + torch.randn(B, T, ld, device=DEV, generator=gen) * 0.4).to(t)[:, :, :V]
+        del base
+        noise = -torch.log(-torch.log(torch.rand(B, T, V, device=DEV, generator=gen) * (1 - 2e-7) + 1e-7))
+        s["drafted"] = (s["draft"].float() / case["tau"] + noise).argmax(dim=-1).to(torch.int32)
+        del noise
+        given = torch.where(torch.rand(B, device=DEV, generator=gen) < case["short"], torch.randint(0, T + 1, (B,), device=DEV, generator=gen), T)
+        s["drafted"][torch.arange(T, device=DEV)[None, :] >= given[:, None]] = -1
+        s["u_accept"], s["u_next"] = torch.rand(B, T, device=DEV, generator=gen), torch.rand(B, device=DEV, generator=gen)
+        s["n_accepted"], s["words"] = torch.empty(B, device=DEV, dtype=torch.int32), torch.empty(B, T + 1, device=DEV, dtype=torch.int32)
+        return s
+    kv, D = case["kv"], case["D"]
+    context = _lengths(B, case["L"], case["even"])
+    if case["op"] == "attn":
+        lengths = [context[i] for i in mixed]
+        _cache(s, case, lengths, gen)
+        s["lengths"] = torch.tensor(lengths, device=DEV, dtype=torch.int32)
+        # queries as a projection leaves them, beside the keys and values of the same tokens
+        all_heads = torch.randn(B, T, case["q"] + 2 * kv, D, device=DEV, generator=gen) * 1.5
+        s["q"] = all_heads.to(t)[:, :, :case["q"]]
+        s["out"] = torch.empty(B, T, case["q"], D, device=DEV, dtype=t)
+        s["lse"] = torch.empty(B, T, case["q"], device=DEV, dtype=torch.float32)
+        return s
+    new = _lengths(B, T, case["even"])
+    context = [context[i] for i in mixed]
+    _cache(s, case, [a + b for a, b in zip(context, new)], gen)
+    places = torch.tensor([(b, context[b] + i) for b in range(B) for i in range(new[b])], dtype=torch.int32)
+    pads = int(round(len(places) * case["pad"]))
+    places = torch.cat([places, torch.full((pads, 2), -1, dtype=torch.int32)])[torch.randperm(len(places) + pads, generator=torch.Generator().manual_seed(seed + 1))]
+    old = torch.tensor([(b, i) for b, n in _old(context, case["back"]) for i in range(n)], dtype=torch.int32).reshape(-1, 2)
+    read = torch.cat([places, old])
+    s["seq"], s["pos"] = (places[:, i].contiguous().to(DEV) for i in (0, 1))
+    s["read_seq"], s["read_pos"] = (read[:, i].contiguous().to(DEV) for i in (0, 1))
+    rows = torch.randn(len(places), 3, kv, D, device=DEV, generator=gen) * torch.exp(torch.randn(len(places), 1, kv, 1, device=DEV, generator=gen))
+    rows[(places[:, 0] < 0).to(DEV)] = math.nan
+    rows = rows.to(t)
+    s["k"], s["v"] = rows[:, 1], rows[:, 2]      # (queries ahead of them)
+    s["k_read"] = torch.empty(len(read), kv, D, device=DEV, dtype=t)
+    s["v_read"] = torch.empty(len(read), kv, D, device=DEV, dtype=t)
+    return s
+
+
+def _old(context, back):
+    """Sequences from the first one on, whole, until `back` places are read: (sequence, places)."""
+    for b, n in enumerate(context):
+        n = min(n, back)
+        back -= n
+        yield b, n
+
+
+# ---- plain forms ----------------------------------------------------------------------------------------------------------
+
+
+def _bytes(pages):
+    """Codes as they can be indexed."""
+    return pages.view(torch.uint8) if pages.dtype == torch.float8_e4m3fn else pages
+
+
+def _cache_plain(s):
+    case, cache, table = s["case"], s["case"]["cache"], s["table"]
+    page, got = case["page"], {}
+    new = (s["seq"] >= 0).nonzero()[:, 0]
+    seq, pos = s["seq"][new].long(), s["pos"][new].long()
+    to, off = table[seq, pos // page].long(), pos % page
+    there = s["read_seq"] >= 0
+    seq, pos = torch.where(there, s["read_seq"], 0).long(), torch.where(there, s["read_pos"], 0).long()
+    of, at = table[seq, pos // page].long(), pos % page
+    for name in ("k", "v"):
+        x, pages, scales = s[name][new].float(), s[name + "_pages"], s[name + "_scales"]
+        if scales is None:
+            pages[to, :, off] = x.to(pages.dtype)
+            x = pages[of, :, at].float()
+        else:
+            codes, scale = _codes(x, cache)
+            _bytes(pages)[to, :, off] = _bytes(codes)
+            scales[to, :, off] = scale
+            x = _bytes(pages)[of, :, at].view(pages.dtype).float() * scales[of, :, at][..., None]
+        got[name] = torch.where(there[:, None, None], x, 0.0).to(s["k_read"].dtype)
+    return got
+
+
+def _attn_plain(s):
+    case, table, n = s["case"], s["table"], s["lengths"].long()
+    B, T, kv, D, q_heads = case["B"], case["T"], case["kv"], case["D"], case["q"]
+    at = table.clamp(min=0).long()
+    long = at.shape[1] * case["page"]
+    here = torch.arange(long, device=DEV)
+    inside = here[None, :] < n[:, None]
+    dense = []
+    for_scales = lambda x: x.transpose(1, 2).reshape(B, kv, long)  # noqa: E731
+    for name in ("k", "v"):
+        pages, scales = s[name + "_pages"], s[name + "_scales"]
+        x = _bytes(pages)[at].view(pages.dtype).float().transpose(1, 2).reshape(B, kv, long, D)
+        if scales is not None:
+            x *= for_scales(scales[at])[..., None]
+        dense.append(x.masked_fill_(~inside[:, None, :, None], 0.0))
+    q = s["q"].float().reshape(B, T, kv, q_heads // kv, D).transpose(1, 2).reshape(B, kv, -1, D)
+    scores = (q @ dense[0].transpose(2, 3)) * (1.0 / math.sqrt(D))
+    last = n[:, None] - T + torch.arange(T, device=DEV)[None, :]        # a token sees itself and what is ahead of it
+    seen = here[None, None, :] <= last[:, :, None]
+    if case["window"]:
+        seen &= here[None, None, :] > last[:, :, None] - case["window"]
+    seen = seen[:, None, :, None, :].expand(B, kv, T, q_heads // kv, long).reshape(scores.shape)
+    scores = torch.where(seen, scores, -math.inf)
+    top = scores.amax(dim=-1, keepdim=True)
+    some = top > -math.inf
+    e = torch.exp(scores - torch.where(some, top, 0.0))
+    total = e.sum(dim=-1, keepdim=True)
+    out = torch.where(some, (e @ dense[1]) / total, 0.0)
+    lse = top + torch.log(total)
+    order = lambda x: x.reshape(B, kv, T, q_heads // kv, -1).transpose(1, 2).reshape(B, T, q_heads, -1)  # noqa: E731
+    return dict(out=order(out).to(s["q"].dtype), lse=order(lse)[..., 0])
+
+
+def _verify_plain(s):
+    # in 64 bits: a word is told from its neighbour by where a random number falls among sums over the vocabulary
+    T, V, x = s["case"]["T"], s["case"]["V"], s["drafted"].long()
+    both = []
+    for_rows = lambda l: torch.exp(l - l.amax(dim=-1, keepdim=True))  # noqa: E731
+    for name in ("target", "draft"):
+        e = for_rows(s[name].double() / s["case"]["tau"])
+        both.append(e / e.sum(dim=-1, keepdim=True))
+    p, q = both
+    given = (x >= 0) & (x < V)
+    at = torch.where(given, x, 0)[:, :, None]
+    ok = given & (s["u_accept"].double() * q.gather(2, at)[..., 0] < p[:, :T].gather(2, at)[..., 0])
+    n = ok.long().cumprod(dim=1).sum(dim=1)
+    row = lambda y, i: y.gather(1, i[:, None, None].expand(-1, 1, V))[:, 0]  # noqa: E731
+    stop = n.clamp(max=T - 1)
+    p = row(p, n)
+    refused = (n < T) & given.gather(1, stop[:, None])[:, 0]
+    left = torch.where(refused[:, None], (p - row(q, stop)).clamp(min=0.0), p)
+    left = torch.where(left.sum(dim=1, keepdim=True) > 0, left, p)
+    sums = left.cumsum(dim=1)
+    word = (sums <= s["u_next"].double()[:, None] * sums[:, -1:]).sum(dim=1).clamp(max=V - 1)
+    here = torch.arange(T + 1, device=DEV)[None, :]
+    words = torch.where(here < n[:, None], torch.cat([x, x[:, :1]], dim=1), torch.where(here == n[:, None], word[:, None], -1))
+    return dict(n_accepted=n.to(torch.int32), words=words.to(torch.int32))
+
+
+# ---- the framework's calls ------------------------------------------------------------------------------------------------
+
+
+def _own(s):
+    import paper_1909_00562_amd as lib
+    case, h = s["case"], s.get("handle")
+    if h is None:   # kept, as a program does that takes more than one step
+        if case["op"] == "verify":
+            h = lib.DeviceVocabVerify(case["B"], case["T"], case["V"], dtype=case["dtype"], temperature=case["tau"], device=s["target"].device)
+        else:
+            h = lib.DeviceKvCache(s["k_pages"], s["v_pages"], s["k_scales"], s["v_scales"], dtype=case["dtype"])
+            if case["op"] == "attn":
+                h = lib.DeviceKvAttn(h, case["B"], case["T"], case["q"], max_len=case["L"], window=case["window"])
+        s["handle"] = h
+    if case["op"] == "verify":
+        h.verify(s["target"], s["draft"], s["drafted"], s["u_accept"], s["u_next"], s["n_accepted"], s["words"])
+        return dict(n_accepted=s["n_accepted"], words=s["words"])
+    if case["op"] == "attn":
+        h.fwd(s["q"], s["table"], s["lengths"], s["out"], s["lse"])
+        return dict(out=s["out"], lse=s["lse"])
+    h.write(s["k"], s["v"], s["seq"], s["pos"], s["table"])
+    h.read(s["read_seq"], s["read_pos"], s["table"], s["k_read"], s["v_read"])
+    return dict(k=s["k_read"], v=s["v_read"])
+
+
+def run(state):
+    if own:
+        return _own(state)
+    return {"cache": _cache_plain, "attn": _attn_plain, "verify": _verify_plain}[state["case"]["op"]](state)
+
+
+# ---- the definition in 64 bits --------------------------------------------------------------------------------------------
+
+
+def exact(case, seed):
+    if case["op"] == "verify":
+        return None      # whole numbers, and the plain form is in 64 bits
+    s = prepare(case, seed)
+    page, D, kv = case["page"], case["D"], case["kv"]
+    if case["op"] == "cache":
+        got, kept = {}, {}
+        n = int((s["seq"] >= 0).numel())
+        for name in ("k", "v"):
+            x = s[name].double()
+            if s[name + "_scales"] is not None:
+                top = LARGEST[case["cache"]]
+                scale = (x.float().abs().amax(dim=-1) / top).clamp(min=LEAST_SCALE)
+                y = (x.float() * (1.0 / scale)[..., None]).double()      # (a float, then a code: so is the format defined)
+                if case["cache"] == "int8":
+                    y = torch.round(y)
+                else:   # 3 bits behind the leading one, 2^-9 at least
+                    step = torch.exp2(torch.floor(torch.log2(y.abs().clamp(min=2.0 ** -6))) - 3)
+                    y = torch.round(y / step) * step
+                x = y * scale.double()[..., None]
+            out = torch.zeros(len(s["read_seq"]), kv, D, device=DEV, dtype=torch.float64)
+            out[:n] = torch.where((s["seq"] >= 0)[:, None, None], x, 0.0)
+            seq, pos = s["read_seq"][n:].long(), s["read_pos"][n:].long()
+            of = s["table"][seq, pos // page].long()
+            for i in range(0, len(seq), 65536):
+                j = slice(i, i + 65536)
+                old = _bytes(s[name + "_pages"])[of[j], :, pos[j] % page].view(s[name + "_pages"].dtype).double()
+                if s[name + "_scales"] is not None:
+                    old *= s[name + "_scales"][of[j], :, pos[j] % page].double()[..., None]
+                out[n:][j] = old
+            got[name] = out
+        return got
+    B, T, G = case["B"], case["T"], case["q"] // case["kv"]
+    out = torch.zeros(B, T, case["q"], D, device=DEV, dtype=torch.float64)
+    lse = torch.full((B, T, case["q"]), -math.inf, device=DEV, dtype=torch.float64)
+    for b, n in enumerate(s["lengths"].tolist()):
+        rows = {}
+        for name in ("k", "v"):
+            of = s["table"][b, :(n + page - 1) // page].long()
+            x = _bytes(s[name + "_pages"])[of].view(s[name + "_pages"].dtype).double()
+            if s[name + "_scales"] is not None:
+                x *= s[name + "_scales"][of].double()[..., None]
+            rows[name] = x.transpose(0, 1).reshape(kv, -1, D)[:, :n]
+        for t in range(T):
+            end = n - T + t + 1
+            begin = max(0, end - case["window"]) if case["window"] else 0
+            if end < 1:
+                continue
+            score = torch.matmul(s["q"][b, t].double().reshape(kv, G, D), rows["k"][:, begin:end].transpose(1, 2).contiguous()) / math.sqrt(D)
+            out[b, t] = torch.matmul(torch.softmax(score, dim=-1), rows["v"][:, begin:end].contiguous()).reshape(-1, D)
+            lse[b, t] = torch.logsumexp(score, dim=-1).reshape(-1)
+    return dict(out=out, lse=lse)
+
+
+def work(case):
+    B, T, e = case["B"], case["T"], SIZE[case["dtype"]]
+    if case["op"] == "verify":
+        rows = B * (2 * T + 1)      # (every row of logits once; three operations for each logit's exponential and sum)
+        return dict(bytes=rows * case["V"] * e + 8 * B * T + 4 * B + 4 * B * (T + 2), flops=3 * rows * case["V"])
+    kv, D = case["kv"], case["D"]
+    c = SIZE[case["cache"]] * D + (4 if case["cache"] in LARGEST else 0)      # a head's row in the cache
+    context = _lengths(B, case["L"], case["even"])
+    if case["op"] == "cache":
+        new = sum(_lengths(B, T, case["even"]))
+        pads = int(round(new * case["pad"]))
+        old = min(case["back"], sum(context))
+        write = new * 2 * kv * (D * e + c) + 8 * (new + pads)
+        read = (new + old) * 2 * kv * c + (new + pads + old) * (2 * kv * D * e + 8)
+        return dict(bytes=write + read, flops=2 * (2 * new + old) * 2 * kv * D)
+    held = seen = 0
+    for n in context:
+        for t in range(T):
+            end = n - T + t + 1
+            seen += max(0, min(end, case["window"]) if case["window"] else end)
+        held += min(n, case["window"] + T - 1) if case["window"] else n
+    return dict(bytes=held * 2 * kv * c + 2 * B * T * case["q"] * D * e + 4 * B * T * case["q"] + 4 * B, flops=4 * seen * case["q"] * D)
