@@ -6,6 +6,7 @@
  *   vocab_xent     softmax cross-entropy of h W^T + b against word ids, and the gradients of h, W and b, without keeping
  *                  the logits: they are made a piece of the vocabulary at a time, in both passes
  *   vocab_distill  the same products with a teacher's top K logits per position as a second, soft target
+ *   vocab_verify   which of the words that a small model drafted the large model's probabilities accept, and the word behind them
  *
  * Used together they make a language model of lstm_stack.h: ids -> vocab_embed_fwd -> lstm_stack_fwd -> vocab_xent_fwd,
  * vocab_xent_bwd -> lstm_stack_bwd -> vocab_embed_bwd; with a tied table (W = table, H = I) vocab_embed_bwd accumulates
@@ -117,6 +118,35 @@ as_status vocab_distill_fwd(const vo_shape* shape, const vo_teacher* teacher, co
 /* Backward of g * loss_sum + s * distill_sum, as vocab_xent_bwd.  (g = 0: distillation alone.) */
 as_status vocab_distill_bwd(const vo_shape* shape, const vo_teacher* teacher, const void* W, const void* b,
                             void* workspace, size_t workspace_bytes, void* dh, void* dW, void* db, void* hip_stream);
+
+/*
+ * Verification of drafted words (speculative sampling): with p[t] = softmax(target[b,t,:] / tau) and q[t] = softmax(draft[b,t,:] / tau),
+ * the words drafted[b,t], t = 0, 1, .., are accepted as long as they lie in [0,V) and u_accept[b,t] q[t][word] < p[t][word].  Of n accepted
+ * words the next one is drawn from p[n] where there is no word at n (n = T, or it lies outside [0,V): a shorter draft), and
+ * from max(p[n] - q[n], 0) where that word was refused (from p[n] should this be 0 throughout): it is the lowest v whose weights up
+ * to and including v add up to more than u_next[b] times all of them (the last v of a weight above 0, should rounding leave none).
+ * If the drafted words were drawn from q, the words are distributed as if all were drawn from p.
+ *   target [B,T+1,V] dtype, rows ld_target elements apart   draft [B,T,V] dtype, rows ld_draft apart (multiples of 16 bytes, >= V; what is
+ *   between rows is not read into results)   drafted [B,T] int32   u_accept [B,T] float, u_next [B] float: uniform in [0,1)
+ *   n_accepted [B] int32   words [B,T+1] int32: the accepted ones, the next one, -1 behind it
+ * A logit of -inf has the probability 0.  A row that holds a NaN or +inf, or nothing but -inf, is no distribution: where one of them is
+ * asked for, the words before are accepted and the next one is -1.  Probabilities and their sums are computed in 64 bits.
+ * grad_dtype and the like play no part.
+ */
+typedef struct {
+  int32_t B;          /* sequences, 1 .. 2^16 */
+  int32_t T;          /* drafted words of each, 1 .. 64 */
+  int32_t V;          /* vocabulary, 1 .. 2^20 */
+  int32_t dtype;      /* as_dtype of the logits */
+  float temperature;  /* tau, 2^-10 .. 2^10 */
+} vo_verify;
+
+/* Bytes of workspace vocab_verify needs; 0 if the shape is invalid. */
+size_t vocab_verify_workspace_bytes(const vo_verify* shape);
+
+as_status vocab_verify(const vo_verify* shape, const void* target, int64_t ld_target, const void* draft, int64_t ld_draft,
+                       const int32_t* drafted, const float* u_accept, const float* u_next, int32_t* n_accepted, int32_t* words,
+                       void* workspace, size_t workspace_bytes, void* hip_stream);
 
 #ifdef __cplusplus
 }

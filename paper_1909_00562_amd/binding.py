@@ -1,4 +1,4 @@
-"""ctypes binding of include/attn_softmax.h, lstm_stack.h and vocab_ops.h: same names, argument marshalling only.
+"""ctypes binding of include/attn_softmax.h, lstm_stack.h, vocab_ops.h and kv_cache.h: same names, argument marshalling only.
 
 PyTorch is used for device memory and streams; every step of the path runs in
 the HIP library.  There is no fallback: if libattn_softmax.so is missing the
@@ -17,6 +17,7 @@ _LIB_PATH = os.path.join(_PKG, "libattn_softmax.so")
 _lib = None
 
 AS_F32, AS_BF16 = 0, 1
+KC_F32, KC_BF16, KC_INT8, KC_E4M3 = 0, 1, 2, 3
 AS_VIEW_ALPHA, AS_VIEW_CTX, AS_VIEW_HC, AS_VIEW_LOGITS, AS_VIEW_LSE, AS_VIEW_ROW_POS = range(6)
 STATUS_NAMES = {0: "AS_OK", 1: "AS_ERR_NULL", 2: "AS_ERR_SHAPE", 3: "AS_ERR_DTYPE",
                 4: "AS_ERR_WORKSPACE", 5: "AS_ERR_ALIGN", 6: "AS_ERR_HIP"}
@@ -31,7 +32,9 @@ EXPORTS = ["attn_softmax_workspace_bytes", "attn_softmax_fwd", "attn_softmax_fwd
            "attn_softmax_step_fwd", "lstm_stack_workspace_bytes", "lstm_stack_fwd", "lstm_stack_bwd"]
 
 VOCAB_EXPORTS = ["vocab_embed_workspace_bytes", "vocab_embed_fwd", "vocab_embed_bwd", "vocab_xent_workspace_bytes",
-                 "vocab_xent_fwd", "vocab_xent_bwd", "vocab_distill_fwd", "vocab_distill_bwd"]
+                 "vocab_xent_fwd", "vocab_xent_bwd", "vocab_distill_fwd", "vocab_distill_bwd", "vocab_verify_workspace_bytes", "vocab_verify"]
+
+KV_EXPORTS = ["kv_cache_write", "kv_cache_read", "kv_cache_attn_workspace_bytes", "kv_cache_attn"]
 
 
 class AttnSoftmaxError(RuntimeError):
@@ -71,6 +74,21 @@ class VoShape(ctypes.Structure):
 
 class VoTeacher(ctypes.Structure):
     _fields_ = [("K", ctypes.c_int32), ("temperature", ctypes.c_float), ("scale", ctypes.c_float)]
+
+
+class VoVerify(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("T", ctypes.c_int32), ("V", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("temperature", ctypes.c_float)]
+
+
+class KcCache(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_int32), ("page", ctypes.c_int32), ("heads", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("cache_type", ctypes.c_int32), ("B", ctypes.c_int32), ("max_pages", ctypes.c_int32)]
+
+
+class KcAttn(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("max_len", ctypes.c_int32), ("window", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
 
 
 def library_path() -> str:
@@ -139,6 +157,20 @@ def load_library():
     lib.vocab_distill_fwd.argtypes = [ps, pt] + [vp] * 12 + [sz, vp]
     lib.vocab_distill_bwd.restype = ctypes.c_int
     lib.vocab_distill_bwd.argtypes = [ps, pt] + [vp] * 3 + [sz] + [vp] * 4
+    pv, i32, i64 = ctypes.POINTER(VoVerify), ctypes.c_int32, ctypes.c_int64
+    lib.vocab_verify_workspace_bytes.restype = sz
+    lib.vocab_verify_workspace_bytes.argtypes = [pv]
+    lib.vocab_verify.restype = ctypes.c_int
+    lib.vocab_verify.argtypes = [pv, vp, i64, vp, i64] + [vp] * 6 + [sz, vp]
+    pc, pa = ctypes.POINTER(KcCache), ctypes.POINTER(KcAttn)
+    lib.kv_cache_write.restype = ctypes.c_int
+    lib.kv_cache_write.argtypes = [pc, i32, vp, i64, vp, i64] + [vp] * 7 + [vp]
+    lib.kv_cache_read.restype = ctypes.c_int
+    lib.kv_cache_read.argtypes = [pc, i32] + [vp] * 9 + [vp]
+    lib.kv_cache_attn_workspace_bytes.restype = sz
+    lib.kv_cache_attn_workspace_bytes.argtypes = [pc, pa]
+    lib.kv_cache_attn.restype = ctypes.c_int
+    lib.kv_cache_attn.argtypes = [pc, pa, vp, i64] + [vp] * 9 + [sz, vp]
     _lib = lib
     return lib
 
@@ -341,6 +373,51 @@ def vocab_distill_fwd(shape, teacher, h, W, b, targets, teacher_ids, teacher_log
 def vocab_distill_bwd(shape, teacher, W, b, workspace, workspace_bytes, dh, dW, db, stream=0, check=True) -> int:
     rc = load_library().vocab_distill_bwd(_ref(shape), _ref(teacher), *_addresses(W, b, workspace),
                                           int(workspace_bytes), *_addresses(dh, dW, db), stream or None)
+    if check:
+        _check(rc)
+    return rc
+
+
+def vocab_verify_workspace_bytes(shape: VoVerify) -> int:
+    return int(load_library().vocab_verify_workspace_bytes(_ref(shape)))
+
+
+def vocab_verify(shape, target, ld_target, draft, ld_draft, drafted, u_accept, u_next, n_accepted, words, workspace,
+                 workspace_bytes, stream=0, check=True) -> int:
+    rc = load_library().vocab_verify(_ref(shape), *_addresses(target), int(ld_target), *_addresses(draft), int(ld_draft),
+                                     *_addresses(drafted, u_accept, u_next, n_accepted, words, workspace),
+                                     int(workspace_bytes), stream or None)
+    if check:
+        _check(rc)
+    return rc
+
+
+def kv_cache_write(cache, N, k, ld_k, v, ld_v, seq, pos, page_table, k_pages, v_pages, k_scales, v_scales, stream=0,
+                   check=True) -> int:
+    rc = load_library().kv_cache_write(_ref(cache), int(N), *_addresses(k), int(ld_k), *_addresses(v), int(ld_v),
+                                       *_addresses(seq, pos, page_table, k_pages, v_pages, k_scales, v_scales), stream or None)
+    if check:
+        _check(rc)
+    return rc
+
+
+def kv_cache_read(cache, N, k_pages, v_pages, k_scales, v_scales, seq, pos, page_table, k, v, stream=0, check=True) -> int:
+    rc = load_library().kv_cache_read(_ref(cache), int(N), *_addresses(k_pages, v_pages, k_scales, v_scales, seq, pos, page_table, k, v),
+                                      stream or None)
+    if check:
+        _check(rc)
+    return rc
+
+
+def kv_cache_attn_workspace_bytes(cache: KcCache, attn: KcAttn) -> int:
+    return int(load_library().kv_cache_attn_workspace_bytes(_ref(cache), _ref(attn)))
+
+
+def kv_cache_attn(cache, attn, q, ld_q, k_pages, v_pages, k_scales, v_scales, page_table, lengths, out, lse, workspace,
+                  workspace_bytes, stream=0, check=True) -> int:
+    rc = load_library().kv_cache_attn(_ref(cache), _ref(attn), *_addresses(q), int(ld_q),
+                                      *_addresses(k_pages, v_pages, k_scales, v_scales, page_table, lengths, out, lse, workspace),
+                                      int(workspace_bytes), stream or None)
     if check:
         _check(rc)
     return rc
@@ -563,6 +640,33 @@ class _DeviceOp:
     def _optional(self, t, shape, dtype, name):
         return None if t is None else self._tensor(t, shape, dtype, name)
 
+    def _rows(self, t, shape, dtype, name, ahead=1):
+        """(address, elements from row to row) of a tensor whose first `ahead` dimensions are rows the same distance apart, each
+        dense: a part of a wider projection, or logits with padding."""
+        if t is None:
+            raise AttnSoftmaxError(1, f"{name} is None")
+        if t.shape != shape:
+            raise AttnSoftmaxError(2, f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+        if t.dtype is not dtype:
+            raise AttnSoftmaxError(3, f"{name} is {t.dtype}, expected {dtype}")
+        if t.get_device() != self.index:
+            raise AttnSoftmaxError(2, f"{name} is on {t.device}, expected {self.dev}")
+        strides = t.stride()
+        width = 1
+        for n, stride in zip(shape[:ahead - 1:-1], strides[:ahead - 1:-1]):
+            if n != 1 and stride != width:
+                raise AttnSoftmaxError(5, f"the rows of {name} are not dense")
+            width *= n
+        whole = 16 // t.element_size()
+        alone = -(-width // whole) * whole      # (a single row: dimensions of one have any stride)
+        if ahead == 1:
+            return t.data_ptr(), strides[0] if shape[0] > 1 else alone
+        a, b = shape[:2]
+        row = strides[1] if b > 1 else strides[0] if a > 1 else alone
+        if a > 1 and b > 1 and strides[0] != b * row:
+            raise AttnSoftmaxError(5, f"the rows of {name} are not the same distance apart")
+        return t.data_ptr(), row
+
     def _call(self, function, *args):
         """function(*args, stream), for addresses that _tensor has checked.  The workspace is the handle's own, so the allocator is
         told here of a stream other than the one it was allocated on: a handle may be dropped while calls are on their way."""
@@ -690,3 +794,146 @@ class DeviceVocabLoss(_DeviceOp):
         if self.teacher is None:
             raise AttnSoftmaxError(1, "no teacher (K = 0): xent_bwd")
         self._bwd(self.lib.vocab_distill_bwd, dh, dW, db)
+
+
+class DeviceVocabVerify(_DeviceOp):
+    """Verification of T drafted words of each of B sequences against the target's logits (vocab_ops.h): owns the workspace and
+    forwards to the C ABI.  Shorter drafts end with ids outside the vocabulary (-1)."""
+
+    def __init__(self, B, T, V, dtype="bf16", temperature=1.0, device="cuda:0"):
+        import torch
+        device = torch.device(device)
+        self._on(torch.device("cuda", torch.cuda.current_device()) if device.type == "cuda" and device.index is None else device)
+        if dtype not in ("f32", "bf16"):
+            raise AttnSoftmaxError(3, f"logits of type {dtype!r}")
+        self.tdt = torch.bfloat16 if dtype == "bf16" else torch.float32
+        self.shape = VoVerify(B, T, V, AS_BF16 if dtype == "bf16" else AS_F32, float(temperature))
+        self.ref = ctypes.byref(self.shape)
+        self.b, self.bt, self.bt1, self.target_shape, self.draft_shape = (B,), (B, T), (B, T + 1), (B, T + 1, V), (B, T, V)
+        self.ws_bytes = vocab_verify_workspace_bytes(self.shape)
+        if self.ws_bytes == 0:
+            raise AttnSoftmaxError(2, "invalid shape for the verification")
+        self._own_workspace()
+
+    def verify(self, target, draft, drafted, u_accept, u_next, n_accepted=None, words=None):
+        """(n_accepted [B], words [B,T+1]) int32; target [B,T+1,V] and draft [B,T,V] logits, drafted [B,T] int32, u_accept [B,T]
+        and u_next [B] float32 in [0,1)."""
+        torch = self.torch
+        f32, i32 = torch.float32, torch.int32
+        if n_accepted is None:
+            n_accepted = torch.empty(self.b, dtype=i32, device=self.dev)
+        if words is None:
+            words = torch.empty(self.bt1, dtype=i32, device=self.dev)
+        check = self._tensor
+        self._call(self.lib.vocab_verify, self.ref, *self._rows(target, self.target_shape, self.tdt, "target", 2),
+                   *self._rows(draft, self.draft_shape, self.tdt, "draft", 2), check(drafted, self.bt, i32, "drafted"),
+                   check(u_accept, self.bt, f32, "u_accept"), check(u_next, self.b, f32, "u_next"),
+                   check(n_accepted, self.b, i32, "n_accepted"), check(words, self.bt1, i32, "words"),
+                   self.workspace.data_ptr(), self.ws_bytes)
+        return n_accepted, words
+
+
+class DeviceKvCache(_DeviceOp):
+    """A paged cache of keys and values (kv_cache.h): k_pages, v_pages [pages, heads, page, D] (device tensors, not copied) of float32,
+    bfloat16, int8 or float8_e4m3fn, in 8 bits with scales [pages, heads, page] float32.  dtype: "f32" or "bf16", the type of what is
+    written and read (in 8 bits; else the pages')."""
+
+    def __init__(self, k_pages, v_pages, k_scales=None, v_scales=None, dtype=None):
+        self._on(k_pages.device)
+        torch = self.torch
+        kinds = {torch.float32: KC_F32, torch.bfloat16: KC_BF16, torch.int8: KC_INT8, torch.float8_e4m3fn: KC_E4M3}
+        if k_pages.dtype not in kinds:
+            raise AttnSoftmaxError(3, f"storage type {k_pages.dtype}")
+        kind = kinds[k_pages.dtype]
+        coded = kind in (KC_INT8, KC_E4M3)
+        own = {KC_F32: "f32", KC_BF16: "bf16"}.get(kind)
+        dtype = own if dtype is None else dtype
+        if dtype not in ("f32", "bf16") or (own is not None and dtype != own):
+            raise AttnSoftmaxError(3, f"a cache of {k_pages.dtype} for values of type {dtype!r}")
+        if k_pages.dim() != 4:
+            raise AttnSoftmaxError(2, f"k_pages has shape {tuple(k_pages.shape)}, expected [pages, heads, page, D]")
+        P, heads, page, D = k_pages.shape
+        self.pages = (self._tensor(k_pages, k_pages.shape, k_pages.dtype, "k_pages"),
+                      self._tensor(v_pages, k_pages.shape, k_pages.dtype, "v_pages"))
+        if coded:
+            self.pages += (self._tensor(k_scales, (P, heads, page), torch.float32, "k_scales"),
+                           self._tensor(v_scales, (P, heads, page), torch.float32, "v_scales"))
+        elif k_scales is not None or v_scales is not None:
+            raise AttnSoftmaxError(1, "scales belong to caches in 8 bits")
+        else:
+            self.pages += (None, None)
+        self.k_pages, self.v_pages, self.k_scales, self.v_scales = k_pages, v_pages, k_scales, v_scales
+        self.tdt = torch.bfloat16 if dtype == "bf16" else torch.float32
+        self.heads, self.D, self.page = heads, D, page
+        self.shape = KcCache(P, page, heads, D, AS_BF16 if dtype == "bf16" else AS_F32, kind, 1, 1)
+
+    def _table(self, page_table):
+        """The cache's description for this table, and the table's address."""
+        if page_table is None or page_table.dim() != 2:
+            raise AttnSoftmaxError(2 if page_table is not None else 1, "page_table is not [sequences, pages]")
+        B, max_pages = page_table.shape
+        c = self.shape
+        if c.B != B or c.max_pages != max_pages:      # (never changed in place: another thread may be in a call with it)
+            self.shape = c = KcCache(c.pages, c.page, c.heads, c.D, c.dtype, c.cache_type, B, max_pages)
+        return ctypes.byref(c), self._tensor(page_table, page_table.shape, self.torch.int32, "page_table")
+
+    def write(self, k, v, seq, pos, page_table):
+        """Rows n of k and v [N, heads, D] to token pos[n] of sequence seq[n] (int32); rows of no sequence (-1) are left out."""
+        i32, N = self.torch.int32, len(seq)
+        rows = (N, self.heads, self.D)
+        k_at, ld_k = self._rows(k, rows, self.tdt, "k")
+        v_at, ld_v = self._rows(v, rows, self.tdt, "v")
+        seq, pos = self._tensor(seq, (N,), i32, "seq"), self._tensor(pos, (N,), i32, "pos")
+        ref, table = self._table(page_table)
+        if N:
+            self._call(self.lib.kv_cache_write, ref, N, k_at, ld_k, v_at, ld_v, seq, pos, table, *self.pages)
+
+    def read(self, seq, pos, page_table, k=None, v=None):
+        """(k, v) [N, heads, D]: what the cache holds at token pos[n] of sequence seq[n] (int32), zeros where it is no place."""
+        torch, N = self.torch, len(seq)
+        rows = (N, self.heads, self.D)
+        if k is None:
+            k = torch.empty(rows, dtype=self.tdt, device=self.dev)
+        if v is None:
+            v = torch.empty(rows, dtype=self.tdt, device=self.dev)
+        ref, table = self._table(page_table)
+        at = (self._tensor(seq, (N,), torch.int32, "seq"), self._tensor(pos, (N,), torch.int32, "pos"), table,
+              self._tensor(k, rows, self.tdt, "k"), self._tensor(v, rows, self.tdt, "v"))
+        if N:
+            self._call(self.lib.kv_cache_read, ref, N, *self.pages, *at)
+        return k, v
+
+
+class DeviceKvAttn(_DeviceOp):
+    """Attention of the newest T tokens of B sequences over a DeviceKvCache: owns the workspace and forwards to the C ABI.
+    max_len: no sequence is longer; window > 0: a token sees itself and the window - 1 ahead of it; scale: 1 / sqrt(D) by itself."""
+
+    def __init__(self, cache, B, T, q_heads, max_len, window=0, scale=None):
+        self._on(cache.dev)
+        self.cache, self.tdt = cache, cache.tdt
+        c = cache.shape
+        self.shape = KcCache(c.pages, c.page, c.heads, c.D, c.dtype, c.cache_type, B, max(1, -(-max_len // c.page)))
+        self.attn = KcAttn(T, q_heads, max_len, window, float(c.D ** -0.5 if scale is None else scale))
+        self.attn_ref = ctypes.byref(self.attn)
+        self.b, self.heads_shape, self.q_shape = (B,), (B, T, q_heads), (B, T, q_heads, c.D)
+        self.ws_bytes = kv_cache_attn_workspace_bytes(self.shape, self.attn)
+        if self.ws_bytes == 0:
+            raise AttnSoftmaxError(2, "invalid shape for the attention: " + attn_softmax_last_error())
+        self._own_workspace()
+
+    def fwd(self, q, page_table, lengths, out=None, lse=None):
+        """out [B,T,q_heads,D] (and lse [B,T,q_heads] float32, if given); lengths [B] int32 with the new tokens, whose keys and values the
+        cache holds; page_table [B, pages] int32 of pages for max_len tokens at least."""
+        torch = self.torch
+        if out is None:
+            out = torch.empty(self.q_shape, dtype=self.tdt, device=self.dev)
+        if page_table is None or page_table.dim() != 2 or page_table.shape[1] * self.shape.page < self.attn.max_len:
+            raise AttnSoftmaxError(2, "page_table is not [sequences, pages for max_len tokens]")
+        c, max_pages = self.shape, page_table.shape[1]
+        if c.max_pages != max_pages:      # (never changed in place: another thread may be in a call with it)
+            self.shape = c = KcCache(c.pages, c.page, c.heads, c.D, c.dtype, c.cache_type, c.B, max_pages)
+        table = self._tensor(page_table, (c.B, max_pages), torch.int32, "page_table")
+        self._call(self.lib.kv_cache_attn, ctypes.byref(c), self.attn_ref, *self._rows(q, self.q_shape, self.tdt, "q", 2), *self.cache.pages, table,
+                   self._tensor(lengths, self.b, torch.int32, "lengths"), self._tensor(out, self.q_shape, self.tdt, "out"),
+                   self._optional(lse, self.heads_shape, torch.float32, "lse"), self.workspace.data_ptr(), self.ws_bytes)
+        return out

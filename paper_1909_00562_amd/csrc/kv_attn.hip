@@ -1,0 +1,785 @@
+// Attention of each sequence's newest tokens over its paged cache (entry point and kernels).
+//
+// The queries that share a head of the cache are the rows of a product of 16 columns: S^T = K Q^T and O^T = V^T P^T, one pass over
+// keys and values with the running maximum and sum of the softmax.  Bound by memory: each cached value is read once; at four
+// queries to a head the products are 16 operations for each of a key's and a value's bf16 elements.
+//
+// Nothing goes through LDS but what waves of a block join at the end.  A wave takes tiles of 16 tokens.  K's fragments are read as they
+// lie.  S^T leaves lane (c, g) = (lane & 15, lane >> 4) with the scores of row c and of tokens 4g .. 4g + 3, which is how the next
+// product takes P^T, with its reduction index numbered to suit: the same lane's V fragment holds the same tokens.  Of V a lane reads
+// consecutive columns of these tokens, and fragments are made of them in its own registers: columns of O^T are numbered to suit.
+// Row c's factor of O^T is then the lane's own too.
+//
+// Work is cut by what the sequences hold: all (sequence, head, chunk of tokens) are numbered in one row, and a block takes a run of
+// equal length.  What is left of a (sequence, head) that several blocks share goes to the workspace, joined by a second launch.
+#include "kv_cache.h"
+
+#include <cmath>
+#include <type_traits>
+
+#include "common.h"
+#include "lds_limit.h"
+#include "status.h"
+
+namespace asx {
+namespace {
+
+typedef uint32_t au32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t au32x2_t __attribute__((ext_vector_type(2)));
+
+constexpr int kAttnThreads = 256, kAttnWaves = 4;
+constexpr int kChunk = 128;            // tokens of a chunk
+constexpr int kMinChunks = 4;          // of a block's run
+constexpr int kMostBlocks = 1024;
+constexpr uint32_t kAttnOob = 0x80000000u;
+
+struct KvAttnDev {
+  const void *q, *k_pages, *v_pages;
+  const float *k_scales, *v_scales;
+  const int32_t *table, *lengths;
+  void* out;
+  float* lse;
+  float *part, *part_ml;   // [slot][row][D], [slot][row][2]: sums relative to the maximum; maximum (of log2) and sum of weights
+  int64_t ld_q;
+  int32_t B, T, heads, G, D, R;        // R = T G rows of a head
+  int32_t row_tiles, tile_waves, row_groups, group_rows;   // tiles of 16 rows; of a block (1, 2 or 4); groups of a block's tiles; rows of a group
+  int32_t page, page_tiles, pages, max_pages, max_len, window;
+  uint32_t magic;                      // of page_tiles
+  int32_t split;                       // 0: a block per (sequence, head, row group), no second launch
+  float scale_log2;
+};
+
+// ---- which tokens -----------------------------------------------------------------
+struct SeqSpan {
+  int32_t len, base, chunks;   // tokens; the first one that is looked at, rounded down to a tile; chunks from there
+};
+__device__ __forceinline__ SeqSpan seq_span(const KvAttnDev& a, int b) {
+  SeqSpan s;
+  int32_t n = a.lengths[b];
+  n = n < 0 ? 0 : n > a.max_len ? a.max_len : n;
+  const int32_t first = a.window > 0 ? n - a.T + 1 - a.window : 0;
+  s.len = n;
+  s.base = first > 0 ? first & ~(kKvTile - 1) : 0;
+  s.chunks = (n - s.base + kChunk - 1) / kChunk;
+  return s;
+}
+
+struct Cut {
+  int32_t per, blocks_used;    // chunks of a run
+  int32_t b;                   // the sequence that holds chunk `at`
+  int32_t ahead;               // chunks of the sequences ahead of it
+};
+// Adds up the sequences' chunks (times the heads and row groups), 256 sequences at a time; the same numbers in every block.
+__device__ __forceinline__ int32_t cut_total(const KvAttnDev& a, int32_t* s_sum) {
+  int32_t n = 0;
+  for (int b = threadIdx.x; b < a.B; b += kAttnThreads) n += seq_span(a, b).chunks;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
+  if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = n;
+  __syncthreads();
+  return (s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3]) * a.heads * a.row_groups;
+}
+__device__ __forceinline__ int32_t cut_per(int32_t total, int blocks) {
+  const int32_t per = (total + blocks - 1) / blocks;
+  return per < kMinChunks ? kMinChunks : per;
+}
+// the sequence of chunk `at` of all, and the chunks ahead of it
+__device__ __forceinline__ void cut_find(const KvAttnDev& a, int32_t at, int32_t* s_sum, int32_t* s_found, int32_t& b_out, int32_t& ahead_out) {
+  const int32_t hr = a.heads * a.row_groups;
+  int32_t carry = 0;
+  for (int b0 = 0; b0 < a.B; b0 += kAttnThreads) {
+    const int b = b0 + threadIdx.x;
+    const int32_t own = b < a.B ? seq_span(a, b).chunks * hr : 0;
+    int32_t run = own;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int32_t x = __shfl_up(run, o, 64);
+      if ((threadIdx.x & 63) >= o) run += x;
+    }
+    __syncthreads();
+    if ((threadIdx.x & 63) == 63) s_sum[threadIdx.x >> 6] = run;
+    __syncthreads();
+    for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) run += s_sum[w];
+    const int32_t ahead = carry + run - own;
+    if (at >= ahead && at < ahead + own) {
+      s_found[0] = b;
+      s_found[1] = ahead;
+    }
+    carry += s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3];
+    if (at < carry) break;
+  }
+  __syncthreads();
+  b_out = s_found[0];
+  ahead_out = s_found[1];
+}
+
+// ---- fragments --------------------------------------------------------------------
+__device__ __forceinline__ bf16x8_t as_frag(au32x4_t x) { return __builtin_bit_cast(bf16x8_t, x); }
+__device__ __forceinline__ uint32_t top_halves(float lo, float hi) {   // two floats that bf16 holds
+  return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302u);
+}
+
+template <int TYPE> __device__ __forceinline__ void codes_to_floats(uint32_t w, float (&x)[4]) {
+  if constexpr (TYPE == KC_INT8) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = (float)(int8_t)(w >> (8 * i));
+  } else {
+    const auto p = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), q = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+    x[0] = p[0];
+    x[1] = p[1];
+    x[2] = q[0];
+    x[3] = q[1];
+  }
+}
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t attn_rsrc(const void* base) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, 0x7fffffff, 0x00020000);
+}
+
+// What a cache type's tiles look like.  TYPE: kc_type, F32Q: queries and results are float, DP: the head's width up to which it serves.
+template <int TYPE, bool F32Q, int DP> struct Form {
+  static constexpr bool kF32 = TYPE == KC_F32, kCoded = TYPE == KC_INT8 || TYPE == KC_E4M3;
+  static constexpr int kBytes = kF32 ? 4 : kCoded ? 1 : 2;
+  static constexpr int kTiles = kF32 ? 1 : 2;                       // of a step
+  static constexpr int kQTerms = kF32 || !F32Q ? 1 : 3, kPTerms = kF32 ? 1 : F32Q ? 3 : 2;
+  static constexpr int kKLoads = DP * kBytes / 64;                  // 16-byte loads of a lane for a tile of K
+  static constexpr int kKElems = 16 / kBytes;                       // elements of each: D index (load * 4 + g) * kKElems + i
+  // V: columns (half * 16 + c) * kVW + i of a token
+  static constexpr int kVAll = DP / 16;                             // columns of a lane
+  static constexpr int kVW = kCoded ? kVAll : kF32 ? 4 : (kVAll < 8 ? kVAll : 8);
+  static constexpr int kVHalves = kVAll / kVW;
+  static constexpr int kVDwords = kVW * kBytes / 4;
+};
+
+template <int N> __device__ __forceinline__ void buffer_load(__amdgpu_buffer_rsrc_t rs, uint32_t off, uint32_t (&x)[N]) {
+  static_assert(N == 1 || N == 2 || N == 4);
+  if constexpr (N == 4) {
+    const au32x4_t q = __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = q[i];
+  } else if constexpr (N == 2) {
+    const au32x2_t q = __builtin_amdgcn_raw_buffer_load_b64(rs, off, 0, 0);
+    x[0] = q[0];
+    x[1] = q[1];
+  } else {
+    x[0] = __builtin_amdgcn_raw_buffer_load_b32(rs, off, 0, 0);
+  }
+}
+
+// ---- the kernel -------------------------------------------------------------------
+template <class F> struct TileAt {
+  int32_t pos;      // first token
+  int32_t valid;    // tokens that there are: up to 16, 0 where there is no page
+};
+
+template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__(kAttnThreads) void kv_attn_kernel(KvAttnDev a) {
+  using F = Form<TYPE, F32Q, DP>;
+  constexpr int NT = F::kTiles, NO = DP / 16, STEP = NT * kKvTile, LD = DP + 4;
+  extern __shared__ float lds[];          // [4 waves][16 rows][LD], and their maxima and sums
+  float* lds_ml = lds + kAttnWaves * 16 * LD;
+  __shared__ int32_t s_sum[4], s_found[2];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 15, g = lane >> 4;
+  const int row_wave = wave % a.tile_waves, tok_wave = wave / a.tile_waves, tok_waves = kAttnWaves / a.tile_waves;
+
+  // this block's run of chunks
+  int32_t b, hr, chunk, left;             // sequence, (head, row group), first chunk there, chunks left
+  if (a.split) {
+    const int32_t total = cut_total(a, s_sum), per = cut_per(total, gridDim.x), at = (int32_t)blockIdx.x * per;
+    if (at >= total) return;
+    left = total - at < per ? total - at : per;
+    int32_t ahead;
+    cut_find(a, at, s_sum, s_found, b, ahead);
+    const int32_t n = seq_span(a, b).chunks;
+    hr = (at - ahead) / n;
+    chunk = at - ahead - hr * n;
+  } else {
+    b = blockIdx.x / (a.heads * a.row_groups);
+    hr = blockIdx.x - b * (a.heads * a.row_groups);
+    chunk = 0;
+    left = 0;                             // (all there are)
+  }
+  b = __builtin_amdgcn_readfirstlane(b);
+  hr = __builtin_amdgcn_readfirstlane(hr);
+  chunk = __builtin_amdgcn_readfirstlane(chunk);
+  left = __builtin_amdgcn_readfirstlane(left);
+
+  do {
+    const SeqSpan span = seq_span(a, b);
+    const int32_t len = span.len;
+    const int head = hr / a.row_groups, group = hr - head * a.row_groups;
+    const int32_t here = a.split ? (left < span.chunks - chunk ? left : span.chunks - chunk) : span.chunks;
+    const int32_t tok0 = span.base + chunk * kChunk;
+    int32_t tok1 = tok0 + here * kChunk;
+    if (tok1 > len) tok1 = len;
+    const bool whole = here == span.chunks;
+
+    // the row of this lane's column of S^T and O^T
+    const int row0 = (group * a.tile_waves + row_wave) * 16, row = row0 + c;
+    const bool row_there = row < a.R;
+    const int t = row_there ? row / a.G : 0, gq = row - t * a.G;
+    const int32_t hi = row_there ? len - a.T + t : -1, lo = a.window > 0 ? hi - a.window + 1 : 0;
+    // tokens that all rows of all t see
+    const int32_t all_hi = len - a.T, all_lo = a.window > 0 ? len - a.window : 0;
+
+    // queries
+    constexpr int QF = F::kF32 ? DP / 16 : DP / 32;   // fragments: of 4 floats, or of 8 bf16
+    float qf[F::kF32 ? QF : 1][4];
+    bf16x8_t qb[F::kQTerms][F::kF32 ? 1 : QF];
+    const int64_t q_at = ((int64_t)b * a.T + t) * a.ld_q + (int64_t)(head * a.G + gq) * a.D;
+    if constexpr (F::kF32) {
+#pragma unroll
+      for (int j = 0; j < QF; ++j) {
+        const int d = (j * 4 + g) * 4;
+        f32x4_t v = {};
+        if (row_there && d < a.D) v = *reinterpret_cast<const f32x4_t*>(reinterpret_cast<const float*>(a.q) + q_at + d);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) qf[j][i] = v[i];
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < QF; ++j) {
+        // codes: 16 of a load are two fragments
+        const int d = F::kCoded ? (j / 2 * 4 + g) * 16 + j % 2 * 8 : (j * 4 + g) * 8;
+        const bool there = row_there && d < a.D;
+        if constexpr (!F32Q) {
+          au32x4_t v = {};
+          if (there) v = *reinterpret_cast<const au32x4_t*>(reinterpret_cast<const uint16_t*>(a.q) + q_at + d);
+          qb[0][j] = as_frag(v);
+        } else {
+          float v[8] = {};
+          if (there) {
+            const float* p = reinterpret_cast<const float*>(a.q) + q_at + d;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = p[i];
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            float rest = v[i];
+#pragma unroll
+            for (int s = 0; s < F::kQTerms; ++s) {
+              const bf16_t x = (bf16_t)rest;
+              qb[s][j][i] = x;
+              rest -= (float)x;
+            }
+          }
+        }
+      }
+    }
+
+    f32x4_t o[NO] = {};
+    float m = -INFINITY, l = 0.f;
+
+    uint32_t kr[NT][F::kKLoads][4], vr[NT][4][F::kVHalves][F::kVDwords];
+    float ks[NT][4], vs[NT][4];
+    TileAt<F> at_k[NT], at_v[NT];
+    const int64_t head_bytes = (int64_t)a.page * a.D * F::kBytes;
+    auto page_of = [&](int32_t pos) {     // the table's entry for the tile at pos (any tile of the sequence's)
+      if (pos >= len) pos = len - 1;
+      const uint32_t tile = (uint32_t)pos >> 4, col = a.page_tiles == 1 ? tile : __umulhi(tile, a.magic);
+      return __builtin_amdgcn_readfirstlane(a.table[(int64_t)b * a.max_pages + col]);
+    };
+    auto place = [&](int32_t pos, int32_t id, int64_t& row_of_pool) {
+      TileAt<F> at;
+      at.pos = pos;
+      const int32_t n = tok1 - pos;
+      at.valid = n < 0 ? 0 : n < kKvTile ? n : kKvTile;
+      const uint32_t tile = (uint32_t)pos >> 4, col = a.page_tiles == 1 ? tile : __umulhi(tile, a.magic);
+      if (id < 0 || id >= a.pages) {
+        at.valid = 0;
+        id = 0;
+      }
+      row_of_pool = ((int64_t)id * a.heads + head) * a.page + (int32_t)(tile - col * a.page_tiles) * kKvTile;
+      return at;
+    };
+    auto load_k = [&](int32_t pos, const int32_t (&id)[NT]) {
+#pragma unroll
+      for (int u = 0; u < NT; ++u) {
+        int64_t r;
+        at_k[u] = place(pos + u * kKvTile, id[u], r);
+        const auto rs = attn_rsrc(reinterpret_cast<const uint8_t*>(a.k_pages) + r * a.D * F::kBytes);
+        const uint32_t off = c < at_k[u].valid ? (uint32_t)(c * a.D * F::kBytes) : kAttnOob;
+#pragma unroll
+        for (int j = 0; j < F::kKLoads; ++j) {
+          const int d = (j * 4 + g) * F::kKElems;
+          buffer_load(rs, d < a.D ? off + d * F::kBytes : kAttnOob, kr[u][j]);
+        }
+        if constexpr (F::kCoded) {
+          uint32_t x[4];
+          buffer_load(attn_rsrc(a.k_scales + r), at_k[u].valid > 4 * g ? g * 16u : kAttnOob, x);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) ks[u][i] = __builtin_bit_cast(float, x[i]);
+        }
+      }
+    };
+    auto load_v = [&](int32_t pos, const int32_t (&id)[NT]) {
+#pragma unroll
+      for (int u = 0; u < NT; ++u) {
+        int64_t r;
+        at_v[u] = place(pos + u * kKvTile, id[u], r);
+        const auto rs = attn_rsrc(reinterpret_cast<const uint8_t*>(a.v_pages) + r * a.D * F::kBytes);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int tok = g * 4 + i;
+          const uint32_t off = tok < at_v[u].valid ? (uint32_t)(tok * a.D * F::kBytes) : kAttnOob;
+#pragma unroll
+          for (int h = 0; h < F::kVHalves; ++h) {
+            const int d = (h * 16 + c) * F::kVW;
+            buffer_load(rs, d < a.D ? off + d * F::kBytes : kAttnOob, vr[u][i][h]);
+          }
+        }
+        if constexpr (F::kCoded) {
+          uint32_t x[4];
+          buffer_load(attn_rsrc(a.v_scales + r), at_v[u].valid > 4 * g ? g * 16u : kAttnOob, x);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) vs[u][i] = __builtin_bit_cast(float, x[i]);
+        }
+      }
+    };
+
+    // O^T += V^T P^T of the step, onto acc
+    auto times_v = [&](const float (&p)[NT][4], f32x4_t (&acc)[NO]) {
+      if constexpr (F::kF32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < NO; ++j)
+            acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, vr[0][i][j / F::kVW][j % F::kVW]), p[0][i], acc[j], 0, 0, 0);
+      } else {
+        bf16x8_t pb[F::kPTerms];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float rest = p[u][i];
+#pragma unroll
+            for (int s = 0; s < F::kPTerms; ++s) {
+              const bf16_t x = (bf16_t)rest;
+              pb[s][u * 4 + i] = x;
+              rest -= (float)x;
+            }
+          }
+        auto add = [&](int j, au32x4_t v) {
+          const bf16x8_t vb = as_frag(v);
+#pragma unroll
+          for (int s = 0; s < F::kPTerms; ++s) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, pb[s], acc[j], 0, 0, 0);
+        };
+        if constexpr (F::kCoded) {
+#pragma unroll
+          for (int w = 0; w < F::kVDwords; ++w) {
+            float x[2][4][4];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) codes_to_floats<TYPE>(vr[u][i][0][w], x[u][i]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              add(w * 4 + e, au32x4_t{top_halves(x[0][0][e], x[0][1][e]), top_halves(x[0][2][e], x[0][3][e]),
+                                      top_halves(x[1][0][e], x[1][1][e]), top_halves(x[1][2][e], x[1][3][e])});
+          }
+        } else {
+#pragma unroll
+          for (int h = 0; h < F::kVHalves; ++h)
+#pragma unroll
+            for (int e = 0; e < F::kVW; ++e) {
+              const uint32_t sel = e % 2 ? 0x07060302u : 0x05040100u;
+              auto two = [&](int u, int i) { return __builtin_amdgcn_perm(vr[u][i + 1][h][e / 2], vr[u][i][h][e / 2], sel); };
+              add(h * F::kVW + e, au32x4_t{two(0, 0), two(0, 2), two(1, 0), two(1, 2)});
+            }
+        }
+      }
+    };
+
+    const int32_t stride = tok_waves * STEP;
+    int32_t pos = tok0 + tok_wave * STEP;
+    int32_t id[NT], id_next[NT];
+    if (pos < tok1 && row0 < a.R) {
+#pragma unroll
+      for (int u = 0; u < NT; ++u) id[u] = page_of(pos + u * kKvTile);
+      load_k(pos, id);
+      load_v(pos, id);
+#pragma unroll
+      for (int u = 0; u < NT; ++u) id_next[u] = page_of(pos + stride + u * kKvTile);
+      for (; pos < tok1; pos += stride) {
+        // S^T
+        f32x4_t s[NT] = {};
+#pragma unroll
+        for (int u = 0; u < NT; ++u) {
+          if constexpr (F::kF32) {
+#pragma unroll
+            for (int j = 0; j < QF; ++j)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) s[u] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, kr[u][j][i]), qf[j][i], s[u], 0, 0, 0);
+          } else {
+            auto add = [&](int j, au32x4_t k) {
+              const bf16x8_t kb = as_frag(k);
+#pragma unroll
+              for (int q = F::kQTerms - 1; q >= 0; --q) s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb, qb[q][j], s[u], 0, 0, 0);
+            };
+#pragma unroll
+            for (int j = 0; j < F::kKLoads; ++j) {
+              if constexpr (F::kCoded) {
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+                  float x[4], y[4];
+                  codes_to_floats<TYPE>(kr[u][j][2 * w], x);
+                  codes_to_floats<TYPE>(kr[u][j][2 * w + 1], y);
+                  add(2 * j + w, au32x4_t{top_halves(x[0], x[1]), top_halves(x[2], x[3]), top_halves(y[0], y[1]), top_halves(y[2], y[3])});
+                }
+              } else {
+                add(j, au32x4_t{kr[u][j][0], kr[u][j][1], kr[u][j][2], kr[u][j][3]});
+              }
+            }
+          }
+        }
+        float p[NT][4];
+#pragma unroll
+        for (int u = 0; u < NT; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            p[u][i] = s[u][i] * a.scale_log2;
+            if constexpr (F::kCoded) p[u][i] *= ks[u][i];
+          }
+        // a step that not all rows see all of
+        bool part = pos < all_lo || pos + STEP - 1 > all_hi;
+#pragma unroll
+        for (int u = 0; u < NT; ++u) part |= at_k[u].valid < kKvTile;
+        if (part) {
+#pragma unroll
+          for (int u = 0; u < NT; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int32_t x = at_k[u].pos + 4 * g + i;
+              if (x < lo || x > hi || 4 * g + i >= at_k[u].valid) p[u][i] = -INFINITY;
+            }
+        }
+        // the next step's keys, into the registers that have been read
+        int32_t id_cur[NT];
+#pragma unroll
+        for (int u = 0; u < NT; ++u) id_cur[u] = id_next[u];
+        load_k(pos + stride, id_cur);
+#pragma unroll
+        for (int u = 0; u < NT; ++u) id_next[u] = page_of(pos + 2 * stride + u * kKvTile);
+
+        float top = p[0][0];
+#pragma unroll
+        for (int u = 0; u < NT; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) top = fmaxf(top, p[u][i]);
+        top = fmaxf(top, __shfl_xor(top, 16, 64));
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const float m_new = fmaxf(m, top), m_use = m_new == -INFINITY ? 0.f : m_new;
+        if (__any(m_new > m)) {
+          const float f = __builtin_amdgcn_exp2f(m - m_use);
+          l *= f;
+#pragma unroll
+          for (int j = 0; j < NO; ++j) o[j] *= f;
+        }
+        m = m_new;
+#pragma unroll
+        for (int u = 0; u < NT; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const bool seen = p[u][i] != -INFINITY;
+            p[u][i] = __builtin_amdgcn_exp2f(p[u][i] - m_use);
+            l += p[u][i];
+            if constexpr (F::kCoded) p[u][i] = seen ? p[u][i] * vs[u][i] : 0.f;
+          }
+        // Values that only some rows see must not reach the others, whatever they are: 0 times an infinity or a NaN is a NaN.
+        bool odd = false;
+        if (part) {
+          uint32_t x = 0;
+#pragma unroll
+          for (int u = 0; u < NT; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int h = 0; h < F::kVHalves; ++h)
+#pragma unroll
+                for (int w = 0; w < F::kVDwords; ++w) {
+                  const uint32_t v = vr[u][i][h][w];
+                  if constexpr (F::kF32) x |= (v & 0x7f800000u) == 0x7f800000u;
+                  else if constexpr (TYPE == KC_BF16) x |= (v & 0x7f80u) == 0x7f80u || (v & 0x7f800000u) == 0x7f800000u;
+                  else if constexpr (TYPE == KC_E4M3) x |= (((v & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+                }
+          odd = __any(x != 0);
+        }
+        if (!odd) {
+          times_v(p, o);
+        } else {
+          // one token's rows after the other, what these do not see taken out
+          uint32_t keep[NT][4][F::kVHalves][F::kVDwords];
+          __builtin_memcpy(keep, vr, sizeof(vr));
+          const int t0 = row0 / a.G, t1 = (row0 + 15) / a.G;
+          for (int tt = t0; tt <= t1 && tt < a.T; ++tt) {
+            const int32_t hi_t = len - a.T + tt, lo_t = a.window > 0 ? hi_t - a.window + 1 : 0;
+#pragma unroll
+            for (int u = 0; u < NT; ++u)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const int32_t x = at_v[u].pos + 4 * g + i;
+                const bool in = x >= lo_t && x <= hi_t;
+#pragma unroll
+                for (int h = 0; h < F::kVHalves; ++h)
+#pragma unroll
+                  for (int w = 0; w < F::kVDwords; ++w) vr[u][i][h][w] = in ? keep[u][i][h][w] : 0u;
+              }
+            f32x4_t some[NO] = {};
+            times_v(p, some);
+            const bool mine = row_there && t == tt;
+#pragma unroll
+            for (int j = 0; j < NO; ++j)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) o[j][i] += mine ? some[j][i] : 0.f;
+          }
+        }
+        load_v(pos + stride, id_cur);
+      }
+    }
+
+    // ---- the waves' parts
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    __syncthreads();                      // (the last segment's have been read)
+    float* own = lds + wave * 16 * LD;
+#pragma unroll
+    for (int h = 0; h < F::kVHalves; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < F::kVW; e += 4)
+          *reinterpret_cast<f32x4_t*>(own + c * LD + (h * 16 + g * 4 + i) * F::kVW + e) =
+              f32x4_t{o[h * F::kVW + e][i], o[h * F::kVW + e + 1][i], o[h * F::kVW + e + 2][i], o[h * F::kVW + e + 3][i]};
+    if (g == 0) {
+      lds_ml[(wave * 16 + c) * 2] = m;
+      lds_ml[(wave * 16 + c) * 2 + 1] = l;
+    }
+    __syncthreads();
+    const int64_t slot = 2 * (int64_t)blockIdx.x + (chunk == 0);
+    const int quads = a.D / 4, rows_here = a.R - group * a.group_rows < a.group_rows ? a.R - group * a.group_rows : a.group_rows;
+    for (int x = threadIdx.x; x < rows_here * quads; x += kAttnThreads) {
+      const int r = x / quads, d = (x - r * quads) * 4, tile = r >> 4, r16 = r & 15;
+      float top = -INFINITY, sum = 0.f;
+      for (int w = tile; w < kAttnWaves; w += a.tile_waves) top = fmaxf(top, lds_ml[(w * 16 + r16) * 2]);
+      const float use = top == -INFINITY ? 0.f : top;
+      f32x4_t v = {};
+      for (int w = tile; w < kAttnWaves; w += a.tile_waves) {
+        const float f = __builtin_amdgcn_exp2f(lds_ml[(w * 16 + r16) * 2] - use);
+        sum += f * lds_ml[(w * 16 + r16) * 2 + 1];
+        v += f * *reinterpret_cast<const f32x4_t*>(lds + (w * 16 + r16) * LD + d);
+      }
+      const int rr = group * a.group_rows + r;
+      if (whole) {
+        const int tt = rr / a.G;
+        const int64_t o_row = ((int64_t)b * a.T + tt) * (a.heads * a.G) + head * a.G + (rr - tt * a.G);
+        const bool some = sum != 0.f;     // (NaN: some)
+        const float inv = 1.f / sum;
+        if (!some) v = f32x4_t{};
+        else v *= inv;
+        if constexpr (F32Q) *reinterpret_cast<f32x4_t*>(reinterpret_cast<float*>(a.out) + o_row * a.D + d) = v;
+        else *reinterpret_cast<au32x2_t*>(reinterpret_cast<uint16_t*>(a.out) + o_row * a.D + d) = au32x2_t{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+        if (d == 0 && a.lse) a.lse[o_row] = some ? top * 0.6931471805599453f + logf(sum) : -INFINITY;
+      } else {
+        *reinterpret_cast<f32x4_t*>(a.part + (slot * a.group_rows + r) * a.D + d) = v;
+        if (d == 0) {
+          a.part_ml[(slot * a.group_rows + r) * 2] = top;
+          a.part_ml[(slot * a.group_rows + r) * 2 + 1] = sum;
+        }
+      }
+    }
+    // on to what comes next in the run
+    left -= here;
+    chunk = 0;
+    if (left > 0 && ++hr == a.heads * a.row_groups) {
+      hr = 0;
+      do ++b;
+      while (seq_span(a, b).chunks == 0);   // (there is one: chunks are left)
+    }
+  } while (left > 0);
+}
+
+// ---- parts of several blocks -------------------------------------------------------
+// A wave per row: (sequence, head, row group) by blockIdx.x, four rows of it by blockIdx.y.
+template <bool F32Q> __global__ __launch_bounds__(kAttnThreads) void kv_join_kernel(KvAttnDev a, int blocks) {
+  __shared__ int32_t s_sum[4], s_found[2];
+  const int hrs = a.heads * a.row_groups, b = blockIdx.x / hrs, hr = blockIdx.x - b * hrs;
+  const int head = hr / a.row_groups, group = hr - head * a.row_groups;
+  const int32_t total = cut_total(a, s_sum), per = cut_per(total, blocks);
+  const SeqSpan span = seq_span(a, b);
+  int32_t k0 = 0, k1 = -1;
+  if (span.chunks > 0) {
+    // chunks ahead of this sequence
+    int32_t n = 0;
+    for (int i = threadIdx.x; i < b; i += kAttnThreads) n += seq_span(a, i).chunks;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = n;
+    __syncthreads();
+    const int32_t at = (s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3]) * hrs + hr * span.chunks;
+    k0 = at / per;
+    k1 = (at + span.chunks - 1) / per;
+    if (k0 == k1) return;                 // one block's, written by it
+  }
+  const int lane = threadIdx.x & 63, r = blockIdx.y * 4 + (threadIdx.x >> 6), rr = group * a.group_rows + r;
+  if (r >= a.group_rows || rr >= a.R) return;
+  auto slot = [&](int32_t k) { return (2 * (int64_t)k + (k == k0)) * a.group_rows + r; };
+  float top = -INFINITY;
+  for (int32_t k = k0 + lane; k <= k1; k += 64) top = fmaxf(top, a.part_ml[slot(k) * 2]);
+  top = wave_max(top);
+  const float use = top == -INFINITY ? 0.f : top;
+  float sum = 0.f;
+  f32x4_t v = {};
+  for (int32_t k = k0; k <= k1; ++k) {
+    const float f = __builtin_amdgcn_exp2f(a.part_ml[slot(k) * 2] - use);
+    sum += f * a.part_ml[slot(k) * 2 + 1];
+    if (lane * 4 < a.D) v += f * *reinterpret_cast<const f32x4_t*>(a.part + slot(k) * a.D + lane * 4);
+  }
+  const int t = rr / a.G;
+  const int64_t o_row = ((int64_t)b * a.T + t) * (a.heads * a.G) + head * a.G + (rr - t * a.G);
+  const bool some = sum != 0.f;
+  if (!some) v = f32x4_t{};
+  else v *= 1.f / sum;
+  if (lane * 4 < a.D) {
+    if constexpr (F32Q) *reinterpret_cast<f32x4_t*>(reinterpret_cast<float*>(a.out) + o_row * a.D + lane * 4) = v;
+    else *reinterpret_cast<au32x2_t*>(reinterpret_cast<uint16_t*>(a.out) + o_row * a.D + lane * 4) = au32x2_t{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+  }
+  if (lane == 0 && a.lse) a.lse[o_row] = some ? top * 0.6931471805599453f + logf(sum) : -INFINITY;
+}
+
+// ---- host --------------------------------------------------------------------------
+struct AttnPlan {
+  int G, R, row_tiles, tile_waves, row_groups, group_rows;
+  bool split;
+  int blocks;
+  size_t part_ml, total;
+};
+
+as_status check_attn(const kc_cache* c, const kc_attn* s) {
+  if (!s) return set_error(AS_ERR_NULL, "attn is NULL");
+  if (s->T < 1 || s->T > 64 || s->q_heads < 1 || s->q_heads % c->heads != 0 || (int64_t)s->T * (s->q_heads / c->heads) > 1024)
+    return set_error(AS_ERR_SHAPE, "%d tokens of %d heads of queries, %d of the cache", s->T, s->q_heads, c->heads);
+  if (s->max_len < 1 || s->max_len > (int64_t)c->max_pages * c->page || s->max_len >= 1 << 28)
+    return set_error(AS_ERR_SHAPE, "max_len=%d with %d pages of %d tokens to a sequence", s->max_len, c->max_pages, c->page);
+  if (s->window < 0 || !std::isfinite(s->scale)) return set_error(AS_ERR_SHAPE, "window=%d scale=%g", s->window, (double)s->scale);
+  const int R = s->T * (s->q_heads / c->heads), groups = (R + 63) / 64;
+  // (chunks are counted in 31 bits)
+  if ((int64_t)c->B * c->heads * groups * ((s->max_len + kChunk - 1) / kChunk + 1) >= (int64_t)1 << 31)
+    return set_error(AS_ERR_SHAPE, "%d sequences of %d heads up to %d tokens are too many for one call", c->B, c->heads, s->max_len);
+  return AS_OK;
+}
+
+AttnPlan attn_plan(const kc_cache* c, const kc_attn* s) {
+  AttnPlan p;
+  p.G = s->q_heads / c->heads;
+  p.R = s->T * p.G;
+  p.row_tiles = (p.R + 15) / 16;
+  p.tile_waves = p.row_tiles >= 3 ? 4 : p.row_tiles;
+  p.row_groups = (p.row_tiles + p.tile_waves - 1) / p.tile_waves;
+  p.group_rows = p.row_groups > 1 ? p.tile_waves * 16 : p.R;
+  int64_t span = s->max_len;
+  if (s->window > 0 && (int64_t)s->window + s->T + kKvTile < span) span = (int64_t)s->window + s->T + kKvTile;
+  const int64_t pairs = (int64_t)c->B * c->heads * p.row_groups, chunks = (span + kChunk - 1) / kChunk;
+  p.split = chunks > kMinChunks;
+  int64_t blocks = pairs;
+  if (p.split) {
+    blocks = (pairs * chunks + kMinChunks - 1) / kMinChunks;
+    if (blocks > kMostBlocks) blocks = kMostBlocks;
+  }
+  p.blocks = (int)blocks;
+  const size_t rows = p.split ? (size_t)2 * p.blocks * p.group_rows : 0;
+  p.part_ml = (rows * c->D * 4 + 255) / 256 * 256;
+  p.total = p.part_ml + rows * 8;
+  if (p.total < 16) p.total = 16;
+  return p;
+}
+
+template <int TYPE, bool F32Q, int DP> hipError_t launch_attn(const KvAttnDev& a, int blocks, hipStream_t st) {
+  constexpr int smem = kAttnWaves * 16 * (DP + 4 + 2) * 4;
+  auto kfn = kv_attn_kernel<TYPE, F32Q, DP>;
+  static LdsLimit limit;
+  const hipError_t e = limit.raise(reinterpret_cast<const void*>(kfn), smem);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kfn, dim3(blocks), dim3(kAttnThreads), smem, st, a);
+  return hipGetLastError();
+}
+template <int TYPE, bool F32Q> hipError_t launch_attn_any(const KvAttnDev& a, int blocks, hipStream_t st) {
+  return a.D <= 64 ? launch_attn<TYPE, F32Q, 64>(a, blocks, st) : a.D <= 128 ? launch_attn<TYPE, F32Q, 128>(a, blocks, st)
+                                                                             : launch_attn<TYPE, F32Q, 256>(a, blocks, st);
+}
+
+}  // namespace
+}  // namespace asx
+
+using namespace asx;
+
+extern "C" size_t kv_cache_attn_workspace_bytes(const kc_cache* cache, const kc_attn* attn) {
+  if (kv_check_cache(cache) != AS_OK || check_attn(cache, attn) != AS_OK) return 0;
+  return attn_plan(cache, attn).total;
+}
+
+extern "C" as_status kv_cache_attn(const kc_cache* cache, const kc_attn* attn, const void* q, int64_t ld_q, const void* k_pages,
+                                   const void* v_pages, const float* k_scales, const float* v_scales, const int32_t* page_table,
+                                   const int32_t* lengths, void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  as_status rc = kv_check_cache(cache);
+  if (rc == AS_OK) rc = check_attn(cache, attn);
+  if (rc != AS_OK) return rc;
+  if (!q || !lengths || !out || !workspace) return set_error(AS_ERR_NULL, "kv_cache_attn: a required pointer is NULL");
+  rc = kv_check_pool(cache, k_pages, v_pages, k_scales, v_scales, page_table, "kv_cache_attn");
+  if (rc != AS_OK) return rc;
+  const bool f32 = cache->dtype == AS_F32;
+  if (ld_q < (int64_t)attn->q_heads * cache->D || ld_q >= (int64_t)1 << 32) return set_error(AS_ERR_SHAPE, "kv_cache_attn: rows %lld elements apart", (long long)ld_q);
+  if (ld_q * (f32 ? 4 : 2) % 16 != 0) return set_error(AS_ERR_ALIGN, "kv_cache_attn: rows %lld elements apart do not start on 16 bytes", (long long)ld_q);
+  const AttnPlan p = attn_plan(cache, attn);
+  if (workspace_bytes < p.total) return set_error(AS_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", workspace_bytes, p.total);
+  for (const void* x : {q, (const void*)lengths, (const void*)out, (const void*)lse, (const void*)workspace})
+    if (!kv_al16(x)) return set_error(AS_ERR_ALIGN, "kv_cache_attn: a pointer is not 16-byte aligned");
+  unsigned char* ws = reinterpret_cast<unsigned char*>(workspace);
+  KvAttnDev a;
+  a.q = q;
+  a.k_pages = k_pages;
+  a.v_pages = v_pages;
+  a.k_scales = k_scales;
+  a.v_scales = v_scales;
+  a.table = page_table;
+  a.lengths = lengths;
+  a.out = out;
+  a.lse = lse;
+  a.part = reinterpret_cast<float*>(ws);
+  a.part_ml = reinterpret_cast<float*>(ws + p.part_ml);
+  a.ld_q = ld_q;
+  a.B = cache->B;
+  a.T = attn->T;
+  a.heads = cache->heads;
+  a.G = p.G;
+  a.D = cache->D;
+  a.R = p.R;
+  a.row_tiles = p.row_tiles;
+  a.tile_waves = p.tile_waves;
+  a.row_groups = p.row_groups;
+  a.group_rows = p.group_rows;
+  a.page = cache->page;
+  a.page_tiles = cache->page / kKvTile;
+  a.pages = cache->pages;
+  a.max_pages = cache->max_pages;
+  a.max_len = attn->max_len;
+  a.window = attn->window;
+  a.magic = kv_magic((uint32_t)a.page_tiles);
+  a.split = p.split;
+  a.scale_log2 = attn->scale * 1.4426950408889634f;
+  hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+  hipError_t e;
+  switch (cache->cache_type) {
+    case KC_F32: e = launch_attn_any<KC_F32, true>(a, p.blocks, st); break;
+    case KC_BF16: e = launch_attn_any<KC_BF16, false>(a, p.blocks, st); break;
+    case KC_INT8: e = f32 ? launch_attn_any<KC_INT8, true>(a, p.blocks, st) : launch_attn_any<KC_INT8, false>(a, p.blocks, st); break;
+    default: e = f32 ? launch_attn_any<KC_E4M3, true>(a, p.blocks, st) : launch_attn_any<KC_E4M3, false>(a, p.blocks, st); break;
+  }
+  if (e == hipSuccess && p.split) {
+    const dim3 grid((unsigned)(cache->B * cache->heads * p.row_groups), (unsigned)((p.group_rows + 3) / 4));
+    if (f32) hipLaunchKernelGGL(kv_join_kernel<true>, grid, dim3(kAttnThreads), 0, st, a, p.blocks);
+    else hipLaunchKernelGGL(kv_join_kernel<false>, grid, dim3(kAttnThreads), 0, st, a, p.blocks);
+    e = hipGetLastError();
+  }
+  return e == hipSuccess ? AS_OK : set_error(AS_ERR_HIP, "kv_cache_attn: %s", hipGetErrorString(e));
+}

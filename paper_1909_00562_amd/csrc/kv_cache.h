@@ -1,0 +1,23 @@
+// What the cache's files share: checks of a cache's description, and the attention's launch.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/kv_cache.h"
+
+namespace asx {
+
+constexpr int kKvTile = 16;   // tokens of a tile; pages are whole ones
+inline int kv_bytes(int cache_type) { return cache_type == KC_F32 ? 4 : cache_type == KC_BF16 ? 2 : 1; }
+inline bool kv_coded(int cache_type) { return cache_type == KC_INT8 || cache_type == KC_E4M3; }
+
+as_status kv_check_cache(const kc_cache* c);
+// the pool's pointers: what has to be there, and on 16 bytes
+as_status kv_check_pool(const kc_cache* c, const void* k_pages, const void* v_pages, const float* k_scales, const float* v_scales,
+                        const int32_t* page_table, const char* what);
+inline bool kv_al16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// division of n < 2^24 by d <= 256 as a product: n (m d - 2^32) < 2^32
+inline uint32_t kv_magic(uint32_t d) { return d == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + d - 1) / d); }
+
+}  // namespace asx

@@ -1,0 +1,257 @@
+// Paged cache of keys and values: rows into it and out of it, as they are or in 8 bits (entry points and kernels).
+//
+// A row is a token's D values of one head, of keys or of values; the largest magnitude of its values, which the scale of its codes is made
+// of, is found by the lanes that hold it.  Bound by memory: each value is read once and each code written once.
+#include "kv_cache.h"
+
+#include <type_traits>
+
+#include "common.h"
+#include "status.h"
+
+namespace asx {
+
+as_status kv_check_cache(const kc_cache* c) {
+  if (!c) return set_error(AS_ERR_NULL, "cache is NULL");
+  if ((c->dtype != AS_F32 && c->dtype != AS_BF16) || (c->cache_type != c->dtype && !kv_coded(c->cache_type)))
+    return set_error(AS_ERR_DTYPE, "cache of type %d for values of dtype %d", c->cache_type, c->dtype);
+  if (c->pages < 1 || c->page < kKvTile || c->page > 4096 || c->page % kKvTile != 0 || (int64_t)c->pages * c->page >= (int64_t)1 << 31)
+    return set_error(AS_ERR_SHAPE, "%d pages of %d tokens", c->pages, c->page);
+  if (c->heads < 1 || c->heads > 1024 || c->D < 16 || c->D > 256 || c->D % 16 != 0)
+    return set_error(AS_ERR_SHAPE, "%d heads of %d", c->heads, c->D);
+  if (c->B < 1 || c->B > (1 << 16) || c->max_pages < 1 || (int64_t)c->B * c->max_pages >= (int64_t)1 << 31 ||
+      (int64_t)c->max_pages * c->page >= (int64_t)1 << 31)
+    return set_error(AS_ERR_SHAPE, "table of %d sequences, %d pages each of %d tokens", c->B, c->max_pages, c->page);
+  return AS_OK;
+}
+
+as_status kv_check_pool(const kc_cache* c, const void* k_pages, const void* v_pages, const float* k_scales, const float* v_scales,
+                        const int32_t* page_table, const char* what) {
+  if (!k_pages || !v_pages || !page_table) return set_error(AS_ERR_NULL, "%s: a required pointer is NULL", what);
+  if (kv_coded(c->cache_type) ? !k_scales || !v_scales : k_scales || v_scales)
+    return set_error(AS_ERR_NULL, "%s: scales belong to caches in 8 bits, and to those alone", what);
+  for (const void* p : {k_pages, v_pages, (const void*)k_scales, (const void*)v_scales, (const void*)page_table})
+    if (!kv_al16(p)) return set_error(AS_ERR_ALIGN, "%s: a pointer is not 16-byte aligned", what);
+  return AS_OK;
+}
+
+namespace {
+
+typedef uint32_t ku32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t ku32x2_t __attribute__((ext_vector_type(2)));
+
+struct KvMove {
+  const int32_t *seq, *pos, *table;
+  int32_t N, heads, D, page, pages, B, max_pages;
+  int32_t lanes_log;    // 2^lanes_log lanes to a row, 8 values each
+  const void* src[2];   // dense side, keys and values, rows of a token ld apart
+  int64_t ld[2];
+  void* dst[2];
+  void* pool[2];
+  float* scales[2];
+};
+
+// a token's place in the pool, (page, place in it) as page * page_size + place, or -1
+__device__ __forceinline__ int64_t place_of(const KvMove& a, int n) {
+  const int32_t b = a.seq[n], p = a.pos[n];
+  if (b < 0 || b >= a.B || p < 0) return -1;
+  const int32_t col = p / a.page;
+  if (col >= a.max_pages) return -1;
+  const int32_t id = a.table[(int64_t)b * a.max_pages + col];
+  if (id < 0 || id >= a.pages) return -1;
+  return (int64_t)id * a.page + (p - col * a.page);
+}
+
+__device__ __forceinline__ void ld8(const uint16_t* p, float (&x)[8]) {
+  const ku32x4_t q = *reinterpret_cast<const ku32x4_t*>(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t w = q[i];
+    x[2 * i] = lo_bf16(w);
+    x[2 * i + 1] = hi_bf16(w);
+  }
+}
+__device__ __forceinline__ void ld8(const float* p, float (&x)[8]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const f32x4_t q = *reinterpret_cast<const f32x4_t*>(p + 4 * h);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[4 * h + i] = q[i];
+  }
+}
+__device__ __forceinline__ void st8(uint16_t* p, const float (&x)[8]) {
+  *reinterpret_cast<ku32x4_t*>(p) = ku32x4_t{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
+}
+__device__ __forceinline__ void st8(float* p, const float (&x)[8]) {
+  *reinterpret_cast<f32x4_t*>(p) = f32x4_t{x[0], x[1], x[2], x[3]};
+  *reinterpret_cast<f32x4_t*>(p + 4) = f32x4_t{x[4], x[5], x[6], x[7]};
+}
+
+// eight codes
+template <int TYPE> __device__ __forceinline__ ku32x2_t encode8(const float (&x)[8], float inv) {
+  ku32x2_t q;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if constexpr (TYPE == KC_INT8) {
+      uint32_t w = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w |= ((uint32_t)(int32_t)rintf(x[4 * h + i] * inv) & 0xffu) << (8 * i);
+      q[h] = w;
+    } else {
+      int w = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * h] * inv, x[4 * h + 1] * inv, 0, false);
+      w = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * h + 2] * inv, x[4 * h + 3] * inv, w, true);
+      q[h] = (uint32_t)w;
+    }
+  }
+  return q;
+}
+template <int TYPE> __device__ __forceinline__ void decode8(ku32x2_t q, float scale, float (&x)[8]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t w = q[h];
+    if constexpr (TYPE == KC_INT8) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[4 * h + i] = (float)(int8_t)(w >> (8 * i)) * scale;
+    } else {
+      const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+      x[4 * h] = a[0] * scale;
+      x[4 * h + 1] = a[1] * scale;
+      x[4 * h + 2] = b[0] * scale;
+      x[4 * h + 3] = b[1] * scale;
+    }
+  }
+}
+
+// row r: token r / (2 heads), then keys' heads, then values'
+template <typename TE, int TYPE, bool WRITE> __global__ __launch_bounds__(256) void kv_move_kernel(KvMove a) {
+  const int64_t r = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> a.lanes_log;
+  const int lane = threadIdx.x & ((1 << a.lanes_log) - 1), d = lane * 8;
+  const int64_t n = r / (2 * a.heads);
+  if (n >= a.N) return;
+  const int hh = (int)(r - n * (2 * a.heads)), of_v = hh >= a.heads, h = of_v ? hh - a.heads : hh;
+  const bool here = d < a.D;
+  const int64_t place = place_of(a, (int)n);
+  const int64_t page = place / a.page;
+  const int64_t row = (page * a.heads + h) * a.page + (place - page * a.page);   // of the pool
+  float x[8] = {};
+  if constexpr (WRITE) {
+    if (place < 0) return;
+    const TE* from = reinterpret_cast<const TE*>(a.src[of_v]) + n * a.ld[of_v] + h * a.D + d;
+    if (here) ld8(from, x);
+    if constexpr (TYPE == KC_F32 || TYPE == KC_BF16) {
+      if (here) st8(reinterpret_cast<TE*>(a.pool[of_v]) + row * a.D + d, x);
+    } else {
+      // the largest magnitude, as bits: a NaN's are above infinity's
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t m = __builtin_bit_cast(uint32_t, x[i]) & 0x7fffffffu;
+        top = m > top ? m : top;
+      }
+      for (int o = 1; o < 1 << a.lanes_log; o <<= 1) {
+        const uint32_t m = __shfl_xor(top, o, 64);
+        top = m > top ? m : top;
+      }
+      constexpr float kLargest = TYPE == KC_INT8 ? 127.f : 448.f;
+      const bool finite = top < 0x7f800000u;
+      const float scale = fmaxf(__builtin_bit_cast(float, top) / kLargest, 0x1p-120f), inv = finite ? 1.f / scale : 0.f;
+      if (!finite)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = 0.f;
+      if (here) *reinterpret_cast<ku32x2_t*>(reinterpret_cast<uint8_t*>(a.pool[of_v]) + row * a.D + d) = encode8<TYPE>(x, inv);
+      if (lane == 0) a.scales[of_v][row] = finite ? scale : __builtin_nanf("");
+    }
+  } else {
+    if (!here) return;
+    if (place >= 0) {
+      if constexpr (TYPE == KC_F32 || TYPE == KC_BF16) ld8(reinterpret_cast<const TE*>(a.pool[of_v]) + row * a.D + d, x);
+      else decode8<TYPE>(*reinterpret_cast<const ku32x2_t*>(reinterpret_cast<const uint8_t*>(a.pool[of_v]) + row * a.D + d), a.scales[of_v][row], x);
+    }
+    st8(reinterpret_cast<TE*>(a.dst[of_v]) + (n * a.heads + h) * a.D + d, x);
+  }
+}
+
+template <bool WRITE> as_status move(const kc_cache* c, const KvMove& a, hipStream_t st) {
+  const int64_t rows = (int64_t)a.N * 2 * a.heads, per_block = 256 >> a.lanes_log, blocks = (rows + per_block - 1) / per_block;
+  if (blocks >= (int64_t)1 << 24) return set_error(AS_ERR_SHAPE, "%d tokens of %d heads in one call", a.N, a.heads);
+  auto run = [&](auto* t, auto type) {
+    using TE = typename std::remove_pointer<decltype(t)>::type;
+    hipLaunchKernelGGL((kv_move_kernel<TE, decltype(type)::value, WRITE>), dim3((unsigned)blocks), dim3(256), 0, st, a);
+  };
+  auto any = [&](auto* t, auto same) {
+    if (c->cache_type == KC_INT8) run(t, std::integral_constant<int, KC_INT8>{});
+    else if (c->cache_type == KC_E4M3) run(t, std::integral_constant<int, KC_E4M3>{});
+    else run(t, same);
+  };
+  if (c->dtype == AS_F32) any((float*)nullptr, std::integral_constant<int, KC_F32>{});
+  else any((uint16_t*)nullptr, std::integral_constant<int, KC_BF16>{});
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? AS_OK : set_error(AS_ERR_HIP, "rows of the cache: %s", hipGetErrorString(e));
+}
+
+KvMove move_args(const kc_cache* c, int32_t N, const int32_t* seq, const int32_t* pos, const int32_t* table, const void* k_pages,
+                 const void* v_pages, const float* k_scales, const float* v_scales) {
+  KvMove a{};
+  a.seq = seq;
+  a.pos = pos;
+  a.table = table;
+  a.N = N;
+  a.heads = c->heads;
+  a.D = c->D;
+  a.page = c->page;
+  a.pages = c->pages;
+  a.B = c->B;
+  a.max_pages = c->max_pages;
+  while (8 << a.lanes_log < c->D) ++a.lanes_log;
+  a.pool[0] = const_cast<void*>(k_pages);
+  a.pool[1] = const_cast<void*>(v_pages);
+  a.scales[0] = const_cast<float*>(k_scales);
+  a.scales[1] = const_cast<float*>(v_scales);
+  return a;
+}
+
+}  // namespace
+}  // namespace asx
+
+using namespace asx;
+
+extern "C" as_status kv_cache_write(const kc_cache* cache, int32_t N, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                                    const int32_t* seq, const int32_t* pos, const int32_t* page_table, void* k_pages, void* v_pages,
+                                    float* k_scales, float* v_scales, void* hip_stream) {
+  as_status rc = kv_check_cache(cache);
+  if (rc != AS_OK) return rc;
+  if (N < 1 || N > (1 << 24)) return set_error(AS_ERR_SHAPE, "kv_cache_write: N=%d", N);
+  if (!k || !v || !seq || !pos) return set_error(AS_ERR_NULL, "kv_cache_write: a required pointer is NULL");
+  rc = kv_check_pool(cache, k_pages, v_pages, k_scales, v_scales, page_table, "kv_cache_write");
+  if (rc != AS_OK) return rc;
+  for (int64_t ld : {ld_k, ld_v}) {
+    if (ld < (int64_t)cache->heads * cache->D || ld >= (int64_t)1 << 32) return set_error(AS_ERR_SHAPE, "kv_cache_write: rows %lld elements apart", (long long)ld);
+    if (ld * (cache->dtype == AS_F32 ? 4 : 2) % 16 != 0)
+      return set_error(AS_ERR_ALIGN, "kv_cache_write: rows %lld elements apart do not start on 16 bytes", (long long)ld);
+  }
+  for (const void* p : {k, v, (const void*)seq, (const void*)pos})
+    if (!kv_al16(p)) return set_error(AS_ERR_ALIGN, "kv_cache_write: a pointer is not 16-byte aligned");
+  KvMove a = move_args(cache, N, seq, pos, page_table, k_pages, v_pages, k_scales, v_scales);
+  a.src[0] = k;
+  a.src[1] = v;
+  a.ld[0] = ld_k;
+  a.ld[1] = ld_v;
+  return move<true>(cache, a, reinterpret_cast<hipStream_t>(hip_stream));
+}
+
+extern "C" as_status kv_cache_read(const kc_cache* cache, int32_t N, const void* k_pages, const void* v_pages, const float* k_scales,
+                                   const float* v_scales, const int32_t* seq, const int32_t* pos, const int32_t* page_table, void* k, void* v,
+                                   void* hip_stream) {
+  as_status rc = kv_check_cache(cache);
+  if (rc != AS_OK) return rc;
+  if (N < 1 || N > (1 << 24)) return set_error(AS_ERR_SHAPE, "kv_cache_read: N=%d", N);
+  if (!k || !v || !seq || !pos) return set_error(AS_ERR_NULL, "kv_cache_read: a required pointer is NULL");
+  rc = kv_check_pool(cache, k_pages, v_pages, k_scales, v_scales, page_table, "kv_cache_read");
+  if (rc != AS_OK) return rc;
+  for (const void* p : {(const void*)k, (const void*)v, (const void*)seq, (const void*)pos})
+    if (!kv_al16(p)) return set_error(AS_ERR_ALIGN, "kv_cache_read: a pointer is not 16-byte aligned");
+  KvMove a = move_args(cache, N, seq, pos, page_table, k_pages, v_pages, k_scales, v_scales);
+  a.dst[0] = k;
+  a.dst[1] = v;
+  return move<false>(cache, a, reinterpret_cast<hipStream_t>(hip_stream));
+}
