@@ -130,7 +130,7 @@ def test_a_draft_that_agrees_is_accepted_and_an_impossible_one_is_not():
     n, words = oracle.verify(t, t[:3], [3, 5, 7], [0.999] * 3, 0.5, 0.8)
     assert n == 3 and list(words[:3]) == [3, 5, 7] and words[3] >= 0
     t[1, 5] = -np.inf
-    n, words = oracle.verify(t, t[:3] * 0, [3, 5, 7], [0.0] * 3, 0.5, 1.0)
+    n, words = oracle.verify(t, np.zeros((3, 20)), [3, 5, 7], [0.0] * 3, 0.5, 1.0)
     assert n == 1 and words[1] not in (-1, 5) and (words[2:] == -1).all()
     n, words = oracle.verify(t, t[:3], [3, -1, 7], [0.0] * 3, 0.0, 1.0)
     assert n == 1 and words[1] == 0
