@@ -209,7 +209,7 @@ def test_rows_that_are_refused():
             assert f(**{name: None}) == 1, name
             assert f(**{name: A[9] + 4}) == 5, name
         assert f(_cache(cache_type=bd.KC_BF16)) == 1                     # scales of a cache that has none
-    assert bd.kv_cache_write(None, 5, *A[:2], 64, *A[2:3], 64, *A[3:10], 0, check=False) == 1
+    assert bd.kv_cache_write(None, 5, A[0], 64, A[1], 64, *A[2:9], check=False) == 1
     for kw in (dict(ld_k=63), dict(ld_v=48), dict(ld_k=-64), dict(ld_v=1 << 32)):
         assert _write(**kw) == 2, kw
     assert _write(ld_k=68) == 5 and _write(_cache(dtype=bd.AS_F32), ld_v=66) == 5
