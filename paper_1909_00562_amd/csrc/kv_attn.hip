@@ -27,10 +27,10 @@ namespace {
 typedef uint32_t au32x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t au32x2_t __attribute__((ext_vector_type(2)));
 
-constexpr int kAttnThreads = 256, kAttnWaves = 4;
-constexpr int kChunk = 128;            // tokens of a chunk
-constexpr int kMinChunks = 4;          // of a block's run
-constexpr int kMostBlocks = 1024;
+constexpr int kJoinThreads = 256;
+constexpr int kMostBlocks = 512;
+constexpr int kLeastChunk = 16;
+constexpr int kWholeChunks = 4;        // up to so many chunks a block takes all of a (sequence, head)
 constexpr uint32_t kAttnOob = 0x80000000u;
 
 struct KvAttnDev {
@@ -45,6 +45,7 @@ struct KvAttnDev {
   int32_t row_tiles, tile_waves, row_groups, group_rows;   // tiles of 16 rows; of a block (1, 2 or 4); groups of a block's tiles; rows of a group
   int32_t page, page_tiles, pages, max_pages, max_len, window;
   uint32_t magic;                      // of page_tiles
+  int32_t chunk;                       // tokens of a chunk
   int32_t split;                       // 0: a block per (sequence, head, row group), no second launch
   float scale_log2;
 };
@@ -60,34 +61,32 @@ __device__ __forceinline__ SeqSpan seq_span(const KvAttnDev& a, int b) {
   const int32_t first = a.window > 0 ? n - a.T + 1 - a.window : 0;
   s.len = n;
   s.base = first > 0 ? first & ~(kKvTile - 1) : 0;
-  s.chunks = (n - s.base + kChunk - 1) / kChunk;
+  s.chunks = (n - s.base + a.chunk - 1) / a.chunk;
   return s;
 }
 
-struct Cut {
-  int32_t per, blocks_used;    // chunks of a run
-  int32_t b;                   // the sequence that holds chunk `at`
-  int32_t ahead;               // chunks of the sequences ahead of it
-};
-// Adds up the sequences' chunks (times the heads and row groups), 256 sequences at a time; the same numbers in every block.
-__device__ __forceinline__ int32_t cut_total(const KvAttnDev& a, int32_t* s_sum) {
+// Adds up the sequences' chunks (times the heads and row groups), a block's threads of them at a time; the same numbers in every block.
+template <int WAVES> __device__ __forceinline__ int32_t cut_total(const KvAttnDev& a, int32_t* s_sum) {
   int32_t n = 0;
-  for (int b = threadIdx.x; b < a.B; b += kAttnThreads) n += seq_span(a, b).chunks;
+  for (int b = threadIdx.x; b < a.B; b += WAVES * 64) n += seq_span(a, b).chunks;
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
   if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = n;
   __syncthreads();
-  return (s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3]) * a.heads * a.row_groups;
+  n = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) n += s_sum[w];
+  return n * a.heads * a.row_groups;
 }
 __device__ __forceinline__ int32_t cut_per(int32_t total, int blocks) {
   const int32_t per = (total + blocks - 1) / blocks;
-  return per < kMinChunks ? kMinChunks : per;
+  return per < 1 ? 1 : per;
 }
 // the sequence of chunk `at` of all, and the chunks ahead of it
-__device__ __forceinline__ void cut_find(const KvAttnDev& a, int32_t at, int32_t* s_sum, int32_t* s_found, int32_t& b_out, int32_t& ahead_out) {
+template <int WAVES> __device__ __forceinline__ void cut_find(const KvAttnDev& a, int32_t at, int32_t* s_sum, int32_t* s_found, int32_t& b_out, int32_t& ahead_out) {
   const int32_t hr = a.heads * a.row_groups;
   int32_t carry = 0;
-  for (int b0 = 0; b0 < a.B; b0 += kAttnThreads) {
+  for (int b0 = 0; b0 < a.B; b0 += WAVES * 64) {
     const int b = b0 + threadIdx.x;
     const int32_t own = b < a.B ? seq_span(a, b).chunks * hr : 0;
     int32_t run = own;
@@ -105,7 +104,7 @@ __device__ __forceinline__ void cut_find(const KvAttnDev& a, int32_t at, int32_t
       s_found[0] = b;
       s_found[1] = ahead;
     }
-    carry += s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3];
+    for (int w = 0; w < WAVES; ++w) carry += s_sum[w];
     if (at < carry) break;
   }
   __syncthreads();
@@ -141,6 +140,8 @@ template <int TYPE, bool F32Q, int DP> struct Form {
   static constexpr bool kF32 = TYPE == KC_F32, kCoded = TYPE == KC_INT8 || TYPE == KC_E4M3;
   static constexpr int kBytes = kF32 ? 4 : kCoded ? 1 : 2;
   static constexpr int kTiles = kF32 ? 1 : 2;                       // of a step
+  // Waves of a block.  A wave holds a step's K and V, the queries and O^T in registers: at a width of 256 those of one wave on a SIMD, below of two.
+  static constexpr int kWaves = DP > 128 ? 4 : 8;
   static constexpr int kQTerms = kF32 || !F32Q ? 1 : 3, kPTerms = kF32 ? 1 : F32Q ? 3 : 2;
   static constexpr int kKLoads = DP * kBytes / 64;                  // 16-byte loads of a lane for a tile of K
   static constexpr int kKElems = 16 / kBytes;                       // elements of each: D index (load * 4 + g) * kKElems + i
@@ -172,24 +173,25 @@ template <class F> struct TileAt {
   int32_t valid;    // tokens that there are: up to 16, 0 where there is no page
 };
 
-template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__(kAttnThreads) void kv_attn_kernel(KvAttnDev a) {
+template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__((Form<TYPE, F32Q, DP>::kWaves * 64)) void kv_attn_kernel(KvAttnDev a) {
   using F = Form<TYPE, F32Q, DP>;
+  constexpr int WAVES = F::kWaves;
   constexpr int NT = F::kTiles, NO = DP / 16, STEP = NT * kKvTile, LD = DP + 4;
-  extern __shared__ float lds[];          // [4 waves][16 rows][LD], and their maxima and sums
-  float* lds_ml = lds + kAttnWaves * 16 * LD;
-  __shared__ int32_t s_sum[4], s_found[2];
+  extern __shared__ float lds[];          // [waves][16 rows][LD], and their maxima and sums
+  float* lds_ml = lds + WAVES * 16 * LD;
+  __shared__ int32_t s_sum[WAVES], s_found[2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, g = lane >> 4;
-  const int row_wave = wave % a.tile_waves, tok_wave = wave / a.tile_waves, tok_waves = kAttnWaves / a.tile_waves;
+  const int row_wave = wave % a.tile_waves, tok_wave = wave / a.tile_waves, tok_waves = WAVES / a.tile_waves;   // (some may be left over)
 
   // this block's run of chunks
   int32_t b, hr, chunk, left;             // sequence, (head, row group), first chunk there, chunks left
   if (a.split) {
-    const int32_t total = cut_total(a, s_sum), per = cut_per(total, gridDim.x), at = (int32_t)blockIdx.x * per;
+    const int32_t total = cut_total<WAVES>(a, s_sum), per = cut_per(total, gridDim.x), at = (int32_t)blockIdx.x * per;
     if (at >= total) return;
     left = total - at < per ? total - at : per;
     int32_t ahead;
-    cut_find(a, at, s_sum, s_found, b, ahead);
+    cut_find<WAVES>(a, at, s_sum, s_found, b, ahead);
     const int32_t n = seq_span(a, b).chunks;
     hr = (at - ahead) / n;
     chunk = at - ahead - hr * n;
@@ -209,8 +211,8 @@ template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__(kAttnThreads
     const int32_t len = span.len;
     const int head = hr / a.row_groups, group = hr - head * a.row_groups;
     const int32_t here = a.split ? (left < span.chunks - chunk ? left : span.chunks - chunk) : span.chunks;
-    const int32_t tok0 = span.base + chunk * kChunk;
-    int32_t tok1 = tok0 + here * kChunk;
+    const int32_t tok0 = span.base + chunk * a.chunk;
+    int32_t tok1 = tok0 + here * a.chunk;
     if (tok1 > len) tok1 = len;
     const bool whole = here == span.chunks;
 
@@ -337,14 +339,32 @@ template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__(kAttnThreads
       }
     };
 
-    // O^T += V^T P^T of the step, onto acc
-    auto times_v = [&](const float (&p)[NT][4], f32x4_t (&acc)[NO]) {
+    // O^T += V^T P^T of the step, a block of 16 columns after the other.  ODD: for the rows of one token alone, with what it does not see taken
+    // out of V (bit u * 4 + i of `in`: this lane's token), since 0 times an infinity or a NaN is a NaN.
+    auto times_v = [&](auto odd, const float (&p)[NT][4], uint32_t in, bool mine) {
+      constexpr bool ODD = decltype(odd)::value;
+      auto raw = [&](int u, int i, int h, int w) -> uint32_t {
+        if constexpr (ODD) return in >> (u * 4 + i) & 1 ? vr[u][i][h][w] : 0u;
+        else return vr[u][i][h][w];
+      };
+      auto onto = [&](int j, auto product) {
+        if constexpr (ODD) {
+          f32x4_t some = {};
+          product(some);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[j][i] += mine ? some[i] : 0.f;
+        } else {
+          product(o[j]);
+        }
+      };
       if constexpr (F::kF32) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int j = 0; j < NO; ++j)
+          onto(j, [&](f32x4_t& acc) {
 #pragma unroll
-          for (int j = 0; j < NO; ++j)
-            acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, vr[0][i][j / F::kVW][j % F::kVW]), p[0][i], acc[j], 0, 0, 0);
+            for (int i = 0; i < 4; ++i)
+              acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, raw(0, i, j / F::kVW, j % F::kVW)), p[0][i], acc, 0, 0, 0);
+          });
       } else {
         bf16x8_t pb[F::kPTerms];
 #pragma unroll
@@ -361,8 +381,10 @@ template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__(kAttnThreads
           }
         auto add = [&](int j, au32x4_t v) {
           const bf16x8_t vb = as_frag(v);
+          onto(j, [&](f32x4_t& acc) {
 #pragma unroll
-          for (int s = 0; s < F::kPTerms; ++s) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, pb[s], acc[j], 0, 0, 0);
+            for (int s = 0; s < F::kPTerms; ++s) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, pb[s], acc, 0, 0, 0);
+          });
         };
         if constexpr (F::kCoded) {
 #pragma unroll
@@ -371,7 +393,7 @@ template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__(kAttnThreads
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) codes_to_floats<TYPE>(vr[u][i][0][w], x[u][i]);
+              for (int i = 0; i < 4; ++i) codes_to_floats<TYPE>(raw(u, i, 0, w), x[u][i]);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
               add(w * 4 + e, au32x4_t{top_halves(x[0][0][e], x[0][1][e]), top_halves(x[0][2][e], x[0][3][e]),
@@ -383,7 +405,7 @@ template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__(kAttnThreads
 #pragma unroll
             for (int e = 0; e < F::kVW; ++e) {
               const uint32_t sel = e % 2 ? 0x07060302u : 0x05040100u;
-              auto two = [&](int u, int i) { return __builtin_amdgcn_perm(vr[u][i + 1][h][e / 2], vr[u][i][h][e / 2], sel); };
+              auto two = [&](int u, int i) { return __builtin_amdgcn_perm(raw(u, i + 1, h, e / 2), raw(u, i, h, e / 2), sel); };
               add(h * F::kVW + e, au32x4_t{two(0, 0), two(0, 2), two(1, 0), two(1, 2)});
             }
         }
@@ -393,7 +415,7 @@ template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__(kAttnThreads
     const int32_t stride = tok_waves * STEP;
     int32_t pos = tok0 + tok_wave * STEP;
     int32_t id[NT], id_next[NT];
-    if (pos < tok1 && row0 < a.R) {
+    if (tok_wave < tok_waves && pos < tok1 && row0 < a.R) {
 #pragma unroll
       for (int u = 0; u < NT; ++u) id[u] = page_of(pos + u * kKvTile);
       load_k(pos, id);
@@ -505,32 +527,20 @@ template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__(kAttnThreads
           odd = __any(x != 0);
         }
         if (!odd) {
-          times_v(p, o);
+          times_v(std::false_type{}, p, 0u, false);
         } else {
-          // one token's rows after the other, what these do not see taken out
-          uint32_t keep[NT][4][F::kVHalves][F::kVDwords];
-          __builtin_memcpy(keep, vr, sizeof(vr));
           const int t0 = row0 / a.G, t1 = (row0 + 15) / a.G;
           for (int tt = t0; tt <= t1 && tt < a.T; ++tt) {
             const int32_t hi_t = len - a.T + tt, lo_t = a.window > 0 ? hi_t - a.window + 1 : 0;
+            uint32_t in = 0;
 #pragma unroll
             for (int u = 0; u < NT; ++u)
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
                 const int32_t x = at_v[u].pos + 4 * g + i;
-                const bool in = x >= lo_t && x <= hi_t;
-#pragma unroll
-                for (int h = 0; h < F::kVHalves; ++h)
-#pragma unroll
-                  for (int w = 0; w < F::kVDwords; ++w) vr[u][i][h][w] = in ? keep[u][i][h][w] : 0u;
+                in |= (uint32_t)(x >= lo_t && x <= hi_t) << (u * 4 + i);
               }
-            f32x4_t some[NO] = {};
-            times_v(p, some);
-            const bool mine = row_there && t == tt;
-#pragma unroll
-            for (int j = 0; j < NO; ++j)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) o[j][i] += mine ? some[j][i] : 0.f;
+            times_v(std::true_type{}, p, in, row_there && t == tt);
           }
         }
         load_v(pos + stride, id_cur);
@@ -557,13 +567,13 @@ template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__(kAttnThreads
     __syncthreads();
     const int64_t slot = 2 * (int64_t)blockIdx.x + (chunk == 0);
     const int quads = a.D / 4, rows_here = a.R - group * a.group_rows < a.group_rows ? a.R - group * a.group_rows : a.group_rows;
-    for (int x = threadIdx.x; x < rows_here * quads; x += kAttnThreads) {
+    for (int x = threadIdx.x; x < rows_here * quads; x += WAVES * 64) {
       const int r = x / quads, d = (x - r * quads) * 4, tile = r >> 4, r16 = r & 15;
       float top = -INFINITY, sum = 0.f;
-      for (int w = tile; w < kAttnWaves; w += a.tile_waves) top = fmaxf(top, lds_ml[(w * 16 + r16) * 2]);
+      for (int w = tile; w < tok_waves * a.tile_waves; w += a.tile_waves) top = fmaxf(top, lds_ml[(w * 16 + r16) * 2]);
       const float use = top == -INFINITY ? 0.f : top;
       f32x4_t v = {};
-      for (int w = tile; w < kAttnWaves; w += a.tile_waves) {
+      for (int w = tile; w < tok_waves * a.tile_waves; w += a.tile_waves) {
         const float f = __builtin_amdgcn_exp2f(lds_ml[(w * 16 + r16) * 2] - use);
         sum += f * lds_ml[(w * 16 + r16) * 2 + 1];
         v += f * *reinterpret_cast<const f32x4_t*>(lds + (w * 16 + r16) * LD + d);
@@ -599,59 +609,87 @@ template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__(kAttnThreads
 }
 
 // ---- parts of several blocks -------------------------------------------------------
-// A wave per row: (sequence, head, row group) by blockIdx.x, four rows of it by blockIdx.y.
-template <bool F32Q> __global__ __launch_bounds__(kAttnThreads) void kv_join_kernel(KvAttnDev a, int blocks) {
-  __shared__ int32_t s_sum[4], s_found[2];
+// A block per row: (sequence, head, row group) by blockIdx.x, its row by blockIdx.y.  Groups of D / 4 lanes (a power of two of them) take
+// the parts in turns; the order of the sums is that of the parts and the groups, whatever the launch.
+template <bool F32Q> __global__ __launch_bounds__(kJoinThreads) void kv_join_kernel(KvAttnDev a, int blocks, int lanes_log) {
+  __shared__ int32_t s_sum[4];
+  __shared__ float s_top[4], s_l[kJoinThreads];
+  __shared__ f32x4_t s_o[kJoinThreads];
   const int hrs = a.heads * a.row_groups, b = blockIdx.x / hrs, hr = blockIdx.x - b * hrs;
   const int head = hr / a.row_groups, group = hr - head * a.row_groups;
-  const int32_t total = cut_total(a, s_sum), per = cut_per(total, blocks);
-  const SeqSpan span = seq_span(a, b);
-  int32_t k0 = 0, k1 = -1;
-  if (span.chunks > 0) {
-    // chunks ahead of this sequence
-    int32_t n = 0;
-    for (int i = threadIdx.x; i < b; i += kAttnThreads) n += seq_span(a, i).chunks;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = n;
-    __syncthreads();
-    const int32_t at = (s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3]) * hrs + hr * span.chunks;
-    k0 = at / per;
-    k1 = (at + span.chunks - 1) / per;
-    if (k0 == k1) return;                 // one block's, written by it
+  const int r = blockIdx.y, rr = group * a.group_rows + r;
+  if (rr >= a.R) return;
+  // chunks in all, and ahead of this sequence
+  int32_t n = 0, before = 0;
+  for (int i = threadIdx.x; i < a.B; i += kJoinThreads) {
+    const int32_t x = seq_span(a, i).chunks;
+    n += x;
+    before += i < b ? x : 0;
   }
-  const int lane = threadIdx.x & 63, r = blockIdx.y * 4 + (threadIdx.x >> 6), rr = group * a.group_rows + r;
-  if (r >= a.group_rows || rr >= a.R) return;
-  auto slot = [&](int32_t k) { return (2 * (int64_t)k + (k == k0)) * a.group_rows + r; };
+  const SeqSpan span = seq_span(a, b);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    n += __shfl_xor(n, o, 64);
+    before += __shfl_xor(before, o, 64);
+  }
+  __shared__ int32_t s_before[4];
+  if ((threadIdx.x & 63) == 0) {
+    s_sum[threadIdx.x >> 6] = n;
+    s_before[threadIdx.x >> 6] = before;
+  }
+  __syncthreads();
+  const int32_t per = cut_per((s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3]) * hrs, blocks);
+  int32_t k0 = 0, parts = 0;
+  if (span.chunks > 0) {
+    const int32_t at = (s_before[0] + s_before[1] + s_before[2] + s_before[3]) * hrs + hr * span.chunks;
+    k0 = at / per;
+    parts = (at + span.chunks - 1) / per - k0 + 1;
+    if (parts == 1) return;               // one block's, written by it
+  }
+  // part k of the pair: its block's slot 2 blk + 1 where the pair begins, else 2 blk
+  auto slot = [&](int32_t k) { return (2 * (int64_t)(k0 + k) + (k == 0)) * a.group_rows + r; };
   float top = -INFINITY;
-  for (int32_t k = k0 + lane; k <= k1; k += 64) top = fmaxf(top, a.part_ml[slot(k) * 2]);
+  for (int32_t k = threadIdx.x; k < parts; k += kJoinThreads) top = fmaxf(top, a.part_ml[slot(k) * 2]);
   top = wave_max(top);
+  if ((threadIdx.x & 63) == 0) s_top[threadIdx.x >> 6] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
   const float use = top == -INFINITY ? 0.f : top;
+  const int groups = kJoinThreads >> lanes_log, gr = threadIdx.x >> lanes_log, d = (threadIdx.x & ((1 << lanes_log) - 1)) * 4;
   float sum = 0.f;
   f32x4_t v = {};
-  for (int32_t k = k0; k <= k1; ++k) {
-    const float f = __builtin_amdgcn_exp2f(a.part_ml[slot(k) * 2] - use);
-    sum += f * a.part_ml[slot(k) * 2 + 1];
-    if (lane * 4 < a.D) v += f * *reinterpret_cast<const f32x4_t*>(a.part + slot(k) * a.D + lane * 4);
+#pragma unroll 4
+  for (int32_t k = gr; k < parts; k += groups) {
+    const int64_t s = slot(k);
+    const float f = __builtin_amdgcn_exp2f(a.part_ml[s * 2] - use);
+    sum += f * a.part_ml[s * 2 + 1];
+    if (d < a.D) v += f * *reinterpret_cast<const f32x4_t*>(a.part + s * a.D + d);
+  }
+  s_o[threadIdx.x] = v;
+  s_l[threadIdx.x] = sum;
+  __syncthreads();
+  if (gr != 0) return;
+  for (int x = 1; x < groups; ++x) {
+    v += s_o[(x << lanes_log) + threadIdx.x];
+    sum += s_l[(x << lanes_log) + threadIdx.x];
   }
   const int t = rr / a.G;
   const int64_t o_row = ((int64_t)b * a.T + t) * (a.heads * a.G) + head * a.G + (rr - t * a.G);
-  const bool some = sum != 0.f;
+  const bool some = sum != 0.f;           // (NaN: some)
   if (!some) v = f32x4_t{};
   else v *= 1.f / sum;
-  if (lane * 4 < a.D) {
-    if constexpr (F32Q) *reinterpret_cast<f32x4_t*>(reinterpret_cast<float*>(a.out) + o_row * a.D + lane * 4) = v;
-    else *reinterpret_cast<au32x2_t*>(reinterpret_cast<uint16_t*>(a.out) + o_row * a.D + lane * 4) = au32x2_t{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+  if (d < a.D) {
+    if constexpr (F32Q) *reinterpret_cast<f32x4_t*>(reinterpret_cast<float*>(a.out) + o_row * a.D + d) = v;
+    else *reinterpret_cast<au32x2_t*>(reinterpret_cast<uint16_t*>(a.out) + o_row * a.D + d) = au32x2_t{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
   }
-  if (lane == 0 && a.lse) a.lse[o_row] = some ? top * 0.6931471805599453f + logf(sum) : -INFINITY;
+  if (d == 0 && a.lse) a.lse[o_row] = some ? top * 0.6931471805599453f + logf(sum) : -INFINITY;
 }
 
 // ---- host --------------------------------------------------------------------------
 struct AttnPlan {
   int G, R, row_tiles, tile_waves, row_groups, group_rows;
   bool split;
-  int blocks;
+  int chunk, blocks;
   size_t part_ml, total;
 };
 
@@ -664,7 +702,7 @@ as_status check_attn(const kc_cache* c, const kc_attn* s) {
   if (s->window < 0 || !std::isfinite(s->scale)) return set_error(AS_ERR_SHAPE, "window=%d scale=%g", s->window, (double)s->scale);
   const int R = s->T * (s->q_heads / c->heads), groups = (R + 63) / 64;
   // (chunks are counted in 31 bits)
-  if ((int64_t)c->B * c->heads * groups * ((s->max_len + kChunk - 1) / kChunk + 1) >= (int64_t)1 << 31)
+  if ((int64_t)c->B * c->heads * groups * ((s->max_len + kLeastChunk - 1) / kLeastChunk + 1) >= (int64_t)1 << 31)
     return set_error(AS_ERR_SHAPE, "%d sequences of %d heads up to %d tokens are too many for one call", c->B, c->heads, s->max_len);
   return AS_OK;
 }
@@ -674,16 +712,18 @@ AttnPlan attn_plan(const kc_cache* c, const kc_attn* s) {
   p.G = s->q_heads / c->heads;
   p.R = s->T * p.G;
   p.row_tiles = (p.R + 15) / 16;
-  p.tile_waves = p.row_tiles >= 3 ? 4 : p.row_tiles;
+  p.tile_waves = p.row_tiles < 4 ? p.row_tiles : 4;
   p.row_groups = (p.row_tiles + p.tile_waves - 1) / p.tile_waves;
   p.group_rows = p.row_groups > 1 ? p.tile_waves * 16 : p.R;
   int64_t span = s->max_len;
   if (s->window > 0 && (int64_t)s->window + s->T + kKvTile < span) span = (int64_t)s->window + s->T + kKvTile;
-  const int64_t pairs = (int64_t)c->B * c->heads * p.row_groups, chunks = (span + kChunk - 1) / kChunk;
-  p.split = chunks > kMinChunks;
+  // a step of every wave
+  p.chunk = (c->D > 128 ? 4 : 8) / p.tile_waves * (c->cache_type == KC_F32 ? kKvTile : 2 * kKvTile);
+  const int64_t pairs = (int64_t)c->B * c->heads * p.row_groups, chunks = (span + p.chunk - 1) / p.chunk;
+  p.split = chunks > kWholeChunks;
   int64_t blocks = pairs;
   if (p.split) {
-    blocks = (pairs * chunks + kMinChunks - 1) / kMinChunks;
+    blocks = pairs * chunks;
     if (blocks > kMostBlocks) blocks = kMostBlocks;
   }
   p.blocks = (int)blocks;
@@ -695,12 +735,12 @@ AttnPlan attn_plan(const kc_cache* c, const kc_attn* s) {
 }
 
 template <int TYPE, bool F32Q, int DP> hipError_t launch_attn(const KvAttnDev& a, int blocks, hipStream_t st) {
-  constexpr int smem = kAttnWaves * 16 * (DP + 4 + 2) * 4;
+  constexpr int waves = Form<TYPE, F32Q, DP>::kWaves, smem = waves * 16 * (DP + 4 + 2) * 4;
   auto kfn = kv_attn_kernel<TYPE, F32Q, DP>;
   static LdsLimit limit;
   const hipError_t e = limit.raise(reinterpret_cast<const void*>(kfn), smem);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kfn, dim3(blocks), dim3(kAttnThreads), smem, st, a);
+  hipLaunchKernelGGL(kfn, dim3(blocks), dim3(waves * 64), smem, st, a);
   return hipGetLastError();
 }
 template <int TYPE, bool F32Q> hipError_t launch_attn_any(const KvAttnDev& a, int blocks, hipStream_t st) {
@@ -765,6 +805,7 @@ extern "C" as_status kv_cache_attn(const kc_cache* cache, const kc_attn* attn, c
   a.max_len = attn->max_len;
   a.window = attn->window;
   a.magic = kv_magic((uint32_t)a.page_tiles);
+  a.chunk = p.chunk;
   a.split = p.split;
   a.scale_log2 = attn->scale * 1.4426950408889634f;
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
@@ -776,9 +817,11 @@ extern "C" as_status kv_cache_attn(const kc_cache* cache, const kc_attn* attn, c
     default: e = f32 ? launch_attn_any<KC_E4M3, true>(a, p.blocks, st) : launch_attn_any<KC_E4M3, false>(a, p.blocks, st); break;
   }
   if (e == hipSuccess && p.split) {
-    const dim3 grid((unsigned)(cache->B * cache->heads * p.row_groups), (unsigned)((p.group_rows + 3) / 4));
-    if (f32) hipLaunchKernelGGL(kv_join_kernel<true>, grid, dim3(kAttnThreads), 0, st, a, p.blocks);
-    else hipLaunchKernelGGL(kv_join_kernel<false>, grid, dim3(kAttnThreads), 0, st, a, p.blocks);
+    const dim3 grid((unsigned)(cache->B * cache->heads * p.row_groups), (unsigned)p.group_rows);
+    int lanes_log = 2;
+    while (4 << lanes_log < cache->D) ++lanes_log;
+    if (f32) hipLaunchKernelGGL(kv_join_kernel<true>, grid, dim3(kJoinThreads), 0, st, a, p.blocks, lanes_log);
+    else hipLaunchKernelGGL(kv_join_kernel<false>, grid, dim3(kJoinThreads), 0, st, a, p.blocks, lanes_log);
     e = hipGetLastError();
   }
   return e == hipSuccess ? AS_OK : set_error(AS_ERR_HIP, "kv_cache_attn: %s", hipGetErrorString(e));

@@ -51,15 +51,14 @@ struct KvMove {
   float* scales[2];
 };
 
-// a token's place in the pool, (page, place in it) as page * page_size + place, or -1
-__device__ __forceinline__ int64_t place_of(const KvMove& a, int n) {
-  const int32_t b = a.seq[n], p = a.pos[n];
+// a token's row of its head 0 in the pool, or -1
+__device__ __forceinline__ int64_t row_of(const KvMove& a, int32_t b, int32_t p) {
   if (b < 0 || b >= a.B || p < 0) return -1;
-  const int32_t col = p / a.page;
+  const int32_t col = (int32_t)((uint32_t)p / (uint32_t)a.page);
   if (col >= a.max_pages) return -1;
   const int32_t id = a.table[(int64_t)b * a.max_pages + col];
   if (id < 0 || id >= a.pages) return -1;
-  return (int64_t)id * a.page + (p - col * a.page);
+  return (int64_t)id * a.heads * a.page + (p - col * a.page);
 }
 
 __device__ __forceinline__ void ld8(const uint16_t* p, float (&x)[8]) {
@@ -122,61 +121,101 @@ template <int TYPE> __device__ __forceinline__ void decode8(ku32x2_t q, float sc
   }
 }
 
-// row r: token r / (2 heads), then keys' heads, then values'
-template <typename TE, int TYPE, bool WRITE> __global__ __launch_bounds__(256) void kv_move_kernel(KvMove a) {
-  const int64_t r = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> a.lanes_log;
-  const int lane = threadIdx.x & ((1 << a.lanes_log) - 1), d = lane * 8;
-  const int64_t n = r / (2 * a.heads);
-  if (n >= a.N) return;
-  const int hh = (int)(r - n * (2 * a.heads)), of_v = hh >= a.heads, h = of_v ? hh - a.heads : hh;
+// A wave moves the same head of keys or of values of ROWS tokens to each of its groups of lanes, neighbours side by side: in the pool their
+// rows and their scales follow each other, and the loads of all are on their way together.
+template <typename TE, int TYPE, bool WRITE, int ROWS> __global__ __launch_bounds__(256) void kv_move_kernel(KvMove a) {
+  constexpr bool kCoded = TYPE == KC_INT8 || TYPE == KC_E4M3;
+  const int groups = 64 >> a.lanes_log, lane = threadIdx.x & ((1 << a.lanes_log) - 1), d = lane * 8;
+  const int quads = (2 * a.heads + 3) / 4, tile = blockIdx.x / quads, hh = (blockIdx.x - tile * quads) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (hh >= 2 * a.heads) return;
+  const int of_v = hh >= a.heads, h = of_v ? hh - a.heads : hh;
+  const int n0 = tile * (groups * ROWS) + ((threadIdx.x & 63) >> a.lanes_log);
   const bool here = d < a.D;
-  const int64_t place = place_of(a, (int)n);
-  const int64_t page = place / a.page;
-  const int64_t row = (page * a.heads + h) * a.page + (place - page * a.page);   // of the pool
-  float x[8] = {};
+  int32_t seq[ROWS], pos[ROWS];
+  float x[ROWS][8];
+  int64_t row[ROWS];
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {
+    const int n = n0 + i * groups, at = n < a.N ? n : a.N - 1;
+    seq[i] = a.seq[at];
+    pos[i] = a.pos[at];
+    if (n >= a.N) seq[i] = -1;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[i][e] = 0.f;
+    if constexpr (WRITE)
+      if (here) ld8(reinterpret_cast<const TE*>(a.src[of_v]) + at * a.ld[of_v] + h * a.D + d, x[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {
+    row[i] = row_of(a, seq[i], pos[i]);
+    if (row[i] >= 0) row[i] += (int64_t)h * a.page;
+  }
   if constexpr (WRITE) {
-    if (place < 0) return;
-    const TE* from = reinterpret_cast<const TE*>(a.src[of_v]) + n * a.ld[of_v] + h * a.D + d;
-    if (here) ld8(from, x);
-    if constexpr (TYPE == KC_F32 || TYPE == KC_BF16) {
-      if (here) st8(reinterpret_cast<TE*>(a.pool[of_v]) + row * a.D + d, x);
-    } else {
-      // the largest magnitude, as bits: a NaN's are above infinity's
-      uint32_t top = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint32_t m = __builtin_bit_cast(uint32_t, x[i]) & 0x7fffffffu;
-        top = m > top ? m : top;
-      }
-      for (int o = 1; o < 1 << a.lanes_log; o <<= 1) {
-        const uint32_t m = __shfl_xor(top, o, 64);
-        top = m > top ? m : top;
-      }
-      constexpr float kLargest = TYPE == KC_INT8 ? 127.f : 448.f;
-      const bool finite = top < 0x7f800000u;
-      const float scale = fmaxf(__builtin_bit_cast(float, top) / kLargest, 0x1p-120f), inv = finite ? 1.f / scale : 0.f;
-      if (!finite)
+    for (int i = 0; i < ROWS; ++i) {
+      if constexpr (!kCoded) {
+        if (here && row[i] >= 0) st8(reinterpret_cast<TE*>(a.pool[of_v]) + row[i] * a.D + d, x[i]);
+      } else {
+        // the largest magnitude, as bits: a NaN's are above infinity's
+        uint32_t top = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = 0.f;
-      if (here) *reinterpret_cast<ku32x2_t*>(reinterpret_cast<uint8_t*>(a.pool[of_v]) + row * a.D + d) = encode8<TYPE>(x, inv);
-      if (lane == 0) a.scales[of_v][row] = finite ? scale : __builtin_nanf("");
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t m = __builtin_bit_cast(uint32_t, x[i][e]) & 0x7fffffffu;
+          top = m > top ? m : top;
+        }
+        for (int o = 1; o < 1 << a.lanes_log; o <<= 1) {
+          const uint32_t m = __shfl_xor(top, o, 64);
+          top = m > top ? m : top;
+        }
+        constexpr float kLargest = TYPE == KC_INT8 ? 127.f : 448.f;
+        const bool finite = top < 0x7f800000u;
+        const float scale = fmaxf(__builtin_bit_cast(float, top) / kLargest, 0x1p-120f), inv = finite ? 1.f / scale : 0.f;
+        if (!finite)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[i][e] = 0.f;
+        if (row[i] >= 0) {
+          if (here) *reinterpret_cast<ku32x2_t*>(reinterpret_cast<uint8_t*>(a.pool[of_v]) + row[i] * a.D + d) = encode8<TYPE>(x[i], inv);
+          if (lane == 0) a.scales[of_v][row[i]] = finite ? scale : __builtin_nanf("");
+        }
+      }
     }
   } else {
-    if (!here) return;
-    if (place >= 0) {
-      if constexpr (TYPE == KC_F32 || TYPE == KC_BF16) ld8(reinterpret_cast<const TE*>(a.pool[of_v]) + row * a.D + d, x);
-      else decode8<TYPE>(*reinterpret_cast<const ku32x2_t*>(reinterpret_cast<const uint8_t*>(a.pool[of_v]) + row * a.D + d), a.scales[of_v][row], x);
+    ku32x2_t q[ROWS];
+    float scale[ROWS];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+      q[i] = ku32x2_t{0u, 0u};
+      scale[i] = 0.f;
+      if (here && row[i] >= 0) {
+        if constexpr (!kCoded) {
+          ld8(reinterpret_cast<const TE*>(a.pool[of_v]) + row[i] * a.D + d, x[i]);
+        } else {
+          q[i] = *reinterpret_cast<const ku32x2_t*>(reinterpret_cast<const uint8_t*>(a.pool[of_v]) + row[i] * a.D + d);
+          scale[i] = a.scales[of_v][row[i]];
+        }
+      }
     }
-    st8(reinterpret_cast<TE*>(a.dst[of_v]) + (n * a.heads + h) * a.D + d, x);
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+      const int n = n0 + i * groups;
+      if (!here || n >= a.N) continue;
+      if constexpr (kCoded) decode8<TYPE>(q[i], scale[i], x[i]);
+      st8(reinterpret_cast<TE*>(a.dst[of_v]) + ((int64_t)n * a.heads + h) * a.D + d, x[i]);
+    }
   }
 }
 
 template <bool WRITE> as_status move(const kc_cache* c, const KvMove& a, hipStream_t st) {
-  const int64_t rows = (int64_t)a.N * 2 * a.heads, per_block = 256 >> a.lanes_log, blocks = (rows + per_block - 1) / per_block;
+  // few tokens: as many lanes as there are rows
+  const int groups = 64 >> a.lanes_log, quads = (2 * a.heads + 3) / 4;
+  const bool few = (int64_t)a.N * quads <= (int64_t)groups * 1024;
+  const int64_t per_block = groups * (few ? 1 : 4), blocks = (a.N + per_block - 1) / per_block * quads;
   if (blocks >= (int64_t)1 << 24) return set_error(AS_ERR_SHAPE, "%d tokens of %d heads in one call", a.N, a.heads);
   auto run = [&](auto* t, auto type) {
     using TE = typename std::remove_pointer<decltype(t)>::type;
-    hipLaunchKernelGGL((kv_move_kernel<TE, decltype(type)::value, WRITE>), dim3((unsigned)blocks), dim3(256), 0, st, a);
+    constexpr int TYPE = decltype(type)::value;
+    if (few) hipLaunchKernelGGL((kv_move_kernel<TE, TYPE, WRITE, 1>), dim3((unsigned)blocks), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((kv_move_kernel<TE, TYPE, WRITE, 4>), dim3((unsigned)blocks), dim3(256), 0, st, a);
   };
   auto any = [&](auto* t, auto same) {
     if (c->cache_type == KC_INT8) run(t, std::integral_constant<int, KC_INT8>{});
