@@ -44,10 +44,11 @@ struct KvAttnDev {
   int32_t B, T, heads, G, D, R;        // R = T G rows of a head
   int32_t row_tiles, tile_waves, row_groups, group_rows;   // tiles of 16 rows; of a block (1, 2 or 4); groups of a block's tiles; rows of a group
   int32_t page, page_tiles, pages, max_pages, max_len, window;
-  uint32_t magic;                      // of page_tiles
+  KvMagic magic;                       // of page_tiles
   int32_t chunk;                       // tokens of a chunk
   int32_t split;                       // 0: a block per (sequence, head, row group), no second launch
-  float scale_log2;
+  float scale_log2;                    // its magnitude: a negative scale's sign goes into the queries
+  uint32_t q_sign;                     // exclusive-ored onto pairs of bf16 or onto floats
 };
 
 // ---- which tokens -----------------------------------------------------------------
@@ -65,51 +66,67 @@ __device__ __forceinline__ SeqSpan seq_span(const KvAttnDev& a, int b) {
   return s;
 }
 
-// Adds up the sequences' chunks (times the heads and row groups), a block's threads of them at a time; the same numbers in every block.
-template <int WAVES> __device__ __forceinline__ int32_t cut_total(const KvAttnDev& a, int32_t* s_sum) {
-  int32_t n = 0;
-  for (int b = threadIdx.x; b < a.B; b += WAVES * 64) n += seq_span(a, b).chunks;
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
-  if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = n;
-  __syncthreads();
-  n = 0;
-#pragma unroll
-  for (int w = 0; w < WAVES; ++w) n += s_sum[w];
-  return n * a.heads * a.row_groups;
-}
 __device__ __forceinline__ int32_t cut_per(int32_t total, int blocks) {
   const int32_t per = (total + blocks - 1) / blocks;
   return per < 1 ? 1 : per;
 }
-// the sequence of chunk `at` of all, and the chunks ahead of it
-template <int WAVES> __device__ __forceinline__ void cut_find(const KvAttnDev& a, int32_t at, int32_t* s_sum, int32_t* s_found, int32_t& b_out, int32_t& ahead_out) {
-  const int32_t hr = a.heads * a.row_groups;
-  int32_t carry = 0;
-  for (int b0 = 0; b0 < a.B; b0 += WAVES * 64) {
-    const int b = b0 + threadIdx.x;
-    const int32_t own = b < a.B ? seq_span(a, b).chunks * hr : 0;
-    int32_t run = own;
+// A block's run of all chunks (of the sequences, their heads and row groups): how many, the sequence of the first one, and the chunks ahead
+// of that sequence.  A block's threads take that many sequences at a time; more of them are gone through twice.
+struct Run {
+  int32_t left, at, b, ahead;
+};
+template <int WAVES> __device__ __forceinline__ Run cut_run(const KvAttnDev& a, int32_t* s_sum, int32_t* s_found) {
+  const int32_t hr = a.heads * a.row_groups, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  auto chunks_of = [&](int b) { return b < a.B ? seq_span(a, b).chunks * hr : 0; };
+  const int32_t first = chunks_of(threadIdx.x);
+  int32_t total = first;
+  for (int b = threadIdx.x + WAVES * 64; b < a.B; b += WAVES * 64) total += chunks_of(b);
+  int32_t own = first, run = first, carry = 0;
+  Run r;
+  for (int b0 = 0;; b0 += WAVES * 64) {
+    if (b0 > 0) run = own = chunks_of(b0 + threadIdx.x);
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
       const int32_t x = __shfl_up(run, o, 64);
-      if ((threadIdx.x & 63) >= o) run += x;
+      if (lane >= o) run += x;
+    }
+    if (b0 == 0) {
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
+    }
+    if (lane == 63) {
+      s_sum[wave] = run;
+      if (b0 == 0) s_sum[WAVES + wave] = total;
     }
     __syncthreads();
-    if ((threadIdx.x & 63) == 63) s_sum[threadIdx.x >> 6] = run;
-    __syncthreads();
-    for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) run += s_sum[w];
-    const int32_t ahead = carry + run - own;
-    if (at >= ahead && at < ahead + own) {
-      s_found[0] = b;
+    int32_t before = carry, here = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      const int32_t x = s_sum[w];
+      before += w < wave ? x : 0;
+      here += x;
+    }
+    if (b0 == 0) {
+      total = 0;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) total += s_sum[WAVES + w];
+      const int32_t per = cut_per(total, gridDim.x);
+      r.at = (int32_t)blockIdx.x * per;
+      r.left = total - r.at < per ? total - r.at : per;
+      if (r.left <= 0) return r;
+    }
+    const int32_t ahead = before + run - own;
+    if (r.at >= ahead && r.at < ahead + own) {
+      s_found[0] = b0 + threadIdx.x;
       s_found[1] = ahead;
     }
-    for (int w = 0; w < WAVES; ++w) carry += s_sum[w];
-    if (at < carry) break;
+    carry += here;
+    __syncthreads();
+    if (r.at < carry) break;
   }
-  __syncthreads();
-  b_out = s_found[0];
-  ahead_out = s_found[1];
+  r.b = s_found[0];
+  r.ahead = s_found[1];
+  return r;
 }
 
 // ---- fragments --------------------------------------------------------------------
@@ -131,8 +148,19 @@ template <int TYPE> __device__ __forceinline__ void codes_to_floats(uint32_t w, 
   }
 }
 
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t attn_rsrc(const void* base) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, 0x7fffffff, 0x00020000);
+// offsets from `bytes` on read as 0
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t attn_rsrc(const void* base, int32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, 0x00020000);
+}
+// the larger of a lane's and of those 16, 32 and 48 lanes away
+__device__ __forceinline__ float max_of_rows(float x) {
+  const uint32_t a = __builtin_bit_cast(uint32_t, x);
+  const auto p = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+  const uint32_t p0 = p[0], p1 = p[1];
+  const uint32_t c = __builtin_bit_cast(uint32_t, fmaxf(__builtin_bit_cast(float, p0), __builtin_bit_cast(float, p1)));
+  const auto q = __builtin_amdgcn_permlane32_swap(c, c, false, false);
+  const uint32_t q0 = q[0], q1 = q[1];
+  return fmaxf(__builtin_bit_cast(float, q0), __builtin_bit_cast(float, q1));
 }
 
 // What a cache type's tiles look like.  TYPE: kc_type, F32Q: queries and results are float, DP: the head's width up to which it serves.
@@ -150,6 +178,7 @@ template <int TYPE, bool F32Q, int DP> struct Form {
   static constexpr int kVW = kCoded ? kVAll : kF32 ? 4 : (kVAll < 8 ? kVAll : 8);
   static constexpr int kVHalves = kVAll / kVW;
   static constexpr int kVDwords = kVW * kBytes / 4;
+  static constexpr bool kCanBeOdd = TYPE != KC_INT8;                // values may be infinities or NaN
 };
 
 template <int N> __device__ __forceinline__ void buffer_load(__amdgpu_buffer_rsrc_t rs, uint32_t off, uint32_t (&x)[N]) {
@@ -168,33 +197,42 @@ template <int N> __device__ __forceinline__ void buffer_load(__amdgpu_buffer_rsr
 }
 
 // ---- the kernel -------------------------------------------------------------------
-template <class F> struct TileAt {
-  int32_t pos;      // first token
-  int32_t valid;    // tokens that there are: up to 16, 0 where there is no page
-};
-
 template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__((Form<TYPE, F32Q, DP>::kWaves * 64)) void kv_attn_kernel(KvAttnDev a) {
   using F = Form<TYPE, F32Q, DP>;
   constexpr int WAVES = F::kWaves;
   constexpr int NT = F::kTiles, NO = DP / 16, STEP = NT * kKvTile, LD = DP + 4;
   extern __shared__ float lds[];          // [waves][16 rows][LD], and their maxima and sums
   float* lds_ml = lds + WAVES * 16 * LD;
-  __shared__ int32_t s_sum[WAVES], s_found[2];
+  __shared__ int32_t s_sum[2 * WAVES], s_found[2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, g = lane >> 4;
   const int row_wave = wave % a.tile_waves, tok_wave = wave / a.tile_waves, tok_waves = WAVES / a.tile_waves;   // (some may be left over)
 
+  // a lane's part of a tile of K and of V; behind a row's end: out of every range
+  uint32_t k_off[F::kKLoads], v_off[4][F::kVHalves];
+#pragma unroll
+  for (int j = 0; j < F::kKLoads; ++j) {
+    const int d = (j * 4 + g) * F::kKElems;
+    k_off[j] = d < a.D ? (uint32_t)((c * a.D + d) * F::kBytes) : kAttnOob;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int h = 0; h < F::kVHalves; ++h) {
+      const int d = (h * 16 + c) * F::kVW;
+      v_off[i][h] = d < a.D ? (uint32_t)(((g * 4 + i) * a.D + d) * F::kBytes) : kAttnOob;
+    }
+
   // this block's run of chunks
   int32_t b, hr, chunk, left;             // sequence, (head, row group), first chunk there, chunks left
   if (a.split) {
-    const int32_t total = cut_total<WAVES>(a, s_sum), per = cut_per(total, gridDim.x), at = (int32_t)blockIdx.x * per;
-    if (at >= total) return;
-    left = total - at < per ? total - at : per;
-    int32_t ahead;
-    cut_find<WAVES>(a, at, s_sum, s_found, b, ahead);
+    const Run run = cut_run<WAVES>(a, s_sum, s_found);
+    if (run.left <= 0) return;
+    b = run.b;
+    left = run.left;
     const int32_t n = seq_span(a, b).chunks;
-    hr = (at - ahead) / n;
-    chunk = at - ahead - hr * n;
+    hr = (run.at - run.ahead) / n;
+    chunk = run.at - run.ahead - hr * n;
   } else {
     b = blockIdx.x / (a.heads * a.row_groups);
     hr = blockIdx.x - b * (a.heads * a.row_groups);
@@ -236,7 +274,10 @@ template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__((Form<TYPE, 
         f32x4_t v = {};
         if (row_there && d < a.D) v = *reinterpret_cast<const f32x4_t*>(reinterpret_cast<const float*>(a.q) + q_at + d);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) qf[j][i] = v[i];
+        for (int i = 0; i < 4; ++i) {
+          const float x = v[i];
+          qf[j][i] = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x) ^ a.q_sign);
+        }
       }
     } else {
 #pragma unroll
@@ -247,7 +288,7 @@ template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__((Form<TYPE, 
         if constexpr (!F32Q) {
           au32x4_t v = {};
           if (there) v = *reinterpret_cast<const au32x4_t*>(reinterpret_cast<const uint16_t*>(a.q) + q_at + d);
-          qb[0][j] = as_frag(v);
+          qb[0][j] = as_frag(v ^ a.q_sign);
         } else {
           float v[8] = {};
           if (there) {
@@ -257,7 +298,7 @@ template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__((Form<TYPE, 
           }
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            float rest = v[i];
+            float rest = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, v[i]) ^ a.q_sign);
 #pragma unroll
             for (int s = 0; s < F::kQTerms; ++s) {
               const bf16_t x = (bf16_t)rest;
@@ -274,65 +315,49 @@ template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__((Form<TYPE, 
 
     uint32_t kr[NT][F::kKLoads][4], vr[NT][4][F::kVHalves][F::kVDwords];
     float ks[NT][4], vs[NT][4];
-    TileAt<F> at_k[NT], at_v[NT];
-    const int64_t head_bytes = (int64_t)a.page * a.D * F::kBytes;
-    auto page_of = [&](int32_t pos) {     // the table's entry for the tile at pos (any tile of the sequence's)
-      if (pos >= len) pos = len - 1;
-      const uint32_t tile = (uint32_t)pos >> 4, col = a.page_tiles == 1 ? tile : __umulhi(tile, a.magic);
-      return __builtin_amdgcn_readfirstlane(a.table[(int64_t)b * a.max_pages + col]);
+    int32_t k_valid[NT];                  // tokens that there are of a tile: up to 16, 0 where there is no page
+    const int32_t row_bytes = a.D * F::kBytes;
+    const int32_t* table = a.table + (int64_t)b * a.max_pages;
+    // the table's entry for the tile at pos (past the end: the last one)
+    auto page_of = [&](int32_t pos) {
+      const uint32_t tile = (uint32_t)(pos < len ? pos : len - 1) >> 4, col = kv_div(tile, a.magic);
+      return __builtin_amdgcn_readfirstlane(table[col]);
     };
-    auto place = [&](int32_t pos, int32_t id, int64_t& row_of_pool) {
-      TileAt<F> at;
-      at.pos = pos;
-      const int32_t n = tok1 - pos;
-      at.valid = n < 0 ? 0 : n < kKvTile ? n : kKvTile;
-      const uint32_t tile = (uint32_t)pos >> 4, col = a.page_tiles == 1 ? tile : __umulhi(tile, a.magic);
-      if (id < 0 || id >= a.pages) {
-        at.valid = 0;
-        id = 0;
-      }
-      row_of_pool = ((int64_t)id * a.heads + head) * a.page + (int32_t)(tile - col * a.page_tiles) * kKvTile;
-      return at;
+    // the tile's first row in the pool, and how many of its tokens there are
+    auto place = [&](int32_t pos, int32_t id, int32_t& valid) {
+      const uint32_t tile = (uint32_t)pos >> 4, col = kv_div(tile, a.magic);
+      const bool there = (uint32_t)id < (uint32_t)a.pages;
+      const int32_t n = there ? tok1 - pos : 0;
+      valid = n < 0 ? 0 : n < kKvTile ? n : kKvTile;
+      return (int64_t)((there ? id : 0) * a.heads + head) * a.page + (int32_t)(tile - col * a.page_tiles) * kKvTile;
     };
+    int64_t at_row[NT];                   // of the tiles whose keys were asked for last
     auto load_k = [&](int32_t pos, const int32_t (&id)[NT]) {
 #pragma unroll
       for (int u = 0; u < NT; ++u) {
-        int64_t r;
-        at_k[u] = place(pos + u * kKvTile, id[u], r);
-        const auto rs = attn_rsrc(reinterpret_cast<const uint8_t*>(a.k_pages) + r * a.D * F::kBytes);
-        const uint32_t off = c < at_k[u].valid ? (uint32_t)(c * a.D * F::kBytes) : kAttnOob;
+        at_row[u] = place(pos + u * kKvTile, id[u], k_valid[u]);
+        const auto rs = attn_rsrc(reinterpret_cast<const uint8_t*>(a.k_pages) + at_row[u] * row_bytes, k_valid[u] * row_bytes);
 #pragma unroll
-        for (int j = 0; j < F::kKLoads; ++j) {
-          const int d = (j * 4 + g) * F::kKElems;
-          buffer_load(rs, d < a.D ? off + d * F::kBytes : kAttnOob, kr[u][j]);
-        }
+        for (int j = 0; j < F::kKLoads; ++j) buffer_load(rs, k_off[j], kr[u][j]);
         if constexpr (F::kCoded) {
           uint32_t x[4];
-          buffer_load(attn_rsrc(a.k_scales + r), at_k[u].valid > 4 * g ? g * 16u : kAttnOob, x);
+          buffer_load(attn_rsrc(a.k_scales + at_row[u], (k_valid[u] + 3) / 4 * 16), g * 16u, x);
 #pragma unroll
           for (int i = 0; i < 4; ++i) ks[u][i] = __builtin_bit_cast(float, x[i]);
         }
       }
     };
-    auto load_v = [&](int32_t pos, const int32_t (&id)[NT]) {
+    auto load_v = [&]() {                 // of the same tiles
 #pragma unroll
       for (int u = 0; u < NT; ++u) {
-        int64_t r;
-        at_v[u] = place(pos + u * kKvTile, id[u], r);
-        const auto rs = attn_rsrc(reinterpret_cast<const uint8_t*>(a.v_pages) + r * a.D * F::kBytes);
+        const auto rs = attn_rsrc(reinterpret_cast<const uint8_t*>(a.v_pages) + at_row[u] * row_bytes, k_valid[u] * row_bytes);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int tok = g * 4 + i;
-          const uint32_t off = tok < at_v[u].valid ? (uint32_t)(tok * a.D * F::kBytes) : kAttnOob;
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int h = 0; h < F::kVHalves; ++h) {
-            const int d = (h * 16 + c) * F::kVW;
-            buffer_load(rs, d < a.D ? off + d * F::kBytes : kAttnOob, vr[u][i][h]);
-          }
-        }
+          for (int h = 0; h < F::kVHalves; ++h) buffer_load(rs, v_off[i][h], vr[u][i][h]);
         if constexpr (F::kCoded) {
           uint32_t x[4];
-          buffer_load(attn_rsrc(a.v_scales + r), at_v[u].valid > 4 * g ? g * 16u : kAttnOob, x);
+          buffer_load(attn_rsrc(a.v_scales + at_row[u], (k_valid[u] + 3) / 4 * 16), g * 16u, x);
 #pragma unroll
           for (int i = 0; i < 4; ++i) vs[u][i] = __builtin_bit_cast(float, x[i]);
         }
@@ -419,7 +444,7 @@ template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__((Form<TYPE, 
 #pragma unroll
       for (int u = 0; u < NT; ++u) id[u] = page_of(pos + u * kKvTile);
       load_k(pos, id);
-      load_v(pos, id);
+      load_v();
 #pragma unroll
       for (int u = 0; u < NT; ++u) id_next[u] = page_of(pos + stride + u * kKvTile);
       for (; pos < tok1; pos += stride) {
@@ -454,25 +479,26 @@ template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__((Form<TYPE, 
             }
           }
         }
+        // scores, in units of which scale_log2 makes powers of two
         float p[NT][4];
 #pragma unroll
         for (int u = 0; u < NT; ++u)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            p[u][i] = s[u][i] * a.scale_log2;
+            p[u][i] = s[u][i];
             if constexpr (F::kCoded) p[u][i] *= ks[u][i];
           }
         // a step that not all rows see all of
         bool part = pos < all_lo || pos + STEP - 1 > all_hi;
 #pragma unroll
-        for (int u = 0; u < NT; ++u) part |= at_k[u].valid < kKvTile;
+        for (int u = 0; u < NT; ++u) part |= k_valid[u] < kKvTile;
         if (part) {
 #pragma unroll
           for (int u = 0; u < NT; ++u)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const int32_t x = at_k[u].pos + 4 * g + i;
-              if (x < lo || x > hi || 4 * g + i >= at_k[u].valid) p[u][i] = -INFINITY;
+              const int32_t x = pos + u * kKvTile + 4 * g + i;
+              if (x < lo || x > hi || 4 * g + i >= k_valid[u]) p[u][i] = -INFINITY;
             }
         }
         // the next step's keys, into the registers that have been read
@@ -488,28 +514,30 @@ template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__((Form<TYPE, 
         for (int u = 0; u < NT; ++u)
 #pragma unroll
           for (int i = 0; i < 4; ++i) top = fmaxf(top, p[u][i]);
-        top = fmaxf(top, __shfl_xor(top, 16, 64));
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
-        const float m_new = fmaxf(m, top), m_use = m_new == -INFINITY ? 0.f : m_new;
-        if (__any(m_new > m)) {
-          const float f = __builtin_amdgcn_exp2f(m - m_use);
-          l *= f;
+        // The maximum that weights are relative to may lag behind the true one by a factor of 2^8, which floats do not mind: it moves less often.
+        const float seen_top = max_of_rows(top) * a.scale_log2;
+        if (__any(seen_top > m + 8.f)) {
+          const float m_new = fmaxf(m, seen_top), f = __builtin_amdgcn_exp2f(m - m_new);   // (seen_top > -inf somewhere: other rows may have none yet)
+          const float by = m_new == -INFINITY ? 1.f : f;
+          l *= by;
 #pragma unroll
-          for (int j = 0; j < NO; ++j) o[j] *= f;
+          for (int j = 0; j < NO; ++j) o[j] *= by;
+          m = m_new;
         }
-        m = m_new;
+        const float m_use = m == -INFINITY ? 0.f : m;
 #pragma unroll
         for (int u = 0; u < NT; ++u)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const bool seen = p[u][i] != -INFINITY;
-            p[u][i] = __builtin_amdgcn_exp2f(p[u][i] - m_use);
+            const float w = __builtin_amdgcn_exp2f(fmaf(p[u][i], a.scale_log2, -m_use));
+            p[u][i] = part && !seen ? 0.f : w;
             l += p[u][i];
-            if constexpr (F::kCoded) p[u][i] = seen ? p[u][i] * vs[u][i] : 0.f;
+            if constexpr (F::kCoded) p[u][i] = part && !seen ? 0.f : p[u][i] * vs[u][i];
           }
         // Values that only some rows see must not reach the others, whatever they are: 0 times an infinity or a NaN is a NaN.
         bool odd = false;
-        if (part) {
+        if (part && F::kCanBeOdd) {
           uint32_t x = 0;
 #pragma unroll
           for (int u = 0; u < NT; ++u)
@@ -526,9 +554,9 @@ template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__((Form<TYPE, 
                 }
           odd = __any(x != 0);
         }
-        if (!odd) {
+        if (!F::kCanBeOdd || !odd) {
           times_v(std::false_type{}, p, 0u, false);
-        } else {
+        } else if constexpr (F::kCanBeOdd) {
           const int t0 = row0 / a.G, t1 = (row0 + 15) / a.G;
           for (int tt = t0; tt <= t1 && tt < a.T; ++tt) {
             const int32_t hi_t = len - a.T + tt, lo_t = a.window > 0 ? hi_t - a.window + 1 : 0;
@@ -537,13 +565,13 @@ template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__((Form<TYPE, 
             for (int u = 0; u < NT; ++u)
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
-                const int32_t x = at_v[u].pos + 4 * g + i;
+                const int32_t x = pos + u * kKvTile + 4 * g + i;
                 in |= (uint32_t)(x >= lo_t && x <= hi_t) << (u * 4 + i);
               }
             times_v(std::true_type{}, p, in, row_there && t == tt);
           }
         }
-        load_v(pos + stride, id_cur);
+        load_v();
       }
     }
 
@@ -807,7 +835,8 @@ extern "C" as_status kv_cache_attn(const kc_cache* cache, const kc_attn* attn, c
   a.magic = kv_magic((uint32_t)a.page_tiles);
   a.chunk = p.chunk;
   a.split = p.split;
-  a.scale_log2 = attn->scale * 1.4426950408889634f;
+  a.scale_log2 = std::fabs(attn->scale) * 1.4426950408889634f;
+  a.q_sign = attn->scale < 0 ? f32 ? 0x80000000u : 0x80008000u : 0u;
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   hipError_t e;
   switch (cache->cache_type) {
