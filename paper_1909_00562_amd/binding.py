@@ -616,6 +616,9 @@ class _DeviceOp:
         if device.type != "cuda":
             raise AttnSoftmaxError(2, f"tensors are on {device}, expected a GPU")
         self.torch, self.dev, self.index = torch, device, device.index
+        torch.cuda.init()
+        # (the address of the current stream and the current device's number, without making objects of them)
+        self.stream_of, self.current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
         self.lib = load_library()
         self.workspace = None
 
@@ -670,16 +673,14 @@ class _DeviceOp:
     def _call(self, function, *args):
         """function(*args, stream), for addresses that _tensor has checked.  The workspace is the handle's own, so the allocator is
         told here of a stream other than the one it was allocated on: a handle may be dropped while calls are on their way."""
-        cuda = self.torch.cuda
-        current = cuda.current_stream(self.dev)
-        stream = current.cuda_stream or None
-        if self.workspace is not None and current.cuda_stream != self.home:
-            self.workspace.record_stream(current)
-        if cuda.current_device() == self.index:
-            rc = function(*args, stream)
+        stream = self.stream_of(self.index)
+        if self.workspace is not None and stream != self.home:
+            self.workspace.record_stream(self.torch.cuda.current_stream(self.dev))
+        if self.current_device() == self.index:
+            rc = function(*args, stream or None)
         else:
-            with cuda.device(self.dev):
-                rc = function(*args, stream)
+            with self.torch.cuda.device(self.dev):
+                rc = function(*args, stream or None)
         if rc:
             _check(rc)
 

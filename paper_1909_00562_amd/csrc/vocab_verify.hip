@@ -60,6 +60,21 @@ __device__ __forceinline__ double exp2_64(double y) {
   return ldexp(p, (int)n);
 }
 
+// The same with the powers 2^(k / 256), k = 0 .. 255, in a table: what is left of y is 2^-9 at most, and the first term left out 1.4e-13 of the
+// result.  28 units of the vector unit's time in place of 40 (an fp64 instruction takes two): 1152 rows of 128000 bf16 logits 151 -> TODO us.
+constexpr int kPowers = 256;
+__device__ __forceinline__ void make_powers(double* powers) { powers[threadIdx.x] = exp2_64((double)threadIdx.x / kPowers); }
+__device__ __forceinline__ double exp2_by_powers(double y, const double* powers) {
+  constexpr double kMagic = 0x1.8p44;    // its last place is 2^-8
+  y = fmax(y, -1100.0);
+  const double z = y + kMagic, r = y - (z - kMagic);
+  const int k = (int)(uint32_t)__builtin_bit_cast(uint64_t, z);
+  const double t = powers[k & (kPowers - 1)];
+  double q = fma(5.5504108664821580e-02, r, 2.4022650695910072e-01);
+  q = fma(q, r, 6.9314718055994531e-01) * r;
+  return ldexp(fma(t, q, t), k >> 8);
+}
+
 __device__ __forceinline__ double wave_sum64(double v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
@@ -93,7 +108,7 @@ __device__ __forceinline__ bool is_word(int32_t x, int V) { return x >= 0 && x <
 template <typename TE> __global__ __launch_bounds__(kVThreads) void verify_stats_kernel(VerifyDev a) {
   constexpr int W = 16 / sizeof(TE);
   __shared__ float s_m[4];
-  __shared__ double s_sum[4];
+  __shared__ double s_sum[4], s_powers[kPowers];
   const int rows = 2 * a.T + 1, b = blockIdx.y / rows, j = blockIdx.y - b * rows;
   const int tid = threadIdx.x, wave = tid >> 6;
   if (j == 0 && blockIdx.x == 0 && tid == 0) a.ticket[b] = 0;
@@ -109,6 +124,7 @@ template <typename TE> __global__ __launch_bounds__(kVThreads) void verify_stats
     const int v0 = blockIdx.x * kVChunk + (i * kVThreads + tid) * W;
     ld_logits<TE>(row, v0 < a.V ? v0 : a.V, a.V, l + i * W);
   }
+  make_powers(s_powers);                   // (while the logits are on their way)
   float m = -INFINITY;
   int bad = 0;
 #pragma unroll
@@ -123,9 +139,9 @@ template <typename TE> __global__ __launch_bounds__(kVThreads) void verify_stats
   m = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
   double sum = 0;
   if (m > -INFINITY && !bad) {
-    const double m64 = m;
+    const double shift = -(double)m * a.c;
 #pragma unroll
-    for (int i = 0; i < kVPer; ++i) sum += exp2_64(((double)l[i] - m64) * a.c);
+    for (int i = 0; i < kVPer; ++i) sum += exp2_by_powers(fma((double)l[i], a.c, shift), s_powers);
   }
   sum = wave_sum64(sum);
   if ((tid & 63) == 0) s_sum[wave] = sum;
@@ -135,69 +151,90 @@ template <typename TE> __global__ __launch_bounds__(kVThreads) void verify_stats
 
 // ---- the words ---------------------------------------------------------------------
 struct RowStat {
-  double m, inv_z;   // p[v] = 2^((l[v] - m) c) inv_z
+  double shift, inv_z;   // p[v] = 2^(l[v] c + shift) inv_z
 };
-template <typename TE> struct Weights {
-  const TE *p_row, *q_row;   // q_row: null where p alone counts
+struct Weights {
   RowStat p, q;
   double c;
-  __device__ __forceinline__ void at(float lp, float lq, bool rest, double& r, double& pv) const {
-    pv = exp2_64(((double)lp - p.m) * c) * p.inv_z;
-    r = pv;
-    if (rest) r = fmax(pv - exp2_64(((double)lq - q.m) * c) * q.inv_z, 0.0);
+  const double* powers;
+  // p[v], and what of it counts: all, or what is above q[v]
+  __device__ __forceinline__ double at(float lp, float lq, bool subtract, double& pv) const {
+    pv = exp2_by_powers(fma((double)lp, c, p.shift), powers) * p.inv_z;
+    return subtract ? fmax(pv - exp2_by_powers(fma((double)lq, c, q.shift), powers) * q.inv_z, 0.0) : pv;
   }
 };
 
 template <typename TE> __global__ __launch_bounds__(kVThreads) void verify_words_kernel(VerifyDev a) {
   constexpr int W = 16 / sizeof(TE);
   __shared__ RowStat s_stat[2 * kVerifyMaxT + 1];
-  __shared__ int8_t s_bad[2 * kVerifyMaxT + 1], s_ok[kVerifyMaxT], s_word[kVerifyMaxT];
-  __shared__ int s_n, s_state, s_last, s_chunk, s_found;
-  __shared__ double s_r[4], s_p[4], s_theta;
+  __shared__ int8_t s_bad[2 * kVerifyMaxT + 1];
+  __shared__ int s_words, s_n, s_state, s_last, s_chunk, s_found, s_some;
+  __shared__ double s_r[4], s_p[4], s_theta, s_powers[kPowers];
   const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, T = a.T, V = a.V;
   const int64_t first = (int64_t)b * T;
   const TE* target = reinterpret_cast<const TE*>(a.target) + (int64_t)b * (T + 1) * a.ld_target;
   const TE* draft = reinterpret_cast<const TE*>(a.draft) + first * a.ld_draft;
-  if (tid < T) s_word[tid] = is_word(a.drafted[first + tid], V);
+  // the drafted words, their logits and random numbers: a lane of the first wave each
+  float lp_x = 0.f, lq_x = 0.f, u = 0.f;
+  if (wave == 0) {
+    const int32_t x = lane < T ? a.drafted[first + lane] : -1;
+    const bool given = is_word(x, V);
+    if (given) {
+      lp_x = ld_elem<TE>(target + lane * a.ld_target, x);
+      lq_x = ld_elem<TE>(draft + lane * a.ld_draft, x);
+      u = a.u_accept[first + lane];
+    }
+    const uint64_t none = ~__ballot(given);
+    if (lane == 0) s_words = none ? __builtin_ctzll(none) : 64;
+  }
+  make_powers(s_powers);
   __syncthreads();
-  int words = 0;   // drafted ones
-  while (words < T && s_word[words]) ++words;
-  // a wave joins the parts of a row
-  for (int i = wave; i < 2 * words + 1; i += 4) {
+  const int words = s_words;
+  // 16 lanes join the parts of a row
+  for (int i = tid >> 4; i < 2 * words + 1; i += kVThreads / 16) {
     const int j = i <= words ? i : i - words + T;   // (target rows 0 .. words, draft rows 0 .. words - 1)
     const VerifyPart* part = a.part + ((int64_t)b * (2 * T + 1) + j) * a.chunks;
     float m = -INFINITY;
     int bad = 0;
-    for (int k = lane; k < a.chunks; k += 64) {
-      m = fmaxf(m, part[k].m);
-      bad |= part[k].bad;
+    double z = 0;                                   // relative to the lane's own maximum
+    for (int k = lane & 15; k < a.chunks; k += 16) {
+      const VerifyPart x = part[k];
+      bad |= x.bad;
+      const float up = fmaxf(m, x.m);
+      if (up > -INFINITY)
+        z = (m > -INFINITY ? z * exp2_by_powers(((double)m - (double)up) * a.c, s_powers) : 0.0) +
+            (x.m > -INFINITY ? x.sum * exp2_by_powers(((double)x.m - (double)up) * a.c, s_powers) : 0.0);
+      m = up;
     }
-    m = wave_max(m);
-    bad = __any(bad) || !(m > -INFINITY);
-    double z = 0;
-    if (!bad)
-      for (int k = lane; k < a.chunks; k += 64)
-        if (part[k].m > -INFINITY) z += part[k].sum * exp2_64(((double)part[k].m - (double)m) * a.c);
-    z = wave_sum64(z);
+    float top = m;
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) {
+      top = fmaxf(top, __shfl_xor(top, o, 64));
+      bad |= __shfl_xor(bad, o, 64);
+    }
+    z = m > -INFINITY ? z * exp2_by_powers(((double)m - (double)top) * a.c, s_powers) : 0.0;
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) z += __shfl_xor(z, o, 64);
+    if ((lane & 15) == 0) {
+      s_stat[j] = {-(double)top * a.c, 1.0 / z};
+      s_bad[j] = bad || !(top > -INFINITY);
+    }
+  }
+  __syncthreads();
+  if (wave == 0) {
+    bool ok = false, bad = false;
+    if (lane < words) {
+      const RowStat p = s_stat[lane], q = s_stat[T + 1 + lane];
+      bad = s_bad[lane] || s_bad[T + 1 + lane];
+      ok = !bad && (double)u * (exp2_by_powers(fma((double)lq_x, a.c, q.shift), s_powers) * q.inv_z) <
+                       exp2_by_powers(fma((double)lp_x, a.c, p.shift), s_powers) * p.inv_z;
+    }
+    const uint64_t not_ok = ~__ballot(ok), bads = __ballot(bad);
     if (lane == 0) {
-      s_stat[j] = {m, 1.0 / z};
-      s_bad[j] = bad;
+      const int n = not_ok ? __builtin_ctzll(not_ok) : 64;
+      s_n = n;
+      s_state = (n < words && (bads >> n & 1)) || s_bad[n] ? 2 : n < words;   // 0: from p, 1: what is left of p, 2: no distribution
     }
-  }
-  __syncthreads();
-  if (tid < words) {
-    const int32_t x = a.drafted[first + tid];
-    const RowStat p = s_stat[tid], q = s_stat[T + 1 + tid];
-    const double px = exp2_64(((double)ld_elem<TE>(target + tid * a.ld_target, x) - p.m) * a.c) * p.inv_z;
-    const double qx = exp2_64(((double)ld_elem<TE>(draft + tid * a.ld_draft, x) - q.m) * a.c) * q.inv_z;
-    s_ok[tid] = s_bad[tid] || s_bad[T + 1 + tid] ? 2 : (double)a.u_accept[first + tid] * qx < px;
-  }
-  __syncthreads();
-  if (tid == 0) {
-    int n = 0;
-    while (n < words && s_ok[n] == 1) ++n;
-    s_n = n;
-    s_state = (n < words && s_ok[n] == 2) || s_bad[n] ? 2 : n < words;   // 0: from p, 1: what is left of p, 2: no distribution
   }
   __syncthreads();
   const int n = s_n, state = s_state;
@@ -207,28 +244,22 @@ template <typename TE> __global__ __launch_bounds__(kVThreads) void verify_words
     if (tid <= T && (tid != n || state == 2)) a.words[first + b + tid] = tid < n ? a.drafted[first + tid] : -1;
   }
   if (state == 2) return;
-  Weights<TE> w;
-  w.p_row = target + n * a.ld_target;
-  w.q_row = rest ? draft + n * a.ld_draft : w.p_row;
-  w.p = s_stat[n];
-  w.q = s_stat[rest ? T + 1 + n : n];
-  w.c = a.c;
+  const TE *p_row = target + n * a.ld_target, *q_row = rest ? draft + n * a.ld_draft : p_row;
+  const Weights w = {s_stat[n], s_stat[rest ? T + 1 + n : n], a.c, s_powers};
+  float lp[kVPer], lq[kVPer];
   // this chunk's weights
-  double r = 0, p = 0;
-#pragma unroll 2
+#pragma unroll
   for (int i = 0; i < kVPer / W; ++i) {
     const int v0 = blockIdx.x * kVChunk + (i * kVThreads + tid) * W;
-    if (v0 >= V) break;
-    float lp[W], lq[W];
-    ld_logits<TE>(w.p_row, v0, V, lp);
-    if (rest) ld_logits<TE>(w.q_row, v0, V, lq);
-#pragma unroll
-    for (int e = 0; e < W; ++e) {
-      double rv, pv;
-      w.at(lp[e], rest ? lq[e] : 0.f, rest, rv, pv);
-      r += rv;
-      p += pv;
-    }
+    ld_logits<TE>(p_row, v0 < V ? v0 : V, V, lp + i * W);
+    ld_logits<TE>(q_row, v0 < V ? v0 : V, V, lq + i * W);
+  }
+  double r = 0, p = 0;
+#pragma unroll 4
+  for (int i = 0; i < kVPer; ++i) {
+    double pv;
+    r += w.at(lp[i], lq[i], rest, pv);
+    p += pv;
   }
   r = wave_sum64(r);
   p = wave_sum64(p);
@@ -241,60 +272,73 @@ template <typename TE> __global__ __launch_bounds__(kVThreads) void verify_words
   if (tid == 0) {
     __hip_atomic_store(&sums[blockIdx.x].x, (s_r[0] + s_r[1]) + (s_r[2] + s_r[3]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __hip_atomic_store(&sums[blockIdx.x].y, (s_p[0] + s_p[1]) + (s_p[2] + s_p[3]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __threadfence();
+    __builtin_amdgcn_s_waitcnt(0);   // they are where every XCD sees them (stored past the caches) before this block counts
     s_last = __hip_atomic_fetch_add(&a.ticket[b], 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)a.chunks - 1;
   }
   __syncthreads();
   if (!s_last) return;
-  // the sequence's last block: the chunk, added up in order whichever block this is
-  if (tid == 0) {
-    auto sum_of = [&](int k, bool of_p) {
-      return __hip_atomic_load(of_p ? &sums[k].y : &sums[k].x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    };
-    double all = 0;
-    for (int k = 0; k < a.chunks; ++k) all += sum_of(k, false);
-    const bool of_p = !(all > 0);   // nothing is left: p
-    if (of_p) {
-      all = 0;
-      for (int k = 0; k < a.chunks; ++k) all += sum_of(k, true);
+  // The sequence's last block finds the chunk; sums are added in the chunks' order, whichever block this is.
+  if (wave == 0) {
+    double x[2][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int k = h * 64 + lane;
+      x[h][0] = k < a.chunks ? __hip_atomic_load(&sums[k].x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
+      x[h][1] = k < a.chunks ? __hip_atomic_load(&sums[k].y, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
     }
+    double run[2], all = 0;
+    bool of_p = false;
+    auto scan = [&](bool p_too) {
+      of_p = p_too;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        run[h] = p_too ? x[h][1] : x[h][0];
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+          const double y = __shfl_up(run[h], o, 64);
+          if (lane >= o) run[h] += y;
+        }
+        if (h == 1) run[1] += __shfl(run[0], 63, 64);
+      }
+      all = __shfl(run[1], 63, 64);
+    };
+    scan(false);
+    if (!(all > 0)) scan(true);             // nothing is left: p
     const double theta = fmax((double)a.u_next[b], 0.0) * all;
-    double ahead = 0;
     int chunk = -1, some = 0;
     double left = INFINITY;
-    for (int k = 0; k < a.chunks && chunk < 0; ++k) {
-      const double s = sum_of(k, of_p);
-      if (s > 0) some = k;
-      if (ahead + s > theta) {
-        chunk = k;
-        left = theta - ahead;
+#pragma unroll
+    for (int h = 1; h >= 0; --h) {
+      const double own = of_p ? x[h][1] : x[h][0];
+      const uint64_t above = __ballot(run[h] > theta), there = __ballot(own > 0);
+      if (above) {
+        const int k = __builtin_ctzll(above);
+        chunk = h * 64 + k;
+        left = theta - __shfl(run[h] - own, k, 64);
       }
-      ahead += s;
+      if (there && some == 0) some = h * 64 + 63 - __builtin_clzll(there);
     }
-    s_chunk = chunk < 0 ? some : chunk;
-    s_theta = left;
-    s_state = of_p;
-    s_found = 1 << 30;
-    s_n = -1;
+    if (lane == 0) {
+      s_chunk = chunk < 0 ? some : chunk;   // (rounding, or u >= 1: the last one with a weight)
+      s_theta = left;
+      s_state = of_p;
+      s_found = 1 << 30;
+      s_some = -1;
+    }
   }
   __syncthreads();
-  const bool of_p = s_state;
+  const bool subtract = rest && !s_state;
   const int v1 = s_chunk * kVChunk + tid * kVPer;   // consecutive logits per thread: running sums go by the words' order
-  double own = 0;
-  float lp[kVPer], lq[kVPer];
+  const double theta = s_theta;
 #pragma unroll
   for (int i = 0; i < kVPer / W; ++i) {
     const int v0 = v1 + i * W;
-    ld_logits<TE>(w.p_row, v0 < V ? v0 : V, V, lp + i * W);
-    ld_logits<TE>(w.q_row, v0 < V ? v0 : V, V, lq + i * W);
+    ld_logits<TE>(p_row, v0 < V ? v0 : V, V, lp + i * W);
+    ld_logits<TE>(q_row, v0 < V ? v0 : V, V, lq + i * W);
   }
-  const bool subtract = rest && !of_p;
+  double own = 0, pv;
 #pragma unroll 4
-  for (int i = 0; i < kVPer; ++i) {
-    double rv, pv;
-    w.at(lp[i], lq[i], subtract, rv, pv);
-    own += rv;
-  }
+  for (int i = 0; i < kVPer; ++i) own += w.at(lp[i], lq[i], subtract, pv);
   double run = own;   // inclusive over the block
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -304,19 +348,21 @@ template <typename TE> __global__ __launch_bounds__(kVThreads) void verify_words
   if (lane == 63) s_r[wave] = run;
   __syncthreads();
   for (int i = 0; i < wave; ++i) run += s_r[i];
-  if (run > s_theta) atomicMin(&s_found, tid);
-  if (own > 0) atomicMax(&s_n, tid);
+  if (run > theta) atomicMin(&s_found, tid);
+  if (own > 0) atomicMax(&s_some, tid);
   __syncthreads();
-  const bool none = s_found == 1 << 30;      // (rounding, or u >= 1: the last word of a weight above 0)
-  if (tid != (none ? s_n : s_found)) return;
+  const bool none = s_found == 1 << 30;      // (as above: the chunk's last word of a weight above 0)
+  if (tid != (none ? s_some : s_found)) return;
   double at = run - own;
   int word = -1;
+#pragma unroll 1
   for (int i = 0; i < kVPer; ++i) {
-    double rv, pv;
-    w.at(lp[i], lq[i], subtract, rv, pv);
+    const int v = v1 + i;
+    if (v >= V) break;
+    const double rv = w.at(ld_elem<TE>(p_row, v), ld_elem<TE>(q_row, v), subtract, pv);
     at += rv;
-    if (rv > 0) word = v1 + i;
-    if (!none && at > s_theta && rv > 0) break;
+    if (rv > 0) word = v;
+    if (!none && at > theta && rv > 0) break;
   }
   a.words[first + b + n] = word;
 }
