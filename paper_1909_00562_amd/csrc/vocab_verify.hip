@@ -4,13 +4,14 @@
 // in 64 bits: with 128000 borders, each off by 1e-8 as in fp32, one draw in a thousand would go to another word.  fp64 additions and
 // multiplications run at fp32's rate here.
 // Two launches.  The first one reads all rows once, a chunk of a row per block: its maximum and the sum of exp relative to it.  In
-// the second every block of a sequence joins those, finds how many words are accepted, and adds up the weights max(p - q, 0) of its
-// chunk; the sequence's last block to arrive finds the chunk in which u times the sum lies, and in it the word.
+// the second every block of a sequence joins those, finds how many words are accepted, and, where one was refused, adds up the weights
+// max(p - q, 0) of its chunk; the sequence's last block to arrive finds the chunk in which u times the sum lies, and in it the word.
 #include "../../include/vocab_ops.h"
 
 #include <hip/hip_runtime.h>
 
 #include <cmath>
+#include <type_traits>
 
 #include "common.h"
 #include "status.h"
@@ -20,8 +21,9 @@ namespace {
 
 typedef uint32_t vu32x4_t __attribute__((ext_vector_type(4)));
 
-constexpr int kVThreads = 256, kVPer = 32, kVChunk = kVThreads * kVPer;   // logits of a thread and of a block
-constexpr int kVerifyMaxT = 64;
+constexpr int kVThreads = 256, kVerifyMaxT = 64;
+// Logits of a thread: a block's chunk of a row is 256 times that.  Fewer where the blocks would not fill the chip: see verify_layout.
+constexpr int kManyPer = 32, kFewPer = 8, kMostChunks = 128;   // (two to a lane of the wave that scans their sums)
 
 struct VerifyPart {
   double sum;    // of 2^((l - m) c)
@@ -35,7 +37,7 @@ struct VerifyDev {
   const float *u_accept, *u_next;
   int32_t *n_accepted, *words;
   VerifyPart* part;    // [B][2T+1][chunks]: T+1 rows of the target, T of the draft
-  double2* sums;       // [B][chunks]: of max(p - q, 0), of p
+  double* sums;        // [B][chunks]: of max(p - q, 0)
   uint32_t* ticket;    // [B]
   int32_t B, T, V, chunks;
   double c;            // log2(e) / tau
@@ -61,12 +63,16 @@ __device__ __forceinline__ double exp2_64(double y) {
 }
 
 // The same with the powers 2^(k / 256), k = 0 .. 255, in a table: what is left of y is 2^-9 at most, and the first term left out 1.4e-13 of the
-// result.  28 units of the vector unit's time in place of 40 (an fp64 instruction takes two): 1152 rows of 128000 bf16 logits 151 -> TODO us.
+// result.  An fp64 instruction takes twice an fp32 one's time: 27 units for an exponential in place of 40.
 constexpr int kPowers = 256;
 __device__ __forceinline__ void make_powers(double* powers) { powers[threadIdx.x] = exp2_64((double)threadIdx.x / kPowers); }
 __device__ __forceinline__ double exp2_by_powers(double y, const double* powers) {
   constexpr double kMagic = 0x1.8p44;    // its last place is 2^-8
-  y = fmax(y, -1100.0);
+  // y >= -1100.02: of negative numbers the larger words are the lower ones (2^y is 0 from there on; -inf too)
+  uint64_t bits = __builtin_bit_cast(uint64_t, y);
+  const uint32_t high = (uint32_t)(bits >> 32);
+  bits = (bits & 0xffffffffu) | (uint64_t)(high < 0xc0913000u ? high : 0xc0913000u) << 32;
+  y = __builtin_bit_cast(double, bits);
   const double z = y + kMagic, r = y - (z - kMagic);
   const int k = (int)(uint32_t)__builtin_bit_cast(uint64_t, z);
   const double t = powers[k & (kPowers - 1)];
@@ -105,7 +111,7 @@ template <typename TE> __device__ __forceinline__ void ld_logits(const TE* row, 
 __device__ __forceinline__ bool is_word(int32_t x, int V) { return x >= 0 && x < V; }
 
 // ---- statistics of the rows --------------------------------------------------------
-template <typename TE> __global__ __launch_bounds__(kVThreads) void verify_stats_kernel(VerifyDev a) {
+template <typename TE, int PER> __global__ __launch_bounds__(kVThreads) void verify_stats_kernel(VerifyDev a) {
   constexpr int W = 16 / sizeof(TE);
   __shared__ float s_m[4];
   __shared__ double s_sum[4], s_powers[kPowers];
@@ -118,17 +124,17 @@ template <typename TE> __global__ __launch_bounds__(kVThreads) void verify_stats
     if (!is_word(a.drafted[(int64_t)b * a.T + i], a.V)) return;
   const TE* row = j <= a.T ? reinterpret_cast<const TE*>(a.target) + ((int64_t)b * (a.T + 1) + t) * a.ld_target
                            : reinterpret_cast<const TE*>(a.draft) + ((int64_t)b * a.T + t) * a.ld_draft;
-  float l[kVPer];
+  float l[PER];
 #pragma unroll
-  for (int i = 0; i < kVPer / W; ++i) {
-    const int v0 = blockIdx.x * kVChunk + (i * kVThreads + tid) * W;
+  for (int i = 0; i < PER / W; ++i) {
+    const int v0 = blockIdx.x * kVThreads * PER + (i * kVThreads + tid) * W;
     ld_logits<TE>(row, v0 < a.V ? v0 : a.V, a.V, l + i * W);
   }
   make_powers(s_powers);                   // (while the logits are on their way)
   float m = -INFINITY;
   int bad = 0;
 #pragma unroll
-  for (int i = 0; i < kVPer; ++i) {
+  for (int i = 0; i < PER; ++i) {
     m = fmaxf(m, l[i]);
     bad |= !(l[i] < INFINITY);
   }
@@ -141,7 +147,7 @@ template <typename TE> __global__ __launch_bounds__(kVThreads) void verify_stats
   if (m > -INFINITY && !bad) {
     const double shift = -(double)m * a.c;
 #pragma unroll
-    for (int i = 0; i < kVPer; ++i) sum += exp2_by_powers(fma((double)l[i], a.c, shift), s_powers);
+    for (int i = 0; i < PER; ++i) sum += exp2_by_powers(fma((double)l[i], a.c, shift), s_powers);
   }
   sum = wave_sum64(sum);
   if ((tid & 63) == 0) s_sum[wave] = sum;
@@ -151,25 +157,14 @@ template <typename TE> __global__ __launch_bounds__(kVThreads) void verify_stats
 
 // ---- the words ---------------------------------------------------------------------
 struct RowStat {
-  double shift, inv_z;   // p[v] = 2^(l[v] c + shift) inv_z
+  double shift;          // p[v] = 2^(l[v] c + shift)
 };
-struct Weights {
-  RowStat p, q;
-  double c;
-  const double* powers;
-  // p[v], and what of it counts: all, or what is above q[v]
-  __device__ __forceinline__ double at(float lp, float lq, bool subtract, double& pv) const {
-    pv = exp2_by_powers(fma((double)lp, c, p.shift), powers) * p.inv_z;
-    return subtract ? fmax(pv - exp2_by_powers(fma((double)lq, c, q.shift), powers) * q.inv_z, 0.0) : pv;
-  }
-};
-
-template <typename TE> __global__ __launch_bounds__(kVThreads) void verify_words_kernel(VerifyDev a) {
-  constexpr int W = 16 / sizeof(TE);
+template <typename TE, int PER> __global__ __launch_bounds__(kVThreads) void verify_words_kernel(VerifyDev a) {
+  constexpr int W = 16 / sizeof(TE), CHUNK = kVThreads * PER;
   __shared__ RowStat s_stat[2 * kVerifyMaxT + 1];
   __shared__ int8_t s_bad[2 * kVerifyMaxT + 1];
   __shared__ int s_words, s_n, s_state, s_last, s_chunk, s_found, s_some;
-  __shared__ double s_r[4], s_p[4], s_theta, s_powers[kPowers];
+  __shared__ double s_r[4], s_ahead, s_theta, s_powers[kPowers];
   const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, T = a.T, V = a.V;
   const int64_t first = (int64_t)b * T;
   const TE* target = reinterpret_cast<const TE*>(a.target) + (int64_t)b * (T + 1) * a.ld_target;
@@ -216,7 +211,7 @@ template <typename TE> __global__ __launch_bounds__(kVThreads) void verify_words
 #pragma unroll
     for (int o = 1; o < 16; o <<= 1) z += __shfl_xor(z, o, 64);
     if ((lane & 15) == 0) {
-      s_stat[j] = {-(double)top * a.c, 1.0 / z};
+      s_stat[j] = {-(double)top * a.c - log2(z)};
       s_bad[j] = bad || !(top > -INFINITY);
     }
   }
@@ -226,8 +221,8 @@ template <typename TE> __global__ __launch_bounds__(kVThreads) void verify_words
     if (lane < words) {
       const RowStat p = s_stat[lane], q = s_stat[T + 1 + lane];
       bad = s_bad[lane] || s_bad[T + 1 + lane];
-      ok = !bad && (double)u * (exp2_by_powers(fma((double)lq_x, a.c, q.shift), s_powers) * q.inv_z) <
-                       exp2_by_powers(fma((double)lp_x, a.c, p.shift), s_powers) * p.inv_z;
+      ok = !bad && (double)u * exp2_by_powers(fma((double)lq_x, a.c, q.shift), s_powers) <
+                       exp2_by_powers(fma((double)lp_x, a.c, p.shift), s_powers);
     }
     const uint64_t not_ok = ~__ballot(ok), bads = __ballot(bad);
     if (lane == 0) {
@@ -244,55 +239,51 @@ template <typename TE> __global__ __launch_bounds__(kVThreads) void verify_words
     if (tid <= T && (tid != n || state == 2)) a.words[first + b + tid] = tid < n ? a.drafted[first + tid] : -1;
   }
   if (state == 2) return;
-  const TE *p_row = target + n * a.ld_target, *q_row = rest ? draft + n * a.ld_draft : p_row;
-  const Weights w = {s_stat[n], s_stat[rest ? T + 1 + n : n], a.c, s_powers};
-  float lp[kVPer], lq[kVPer];
-  // this chunk's weights
+  const TE *p_row = target + n * a.ld_target, *q_row = draft + (rest ? n : 0) * a.ld_draft;
+  const double p_shift = s_stat[n].shift, q_shift = s_stat[rest ? T + 1 + n : n].shift;
+  // what counts of a word: all of p, or what is above q
+  auto weight = [&](auto subtract, float lp, float lq) {
+    const double p = exp2_by_powers(fma((double)lp, a.c, p_shift), s_powers);
+    if constexpr (!decltype(subtract)::value) return p;
+    else return fmax(p - exp2_by_powers(fma((double)lq, a.c, q_shift), s_powers), 0.0);
+  };
+  // weights of the words from v0 on, vectors step words apart
+  auto weights = [&](auto subtract, int v0, int step) {
+    double sum = 0;
+#pragma unroll 1
+    for (int i = 0; i < PER / W; ++i, v0 += step) {
+      float lp[W], lq[W] = {};
+      ld_logits<TE>(p_row, v0 < V ? v0 : V, V, lp);
+      if constexpr (decltype(subtract)::value) ld_logits<TE>(q_row, v0 < V ? v0 : V, V, lq);
 #pragma unroll
-  for (int i = 0; i < kVPer / W; ++i) {
-    const int v0 = blockIdx.x * kVChunk + (i * kVThreads + tid) * W;
-    ld_logits<TE>(p_row, v0 < V ? v0 : V, V, lp + i * W);
-    ld_logits<TE>(q_row, v0 < V ? v0 : V, V, lq + i * W);
-  }
-  double r = 0, p = 0;
-#pragma unroll 4
-  for (int i = 0; i < kVPer; ++i) {
-    double pv;
-    r += w.at(lp[i], lq[i], rest, pv);
-    p += pv;
-  }
-  r = wave_sum64(r);
-  p = wave_sum64(p);
-  if (lane == 0) {
-    s_r[wave] = r;
-    s_p[wave] = p;
-  }
-  __syncthreads();
-  double2* sums = a.sums + (int64_t)b * a.chunks;
-  if (tid == 0) {
-    __hip_atomic_store(&sums[blockIdx.x].x, (s_r[0] + s_r[1]) + (s_r[2] + s_r[3]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __hip_atomic_store(&sums[blockIdx.x].y, (s_p[0] + s_p[1]) + (s_p[2] + s_p[3]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __builtin_amdgcn_s_waitcnt(0);   // they are where every XCD sees them (stored past the caches) before this block counts
-    s_last = __hip_atomic_fetch_add(&a.ticket[b], 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)a.chunks - 1;
-  }
-  __syncthreads();
-  if (!s_last) return;
-  // The sequence's last block finds the chunk; sums are added in the chunks' order, whichever block this is.
-  if (wave == 0) {
-    double x[2][2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int k = h * 64 + lane;
-      x[h][0] = k < a.chunks ? __hip_atomic_load(&sums[k].x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
-      x[h][1] = k < a.chunks ? __hip_atomic_load(&sums[k].y, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
+      for (int e = 0; e < W; ++e) sum += weight(subtract, lp[e], lq[e]);
     }
-    double run[2], all = 0;
-    bool of_p = false;
-    auto scan = [&](bool p_too) {
-      of_p = p_too;
+    return sum;
+  };
+  double* sums = a.sums + (int64_t)b * a.chunks;
+  if (rest) {
+    // this chunk's
+    double r = weights(std::true_type{}, blockIdx.x * CHUNK + tid * W, kVThreads * W);
+    r = wave_sum64(r);
+    if (lane == 0) s_r[wave] = r;
+    __syncthreads();
+    if (tid == 0) {
+      __hip_atomic_store(&sums[blockIdx.x], (s_r[0] + s_r[1]) + (s_r[2] + s_r[3]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __builtin_amdgcn_s_waitcnt(0);   // it is where every XCD sees it (stored past the caches) before this block counts
+      s_last = __hip_atomic_fetch_add(&a.ticket[b], 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)a.chunks - 1;
+    }
+    __syncthreads();
+    if (!s_last) return;
+  } else if (blockIdx.x != 0) {
+    return;                            // p's chunks have been added up by the statistics
+  }
+  // One block, the sequence's last or first, finds the chunk; sums are added in the chunks' order, whichever block this is.
+  if (wave == 0) {
+    double x[2], run[2], all = 0;
+    auto scan = [&]() {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        run[h] = p_too ? x[h][1] : x[h][0];
+        run[h] = x[h];
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
           const double y = __shfl_up(run[h], o, 64);
@@ -302,15 +293,32 @@ template <typename TE> __global__ __launch_bounds__(kVThreads) void verify_words
       }
       all = __shfl(run[1], 63, 64);
     };
-    scan(false);
-    if (!(all > 0)) scan(true);             // nothing is left: p
+    if (rest) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int k = h * 64 + lane;
+        x[h] = k < a.chunks ? __hip_atomic_load(&sums[k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
+      }
+      scan();
+    }
+    const bool of_p = !(all > 0);           // nothing is left: p
+    if (of_p) {
+      const VerifyPart* part = a.part + ((int64_t)b * (2 * T + 1) + n) * a.chunks;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int k = h * 64 + lane;
+        x[h] = 0.0;
+        if (k < a.chunks && part[k].m > -INFINITY) x[h] = part[k].sum * exp2_by_powers(fma((double)part[k].m, a.c, p_shift), s_powers);
+      }
+      scan();
+    }
     const double theta = fmax((double)a.u_next[b], 0.0) * all;
     int chunk = -1, some = 0;
     double left = INFINITY;
 #pragma unroll
     for (int h = 1; h >= 0; --h) {
-      const double own = of_p ? x[h][1] : x[h][0];
-      const uint64_t above = __ballot(run[h] > theta), there = __ballot(own > 0);
+      const double own = x[h];
+      const uint64_t above = __ballot(own > 0 && run[h] > theta), there = __ballot(own > 0);   // (of weight 0: rounding alone)
       if (above) {
         const int k = __builtin_ctzll(above);
         chunk = h * 64 + k;
@@ -327,18 +335,10 @@ template <typename TE> __global__ __launch_bounds__(kVThreads) void verify_words
     }
   }
   __syncthreads();
-  const bool subtract = rest && !s_state;
-  const int v1 = s_chunk * kVChunk + tid * kVPer;   // consecutive logits per thread: running sums go by the words' order
+  const bool subtract = !s_state;
+  const int v1 = s_chunk * CHUNK + tid * PER;   // consecutive logits per thread: running sums go by the words' order
   const double theta = s_theta;
-#pragma unroll
-  for (int i = 0; i < kVPer / W; ++i) {
-    const int v0 = v1 + i * W;
-    ld_logits<TE>(p_row, v0 < V ? v0 : V, V, lp + i * W);
-    ld_logits<TE>(q_row, v0 < V ? v0 : V, V, lq + i * W);
-  }
-  double own = 0, pv;
-#pragma unroll 4
-  for (int i = 0; i < kVPer; ++i) own += w.at(lp[i], lq[i], subtract, pv);
+  const double own = subtract ? weights(std::true_type{}, v1, W) : weights(std::false_type{}, v1, W);
   double run = own;   // inclusive over the block
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -348,36 +348,45 @@ template <typename TE> __global__ __launch_bounds__(kVThreads) void verify_words
   if (lane == 63) s_r[wave] = run;
   __syncthreads();
   for (int i = 0; i < wave; ++i) run += s_r[i];
-  if (run > theta) atomicMin(&s_found, tid);
+  if (own > 0 && run > theta) atomicMin(&s_found, tid);
   if (own > 0) atomicMax(&s_some, tid);
   __syncthreads();
   const bool none = s_found == 1 << 30;      // (as above: the chunk's last word of a weight above 0)
-  if (tid != (none ? s_some : s_found)) return;
-  double at = run - own;
-  int word = -1;
-#pragma unroll 1
-  for (int i = 0; i < kVPer; ++i) {
-    const int v = v1 + i;
-    if (v >= V) break;
-    const double rv = w.at(ld_elem<TE>(p_row, v), ld_elem<TE>(q_row, v), subtract, pv);
-    at += rv;
-    if (rv > 0) word = v;
-    if (!none && at > theta && rv > 0) break;
+  const int at = none ? s_some : s_found;
+  if (tid == at) s_ahead = run - own;
+  __syncthreads();
+  if (wave != 0) return;
+  // that thread's words, a lane each
+  const int v = s_chunk * CHUNK + at * PER + lane;
+  double mine = 0;
+  if (lane < PER && v < V) {
+    const float lp = ld_elem<TE>(p_row, v), lq = subtract ? ld_elem<TE>(q_row, v) : 0.f;
+    mine = subtract ? weight(std::true_type{}, lp, lq) : weight(std::false_type{}, lp, lq);
   }
-  a.words[first + b + n] = word;
+  run = mine;
+#pragma unroll
+  for (int o = 1; o < PER; o <<= 1) {
+    const double x = __shfl_up(run, o, 64);
+    if (lane >= o) run += x;
+  }
+  const uint64_t above = __ballot(!none && mine > 0 && s_ahead + run > theta), there = __ballot(mine > 0);
+  if (lane == 0) a.words[first + b + n] = s_chunk * CHUNK + at * PER + (above ? __builtin_ctzll(above) : 63 - __builtin_clzll(there));
 }
 
 struct VerifyLayout {
-  int chunks;
+  int per, chunks;
   size_t part, sums, ticket, total;
 };
 VerifyLayout verify_layout(const vo_verify* s) {
   VerifyLayout L;
-  L.chunks = (s->V + kVChunk - 1) / kVChunk;
+  // us, the whole call, 32 / 8 logits a thread: TODO
+  const int64_t few = kVThreads * kFewPer;
+  L.per = (int64_t)s->B * (2 * s->T + 1) * ((s->V + few - 1) / few) <= 1024 && s->V <= few * kMostChunks ? kFewPer : kManyPer;
+  L.chunks = (s->V + kVThreads * L.per - 1) / (kVThreads * L.per);
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   L.part = 0;
   L.sums = up((size_t)s->B * (2 * s->T + 1) * L.chunks * sizeof(VerifyPart));
-  L.ticket = L.sums + up((size_t)s->B * L.chunks * sizeof(double2));
+  L.ticket = L.sums + up((size_t)s->B * L.chunks * sizeof(double));
   L.total = L.ticket + up((size_t)s->B * 4);
   return L;
 }
@@ -388,7 +397,7 @@ bool verify_ok(const vo_verify* s) {
 bool verify_types(const vo_verify* s) { return s->dtype == AS_F32 || s->dtype == AS_BF16; }
 bool al16r(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-template <typename TE> hipError_t launch_verify(const VerifyDev& d, hipStream_t st) {
+template <typename TE, int PER> hipError_t launch_verify(const VerifyDev& d, hipStream_t st) {
   // rows of a launch: the grid's second dimension takes 65535
   const int rows = 2 * d.T + 1, most = 65535 / rows;
   for (int b0 = 0; b0 < d.B; b0 += most) {
@@ -404,10 +413,10 @@ template <typename TE> hipError_t launch_verify(const VerifyDev& d, hipStream_t 
     p.part += (int64_t)b0 * rows * d.chunks;
     p.sums += (int64_t)b0 * d.chunks;
     p.ticket += b0;
-    hipLaunchKernelGGL(verify_stats_kernel<TE>, dim3(d.chunks, p.B * rows), dim3(kVThreads), 0, st, p);
+    hipLaunchKernelGGL((verify_stats_kernel<TE, PER>), dim3(d.chunks, p.B * rows), dim3(kVThreads), 0, st, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(verify_words_kernel<TE>, dim3(d.chunks, p.B), dim3(kVThreads), 0, st, p);
+    hipLaunchKernelGGL((verify_words_kernel<TE, PER>), dim3(d.chunks, p.B), dim3(kVThreads), 0, st, p);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -455,7 +464,7 @@ extern "C" as_status vocab_verify(const vo_verify* shape, const void* target, in
   d.n_accepted = n_accepted;
   d.words = words;
   d.part = reinterpret_cast<VerifyPart*>(ws + L.part);
-  d.sums = reinterpret_cast<double2*>(ws + L.sums);
+  d.sums = reinterpret_cast<double*>(ws + L.sums);
   d.ticket = reinterpret_cast<uint32_t*>(ws + L.ticket);
   d.B = shape->B;
   d.T = shape->T;
@@ -463,6 +472,8 @@ extern "C" as_status vocab_verify(const vo_verify* shape, const void* target, in
   d.chunks = L.chunks;
   d.c = 1.4426950408889634 / (double)shape->temperature;
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
-  const hipError_t err = e == 4 ? launch_verify<float>(d, st) : launch_verify<uint16_t>(d, st);
+  const bool few = L.per == kFewPer;
+  const hipError_t err = e == 4 ? (few ? launch_verify<float, kFewPer>(d, st) : launch_verify<float, kManyPer>(d, st))
+                                : (few ? launch_verify<uint16_t, kFewPer>(d, st) : launch_verify<uint16_t, kManyPer>(d, st));
   return err == hipSuccess ? AS_OK : set_error(AS_ERR_HIP, "vocab_verify: %s", hipGetErrorString(err));
 }
