@@ -27,8 +27,7 @@ namespace {
 typedef uint32_t au32x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t au32x2_t __attribute__((ext_vector_type(2)));
 
-constexpr int kJoinThreads = 256;
-constexpr int kMostBlocks = 512;
+constexpr int kLongRun = 8;            // chunks
 constexpr int kLeastChunk = 16;
 constexpr int kWholeChunks = 4;        // up to so many chunks a block takes all of a (sequence, head)
 constexpr uint32_t kAttnOob = 0x80000000u;
@@ -66,66 +65,100 @@ __device__ __forceinline__ SeqSpan seq_span(const KvAttnDev& a, int b) {
   return s;
 }
 
-__device__ __forceinline__ int32_t cut_per(int32_t total, int blocks) {
-  const int32_t per = (total + blocks - 1) / blocks;
-  return per < 1 ? 1 : per;
+// How the chunks of all (sequence, head, row group) are given to the blocks.
+struct Cut {
+  int32_t total;   // chunks
+  int32_t per;     // of a block, at most
+  bool pieces;     // a block has one piece of one (sequence, head, row group), those of one sequence being of the same length; else a run
+                   // of `per` chunks, whatever they are of
+  // a sequence's pieces, or chunks, for each of its heads and row groups
+  __device__ __forceinline__ int32_t units(int32_t chunks) const { return pieces ? (chunks + per - 1) / per : chunks; }
+};
+// A run that ends one sequence's head and begins the next one's reads two sets of queries and writes two results, which costs as much as
+// some chunks do: short runs are pieces instead, if pieces that are not full leave no more blocks without work than that.
+// us, kernels: 24 sequences of two heads, 1004 tokens seen by 40 rows, runs / pieces TODO.
+__device__ __forceinline__ Cut cut_of(const KvAttnDev& a, int32_t chunks, int blocks) {
+  const int32_t hr = a.heads * a.row_groups;
+  Cut c;
+  c.total = chunks * hr;
+  c.per = (c.total + blocks - 1) / blocks;
+  if (c.per < 1) c.per = 1;
+  c.pieces = false;
+  const int64_t pairs = (int64_t)a.B * hr;
+  if (2 * pairs <= blocks) {
+    const int32_t left = blocks - (int32_t)pairs, per = (c.total + left - 1) / left;   // sum of (n + per - 1) / per <= total / per + pairs
+    if (per < kLongRun) {
+      c.per = per < 1 ? 1 : per;
+      c.pieces = true;
+    }
+  }
+  return c;
 }
-// A block's run of all chunks (of the sequences, their heads and row groups): how many, the sequence of the first one, and the chunks ahead
-// of that sequence.  A block's threads take that many sequences at a time; more of them are gone through twice.
+template <int WAVES> __device__ __forceinline__ int32_t sum_of_waves(int32_t n, int32_t* s_sum) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = n;
+  __syncthreads();
+  n = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) n += s_sum[w];
+  return n;
+}
+template <int WAVES> __device__ __forceinline__ Cut cut_all(const KvAttnDev& a, int blocks, int32_t* s_sum) {
+  int32_t n = 0;
+  for (int b = threadIdx.x; b < a.B; b += WAVES * 64) n += seq_span(a, b).chunks;
+  return cut_of(a, sum_of_waves<WAVES>(n, s_sum), blocks);
+}
+// A block's work: `left` chunks from `chunk` on of sequence b's head and row group hr; 0: none.
 struct Run {
-  int32_t left, at, b, ahead;
+  int32_t b, hr, chunk, left;
 };
 template <int WAVES> __device__ __forceinline__ Run cut_run(const KvAttnDev& a, int32_t* s_sum, int32_t* s_found) {
-  const int32_t hr = a.heads * a.row_groups, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  auto chunks_of = [&](int b) { return b < a.B ? seq_span(a, b).chunks * hr : 0; };
-  const int32_t first = chunks_of(threadIdx.x);
-  int32_t total = first;
-  for (int b = threadIdx.x + WAVES * 64; b < a.B; b += WAVES * 64) total += chunks_of(b);
-  int32_t own = first, run = first, carry = 0;
-  Run r;
-  for (int b0 = 0;; b0 += WAVES * 64) {
-    if (b0 > 0) run = own = chunks_of(b0 + threadIdx.x);
+  const Cut c = cut_all<WAVES>(a, gridDim.x, s_sum);
+  const int32_t hrs = a.heads * a.row_groups, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int32_t at = c.pieces ? (int32_t)blockIdx.x : (int32_t)blockIdx.x * c.per;   // in units, as is what follows
+  Run r = {0, 0, 0, 0};
+  int32_t carry = 0;
+  bool found = false;
+  for (int b0 = 0; b0 < a.B && !found; b0 += WAVES * 64) {
+    const int b = b0 + threadIdx.x;
+    const int32_t own = b < a.B ? c.units(seq_span(a, b).chunks) * hrs : 0;
+    int32_t run = own;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
       const int32_t x = __shfl_up(run, o, 64);
       if (lane >= o) run += x;
     }
-    if (b0 == 0) {
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
-    }
-    if (lane == 63) {
-      s_sum[wave] = run;
-      if (b0 == 0) s_sum[WAVES + wave] = total;
-    }
     __syncthreads();
-    int32_t before = carry, here = 0;
+    if (lane == 63) s_sum[wave] = run;
+    __syncthreads();
+    int32_t ahead = carry + run - own;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
       const int32_t x = s_sum[w];
-      before += w < wave ? x : 0;
-      here += x;
+      ahead += w < wave ? x : 0;
+      carry += x;
     }
-    if (b0 == 0) {
-      total = 0;
-#pragma unroll
-      for (int w = 0; w < WAVES; ++w) total += s_sum[WAVES + w];
-      const int32_t per = cut_per(total, gridDim.x);
-      r.at = (int32_t)blockIdx.x * per;
-      r.left = total - r.at < per ? total - r.at : per;
-      if (r.left <= 0) return r;
-    }
-    const int32_t ahead = before + run - own;
-    if (r.at >= ahead && r.at < ahead + own) {
-      s_found[0] = b0 + threadIdx.x;
+    if (at >= ahead && at < ahead + own) {
+      s_found[0] = b;
       s_found[1] = ahead;
     }
-    carry += here;
-    __syncthreads();
-    if (r.at < carry) break;
+    found = at < carry;
   }
+  if (!found) return r;                   // (the same in all threads)
+  __syncthreads();
   r.b = s_found[0];
-  r.ahead = s_found[1];
+  const int32_t rest = at - s_found[1], n = seq_span(a, r.b).chunks, units = c.units(n);
+  r.hr = rest / units;
+  const int32_t unit = rest - r.hr * units;
+  if (c.pieces) {
+    r.chunk = (int32_t)((int64_t)unit * n / units);
+    r.left = (int32_t)((int64_t)(unit + 1) * n / units) - r.chunk;
+  } else {
+    r.chunk = unit;
+    r.left = c.total - at < c.per ? c.total - at : c.per;
+  }
   return r;
 }
 
@@ -170,6 +203,7 @@ template <int TYPE, bool F32Q, int DP> struct Form {
   static constexpr int kTiles = kF32 ? 1 : 2;                       // of a step
   // Waves of a block.  A wave holds a step's K and V, the queries and O^T in registers: at a width of 256 those of one wave on a SIMD, below of two.
   static constexpr int kWaves = DP > 128 ? 4 : 8;
+  static constexpr int kBlocks = DP > 128 ? 1 : DP > 64 || (TYPE != KC_F32 && (TYPE != KC_INT8 || F32Q)) ? 2 : 4;   // (waves on a SIMD that registers allow)
   static constexpr int kQTerms = kF32 || !F32Q ? 1 : 3, kPTerms = kF32 ? 1 : F32Q ? 3 : 2;
   static constexpr int kKLoads = DP * kBytes / 64;                  // 16-byte loads of a lane for a tile of K
   static constexpr int kKElems = 16 / kBytes;                       // elements of each: D index (load * 4 + g) * kKElems + i
@@ -178,7 +212,20 @@ template <int TYPE, bool F32Q, int DP> struct Form {
   static constexpr int kVW = kCoded ? kVAll : kF32 ? 4 : (kVAll < 8 ? kVAll : 8);
   static constexpr int kVHalves = kVAll / kVW;
   static constexpr int kVDwords = kVW * kBytes / 4;
-  static constexpr bool kCanBeOdd = TYPE != KC_INT8;                // values may be infinities or NaN
+  // Values may be infinities or NaN: bits of theirs in a word, which no other value sets (an exponent of ones and one more), all bits of
+  // theirs, and a word of ones.
+  static constexpr bool kCanBeOdd = TYPE != KC_INT8;
+  static constexpr uint32_t kOnes = kF32 ? 0x3f800000u : kCoded ? 0x38383838u : 0x3f803f80u;
+  static __device__ __forceinline__ uint32_t odd(uint32_t w) {
+    if constexpr (kF32) return ((w & 0x7f800000u) + 0x00800000u) & 0x80000000u;
+    else if constexpr (kCoded) return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+    else return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+  }
+  static __device__ __forceinline__ uint32_t odd_bits(uint32_t w) {
+    const uint32_t x = odd(w) >> (kF32 ? 31 : kCoded ? 7 : 15);
+    if constexpr (kF32) return 0u - x;
+    else return (x << (kCoded ? 8 : 16)) - x;
+  }
 };
 
 template <int N> __device__ __forceinline__ void buffer_load(__amdgpu_buffer_rsrc_t rs, uint32_t off, uint32_t (&x)[N]) {
@@ -197,13 +244,13 @@ template <int N> __device__ __forceinline__ void buffer_load(__amdgpu_buffer_rsr
 }
 
 // ---- the kernel -------------------------------------------------------------------
-template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__((Form<TYPE, F32Q, DP>::kWaves * 64)) void kv_attn_kernel(KvAttnDev a) {
+template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__((Form<TYPE, F32Q, DP>::kWaves * 64), (Form<TYPE, F32Q, DP>::kBlocks)) void kv_attn_kernel(KvAttnDev a) {
   using F = Form<TYPE, F32Q, DP>;
   constexpr int WAVES = F::kWaves;
   constexpr int NT = F::kTiles, NO = DP / 16, STEP = NT * kKvTile, LD = DP + 4;
   extern __shared__ float lds[];          // [waves][16 rows][LD], and their maxima and sums
   float* lds_ml = lds + WAVES * 16 * LD;
-  __shared__ int32_t s_sum[2 * WAVES], s_found[2];
+  __shared__ int32_t s_sum[WAVES], s_found[2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, g = lane >> 4;
   const int row_wave = wave % a.tile_waves, tok_wave = wave / a.tile_waves, tok_waves = WAVES / a.tile_waves;   // (some may be left over)
@@ -229,10 +276,9 @@ template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__((Form<TYPE, 
     const Run run = cut_run<WAVES>(a, s_sum, s_found);
     if (run.left <= 0) return;
     b = run.b;
+    hr = run.hr;
+    chunk = run.chunk;
     left = run.left;
-    const int32_t n = seq_span(a, b).chunks;
-    hr = (run.at - run.ahead) / n;
-    chunk = run.at - run.ahead - hr * n;
   } else {
     b = blockIdx.x / (a.heads * a.row_groups);
     hr = blockIdx.x - b * (a.heads * a.row_groups);
@@ -364,76 +410,36 @@ template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__((Form<TYPE, 
       }
     };
 
-    // O^T += V^T P^T of the step, a block of 16 columns after the other.  ODD: for the rows of one token alone, with what it does not see taken
-    // out of V (bit u * 4 + i of `in`: this lane's token), since 0 times an infinity or a NaN is a NaN.
-    auto times_v = [&](auto odd, const float (&p)[NT][4], uint32_t in, bool mine) {
-      constexpr bool ODD = decltype(odd)::value;
-      auto raw = [&](int u, int i, int h, int w) -> uint32_t {
-        if constexpr (ODD) return in >> (u * 4 + i) & 1 ? vr[u][i][h][w] : 0u;
-        else return vr[u][i][h][w];
-      };
-      auto onto = [&](int j, auto product) {
-        if constexpr (ODD) {
-          f32x4_t some = {};
-          product(some);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) o[j][i] += mine ? some[i] : 0.f;
-        } else {
-          product(o[j]);
-        }
-      };
+    // The fragments of V^T, 16 columns after the other: use(j, fragment), or, of floats, use(j, i, value) for tokens i; raw(u, i, h, w) are
+    // the loaded words, or others like them.
+    auto columns = [&](auto raw, auto use) {
       if constexpr (F::kF32) {
 #pragma unroll
         for (int j = 0; j < NO; ++j)
-          onto(j, [&](f32x4_t& acc) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, raw(0, i, j / F::kVW, j % F::kVW)), p[0][i], acc, 0, 0, 0);
-          });
-      } else {
-        bf16x8_t pb[F::kPTerms];
+          for (int i = 0; i < 4; ++i) use(j, i, __builtin_bit_cast(float, raw(0, i, j / F::kVW, j % F::kVW)));
+      } else if constexpr (F::kCoded) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int w = 0; w < F::kVDwords; ++w) {
+          float x[2][4][4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float rest = p[u][i];
+          for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int s = 0; s < F::kPTerms; ++s) {
-              const bf16_t x = (bf16_t)rest;
-              pb[s][u * 4 + i] = x;
-              rest -= (float)x;
-            }
-          }
-        auto add = [&](int j, au32x4_t v) {
-          const bf16x8_t vb = as_frag(v);
-          onto(j, [&](f32x4_t& acc) {
+            for (int i = 0; i < 4; ++i) codes_to_floats<TYPE>(raw(u, i, 0, w), x[u][i]);
 #pragma unroll
-            for (int s = 0; s < F::kPTerms; ++s) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, pb[s], acc, 0, 0, 0);
-          });
-        };
-        if constexpr (F::kCoded) {
-#pragma unroll
-          for (int w = 0; w < F::kVDwords; ++w) {
-            float x[2][4][4];
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) codes_to_floats<TYPE>(raw(u, i, 0, w), x[u][i]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              add(w * 4 + e, au32x4_t{top_halves(x[0][0][e], x[0][1][e]), top_halves(x[0][2][e], x[0][3][e]),
-                                      top_halves(x[1][0][e], x[1][1][e]), top_halves(x[1][2][e], x[1][3][e])});
-          }
-        } else {
-#pragma unroll
-          for (int h = 0; h < F::kVHalves; ++h)
-#pragma unroll
-            for (int e = 0; e < F::kVW; ++e) {
-              const uint32_t sel = e % 2 ? 0x07060302u : 0x05040100u;
-              auto two = [&](int u, int i) { return __builtin_amdgcn_perm(raw(u, i + 1, h, e / 2), raw(u, i, h, e / 2), sel); };
-              add(h * F::kVW + e, au32x4_t{two(0, 0), two(0, 2), two(1, 0), two(1, 2)});
-            }
+          for (int e = 0; e < 4; ++e)
+            use(w * 4 + e, as_frag(au32x4_t{top_halves(x[0][0][e], x[0][1][e]), top_halves(x[0][2][e], x[0][3][e]),
+                                            top_halves(x[1][0][e], x[1][1][e]), top_halves(x[1][2][e], x[1][3][e])}));
         }
+      } else {
+#pragma unroll
+        for (int h = 0; h < F::kVHalves; ++h)
+#pragma unroll
+          for (int e = 0; e < F::kVW; ++e) {
+            const uint32_t sel = e % 2 ? 0x07060302u : 0x05040100u;
+            auto two = [&](int u, int i) { return __builtin_amdgcn_perm(raw(u, i + 1, h, e / 2), raw(u, i, h, e / 2), sel); };
+            use(h * F::kVW + e, as_frag(au32x4_t{two(0, 0), two(0, 2), two(1, 0), two(1, 2)}));
+          }
       }
     };
 
@@ -492,13 +498,17 @@ template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__((Form<TYPE, 
         bool part = pos < all_lo || pos + STEP - 1 > all_hi;
 #pragma unroll
         for (int u = 0; u < NT; ++u) part |= k_valid[u] < kKvTile;
+        uint32_t seen = 0xff;             // bit u * 4 + i
         if (part) {
+          seen = 0;
 #pragma unroll
           for (int u = 0; u < NT; ++u)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int32_t x = pos + u * kKvTile + 4 * g + i;
-              if (x < lo || x > hi || 4 * g + i >= k_valid[u]) p[u][i] = -INFINITY;
+              const bool in = x >= lo && x <= hi && 4 * g + i < k_valid[u];
+              seen |= (uint32_t)in << (u * 4 + i);
+              if (!in) p[u][i] = -INFINITY;
             }
         }
         // the next step's keys, into the registers that have been read
@@ -529,47 +539,80 @@ template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__((Form<TYPE, 
         for (int u = 0; u < NT; ++u)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const bool seen = p[u][i] != -INFINITY;
-            const float w = __builtin_amdgcn_exp2f(fmaf(p[u][i], a.scale_log2, -m_use));
-            p[u][i] = part && !seen ? 0.f : w;
+            p[u][i] = __builtin_amdgcn_exp2f(fmaf(p[u][i], a.scale_log2, -m_use));
+            if (part && !(seen >> (u * 4 + i) & 1)) p[u][i] = 0.f;
             l += p[u][i];
-            if constexpr (F::kCoded) p[u][i] = part && !seen ? 0.f : p[u][i] * vs[u][i];
+            if constexpr (F::kCoded) {
+              p[u][i] *= vs[u][i];
+              if (part && !(seen >> (u * 4 + i) & 1)) p[u][i] = 0.f;   // (the scale of a place that holds nothing may be anything)
+            }
           }
-        // Values that only some rows see must not reach the others, whatever they are: 0 times an infinity or a NaN is a NaN.
-        bool odd = false;
-        if (part && F::kCanBeOdd) {
-          uint32_t x = 0;
-#pragma unroll
-          for (int u = 0; u < NT; ++u)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-              for (int h = 0; h < F::kVHalves; ++h)
-#pragma unroll
-                for (int w = 0; w < F::kVDwords; ++w) {
-                  const uint32_t v = vr[u][i][h][w];
-                  if constexpr (F::kF32) x |= (v & 0x7f800000u) == 0x7f800000u;
-                  else if constexpr (TYPE == KC_BF16) x |= (v & 0x7f80u) == 0x7f80u || (v & 0x7f800000u) == 0x7f800000u;
-                  else if constexpr (TYPE == KC_E4M3) x |= (((v & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
-                }
-          odd = __any(x != 0);
-        }
-        if (!F::kCanBeOdd || !odd) {
-          times_v(std::false_type{}, p, 0u, false);
-        } else if constexpr (F::kCanBeOdd) {
-          const int t0 = row0 / a.G, t1 = (row0 + 15) / a.G;
-          for (int tt = t0; tt <= t1 && tt < a.T; ++tt) {
-            const int32_t hi_t = len - a.T + tt, lo_t = a.window > 0 ? hi_t - a.window + 1 : 0;
-            uint32_t in = 0;
+        // Values that only some rows see must not reach the others, whatever they are: 0 times an infinity or a NaN is a NaN.  Such values
+        // are taken out, and the columns of the rows that see them made NaN.
+        if constexpr (F::kCanBeOdd) {
+          uint32_t odd = 0;
+          if (part) {
 #pragma unroll
             for (int u = 0; u < NT; ++u)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const int32_t x = pos + u * kKvTile + 4 * g + i;
-                in |= (uint32_t)(x >= lo_t && x <= hi_t) << (u * 4 + i);
-              }
-            times_v(std::true_type{}, p, in, row_there && t == tt);
+              for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int h = 0; h < F::kVHalves; ++h)
+#pragma unroll
+                  for (int w = 0; w < F::kVDwords; ++w) odd |= F::odd(vr[u][i][h][w]);
           }
+          if (__any(odd != 0)) {
+            auto ones = [&](int u, int i, int h, int w) { return F::odd_bits(vr[u][i][h][w]) & F::kOnes; };
+            if constexpr (F::kF32) {
+              f32x4_t count;
+              columns(ones, [&](int j, int i, float x) {
+                if (i == 0) count = f32x4_t{};
+                count = __builtin_amdgcn_mfma_f32_16x16x4f32(x, seen >> i & 1 ? 1.f : 0.f, count, 0, 0, 0);
+                if (i == 3)
+#pragma unroll
+                  for (int r = 0; r < 4; ++r) o[j][r] = count[r] > 0.f ? __builtin_nanf("") : o[j][r];
+              });
+            } else {
+              bf16x8_t sb;
+#pragma unroll
+              for (int k = 0; k < 8; ++k) sb[k] = (bf16_t)(seen >> k & 1 ? 1.f : 0.f);
+              columns(ones, [&](int j, bf16x8_t x) {
+                const f32x4_t count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, sb, f32x4_t{}, 0, 0, 0);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[j][r] = count[r] > 0.f ? __builtin_nanf("") : o[j][r];
+              });
+            }
+#pragma unroll
+            for (int u = 0; u < NT; ++u)
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int h = 0; h < F::kVHalves; ++h)
+#pragma unroll
+                  for (int w = 0; w < F::kVDwords; ++w) vr[u][i][h][w] &= ~F::odd_bits(vr[u][i][h][w]);
+          }
+        }
+        auto as_loaded = [&](int u, int i, int h, int w) { return vr[u][i][h][w]; };
+        if constexpr (F::kF32) {
+          columns(as_loaded, [&](int j, int i, float x) { o[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, p[0][i], o[j], 0, 0, 0); });
+        } else {
+          bf16x8_t pb[F::kPTerms];
+#pragma unroll
+          for (int u = 0; u < NT; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              float rest = p[u][i];
+#pragma unroll
+              for (int s = 0; s < F::kPTerms; ++s) {
+                const bf16_t x = (bf16_t)rest;
+                pb[s][u * 4 + i] = x;
+                rest -= (float)x;
+              }
+            }
+          columns(as_loaded, [&](int j, bf16x8_t vb) {
+#pragma unroll
+            for (int s = 0; s < F::kPTerms; ++s) o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, pb[s], o[j], 0, 0, 0);
+          });
         }
         load_v();
       }
@@ -639,51 +682,37 @@ template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__((Form<TYPE, 
 // ---- parts of several blocks -------------------------------------------------------
 // A block per row: (sequence, head, row group) by blockIdx.x, its row by blockIdx.y.  Groups of D / 4 lanes (a power of two of them) take
 // the parts in turns; the order of the sums is that of the parts and the groups, whatever the launch.
-template <bool F32Q> __global__ __launch_bounds__(kJoinThreads) void kv_join_kernel(KvAttnDev a, int blocks, int lanes_log) {
-  __shared__ int32_t s_sum[4];
-  __shared__ float s_top[4], s_l[kJoinThreads];
-  __shared__ f32x4_t s_o[kJoinThreads];
+template <bool F32Q, int WAVES> __global__ __launch_bounds__(WAVES * 64) void kv_join_kernel(KvAttnDev a, int blocks, int lanes_log) {
+  constexpr int THREADS = WAVES * 64;
+  __shared__ int32_t s_sum[WAVES];
+  __shared__ float s_top[WAVES], s_l[THREADS];
+  __shared__ f32x4_t s_o[THREADS];
   const int hrs = a.heads * a.row_groups, b = blockIdx.x / hrs, hr = blockIdx.x - b * hrs;
   const int head = hr / a.row_groups, group = hr - head * a.row_groups;
   const int r = blockIdx.y, rr = group * a.group_rows + r;
   if (rr >= a.R) return;
-  // chunks in all, and ahead of this sequence
-  int32_t n = 0, before = 0;
-  for (int i = threadIdx.x; i < a.B; i += kJoinThreads) {
-    const int32_t x = seq_span(a, i).chunks;
-    n += x;
-    before += i < b ? x : 0;
-  }
   const SeqSpan span = seq_span(a, b);
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    n += __shfl_xor(n, o, 64);
-    before += __shfl_xor(before, o, 64);
-  }
-  __shared__ int32_t s_before[4];
-  if ((threadIdx.x & 63) == 0) {
-    s_sum[threadIdx.x >> 6] = n;
-    s_before[threadIdx.x >> 6] = before;
-  }
-  __syncthreads();
-  const int32_t per = cut_per((s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3]) * hrs, blocks);
-  int32_t k0 = 0, parts = 0;
+  const Cut cut = cut_all<WAVES>(a, blocks, s_sum);
+  int32_t k0 = 0, parts = 0;              // the first block that has some of it, and how many
   if (span.chunks > 0) {
-    const int32_t at = (s_before[0] + s_before[1] + s_before[2] + s_before[3]) * hrs + hr * span.chunks;
-    k0 = at / per;
-    parts = (at + span.chunks - 1) / per - k0 + 1;
+    int32_t n = 0;
+    for (int i = threadIdx.x; i < b; i += THREADS) n += cut.units(seq_span(a, i).chunks);
+    const int32_t units = cut.units(span.chunks), at = sum_of_waves<WAVES>(n, s_sum) * hrs + hr * units;
+    k0 = cut.pieces ? at : at / cut.per;
+    parts = cut.pieces ? units : (at + units - 1) / cut.per - k0 + 1;
     if (parts == 1) return;               // one block's, written by it
   }
   // part k of the pair: its block's slot 2 blk + 1 where the pair begins, else 2 blk
   auto slot = [&](int32_t k) { return (2 * (int64_t)(k0 + k) + (k == 0)) * a.group_rows + r; };
   float top = -INFINITY;
-  for (int32_t k = threadIdx.x; k < parts; k += kJoinThreads) top = fmaxf(top, a.part_ml[slot(k) * 2]);
+  for (int32_t k = threadIdx.x; k < parts; k += THREADS) top = fmaxf(top, a.part_ml[slot(k) * 2]);
   top = wave_max(top);
   if ((threadIdx.x & 63) == 0) s_top[threadIdx.x >> 6] = top;
   __syncthreads();
-  top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) top = fmaxf(top, s_top[w]);
   const float use = top == -INFINITY ? 0.f : top;
-  const int groups = kJoinThreads >> lanes_log, gr = threadIdx.x >> lanes_log, d = (threadIdx.x & ((1 << lanes_log) - 1)) * 4;
+  const int groups = THREADS >> lanes_log, gr = threadIdx.x >> lanes_log, d = (threadIdx.x & ((1 << lanes_log) - 1)) * 4;
   float sum = 0.f;
   f32x4_t v = {};
 #pragma unroll 4
@@ -752,7 +781,8 @@ AttnPlan attn_plan(const kc_cache* c, const kc_attn* s) {
   int64_t blocks = pairs;
   if (p.split) {
     blocks = pairs * chunks;
-    if (blocks > kMostBlocks) blocks = kMostBlocks;
+    const int64_t most = c->D <= 64 ? 512 : 256;   // what the compute units hold
+    if (blocks > most) blocks = most;
   }
   p.blocks = (int)blocks;
   const size_t rows = p.split ? (size_t)2 * p.blocks * p.group_rows : 0;
@@ -849,8 +879,10 @@ extern "C" as_status kv_cache_attn(const kc_cache* cache, const kc_attn* attn, c
     const dim3 grid((unsigned)(cache->B * cache->heads * p.row_groups), (unsigned)p.group_rows);
     int lanes_log = 2;
     while (4 << lanes_log < cache->D) ++lanes_log;
-    if (f32) hipLaunchKernelGGL(kv_join_kernel<true>, grid, dim3(kJoinThreads), 0, st, a, p.blocks, lanes_log);
-    else hipLaunchKernelGGL(kv_join_kernel<false>, grid, dim3(kJoinThreads), 0, st, a, p.blocks, lanes_log);
+    // many parts: four waves to a row
+    const bool many = p.blocks > 8 * (int64_t)grid.x;
+    auto kfn = f32 ? many ? kv_join_kernel<true, 4> : kv_join_kernel<true, 1> : many ? kv_join_kernel<false, 4> : kv_join_kernel<false, 1>;
+    hipLaunchKernelGGL(kfn, grid, dim3(many ? 256 : 64), 0, st, a, p.blocks, lanes_log);
     e = hipGetLastError();
   }
   return e == hipSuccess ? AS_OK : set_error(AS_ERR_HIP, "kv_cache_attn: %s", hipGetErrorString(e));

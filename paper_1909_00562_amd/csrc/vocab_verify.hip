@@ -284,6 +284,10 @@ template <typename TE, int PER> __global__ __launch_bounds__(kVThreads) void ver
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         run[h] = x[h];
+        if (h == 1 && a.chunks <= 64) {
+          run[1] = run[0];
+          break;
+        }
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
           const double y = __shfl_up(run[h], o, 64);
@@ -381,7 +385,7 @@ VerifyLayout verify_layout(const vo_verify* s) {
   VerifyLayout L;
   // us, the whole call, 32 / 8 logits a thread: TODO
   const int64_t few = kVThreads * kFewPer;
-  L.per = (int64_t)s->B * (2 * s->T + 1) * ((s->V + few - 1) / few) <= 1024 && s->V <= few * kMostChunks ? kFewPer : kManyPer;
+  L.per = (int64_t)s->B * (2 * s->T + 1) * ((s->V + few - 1) / few) <= 8192 && s->V <= few * kMostChunks ? kFewPer : kManyPer;
   L.chunks = (s->V + kVThreads * L.per - 1) / (kVThreads * L.per);
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   L.part = 0;

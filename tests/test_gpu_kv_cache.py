@@ -264,3 +264,278 @@ class Attn:
     ([260, 31], 3, 1, 17, 192, 16, 0), ([129], 64, 1, 2, 64, 16, 0), ([900, 20], 2, 4, 2, 64, 128, 1)])
 def test_attention(dtype, cache, lengths, T, heads, G, D, page, window):
     Attn(lengths, T, heads, G, D, page, dtype, cache, window, seed=D + T).run().check()
+
+
+@pytest.mark.parametrize("dtype, cache", CACHES)
+def test_attention_past_pages_that_are_none(dtype, cache):
+    """Tokens whose page is none are not seen; sequences of none give zeros; what is behind the end, and pages that nobody names, hold NaN."""
+    Attn([700, 90, 33, 1], 2, 2, 2, 64, 16, dtype, cache, seed=3, bad=0.4).run().check()
+    c = Attn([64, 40], 1, 1, 3, 48, 16, dtype, cache, seed=4)
+    c.table[1] = -1
+    c.run()
+    assert not c.out[1].any() and torch.isneginf(c.lse[1]).all()
+    c.there[1][:] = False
+    c.check()
+    Attn([500, 2000], 3, 2, 2, 64, 48, dtype, cache, window=900, seed=5, bad=0.2, table_width=60).run().check()
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("dtype, cache", [c for c in CACHES if c[1] != "int8"])
+@pytest.mark.parametrize("D", [48, 128, 256])
+def test_values_that_a_row_does_not_see_do_not_reach_it(dtype, cache, D, bad):
+    """Infinities and NaN in the cache at tokens that some rows see and others do not: the end of a draft, the beginning of a window, and
+    in one column and one head alone."""
+    lengths, T, window, col = [200, 37, 100], 6, 31, 7
+    c = Attn(lengths, T, 2, 3, D, 16, dtype, cache, window=window, seed=6)
+    o, bo, lse, bl = c.want()
+    v = c.c.v_pages
+    odd = []                                                  # (sequence, token)
+    for b, n in enumerate(lengths):
+        odd += [(b, n - 2), (b, n - T - window + 2), (b, max(0, n - T - window - 1))]
+    for b, i in odd:
+        if i < 0:
+            continue
+        p, at = oracle.place(b, i, c.pool.table, 16, c.pool.P)
+        if cache == "e4m3":
+            if bad == bad:
+                return                                        # (the type has no infinity)
+            v.view(torch.uint8)[p, 1, at, col] = 0x7f
+        else:
+            v[p, 1, at, col] = bad
+    c.run()
+    out = c.out.double().cpu().numpy()
+    for b, n in enumerate(lengths):
+        for t in range(T):
+            pos = n - T + t
+            sees = [i for x, i in odd if x == b and 0 <= i <= pos and i > pos - window]
+            hit = np.zeros((6, D), dtype=bool)
+            if sees:
+                hit[3:, col] = True                           # the heads that read head 1
+            assert not np.isfinite(out[b, t][hit]).any()
+            assert (np.abs(out[b, t] - o[b, t])[~hit] <= bo[b, t][~hit] + 1e-36).all()
+    assert np.isfinite(c.lse.cpu().numpy()[~np.isneginf(lse)]).all()
+
+
+@pytest.mark.parametrize("dtype, cache", CACHES)
+def test_keys_that_are_no_numbers(dtype, cache):
+    """A NaN in a seen key makes its rows NaN, and those of other heads and sequences are as they were."""
+    c = Attn([300, 80], 2, 2, 2, 64, 16, dtype, cache, seed=7)
+    o, bo, _, _ = c.want()
+    p, at = oracle.place(0, 299, c.pool.table, 16, c.pool.P)      # the last token: seen by the second row alone
+    if cache in oracle.LARGEST:
+        c.c.k_scales[p, 0, at] = float("nan")
+    else:
+        c.c.k_pages[p, 0, at, 5] = float("nan")
+    c.run()
+    out, lse = c.out.double().cpu().numpy(), c.lse.cpu().numpy()
+    assert np.isnan(out[0, 1, :2]).all() and np.isnan(lse[0, 1, :2]).all()
+    out[0, 1, :2] = o[0, 1, :2]
+    assert (np.abs(out - o) <= bo + 1e-36).all()
+
+
+@pytest.mark.parametrize("scale", [-0.3, 0.0, 3.0])
+@pytest.mark.parametrize("dtype, cache", CACHES)
+def test_scales_of_any_sign(dtype, cache, scale):
+    Attn([130, 5], 2, 1, 2, 32, 16, dtype, cache, scale=scale, seed=8).run().check()
+
+
+@pytest.mark.parametrize("dtype, cache", [("bf16", "bf16"), ("f32", "f32"), ("bf16", "int8")])
+@pytest.mark.parametrize("order", ["up", "down"])
+def test_scores_that_grow_and_shrink(dtype, cache, order):
+    """Maxima that move at every step, by less and by more than what the running one may lag behind: keys in the order of their scores,
+    over powers of two from 2^-60 to 2^60 of weight."""
+    c = Attn([900], 1, 1, 1, 16, 16, dtype, cache, scale=1.0, seed=9)
+    rows = np.zeros((900, 1, 16), dtype=np.float32)
+    ramp = np.linspace(-42, 42, 900)
+    rows[:, 0, 0] = torch.from_numpy(ramp if order == "up" else ramp[::-1].copy()).to(TYPES[dtype]).float().numpy()
+    for i in range(900):
+        got = c.pool.put(0, i, rows[i], c.v[0][i].astype(np.float32) if cache not in oracle.LARGEST else rows[i] * 0.1 + 1)
+        c.k[0][i], c.v[0][i] = got
+    c.c = c.pool.device()
+    c.h = lib.DeviceKvAttn(c.c, 1, 1, 1, 900, scale=1.0)
+    q = torch.zeros(1, 1, 1, 16)
+    q[..., 0] = 1
+    c.q, c.q64 = q.to(TYPES[dtype]).cuda(), q.double().numpy()
+    c.run().check()
+
+
+def test_keys_and_values_in_one_pool_and_shared_pages():
+    c = Attn([100, 100], 1, 2, 2, 64, 16, "bf16", "bf16", seed=10)
+    one = lib.DeviceKvCache(c.c.k_pages, c.c.k_pages)
+    c.h = lib.DeviceKvAttn(one, 2, 1, 4, 100)
+    c.v = c.k
+    c.run().check()
+    # the second sequence begins with the first one's pages
+    c.table[1, :4] = c.table[0, :4]
+    c.k[1][:64] = c.k[0][:64]
+    c.run().check()
+
+
+def _in_64_bits(c, b, h):
+    """out and lse of a sequence's head of queries on the GPU, T = 1; and magnitudes, for its bound."""
+    n, kv = c["lengths"][b], h // c["G"]
+    ids = c["table"][b, :-(-n // c["page"])].long()
+    rows = []
+    for pages, scales in ((c["c"].k_pages, c["c"].k_scales), (c["c"].v_pages, c["c"].v_scales)):
+        x = pages.view(torch.uint8)[ids, kv].view(pages.dtype) if pages.dtype == torch.float8_e4m3fn else pages[ids, kv]
+        x = x.double()
+        if scales is not None:
+            x = x * scales[ids, kv].double()[..., None]
+        rows.append(x.reshape(-1, pages.shape[3])[:n])
+    q = c["q"][b, 0, h].double()
+    s = rows[0] @ q * c["scale"]
+    w = torch.softmax(s, 0)
+    mag = rows[0].abs() @ q.abs() * c["scale"]
+    return w @ rows[1], torch.logsumexp(s, 0), w @ rows[1].abs(), float(mag.max()), float(s.abs().max())
+
+
+# Long sequences, many of them, offsets past 32 bits: a pool of 5 GB in bf16.  Against float64 on the GPU, some heads of each.
+@pytest.mark.parametrize("lengths, heads, G, D, page, dtype, cache, spread", [
+    ([131071, 3, 70000], 2, 4, 128, 128, "bf16", "int8", 1), ([40000, 39999], 8, 1, 64, 16, "f32", "f32", 1), ([9000] * 40, 4, 8, 128, 64, "bf16", "bf16", 1),
+    (list(range(1, 601)), 2, 2, 32, 16, "bf16", "e4m3", 1), ([5000, 60000], 8, 2, 128, 64, "bf16", "bf16", 36)])
+def test_attention_of_long_sequences(lengths, heads, G, D, page, dtype, cache, spread):
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    counts = [-(-n // page) for n in lengths]
+    P = sum(counts) * spread
+    ids = torch.randperm(P, device="cuda", generator=gen)[:sum(counts)].to(torch.int32)
+    ids[-1] = P - 1 if not (ids == P - 1).any() else ids[-1]
+    table = torch.full((len(lengths), max(counts)), -1, device="cuda", dtype=torch.int32)
+    for b, part in enumerate(ids.split(counts)):
+        table[b, :len(part)] = part
+    t = TYPES[cache]
+    make = lambda: torch.randn(P, heads, page, D, device="cuda", generator=gen) * 1.3  # noqa: E731
+    if cache in oracle.LARGEST:
+        codes = lambda: (make() * 40).clamp(-127, 127).to(t)  # noqa: E731
+        scales = lambda: torch.rand(P, heads, page, device="cuda", generator=gen) * 0.03 + 0.01  # noqa: E731
+        c = lib.DeviceKvCache(codes(), codes(), scales(), scales(), dtype=dtype)
+    else:
+        pages = []
+        for _ in range(2):
+            x = torch.empty(P, heads, page, D, device="cuda", dtype=t)
+            for part in x.split(4096):
+                part.normal_(generator=gen)
+            pages.append(x)
+        c = lib.DeviceKvCache(*pages)
+    q = torch.randn(len(lengths), 1, heads * G, D, device="cuda", generator=gen).to(TYPES[dtype])
+    h = lib.DeviceKvAttn(c, len(lengths), 1, heads * G, max(lengths))
+    lse = torch.empty(len(lengths), 1, heads * G, device="cuda")
+    out = h.fwd(q, table, torch.tensor(lengths, dtype=torch.int32, device="cuda"), lse=lse)
+    what = dict(lengths=lengths, G=G, page=page, table=table, c=c, q=q, scale=D ** -0.5)
+    for b in (range(len(lengths)) if len(lengths) < 10 else range(0, len(lengths), len(lengths) // 9)):
+        for head in (0, heads * G - 1):
+            o, l, mag, qk, top = _in_64_bits(what, b, head)
+            # weights' errors are independent of each other's sign, but count in full here; sums of n: in runs of 32 and of a wave's steps
+            n = lengths[b]
+            ds = 2 * (D + 8) * U * qk + 8 * U * top
+            rel = 2 * ds + 2 * (6 + 2 * top) * U + 4 * (n / 8 + 64) * U + (2.0 ** -16 if dtype == "bf16" else 2.0 ** -22)
+            bound = rel * mag + (BF if dtype == "bf16" else 0) * (o.abs() + rel * mag)
+            assert ((out[b, 0, head].double() - o).abs() <= bound).all(), (b, head)
+            assert abs(float(lse[b, 0, head]) - float(l)) <= ds + (6 + 2 * top + 2 * (n / 8 + 64)) * U + abs(float(l)) * 4 * U
+
+
+def test_long_lists_of_rows_and_offsets_past_32_bits():
+    """More rows than fit the launch one after the other, and a pool of 5 GB."""
+    heads, page, D = 4, 64, 128
+    P = 5 * 2 ** 30 // (heads * page * D * 2)
+    pages = torch.zeros(P, heads, page, D, device="cuda", dtype=torch.bfloat16)
+    c = lib.DeviceKvCache(pages, torch.zeros_like(pages))
+    N = 300000
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    table = torch.randperm(P, device="cuda", generator=gen).to(torch.int32)[None]
+    pos = torch.randperm(P * page, device="cuda", generator=gen)[:N].to(torch.int32)
+    pos[0] = P * page - 1
+    pos = pos.unique().flip(0).contiguous()
+    N = len(pos)
+    seq = torch.zeros(N, dtype=torch.int32, device="cuda")
+    k = torch.randn(N, heads, D, device="cuda", generator=gen).bfloat16()
+    c.write(k, -k, seq, pos, table)
+    got_k, got_v = c.read(seq, pos, table)
+    assert torch.equal(got_k, k) and torch.equal(got_v, -k)
+    at = table[0, (pos // page).long()].long()
+    assert torch.equal(c.k_pages[at, :, (pos % page).long()], k)
+    assert int((c.k_pages != 0).any(dim=3).sum()) <= N * heads
+
+
+def test_calls_are_alike_and_captured():
+    """The same bits again, on another stream, and from graphs that are replayed with eager calls between them; two graphs that share a workspace."""
+    c = Attn([900, 40, 513, 1300], 2, 2, 4, 128, 64, "bf16", "int8", seed=11).run()
+    out, lse = c.out.clone(), c.lse.clone()
+    c.run()
+    assert torch.equal(c.out, out) and torch.equal(c.lse, lse)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = c.h.fwd(c.q, c.table, c.len_d)
+    side.synchronize()
+    assert torch.equal(other, out)
+    short = torch.tensor([90, 4, 51, 130], dtype=torch.int32, device="cuda")
+    want_short = c.h.fwd(c.q, c.table, short).clone()
+    graphs, outs = [], []
+    for lengths in (c.len_d, short):
+        o = torch.empty_like(out)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            c.h.fwd(c.q, c.table, lengths, o)
+        graphs.append(g)
+        outs.append(o)
+    for _ in range(4):
+        for g, o, want in zip(graphs, outs, (out, want_short)):
+            o.zero_()
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(o, want)
+        assert torch.equal(c.h.fwd(c.q, c.table, c.len_d), out)
+    # lengths are data of the graph
+    short.copy_(c.len_d)
+    graphs[1].replay()
+    torch.cuda.synchronize()
+    assert torch.equal(outs[1], out)
+
+
+def test_lengths_are_clamped():
+    c = Attn([50, 64], 1, 1, 2, 32, 16, "bf16", "bf16", seed=12, max_len=64).run()
+    out = c.out.clone()
+    c.len_d.copy_(torch.tensor([50, 2 ** 31 - 1], dtype=torch.int32))
+    assert torch.equal(c.h.fwd(c.q, c.table, c.len_d), out)
+    c.len_d.copy_(torch.tensor([-5, -2 ** 31], dtype=torch.int32))
+    lse = torch.empty(2, 1, 2, device="cuda")
+    assert not c.h.fwd(c.q, c.table, c.len_d, lse=lse).any() and torch.isneginf(lse).all()
+
+
+def test_refusals_of_the_handles():
+    c = Attn([20, 30], 1, 2, 2, 32, 16, "bf16", "int8", seed=13)
+    k = torch.zeros(3, 2, 32, device="cuda", dtype=torch.bfloat16)
+    i = torch.zeros(3, device="cuda", dtype=torch.int32)
+
+    def code(f):
+        with pytest.raises(bd.AttnSoftmaxError) as e:
+            f()
+        return e.value.code
+
+    assert code(lambda: lib.DeviceKvCache(c.c.k_pages, c.c.v_pages, c.c.k_scales, dtype="bf16")) == 1
+    assert code(lambda: lib.DeviceKvCache(c.c.k_pages, c.c.v_pages, c.c.k_scales, c.c.v_scales)) == 3
+    assert code(lambda: lib.DeviceKvCache(c.c.k_pages.half(), c.c.v_pages.half())) == 3
+    assert code(lambda: lib.DeviceKvCache(c.c.k_pages.bfloat16(), c.c.v_pages.float())) == 3
+    assert code(lambda: lib.DeviceKvCache(c.c.k_pages.bfloat16(), c.c.v_pages.bfloat16(), c.c.k_scales, c.c.v_scales)) == 1
+    assert code(lambda: lib.DeviceKvCache(c.c.k_pages.bfloat16(), c.c.v_pages.bfloat16(), dtype="f32")) == 3
+    assert code(lambda: lib.DeviceKvCache(c.c.k_pages, c.c.v_pages[1:], c.c.k_scales, c.c.v_scales, dtype="bf16")) == 2
+    assert code(lambda: c.c.write(k.float(), k, i, i, c.table)) == 3
+    assert code(lambda: c.c.write(k[:2], k, i, i, c.table)) == 2
+    assert code(lambda: c.c.write(k.transpose(0, 1).contiguous().transpose(0, 1), k, i, i, c.table)) == 5
+    assert code(lambda: c.c.write(k, k, i.long(), i, c.table)) == 3
+    assert code(lambda: c.c.write(k, k, i, i.cpu(), c.table)) == 2
+    assert code(lambda: c.c.write(k, k, i, i, c.table[0])) == 2
+    assert code(lambda: c.c.write(k, k, i, i, None)) == 1
+    assert code(lambda: c.c.read(i, i, c.table, k=k.float())) == 3
+    assert code(lambda: c.h.fwd(c.q, c.table, c.len_d.long())) == 3
+    assert code(lambda: c.h.fwd(c.q, c.table[:, :1], c.len_d)) == 2
+    assert code(lambda: c.h.fwd(c.q, c.table[:1], c.len_d)) == 2
+    assert code(lambda: c.h.fwd(c.q.float(), c.table, c.len_d)) == 3
+    assert code(lambda: c.h.fwd(c.q[..., :16], c.table, c.len_d)) == 2
+    assert code(lambda: lib.DeviceKvAttn(c.c, 2, 1, 3, 30)) == 2
+    assert code(lambda: lib.DeviceKvAttn(c.c, 2, 1, 4, 0)) == 2
+    assert code(lambda: lib.DeviceKvAttn(c.c, 2, 1, 4, 30, window=-1)) == 2
+    # no rows at all
+    none = torch.zeros(0, device="cuda", dtype=torch.int32)
+    c.c.write(k[:0], k[:0], none, none, c.table)
+    assert c.c.read(none, none, c.table)[0].shape == (0, 2, 32)
