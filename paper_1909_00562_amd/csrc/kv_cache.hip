@@ -61,8 +61,10 @@ __device__ __forceinline__ int64_t row_of(const KvMove& a, int32_t b, int32_t p)
   return (int64_t)id * a.heads * a.page + (p - col * a.page);
 }
 
-__device__ __forceinline__ void ld8(const uint16_t* p, float (&x)[8]) {
-  const ku32x4_t q = *reinterpret_cast<const ku32x4_t*>(p);
+// PAST: past the caches
+template <bool PAST = false> __device__ __forceinline__ void ld8(const uint16_t* p, float (&x)[8]) {
+  const ku32x4_t* from = reinterpret_cast<const ku32x4_t*>(p);
+  const ku32x4_t q = PAST ? __builtin_nontemporal_load(from) : *from;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const uint32_t w = q[i];
@@ -70,32 +72,42 @@ __device__ __forceinline__ void ld8(const uint16_t* p, float (&x)[8]) {
     x[2 * i + 1] = hi_bf16(w);
   }
 }
-__device__ __forceinline__ void ld8(const float* p, float (&x)[8]) {
+template <bool PAST = false> __device__ __forceinline__ void ld8(const float* p, float (&x)[8]) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const f32x4_t q = *reinterpret_cast<const f32x4_t*>(p + 4 * h);
+    const f32x4_t* from = reinterpret_cast<const f32x4_t*>(p + 4 * h);
+    const f32x4_t q = PAST ? __builtin_nontemporal_load(from) : *from;
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[4 * h + i] = q[i];
   }
 }
-__device__ __forceinline__ void st8(uint16_t* p, const float (&x)[8]) {
-  *reinterpret_cast<ku32x4_t*>(p) = ku32x4_t{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
+template <bool PAST, typename V> __device__ __forceinline__ void st_vec(V* p, V v) {
+  if constexpr (PAST) __builtin_nontemporal_store(v, p);
+  else *p = v;
 }
-__device__ __forceinline__ void st8(float* p, const float (&x)[8]) {
-  *reinterpret_cast<f32x4_t*>(p) = f32x4_t{x[0], x[1], x[2], x[3]};
-  *reinterpret_cast<f32x4_t*>(p + 4) = f32x4_t{x[4], x[5], x[6], x[7]};
+template <bool PAST = false> __device__ __forceinline__ void st8(uint16_t* p, const float (&x)[8]) {
+  st_vec<PAST>(reinterpret_cast<ku32x4_t*>(p), ku32x4_t{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])});
+}
+template <bool PAST = false> __device__ __forceinline__ void st8(float* p, const float (&x)[8]) {
+  st_vec<PAST>(reinterpret_cast<f32x4_t*>(p), f32x4_t{x[0], x[1], x[2], x[3]});
+  st_vec<PAST>(reinterpret_cast<f32x4_t*>(p + 4), f32x4_t{x[4], x[5], x[6], x[7]});
 }
 
 // eight codes
 template <int TYPE> __device__ __forceinline__ ku32x2_t encode8(const float (&x)[8], float inv) {
+#pragma clang fp contract(off)   // the product is a float before it is rounded to a code
   ku32x2_t q;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     if constexpr (TYPE == KC_INT8) {
-      uint32_t w = 0;
+      // of 1.5 2^23 + x the lowest bits are x's, rounded to even
+      uint32_t w[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w |= ((uint32_t)(int32_t)rintf(x[4 * h + i] * inv) & 0xffu) << (8 * i);
-      q[h] = w;
+      for (int i = 0; i < 4; ++i) {
+        const float y = x[4 * h + i] * inv;
+        w[i] = __builtin_bit_cast(uint32_t, y + 12582912.f);
+      }
+      q[h] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(w[3], w[2], 0x0c0c0400u), __builtin_amdgcn_perm(w[1], w[0], 0x0c0c0400u), 0x05040100u);
     } else {
       int w = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * h] * inv, x[4 * h + 1] * inv, 0, false);
       w = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * h + 2] * inv, x[4 * h + 3] * inv, w, true);
@@ -121,9 +133,26 @@ template <int TYPE> __device__ __forceinline__ void decode8(ku32x2_t q, float sc
   }
 }
 
+template <int PATTERN> __device__ __forceinline__ uint32_t max_with(uint32_t x) {
+  const uint32_t y = (uint32_t)__builtin_amdgcn_mov_dpp((int)x, PATTERN, 0xf, 0xf, true);
+  return x > y ? x : y;
+}
+// over 2^lanes_log neighbouring lanes (the same for all)
+__device__ __forceinline__ uint32_t max_of_lanes(uint32_t x, int lanes_log) {
+  x = max_with<0xb1>(x);                        // lanes 1 apart
+  if (lanes_log > 1) x = max_with<0x4e>(x);     // 2 apart
+  if (lanes_log > 2) x = max_with<0x141>(x);    // the other half of 8
+  if (lanes_log > 3) x = max_with<0x140>(x);    // the other half of 16
+  if (lanes_log > 4) {
+    const auto p = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = p[0] > p[1] ? p[0] : p[1];
+  }
+  return x;
+}
+
 // A wave moves the same head of keys or of values of ROWS tokens to each of its groups of lanes, neighbours side by side: in the pool their
 // rows and their scales follow each other, and the loads of all are on their way together.
-template <typename TE, int TYPE, bool WRITE, int ROWS> __global__ __launch_bounds__(256) void kv_move_kernel(KvMove a) {
+template <typename TE, int TYPE, bool WRITE, int ROWS, bool PAST> __global__ __launch_bounds__(256) void kv_move_kernel(KvMove a) {
   constexpr bool kCoded = TYPE == KC_INT8 || TYPE == KC_E4M3;
   const int groups = 64 >> a.lanes_log, lane = threadIdx.x & ((1 << a.lanes_log) - 1), d = lane * 8;
   const int quads = (2 * a.heads + 3) / 4, tile = blockIdx.x / quads, hh = (blockIdx.x - tile * quads) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -143,7 +172,7 @@ template <typename TE, int TYPE, bool WRITE, int ROWS> __global__ __launch_bound
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[i][e] = 0.f;
     if constexpr (WRITE)
-      if (here) ld8(reinterpret_cast<const TE*>(a.src[of_v]) + at * a.ld[of_v] + h * a.D + d, x[i]);
+      if (here) ld8<PAST>(reinterpret_cast<const TE*>(a.src[of_v]) + at * a.ld[of_v] + h * a.D + d, x[i]);
   }
 #pragma unroll
   for (int i = 0; i < ROWS; ++i) {
@@ -163,10 +192,7 @@ template <typename TE, int TYPE, bool WRITE, int ROWS> __global__ __launch_bound
           const uint32_t m = __builtin_bit_cast(uint32_t, x[i][e]) & 0x7fffffffu;
           top = m > top ? m : top;
         }
-        for (int o = 1; o < 1 << a.lanes_log; o <<= 1) {
-          const uint32_t m = __shfl_xor(top, o, 64);
-          top = m > top ? m : top;
-        }
+        top = max_of_lanes(top, a.lanes_log);
         constexpr float kLargest = TYPE == KC_INT8 ? 127.f : 448.f;
         const bool finite = top < 0x7f800000u;
         const float scale = fmaxf(__builtin_bit_cast(float, top) / kLargest, 0x1p-120f), inv = finite ? 1.f / scale : 0.f;
@@ -200,7 +226,7 @@ template <typename TE, int TYPE, bool WRITE, int ROWS> __global__ __launch_bound
       const int n = n0 + i * groups;
       if (!here || n >= a.N) continue;
       if constexpr (kCoded) decode8<TYPE>(q[i], scale[i], x[i]);
-      st8(reinterpret_cast<TE*>(a.dst[of_v]) + ((int64_t)n * a.heads + h) * a.D + d, x[i]);
+      st8<PAST>(reinterpret_cast<TE*>(a.dst[of_v]) + ((int64_t)n * a.heads + h) * a.D + d, x[i]);
     }
   }
 }
@@ -214,8 +240,11 @@ template <bool WRITE> as_status move(const kc_cache* c, const KvMove& a, hipStre
   auto run = [&](auto* t, auto type) {
     using TE = typename std::remove_pointer<decltype(t)>::type;
     constexpr int TYPE = decltype(type)::value;
-    if (few) hipLaunchKernelGGL((kv_move_kernel<TE, TYPE, WRITE, 1>), dim3((unsigned)blocks), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((kv_move_kernel<TE, TYPE, WRITE, 4>), dim3((unsigned)blocks), dim3(256), 0, st, a);
+    // The dense side past the caches where it is more than they may keep for the next reader.  us, int8, rows of 256 MB through / past them:
+    // write 104 / 97, read 115 / 63; of 128 MB 47 / 50 and 36 / 34; of 64 MB 25 / 27 and 20 / 19.
+    const bool past = (int64_t)a.N * 2 * a.heads * a.D * sizeof(TE) > (int64_t)96 << 20;
+    auto kfn = few ? kv_move_kernel<TE, TYPE, WRITE, 1, false> : past ? kv_move_kernel<TE, TYPE, WRITE, 4, true> : kv_move_kernel<TE, TYPE, WRITE, 4, false>;
+    hipLaunchKernelGGL(kfn, dim3((unsigned)blocks), dim3(256), 0, st, a);
   };
   auto any = [&](auto* t, auto same) {
     if (c->cache_type == KC_INT8) run(t, std::integral_constant<int, KC_INT8>{});
