@@ -114,7 +114,57 @@ template <int WAVES> __device__ __forceinline__ Cut cut_all(const KvAttnDev& a, 
 struct Run {
   int32_t b, hr, chunk, left;
 };
+// lanes' sums up to and including their own
+__device__ __forceinline__ int32_t scan_lanes(int32_t n) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int32_t x = __shfl_up(n, o, 64);
+    if (lane >= o) n += x;
+  }
+  return n;
+}
+// Up to 64 sequences a wave cuts by itself, a lane for each: its chunks, and its units for all heads with those of the sequences ahead.
+struct LaneCut {
+  Cut cut;
+  int32_t chunks, own, ahead;
+};
+__device__ __forceinline__ LaneCut cut_lanes(const KvAttnDev& a, int blocks) {
+  const int lane = threadIdx.x & 63;
+  LaneCut r;
+  r.chunks = lane < a.B ? seq_span(a, lane).chunks : 0;
+  const int32_t hrs = a.heads * a.row_groups, upto = scan_lanes(r.chunks);
+  r.cut = cut_of(a, __builtin_amdgcn_readlane(upto, 63), blocks);
+  const int32_t units = r.cut.units(r.chunks);
+  r.own = units * hrs;
+  r.ahead = (r.cut.pieces ? scan_lanes(units) : upto) * hrs - r.own;
+  return r;
+}
+// what a block does of sequence b, from unit `rest` of it on
+__device__ __forceinline__ Run run_of(const Cut& c, int32_t b, int32_t n, int32_t rest, int32_t at) {
+  Run r;
+  r.b = b;
+  const int32_t units = c.units(n);
+  r.hr = rest / units;
+  const int32_t unit = rest - r.hr * units;
+  if (c.pieces) {
+    r.chunk = (int32_t)((int64_t)unit * n / units);
+    r.left = (int32_t)((int64_t)(unit + 1) * n / units) - r.chunk;
+  } else {
+    r.chunk = unit;
+    r.left = c.total - at < c.per ? c.total - at : c.per;
+  }
+  return r;
+}
 template <int WAVES> __device__ __forceinline__ Run cut_run(const KvAttnDev& a, int32_t* s_sum, int32_t* s_found) {
+  if (a.B <= 64) {
+    const LaneCut l = cut_lanes(a, gridDim.x);
+    const int32_t at = l.cut.pieces ? (int32_t)blockIdx.x : (int32_t)blockIdx.x * l.cut.per;
+    const uint64_t here = __ballot(at >= l.ahead && at < l.ahead + l.own);
+    if (!here) return {0, 0, 0, 0};
+    const int b = __builtin_ctzll(here);
+    return run_of(l.cut, b, __builtin_amdgcn_readlane(l.chunks, b), at - __builtin_amdgcn_readlane(l.ahead, b), at);
+  }
   const Cut c = cut_all<WAVES>(a, gridDim.x, s_sum);
   const int32_t hrs = a.heads * a.row_groups, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int32_t at = c.pieces ? (int32_t)blockIdx.x : (int32_t)blockIdx.x * c.per;   // in units, as is what follows
@@ -148,18 +198,7 @@ template <int WAVES> __device__ __forceinline__ Run cut_run(const KvAttnDev& a, 
   }
   if (!found) return r;                   // (the same in all threads)
   __syncthreads();
-  r.b = s_found[0];
-  const int32_t rest = at - s_found[1], n = seq_span(a, r.b).chunks, units = c.units(n);
-  r.hr = rest / units;
-  const int32_t unit = rest - r.hr * units;
-  if (c.pieces) {
-    r.chunk = (int32_t)((int64_t)unit * n / units);
-    r.left = (int32_t)((int64_t)(unit + 1) * n / units) - r.chunk;
-  } else {
-    r.chunk = unit;
-    r.left = c.total - at < c.per ? c.total - at : c.per;
-  }
-  return r;
+  return run_of(c, s_found[0], seq_span(a, s_found[0]).chunks, at - s_found[1], at);
 }
 
 // ---- fragments --------------------------------------------------------------------
@@ -168,17 +207,13 @@ __device__ __forceinline__ uint32_t top_halves(float lo, float hi) {   // two fl
   return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302u);
 }
 
-template <int TYPE> __device__ __forceinline__ void codes_to_floats(uint32_t w, float (&x)[4]) {
-  if constexpr (TYPE == KC_INT8) {
+// bytes 2 HIGH and 2 HIGH + 1 of a word of e4m3 codes as bf16, which holds them
+template <bool HIGH> __device__ __forceinline__ uint32_t e4m3_to_bf16(uint32_t w) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, HIGH));
+}
+__device__ __forceinline__ void int8_to_floats(uint32_t w, float (&x)[4]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = (float)(int8_t)(w >> (8 * i));
-  } else {
-    const auto p = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), q = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
-    x[0] = p[0];
-    x[1] = p[1];
-    x[2] = q[0];
-    x[3] = q[1];
-  }
+  for (int i = 0; i < 4; ++i) x[i] = (float)(int8_t)(w >> (8 * i));
 }
 
 // offsets from `bytes` on read as 0
@@ -308,6 +343,25 @@ template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__((Form<TYPE, 
     // tokens that all rows of all t see
     const int32_t all_hi = len - a.T, all_lo = a.window > 0 ? len - a.window : 0;
 
+    // the first tiles' pages are looked up ahead of everything else
+    const int32_t* table = a.table + (int64_t)b * a.max_pages;
+    // the table's entry for the tile at pos (past the end: the last one)
+    auto page_of = [&](int32_t pos) {
+      const uint32_t tile = (uint32_t)(pos < len ? pos : len - 1) >> 4, col = kv_div(tile, a.magic);
+      return __builtin_amdgcn_readfirstlane(table[col]);
+    };
+    const int32_t stride = tok_waves * STEP;
+    int32_t pos = tok0 + tok_wave * STEP;
+    int32_t id[NT], id_next[NT];
+    const bool any_steps = tok_wave < tok_waves && pos < tok1 && row0 < a.R;
+    if (any_steps) {
+#pragma unroll
+      for (int u = 0; u < NT; ++u) {
+        id[u] = page_of(pos + u * kKvTile);
+        id_next[u] = page_of(pos + stride + u * kKvTile);
+      }
+    }
+
     // queries
     constexpr int QF = F::kF32 ? DP / 16 : DP / 32;   // fragments: of 4 floats, or of 8 bf16
     float qf[F::kF32 ? QF : 1][4];
@@ -363,12 +417,6 @@ template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__((Form<TYPE, 
     float ks[NT][4], vs[NT][4];
     int32_t k_valid[NT];                  // tokens that there are of a tile: up to 16, 0 where there is no page
     const int32_t row_bytes = a.D * F::kBytes;
-    const int32_t* table = a.table + (int64_t)b * a.max_pages;
-    // the table's entry for the tile at pos (past the end: the last one)
-    auto page_of = [&](int32_t pos) {
-      const uint32_t tile = (uint32_t)(pos < len ? pos : len - 1) >> 4, col = kv_div(tile, a.magic);
-      return __builtin_amdgcn_readfirstlane(table[col]);
-    };
     // the tile's first row in the pool, and how many of its tokens there are
     auto place = [&](int32_t pos, int32_t id, int32_t& valid) {
       const uint32_t tile = (uint32_t)pos >> 4, col = kv_div(tile, a.magic);
@@ -418,19 +466,31 @@ template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__((Form<TYPE, 
         for (int j = 0; j < NO; ++j)
 #pragma unroll
           for (int i = 0; i < 4; ++i) use(j, i, __builtin_bit_cast(float, raw(0, i, j / F::kVW, j % F::kVW)));
-      } else if constexpr (F::kCoded) {
+      } else if constexpr (TYPE == KC_INT8) {
 #pragma unroll
         for (int w = 0; w < F::kVDwords; ++w) {
           float x[2][4][4];
 #pragma unroll
           for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) codes_to_floats<TYPE>(raw(u, i, 0, w), x[u][i]);
+            for (int i = 0; i < 4; ++i) int8_to_floats(raw(u, i, 0, w), x[u][i]);
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             use(w * 4 + e, as_frag(au32x4_t{top_halves(x[0][0][e], x[0][1][e]), top_halves(x[0][2][e], x[0][3][e]),
                                             top_halves(x[1][0][e], x[1][1][e]), top_halves(x[1][2][e], x[1][3][e])}));
         }
+      } else if constexpr (TYPE == KC_E4M3) {
+#pragma unroll
+        for (int w = 0; w < F::kVDwords; ++w)
+#pragma unroll
+          for (int e = 0; e < 4; e += 2) {
+            // codes e and e + 1 of two tokens, side by side
+            const uint32_t sel = e ? 0x07030602u : 0x05010400u;
+            auto two = [&](int u, int i) { return __builtin_amdgcn_perm(raw(u, i + 1, 0, w), raw(u, i, 0, w), sel); };
+            const uint32_t x[4] = {two(0, 0), two(0, 2), two(1, 0), two(1, 2)};
+            use(w * 4 + e, as_frag(au32x4_t{e4m3_to_bf16<false>(x[0]), e4m3_to_bf16<false>(x[1]), e4m3_to_bf16<false>(x[2]), e4m3_to_bf16<false>(x[3])}));
+            use(w * 4 + e + 1, as_frag(au32x4_t{e4m3_to_bf16<true>(x[0]), e4m3_to_bf16<true>(x[1]), e4m3_to_bf16<true>(x[2]), e4m3_to_bf16<true>(x[3])}));
+          }
       } else {
 #pragma unroll
         for (int h = 0; h < F::kVHalves; ++h)
@@ -443,16 +503,9 @@ template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__((Form<TYPE, 
       }
     };
 
-    const int32_t stride = tok_waves * STEP;
-    int32_t pos = tok0 + tok_wave * STEP;
-    int32_t id[NT], id_next[NT];
-    if (tok_wave < tok_waves && pos < tok1 && row0 < a.R) {
-#pragma unroll
-      for (int u = 0; u < NT; ++u) id[u] = page_of(pos + u * kKvTile);
+    if (any_steps) {
       load_k(pos, id);
       load_v();
-#pragma unroll
-      for (int u = 0; u < NT; ++u) id_next[u] = page_of(pos + stride + u * kKvTile);
       for (; pos < tok1; pos += stride) {
         // S^T
         f32x4_t s[NT] = {};
@@ -471,13 +524,19 @@ template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__((Form<TYPE, 
             };
 #pragma unroll
             for (int j = 0; j < F::kKLoads; ++j) {
-              if constexpr (F::kCoded) {
+              if constexpr (TYPE == KC_INT8) {
 #pragma unroll
                 for (int w = 0; w < 2; ++w) {
                   float x[4], y[4];
-                  codes_to_floats<TYPE>(kr[u][j][2 * w], x);
-                  codes_to_floats<TYPE>(kr[u][j][2 * w + 1], y);
+                  int8_to_floats(kr[u][j][2 * w], x);
+                  int8_to_floats(kr[u][j][2 * w + 1], y);
                   add(2 * j + w, au32x4_t{top_halves(x[0], x[1]), top_halves(x[2], x[3]), top_halves(y[0], y[1]), top_halves(y[2], y[3])});
+                }
+              } else if constexpr (TYPE == KC_E4M3) {
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+                  const uint32_t x = kr[u][j][2 * w], y = kr[u][j][2 * w + 1];
+                  add(2 * j + w, au32x4_t{e4m3_to_bf16<false>(x), e4m3_to_bf16<true>(x), e4m3_to_bf16<false>(y), e4m3_to_bf16<true>(y)});
                 }
               } else {
                 add(j, au32x4_t{kr[u][j][0], kr[u][j][1], kr[u][j][2], kr[u][j][3]});
@@ -640,14 +699,27 @@ template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__((Form<TYPE, 
     const int quads = a.D / 4, rows_here = a.R - group * a.group_rows < a.group_rows ? a.R - group * a.group_rows : a.group_rows;
     for (int x = threadIdx.x; x < rows_here * quads; x += WAVES * 64) {
       const int r = x / quads, d = (x - r * quads) * 4, tile = r >> 4, r16 = r & 15;
-      float top = -INFINITY, sum = 0.f;
-      for (int w = tile; w < tok_waves * a.tile_waves; w += a.tile_waves) top = fmaxf(top, lds_ml[(w * 16 + r16) * 2]);
+      // (all waves' at once: those of other tiles of rows do not count, whatever they are)
+      float ms[WAVES], ls[WAVES];
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {
+        ms[w] = lds_ml[(w * 16 + r16) * 2];
+        ls[w] = lds_ml[(w * 16 + r16) * 2 + 1];
+        if (w % a.tile_waves != tile) ms[w] = -INFINITY;
+      }
+      float top = ms[0], sum = 0.f;
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w) top = fmaxf(top, ms[w]);
       const float use = top == -INFINITY ? 0.f : top;
       f32x4_t v = {};
-      for (int w = tile; w < tok_waves * a.tile_waves; w += a.tile_waves) {
-        const float f = __builtin_amdgcn_exp2f(lds_ml[(w * 16 + r16) * 2] - use);
-        sum += f * lds_ml[(w * 16 + r16) * 2 + 1];
-        v += f * *reinterpret_cast<const f32x4_t*>(lds + (w * 16 + r16) * LD + d);
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {
+        const float f = __builtin_amdgcn_exp2f(ms[w] - use);
+        const f32x4_t part = *reinterpret_cast<const f32x4_t*>(lds + (w * 16 + r16) * LD + d);
+        if (w % a.tile_waves == tile) {
+          sum += f * ls[w];
+          v += f * part;
+        }
       }
       const int rr = group * a.group_rows + r;
       if (whole) {
@@ -692,12 +764,21 @@ template <bool F32Q, int WAVES> __global__ __launch_bounds__(WAVES * 64) void kv
   const int r = blockIdx.y, rr = group * a.group_rows + r;
   if (rr >= a.R) return;
   const SeqSpan span = seq_span(a, b);
-  const Cut cut = cut_all<WAVES>(a, blocks, s_sum);
   int32_t k0 = 0, parts = 0;              // the first block that has some of it, and how many
   if (span.chunks > 0) {
-    int32_t n = 0;
-    for (int i = threadIdx.x; i < b; i += THREADS) n += cut.units(seq_span(a, i).chunks);
-    const int32_t units = cut.units(span.chunks), at = sum_of_waves<WAVES>(n, s_sum) * hrs + hr * units;
+    Cut cut;
+    int32_t ahead;                        // units of the sequences ahead
+    if (a.B <= 64) {
+      const LaneCut l = cut_lanes(a, blocks);
+      cut = l.cut;
+      ahead = __builtin_amdgcn_readlane(l.ahead, b);
+    } else {
+      cut = cut_all<WAVES>(a, blocks, s_sum);
+      int32_t n = 0;
+      for (int i = threadIdx.x; i < b; i += THREADS) n += cut.units(seq_span(a, i).chunks);
+      ahead = sum_of_waves<WAVES>(n, s_sum) * hrs;
+    }
+    const int32_t units = cut.units(span.chunks), at = ahead + hr * units;
     k0 = cut.pieces ? at : at / cut.per;
     parts = cut.pieces ? units : (at + units - 1) / cut.per - k0 + 1;
     if (parts == 1) return;               // one block's, written by it

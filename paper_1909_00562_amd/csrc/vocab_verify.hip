@@ -163,7 +163,7 @@ template <typename TE, int PER> __global__ __launch_bounds__(kVThreads, 8) void 
   constexpr int W = 16 / sizeof(TE), CHUNK = kVThreads * PER;
   __shared__ RowStat s_stat[2 * kVerifyMaxT + 1];
   __shared__ int8_t s_bad[2 * kVerifyMaxT + 1];
-  __shared__ int s_words, s_n, s_state, s_last, s_chunk, s_found, s_some;
+  __shared__ int s_words, s_n, s_state, s_last, s_chunk, s_past[kVThreads / 64], s_some[kVThreads / 64];
   __shared__ double s_r[4], s_ahead, s_theta, s_powers[kPowers];
   const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, T = a.T, V = a.V;
   const int64_t first = (int64_t)b * T;
@@ -338,8 +338,6 @@ template <typename TE, int PER> __global__ __launch_bounds__(kVThreads, 8) void 
       s_chunk = chunk < 0 ? some : chunk;   // (rounding, or u >= 1: the last one with a weight)
       s_theta = left;
       s_state = of_p;
-      s_found = 1 << 30;
-      s_some = -1;
     }
   }
   __syncthreads();
@@ -356,11 +354,21 @@ template <typename TE, int PER> __global__ __launch_bounds__(kVThreads, 8) void 
   if (lane == 63) s_r[wave] = run;
   __syncthreads();
   for (int i = 0; i < wave; ++i) run += s_r[i];
-  if (own > 0 && run > theta) atomicMin(&s_found, tid);
-  if (own > 0) atomicMax(&s_some, tid);
+  // the first thread past theta, and the last one with a weight
+  const uint64_t past = __ballot(own > 0 && run > theta), some = __ballot(own > 0);
+  if (lane == 0) {
+    s_past[wave] = past ? wave * 64 + __builtin_ctzll(past) : kVThreads;
+    s_some[wave] = some ? wave * 64 + 63 - __builtin_clzll(some) : -1;
+  }
   __syncthreads();
-  const bool none = s_found == 1 << 30;      // (as above: the chunk's last word of a weight above 0)
-  const int at = none ? s_some : s_found;
+  int at = kVThreads, last = -1;
+#pragma unroll
+  for (int i = 0; i < kVThreads / 64; ++i) {
+    at = s_past[i] < at ? s_past[i] : at;
+    last = s_some[i] > last ? s_some[i] : last;
+  }
+  const bool none = at == kVThreads;         // (as above: the chunk's last word of a weight above 0)
+  if (none) at = last > 0 ? last : 0;
   if (tid == at) s_ahead = run - own;
   __syncthreads();
   if (wave != 0) return;
@@ -378,7 +386,7 @@ template <typename TE, int PER> __global__ __launch_bounds__(kVThreads, 8) void 
     if (lane >= o) run += x;
   }
   const uint64_t above = __ballot(!none && mine > 0 && s_ahead + run > theta), there = __ballot(mine > 0);
-  if (lane == 0) a.words[first + b + n] = s_chunk * CHUNK + at * PER + (above ? __builtin_ctzll(above) : 63 - __builtin_clzll(there));
+  if (lane == 0) a.words[first + b + n] = s_chunk * CHUNK + at * PER + (above ? __builtin_ctzll(above) : there ? 63 - __builtin_clzll(there) : 0);
 }
 
 struct VerifyLayout {
