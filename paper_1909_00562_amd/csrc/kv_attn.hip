@@ -148,8 +148,9 @@ __device__ __forceinline__ Run run_of(const Cut& c, int32_t b, int32_t n, int32_
   r.hr = rest / units;
   const int32_t unit = rest - r.hr * units;
   if (c.pieces) {
-    r.chunk = (int32_t)((int64_t)unit * n / units);
-    r.left = (int32_t)((int64_t)(unit + 1) * n / units) - r.chunk;
+    const int32_t each = n / units, more = n - each * units;   // the first `more` pieces have one chunk more
+    r.chunk = unit * each + (unit < more ? unit : more);
+    r.left = each + (unit < more);
   } else {
     r.chunk = unit;
     r.left = c.total - at < c.per ? c.total - at : c.per;

@@ -14,6 +14,7 @@
 #include <type_traits>
 
 #include "common.h"
+#include "lds_limit.h"
 #include "status.h"
 
 namespace asx {
@@ -153,6 +154,149 @@ template <typename TE, int PER> __global__ __launch_bounds__(kVThreads) void ver
   if ((tid & 63) == 0) s_sum[wave] = sum;
   __syncthreads();
   if (tid == 0) a.part[(int64_t)blockIdx.y * a.chunks + blockIdx.x] = {(s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]), m, bad};
+}
+
+// The same of many bf16 logits.  Of those there are few different ones: 24 exponents of 128 and two signs are a table of 48 KB, which
+// takes the place of an exponential each by a read of LDS; it is made once by blocks that stay for all chunks.  Sums are relative to
+// 2^0 instead of the chunk's maximum.  A chunk with other logits (64 and more in magnitude, 2^-18 and less, infinities, NaN) goes the general
+// way.  us, 1152 rows of 128000 (295 MB): general 112, this TODO.
+constexpr int kTabThreads = 512, kTabPer = 16, kTabBlocks = 768;
+constexpr uint32_t kTabFirst = (127 - 18) << 7, kTabCount = 24 << 7;   // the lowest magnitude's bits, how many
+constexpr double kTabMost = 1000.0;                                    // 64 c: powers and sums of 2^20 of them are in fp64's range
+typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+__global__ __launch_bounds__(kTabThreads) void verify_stats_table_kernel(VerifyDev a) {
+  static_assert(kTabThreads * kTabPer == kVThreads * kManyPer, "the same chunks");
+  constexpr int WAVES = kTabThreads / 64;
+  extern __shared__ double s_table[];      // [kTabCount + 1][2]: positive and negative ones; zeros for what is not in it
+  __shared__ double s_powers[kPowers], s_sum[2][WAVES];
+  __shared__ int s_odd[2][WAVES];
+  __shared__ float s_m[WAVES];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, rows = 2 * a.T + 1;
+  if (tid < kPowers) make_powers(s_powers);
+  for (int i = tid; i < 2 * ((int)kTabCount + 1); i += kTabThreads) {
+    const double l = bf16_bits_to_f32((uint32_t)(i >> 1) + kTabFirst | (uint32_t)(i & 1) << 15);
+    s_table[i] = i >> 1 < (int)kTabCount ? exp2_64(l * a.c) : 0.0;
+  }
+  if (blockIdx.x == 0)
+    for (int b = tid; b < a.B; b += kTabThreads) a.ticket[b] = 0;
+  __syncthreads();
+  const int64_t items = (int64_t)a.B * rows * a.chunks;
+  int64_t item = blockIdx.x;
+  const uint16_t* from = nullptr;          // of the item's row
+  int v0 = 0;                              // of this thread's first logit
+  // the block's next chunk of a row that is looked at
+  auto find = [&]() {
+    for (; item < items; item += gridDim.x) {
+      const int64_t row = item / a.chunks;
+      const int b = (int)(row / rows), j = (int)(row - (int64_t)b * rows), t = j <= a.T ? j : j - a.T - 1, ahead = j <= a.T ? t : t + 1;
+      bool there = true;
+      for (int i = 0; i < ahead && there; ++i) there = is_word(a.drafted[(int64_t)b * a.T + i], a.V);
+      if (!there) continue;
+      from = j <= a.T ? reinterpret_cast<const uint16_t*>(a.target) + ((int64_t)b * (a.T + 1) + t) * a.ld_target
+                      : reinterpret_cast<const uint16_t*>(a.draft) + ((int64_t)b * a.T + t) * a.ld_draft;
+      v0 = (int)(item - row * a.chunks) * (kTabThreads * kTabPer) + tid * 8;
+      return;
+    }
+  };
+  vu32x4_t next[2];
+  bool next_there[2];
+  auto load = [&]() {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int v = v0 + h * kTabThreads * 8;
+      next_there[h] = v < a.V;
+      if (v + 8 <= a.V) {
+        next[h] = *reinterpret_cast<const vu32x4_t*>(from + v);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t lo = v + 2 * i < a.V ? from[v + 2 * i] : 0xff80u, hi = v + 2 * i + 1 < a.V ? from[v + 2 * i + 1] : 0xff80u;
+          next[h][i] = lo | hi << 16;
+        }
+      }
+    }
+  };
+  find();
+  if (item < items) load();
+  for (int par = 0; item < items; par ^= 1) {
+    const int64_t at = item;
+    vu32x4_t x[2];
+    bool there[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      x[h] = next[h];
+      there[h] = next_there[h];
+    }
+    item += gridDim.x;
+    find();
+    if (item < items) load();
+    double sum = 0, sum2 = 0;
+    u16x2_t most = {0, 0}, least = {0xffff, 0xffff};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (!there[h]) continue;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t w = x[h][i], mag = w & 0x7fff7fffu;
+        most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2_t, mag));
+        least = __builtin_elementwise_min(least, __builtin_bit_cast(u16x2_t, mag));
+        const uint32_t lo = (mag & 0xffffu) - kTabFirst, hi = (mag >> 16) - kTabFirst;
+        sum += s_table[(lo < kTabCount ? lo : kTabCount) * 2 + (w >> 15 & 1)];
+        sum2 += s_table[(hi < kTabCount ? hi : kTabCount) * 2 + (w >> 31)];
+      }
+    }
+    const uint32_t top = most[0] > most[1] ? most[0] : most[1], low = least[0] < least[1] ? least[0] : least[1];
+    const bool odd = __any(top >= kTabFirst + kTabCount || low < kTabFirst);
+    sum = wave_sum64(sum + sum2);
+    if (lane == 0) {
+      s_sum[par][wave] = sum;
+      s_odd[par][wave] = odd;
+    }
+    __syncthreads();
+    int any_odd = 0;
+    sum = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      any_odd |= s_odd[par][w];
+      sum += s_sum[par][w];
+    }
+    if (!any_odd) {
+      if (tid == 0) a.part[at] = {sum, 0.f, 0};
+      continue;
+    }
+    // the general way
+    float m = -INFINITY;
+    int bad = 0;
+    float l[kTabPer];
+#pragma unroll
+    for (int k = 0; k < kTabPer; ++k) {
+      const uint32_t w = x[k / 8][k % 8 / 2];
+      l[k] = there[k / 8] ? (k % 2 ? hi_bf16(w) : lo_bf16(w)) : -INFINITY;
+      m = fmaxf(m, l[k]);
+      bad |= !(l[k] < INFINITY);
+    }
+    m = wave_max(m);
+    bad = __syncthreads_or(bad);
+    if (lane == 0) s_m[wave] = m;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) m = fmaxf(m, s_m[w]);
+    sum = 0;
+    if (m > -INFINITY && !bad) {
+      const double shift = -(double)m * a.c;
+#pragma unroll
+      for (int k = 0; k < kTabPer; ++k) sum += exp2_by_powers(fma((double)l[k], a.c, shift), s_powers);
+    }
+    sum = wave_sum64(sum);
+    __syncthreads();
+    if (lane == 0) s_sum[par][wave] = sum;
+    __syncthreads();
+    if (tid == 0) {
+      sum = 0;
+      for (int w = 0; w < WAVES; ++w) sum += s_sum[par][w];
+      a.part[at] = {sum, m, bad};
+    }
+  }
 }
 
 // ---- the words ---------------------------------------------------------------------
@@ -429,8 +573,17 @@ template <typename TE, int PER> hipError_t launch_verify(const VerifyDev& d, hip
     p.part += (int64_t)b0 * rows * d.chunks;
     p.sums += (int64_t)b0 * d.chunks;
     p.ticket += b0;
-    hipLaunchKernelGGL((verify_stats_kernel<TE, PER>), dim3(d.chunks, p.B * rows), dim3(kVThreads), 0, st, p);
-    hipError_t e = hipGetLastError();
+    hipError_t e;
+    if (sizeof(TE) == 2 && PER == kManyPer && d.c * 64 <= kTabMost && (int64_t)p.B * rows * d.chunks >= 4 * kTabBlocks) {
+      constexpr int smem = 2 * ((int)kTabCount + 1) * 8;
+      static LdsLimit limit;
+      e = limit.raise(reinterpret_cast<const void*>(verify_stats_table_kernel), smem);
+      if (e != hipSuccess) return e;
+      hipLaunchKernelGGL(verify_stats_table_kernel, dim3(kTabBlocks), dim3(kTabThreads), smem, st, p);
+    } else {
+      hipLaunchKernelGGL((verify_stats_kernel<TE, PER>), dim3(d.chunks, p.B * rows), dim3(kVThreads), 0, st, p);
+    }
+    e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((verify_words_kernel<TE, PER>), dim3(d.chunks, p.B), dim3(kVThreads), 0, st, p);
     e = hipGetLastError();
