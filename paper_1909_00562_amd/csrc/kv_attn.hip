@@ -76,7 +76,7 @@ struct Cut {
 };
 // A run that ends one sequence's head and begins the next one's reads two sets of queries and writes two results, which costs as much as
 // some chunks do: short runs are pieces instead, if pieces that are not full leave no more blocks without work than that.
-// us, kernels: 24 sequences of two heads, 1004 tokens seen by 40 rows, runs / pieces TODO.
+// us, kernels: 24 sequences of two heads, 1004 tokens seen by 40 rows, e4m3, runs / pieces 23.3 / 17.8.
 __device__ __forceinline__ Cut cut_of(const KvAttnDev& a, int32_t chunks, int blocks) {
   const int32_t hr = a.heads * a.row_groups;
   Cut c;

@@ -14,7 +14,6 @@
 #include <type_traits>
 
 #include "common.h"
-#include "lds_limit.h"
 #include "status.h"
 
 namespace asx {
@@ -159,15 +158,16 @@ template <typename TE, int PER> __global__ __launch_bounds__(kVThreads) void ver
 // The same of many bf16 logits.  Of those there are few different ones: 24 exponents of 128 and two signs are a table of 48 KB, which
 // takes the place of an exponential each by a read of LDS; it is made once by blocks that stay for all chunks.  Sums are relative to
 // 2^0 instead of the chunk's maximum.  A chunk with other logits (64 and more in magnitude, 2^-18 and less, infinities, NaN) goes the general
-// way.  us, 1152 rows of 128000 (295 MB): general 112, this TODO.
+// way.  us, 1152 rows of 128000 (295 MB): the general way 112, this 85, of which the vector units and LDS (a quarter of its time conflicts of
+// banks) are busy 55 each.
 constexpr int kTabThreads = 512, kTabPer = 16, kTabBlocks = 768;
 constexpr uint32_t kTabFirst = (127 - 18) << 7, kTabCount = 24 << 7;   // the lowest magnitude's bits, how many
 constexpr double kTabMost = 1000.0;                                    // 64 c: powers and sums of 2^20 of them are in fp64's range
 typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
 __global__ __launch_bounds__(kTabThreads) void verify_stats_table_kernel(VerifyDev a) {
-  static_assert(kTabThreads * kTabPer == kVThreads * kManyPer, "the same chunks");
+  static_assert(kTabThreads * kTabPer == kVThreads * kManyPer && 16 * (kTabCount + 1) < 1 << 16, "the same chunks; places in 16 bits");
   constexpr int WAVES = kTabThreads / 64;
-  extern __shared__ double s_table[];      // [kTabCount + 1][2]: positive and negative ones; zeros for what is not in it
+  __shared__ double s_table[2 * (kTabCount + 1)];   // positive and negative ones in turns; zeros for what is not in it
   __shared__ double s_powers[kPowers], s_sum[2][WAVES];
   __shared__ int s_odd[2][WAVES];
   __shared__ float s_m[WAVES];
@@ -180,46 +180,70 @@ __global__ __launch_bounds__(kTabThreads) void verify_stats_table_kernel(VerifyD
   if (blockIdx.x == 0)
     for (int b = tid; b < a.B; b += kTabThreads) a.ticket[b] = 0;
   __syncthreads();
-  const int64_t items = (int64_t)a.B * rows * a.chunks;
-  int64_t item = blockIdx.x;
-  const uint16_t* from = nullptr;          // of the item's row
-  int v0 = 0;                              // of this thread's first logit
-  // the block's next chunk of a row that is looked at
-  auto find = [&]() {
-    for (; item < items; item += gridDim.x) {
-      const int64_t row = item / a.chunks;
-      const int b = (int)(row / rows), j = (int)(row - (int64_t)b * rows), t = j <= a.T ? j : j - a.T - 1, ahead = j <= a.T ? t : t + 1;
-      bool there = true;
-      for (int i = 0; i < ahead && there; ++i) there = is_word(a.drafted[(int64_t)b * a.T + i], a.V);
-      if (!there) continue;
-      from = j <= a.T ? reinterpret_cast<const uint16_t*>(a.target) + ((int64_t)b * (a.T + 1) + t) * a.ld_target
-                      : reinterpret_cast<const uint16_t*>(a.draft) + ((int64_t)b * a.T + t) * a.ld_draft;
-      v0 = (int)(item - row * a.chunks) * (kTabThreads * kTabPer) + tid * 8;
-      return;
+  // An item is a chunk of a row.  While one is added up, the next one's logits are on their way, and the drafted words that say whether
+  // the one behind it is looked at at all.
+  // An item is a chunk of a row.  While one is added up, the next one's logits are on their way, and the drafted words that say whether
+  // the one behind it is looked at at all.
+  struct Item {
+    int b, j, chunk;
+  };
+  auto item_at = [&](int n) {
+    Item i;
+    const int row = n / a.chunks;
+    i.chunk = n - row * a.chunks;
+    i.b = row / rows;
+    i.j = row - i.b * rows;
+    return i;
+  };
+  const Item step = item_at(gridDim.x);
+  auto behind = [&](Item i) {              // (divisions in every step kept the scalar unit busier than the vector units)
+    i.chunk += step.chunk;
+    i.j += step.j;
+    i.b += step.b;
+    if (i.chunk >= a.chunks) {
+      i.chunk -= a.chunks;
+      ++i.j;
     }
+    if (i.j >= rows) {
+      i.j -= rows;
+      ++i.b;
+    }
+    return i;
+  };
+  auto ask = [&](const Item& i) {          // drafted words of the item's sequence, a lane each
+    return lane < a.T && i.b < a.B ? a.drafted[(int64_t)i.b * a.T + lane] : -1;
   };
   vu32x4_t next[2];
   bool next_there[2];
-  auto load = [&]() {
+  auto load = [&](const Item& i, int32_t word) {
+    next_there[0] = next_there[1] = false;
+    if (i.b >= a.B) return;
+    const int t = i.j <= a.T ? i.j : i.j - a.T - 1, ahead = i.j <= a.T ? t : t + 1;
+    const uint64_t none = ~__ballot(is_word(word, a.V));
+    if (none && __builtin_ctzll(none) < ahead) return;
+    const uint16_t* from = i.j <= a.T ? reinterpret_cast<const uint16_t*>(a.target) + ((int64_t)i.b * (a.T + 1) + t) * a.ld_target
+                                      : reinterpret_cast<const uint16_t*>(a.draft) + ((int64_t)i.b * a.T + t) * a.ld_draft;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int v = v0 + h * kTabThreads * 8;
+      const int v = i.chunk * (kTabThreads * kTabPer) + (h * kTabThreads + tid) * 8;
       next_there[h] = v < a.V;
       if (v + 8 <= a.V) {
         next[h] = *reinterpret_cast<const vu32x4_t*>(from + v);
-      } else {
+      } else if (v < a.V) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t lo = v + 2 * i < a.V ? from[v + 2 * i] : 0xff80u, hi = v + 2 * i + 1 < a.V ? from[v + 2 * i + 1] : 0xff80u;
-          next[h][i] = lo | hi << 16;
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t lo = v + 2 * k < a.V ? from[v + 2 * k] : 0xff80u, hi = v + 2 * k + 1 < a.V ? from[v + 2 * k + 1] : 0xff80u;
+          next[h][k] = lo | hi << 16;
         }
       }
     }
   };
-  find();
-  if (item < items) load();
-  for (int par = 0; item < items; par ^= 1) {
-    const int64_t at = item;
+  Item i0 = item_at(blockIdx.x), i1 = behind(i0);
+  load(i0, ask(i0));
+  int32_t word = ask(i1);
+  int par = 0;
+  for (; i0.b < a.B; i0 = i1, i1 = behind(i1), par ^= 1) {
+    const int64_t at = ((int64_t)i0.b * rows + i0.j) * a.chunks + i0.chunk;
     vu32x4_t x[2];
     bool there[2];
 #pragma unroll
@@ -227,26 +251,26 @@ __global__ __launch_bounds__(kTabThreads) void verify_stats_table_kernel(VerifyD
       x[h] = next[h];
       there[h] = next_there[h];
     }
-    item += gridDim.x;
-    find();
-    if (item < items) load();
+    load(i1, word);
+    word = ask(behind(i1));
+    // two logits at a time: places in the table, in bytes
     double sum = 0, sum2 = 0;
-    u16x2_t most = {0, 0}, least = {0xffff, 0xffff};
+    u16x2_t most = {0, 0};
+    constexpr u16x2_t kFirst = {kTabFirst, kTabFirst}, kCount = {kTabCount, kTabCount};
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       if (!there[h]) continue;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const uint32_t w = x[h][i], mag = w & 0x7fff7fffu;
-        most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2_t, mag));
-        least = __builtin_elementwise_min(least, __builtin_bit_cast(u16x2_t, mag));
-        const uint32_t lo = (mag & 0xffffu) - kTabFirst, hi = (mag >> 16) - kTabFirst;
-        sum += s_table[(lo < kTabCount ? lo : kTabCount) * 2 + (w >> 15 & 1)];
-        sum2 += s_table[(hi < kTabCount ? hi : kTabCount) * 2 + (w >> 31)];
+        const uint32_t w = x[h][i];
+        const u16x2_t u = __builtin_elementwise_min((u16x2_t)(__builtin_bit_cast(u16x2_t, w & 0x7fff7fffu) - kFirst), kCount);   // (below: wraps)
+        most = __builtin_elementwise_max(most, u);
+        const uint32_t at = __builtin_bit_cast(uint32_t, (u16x2_t)(u * (uint16_t)16 + __builtin_bit_cast(u16x2_t, w >> 12 & 0x00080008u)));
+        sum += *reinterpret_cast<const double*>(reinterpret_cast<const unsigned char*>(s_table) + (at & 0xffffu));
+        sum2 += *reinterpret_cast<const double*>(reinterpret_cast<const unsigned char*>(s_table) + (at >> 16));
       }
     }
-    const uint32_t top = most[0] > most[1] ? most[0] : most[1], low = least[0] < least[1] ? least[0] : least[1];
-    const bool odd = __any(top >= kTabFirst + kTabCount || low < kTabFirst);
+    const bool odd = __any(most[0] == kTabCount || most[1] == kTabCount);
     sum = wave_sum64(sum + sum2);
     if (lane == 0) {
       s_sum[par][wave] = sum;
@@ -539,7 +563,7 @@ struct VerifyLayout {
 };
 VerifyLayout verify_layout(const vo_verify* s) {
   VerifyLayout L;
-  // us, the whole call, 32 / 8 logits a thread: TODO
+  // us, the whole call, 32 / 8 logits a thread: 4 words of one sentence of 32000 28 / 18, 37 x 5 of 32003 in fp32 37 / 35; 128 x 4 of 128000 only 32.
   const int64_t few = kVThreads * kFewPer;
   L.per = (int64_t)s->B * (2 * s->T + 1) * ((s->V + few - 1) / few) <= 8192 && s->V <= few * kMostChunks ? kFewPer : kManyPer;
   L.chunks = (s->V + kVThreads * L.per - 1) / (kVThreads * L.per);
@@ -575,11 +599,7 @@ template <typename TE, int PER> hipError_t launch_verify(const VerifyDev& d, hip
     p.ticket += b0;
     hipError_t e;
     if (sizeof(TE) == 2 && PER == kManyPer && d.c * 64 <= kTabMost && (int64_t)p.B * rows * d.chunks >= 4 * kTabBlocks) {
-      constexpr int smem = 2 * ((int)kTabCount + 1) * 8;
-      static LdsLimit limit;
-      e = limit.raise(reinterpret_cast<const void*>(verify_stats_table_kernel), smem);
-      if (e != hipSuccess) return e;
-      hipLaunchKernelGGL(verify_stats_table_kernel, dim3(kTabBlocks), dim3(kTabThreads), smem, st, p);
+      hipLaunchKernelGGL(verify_stats_table_kernel, dim3(kTabBlocks), dim3(kTabThreads), 0, st, p);
     } else {
       hipLaunchKernelGGL((verify_stats_kernel<TE, PER>), dim3(d.chunks, p.B * rows), dim3(kVThreads), 0, st, p);
     }

@@ -216,3 +216,23 @@ def test_refusals_of_the_handle():
         with pytest.raises(bd.AttnSoftmaxError) as e:
             h.verify(*args)
         assert e.value.code == code
+
+
+@pytest.mark.parametrize("tau", [1.0, 0.1, 0.09])
+def test_many_rows_of_bf16(tau):
+    """Enough chunks for the table of powers (0.09: a temperature past its range), and logits that are not in it: zeros, tiny and large ones, -inf;
+    rows that are no distributions; short drafts whose further rows hold NaN."""
+    c = Case(70, 4, 40003, "bf16", tau=tau, seed=20, spread=2.0 * tau, off=0.4 * tau)
+    t, d = c.t64.copy(), c.d64.copy()
+    t[3, 1, 5:9], t[4, 0, 40000], t[5, 2, ::2], t[6, 3, 77] = 0.0, 1e-7, -np.inf, 300.0 * tau
+    d[3, 0, 39999], d[4, 1, 100:9000], d[5, 0, 1::2], d[6, 2, 9] = -1e-30, 0.0, -np.inf, 70.0 * tau
+    t[7, 0, 3], t[8, 1, 12000], d[9, 0, 40002] = np.nan, np.inf, np.nan
+    t[10] = 0.0
+    d[10] = 0.0
+    c.drafted[11, 2:] = -1
+    t[11, 3:], d[11, 2:] = np.nan, np.nan
+    unit = -(-c.V // 8) * 8
+    c.target, c.t64 = _rows(t, "bf16", unit)
+    c.draft, c.d64 = _rows(d, "bf16", unit + 8)
+    n, words = c.check()
+    assert words[7, 0] == -1 and n[7] == 0 and n[9] == 0
