@@ -22,10 +22,10 @@
  * Token `pos` of sequence b lies in page page_table[b, pos / page] at place pos % page.  A page outside [0, pages) is no page: what
  * would lie there is not written, reads as 0, and is not attended to.
  *
- * 8 bits: each token's row of each head has a scale s = max(max |x| / Q, 2^-120), Q = 127 (KC_INT8) or 448 (KC_E4M3), and holds
- * the codes x * (1 / s), the float product rounded to the nearest code, ties to even; it stands for code * s.  (All steps in
- * fp32.)  The error is at most half a code: max |x| / 254, or 2^-4 of the value above max |x| 2^-15.  A row that holds an infinity
- * or a NaN has the scale NaN and reads as NaN.
+ * 8 bits: each token's row of each head has a scale s = max(max |x| * (1 / Q), 2^-120), Q = 127 (KC_INT8) or 448 (KC_E4M3), and
+ * holds the codes x * (1 / s), the float product rounded to the nearest code, ties to even; it stands for code * s.  (All
+ * steps in fp32, 1 / Q among them.)  The error is at most half a code and a few roundings of fp32: max |x| / 254, or 2^-4 of
+ * the value above max |x| 2^-15.  A row that holds an infinity or a NaN has the scale NaN and reads as NaN.
  */
 #ifndef KV_CACHE_H
 #define KV_CACHE_H
@@ -57,7 +57,7 @@ typedef struct {
 /*
  * Rows n of k and v [N, heads, D] dtype, ld_k and ld_v elements apart (at least heads * D, a multiple of 16 bytes), to token pos[n] of sequence
  * seq[n].  Rows whose seq lies outside [0,B), whose pos lies outside [0, max_pages * page) or whose page is none are not
- * written, and their k and v not read (they may hold anything).  The places of a call differ: of rows with the same one any may be
+ * written, and their k and v play no part (they may hold anything).  The places of a call differ: of rows with the same one any may be
  * left, in parts.  k_scales, v_scales: in 8 bits only (else NULL).  N in 1 .. 2^24.
  */
 as_status kv_cache_write(const kc_cache* cache, int32_t N, const void* k, int64_t ld_k, const void* v, int64_t ld_v,

@@ -15,7 +15,7 @@ def encode(x, cache):
     x = np.asarray(x, dtype=np.float32)
     if not np.isfinite(x).all():
         return np.zeros(x.shape), np.float32(np.nan)
-    scale = np.maximum(np.abs(x).max() / np.float32(LARGEST[cache]), np.float32(2.0 ** -120))
+    scale = np.maximum(np.abs(x).max() * (np.float32(1.0) / np.float32(LARGEST[cache])), np.float32(2.0 ** -120))
     y = (x * (np.float32(1.0) / scale)).astype(np.float64)
     if cache == "int8":
         return np.rint(y) + 0.0, scale      # (no zero below zero)

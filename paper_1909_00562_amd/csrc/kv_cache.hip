@@ -193,9 +193,9 @@ template <typename TE, int TYPE, bool WRITE, int ROWS, bool PAST> __global__ __l
           top = m > top ? m : top;
         }
         top = max_of_lanes(top, a.lanes_log);
-        constexpr float kLargest = TYPE == KC_INT8 ? 127.f : 448.f;
+        constexpr float kPer = TYPE == KC_INT8 ? 1.f / 127.f : 1.f / 448.f;
         const bool finite = top < 0x7f800000u;
-        const float scale = fmaxf(__builtin_bit_cast(float, top) / kLargest, 0x1p-120f), inv = finite ? 1.f / scale : 0.f;
+        const float scale = fmaxf(__builtin_bit_cast(float, top) * kPer, 0x1p-120f), inv = finite ? 1.f / scale : 0.f;
         if (!finite)
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[i][e] = 0.f;
