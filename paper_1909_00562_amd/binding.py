@@ -643,9 +643,9 @@ class _DeviceOp:
     def _optional(self, t, shape, dtype, name):
         return None if t is None else self._tensor(t, shape, dtype, name)
 
-    def _rows(self, t, shape, dtype, name, ahead=1):
-        """(address, elements from row to row) of a tensor whose first `ahead` dimensions are rows the same distance apart, each
-        dense: a part of a wider projection, or logits with padding."""
+    def _rows(self, t, shape, dtype, name, inner):
+        """(address, elements from row to row) of a tensor whose first dimensions are rows the same distance apart, each dense with
+        the strides `inner`: a part of a wider projection, or logits with padding."""
         if t is None:
             raise AttnSoftmaxError(1, f"{name} is None")
         if t.shape != shape:
@@ -655,19 +655,19 @@ class _DeviceOp:
         if t.get_device() != self.index:
             raise AttnSoftmaxError(2, f"{name} is on {t.device}, expected {self.dev}")
         strides = t.stride()
-        width = 1
-        for n, stride in zip(shape[:ahead - 1:-1], strides[:ahead - 1:-1]):
-            if n != 1 and stride != width:
-                raise AttnSoftmaxError(5, f"the rows of {name} are not dense")
-            width *= n
-        whole = 16 // t.element_size()
-        alone = -(-width // whole) * whole      # (a single row: dimensions of one have any stride)
-        if ahead == 1:
-            return t.data_ptr(), strides[0] if shape[0] > 1 else alone
-        a, b = shape[:2]
-        row = strides[1] if b > 1 else strides[0] if a > 1 else alone
-        if a > 1 and b > 1 and strides[0] != b * row:
-            raise AttnSoftmaxError(5, f"the rows of {name} are not the same distance apart")
+        ahead = len(shape) - len(inner)
+        if strides[ahead:] != inner:
+            for n, stride, dense in zip(shape[ahead:], strides[ahead:], inner):
+                if n != 1 and stride != dense:
+                    raise AttnSoftmaxError(5, f"the rows of {name} are not dense")
+        row = strides[ahead - 1]
+        if shape[ahead - 1] == 1 or ahead == 2 and shape[0] > 1:
+            a, b = (1, shape[0]) if ahead == 1 else shape[:2]      # (dimensions of one have any stride)
+            if b == 1:
+                whole = 16 // t.element_size()
+                row = strides[0] if a > 1 else -(-inner[0] * shape[ahead] // whole) * whole
+            elif a > 1 and strides[0] != b * row:
+                raise AttnSoftmaxError(5, f"the rows of {name} are not the same distance apart")
         return t.data_ptr(), row
 
     def _call(self, function, *args):
@@ -826,8 +826,8 @@ class DeviceVocabVerify(_DeviceOp):
         if words is None:
             words = torch.empty(self.bt1, dtype=i32, device=self.dev)
         check = self._tensor
-        self._call(self.lib.vocab_verify, self.ref, *self._rows(target, self.target_shape, self.tdt, "target", 2),
-                   *self._rows(draft, self.draft_shape, self.tdt, "draft", 2), check(drafted, self.bt, i32, "drafted"),
+        self._call(self.lib.vocab_verify, self.ref, *self._rows(target, self.target_shape, self.tdt, "target", (1,)),
+                   *self._rows(draft, self.draft_shape, self.tdt, "draft", (1,)), check(drafted, self.bt, i32, "drafted"),
                    check(u_accept, self.bt, f32, "u_accept"), check(u_next, self.b, f32, "u_next"),
                    check(n_accepted, self.b, i32, "n_accepted"), check(words, self.bt1, i32, "words"),
                    self.workspace.data_ptr(), self.ws_bytes)
@@ -865,7 +865,7 @@ class DeviceKvCache(_DeviceOp):
             self.pages += (None, None)
         self.k_pages, self.v_pages, self.k_scales, self.v_scales = k_pages, v_pages, k_scales, v_scales
         self.tdt = torch.bfloat16 if dtype == "bf16" else torch.float32
-        self.heads, self.D, self.page = heads, D, page
+        self.heads, self.D, self.page, self.inner = heads, D, page, (D, 1)
         self.shape = KcCache(P, page, heads, D, AS_BF16 if dtype == "bf16" else AS_F32, kind, 1, 1)
 
     def _table(self, page_table):
@@ -880,10 +880,12 @@ class DeviceKvCache(_DeviceOp):
 
     def write(self, k, v, seq, pos, page_table):
         """Rows n of k and v [N, heads, D] to token pos[n] of sequence seq[n] (int32); rows of no sequence (-1) are left out."""
-        i32, N = self.torch.int32, len(seq)
+        if seq is None:
+            raise AttnSoftmaxError(1, "seq is None")
+        i32, N = self.torch.int32, seq.shape[0]
         rows = (N, self.heads, self.D)
-        k_at, ld_k = self._rows(k, rows, self.tdt, "k")
-        v_at, ld_v = self._rows(v, rows, self.tdt, "v")
+        k_at, ld_k = self._rows(k, rows, self.tdt, "k", self.inner)
+        v_at, ld_v = self._rows(v, rows, self.tdt, "v", self.inner)
         seq, pos = self._tensor(seq, (N,), i32, "seq"), self._tensor(pos, (N,), i32, "pos")
         ref, table = self._table(page_table)
         if N:
@@ -891,7 +893,9 @@ class DeviceKvCache(_DeviceOp):
 
     def read(self, seq, pos, page_table, k=None, v=None):
         """(k, v) [N, heads, D]: what the cache holds at token pos[n] of sequence seq[n] (int32), zeros where it is no place."""
-        torch, N = self.torch, len(seq)
+        if seq is None:
+            raise AttnSoftmaxError(1, "seq is None")
+        torch, N = self.torch, seq.shape[0]
         rows = (N, self.heads, self.D)
         if k is None:
             k = torch.empty(rows, dtype=self.tdt, device=self.dev)
@@ -916,7 +920,7 @@ class DeviceKvAttn(_DeviceOp):
         self.shape = KcCache(c.pages, c.page, c.heads, c.D, c.dtype, c.cache_type, B, max(1, -(-max_len // c.page)))
         self.attn = KcAttn(T, q_heads, max_len, window, float(c.D ** -0.5 if scale is None else scale))
         self.attn_ref = ctypes.byref(self.attn)
-        self.b, self.heads_shape, self.q_shape = (B,), (B, T, q_heads), (B, T, q_heads, c.D)
+        self.b, self.heads_shape, self.q_shape, self.inner = (B,), (B, T, q_heads), (B, T, q_heads, c.D), (c.D, 1)
         self.ws_bytes = kv_cache_attn_workspace_bytes(self.shape, self.attn)
         if self.ws_bytes == 0:
             raise AttnSoftmaxError(2, "invalid shape for the attention: " + attn_softmax_last_error())
@@ -934,7 +938,7 @@ class DeviceKvAttn(_DeviceOp):
         if c.max_pages != max_pages:      # (never changed in place: another thread may be in a call with it)
             self.shape = c = KcCache(c.pages, c.page, c.heads, c.D, c.dtype, c.cache_type, c.B, max_pages)
         table = self._tensor(page_table, (c.B, max_pages), torch.int32, "page_table")
-        self._call(self.lib.kv_cache_attn, ctypes.byref(c), self.attn_ref, *self._rows(q, self.q_shape, self.tdt, "q", 2), *self.cache.pages, table,
+        self._call(self.lib.kv_cache_attn, ctypes.byref(c), self.attn_ref, *self._rows(q, self.q_shape, self.tdt, "q", self.inner), *self.cache.pages, table,
                    self._tensor(lengths, self.b, torch.int32, "lengths"), self._tensor(out, self.q_shape, self.tdt, "out"),
                    self._optional(lse, self.heads_shape, torch.float32, "lse"), self.workspace.data_ptr(), self.ws_bytes)
         return out
