@@ -59,6 +59,7 @@ typedef struct {
  * seq[n].  Rows whose seq lies outside [0,B), whose pos lies outside [0, max_pages * page) or whose page is none are not
  * written, and their k and v play no part (they may hold anything).  The places of a call differ: of rows with the same one any may be
  * left, in parts.  k_scales, v_scales: in 8 bits only (else NULL).  N in 1 .. 2^24.
+ * k_pages and v_pages differ here.
  */
 as_status kv_cache_write(const kc_cache* cache, int32_t N, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
                          const int32_t* seq, const int32_t* pos, const int32_t* page_table,
@@ -73,12 +74,13 @@ as_status kv_cache_read(const kc_cache* cache, int32_t N, const void* k_pages, c
 typedef struct {
   int32_t T;        /* new tokens of each sequence, 1 .. 64: one for decoding, drafted ones and one for verification */
   int32_t q_heads;  /* heads of queries, a multiple of the cache's; head i reads head i / (q_heads / heads); T * q_heads / heads <= 1024 */
-  int32_t max_len;  /* no sequence is longer, 1 .. max_pages * page: lengths are clamped to [0, max_len] */
+  int32_t max_len;  /* no sequence is longer, 1 .. max_pages * page and below 2^28: lengths are clamped to [0, max_len] */
   int32_t window;   /* > 0: a token sees itself and the window - 1 ahead of it; 0: all */
-  float scale;      /* of the products q . k, finite */
+  float scale;      /* of the products q . k; finite, and 1.45 times it too */
 } kc_attn;
 
-/* Bytes of workspace kv_cache_attn needs (it may need none: then 16); 0 if the shape is invalid. */
+/* Bytes of workspace kv_cache_attn needs (it may need none: then 16); 0 if the shape is invalid.  B * heads * ceil(T q_heads / heads / 64)
+ * is at most 2^22, and less than 2^30 times that with max_len / 16 + 1. */
 size_t kv_cache_attn_workspace_bytes(const kc_cache* cache, const kc_attn* attn);
 
 /*

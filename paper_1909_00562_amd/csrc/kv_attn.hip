@@ -31,6 +31,7 @@ constexpr int kLongRun = 8;            // chunks
 constexpr int kLeastChunk = 16;
 constexpr int kWholeChunks = 4;        // up to so many chunks a block takes all of a (sequence, head)
 constexpr uint32_t kAttnOob = 0x80000000u;
+constexpr float kLog2e = 1.4426950408889634f;
 
 struct KvAttnDev {
   const void *q, *k_pages, *v_pages;
@@ -838,10 +839,10 @@ as_status check_attn(const kc_cache* c, const kc_attn* s) {
     return set_error(AS_ERR_SHAPE, "%d tokens of %d heads of queries, %d of the cache", s->T, s->q_heads, c->heads);
   if (s->max_len < 1 || s->max_len > (int64_t)c->max_pages * c->page || s->max_len >= 1 << 28)
     return set_error(AS_ERR_SHAPE, "max_len=%d with %d pages of %d tokens to a sequence", s->max_len, c->max_pages, c->page);
-  if (s->window < 0 || !std::isfinite(s->scale)) return set_error(AS_ERR_SHAPE, "window=%d scale=%g", s->window, (double)s->scale);
-  const int R = s->T * (s->q_heads / c->heads), groups = (R + 63) / 64;
-  // (chunks are counted in 31 bits)
-  if ((int64_t)c->B * c->heads * groups * ((s->max_len + kLeastChunk - 1) / kLeastChunk + 1) >= (int64_t)1 << 31)
+  if (s->window < 0 || !std::isfinite(s->scale * kLog2e)) return set_error(AS_ERR_SHAPE, "window=%d scale=%g", s->window, (double)s->scale);
+  const int64_t pairs = (int64_t)c->B * c->heads * ((s->T * (s->q_heads / c->heads) + 63) / 64);
+  // a launch takes less than 2^32 threads along a dimension, and chunks are counted in 31 bits
+  if (pairs > 1 << 22 || pairs * ((s->max_len + kLeastChunk - 1) / kLeastChunk + 1) >= (int64_t)1 << 30)
     return set_error(AS_ERR_SHAPE, "%d sequences of %d heads up to %d tokens are too many for one call", c->B, c->heads, s->max_len);
   return AS_OK;
 }
@@ -943,11 +944,11 @@ extern "C" as_status kv_cache_attn(const kc_cache* cache, const kc_attn* attn, c
   a.pages = cache->pages;
   a.max_pages = cache->max_pages;
   a.max_len = attn->max_len;
-  a.window = attn->window;
+  a.window = attn->window < attn->max_len ? attn->window : 0;   // (longer ones are none)
   a.magic = kv_magic((uint32_t)a.page_tiles);
   a.chunk = p.chunk;
   a.split = p.split;
-  a.scale_log2 = std::fabs(attn->scale) * 1.4426950408889634f;
+  a.scale_log2 = std::fabs(attn->scale) * kLog2e;
   a.q_sign = attn->scale < 0 ? f32 ? 0x80000000u : 0x80008000u : 0u;
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   hipError_t e;

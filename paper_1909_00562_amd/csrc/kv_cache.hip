@@ -235,8 +235,10 @@ template <bool WRITE> as_status move(const kc_cache* c, const KvMove& a, hipStre
   // few tokens: as many lanes as there are rows
   const int groups = 64 >> a.lanes_log, quads = (2 * a.heads + 3) / 4;
   const bool few = (int64_t)a.N * quads <= (int64_t)groups * 1024;
-  const int64_t per_block = groups * (few ? 1 : 4), blocks = (a.N + per_block - 1) / per_block * quads;
-  if (blocks >= (int64_t)1 << 24) return set_error(AS_ERR_SHAPE, "%d tokens of %d heads in one call", a.N, a.heads);
+  const int per_block = groups * (few ? 1 : 4);
+  // a launch takes less than 2^32 threads along a dimension
+  const int64_t most = (((int64_t)1 << 24) - 1) / quads * per_block;
+  hipError_t e = hipSuccess;
   auto run = [&](auto* t, auto type) {
     using TE = typename std::remove_pointer<decltype(t)>::type;
     constexpr int TYPE = decltype(type)::value;
@@ -244,7 +246,18 @@ template <bool WRITE> as_status move(const kc_cache* c, const KvMove& a, hipStre
     // write 104 / 97, read 115 / 63; of 128 MB 47 / 50 and 36 / 34; of 64 MB 25 / 27 and 20 / 19.
     const bool past = (int64_t)a.N * 2 * a.heads * a.D * sizeof(TE) > (int64_t)96 << 20;
     auto kfn = few ? kv_move_kernel<TE, TYPE, WRITE, 1, false> : past ? kv_move_kernel<TE, TYPE, WRITE, 4, true> : kv_move_kernel<TE, TYPE, WRITE, 4, false>;
-    hipLaunchKernelGGL(kfn, dim3((unsigned)blocks), dim3(256), 0, st, a);
+    for (int64_t n0 = 0; n0 < a.N && e == hipSuccess; n0 += most) {
+      KvMove p = a;
+      p.N = (int32_t)(a.N - n0 < most ? a.N - n0 : most);
+      p.seq += n0;
+      p.pos += n0;
+      for (int i = 0; i < 2; ++i) {
+        if (WRITE) p.src[i] = reinterpret_cast<const TE*>(a.src[i]) + n0 * a.ld[i];
+        else p.dst[i] = reinterpret_cast<TE*>(a.dst[i]) + n0 * a.heads * a.D;
+      }
+      hipLaunchKernelGGL(kfn, dim3((unsigned)((p.N + per_block - 1) / per_block * quads)), dim3(256), 0, st, p);
+      e = hipGetLastError();
+    }
   };
   auto any = [&](auto* t, auto same) {
     if (c->cache_type == KC_INT8) run(t, std::integral_constant<int, KC_INT8>{});
@@ -253,7 +266,6 @@ template <bool WRITE> as_status move(const kc_cache* c, const KvMove& a, hipStre
   };
   if (c->dtype == AS_F32) any((float*)nullptr, std::integral_constant<int, KC_F32>{});
   else any((uint16_t*)nullptr, std::integral_constant<int, KC_BF16>{});
-  const hipError_t e = hipGetLastError();
   return e == hipSuccess ? AS_OK : set_error(AS_ERR_HIP, "rows of the cache: %s", hipGetErrorString(e));
 }
 
@@ -299,6 +311,8 @@ extern "C" as_status kv_cache_write(const kc_cache* cache, int32_t N, const void
   }
   for (const void* p : {k, v, (const void*)seq, (const void*)pos})
     if (!kv_al16(p)) return set_error(AS_ERR_ALIGN, "kv_cache_write: a pointer is not 16-byte aligned");
+  if (k_pages == v_pages || (k_scales && k_scales == v_scales))
+    return set_error(AS_ERR_SHAPE, "kv_cache_write: keys and values would be written to the same places");
   KvMove a = move_args(cache, N, seq, pos, page_table, k_pages, v_pages, k_scales, v_scales);
   a.src[0] = k;
   a.src[1] = v;

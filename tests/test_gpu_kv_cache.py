@@ -539,3 +539,29 @@ def test_refusals_of_the_handles():
     none = torch.zeros(0, device="cuda", dtype=torch.int32)
     c.c.write(k[:0], k[:0], none, none, c.table)
     assert c.c.read(none, none, c.table)[0].shape == (0, 2, 32)
+
+
+# max_len far beyond the lengths: the launches of long sequences.  Up to 64 sequences a wave cuts them, beyond a block, 512 at a time; few (sequence,
+# head) are cut into pieces, many into runs.
+@pytest.mark.parametrize("dtype, cache, D", [("bf16", "bf16", 64), ("f32", "f32", 128), ("bf16", "e4m3", 256), ("f32", "int8", 32)])
+@pytest.mark.parametrize("lengths, T, heads, G, window", [
+    ([0, 1500, 0, 1], 1, 2, 2, 0), ([0, 0, 0], 2, 1, 1, 0), ([2, 600, 0, 1300, 44], 5, 1, 9, 300), ([i * 37 % 211 for i in range(70)], 1, 1, 2, 0),
+    ([0] * 65 + [700, 5], 3, 1, 2, 0), ([i % 23 for i in range(600)], 1, 2, 1, 5), ([1100], 64, 1, 2, 2 ** 31 - 1)])
+def test_attention_cut_into_runs_and_pieces(dtype, cache, D, lengths, T, heads, G, window):
+    Attn(lengths, T, heads, G, D, 16, dtype, cache, window, seed=14, max_len=9000).run().check()
+
+
+def test_more_blocks_than_the_chip_holds():
+    """As many (sequence, head) as runs and more; long and short calls on the same cache give the same up to rounding."""
+    lengths = [int(x) for x in np.random.default_rng(0).integers(0, 900, 300)]
+    c = Attn(lengths, 1, 4, 2, 64, 16, "f32", "f32", seed=15)
+    c.run()
+    long = lib.DeviceKvAttn(c.c, 300, 1, 8, 4000)
+    table = torch.full((300, 250), -1, dtype=torch.int32, device="cuda")
+    table[:, :c.table.shape[1]] = c.table
+    lse = torch.empty_like(c.lse)
+    out = long.fwd(c.q, table, c.len_d, lse=lse)
+    # two results, each within 4 (n + 24) u of the sum of weights times magnitudes (at most the largest value, here below 200)
+    assert (out - c.out).abs().max() <= 2 * 4 * (900 + 24) * U * float(c.c.v_pages[~torch.isnan(c.c.v_pages)].abs().max())
+    some = ~torch.isneginf(c.lse)
+    assert torch.equal(torch.isneginf(lse), ~some) and (lse - c.lse)[some].abs().max() <= 1e-4

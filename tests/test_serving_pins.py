@@ -209,6 +209,7 @@ def test_rows_that_are_refused():
             assert f(**{name: None}) == 1, name
             assert f(**{name: A[9] + 4}) == 5, name
         assert f(_cache(cache_type=bd.KC_BF16)) == 1                     # scales of a cache that has none
+    assert _write(vp=A[5]) == 2 and _write(vs=A[7]) == 2 and _read(vp=A[5], N=0) == 2      # (one pool for both is only read)
     assert bd.kv_cache_write(None, 5, A[0], 64, A[1], 64, *A[2:9], check=False) == 1
     for kw in (dict(ld_k=63), dict(ld_v=48), dict(ld_k=-64), dict(ld_v=1 << 32)):
         assert _write(**kw) == 2, kw
@@ -219,7 +220,7 @@ def test_attention_that_is_refused():
     assert bd.kv_cache_attn_workspace_bytes(_cache(), _attn()) >= 16
     assert bd.kv_cache_attn_workspace_bytes(_cache(max_pages=400), _attn(max_len=6400)) > 16
     for kw in (dict(T=0), dict(T=65), dict(q_heads=0), dict(q_heads=3), dict(T=64, q_heads=34), dict(max_len=0), dict(max_len=65), dict(window=-1),
-               dict(scale=float("nan")), dict(scale=float("inf"))):
+               dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=-3e38)):
         assert _run(a=_attn(**kw)) == 2, kw
         assert bd.kv_cache_attn_workspace_bytes(_cache(), _attn(**kw)) == 0, kw
     for name in ("q", "kp", "vp", "ks", "vs", "table", "lengths", "out", "workspace"):
@@ -231,6 +232,12 @@ def test_attention_that_is_refused():
     # 2^16 sequences of 1024 heads and 2^20 tokens are more chunks than are counted
     big = _cache(B=65536, heads=1024, max_pages=1 << 9, page=2048)
     assert _run(big, _attn(q_heads=1024, max_len=1 << 20), ld_q=1 << 20) == 2
+    many = _cache(B=65536, heads=65, max_pages=1)                            # 65536 x 65 blocks of 512 threads
+    assert _run(many, _attn(T=1, q_heads=65, max_len=16), ld_q=1 << 16) == 2
+    assert bd.kv_cache_attn_workspace_bytes(_cache(B=65536, heads=64, max_pages=1), _attn(T=1, q_heads=64, max_len=16)) > 0
+    assert bd.kv_cache_attn_workspace_bytes(_cache(max_pages=1 << 24), _attn(max_len=(1 << 28) - 1)) > 0
+    assert bd.kv_cache_attn_workspace_bytes(_cache(max_pages=1 << 24), _attn(max_len=1 << 28)) == 0
+    assert bd.kv_cache_attn_workspace_bytes(_cache(), _attn(window=2 ** 31 - 1)) > 0
 
 
 def test_verification_that_is_refused():
