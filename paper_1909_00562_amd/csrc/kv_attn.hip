@@ -29,7 +29,7 @@ typedef uint32_t au32x2_t __attribute__((ext_vector_type(2)));
 
 constexpr int kLongRun = 8;            // chunks
 constexpr int kLeastChunk = 16;
-constexpr int kWholeChunks = 4;        // up to so many chunks a block takes all of a (sequence, head)
+constexpr int kWholeSteps = 4;
 constexpr uint32_t kAttnOob = 0x80000000u;
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -238,9 +238,8 @@ template <int TYPE, bool F32Q, int DP> struct Form {
   static constexpr bool kF32 = TYPE == KC_F32, kCoded = TYPE == KC_INT8 || TYPE == KC_E4M3;
   static constexpr int kBytes = kF32 ? 4 : kCoded ? 1 : 2;
   static constexpr int kTiles = kF32 ? 1 : 2;                       // of a step
-  // Waves of a block.  A wave holds a step's K and V, the queries and O^T in registers: at a width of 256 those of one wave on a SIMD, below of two.
-  static constexpr int kWaves = DP > 128 ? 4 : 8;
-  static constexpr int kBlocks = DP > 128 ? 1 : DP > 64 || (TYPE != KC_F32 && (TYPE != KC_INT8 || F32Q)) ? 2 : 4;   // (waves on a SIMD that registers allow)
+  // Waves on a SIMD that registers allow: a wave holds a step's K and V, the queries and O^T in them.
+  static constexpr int kOnSimd = DP > 128 ? 1 : DP > 64 || (TYPE != KC_F32 && (TYPE != KC_INT8 || F32Q)) ? 2 : 4;
   static constexpr int kQTerms = kF32 || !F32Q ? 1 : 3, kPTerms = kF32 ? 1 : F32Q ? 3 : 2;
   static constexpr int kKLoads = DP * kBytes / 64;                  // 16-byte loads of a lane for a tile of K
   static constexpr int kKElems = 16 / kBytes;                       // elements of each: D index (load * 4 + g) * kKElems + i
@@ -281,9 +280,9 @@ template <int N> __device__ __forceinline__ void buffer_load(__amdgpu_buffer_rsr
 }
 
 // ---- the kernel -------------------------------------------------------------------
-template <int TYPE, bool F32Q, int DP> __global__ __launch_bounds__((Form<TYPE, F32Q, DP>::kWaves * 64), (Form<TYPE, F32Q, DP>::kBlocks)) void kv_attn_kernel(KvAttnDev a) {
+template <int TYPE, bool F32Q, int DP, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, (Form<TYPE, F32Q, DP>::kOnSimd)) void kv_attn_kernel(KvAttnDev a) {
   using F = Form<TYPE, F32Q, DP>;
-  constexpr int WAVES = F::kWaves;
   constexpr int NT = F::kTiles, NO = DP / 16, STEP = NT * kKvTile, LD = DP + 4;
   extern __shared__ float lds[];          // [waves][16 rows][LD], and their maxima and sums
   float* lds_ml = lds + WAVES * 16 * LD;
@@ -829,7 +828,7 @@ template <bool F32Q, int WAVES> __global__ __launch_bounds__(WAVES * 64) void kv
 struct AttnPlan {
   int G, R, row_tiles, tile_waves, row_groups, group_rows;
   bool split;
-  int chunk, blocks;
+  int waves, chunk, blocks;
   size_t part_ml, total;
 };
 
@@ -857,14 +856,21 @@ AttnPlan attn_plan(const kc_cache* c, const kc_attn* s) {
   p.group_rows = p.row_groups > 1 ? p.tile_waves * 16 : p.R;
   int64_t span = s->max_len;
   if (s->window > 0 && (int64_t)s->window + s->T + kKvTile < span) span = (int64_t)s->window + s->T + kKvTile;
-  // a step of every wave
-  p.chunk = (c->D > 128 ? 4 : 8) / p.tile_waves * (c->cache_type == KC_F32 ? kKvTile : 2 * kKvTile);
-  const int64_t pairs = (int64_t)c->B * c->heads * p.row_groups, chunks = (span + p.chunk - 1) / p.chunk;
-  p.split = chunks > kWholeChunks;
+  const int step = c->cache_type == KC_F32 ? kKvTile : 2 * kKvTile;
+  const int64_t pairs = (int64_t)c->B * c->heads * p.row_groups;
+  // Up to so many steps of eight waves a block takes all of a (sequence, head).
+  p.split = span > (int64_t)kWholeSteps * (c->D > 128 ? 4 : 8) / p.tile_waves * step;
+  // Four waves to a block: twice as many blocks, so that one's beginning and end are the other's middle.  Eight where few blocks are all
+  // there are, and for three and four tiles of rows, whose waves share tokens.  us, 8 / 4: 64 sequences up to 8192 tokens, 32 heads on 8 of 128,
+  // bf16 210 / 205, e4m3 141 / 123; 256 up to 300 74 / 44; one of 700, 8 heads of 64 10.5 / 13.2; 24 of 1004 tokens seen by 40 rows 22 / 25.
+  p.waves = c->D > 128 ? 4 : p.tile_waves >= 3 || (!p.split && pairs < 512) ? 8 : 4;
+  p.chunk = p.waves / p.tile_waves * step;   // a step of every wave
+  const int64_t chunks = (span + p.chunk - 1) / p.chunk;
   int64_t blocks = pairs;
   if (p.split) {
     blocks = pairs * chunks;
-    const int64_t most = c->D <= 64 ? 512 : 256;   // what the compute units hold
+    // what the compute units hold
+    const int64_t most = c->D > 128 ? 256 : (c->D <= 64 ? 4096 : 2048) / p.waves;
     if (blocks > most) blocks = most;
   }
   p.blocks = (int)blocks;
@@ -875,18 +881,19 @@ AttnPlan attn_plan(const kc_cache* c, const kc_attn* s) {
   return p;
 }
 
-template <int TYPE, bool F32Q, int DP> hipError_t launch_attn(const KvAttnDev& a, int blocks, hipStream_t st) {
-  constexpr int waves = Form<TYPE, F32Q, DP>::kWaves, smem = waves * 16 * (DP + 4 + 2) * 4;
-  auto kfn = kv_attn_kernel<TYPE, F32Q, DP>;
+template <int TYPE, bool F32Q, int DP, int WAVES> hipError_t launch_attn(const KvAttnDev& a, int blocks, hipStream_t st) {
+  constexpr int smem = WAVES * 16 * (DP + 4 + 2) * 4;
+  auto kfn = kv_attn_kernel<TYPE, F32Q, DP, WAVES>;
   static LdsLimit limit;
   const hipError_t e = limit.raise(reinterpret_cast<const void*>(kfn), smem);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kfn, dim3(blocks), dim3(waves * 64), smem, st, a);
+  hipLaunchKernelGGL(kfn, dim3(blocks), dim3(WAVES * 64), smem, st, a);
   return hipGetLastError();
 }
-template <int TYPE, bool F32Q> hipError_t launch_attn_any(const KvAttnDev& a, int blocks, hipStream_t st) {
-  return a.D <= 64 ? launch_attn<TYPE, F32Q, 64>(a, blocks, st) : a.D <= 128 ? launch_attn<TYPE, F32Q, 128>(a, blocks, st)
-                                                                             : launch_attn<TYPE, F32Q, 256>(a, blocks, st);
+template <int TYPE, bool F32Q> hipError_t launch_attn_any(const KvAttnDev& a, const AttnPlan& p, hipStream_t st) {
+  if (a.D > 128) return launch_attn<TYPE, F32Q, 256, 4>(a, p.blocks, st);
+  if (a.D > 64) return p.waves == 8 ? launch_attn<TYPE, F32Q, 128, 8>(a, p.blocks, st) : launch_attn<TYPE, F32Q, 128, 4>(a, p.blocks, st);
+  return p.waves == 8 ? launch_attn<TYPE, F32Q, 64, 8>(a, p.blocks, st) : launch_attn<TYPE, F32Q, 64, 4>(a, p.blocks, st);
 }
 
 }  // namespace
@@ -953,10 +960,10 @@ extern "C" as_status kv_cache_attn(const kc_cache* cache, const kc_attn* attn, c
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   hipError_t e;
   switch (cache->cache_type) {
-    case KC_F32: e = launch_attn_any<KC_F32, true>(a, p.blocks, st); break;
-    case KC_BF16: e = launch_attn_any<KC_BF16, false>(a, p.blocks, st); break;
-    case KC_INT8: e = f32 ? launch_attn_any<KC_INT8, true>(a, p.blocks, st) : launch_attn_any<KC_INT8, false>(a, p.blocks, st); break;
-    default: e = f32 ? launch_attn_any<KC_E4M3, true>(a, p.blocks, st) : launch_attn_any<KC_E4M3, false>(a, p.blocks, st); break;
+    case KC_F32: e = launch_attn_any<KC_F32, true>(a, p, st); break;
+    case KC_BF16: e = launch_attn_any<KC_BF16, false>(a, p, st); break;
+    case KC_INT8: e = f32 ? launch_attn_any<KC_INT8, true>(a, p, st) : launch_attn_any<KC_INT8, false>(a, p, st); break;
+    default: e = f32 ? launch_attn_any<KC_E4M3, true>(a, p, st) : launch_attn_any<KC_E4M3, false>(a, p, st); break;
   }
   if (e == hipSuccess && p.split) {
     const dim3 grid((unsigned)(cache->B * cache->heads * p.row_groups), (unsigned)p.group_rows);
