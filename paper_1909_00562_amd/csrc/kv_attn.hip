@@ -27,6 +27,8 @@ namespace {
 typedef uint32_t au32x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t au32x2_t __attribute__((ext_vector_type(2)));
 
+// The table is read past the vector memory's counter: a page looked up among the loads of a step would have to wait for those ahead of it.
+typedef __attribute__((address_space(4))) int32_t scalar_int32_t;
 constexpr int kLongRun = 8;            // chunks
 constexpr int kLeastChunk = 16;
 constexpr int kWholeSteps = 4;
@@ -48,6 +50,7 @@ struct KvAttnDev {
   int32_t chunk;                       // tokens of a chunk
   int32_t split;                       // 0: a block per (sequence, head, row group), no second launch
   float scale_log2;                    // its magnitude: a negative scale's sign goes into the queries
+  int32_t no_q;                        // queries count as 0
   uint32_t q_sign;                     // exclusive-ored onto pairs of bf16 or onto floats
 };
 
@@ -345,11 +348,11 @@ __global__ __launch_bounds__(WAVES * 64, (Form<TYPE, F32Q, DP>::kOnSimd)) void k
     const int32_t all_hi = len - a.T, all_lo = a.window > 0 ? len - a.window : 0;
 
     // the first tiles' pages are looked up ahead of everything else
-    const int32_t* table = a.table + (int64_t)b * a.max_pages;
+    const scalar_int32_t* table = (const scalar_int32_t*)(uintptr_t)(a.table + (int64_t)b * a.max_pages);
     // the table's entry for the tile at pos (past the end: the last one)
     auto page_of = [&](int32_t pos) {
       const uint32_t tile = (uint32_t)(pos < len ? pos : len - 1) >> 4, col = kv_div(tile, a.magic);
-      return __builtin_amdgcn_readfirstlane(table[col]);
+      return table[col];
     };
     const int32_t stride = tok_waves * STEP;
     int32_t pos = tok0 + tok_wave * STEP;
@@ -367,13 +370,14 @@ __global__ __launch_bounds__(WAVES * 64, (Form<TYPE, F32Q, DP>::kOnSimd)) void k
     constexpr int QF = F::kF32 ? DP / 16 : DP / 32;   // fragments: of 4 floats, or of 8 bf16
     float qf[F::kF32 ? QF : 1][4];
     bf16x8_t qb[F::kQTerms][F::kF32 ? 1 : QF];
+    const bool q_there = row_there && !a.no_q;
     const int64_t q_at = ((int64_t)b * a.T + t) * a.ld_q + (int64_t)(head * a.G + gq) * a.D;
     if constexpr (F::kF32) {
 #pragma unroll
       for (int j = 0; j < QF; ++j) {
         const int d = (j * 4 + g) * 4;
         f32x4_t v = {};
-        if (row_there && d < a.D) v = *reinterpret_cast<const f32x4_t*>(reinterpret_cast<const float*>(a.q) + q_at + d);
+        if (q_there && d < a.D) v = *reinterpret_cast<const f32x4_t*>(reinterpret_cast<const float*>(a.q) + q_at + d);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float x = v[i];
@@ -385,7 +389,7 @@ __global__ __launch_bounds__(WAVES * 64, (Form<TYPE, F32Q, DP>::kOnSimd)) void k
       for (int j = 0; j < QF; ++j) {
         // codes: 16 of a load are two fragments
         const int d = F::kCoded ? (j / 2 * 4 + g) * 16 + j % 2 * 8 : (j * 4 + g) * 8;
-        const bool there = row_there && d < a.D;
+        const bool there = q_there && d < a.D;
         if constexpr (!F32Q) {
           au32x4_t v = {};
           if (there) v = *reinterpret_cast<const au32x4_t*>(reinterpret_cast<const uint16_t*>(a.q) + q_at + d);
@@ -423,7 +427,7 @@ __global__ __launch_bounds__(WAVES * 64, (Form<TYPE, F32Q, DP>::kOnSimd)) void k
       const uint32_t tile = (uint32_t)pos >> 4, col = kv_div(tile, a.magic);
       const bool there = (uint32_t)id < (uint32_t)a.pages;
       const int32_t n = there ? tok1 - pos : 0;
-      valid = n < 0 ? 0 : n < kKvTile ? n : kKvTile;
+      valid = __builtin_amdgcn_readfirstlane(n < 0 ? 0 : n < kKvTile ? n : kKvTile);   // (a median of three is the vector unit's)
       return (int64_t)((there ? id : 0) * a.heads + head) * a.page + (int32_t)(tile - col * a.page_tiles) * kKvTile;
     };
     int64_t at_row[NT];                   // of the tiles whose keys were asked for last
@@ -569,6 +573,7 @@ __global__ __launch_bounds__(WAVES * 64, (Form<TYPE, F32Q, DP>::kOnSimd)) void k
               const bool in = x >= lo && x <= hi && 4 * g + i < k_valid[u];
               seen |= (uint32_t)in << (u * 4 + i);
               if (!in) p[u][i] = -INFINITY;
+              if constexpr (F::kCoded) vs[u][i] = in ? vs[u][i] : 0.f;   // (the scale of a place that holds nothing may be anything)
             }
         }
         // the next step's keys, into the registers that have been read
@@ -600,12 +605,8 @@ __global__ __launch_bounds__(WAVES * 64, (Form<TYPE, F32Q, DP>::kOnSimd)) void k
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             p[u][i] = __builtin_amdgcn_exp2f(fmaf(p[u][i], a.scale_log2, -m_use));
-            if (part && !(seen >> (u * 4 + i) & 1)) p[u][i] = 0.f;
             l += p[u][i];
-            if constexpr (F::kCoded) {
-              p[u][i] *= vs[u][i];
-              if (part && !(seen >> (u * 4 + i) & 1)) p[u][i] = 0.f;   // (the scale of a place that holds nothing may be anything)
-            }
+            if constexpr (F::kCoded) p[u][i] *= vs[u][i];
           }
         // Values that only some rows see must not reach the others, whatever they are: 0 times an infinity or a NaN is a NaN.  Such values
         // are taken out, and the columns of the rows that see them made NaN.
@@ -619,7 +620,11 @@ __global__ __launch_bounds__(WAVES * 64, (Form<TYPE, F32Q, DP>::kOnSimd)) void k
 #pragma unroll
                 for (int h = 0; h < F::kVHalves; ++h)
 #pragma unroll
-                  for (int w = 0; w < F::kVDwords; ++w) odd |= F::odd(vr[u][i][h][w]);
+                  for (int w = 0; w < F::kVDwords; ++w) {
+                    uint32_t x = vr[u][i][h][w];
+                    asm volatile("" : "+v"(x));   // (or the compiler does this in every step, ahead of the branch)
+                    odd |= F::odd(x);
+                  }
           }
           if (__any(odd != 0)) {
             auto ones = [&](int u, int i, int h, int w) { return F::odd_bits(vr[u][i][h][w]) & F::kOnes; };
@@ -657,18 +662,23 @@ __global__ __launch_bounds__(WAVES * 64, (Form<TYPE, F32Q, DP>::kOnSimd)) void k
           columns(as_loaded, [&](int j, int i, float x) { o[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, p[0][i], o[j], 0, 0, 0); });
         } else {
           bf16x8_t pb[F::kPTerms];
+          float rest[8];
 #pragma unroll
           for (int u = 0; u < NT; ++u)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              float rest = p[u][i];
+            for (int i = 0; i < 4; ++i) rest[u * 4 + i] = p[u][i];
 #pragma unroll
-              for (int s = 0; s < F::kPTerms; ++s) {
-                const bf16_t x = (bf16_t)rest;
-                pb[s][u * 4 + i] = x;
-                rest -= (float)x;
-              }
+          for (int s = 0; s < F::kPTerms; ++s) {
+            au32x4_t term;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const uint32_t two = pack_bf16(rest[2 * k], rest[2 * k + 1]);
+              term[k] = two;
+              rest[2 * k] -= lo_bf16(two);
+              rest[2 * k + 1] -= hi_bf16(two);
             }
+            pb[s] = as_frag(term);
+          }
           columns(as_loaded, [&](int j, bf16x8_t vb) {
 #pragma unroll
             for (int s = 0; s < F::kPTerms; ++s) o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, pb[s], o[j], 0, 0, 0);
@@ -955,7 +965,9 @@ extern "C" as_status kv_cache_attn(const kc_cache* cache, const kc_attn* attn, c
   a.magic = kv_magic((uint32_t)a.page_tiles);
   a.chunk = p.chunk;
   a.split = p.split;
-  a.scale_log2 = std::fabs(attn->scale) * kLog2e;
+  // (of scale 0 the queries are read as 0: masked scores are -inf, whose product with 0 would be none)
+  a.scale_log2 = attn->scale != 0.f ? std::fabs(attn->scale) * kLog2e : 1.f;
+  a.no_q = attn->scale == 0.f;
   a.q_sign = attn->scale < 0 ? f32 ? 0x80000000u : 0x80008000u : 0u;
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   hipError_t e;
