@@ -44,7 +44,8 @@ struct KvAttnDev {
   float *part, *part_ml;   // [slot][row][D], [slot][row][2]: sums relative to the maximum; maximum (of log2) and sum of weights
   int64_t ld_q;
   int32_t B, T, heads, G, D, R;        // R = T G rows of a head
-  int32_t row_tiles, tile_waves, row_groups, group_rows;   // tiles of 16 rows; of a block (1, 2 or 4); groups of a block's tiles; rows of a group
+  int32_t tile_waves, tok_waves, row_groups, group_rows;   // tiles of 16 rows of a block (1 to 4); waves of each, sharing tokens; groups of a block's tiles; rows of a group
+  KvMagic by_tile_waves, by_quads;     // divisions by tile_waves and by D / 4
   int32_t page, page_tiles, pages, max_pages, max_len, window;
   KvMagic magic;                       // of page_tiles
   int32_t chunk;                       // tokens of a chunk
@@ -292,22 +293,19 @@ __global__ __launch_bounds__(WAVES * 64, (Form<TYPE, F32Q, DP>::kOnSimd)) void k
   __shared__ int32_t s_sum[WAVES], s_found[2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, g = lane >> 4;
-  const int row_wave = wave % a.tile_waves, tok_wave = wave / a.tile_waves, tok_waves = WAVES / a.tile_waves;   // (some may be left over)
+  const int tok_wave = kv_div(wave, a.by_tile_waves), row_wave = wave - tok_wave * a.tile_waves, tok_waves = a.tok_waves;   // (some waves may be left over)
 
   // a lane's part of a tile of K and of V; behind a row's end: out of every range
   uint32_t k_off[F::kKLoads], v_off[4][F::kVHalves];
+  const int32_t row_bytes = a.D * F::kBytes;
+  const uint32_t k_at = c * row_bytes + g * 16, v_at = g * 4 * row_bytes + c * F::kVW * F::kBytes;
 #pragma unroll
-  for (int j = 0; j < F::kKLoads; ++j) {
-    const int d = (j * 4 + g) * F::kKElems;
-    k_off[j] = d < a.D ? (uint32_t)((c * a.D + d) * F::kBytes) : kAttnOob;
-  }
+  for (int j = 0; j < F::kKLoads; ++j) k_off[j] = (j * 4 + g) * F::kKElems < a.D ? k_at + j * 64 : kAttnOob;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int h = 0; h < F::kVHalves; ++h) {
-      const int d = (h * 16 + c) * F::kVW;
-      v_off[i][h] = d < a.D ? (uint32_t)(((g * 4 + i) * a.D + d) * F::kBytes) : kAttnOob;
-    }
+    for (int h = 0; h < F::kVHalves; ++h)
+      v_off[i][h] = (h * 16 + c) * F::kVW < a.D ? v_at + i * row_bytes + h * 16 * F::kVW * F::kBytes : kAttnOob;
 
   // this block's run of chunks
   int32_t b, hr, chunk, left;             // sequence, (head, row group), first chunk there, chunks left
@@ -319,8 +317,8 @@ __global__ __launch_bounds__(WAVES * 64, (Form<TYPE, F32Q, DP>::kOnSimd)) void k
     chunk = run.chunk;
     left = run.left;
   } else {
-    b = blockIdx.x / (a.heads * a.row_groups);
-    hr = blockIdx.x - b * (a.heads * a.row_groups);
+    b = blockIdx.x;
+    hr = blockIdx.y;
     chunk = 0;
     left = 0;                             // (all there are)
   }
@@ -332,7 +330,7 @@ __global__ __launch_bounds__(WAVES * 64, (Form<TYPE, F32Q, DP>::kOnSimd)) void k
   do {
     const SeqSpan span = seq_span(a, b);
     const int32_t len = span.len;
-    const int head = hr / a.row_groups, group = hr - head * a.row_groups;
+    const int head = a.row_groups == 1 ? hr : hr / a.row_groups, group = hr - head * a.row_groups;
     const int32_t here = a.split ? (left < span.chunks - chunk ? left : span.chunks - chunk) : span.chunks;
     const int32_t tok0 = span.base + chunk * a.chunk;
     int32_t tok1 = tok0 + here * a.chunk;
@@ -342,7 +340,7 @@ __global__ __launch_bounds__(WAVES * 64, (Form<TYPE, F32Q, DP>::kOnSimd)) void k
     // the row of this lane's column of S^T and O^T
     const int row0 = (group * a.tile_waves + row_wave) * 16, row = row0 + c;
     const bool row_there = row < a.R;
-    const int t = row_there ? row / a.G : 0, gq = row - t * a.G;
+    const int t = a.T == 1 || !row_there ? 0 : row / a.G, gq = row - t * a.G;
     const int32_t hi = row_there ? len - a.T + t : -1, lo = a.window > 0 ? hi - a.window + 1 : 0;
     // tokens that all rows of all t see
     const int32_t all_hi = len - a.T, all_lo = a.window > 0 ? len - a.window : 0;
@@ -421,7 +419,6 @@ __global__ __launch_bounds__(WAVES * 64, (Form<TYPE, F32Q, DP>::kOnSimd)) void k
     uint32_t kr[NT][F::kKLoads][4], vr[NT][4][F::kVHalves][F::kVDwords];
     float ks[NT][4], vs[NT][4];
     int32_t k_valid[NT];                  // tokens that there are of a tile: up to 16, 0 where there is no page
-    const int32_t row_bytes = a.D * F::kBytes;
     // the tile's first row in the pool, and how many of its tokens there are
     auto place = [&](int32_t pos, int32_t id, int32_t& valid) {
       const uint32_t tile = (uint32_t)pos >> 4, col = kv_div(tile, a.magic);
@@ -709,14 +706,20 @@ __global__ __launch_bounds__(WAVES * 64, (Form<TYPE, F32Q, DP>::kOnSimd)) void k
     const int64_t slot = 2 * (int64_t)blockIdx.x + (chunk == 0);
     const int quads = a.D / 4, rows_here = a.R - group * a.group_rows < a.group_rows ? a.R - group * a.group_rows : a.group_rows;
     for (int x = threadIdx.x; x < rows_here * quads; x += WAVES * 64) {
-      const int r = x / quads, d = (x - r * quads) * 4, tile = r >> 4, r16 = r & 15;
+      const int r = kv_div(x, a.by_quads), d = (x - r * quads) * 4, tile = r >> 4, r16 = r & 15;
       // (all waves' at once: those of other tiles of rows do not count, whatever they are)
       float ms[WAVES], ls[WAVES];
 #pragma unroll
       for (int w = 0; w < WAVES; ++w) {
         ms[w] = lds_ml[(w * 16 + r16) * 2];
         ls[w] = lds_ml[(w * 16 + r16) * 2 + 1];
-        if (w % a.tile_waves != tile) ms[w] = -INFINITY;
+      }
+      bool ours[WAVES];
+#pragma unroll
+      for (int w = 0, of = 0; w < WAVES; ++w) {
+        ours[w] = of == tile;
+        if (!ours[w]) ms[w] = -INFINITY;
+        of = of + 1 == a.tile_waves ? 0 : of + 1;
       }
       float top = ms[0], sum = 0.f;
 #pragma unroll
@@ -727,14 +730,14 @@ __global__ __launch_bounds__(WAVES * 64, (Form<TYPE, F32Q, DP>::kOnSimd)) void k
       for (int w = 0; w < WAVES; ++w) {
         const float f = __builtin_amdgcn_exp2f(ms[w] - use);
         const f32x4_t part = *reinterpret_cast<const f32x4_t*>(lds + (w * 16 + r16) * LD + d);
-        if (w % a.tile_waves == tile) {
+        if (ours[w]) {
           sum += f * ls[w];
           v += f * part;
         }
       }
       const int rr = group * a.group_rows + r;
       if (whole) {
-        const int tt = rr / a.G;
+        const int tt = a.T == 1 ? 0 : rr / a.G;
         const int64_t o_row = ((int64_t)b * a.T + tt) * (a.heads * a.G) + head * a.G + (rr - tt * a.G);
         const bool some = sum != 0.f;     // (NaN: some)
         const float inv = 1.f / sum;
@@ -822,7 +825,7 @@ template <bool F32Q, int WAVES> __global__ __launch_bounds__(WAVES * 64) void kv
     v += s_o[(x << lanes_log) + threadIdx.x];
     sum += s_l[(x << lanes_log) + threadIdx.x];
   }
-  const int t = rr / a.G;
+  const int t = a.T == 1 ? 0 : rr / a.G;
   const int64_t o_row = ((int64_t)b * a.T + t) * (a.heads * a.G) + head * a.G + (rr - t * a.G);
   const bool some = sum != 0.f;           // (NaN: some)
   if (!some) v = f32x4_t{};
@@ -891,19 +894,20 @@ AttnPlan attn_plan(const kc_cache* c, const kc_attn* s) {
   return p;
 }
 
-template <int TYPE, bool F32Q, int DP, int WAVES> hipError_t launch_attn(const KvAttnDev& a, int blocks, hipStream_t st) {
+template <int TYPE, bool F32Q, int DP, int WAVES> hipError_t launch_attn(const KvAttnDev& a, dim3 blocks, hipStream_t st) {
   constexpr int smem = WAVES * 16 * (DP + 4 + 2) * 4;
   auto kfn = kv_attn_kernel<TYPE, F32Q, DP, WAVES>;
   static LdsLimit limit;
   const hipError_t e = limit.raise(reinterpret_cast<const void*>(kfn), smem);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kfn, dim3(blocks), dim3(WAVES * 64), smem, st, a);
+  hipLaunchKernelGGL(kfn, blocks, dim3(WAVES * 64), smem, st, a);
   return hipGetLastError();
 }
 template <int TYPE, bool F32Q> hipError_t launch_attn_any(const KvAttnDev& a, const AttnPlan& p, hipStream_t st) {
-  if (a.D > 128) return launch_attn<TYPE, F32Q, 256, 4>(a, p.blocks, st);
-  if (a.D > 64) return p.waves == 8 ? launch_attn<TYPE, F32Q, 128, 8>(a, p.blocks, st) : launch_attn<TYPE, F32Q, 128, 4>(a, p.blocks, st);
-  return p.waves == 8 ? launch_attn<TYPE, F32Q, 64, 8>(a, p.blocks, st) : launch_attn<TYPE, F32Q, 64, 4>(a, p.blocks, st);
+  const dim3 blocks = p.split ? dim3(p.blocks) : dim3(a.B, a.heads * a.row_groups);
+  if (a.D > 128) return launch_attn<TYPE, F32Q, 256, 4>(a, blocks, st);
+  if (a.D > 64) return p.waves == 8 ? launch_attn<TYPE, F32Q, 128, 8>(a, blocks, st) : launch_attn<TYPE, F32Q, 128, 4>(a, blocks, st);
+  return p.waves == 8 ? launch_attn<TYPE, F32Q, 64, 8>(a, blocks, st) : launch_attn<TYPE, F32Q, 64, 4>(a, blocks, st);
 }
 
 }  // namespace
@@ -952,8 +956,10 @@ extern "C" as_status kv_cache_attn(const kc_cache* cache, const kc_attn* attn, c
   a.G = p.G;
   a.D = cache->D;
   a.R = p.R;
-  a.row_tiles = p.row_tiles;
   a.tile_waves = p.tile_waves;
+  a.tok_waves = p.waves / p.tile_waves;
+  a.by_tile_waves = kv_magic((uint32_t)p.tile_waves);
+  a.by_quads = kv_magic((uint32_t)cache->D / 4);
   a.row_groups = p.row_groups;
   a.group_rows = p.group_rows;
   a.page = cache->page;
