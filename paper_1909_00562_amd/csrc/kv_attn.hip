@@ -118,6 +118,7 @@ template <int WAVES> __device__ __forceinline__ Cut cut_all(const KvAttnDev& a, 
 // A block's work: `left` chunks from `chunk` on of sequence b's head and row group hr; 0: none.
 struct Run {
   int32_t b, hr, chunk, left;
+  int32_t per;   // Cut's
 };
 // lanes' sums up to and including their own
 __device__ __forceinline__ int32_t scan_lanes(int32_t n) {
@@ -149,6 +150,7 @@ __device__ __forceinline__ LaneCut cut_lanes(const KvAttnDev& a, int blocks) {
 __device__ __forceinline__ Run run_of(const Cut& c, int32_t b, int32_t n, int32_t rest, int32_t at) {
   Run r;
   r.b = b;
+  r.per = c.per;
   const int32_t units = c.units(n);
   r.hr = rest / units;
   const int32_t unit = rest - r.hr * units;
@@ -167,14 +169,14 @@ template <int WAVES> __device__ __forceinline__ Run cut_run(const KvAttnDev& a, 
     const LaneCut l = cut_lanes(a, gridDim.x);
     const int32_t at = l.cut.pieces ? (int32_t)blockIdx.x : (int32_t)blockIdx.x * l.cut.per;
     const uint64_t here = __ballot(at >= l.ahead && at < l.ahead + l.own);
-    if (!here) return {0, 0, 0, 0};
+    if (!here) return {0, 0, 0, 0, 0};
     const int b = __builtin_ctzll(here);
     return run_of(l.cut, b, __builtin_amdgcn_readlane(l.chunks, b), at - __builtin_amdgcn_readlane(l.ahead, b), at);
   }
   const Cut c = cut_all<WAVES>(a, gridDim.x, s_sum);
   const int32_t hrs = a.heads * a.row_groups, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int32_t at = c.pieces ? (int32_t)blockIdx.x : (int32_t)blockIdx.x * c.per;   // in units, as is what follows
-  Run r = {0, 0, 0, 0};
+  Run r = {0, 0, 0, 0, 0};
   int32_t carry = 0;
   bool found = false;
   for (int b0 = 0; b0 < a.B && !found; b0 += WAVES * 64) {
@@ -766,36 +768,65 @@ __global__ __launch_bounds__(WAVES * 64, (Form<TYPE, F32Q, DP>::kOnSimd)) void k
 }
 
 // ---- parts of several blocks -------------------------------------------------------
-// A block per row: (sequence, head, row group) by blockIdx.x, its row by blockIdx.y.  Groups of D / 4 lanes (a power of two of them) take
-// the parts in turns; the order of the sums is that of the parts and the groups, whatever the launch.
-template <bool F32Q, int WAVES> __global__ __launch_bounds__(WAVES * 64) void kv_join_kernel(KvAttnDev a, int blocks, int lanes_log) {
+// A row of a (sequence, head, row group) joined by a block, its row by blockIdx.y.  Which one: by blockIdx.x, or, where there are more of them
+// than runs (by_runs), the one inside of which run blockIdx.x begins: few are shared then.  Groups of D / 4 lanes (a power of two of
+// them) take the parts in turns; the order of the sums is that of the parts and the groups.
+// us, the whole call, by number / by run: 1024 sequences up to 2048 tokens, 8 heads of 128 in bf16 803 / 767; 4096 up to 1100, 8 of 64 in int8
+// 1160 / 632.
+template <bool F32Q, int WAVES> __global__ __launch_bounds__(WAVES * 64) void kv_join_kernel(KvAttnDev a, int blocks, int lanes_log, bool by_runs) {
   constexpr int THREADS = WAVES * 64;
-  __shared__ int32_t s_sum[WAVES];
+  __shared__ int32_t s_sum[WAVES], s_found[2];
   __shared__ float s_top[WAVES], s_l[THREADS];
   __shared__ f32x4_t s_o[THREADS];
-  const int hrs = a.heads * a.row_groups, b = blockIdx.x / hrs, hr = blockIdx.x - b * hrs;
-  const int head = hr / a.row_groups, group = hr - head * a.row_groups;
-  const int r = blockIdx.y, rr = group * a.group_rows + r;
-  if (rr >= a.R) return;
-  const SeqSpan span = seq_span(a, b);
+  const int hrs = a.heads * a.row_groups, r = blockIdx.y;
+  int b, hr;
   int32_t k0 = 0, parts = 0;              // the first block that has some of it, and how many
-  if (span.chunks > 0) {
-    Cut cut;
-    int32_t ahead;                        // units of the sequences ahead
-    if (a.B <= 64) {
-      const LaneCut l = cut_lanes(a, blocks);
-      cut = l.cut;
-      ahead = __builtin_amdgcn_readlane(l.ahead, b);
-    } else {
-      cut = cut_all<WAVES>(a, blocks, s_sum);
-      int32_t n = 0;
-      for (int i = threadIdx.x; i < b; i += THREADS) n += cut.units(seq_span(a, i).chunks);
-      ahead = sum_of_waves<WAVES>(n, s_sum) * hrs;
+  auto store = [&](int b, int hr, int d, f32x4_t v, float lse) {
+    const int head = hr / a.row_groups, rr = (hr - head * a.row_groups) * a.group_rows + r, t = a.T == 1 ? 0 : rr / a.G;
+    const int64_t o_row = ((int64_t)b * a.T + t) * (a.heads * a.G) + head * a.G + (rr - t * a.G);
+    if constexpr (F32Q) *reinterpret_cast<f32x4_t*>(reinterpret_cast<float*>(a.out) + o_row * a.D + d) = v;
+    else *reinterpret_cast<au32x2_t*>(reinterpret_cast<uint16_t*>(a.out) + o_row * a.D + d) = au32x2_t{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    if (d == 0 && a.lse) a.lse[o_row] = lse;
+  };
+  auto row_there = [&](int hr) { return hr % a.row_groups * a.group_rows + r < a.R; };
+  if (by_runs) {
+    // those of sequences that hold nothing no run has: a lane each
+    for (int64_t x = (int64_t)blockIdx.x * THREADS + threadIdx.x; x < (int64_t)a.B * hrs; x += (int64_t)blocks * THREADS) {
+      const int eb = (int)x / hrs, ehr = (int)x - eb * hrs;
+      if (!row_there(ehr) || seq_span(a, eb).chunks > 0) continue;
+      for (int d = 0; d < a.D; d += 4) store(eb, ehr, d, f32x4_t{}, -INFINITY);
     }
-    const int32_t units = cut.units(span.chunks), at = ahead + hr * units;
-    k0 = cut.pieces ? at : at / cut.per;
-    parts = cut.pieces ? units : (at + units - 1) / cut.per - k0 + 1;
-    if (parts == 1) return;               // one block's, written by it
+    const Run run = cut_run<WAVES>(a, s_sum, s_found);
+    if (run.left <= 0 || run.chunk == 0 || !row_there(run.hr)) return;
+    b = run.b;
+    hr = run.hr;
+    const int32_t at = (int32_t)blockIdx.x * run.per - run.chunk;
+    k0 = at / run.per;
+    if (k0 + 1 != (int32_t)blockIdx.x) return;   // an earlier run begins in it too
+    parts = (at + seq_span(a, b).chunks - 1) / run.per - k0 + 1;
+  } else {
+    b = blockIdx.x / hrs;
+    hr = blockIdx.x - b * hrs;
+    if (!row_there(hr)) return;
+    const SeqSpan span = seq_span(a, b);
+    if (span.chunks > 0) {
+      Cut cut;
+      int32_t ahead;                      // units of the sequences ahead
+      if (a.B <= 64) {
+        const LaneCut l = cut_lanes(a, blocks);
+        cut = l.cut;
+        ahead = __builtin_amdgcn_readlane(l.ahead, b);
+      } else {
+        cut = cut_all<WAVES>(a, blocks, s_sum);
+        int32_t n = 0;
+        for (int i = threadIdx.x; i < b; i += THREADS) n += cut.units(seq_span(a, i).chunks);
+        ahead = sum_of_waves<WAVES>(n, s_sum) * hrs;
+      }
+      const int32_t units = cut.units(span.chunks), at = ahead + hr * units;
+      k0 = cut.pieces ? at : at / cut.per;
+      parts = cut.pieces ? units : (at + units - 1) / cut.per - k0 + 1;
+      if (parts == 1) return;             // one block's, written by it
+    }
   }
   // part k of the pair: its block's slot 2 blk + 1 where the pair begins, else 2 blk
   auto slot = [&](int32_t k) { return (2 * (int64_t)(k0 + k) + (k == 0)) * a.group_rows + r; };
@@ -825,16 +856,10 @@ template <bool F32Q, int WAVES> __global__ __launch_bounds__(WAVES * 64) void kv
     v += s_o[(x << lanes_log) + threadIdx.x];
     sum += s_l[(x << lanes_log) + threadIdx.x];
   }
-  const int t = a.T == 1 ? 0 : rr / a.G;
-  const int64_t o_row = ((int64_t)b * a.T + t) * (a.heads * a.G) + head * a.G + (rr - t * a.G);
   const bool some = sum != 0.f;           // (NaN: some)
   if (!some) v = f32x4_t{};
   else v *= 1.f / sum;
-  if (d < a.D) {
-    if constexpr (F32Q) *reinterpret_cast<f32x4_t*>(reinterpret_cast<float*>(a.out) + o_row * a.D + d) = v;
-    else *reinterpret_cast<au32x2_t*>(reinterpret_cast<uint16_t*>(a.out) + o_row * a.D + d) = au32x2_t{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
-  }
-  if (d == 0 && a.lse) a.lse[o_row] = some ? top * 0.6931471805599453f + logf(sum) : -INFINITY;
+  if (d < a.D) store(b, hr, d, v, some ? top * 0.6931471805599453f + logf(sum) : -INFINITY);
 }
 
 // ---- host --------------------------------------------------------------------------
@@ -984,13 +1009,15 @@ extern "C" as_status kv_cache_attn(const kc_cache* cache, const kc_attn* attn, c
     default: e = f32 ? launch_attn_any<KC_E4M3, true>(a, p, st) : launch_attn_any<KC_E4M3, false>(a, p, st); break;
   }
   if (e == hipSuccess && p.split) {
-    const dim3 grid((unsigned)(cache->B * cache->heads * p.row_groups), (unsigned)p.group_rows);
+    const int64_t pairs = (int64_t)cache->B * cache->heads * p.row_groups;
+    const bool by_runs = pairs > p.blocks;      // (runs they are then, not pieces)
+    const dim3 grid((unsigned)(by_runs ? p.blocks : pairs), (unsigned)p.group_rows);
     int lanes_log = 2;
     while (4 << lanes_log < cache->D) ++lanes_log;
-    // many parts: four waves to a row
-    const bool many = p.blocks > 8 * (int64_t)grid.x;
+    // many parts, or many sequences to look through: four waves to a row (256 sequences, one wave / four: 80 / 85 us)
+    const bool many = by_runs ? cache->B > 1024 : p.blocks > 8 * pairs;
     auto kfn = f32 ? many ? kv_join_kernel<true, 4> : kv_join_kernel<true, 1> : many ? kv_join_kernel<false, 4> : kv_join_kernel<false, 1>;
-    hipLaunchKernelGGL(kfn, grid, dim3(many ? 256 : 64), 0, st, a, p.blocks, lanes_log);
+    hipLaunchKernelGGL(kfn, grid, dim3(many ? 256 : 64), 0, st, a, p.blocks, lanes_log, by_runs);
     e = hipGetLastError();
   }
   return e == hipSuccess ? AS_OK : set_error(AS_ERR_HIP, "kv_cache_attn: %s", hipGetErrorString(e));

@@ -551,6 +551,15 @@ def test_attention_cut_into_runs_and_pieces(dtype, cache, D, lengths, T, heads, 
     Attn(lengths, T, heads, G, D, 16, dtype, cache, window, seed=14, max_len=9000).run().check()
 
 
+# More (sequence, head, group of rows) than runs: those that are shared are found from the runs, those that hold nothing apart.
+@pytest.mark.parametrize("dtype, cache, D", [("bf16", "bf16", 64), ("f32", "f32", 128), ("f32", "e4m3", 16)])
+@pytest.mark.parametrize("lengths, T, heads, G, window", [
+    ([i * 5 % 9 for i in range(300)] + [400, 0, 33] + [0] * 297 + [1], 40, 3, 2, 0),       # two groups of rows to a head, the second one not full
+    ([3, 0, 900, 1] + [i % 3 for i in range(56)], 1, 70, 1, 0), ([0] * 200 + [5, 700] + [2] * 3, 2, 21, 1, 0), ([0] * 130, 3, 33, 1, 4)])
+def test_more_heads_than_runs(dtype, cache, D, lengths, T, heads, G, window):
+    Attn(lengths, T, heads, G, D, 16, dtype, cache, window, seed=16, max_len=9000).run().check()
+
+
 def test_more_blocks_than_the_chip_holds():
     """As many (sequence, head) as runs and more; long and short calls on the same cache give the same up to rounding."""
     lengths = [int(x) for x in np.random.default_rng(0).integers(0, 900, 300)]
