@@ -92,6 +92,8 @@ size_t kv_cache_attn_workspace_bytes(const kc_cache* cache, const kc_attn* attn)
  * A token that sees none (its position is negative: the sequence has fewer than T tokens; or all of its pages are none) gives 0 and -inf.
  * Tokens that are not seen, and what lies behind a sequence's end in its last page, may hold anything.  What a seen value's
  * infinity makes of its column of out is unspecified (an infinity or NaN).  k_pages and v_pages may be the same.
+ * Sums are divided by the sum of their weights at the end, and weights go up to 2^8: values above 2^120 divided by the number of tokens may
+ * leave fp32's range on the way and give infinities.
  * Products and sums are fp32 or better: fp32 caches on the fp32 matrix instructions; bf16 and 8-bit codes, which bf16 holds, with
  * the probabilities as two (dtype AS_BF16) or three bf16 terms and fp32 queries as three.
  */

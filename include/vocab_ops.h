@@ -131,7 +131,6 @@ as_status vocab_distill_bwd(const vo_shape* shape, const vo_teacher* teacher, co
  *   n_accepted [B] int32   words [B,T+1] int32: the accepted ones, the next one, -1 behind it
  * A logit of -inf has the probability 0.  A row that holds a NaN or +inf, or nothing but -inf, is no distribution: where one of them is
  * asked for, the words before are accepted and the next one is -1.  Probabilities and their sums are computed in 64 bits.
- * grad_dtype and the like play no part.
  */
 typedef struct {
   int32_t B;          /* sequences, 1 .. 2^16 */

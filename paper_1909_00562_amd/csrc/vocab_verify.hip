@@ -182,8 +182,6 @@ __global__ __launch_bounds__(kTabThreads) void verify_stats_table_kernel(VerifyD
   __syncthreads();
   // An item is a chunk of a row.  While one is added up, the next one's logits are on their way, and the drafted words that say whether
   // the one behind it is looked at at all.
-  // An item is a chunk of a row.  While one is added up, the next one's logits are on their way, and the drafted words that say whether
-  // the one behind it is looked at at all.
   struct Item {
     int b, j, chunk;
   };
@@ -324,12 +322,9 @@ __global__ __launch_bounds__(kTabThreads) void verify_stats_table_kernel(VerifyD
 }
 
 // ---- the words ---------------------------------------------------------------------
-struct RowStat {
-  double shift;          // p[v] = 2^(l[v] c + shift)
-};
 template <typename TE, int PER> __global__ __launch_bounds__(kVThreads, 8) void verify_words_kernel(VerifyDev a) {
   constexpr int W = 16 / sizeof(TE), CHUNK = kVThreads * PER;
-  __shared__ RowStat s_stat[2 * kVerifyMaxT + 1];
+  __shared__ double s_shift[2 * kVerifyMaxT + 1];    // p[v] = 2^(l[v] c + shift)
   __shared__ int8_t s_bad[2 * kVerifyMaxT + 1];
   __shared__ int s_words, s_n, s_state, s_last, s_chunk, s_past[kVThreads / 64], s_some[kVThreads / 64];
   __shared__ double s_r[4], s_ahead, s_theta, s_powers[kPowers];
@@ -379,7 +374,7 @@ template <typename TE, int PER> __global__ __launch_bounds__(kVThreads, 8) void 
 #pragma unroll
     for (int o = 1; o < 16; o <<= 1) z += __shfl_xor(z, o, 64);
     if ((lane & 15) == 0) {
-      s_stat[j] = {-(double)top * a.c - log2(z)};
+      s_shift[j] = -(double)top * a.c - log2(z);
       s_bad[j] = bad || !(top > -INFINITY);
     }
   }
@@ -387,10 +382,10 @@ template <typename TE, int PER> __global__ __launch_bounds__(kVThreads, 8) void 
   if (wave == 0) {
     bool ok = false, bad = false;
     if (lane < words) {
-      const RowStat p = s_stat[lane], q = s_stat[T + 1 + lane];
+      const double p = s_shift[lane], q = s_shift[T + 1 + lane];
       bad = s_bad[lane] || s_bad[T + 1 + lane];
-      ok = !bad && (double)u * exp2_by_powers(fma((double)lq_x, a.c, q.shift), s_powers) <
-                       exp2_by_powers(fma((double)lp_x, a.c, p.shift), s_powers);
+      ok = !bad && (double)u * exp2_by_powers(fma((double)lq_x, a.c, q), s_powers) <
+                       exp2_by_powers(fma((double)lp_x, a.c, p), s_powers);
     }
     const uint64_t not_ok = ~__ballot(ok), bads = __ballot(bad);
     if (lane == 0) {
@@ -408,7 +403,7 @@ template <typename TE, int PER> __global__ __launch_bounds__(kVThreads, 8) void 
   }
   if (state == 2) return;
   const TE *p_row = target + n * a.ld_target, *q_row = draft + (rest ? n : 0) * a.ld_draft;
-  const double p_shift = s_stat[n].shift, q_shift = s_stat[rest ? T + 1 + n : n].shift;
+  const double p_shift = s_shift[n], q_shift = s_shift[rest ? T + 1 + n : n];
   // what counts of a word: all of p, or what is above q
   auto weight = [&](auto subtract, float lp, float lq) {
     const double p = exp2_by_powers(fma((double)lp, a.c, p_shift), s_powers);

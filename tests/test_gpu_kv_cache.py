@@ -267,6 +267,12 @@ def test_attention(dtype, cache, lengths, T, heads, G, D, page, window):
 
 
 @pytest.mark.parametrize("dtype, cache", CACHES)
+def test_attention_of_most_rows_and_most_heads(dtype, cache):
+    Attn([90, 64], 64, 1, 16, 16, 4096, dtype, cache, seed=17).run().check()
+    Attn([18, 0, 1], 1, 1024, 1, 16, 16, dtype, cache, seed=18).run().check()
+
+
+@pytest.mark.parametrize("dtype, cache", CACHES)
 def test_attention_past_pages_that_are_none(dtype, cache):
     """Tokens whose page is none are not seen; sequences of none give zeros; what is behind the end, and pages that nobody names, hold NaN."""
     Attn([700, 90, 33, 1], 2, 2, 2, 64, 16, dtype, cache, seed=3, bad=0.4).run().check()

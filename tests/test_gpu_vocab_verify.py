@@ -88,7 +88,7 @@ class Case:
 @pytest.mark.parametrize("B, T, V, dtype, tau, wide", [
     (1, 1, 1, "f32", 1.0, 0), (1, 1, 2, "bf16", 1.0, 1), (7, 3, 5, "f32", 0.5, 0), (33, 4, 100, "bf16", 1.0, 0), (9, 5, 8191, "f32", 0.7, 2),
     (9, 2, 8192, "bf16", 1.3, 0), (9, 5, 8193, "bf16", 1.0, 0), (5, 64, 1003, "f32", 1.0, 0), (16, 4, 32003, "bf16", 0.9, 0), (3, 8, 128000, "f32", 1.0, 0),
-    (2, 1, 1 << 20, "bf16", 1.0, 0), (300, 1, 17, "bf16", 2.0, 0)])
+    (2, 1, 1 << 20, "bf16", 1.0, 0), (300, 1, 17, "bf16", 2.0, 0), (30000, 1, 3, "f32", 1.0, 0)])
 def test_words(B, T, V, dtype, tau, wide):
     Case(B, T, V, dtype, tau, seed=B, wide=wide).check()
 
