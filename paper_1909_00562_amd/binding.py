@@ -867,16 +867,20 @@ class DeviceKvCache(_DeviceOp):
         self.tdt = torch.bfloat16 if dtype == "bf16" else torch.float32
         self.heads, self.D, self.page, self.inner = heads, D, page, (D, 1)
         self.shape = KcCache(P, page, heads, D, AS_BF16 if dtype == "bf16" else AS_F32, kind, 1, 1)
+        self.described = (1, 1), ctypes.byref(self.shape)
 
     def _table(self, page_table):
         """The cache's description for this table, and the table's address."""
         if page_table is None or page_table.dim() != 2:
             raise AttnSoftmaxError(2 if page_table is not None else 1, "page_table is not [sequences, pages]")
-        B, max_pages = page_table.shape
-        c = self.shape
-        if c.B != B or c.max_pages != max_pages:      # (never changed in place: another thread may be in a call with it)
+        of = page_table.shape
+        described, ref = self.described     # (replaced as a whole: another thread may be in a call with it)
+        if of != described:
+            c, (B, max_pages) = self.shape, of
             self.shape = c = KcCache(c.pages, c.page, c.heads, c.D, c.dtype, c.cache_type, B, max_pages)
-        return ctypes.byref(c), self._tensor(page_table, page_table.shape, self.torch.int32, "page_table")
+            ref = ctypes.byref(c)
+            self.described = of, ref
+        return ref, self._tensor(page_table, of, self.torch.int32, "page_table")
 
     def write(self, k, v, seq, pos, page_table):
         """Rows n of k and v [N, heads, D] to token pos[n] of sequence seq[n] (int32); rows of no sequence (-1) are left out."""
