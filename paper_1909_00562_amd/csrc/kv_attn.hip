@@ -26,6 +26,7 @@ namespace {
 
 typedef uint32_t au32x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t au32x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
 
 // The table is read past the vector memory's counter: a page looked up among the loads of a step would have to wait for those ahead of it.
 typedef __attribute__((address_space(4))) int32_t scalar_int32_t;
@@ -776,7 +777,7 @@ __global__ __launch_bounds__(WAVES * 64, (Form<TYPE, F32Q, DP>::kOnSimd)) void k
 template <bool F32Q, int WAVES> __global__ __launch_bounds__(WAVES * 64) void kv_join_kernel(KvAttnDev a, int blocks, int lanes_log, bool by_runs) {
   constexpr int THREADS = WAVES * 64;
   __shared__ int32_t s_sum[WAVES], s_found[2];
-  __shared__ float s_top[WAVES], s_l[THREADS];
+  __shared__ f32x2_t s_l[THREADS];
   __shared__ f32x4_t s_o[THREADS];
   const int hrs = a.heads * a.row_groups, r = blockIdx.y;
   int b, hr;
@@ -830,31 +831,34 @@ template <bool F32Q, int WAVES> __global__ __launch_bounds__(WAVES * 64) void kv
   }
   // part k of the pair: its block's slot 2 blk + 1 where the pair begins, else 2 blk
   auto slot = [&](int32_t k) { return (2 * (int64_t)(k0 + k) + (k == 0)) * a.group_rows + r; };
-  float top = -INFINITY;
-  for (int32_t k = threadIdx.x; k < parts; k += THREADS) top = fmaxf(top, a.part_ml[slot(k) * 2]);
-  top = wave_max(top);
-  if ((threadIdx.x & 63) == 0) s_top[threadIdx.x >> 6] = top;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < WAVES; ++w) top = fmaxf(top, s_top[w]);
-  const float use = top == -INFINITY ? 0.f : top;
   const int groups = THREADS >> lanes_log, gr = threadIdx.x >> lanes_log, d = (threadIdx.x & ((1 << lanes_log) - 1)) * 4;
-  float sum = 0.f;
+  float top = -INFINITY, sum = 0.f;       // a group's, with its running maximum: one wait for the loads of all its parts
   f32x4_t v = {};
 #pragma unroll 4
   for (int32_t k = gr; k < parts; k += groups) {
     const int64_t s = slot(k);
-    const float f = __builtin_amdgcn_exp2f(a.part_ml[s * 2] - use);
-    sum += f * a.part_ml[s * 2 + 1];
-    if (d < a.D) v += f * *reinterpret_cast<const f32x4_t*>(a.part + s * a.D + d);
+    const f32x2_t ml = *reinterpret_cast<const f32x2_t*>(a.part_ml + s * 2);
+    f32x4_t part = {};
+    if (d < a.D) part = *reinterpret_cast<const f32x4_t*>(a.part + s * a.D + d);
+    const float m = fmaxf(top, ml[0]), use = m == -INFINITY ? 0.f : m;
+    const float f = __builtin_amdgcn_exp2f(top - use), by = __builtin_amdgcn_exp2f(ml[0] - use);
+    sum = sum * f + by * ml[1];
+    v = v * f + by * part;
+    top = m;
   }
   s_o[threadIdx.x] = v;
-  s_l[threadIdx.x] = sum;
+  s_l[threadIdx.x] = f32x2_t{top, sum};
   __syncthreads();
   if (gr != 0) return;
-  for (int x = 1; x < groups; ++x) {
-    v += s_o[(x << lanes_log) + threadIdx.x];
-    sum += s_l[(x << lanes_log) + threadIdx.x];
+  for (int x = 1; x < groups; ++x) top = fmaxf(top, s_l[(x << lanes_log) + threadIdx.x][0]);
+  const float use = top == -INFINITY ? 0.f : top;
+  v = f32x4_t{};
+  sum = 0.f;
+  for (int x = 0; x < groups; ++x) {
+    const f32x2_t ml = s_l[(x << lanes_log) + threadIdx.x];
+    const float by = __builtin_amdgcn_exp2f(ml[0] - use);
+    sum += by * ml[1];
+    v += by * s_o[(x << lanes_log) + threadIdx.x];
   }
   const bool some = sum != 0.f;           // (NaN: some)
   if (!some) v = f32x4_t{};
