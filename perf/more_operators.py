@@ -281,7 +281,9 @@ def _own(s):
         else:
             h = lib.DeviceKvCache(s["k_pages"], s["v_pages"], s["k_scales"], s["v_scales"], dtype=case["dtype"])
             if case["op"] == "attn":
-                h = lib.DeviceKvAttn(h, case["B"], case["T"], case["q"], max_len=case["L"], window=case["window"])
+                # (one sequence of uneven lengths is one token long: its table has pages for that)
+                longest = min(case["L"], s["table"].shape[1] * case["page"])
+                h = lib.DeviceKvAttn(h, case["B"], case["T"], case["q"], max_len=longest, window=case["window"])
         s["handle"] = h
     if case["op"] == "verify":
         h.verify(s["target"], s["draft"], s["drafted"], s["u_accept"], s["u_next"], s["n_accepted"], s["words"])
