@@ -326,7 +326,8 @@ template <typename TE, int PER> __global__ __launch_bounds__(kVThreads, 8) void 
   constexpr int W = 16 / sizeof(TE), CHUNK = kVThreads * PER;
   __shared__ double s_shift[2 * kVerifyMaxT + 1];    // p[v] = 2^(l[v] c + shift)
   __shared__ int8_t s_bad[2 * kVerifyMaxT + 1];
-  __shared__ int s_words, s_n, s_state, s_last, s_chunk, s_past[kVThreads / 64], s_some[kVThreads / 64];
+  // (single values are written in one place each: no wave can be late to read what was there before)
+  __shared__ int s_words, s_n, s_state, s_last, s_chunk, s_of_p, s_past[kVThreads / 64], s_some[kVThreads / 64];
   __shared__ double s_r[4], s_ahead, s_theta, s_powers[kPowers];
   const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, T = a.T, V = a.V;
   const int64_t first = (int64_t)b * T;
@@ -500,11 +501,11 @@ template <typename TE, int PER> __global__ __launch_bounds__(kVThreads, 8) void 
     if (lane == 0) {
       s_chunk = chunk < 0 ? some : chunk;   // (rounding, or u >= 1: the last one with a weight)
       s_theta = left;
-      s_state = of_p;
+      s_of_p = of_p;
     }
   }
   __syncthreads();
-  const bool subtract = !s_state;
+  const bool subtract = !s_of_p;
   const int v1 = s_chunk * CHUNK + tid * PER;   // consecutive logits per thread: running sums go by the words' order
   const double theta = s_theta;
   const double own = subtract ? weights(std::true_type{}, v1, W) : weights(std::false_type{}, v1, W);
