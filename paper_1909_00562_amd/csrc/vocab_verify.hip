@@ -81,6 +81,10 @@ __device__ __forceinline__ double exp2_by_powers(double y, const double* powers)
   return ldexp(fma(t, q, t), k >> 8);
 }
 
+// Of 2 to the power of this: the difference first, which is 0 at l = m.  Were c m taken off c l, its rounding would be in the exponent, 1e22 of
+// them at the lowest float, and such are what excluded words are given.
+__device__ __forceinline__ double exponent(float l, float m, double c) { return ((double)l - (double)m) * c; }
+
 __device__ __forceinline__ double wave_sum64(double v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
@@ -145,9 +149,8 @@ template <typename TE, int PER> __global__ __launch_bounds__(kVThreads) void ver
   m = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
   double sum = 0;
   if (m > -INFINITY && !bad) {
-    const double shift = -(double)m * a.c;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) sum += exp2_by_powers(fma((double)l[i], a.c, shift), s_powers);
+    for (int i = 0; i < PER; ++i) sum += exp2_by_powers(exponent(l[i], m, a.c), s_powers);
   }
   sum = wave_sum64(sum);
   if ((tid & 63) == 0) s_sum[wave] = sum;
@@ -305,9 +308,8 @@ __global__ __launch_bounds__(kTabThreads) void verify_stats_table_kernel(VerifyD
     for (int w = 0; w < WAVES; ++w) m = fmaxf(m, s_m[w]);
     sum = 0;
     if (m > -INFINITY && !bad) {
-      const double shift = -(double)m * a.c;
 #pragma unroll
-      for (int k = 0; k < kTabPer; ++k) sum += exp2_by_powers(fma((double)l[k], a.c, shift), s_powers);
+      for (int k = 0; k < kTabPer; ++k) sum += exp2_by_powers(exponent(l[k], m, a.c), s_powers);
     }
     sum = wave_sum64(sum);
     __syncthreads();
@@ -324,7 +326,8 @@ __global__ __launch_bounds__(kTabThreads) void verify_stats_table_kernel(VerifyD
 // ---- the words ---------------------------------------------------------------------
 template <typename TE, int PER> __global__ __launch_bounds__(kVThreads, 8) void verify_words_kernel(VerifyDev a) {
   constexpr int W = 16 / sizeof(TE), CHUNK = kVThreads * PER;
-  __shared__ double s_shift[2 * kVerifyMaxT + 1];    // p[v] = 2^(l[v] c + shift)
+  __shared__ double s_lift[2 * kVerifyMaxT + 1];     // p[v] = 2^((l[v] - top) c + lift)
+  __shared__ float s_top[2 * kVerifyMaxT + 1];
   __shared__ int8_t s_bad[2 * kVerifyMaxT + 1];
   // (single values are written in one place each: no wave can be late to read what was there before)
   __shared__ int s_words, s_n, s_state, s_last, s_chunk, s_of_p, s_past[kVThreads / 64], s_some[kVThreads / 64];
@@ -361,8 +364,8 @@ template <typename TE, int PER> __global__ __launch_bounds__(kVThreads, 8) void 
       bad |= x.bad;
       const float up = fmaxf(m, x.m);
       if (up > -INFINITY)
-        z = (m > -INFINITY ? z * exp2_by_powers(((double)m - (double)up) * a.c, s_powers) : 0.0) +
-            (x.m > -INFINITY ? x.sum * exp2_by_powers(((double)x.m - (double)up) * a.c, s_powers) : 0.0);
+        z = (m > -INFINITY ? z * exp2_by_powers(exponent(m, up, a.c), s_powers) : 0.0) +
+            (x.m > -INFINITY ? x.sum * exp2_by_powers(exponent(x.m, up, a.c), s_powers) : 0.0);
       m = up;
     }
     float top = m;
@@ -371,11 +374,12 @@ template <typename TE, int PER> __global__ __launch_bounds__(kVThreads, 8) void 
       top = fmaxf(top, __shfl_xor(top, o, 64));
       bad |= __shfl_xor(bad, o, 64);
     }
-    z = m > -INFINITY ? z * exp2_by_powers(((double)m - (double)top) * a.c, s_powers) : 0.0;
+    z = m > -INFINITY ? z * exp2_by_powers(exponent(m, top, a.c), s_powers) : 0.0;
 #pragma unroll
     for (int o = 1; o < 16; o <<= 1) z += __shfl_xor(z, o, 64);
     if ((lane & 15) == 0) {
-      s_shift[j] = -(double)top * a.c - log2(z);
+      s_top[j] = top;
+      s_lift[j] = -log2(z);
       s_bad[j] = bad || !(top > -INFINITY);
     }
   }
@@ -383,10 +387,9 @@ template <typename TE, int PER> __global__ __launch_bounds__(kVThreads, 8) void 
   if (wave == 0) {
     bool ok = false, bad = false;
     if (lane < words) {
-      const double p = s_shift[lane], q = s_shift[T + 1 + lane];
       bad = s_bad[lane] || s_bad[T + 1 + lane];
-      ok = !bad && (double)u * exp2_by_powers(fma((double)lq_x, a.c, q), s_powers) <
-                       exp2_by_powers(fma((double)lp_x, a.c, p), s_powers);
+      ok = !bad && (double)u * exp2_by_powers(exponent(lq_x, s_top[T + 1 + lane], a.c) + s_lift[T + 1 + lane], s_powers) <
+                       exp2_by_powers(exponent(lp_x, s_top[lane], a.c) + s_lift[lane], s_powers);
     }
     const uint64_t not_ok = ~__ballot(ok), bads = __ballot(bad);
     if (lane == 0) {
@@ -404,12 +407,13 @@ template <typename TE, int PER> __global__ __launch_bounds__(kVThreads, 8) void 
   }
   if (state == 2) return;
   const TE *p_row = target + n * a.ld_target, *q_row = draft + (rest ? n : 0) * a.ld_draft;
-  const double p_shift = s_shift[n], q_shift = s_shift[rest ? T + 1 + n : n];
+  const float p_top = s_top[n], q_top = s_top[rest ? T + 1 + n : n];
+  const double p_lift = s_lift[n], q_lift = s_lift[rest ? T + 1 + n : n];
   // what counts of a word: all of p, or what is above q
   auto weight = [&](auto subtract, float lp, float lq) {
-    const double p = exp2_by_powers(fma((double)lp, a.c, p_shift), s_powers);
+    const double p = exp2_by_powers(exponent(lp, p_top, a.c) + p_lift, s_powers);
     if constexpr (!decltype(subtract)::value) return p;
-    else return fmax(p - exp2_by_powers(fma((double)lq, a.c, q_shift), s_powers), 0.0);
+    else return fmax(p - exp2_by_powers(exponent(lq, q_top, a.c) + q_lift, s_powers), 0.0);
   };
   // weights of the words from v0 on, vectors step words apart
   auto weights = [&](auto subtract, int v0, int step) {
@@ -480,7 +484,7 @@ template <typename TE, int PER> __global__ __launch_bounds__(kVThreads, 8) void 
       for (int h = 0; h < 2; ++h) {
         const int k = h * 64 + lane;
         x[h] = 0.0;
-        if (k < a.chunks && part[k].m > -INFINITY) x[h] = part[k].sum * exp2_by_powers(fma((double)part[k].m, a.c, p_shift), s_powers);
+        if (k < a.chunks && part[k].m > -INFINITY) x[h] = part[k].sum * exp2_by_powers(exponent(part[k].m, p_top, a.c) + p_lift, s_powers);
       }
       scan();
     }
