@@ -92,6 +92,7 @@ size_t kv_cache_attn_workspace_bytes(const kc_cache* cache, const kc_attn* attn)
  * A token that sees none (its position is negative: the sequence has fewer than T tokens; or all of its pages are none) gives 0 and -inf.
  * Tokens that are not seen, and what lies behind a sequence's end in its last page, may hold anything.  What a seen value's
  * infinity makes of its column of out is unspecified (an infinity or NaN).  k_pages and v_pages may be the same.
+ * Scores may be of any size: q . k, in 8 bits of q and the codes, has to lie within 2^126 of zero (sums, and differences of sums, are fp32).
  * Sums are divided by the sum of their weights at the end, and weights go up to 2^8: values above 2^120 divided by the number of tokens may
  * leave fp32's range on the way and give infinities.
  * Products and sums are fp32 or better: fp32 caches on the fp32 matrix instructions; bf16 and 8-bit codes, which bf16 holds, with

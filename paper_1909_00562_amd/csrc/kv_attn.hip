@@ -42,7 +42,7 @@ struct KvAttnDev {
   const int32_t *table, *lengths;
   void* out;
   float* lse;
-  float *part, *part_ml;   // [slot][row][D], [slot][row][2]: sums relative to the maximum; maximum (of log2) and sum of weights
+  float *part, *part_ml;   // [slot][row][D], [slot][row][2]: sums relative to the maximum; the largest score ahead of its scale, and the sum of weights
   int64_t ld_q;
   int32_t B, T, heads, G, D, R;        // R = T G rows of a head
   int32_t tile_waves, tok_waves, row_groups, group_rows;   // tiles of 16 rows of a block (1 to 4); waves of each, sharing tokens; groups of a block's tiles; rows of a group
@@ -51,7 +51,7 @@ struct KvAttnDev {
   KvMagic magic;                       // of page_tiles
   int32_t chunk;                       // tokens of a chunk
   int32_t split;                       // 0: a block per (sequence, head, row group), no second launch
-  float scale_log2;                    // its magnitude: a negative scale's sign goes into the queries
+  float scale, scale_log2;             // magnitudes, the second one times log2(e): a negative scale's sign goes into the queries
   int32_t no_q;                        // queries count as 0
   uint32_t q_sign;                     // exclusive-ored onto pairs of bf16 or onto floats
 };
@@ -549,7 +549,7 @@ __global__ __launch_bounds__(WAVES * 64, (Form<TYPE, F32Q, DP>::kOnSimd)) void k
             }
           }
         }
-        // scores, in units of which scale_log2 makes powers of two
+        // scores ahead of their scale
         float p[NT][4];
 #pragma unroll
         for (int u = 0; u < NT; ++u)
@@ -590,9 +590,11 @@ __global__ __launch_bounds__(WAVES * 64, (Form<TYPE, F32Q, DP>::kOnSimd)) void k
 #pragma unroll
           for (int i = 0; i < 4; ++i) top = fmaxf(top, p[u][i]);
         // The maximum that weights are relative to may lag behind the true one by a factor of 2^8, which floats do not mind: it moves less often.
-        const float seen_top = max_of_rows(top) * a.scale_log2;
-        if (__any(seen_top > m + 8.f)) {
-          const float m_new = fmaxf(m, seen_top), f = __builtin_amdgcn_exp2f(m - m_new);   // (seen_top > -inf somewhere: other rows may have none yet)
+        // It is held ahead of the scale, which the difference is multiplied with: 0 where a score is the maximum, whatever its size (that of
+        // scaled ones is a rounding error, past the exponential's range from 2^31 on).
+        const float seen_top = max_of_rows(top);
+        if (__any((seen_top - m) * a.scale_log2 > 8.f)) {
+          const float m_new = fmaxf(m, seen_top), f = __builtin_amdgcn_exp2f((m - m_new) * a.scale_log2);   // (seen_top > -inf somewhere: other rows may have none yet)
           const float by = m_new == -INFINITY ? 1.f : f;
           l *= by;
 #pragma unroll
@@ -604,7 +606,7 @@ __global__ __launch_bounds__(WAVES * 64, (Form<TYPE, F32Q, DP>::kOnSimd)) void k
         for (int u = 0; u < NT; ++u)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            p[u][i] = __builtin_amdgcn_exp2f(fmaf(p[u][i], a.scale_log2, -m_use));
+            p[u][i] = __builtin_amdgcn_exp2f((p[u][i] - m_use) * a.scale_log2);
             l += p[u][i];
             if constexpr (F::kCoded) p[u][i] *= vs[u][i];
           }
@@ -731,7 +733,7 @@ __global__ __launch_bounds__(WAVES * 64, (Form<TYPE, F32Q, DP>::kOnSimd)) void k
       f32x4_t v = {};
 #pragma unroll
       for (int w = 0; w < WAVES; ++w) {
-        const float f = __builtin_amdgcn_exp2f(ms[w] - use);
+        const float f = __builtin_amdgcn_exp2f((ms[w] - use) * a.scale_log2);
         const f32x4_t part = *reinterpret_cast<const f32x4_t*>(lds + (w * 16 + r16) * LD + d);
         if (ours[w]) {
           sum += f * ls[w];
@@ -748,7 +750,7 @@ __global__ __launch_bounds__(WAVES * 64, (Form<TYPE, F32Q, DP>::kOnSimd)) void k
         else v *= inv;
         if constexpr (F32Q) *reinterpret_cast<f32x4_t*>(reinterpret_cast<float*>(a.out) + o_row * a.D + d) = v;
         else *reinterpret_cast<au32x2_t*>(reinterpret_cast<uint16_t*>(a.out) + o_row * a.D + d) = au32x2_t{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
-        if (d == 0 && a.lse) a.lse[o_row] = some ? top * 0.6931471805599453f + logf(sum) : -INFINITY;
+        if (d == 0 && a.lse) a.lse[o_row] = some ? top * a.scale + logf(sum) : -INFINITY;
       } else {
         *reinterpret_cast<f32x4_t*>(a.part + (slot * a.group_rows + r) * a.D + d) = v;
         if (d == 0) {
@@ -841,7 +843,7 @@ template <bool F32Q, int WAVES> __global__ __launch_bounds__(WAVES * 64) void kv
     f32x4_t part = {};
     if (d < a.D) part = *reinterpret_cast<const f32x4_t*>(a.part + s * a.D + d);
     const float m = fmaxf(top, ml[0]), use = m == -INFINITY ? 0.f : m;
-    const float f = __builtin_amdgcn_exp2f(top - use), by = __builtin_amdgcn_exp2f(ml[0] - use);
+    const float f = __builtin_amdgcn_exp2f((top - use) * a.scale_log2), by = __builtin_amdgcn_exp2f((ml[0] - use) * a.scale_log2);
     sum = sum * f + by * ml[1];
     v = v * f + by * part;
     top = m;
@@ -856,14 +858,14 @@ template <bool F32Q, int WAVES> __global__ __launch_bounds__(WAVES * 64) void kv
   sum = 0.f;
   for (int x = 0; x < groups; ++x) {
     const f32x2_t ml = s_l[(x << lanes_log) + threadIdx.x];
-    const float by = __builtin_amdgcn_exp2f(ml[0] - use);
+    const float by = __builtin_amdgcn_exp2f((ml[0] - use) * a.scale_log2);
     sum += by * ml[1];
     v += by * s_o[(x << lanes_log) + threadIdx.x];
   }
   const bool some = sum != 0.f;           // (NaN: some)
   if (!some) v = f32x4_t{};
   else v *= 1.f / sum;
-  if (d < a.D) store(b, hr, d, v, some ? top * 0.6931471805599453f + logf(sum) : -INFINITY);
+  if (d < a.D) store(b, hr, d, v, some ? top * a.scale + logf(sum) : -INFINITY);
 }
 
 // ---- host --------------------------------------------------------------------------
@@ -1001,6 +1003,7 @@ extern "C" as_status kv_cache_attn(const kc_cache* cache, const kc_attn* attn, c
   a.chunk = p.chunk;
   a.split = p.split;
   // (of scale 0 the queries are read as 0: masked scores are -inf, whose product with 0 would be none)
+  a.scale = std::fabs(attn->scale);
   a.scale_log2 = attn->scale != 0.f ? std::fabs(attn->scale) * kLog2e : 1.f;
   a.no_q = attn->scale == 0.f;
   a.q_sign = attn->scale < 0 ? f32 ? 0x80000000u : 0x80008000u : 0u;
