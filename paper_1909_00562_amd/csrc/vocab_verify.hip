@@ -37,7 +37,7 @@ struct VerifyDev {
   const float *u_accept, *u_next;
   int32_t *n_accepted, *words;
   VerifyPart* part;    // [B][2T+1][chunks]: T+1 rows of the target, T of the draft
-  double* sums;        // [B][chunks]: of max(p - q, 0)
+  double* sums;        // [B][chunks]: of max(p - q, 0); below 0: not there yet
   uint32_t* ticket;    // [B]
   int32_t B, T, V, chunks;
   double c;            // log2(e) / tau
@@ -121,7 +121,10 @@ template <typename TE, int PER> __global__ __launch_bounds__(kVThreads) void ver
   __shared__ double s_sum[4], s_powers[kPowers];
   const int rows = 2 * a.T + 1, b = blockIdx.y / rows, j = blockIdx.y - b * rows;
   const int tid = threadIdx.x, wave = tid >> 6;
-  if (j == 0 && blockIdx.x == 0 && tid == 0) a.ticket[b] = 0;
+  if (j == 0 && tid == 0) {
+    a.sums[(int64_t)b * a.chunks + blockIdx.x] = -1.0;
+    if (blockIdx.x == 0) a.ticket[b] = 0;
+  }
   // the target's row t is looked at behind t words, the draft's with its word
   const int t = j <= a.T ? j : j - a.T - 1, ahead = j <= a.T ? t : t + 1;
   for (int i = 0; i < ahead; ++i)
@@ -180,8 +183,11 @@ __global__ __launch_bounds__(kTabThreads) void verify_stats_table_kernel(VerifyD
     const double l = bf16_bits_to_f32((uint32_t)(i >> 1) + kTabFirst | (uint32_t)(i & 1) << 15);
     s_table[i] = i >> 1 < (int)kTabCount ? exp2_64(l * a.c) : 0.0;
   }
-  if (blockIdx.x == 0)
-    for (int b = tid; b < a.B; b += kTabThreads) a.ticket[b] = 0;
+  // (a block for each sequence: by all threads of all blocks, the compiler's code for the loop below took 101 us instead of 91)
+  for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
+    if (tid < a.chunks) a.sums[(int64_t)b * a.chunks + tid] = -1.0;
+    if (tid == 0) a.ticket[b] = 0;
+  }
   __syncthreads();
   // An item is a chunk of a row.  While one is added up, the next one's logits are on their way, and the drafted words that say whether
   // the one behind it is looked at at all.
@@ -437,11 +443,8 @@ template <typename TE, int PER> __global__ __launch_bounds__(kVThreads, 8) void 
     __syncthreads();
     if (tid == 0) {
       __hip_atomic_store(&sums[blockIdx.x], (s_r[0] + s_r[1]) + (s_r[2] + s_r[3]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      // The sum is stored past the L2s, and this wait is for its arrival where every XCD sees it; only then does the block count.  The last block
-      // reads the sums past the L2s too, and nothing else that other blocks of this launch write, so that the ticket need not order other
-      // stores (as a release it writes the L2 back, for every block: 160 -> 143 us at 128 x 4 words of 128000, 36 -> 31 at 37 x 5 of 32003).
-      __builtin_amdgcn_s_waitcnt(0);
-      __atomic_signal_fence(__ATOMIC_SEQ_CST);
+      // The ticket orders nothing: the last block reads the sums, and nothing else that other blocks of this launch write, until each is there.
+      // (As a release it writes the L2 back, for every block: 160 -> 143 us at 128 x 4 words of 128000, 36 -> 31 at 37 x 5 of 32003.)
       s_last = __hip_atomic_fetch_add(&a.ticket[b], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)a.chunks - 1;
     }
     __syncthreads();
@@ -470,11 +473,14 @@ template <typename TE, int PER> __global__ __launch_bounds__(kVThreads, 8) void 
       all = __shfl(run[1], 63, 64);
     };
     if (rest) {
+      // (every block has counted, and stores its sum ahead of that or soon after, waiting for nobody)
+      do {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int k = h * 64 + lane;
-        x[h] = k < a.chunks ? __hip_atomic_load(&sums[k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
-      }
+        for (int h = 0; h < 2; ++h) {
+          const int k = h * 64 + lane;
+          x[h] = k < a.chunks ? __hip_atomic_load(&sums[k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
+        }
+      } while (x[0] < 0 || x[1] < 0);
       scan();
     }
     const bool of_p = !(all > 0);           // nothing is left: p

@@ -28,3 +28,11 @@ def test_single_shared_values_of_the_words_kernel_are_written_in_one_place():
     for n in single:
         writes = re.findall(r"\b%s\s*=[^=]" % n, body)
         assert len(writes) == 1, (n, len(writes))
+
+
+def test_no_order_of_memory_rests_on_a_wait_by_hand():
+    """What blocks of one launch tell each other is ordered by atomics, or holds without an order: a wait for the chip's counters is none
+    that the compiler knows of."""
+    for file in ("vocab_verify.hip", "kv_attn.hip", "kv_cache.hip"):
+        with open(os.path.join(CSRC, file)) as f:
+            assert not re.search(r"s_waitcnt|signal_fence", re.sub(r"//[^\n]*", "", f.read())), file
