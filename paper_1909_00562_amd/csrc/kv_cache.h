@@ -1,4 +1,4 @@
-// What the cache's files share: checks of a cache's description, and the attention's launch.
+// What the cache's files share: checks of a cache's description and pointers, and division by products.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -8,7 +8,6 @@
 namespace asx {
 
 constexpr int kKvTile = 16;   // tokens of a tile; pages are whole ones
-inline int kv_bytes(int cache_type) { return cache_type == KC_F32 ? 4 : cache_type == KC_BF16 ? 2 : 1; }
 inline bool kv_coded(int cache_type) { return cache_type == KC_INT8 || cache_type == KC_E4M3; }
 
 as_status kv_check_cache(const kc_cache* c);
