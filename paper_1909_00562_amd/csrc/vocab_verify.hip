@@ -164,7 +164,7 @@ template <typename TE, int PER> __global__ __launch_bounds__(kVThreads) void ver
 // The same of many bf16 logits.  Of those there are few different ones: 24 exponents of 128 and two signs are a table of 48 KB, which
 // takes the place of an exponential each by a read of LDS; it is made once by blocks that stay for all chunks.  Sums are relative to
 // 2^0 instead of the chunk's maximum.  A chunk with other logits (64 and more in magnitude, 2^-18 and less, infinities, NaN) goes the general
-// way.  us, 1152 rows of 128000 (295 MB): the general way 112, this 85, of which the vector units and LDS (a quarter of its time conflicts of
+// way.  us, 1152 rows of 128000 (295 MB): the general way 120, this 84, of which the vector units and LDS (a quarter of its time conflicts of
 // banks) are busy 55 each.
 constexpr int kTabThreads = 512, kTabPer = 16, kTabBlocks = 768;
 constexpr uint32_t kTabFirst = (127 - 18) << 7, kTabCount = 24 << 7;   // the lowest magnitude's bits, how many
