@@ -24,6 +24,7 @@ typedef uint32_t vu32x4_t __attribute__((ext_vector_type(4)));
 constexpr int kVThreads = 256, kVerifyMaxT = 64;
 // Logits of a thread: a block's chunk of a row is 256 times that.  Fewer where the blocks would not fill the chip: see verify_layout.
 constexpr int kManyPer = 32, kFewPer = 8, kMostChunks = 128;   // (two to a lane of the wave that scans their sums)
+constexpr int kMostTries = 100000;                                // of reading a sum
 
 struct VerifyPart {
   double sum;    // of 2^((l - m) c)
@@ -455,6 +456,7 @@ template <typename TE, int PER> __global__ __launch_bounds__(kVThreads, 8) void 
   // One block, the sequence's last or first, finds the chunk; sums are added in the chunks' order, whichever block this is.
   if (wave == 0) {
     double x[2], run[2], all = 0;
+    bool missing = false;
     auto scan = [&]() {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -473,14 +475,17 @@ template <typename TE, int PER> __global__ __launch_bounds__(kVThreads, 8) void 
       all = __shfl(run[1], 63, 64);
     };
     if (rest) {
-      // (every block has counted, and stores its sum ahead of that or soon after, waiting for nobody)
+      // Every block has counted, and stores its sum ahead of that or soon after, waiting for nobody.  Some 1e5 reads of 1 us each find one
+      // missing only where another call takes the workspace meanwhile, which no caller may do: no word then, but an end.
+      int tries = 0;
       do {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const int k = h * 64 + lane;
           x[h] = k < a.chunks ? __hip_atomic_load(&sums[k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
         }
-      } while (x[0] < 0 || x[1] < 0);
+      } while ((x[0] < 0 || x[1] < 0) && ++tries < kMostTries);
+      missing = __any(x[0] < 0 || x[1] < 0);
       scan();
     }
     const bool of_p = !(all > 0);           // nothing is left: p
@@ -509,12 +514,16 @@ template <typename TE, int PER> __global__ __launch_bounds__(kVThreads, 8) void 
       if (there && some == 0) some = h * 64 + 63 - __builtin_clzll(there);
     }
     if (lane == 0) {
-      s_chunk = chunk < 0 ? some : chunk;   // (rounding, or u >= 1: the last one with a weight)
+      s_chunk = missing ? -1 : chunk < 0 ? some : chunk;   // (rounding, or u >= 1: the last one with a weight)
       s_theta = left;
       s_of_p = of_p;
     }
   }
   __syncthreads();
+  if (s_chunk < 0) {
+    if (tid == 0) a.words[first + b + n] = -1;
+    return;
+  }
   const bool subtract = !s_of_p;
   const int v1 = s_chunk * CHUNK + tid * PER;   // consecutive logits per thread: running sums go by the words' order
   const double theta = s_theta;

@@ -36,3 +36,15 @@ def test_no_order_of_memory_rests_on_a_wait_by_hand():
     for file in ("vocab_verify.hip", "kv_attn.hip", "kv_cache.hip"):
         with open(os.path.join(CSRC, file)) as f:
             assert not re.search(r"s_waitcnt|signal_fence", re.sub(r"//[^\n]*", "", f.read())), file
+
+
+def test_every_wait_for_other_blocks_ends():
+    """A loop that reads what another block is to write counts its tries."""
+    for file in ("vocab_verify.hip", "kv_attn.hip", "kv_cache.hip"):
+        with open(os.path.join(CSRC, file)) as f:
+            text = re.sub(r"//[^\n]*", "", f.read())
+        for at in re.finditer(r"\bdo \{", text):
+            body, condition = re.match(r"(.*?)\} while \(([^;]*)\);", text[at.end():], re.S).groups()
+            if "__hip_atomic_load" in body:
+                assert "++tries <" in condition, (file, condition)
+        assert not re.search(r"while \([^;{]*__hip_atomic_load", text), file
